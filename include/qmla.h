@@ -18,6 +18,11 @@
  *   qmla_mla_decode_multi  several query tokens per sequence under the causal mask
  *   qmla_mla_decode_ex  every decode variant from one descriptor, with optional
  *                       per-call events around the main kernel
+ *   qmla_rope_append    the cache writer for rows as the projections leave them: the
+ *                       latent normalised and the RoPE key rotated on the way
+ *   qmla_rope_query     rotates the RoPE part of queries
+ *   qmla_cache_read     cached tokens back as bf16 rows
+ *   qmla_mla_prefill    attention of ragged prompts over expanded keys and values
  *
  * Conventions for every call
  * --------------------------
@@ -92,8 +97,13 @@ enum qmla_device_error {
   QMLA_DEVERR_BAD_BLOCK = 1u,     /* a block-table entry outside [0, num_blocks) was needed */
   QMLA_DEVERR_BAD_POSITION = 2u,  /* a position or sequence length < 0 or beyond max_blocks*64 */
   QMLA_DEVERR_BAD_SEQ = 4u,       /* an append sequence id outside [0, num_seqs) */
-  QMLA_DEVERR_TIMEOUT = 8u        /* an on-chip pipeline wait ran out; that kernel left early */
+  QMLA_DEVERR_TIMEOUT = 8u,       /* an on-chip pipeline wait ran out; that kernel left early */
+  QMLA_DEVERR_BAD_OFFSETS = 16u   /* a prompt's offsets decrease or leave the rows given; it was left out */
 };
+
+/* Cache kinds besides the content bit widths 4 and 2: the paper's page, the BF16 cache. */
+#define QMLA_CACHE_C4R4 5
+#define QMLA_CACHE_BF16 16
 
 /* Most query tokens per sequence qmla_mla_decode_multi accepts. */
 #define QMLA_MAX_Q_TOKENS 8
@@ -361,6 +371,174 @@ typedef struct qmla_decode_desc {
 } qmla_decode_desc;
 int qmla_mla_decode_ex(const qmla_decode_desc* desc, qmla_stream_t stream);
 
+/*
+ * The cache writer for rows as a layer's down-projection leaves them: the latent is
+ * normalised and the RoPE key rotated on the way into any of the four caches, in one
+ * pass (App. C.5's fused writer takes them normalised and rotated; the offline
+ * transformations are folded into the weights, so with a content rotation the norm's
+ * weight is the content scale S_C). Token i, with latent x, RoPE key k and position p:
+ *     x'_c = RN_bf16(RN_f32(w_c x_c / sqrt(mean_c(x_c^2) + eps)))          (norm != 0)
+ *     k'   = RN_bf16(RN_f32(k turned by the angles of position p))
+ * and (x', k') is then stored exactly as qmla_quant_append (_protected, _c4r4) or
+ * qmla_bf16_append store a row. The sums and products carry their rounding errors
+ * along, so that the stored bytes do not depend on the order of a sum. Squares are
+ * taken in fp32: |x_c| below 2^60.
+ *
+ *   pool, num_blocks, seq_ids, positions, n, block_table, num_seqs, max_blocks, dev_err
+ *                   as in qmla_quant_append; cache_kind 4, 2, QMLA_CACHE_C4R4 or
+ *                   QMLA_CACHE_BF16
+ *   latent, latent_stride
+ *                   [n] rows of 512 bf16, latent_stride elements apart (even, >= 512 when n > 1)
+ *   k_pe, k_pe_stride
+ *                   [n] rows of 64 bf16, k_pe_stride elements apart (even, >= 64 when n > 1).
+ *                   Both 4-byte aligned; 16-byte aligned rows are read in wider pieces.
+ *                   (So the two may be the columns of one [n, 576] projection output.)
+ *   norm, norm_weight, norm_eps
+ *                   norm 0: the latent is stored as it is. Otherwise w is norm_weight
+ *                   [512] bf16 (16-byte aligned) or, NULL, all ones, and eps >= 0
+ *   cos_sin, rope_len
+ *                   [rope_len][64] fp32, 16-byte aligned: the cosines of a position's 32
+ *                   angles, then the sines. A position at or beyond rope_len is a bad position
+ *   interleaved     0: channel i turns with channel i + 32 (a, b -> a c - b s, a s + b c);
+ *                   1: channel 2 i turns with channel 2 i + 1
+ *   seq_lens, prot  the sink4/local128 protection buffer and the lengths after this call,
+ *                   as in qmla_quant_append_protected, or NULL (not with QMLA_CACHE_BF16).
+ *                   The protection rows hold the normalised and rotated values
+ * A token with a bad sequence, position or block is not written (dev_err says so).
+ * The descriptor is read during the call only. n == 0 is a no-op.
+ */
+typedef struct qmla_append_desc {
+  void* pool;
+  int cache_kind;
+  int num_blocks;
+  const uint16_t* latent;
+  long long latent_stride;
+  const uint16_t* k_pe;
+  long long k_pe_stride;
+  int norm;
+  float norm_eps;
+  const uint16_t* norm_weight;
+  const float* cos_sin;
+  int rope_len;
+  int interleaved;
+  const int32_t* seq_ids;
+  const int32_t* positions;
+  int n;
+  int num_seqs;
+  const int32_t* block_table;
+  int max_blocks;
+  const int32_t* seq_lens;
+  void* prot;
+  uint32_t* dev_err;
+} qmla_append_desc;
+int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream);
+
+/*
+ * Turns the RoPE part of queries by the angles of their positions, with the
+ * convention, table and rounding of qmla_rope_append:
+ *   q_pe_dev        [n, heads, 64] bf16, rows q_token_stride and q_head_stride elements
+ *                   apart (multiples of 8, not negative), 16-byte aligned. (So it may be
+ *                   the last 64 columns of a [n, heads, 192] projection output.)
+ *   positions_dev   [n] int32
+ *   out_dev         [n, heads, 64] bf16 with strides of its own, 16-byte aligned. It may
+ *                   be q_pe_dev with the same strides (in place) or share no memory with it;
+ *                   its rows must not overlap one another
+ * The heads of a token whose position is negative or at or beyond rope_len are left
+ * unwritten (QMLA_DEVERR_BAD_POSITION). n == 0 is a no-op.
+ */
+int qmla_rope_query(const uint16_t* q_pe_dev, long long q_token_stride, long long q_head_stride,
+                    const int32_t* positions_dev, int n, int heads, const float* cos_sin_dev, int rope_len,
+                    int interleaved, uint16_t* out_dev, long long out_token_stride, long long out_head_stride,
+                    uint32_t* dev_err_dev, qmla_stream_t stream);
+
+/*
+ * Reads cached tokens back as bf16 rows (512 latent values, then the RoPE key's 64),
+ * for whatever needs the values themselves: the up-projection of a chunked prompt's
+ * context (qmla_mla_prefill), a cache handed to another replica.
+ *   rows[i] = RN_bf16(RN_f32(s (q - z))) of the token at positions[i] of sequence
+ *   seq_ids[i] (NULL: sequence i); the BF16 cache's rows and protected positions
+ *   (prot non-NULL; P_L from seq_lens, as in qmla_mla_decode_protected) unchanged.
+ *   rows, row_stride   [n] rows of 576 bf16, row_stride elements apart (a multiple of 8,
+ *                   >= 576 when n > 1), 16-byte aligned
+ * Other fields as in qmla_append_desc. A token with a bad sequence, position (with prot
+ * also one at or beyond its sequence's length) or block leaves its row unwritten
+ * (dev_err says so). n == 0 is a no-op.
+ */
+typedef struct qmla_read_desc {
+  const void* pool;
+  int cache_kind;
+  int num_blocks;
+  const int32_t* seq_ids;
+  const int32_t* positions;
+  int n;
+  int num_seqs;
+  const int32_t* block_table;
+  int max_blocks;
+  const int32_t* seq_lens;
+  const void* prot;
+  uint16_t* rows;
+  long long row_stride;
+  uint32_t* dev_err;
+} qmla_read_desc;
+int qmla_cache_read(const qmla_read_desc* desc, qmla_stream_t stream);
+
+/*
+ * The expanded form of the attention, for prompts: every head has its own 128
+ * content channels of key and value (the up-projected latent), and all heads share
+ * the token's RoPE key. Sequence b holds the queries cu_q[b] .. cu_q[b + 1] - 1 and
+ * the keys cu_kv[b] .. cu_kv[b + 1] - 1, Lq and Lk of them; query i of it sees key j when
+ *     causal != 0:  j <= i + Lk - Lq   (the queries are the last Lq of Lk tokens)
+ *     causal == 0:  always
+ *     S[i,h,j]   = softmax_scale * (q[i,h,:128] . k[j,h,:] + q[i,h,128:] . k_pe[j,:])
+ *     out[i,h,:] = RN_bf16(sum_j softmax_j(S[i,h,:]) v[j,h,:]);  lse[i,h] = log sum_j exp(S[i,h,j])
+ * over the keys it sees; a query that sees none gets out = 0 and lse = -inf. Scores,
+ * softmax statistics and sums are fp32; the weights reach the tensor cores as bf16.
+ *
+ *   q, q_token_stride, q_head_stride   [n_q, heads, 192] bf16, RoPE part rotated
+ *   k, v and their strides             [n_kv, heads, 128] bf16 each (so the two may be
+ *                   the halves of one [n_kv, heads, 256] projection output)
+ *   k_pe, k_pe_stride                  [n_kv, 64] bf16, rotated
+ *                   All four 16-byte aligned; strides in elements, positive multiples of 8
+ *                   below 2^38 (ignored where that axis has one element)
+ *   n_q, n_kv, heads, batch            rows given (at most 2^28), heads 1..1024, sequences
+ *                   1..65536. n_kv may be 0 (k, v and k_pe are not used then); n_q == 0 is a
+ *                   no-op
+ *   cu_q, cu_kv     [batch + 1] int32 offsets, not decreasing. A sequence whose offsets
+ *                   decrease, are negative or lie beyond n_q / n_kv is left out
+ *                   (QMLA_DEVERR_BAD_OFFSETS)
+ *   out             [n_q, heads, 128] bf16, contiguous, 16-byte aligned
+ *   lse             [n_q, heads] float32, contiguous, or NULL
+ *                   Rows that belong to no sequence are left as they were
+ *   workspace       >= qmla_prefill_workspace_bytes(batch, n_q) bytes, 256-byte aligned,
+ *                   scratch as for qmla_mla_decode. Calls that overlap need one each
+ * Keys and values of other sequences never reach a result, whatever they hold. Within
+ * a sequence a value that is not finite may reach queries before it (weight 0 x inf).
+ */
+typedef struct qmla_prefill_desc {
+  const uint16_t* q;
+  long long q_token_stride, q_head_stride;
+  const uint16_t* k;
+  long long k_token_stride, k_head_stride;
+  const uint16_t* v;
+  long long v_token_stride, v_head_stride;
+  const uint16_t* k_pe;
+  long long k_pe_stride;
+  int n_q, n_kv, heads, batch;
+  const int32_t* cu_q;
+  const int32_t* cu_kv;
+  int causal;
+  float softmax_scale;
+  uint16_t* out;
+  float* lse;
+  void* workspace;
+  size_t workspace_bytes;
+  uint32_t* dev_err;
+} qmla_prefill_desc;
+int qmla_mla_prefill(const qmla_prefill_desc* desc, qmla_stream_t stream);
+
+/* Workspace bytes qmla_mla_prefill needs; 0 for bad arguments. */
+size_t qmla_prefill_workspace_bytes(int batch, int n_q);
+
 /* Bytes of the fixed device scratch array qmla_mla_decode_static uses
  * (32 MiB). */
 size_t qmla_static_scratch_bytes(void);
@@ -416,8 +594,6 @@ int qmla_mla_decode_static(const void* pool_dev, int c_bits, int num_blocks, con
  * Table, lengths and errors as qmla_mla_decode; 0 <= b < batch, 0 <= j. One CTA
  * of 128 threads; not a fast path.
  */
-#define QMLA_CACHE_C4R4 5
-#define QMLA_CACHE_BF16 16
 int qmla_debug_tile(const void* pool_dev, int cache_kind, int num_blocks, const int32_t* block_table_dev,
                     int max_blocks, const int32_t* seq_lens_dev, int batch, int b, int j, const void* prot_dev,
                     uint16_t* tile_dev, uint32_t* dev_err_dev, qmla_stream_t stream);

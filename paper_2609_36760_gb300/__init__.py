@@ -23,6 +23,7 @@ DEVERR_BAD_BLOCK = 1
 DEVERR_BAD_POSITION = 2
 DEVERR_BAD_SEQ = 4
 DEVERR_TIMEOUT = 8
+DEVERR_BAD_OFFSETS = 16
 
 
 CACHE_KINDS = {4: 4, 2: 2, "c4r4": 5, "bf16": 16}  # qmla_decode_desc.cache_kind codes
@@ -37,6 +38,39 @@ class DecodeDesc(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("dev_err", ctypes.c_void_p),
                 ("ev_before_main", ctypes.c_void_p), ("ev_after_main", ctypes.c_void_p)]
+
+
+class AppendDesc(ctypes.Structure):
+    """qmla_append_desc (include/qmla.h), field for field."""
+    _fields_ = [("pool", ctypes.c_void_p), ("cache_kind", ctypes.c_int), ("num_blocks", ctypes.c_int),
+                ("latent", ctypes.c_void_p), ("latent_stride", ctypes.c_longlong), ("k_pe", ctypes.c_void_p),
+                ("k_pe_stride", ctypes.c_longlong), ("norm", ctypes.c_int), ("norm_eps", ctypes.c_float),
+                ("norm_weight", ctypes.c_void_p), ("cos_sin", ctypes.c_void_p), ("rope_len", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("seq_ids", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("n", ctypes.c_int), ("num_seqs", ctypes.c_int), ("block_table", ctypes.c_void_p),
+                ("max_blocks", ctypes.c_int), ("seq_lens", ctypes.c_void_p), ("prot", ctypes.c_void_p),
+                ("dev_err", ctypes.c_void_p)]
+
+
+class ReadDesc(ctypes.Structure):
+    """qmla_read_desc (include/qmla.h), field for field."""
+    _fields_ = [("pool", ctypes.c_void_p), ("cache_kind", ctypes.c_int), ("num_blocks", ctypes.c_int),
+                ("seq_ids", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("n", ctypes.c_int),
+                ("num_seqs", ctypes.c_int), ("block_table", ctypes.c_void_p), ("max_blocks", ctypes.c_int),
+                ("seq_lens", ctypes.c_void_p), ("prot", ctypes.c_void_p), ("rows", ctypes.c_void_p),
+                ("row_stride", ctypes.c_longlong), ("dev_err", ctypes.c_void_p)]
+
+
+class PrefillDesc(ctypes.Structure):
+    """qmla_prefill_desc (include/qmla.h), field for field."""
+    _fields_ = [("q", ctypes.c_void_p), ("q_token_stride", ctypes.c_longlong), ("q_head_stride", ctypes.c_longlong),
+                ("k", ctypes.c_void_p), ("k_token_stride", ctypes.c_longlong), ("k_head_stride", ctypes.c_longlong),
+                ("v", ctypes.c_void_p), ("v_token_stride", ctypes.c_longlong), ("v_head_stride", ctypes.c_longlong),
+                ("k_pe", ctypes.c_void_p), ("k_pe_stride", ctypes.c_longlong), ("n_q", ctypes.c_int),
+                ("n_kv", ctypes.c_int), ("heads", ctypes.c_int), ("batch", ctypes.c_int), ("cu_q", ctypes.c_void_p),
+                ("cu_kv", ctypes.c_void_p), ("causal", ctypes.c_int), ("softmax_scale", ctypes.c_float),
+                ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t), ("dev_err", ctypes.c_void_p)]
 
 
 class QmlaError(RuntimeError):
@@ -101,6 +135,13 @@ def lib():
     L.qmla_quant_append_c4r4.restype = i32
     L.qmla_mla_decode_c4r4.argtypes = [vp, i32, vp, vp, i32, i32, vp, i32, vp, vp, f32, vp, vp, vp, sz, vp, vp]
     L.qmla_mla_decode_c4r4.restype = i32
+    L.qmla_rope_append.argtypes, L.qmla_rope_append.restype = [ctypes.POINTER(AppendDesc), vp], i32
+    L.qmla_cache_read.argtypes, L.qmla_cache_read.restype = [ctypes.POINTER(ReadDesc), vp], i32
+    i64 = ctypes.c_longlong
+    L.qmla_rope_query.argtypes = [vp, i64, i64, vp, i32, i32, vp, i32, i32, vp, i64, i64, vp, vp]
+    L.qmla_rope_query.restype = i32
+    L.qmla_mla_prefill.argtypes, L.qmla_mla_prefill.restype = [ctypes.POINTER(PrefillDesc), vp], i32
+    L.qmla_prefill_workspace_bytes.argtypes, L.qmla_prefill_workspace_bytes.restype = [i32, i32], sz
     _lib = L
     return L
 
@@ -346,6 +387,116 @@ def read_dev_err(dev_err: torch.Tensor, stream=None) -> int:
     out = ctypes.c_uint32(0)
     _check("qmla_read_dev_err", lib().qmla_read_dev_err(_ptr(dev_err), ctypes.byref(out), _stream(stream)))
     return int(out.value)
+
+
+# The calls below take strided rows, so they look at shapes, types and devices too: a
+# tensor of another shape than the call's would be read out of range.
+def _want(name: str, t: torch.Tensor, dtype: torch.dtype, *shape) -> int:
+    """Address of a CUDA tensor of this type and shape (None: any size)."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.dim() != len(shape) or any(w is not None and w != s for w, s in zip(shape, t.shape)):
+        raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device, not on {t.device}")
+    return t.data_ptr()
+
+
+def _flat(name: str, t: torch.Tensor | None, dtype: torch.dtype, *shape):
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return _want(name, t, dtype, *shape)
+
+
+def _strided(name: str, t: torch.Tensor, *shape) -> int:
+    """The same for bf16 rows whose last axis lies side by side."""
+    if t.size(-1) != 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last axis")
+    return _want(name, t, torch.bfloat16, *shape)
+
+
+def _cache_fields(d, pool, cache_kind, seq_ids, positions, n, block_table, seq_lens, prot, dev_err) -> None:
+    if cache_kind not in CACHE_KINDS:
+        raise ValueError(f"unknown cache kind {cache_kind!r}")
+    width = {4: 20736, 2: 12544, "c4r4": 20480, "bf16": 73728}[cache_kind]
+    i32, seqs = torch.int32, block_table.size(0)
+    d.pool, d.cache_kind, d.num_blocks = _flat("pool", pool, torch.uint8, None, width), CACHE_KINDS[cache_kind], pool.size(0)
+    d.seq_ids, d.positions = _flat("seq_ids", seq_ids, i32, n), _flat("positions", positions, i32, n)
+    d.n, d.num_seqs = n, seqs
+    d.block_table, d.max_blocks = _flat("block_table", block_table, i32, None, None), block_table.size(1)
+    d.seq_lens = _flat("seq_lens", seq_lens, i32, seqs)
+    d.prot = _flat("prot", prot, torch.bfloat16, seqs, 132, 576)
+    d.dev_err = _flat("dev_err", dev_err, i32, None)
+
+
+def rope_append(pool: torch.Tensor, cache_kind, latent: torch.Tensor, k_pe: torch.Tensor,
+                seq_ids: torch.Tensor | None, positions: torch.Tensor, block_table: torch.Tensor,
+                cos_sin: torch.Tensor, dev_err: torch.Tensor, norm_weight: torch.Tensor | None = None,
+                eps: float = 1e-6, norm: bool | None = None, interleaved: bool = False,
+                seq_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None, stream=None) -> None:
+    """qmla_rope_append: cache_kind 4, 2, "c4r4" or "bf16"; latent bf16 [n,512] and k_pe bf16
+    [n,64] with any row stride (columns of one projection output); cos_sin f32
+    [rope_len,64]; norm_weight bf16 [512] (norm=True without it: weights of one);
+    with prot (and seq_lens = lengths after this call) also the sink/recent rows."""
+    n = latent.size(0)
+    d = AppendDesc()
+    d.latent, d.latent_stride = _strided("latent", latent, n, 512), latent.stride(0)
+    d.k_pe, d.k_pe_stride = _strided("k_pe", k_pe, n, 64), k_pe.stride(0)
+    d.norm, d.norm_eps = int(norm_weight is not None if norm is None else norm), eps
+    d.norm_weight = _flat("norm_weight", norm_weight, torch.bfloat16, 512)
+    d.cos_sin, d.rope_len = _flat("cos_sin", cos_sin, torch.float32, None, 64), cos_sin.size(0)
+    d.interleaved = int(interleaved)
+    _cache_fields(d, pool, cache_kind, seq_ids, positions, n, block_table, seq_lens, prot, dev_err)
+    _check("qmla_rope_append", lib().qmla_rope_append(ctypes.byref(d), _stream(stream)))
+
+
+def cache_read(pool: torch.Tensor, cache_kind, seq_ids: torch.Tensor | None, positions: torch.Tensor,
+               block_table: torch.Tensor, rows: torch.Tensor, dev_err: torch.Tensor,
+               seq_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None, stream=None) -> None:
+    """qmla_cache_read: the values of cached tokens into rows bf16 [n,576] (any row stride)."""
+    n = positions.size(0)
+    d = ReadDesc()
+    d.rows, d.row_stride = _strided("rows", rows, n, 576), rows.stride(0)
+    _cache_fields(d, pool, cache_kind, seq_ids, positions, n, block_table, seq_lens, prot, dev_err)
+    _check("qmla_cache_read", lib().qmla_cache_read(ctypes.byref(d), _stream(stream)))
+
+
+def rope_query(q_pe: torch.Tensor, positions: torch.Tensor, cos_sin: torch.Tensor, out: torch.Tensor,
+               dev_err: torch.Tensor, interleaved: bool = False, stream=None) -> None:
+    """qmla_rope_query: q_pe and out bf16 [n,heads,64] with any strides; out may be q_pe (in place)."""
+    n, heads = q_pe.size(0), q_pe.size(1)
+    st = lib().qmla_rope_query(_strided("q_pe", q_pe, n, heads, 64), q_pe.stride(0), q_pe.stride(1),
+                               _flat("positions", positions, torch.int32, n), n, heads,
+                               _flat("cos_sin", cos_sin, torch.float32, None, 64), cos_sin.size(0), int(interleaved),
+                               _strided("out", out, n, heads, 64), out.stride(0), out.stride(1),
+                               _flat("dev_err", dev_err, torch.int32, None), _stream(stream))
+    _check("qmla_rope_query", st)
+
+
+def prefill_workspace_bytes(batch: int, n_q: int) -> int:
+    return int(lib().qmla_prefill_workspace_bytes(batch, n_q))
+
+
+def mla_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pe: torch.Tensor, cu_q: torch.Tensor,
+                cu_kv: torch.Tensor, softmax_scale: float, out: torch.Tensor, lse: torch.Tensor | None,
+                workspace: torch.Tensor, dev_err: torch.Tensor, causal: bool = True, stream=None) -> None:
+    """qmla_mla_prefill: q bf16 [n_q,H,192], k and v bf16 [n_kv,H,128], k_pe bf16 [n_kv,64] with any
+    strides; cu_q, cu_kv int32 [batch+1]; out bf16 [n_q,H,128], lse f32 [n_q,H]."""
+    nq, H, nkv = q.size(0), q.size(1), k.size(0)
+    d = PrefillDesc()
+    d.q, d.q_token_stride, d.q_head_stride = _strided("q", q, nq, H, 192), q.stride(0), q.stride(1)
+    d.k, d.k_token_stride, d.k_head_stride = _strided("k", k, nkv, H, 128), k.stride(0), k.stride(1)
+    d.v, d.v_token_stride, d.v_head_stride = _strided("v", v, nkv, H, 128), v.stride(0), v.stride(1)
+    d.k_pe, d.k_pe_stride = _strided("k_pe", k_pe, nkv, 64), k_pe.stride(0)
+    d.n_q, d.n_kv, d.heads, d.batch = nq, nkv, H, cu_q.size(0) - 1
+    d.cu_q, d.cu_kv = _flat("cu_q", cu_q, torch.int32, None), _flat("cu_kv", cu_kv, torch.int32, cu_q.size(0))
+    d.causal, d.softmax_scale = int(causal), float(softmax_scale)
+    d.out, d.lse = _flat("out", out, torch.bfloat16, nq, H, 128), _flat("lse", lse, torch.float32, nq, H)
+    d.workspace, d.workspace_bytes = _flat("workspace", workspace, torch.uint8, None), workspace.nbytes
+    d.dev_err = _flat("dev_err", dev_err, torch.int32, None)
+    _check("qmla_mla_prefill", lib().qmla_mla_prefill(ctypes.byref(d), _stream(stream)))
 
 
 def workspace_for(batch: int, heads: int, device="cuda") -> torch.Tensor:

@@ -43,6 +43,8 @@ int current_device_info(DevInfo& out) {
   return out.supported ? QMLA_OK : QMLA_ERR_UNSUPPORTED;
 }
 
+bool known_cache(int kind) { return kind == 4 || kind == 2 || kind == QMLA_CACHE_C4R4 || kind == QMLA_CACHE_BF16; }
+
 int append_common_checks(const void* pool, int num_blocks, const uint16_t* latent, const uint16_t* k_pe,
                          const int32_t* positions, int n, const int32_t* table, int num_seqs,
                          int max_blocks) {
@@ -363,6 +365,106 @@ int qmla_mla_decode_ex(const qmla_decode_desc* d, qmla_stream_t stream) {
                        d->block_table, d->max_blocks, d->seq_lens, d->softmax_scale, d->out, d->lse, d->workspace,
                        d->workspace_bytes, d->dev_err, stream, d->prot, d->q_tokens, d->ev_before_main,
                        d->ev_after_main, d->max_len);
+}
+
+int qmla_rope_append(const qmla_append_desc* d, qmla_stream_t stream) {
+  if (d == nullptr || !known_cache(d->cache_kind)) return QMLA_ERR_INVALID_ARG;
+  int st = append_common_checks(d->pool, d->num_blocks, d->latent, d->k_pe, d->positions, d->n, d->block_table,
+                                d->num_seqs, d->max_blocks);
+  if (st != QMLA_OK) return st;
+  if (d->rope_len < 1 || (d->interleaved != 0 && d->interleaved != 1)) return QMLA_ERR_INVALID_ARG;
+  if (d->norm != 0 && (!(d->norm_eps >= 0.0f) || d->norm_eps > 1e30f || !aligned(d->norm_weight, 16)))
+    return QMLA_ERR_INVALID_ARG;
+  if (d->prot != nullptr && (d->cache_kind == QMLA_CACHE_BF16 || d->seq_lens == nullptr || !aligned(d->prot, 16) ||
+                             !aligned(d->seq_lens, 4)))
+    return QMLA_ERR_INVALID_ARG;
+  if (d->n == 0) return QMLA_OK;
+  if (d->cos_sin == nullptr || !aligned(d->cos_sin, 16) || !aligned(d->seq_ids, 4)) return QMLA_ERR_INVALID_ARG;
+  if (d->latent_stride % 2 != 0 || d->k_pe_stride % 2 != 0 || (d->n > 1 && (d->latent_stride < qmla::kDc || d->k_pe_stride < qmla::kDr)))
+    return QMLA_ERR_INVALID_ARG;
+  DevInfo di;
+  if ((st = current_device_info(di)) != QMLA_OK) return st;
+  cudaError_t e = qmla::launch_rope_append(*d, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
+}
+
+int qmla_rope_query(const uint16_t* q_pe_dev, long long q_token_stride, long long q_head_stride,
+                    const int32_t* positions_dev, int n, int heads, const float* cos_sin_dev, int rope_len,
+                    int interleaved, uint16_t* out_dev, long long out_token_stride, long long out_head_stride,
+                    uint32_t* dev_err_dev, qmla_stream_t stream) {
+  // (rows times 8 lanes fill the grid's 2^31 - 1 blocks of 128 rows at most)
+  if (n < 0 || heads < 1 || static_cast<long long>(n) * heads > (1ll << 37) || rope_len < 1 ||
+      (interleaved != 0 && interleaved != 1))
+    return QMLA_ERR_INVALID_ARG;
+  if (n == 0) return QMLA_OK;
+  if (q_pe_dev == nullptr || positions_dev == nullptr || cos_sin_dev == nullptr || out_dev == nullptr)
+    return QMLA_ERR_INVALID_ARG;
+  if (!aligned(q_pe_dev, 16) || !aligned(out_dev, 16) || !aligned(cos_sin_dev, 16) || !aligned(positions_dev, 4))
+    return QMLA_ERR_INVALID_ARG;
+  for (long long s : {q_token_stride, q_head_stride, out_token_stride, out_head_stride})
+    if (s < 0 || s % 8 != 0) return QMLA_ERR_INVALID_ARG;
+  // two rows of out at one place would race
+  if ((n > 1 && out_token_stride < qmla::kDr) || (heads > 1 && out_head_stride < qmla::kDr)) return QMLA_ERR_INVALID_ARG;
+  DevInfo di;
+  int st = current_device_info(di);
+  if (st != QMLA_OK) return st;
+  cudaError_t e = qmla::launch_rope_query(q_pe_dev, q_token_stride, q_head_stride, positions_dev, n, heads, cos_sin_dev,
+                                          rope_len, interleaved != 0, out_dev, out_token_stride, out_head_stride,
+                                          dev_err_dev, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
+}
+
+int qmla_cache_read(const qmla_read_desc* d, qmla_stream_t stream) {
+  if (d == nullptr || !known_cache(d->cache_kind)) return QMLA_ERR_INVALID_ARG;
+  if (d->n < 0 || d->num_blocks <= 0 || d->num_seqs <= 0 || d->max_blocks <= 0 ||
+      static_cast<long long>(d->max_blocks) * qmla::kBlockTokens > INT32_MAX)
+    return QMLA_ERR_INVALID_ARG;
+  if (d->prot != nullptr && (d->cache_kind == QMLA_CACHE_BF16 || d->seq_lens == nullptr || !aligned(d->prot, 16) ||
+                             !aligned(d->seq_lens, 4)))
+    return QMLA_ERR_INVALID_ARG;
+  if (d->n == 0) return QMLA_OK;
+  if (d->pool == nullptr || d->positions == nullptr || d->block_table == nullptr || d->rows == nullptr)
+    return QMLA_ERR_INVALID_ARG;
+  if (!aligned(d->pool, 32) || !aligned(d->rows, 16) || !aligned(d->seq_ids, 4) || !aligned(d->positions, 4) ||
+      !aligned(d->block_table, 4) || d->row_stride % 8 != 0 || (d->n > 1 && d->row_stride < qmla::kDqk))
+    return QMLA_ERR_INVALID_ARG;
+  DevInfo di;
+  int st = current_device_info(di);
+  if (st != QMLA_OK) return st;
+  cudaError_t e = qmla::launch_cache_read(*d, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
+}
+
+size_t qmla_prefill_workspace_bytes(int batch, int n_q) {
+  if (batch < 1 || batch > 65536 || n_q < 0 || n_q > (1 << 28)) return 0;
+  return qmla::prefill_workspace_bytes(batch, n_q);
+}
+
+int qmla_mla_prefill(const qmla_prefill_desc* d, qmla_stream_t stream) {
+  if (d == nullptr) return QMLA_ERR_INVALID_ARG;
+  if (d->n_q < 0 || d->n_kv < 0 || d->n_q > (1 << 28) || d->n_kv > (1 << 28) || d->heads < 1 || d->heads > 1024 ||
+      d->batch < 1 || d->batch > 65536 || (d->causal != 0 && d->causal != 1))
+    return QMLA_ERR_INVALID_ARG;
+  if (!(d->softmax_scale > 0.0f) || d->softmax_scale > 1e30f) return QMLA_ERR_INVALID_ARG;
+  if (d->n_q == 0) return QMLA_OK;
+  if (d->q == nullptr || d->cu_q == nullptr || d->cu_kv == nullptr || d->out == nullptr || d->workspace == nullptr ||
+      (d->n_kv > 0 && (d->k == nullptr || d->v == nullptr || d->k_pe == nullptr)))
+    return QMLA_ERR_INVALID_ARG;
+  if (!aligned(d->q, 16) || !aligned(d->out, 16) || !aligned(d->cu_q, 4) || !aligned(d->cu_kv, 4) ||
+      !aligned(d->lse, 4) || !aligned(d->workspace, 256) ||
+      (d->n_kv > 0 && (!aligned(d->k, 16) || !aligned(d->v, 16) || !aligned(d->k_pe, 16))))
+    return QMLA_ERR_INVALID_ARG;
+  auto bad = [](int n, long long s) { return n > 1 && (s < 8 || s % 8 != 0 || s >= (1ll << 38)); };
+  if (bad(d->n_q, d->q_token_stride) || bad(d->heads, d->q_head_stride) || bad(d->n_kv, d->k_token_stride) ||
+      bad(d->n_kv, d->v_token_stride) || bad(d->n_kv, d->k_pe_stride) ||
+      (d->n_kv > 0 && (bad(d->heads, d->k_head_stride) || bad(d->heads, d->v_head_stride))))
+    return QMLA_ERR_INVALID_ARG;
+  if (d->workspace_bytes < qmla::prefill_workspace_bytes(d->batch, d->n_q)) return QMLA_ERR_WORKSPACE_TOO_SMALL;
+  DevInfo di;
+  int st = current_device_info(di);
+  if (st != QMLA_OK) return st;
+  cudaError_t e = qmla::launch_prefill(*d, di.sms, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
 }
 
 int qmla_last_cuda_error(void) { return g_last_cuda_error; }

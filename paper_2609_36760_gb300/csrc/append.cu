@@ -1,7 +1,9 @@
 // Quantise-and-pack cache writer (App. C.4 quantiser; App. C.5 cache update:
 // content- and RoPE-cache quantisation, integer packing and slot-mapped page
 // insertion) for this library's block and for the paper's own page, and the
-// plain BF16 writer for the comparison cache.
+// plain BF16 writer for the comparison cache. The fused form takes the rows as the
+// projections leave them: it normalises the latent and rotates the RoPE key on
+// the way into any of the four caches.
 //
 // A block of nine warps writes a few tokens: warp g quantises group g (64
 // coordinates) of four or sixteen tokens, eight lanes per token with eight
@@ -14,6 +16,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "ptx.cuh"
+#include "rope.cuh"
 
 namespace qmla {
 namespace {
@@ -73,14 +76,14 @@ __device__ __forceinline__ void codes8(const uint32_t (&w)[4], float s, float y,
 // recording the error) when the token cannot be written.
 __device__ __forceinline__ int token_block(int num_blocks, const int32_t* seq_ids, const int32_t* positions, int i,
                                            const int32_t* table, int num_seqs, int max_blocks, uint32_t* dev_err,
-                                           int& seq, int& pos) {
+                                           int& seq, int& pos, int rope_len = INT32_MAX) {
   seq = seq_ids != nullptr ? seq_ids[i] : i;
   pos = positions[i];
   if (seq < 0 || seq >= num_seqs) {
     report(dev_err, QMLA_DEVERR_BAD_SEQ);
     return -1;
   }
-  if (pos < 0 || pos >= max_blocks * kBlockTokens) {
+  if (pos < 0 || pos >= max_blocks * kBlockTokens || pos >= rope_len) {
     report(dev_err, QMLA_DEVERR_BAD_POSITION);
     return -1;
   }
@@ -99,11 +102,86 @@ __device__ __forceinline__ int token_block(int num_blocks, const int32_t* seq_id
 
 constexpr int kAppendThreads = kGroups * 32;
 
+// What the fused writer does to a row on its way into the cache.
+struct RowTransform {
+  size_t latent_words, k_pe_words;  // row strides in 4-byte words
+  const uint4* weight;              // [512] bf16, or null: all ones
+  bool norm;
+  float eps;
+  const float* cos_sin;  // [rope_len][64]: cos[32] | sin[32]
+  int rope_len;
+  bool interleaved;
+};
+
+// Warp g's rows (four tokens per pass, eight lanes each) normalised (g < 8) or
+// rotated (g = 8) in registers. The row's sum of squares needs all eight content
+// warps: each leaves its 64 channels' share in shared memory and every warp adds
+// the eight shares in the same order, so the result does not depend on the launch.
+// Every thread of the block takes part.
+template <int NT>
+__device__ __forceinline__ void transform_rows(uint4 (&raw)[NT], const RowTransform& tr,
+                                               const int32_t* __restrict__ positions, int n, int tok0, int g,
+                                               int lane) {
+  __shared__ float2 share[8][4 * NT];
+  const int piece = lane & 7, sub = lane >> 3;
+  if (g == 8) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int tok = tok0 + 4 * i;
+      const int pos = tok < n ? positions[tok] : -1;
+      Angles a;
+      load_angles(a, pos >= 0 && pos < tr.rope_len ? tr.cos_sin + static_cast<size_t>(pos) * kDr : nullptr, piece,
+                  tr.interleaved);
+      uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+      rotate_row(w, a, piece, tr.interleaved);
+      raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  if (!tr.norm) return;
+  if (g < 8) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+      F2 s = square_sum8(w);
+#pragma unroll
+      for (int off = 1; off < 8; off <<= 1)
+        s = add_f2(s, {__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off)});
+      if (piece == 0) share[g][sub + 4 * i] = make_float2(s.hi, s.lo);
+    }
+  }
+  __syncthreads();
+  if (g == 8) return;
+  // this lane's share: token `own` of the lane's NT, handed round by shuffles
+  const int own = piece & (NT - 1);
+  F2 sum = {0.0f, 0.0f};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float2 v = share[k][sub + 4 * own];
+    sum = add_f2(sum, {v.x, v.y});
+  }
+  const F2 rs = row_rstd(sum, tr.eps);
+  const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+  const uint4 gv = tr.weight != nullptr ? tr.weight[g * 8 + piece] : ones;
+  const uint32_t gw[4] = {gv.x, gv.y, gv.z, gv.w};
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int from = (lane & 24) | i;
+    const F2 r = NT == 1 ? rs : F2{__shfl_sync(0xffffffffu, rs.hi, from), __shfl_sync(0xffffffffu, rs.lo, from)};
+    uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+    scale_row(w, gw, r);
+    raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+constexpr int kBf16Rows = 16;  // cache kind of the BF16 cache
+
 // Quantises and packs n tokens. CB: content bits (4, 2) or kC4R4 for the paper's
 // page (INT4 codes). NT: tokens per lane, 1 or 4 (a block writes 4 NT). VEC: latent
 // and k_pe are 16-byte aligned (one 16-byte load per lane, else four 4-byte ones).
 // prot / lens: the protection buffer [num_seqs][132][576] bf16 and the requests'
 // lengths after this write, or null for an unprotected cache.
+// FUSED: the rows are normalised and rotated first (RowTransform), which also gives
+// their strides; then CB may be kBf16Rows, which stores them as they are.
 //
 // What bounds it: for a prefill the issue slots, then the HBM traffic (1152 bytes
 // read and 324 written per token, INT4); for a decode step's few tokens the latency
@@ -117,14 +195,16 @@ constexpr int kAppendThreads = kGroups * 32;
 // fp32 quotient, divide value by value. 32,797 tokens of eight ragged prompts (INT4, calls
 // on buffers larger together than L2) take 16.5 us, 2.9 TB/s of 6.8; a warp per (token,
 // group) with two coordinates per lane and a division per code took 61.5.
-template <int CB, int NT, bool VEC>
+template <int CB, int NT, bool VEC, bool FUSED>
 __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     uint8_t* __restrict__ pool, int num_blocks, const uint32_t* __restrict__ latent,
     const uint32_t* __restrict__ k_pe, const int32_t* __restrict__ seq_ids,
     const int32_t* __restrict__ positions, int n, const int32_t* __restrict__ table, int num_seqs,
-    int max_blocks, uint32_t* dev_err, uint4* __restrict__ prot, const int32_t* __restrict__ lens) {
+    int max_blocks, uint32_t* dev_err, uint4* __restrict__ prot, const int32_t* __restrict__ lens,
+    const RowTransform tr) {
   static_assert(NT == 1 || NT == 4, "tokens per lane");
-  using L = BlockLayout<CB>;
+  static_assert(FUSED || CB != kBf16Rows, "bf16 rows have a writer of their own");
+  using L = BlockLayout<CB == kBf16Rows ? 4 : CB>;
   // The decode's prep kernel may start meanwhile: it does not read the cache, and it
   // neither writes anything nor ends before this kernel has ended. (A decode step with
   // prep after the writer / beside it, us: 8 sequences x 128 heads, 300..2,500 tokens,
@@ -144,8 +224,9 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     const int tok = tok0 + 4 * i;
     raw[i] = make_uint4(0, 0, 0, 0);
     if (tok < n) {
-      const uint32_t* src = g < 8 ? latent + static_cast<size_t>(tok) * (kDc / 2) + g * 32 + piece * 4
-                                  : k_pe + static_cast<size_t>(tok) * (kDr / 2) + piece * 4;
+      const size_t row = static_cast<size_t>(tok);
+      const uint32_t* src = g < 8 ? latent + row * (FUSED ? tr.latent_words : kDc / 2) + g * 32 + piece * 4
+                                  : k_pe + row * (FUSED ? tr.k_pe_words : kDr / 2) + piece * 4;
       if constexpr (VEC) {
         raw[i] = *reinterpret_cast<const uint4*>(src);
       } else {
@@ -162,13 +243,26 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     const int tok = tok0 + 4 * own;
     int seq = 0, pos = 0;
     const int blk = token_block(num_blocks, seq_ids, positions, tok, table, num_seqs, max_blocks,
-                                piece == own && g == 0 ? dev_err : nullptr, seq, pos);
+                                piece == own && g == 0 ? dev_err : nullptr, seq, pos, FUSED ? tr.rope_len : INT32_MAX);
     if (blk >= 0) {
       dst = blk * kBlockTokens + pos % kBlockTokens;
       if (prot != nullptr) {
         if (pos < kSinkTokens) sink = seq * kProtRows + pos;
         if (pos >= lens[seq] - kRecentTokens) ring = seq * kProtRows + kSinkTokens + pos % kRecentTokens;
       }
+    }
+  }
+  if constexpr (FUSED) {
+    transform_rows<NT>(raw, tr, positions, n, tok0, g, lane);
+    if constexpr (CB == kBf16Rows) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const int d = NT == 1 ? dst : __shfl_sync(0xffffffffu, dst, (lane & 24) | i);
+        if (d >= 0)
+          reinterpret_cast<uint4*>(pool + static_cast<size_t>(d / kBlockTokens) * kBf16BlockBytes +
+                                   d % kBlockTokens * (kDqk * 2))[g * 8 + piece] = raw[i];
+      }
+      return;
     }
   }
   // Extrema of each token's 64 values: (min, -max) as a bf16 pair, so that one packed
@@ -303,15 +397,26 @@ bool aligned16(const void* a, const void* b) {
   return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15) == 0;
 }
 
-template <int CB, int NT, bool VEC>
-void launch_quant(void* pool, int num_blocks, const uint16_t* latent, const uint16_t* k_pe, const int32_t* seq_ids,
-                  const int32_t* positions, int n, const int32_t* table, int num_seqs, int max_blocks,
-                  uint32_t* dev_err, cudaStream_t stream, void* prot, const int32_t* lens) {
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(n) + 4 * NT - 1) / (4 * NT));
-  quant_append_kernel<CB, NT, VEC><<<grid, kAppendThreads, 0, stream>>>(
-      static_cast<uint8_t*>(pool), num_blocks, reinterpret_cast<const uint32_t*>(latent),
-      reinterpret_cast<const uint32_t*>(k_pe), seq_ids, positions, n, table, num_seqs, max_blocks, dev_err,
-      static_cast<uint4*>(prot), lens);
+struct AppendArgs {
+  void* pool;
+  int num_blocks;
+  const uint16_t *latent, *k_pe;
+  const int32_t *seq_ids, *positions;
+  int n;
+  const int32_t* table;
+  int num_seqs, max_blocks;
+  uint32_t* dev_err;
+  void* prot;
+  const int32_t* lens;
+};
+
+template <int CB, int NT, bool VEC, bool FUSED>
+void launch_quant(const AppendArgs& a, const RowTransform& tr, cudaStream_t stream) {
+  const unsigned grid = static_cast<unsigned>((static_cast<long long>(a.n) + 4 * NT - 1) / (4 * NT));
+  quant_append_kernel<CB, NT, VEC, FUSED><<<grid, kAppendThreads, 0, stream>>>(
+      static_cast<uint8_t*>(a.pool), a.num_blocks, reinterpret_cast<const uint32_t*>(a.latent),
+      reinterpret_cast<const uint32_t*>(a.k_pe), a.seq_ids, a.positions, a.n, a.table, a.num_seqs, a.max_blocks,
+      a.dev_err, static_cast<uint4*>(a.prot), a.lens, tr);
 }
 
 // Tokens from which a lane takes four: below, one token per lane spreads the
@@ -321,13 +426,11 @@ void launch_quant(void* pool, int num_blocks, const uint16_t* latent, const uint
 // 32,768 15.1 against 19.5 / 19.8 against 20.7.
 constexpr int kFourPerLane = 8192;
 
-template <int CB>
-void launch_quant(void* pool, int num_blocks, const uint16_t* latent, const uint16_t* k_pe, const int32_t* seq_ids,
-                  const int32_t* positions, int n, const int32_t* table, int num_seqs, int max_blocks,
-                  uint32_t* dev_err, cudaStream_t stream, void* prot, const int32_t* lens) {
-  auto* f = !aligned16(latent, k_pe) ? launch_quant<CB, 1, false>
-                                     : (n >= kFourPerLane ? launch_quant<CB, 4, true> : launch_quant<CB, 1, true>);
-  f(pool, num_blocks, latent, k_pe, seq_ids, positions, n, table, num_seqs, max_blocks, dev_err, stream, prot, lens);
+template <int CB, bool FUSED>
+void launch_quant(const AppendArgs& a, const RowTransform& tr, bool vec, cudaStream_t stream) {
+  auto* f = !vec ? launch_quant<CB, 1, false, FUSED>
+                 : (a.n >= kFourPerLane ? launch_quant<CB, 4, true, FUSED> : launch_quant<CB, 1, true, FUSED>);
+  f(a, tr, stream);
 }
 
 }  // namespace
@@ -338,8 +441,30 @@ cudaError_t launch_quant_append(void* pool, int c_bits, int num_blocks, const ui
                                 int max_blocks, uint32_t* dev_err, cudaStream_t stream, void* prot,
                                 const int32_t* lens) {
   if (n == 0) return cudaSuccess;
-  auto* f = c_bits == kC4R4 ? launch_quant<kC4R4> : (c_bits == 4 ? launch_quant<4> : launch_quant<2>);
-  f(pool, num_blocks, latent, k_pe, seq_ids, positions, n, table, num_seqs, max_blocks, dev_err, stream, prot, lens);
+  const AppendArgs a = {pool,     num_blocks, latent, k_pe,       seq_ids, positions,
+                        n,        table,      num_seqs, max_blocks, dev_err, prot, lens};
+  auto* f = c_bits == kC4R4 ? launch_quant<kC4R4, false> : (c_bits == 4 ? launch_quant<4, false> : launch_quant<2, false>);
+  f(a, RowTransform{}, aligned16(latent, k_pe), stream);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_rope_append(const qmla_append_desc& d, cudaStream_t stream) {
+  const AppendArgs a = {d.pool,        d.num_blocks, d.latent,     d.k_pe,    d.seq_ids, d.positions, d.n,
+                        d.block_table, d.num_seqs,   d.max_blocks, d.dev_err, d.prot,    d.prot != nullptr ? d.seq_lens : nullptr};
+  RowTransform tr;
+  tr.latent_words = static_cast<size_t>(d.latent_stride) / 2;
+  tr.k_pe_words = static_cast<size_t>(d.k_pe_stride) / 2;
+  tr.norm = d.norm != 0;
+  tr.weight = reinterpret_cast<const uint4*>(d.norm_weight);
+  tr.eps = d.norm_eps;
+  tr.cos_sin = d.cos_sin;
+  tr.rope_len = d.rope_len;
+  tr.interleaved = d.interleaved != 0;
+  const bool vec = aligned16(d.latent, d.k_pe) && d.latent_stride % 8 == 0 && d.k_pe_stride % 8 == 0;
+  auto* f = d.cache_kind == kC4R4
+                ? launch_quant<kC4R4, true>
+                : (d.cache_kind == 4 ? launch_quant<4, true> : (d.cache_kind == 2 ? launch_quant<2, true> : launch_quant<kBf16Rows, true>));
+  f(a, tr, vec, stream);
   return cudaGetLastError();
 }
 

@@ -20,6 +20,15 @@ cudaError_t launch_bf16_append(void* pool, int num_blocks, const uint16_t* laten
                                const int32_t* positions, int n, const int32_t* table, int num_seqs,
                                int max_blocks, uint32_t* dev_err, cudaStream_t stream);
 
+// The fused writer (see qmla_rope_append; d.n > 0).
+cudaError_t launch_rope_append(const qmla_append_desc& d, cudaStream_t stream);
+cudaError_t launch_cache_read(const qmla_read_desc& d, cudaStream_t stream);
+cudaError_t launch_rope_query(const uint16_t* q, long long q_token, long long q_head, const int32_t* positions, int n,
+                              int heads, const float* cos_sin, int rope_len, bool interleaved, uint16_t* out,
+                              long long out_token, long long out_head, uint32_t* dev_err, cudaStream_t stream);
+size_t prefill_workspace_bytes(int batch, int n_q);
+cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t stream);
+
 // Heads handled by one CTA (the N of every MMA): 16, 32 or 64.
 int head_group_size(int heads);
 

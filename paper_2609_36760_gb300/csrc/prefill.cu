@@ -1,0 +1,674 @@
+// Attention of ragged prompts over expanded keys and values (include/qmla.h,
+// qmla_mla_prefill): 128 content channels and 64 shared RoPE channels in QK, 128
+// in PV.
+//
+// plan_kernel cuts every sequence into items of 256 query rows and orders them,
+// the longest first; prefill_kernel (persistent, one CTA per SM) works (item, head)
+// pairs off that list. In a CTA the two 128-row tiles of an item take turns on the
+// tensor core: while one tile's scores are turned into weights, the other's MMAs
+// run (PV of the old keys, QK of the next).
+//
+//   warps 0..3 / 4..7   softmax of tile 0 / 1, a query row per thread; epilogue
+//   warp 8              one thread that issues every MMA
+//   warp 9              TMA loads of queries, keys and values
+//
+// Shared memory: the queries (2 x 3 chunks of 128 rows x 64 channels, 96 KB) and a
+// ring of eight 16 KB slots for keys (three slots per 128 tokens: two content
+// chunks, one RoPE chunk) and values (two slots, 64 tokens x 128 channels each).
+// TMEM: S0, S1 (fp32, 128 columns each; the bf16 weights overwrite the first half
+// of their scores) and O0, O1.
+//
+// Mathematics: online softmax. Row r keeps a reference m and the sum l of
+// 2^(s - m) over the keys seen; O accumulates P V with P = RN_bf16(2^(s - m)). m is
+// raised, and O and l rescaled, only when a score exceeds it by more than 2^8: the
+// weights then stay below 2^8, which fp32 sums and bf16 weights hold as well as
+// weights below one.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace qmla {
+namespace {
+
+constexpr int kDn = 128;               // content channels of a query and key head
+constexpr int kDv = 128;               // channels of a value head
+constexpr int kTile = 128;             // query rows of a tile, keys of a step
+constexpr int kItemRows = 2 * kTile;   // query rows of an item
+constexpr int kSlotBytes = 16384;      // 128 rows of 64 channels, or 64 tokens of 128
+constexpr int kQChunks = 3, kKChunks = 3, kVSlots = 2;
+constexpr int kRing = 8;
+constexpr int kInFlight = 3;  // entries (a step's keys or values) that the ring holds at once
+constexpr int kSoftWarps = 8;
+constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kThreads = 12 * 32;  // (two warps leave at once: registers are split by groups of four)
+// 168 registers a thread at launch: 2 x 208 + 88 = 3 x 168.
+constexpr int kSoftRegs = 208, kOtherRegs = 88;
+constexpr int kRingOff = 2 * kQChunks * kSlotBytes;
+constexpr int kCtlOff = kRingOff + kRing * kSlotBytes;
+constexpr uint32_t kColO = 256;  // O0; O1 128 columns on
+constexpr uint64_t kLimitNs = 2000000000ull;  // of every wait
+constexpr float kRaise = 8.0f;                // log2 of the growth that raises a reference
+
+// Wait sites in the error word (bits 8 ..), after the decode's.
+enum : uint32_t { kSiteLoad = 10, kSiteMma, kSiteSoftmax, kSiteEnd };
+
+struct Ctl {
+  uint64_t q_full[2], q_free[2];
+  uint64_t full[4], freed[4];  // of entry e: [e & 3]
+  uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t tail, fin;
+  uint32_t tmem_base, abort;
+};
+constexpr int kSmem = kCtlOff + static_cast<int>(sizeof(Ctl)) + 1024;  // (the base is moved to a multiple of 1024)
+static_assert(kSmem <= 232448, "shared memory of a CTA");
+
+// Two tiles of one sequence: rows q_row .. of q, `rows` of them (at most 256); keys
+// kv_start .. + kv_len. Row r sees the first min(kv_len, vis0 + r * step) keys.
+struct Item {
+  int q_row, rows, kv_start, kv_len;
+  int vis0, step, n0, n1;  // n0, n1: key steps of the tiles
+};
+static_assert(sizeof(Item) == 32, "two 16-byte loads");
+
+struct Workspace {
+  size_t prefix_off, items_off, total;
+  int max_items;
+};
+Workspace workspace_layout(int batch, int n_q) {
+  Workspace w;
+  w.max_items = n_q / kItemRows + batch;  // disjoint sequences have no more
+  w.prefix_off = 256;                     // int: items written
+  w.items_off = (w.prefix_off + 4 * (static_cast<size_t>(batch) + 1) + 255) / 256 * 256;
+  w.total = w.items_off + sizeof(Item) * static_cast<size_t>(w.max_items);
+  return w;
+}
+
+// ------------------------------------------------------------------------- plan
+constexpr int kPlanThreads = 1024;
+
+__device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, off);
+    if (lane >= off) x += y;
+  }
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  int s = warp_sums[lane];
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, s, off);
+    if (lane >= off) s += y;
+  }
+  total = __shfl_sync(0xffffffffu, s, 31);
+  const int before = __shfl_sync(0xffffffffu, s, warp == 0 ? 0 : warp - 1);
+  __syncthreads();
+  return (warp == 0 ? 0 : before) + x - v;  // exclusive
+}
+
+// One block. Items of a sequence: ceil(Lq / 256); a counting sort by their key steps
+// puts the longest first (the order among equals is free: items do not meet).
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ cu_q,
+                                                            const int32_t* __restrict__ cu_kv, int batch, int n_q,
+                                                            int n_kv, int causal, int shift, int max_items,
+                                                            int* __restrict__ count, int* __restrict__ prefix,
+                                                            Item* __restrict__ items, uint32_t* dev_err) {
+  __shared__ int warp_sums[32];
+  __shared__ int bucket[kPlanThreads];
+  griddep_launch_dependents();  // prefill_kernel may start its set-up meanwhile
+  const int tid = threadIdx.x;
+  bucket[tid] = 0;
+  int base = 0;
+  for (int b0 = 0; b0 < batch; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    int tiles = 0;
+    if (b < batch) {
+      const int q0 = cu_q[b], q1 = cu_q[b + 1], k0 = cu_kv[b], k1 = cu_kv[b + 1];
+      if (q0 < 0 || q1 < q0 || q1 > n_q || k0 < 0 || k1 < k0 || k1 > n_kv) {
+        report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
+      } else {
+        tiles = (q1 - q0 + kItemRows - 1) / kItemRows;
+      }
+    }
+    int total;
+    const int at = block_scan(tiles, warp_sums, total);
+    if (b < batch) prefix[b] = base + at;
+    base += total;
+    if (base > max_items) base = max_items + 1;  // (decreasing offsets can make sequences overlap)
+  }
+  if (base > max_items) {
+    if (tid == 0) report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
+    base = max_items;
+  }
+  __syncthreads();
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int i = tid; i < base; i += kPlanThreads) {
+      int lo = 0, hi = batch - 1;  // the last sequence with prefix <= i: it has items
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (prefix[mid] <= i) {
+          lo = mid;
+        } else {
+          hi = mid - 1;
+        }
+      }
+      const int q0 = cu_q[lo], lq = cu_q[lo + 1] - q0, k0 = cu_kv[lo], lk = cu_kv[lo + 1] - k0;
+      const int r0 = (i - prefix[lo]) * kItemRows;
+      Item it;
+      it.q_row = q0 + r0;
+      it.rows = min(lq - r0, kItemRows);
+      it.kv_start = k0;
+      it.kv_len = lk;
+      it.vis0 = causal ? r0 + lk - lq + 1 : lk;
+      it.step = causal ? 1 : 0;
+      const int last0 = min(it.rows, kTile) - 1, last1 = it.rows - 1;
+      it.n0 = (max(min(lk, it.vis0 + it.step * last0), 0) + kTile - 1) / kTile;
+      it.n1 = it.rows > kTile ? (max(min(lk, it.vis0 + it.step * last1), 0) + kTile - 1) / kTile : 0;
+      const int key = kPlanThreads - 1 - min(max(it.n0, it.n1) >> shift, kPlanThreads - 1);
+      const int at = atomicAdd(&bucket[key], 1);
+      if (pass == 1 && at < max_items) items[at] = it;
+    }
+    __syncthreads();
+    if (pass == 0) {
+      int total;
+      const int before = block_scan(bucket[tid], warp_sums, total);
+      bucket[tid] = before;
+      __syncthreads();
+    }
+  }
+  if (tid == 0) *count = base;
+}
+
+// ------------------------------------------------------------------------ main
+struct PrefillParams {
+  const int* count;
+  const Item* items;
+  int heads, group;  // group: heads that are worked on together (their keys fit into L2)
+  float scale, scale_log2;
+  uint16_t* out;
+  float* lse;
+  uint32_t* dev_err;
+};
+
+// The (item, head) pairs of this CTA: the list goes by groups of heads, in a group
+// by item (longest first), then head; round k takes pair k * grid + cta, every other
+// round from the other end, which evens the sums out.
+struct Walk {
+  long long total;
+  int count, round;
+  __device__ __forceinline__ void init(const PrefillParams& p) {
+    count = *p.count;
+    total = static_cast<long long>(count) * p.heads;
+    round = 0;
+  }
+  __device__ __forceinline__ bool next(const PrefillParams& p, Item& it, int& head) {
+    const int g = static_cast<int>(gridDim.x), c = static_cast<int>(blockIdx.x);
+    const long long at = static_cast<long long>(round) * g + ((round & 1) ? g - 1 - c : c);
+    ++round;
+    if (at >= total) return false;
+    const long long per = static_cast<long long>(count) * p.group;
+    const int grp = static_cast<int>(at / per), rem = static_cast<int>(at - grp * per);
+    const int in = min(p.group, p.heads - grp * p.group);
+    const int i = rem / in;
+    head = grp * p.group + rem - i * in;
+    const int4* src = reinterpret_cast<const int4*>(p.items + i);
+    const int4 a = src[0], b = src[1];
+    it = Item{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    return true;
+  }
+};
+
+__device__ __forceinline__ void give_up(Ctl& c, uint32_t* dev_err, uint32_t site) {
+  report(dev_err, QMLA_DEVERR_TIMEOUT | (0x100u << site));
+  *reinterpret_cast<volatile uint32_t*>(&c.abort) = 1u;
+}
+// One thread's bounded wait.
+__device__ __forceinline__ bool wait1(uint64_t* bar, uint32_t parity, Ctl& c, uint32_t site, uint32_t* dev_err) {
+  const int r = mbar_wait(bar, parity & 1u, kLimitNs, &c.abort);
+  if (r == 0) give_up(c, dev_err, site);
+  return r == 1;
+}
+// A whole warp's (every lane waits on the barrier itself).
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl& c, uint32_t site, uint32_t* dev_err) {
+  return __all_sync(0xffffffffu, wait1(bar, parity, c, site, dev_err));
+}
+
+// First slot of entry e: keys (even e) take three, values two.
+__device__ __forceinline__ uint32_t entry_slot(uint32_t e) { return 5u * (e >> 1) + 3u * (e & 1u); }
+
+__device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
+                          const CUtensorMap& tpe, uint8_t* sm, Ctl& ctl, int lane) {
+  uint8_t* ring = sm + kRingOff;
+  uint32_t e = 0, nq[2] = {0, 0}, tails = 0;
+  bool ok = true;
+  Walk walk;
+  walk.init(p);
+  Item it;
+  int head;
+  auto load_q = [&](int i) {
+    if (nq[i] > 0 && !(ok = wait_warp(&ctl.q_free[i], nq[i] - 1, ctl, kSiteLoad, p.dev_err))) return;
+    if (lane == 0) {
+      mbar_arrive_expect_tx(&ctl.q_full[i], kQChunks * kSlotBytes);
+      for (int c = 0; c < kQChunks; ++c)
+        tma_load_3d(sm + (i * kQChunks + c) * kSlotBytes, &tq, c * 64, head, it.q_row + i * kTile, &ctl.q_full[i]);
+    }
+    ++nq[i];
+  };
+  while (ok && walk.next(p, it, head)) {
+    const int n = max(it.n0, it.n1);
+    if (it.n0 > 0) load_q(0);
+    for (int j = 0; ok && j < n; ++j) {
+      const int row = it.kv_start + j * kTile;
+      for (int v = 0; ok && v < 2; ++v, ++e) {
+        if (e >= kInFlight &&
+            !(ok = wait_warp(&ctl.freed[(e - kInFlight) & 3u], (e - kInFlight) >> 2, ctl, kSiteLoad, p.dev_err)))
+          break;
+        uint64_t* bar = &ctl.full[e & 3u];
+        const uint32_t slot = entry_slot(e);
+        uint8_t* s0 = ring + (slot & 7u) * kSlotBytes;
+        uint8_t* s1 = ring + ((slot + 1) & 7u) * kSlotBytes;
+        if (v == 0) {
+          if (lane == 0) {
+            mbar_arrive_expect_tx(bar, kKChunks * kSlotBytes);
+            tma_load_3d(s0, &tk, 0, head, row, bar);
+            tma_load_3d(s1, &tk, 64, head, row, bar);
+            tma_load_2d(ring + ((slot + 2) & 7u) * kSlotBytes, &tpe, 0, row, bar);
+          }
+          if (j == 0 && it.n1 > 0) load_q(1);
+          continue;
+        }
+        // Rows behind the sequence's last token belong to others: their weights are 0,
+        // but 0 x inf is not, so they are cleared before the tensor core sees them.
+        const int left = it.kv_len - j * kTile;
+        uint64_t* on = left < kTile ? &ctl.tail : bar;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(on, kVSlots * kSlotBytes);
+          for (int c = 0; c < 2; ++c) {
+            tma_load_3d(s0 + c * 8192, &tv, c * 64, head, row, on);
+            tma_load_3d(s1 + c * 8192, &tv, c * 64, head, row + 64, on);
+          }
+        }
+        if (left < kTile) {
+          if (!(ok = wait_warp(&ctl.tail, tails, ctl, kSiteLoad, p.dev_err))) {
+            if (lane == 0) mbar_wait(&ctl.tail, tails & 1u, kLimitNs, nullptr);  // (its copy may be on its way)
+            break;
+          }
+          ++tails;
+          for (int x = lane; x < (kTile - left) * 16; x += 32) {  // 16-byte pieces: 8 per row and half
+            const int t = left + (x >> 4), c = (x >> 3) & 1;
+            uint8_t* dst = (t < 64 ? s0 : s1) + c * 8192 + (t & 63) * 128 + (x & 7) * 16;
+            *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          mbar_arrive_if(lane == 0 ? 1u : 0u, bar);
+        }
+      }
+    }
+  }
+  if (lane != 0) return;
+  // No copy may be on its way when the CTA's shared memory is released; these waits
+  // ignore the abort flag.
+  for (int i = 0; i < 2; ++i)
+    if (nq[i] > 0 && mbar_wait(&ctl.q_full[i], (nq[i] - 1) & 1u, kLimitNs, nullptr) != 1) give_up(ctl, p.dev_err, kSiteEnd);
+  for (uint32_t k = 1; k <= kInFlight && k <= e; ++k)
+    if (mbar_wait(&ctl.full[(e - k) & 3u], ((e - k) >> 2) & 1u, kLimitNs, nullptr) != 1) give_up(ctl, p.dev_err, kSiteEnd);
+}
+
+// One thread.
+__device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32_t tmem) {
+  constexpr uint32_t kIdQK = idesc_bf16_f32(kTile, kTile, false, false);
+  constexpr uint32_t kIdPV = idesc_bf16_f32(kTile, kDv, false, true);
+  const uint64_t q0 = smem_desc(smem, 16, 1024, SWZ_128B);
+  const uint64_t r_k = smem_desc(smem + kRingOff, 16, 1024, SWZ_128B);
+  const uint64_t r_v = smem_desc(smem + kRingOff, 8192, 1024, SWZ_128B);
+  uint32_t e0 = 0, nq[2] = {0, 0}, np[2] = {0, 0};
+  bool ok = true;
+  auto qk = [&](int i, uint32_t e) {
+    const uint32_t slot = entry_slot(e);
+#pragma unroll
+    for (int c = 0; c < kKChunks; ++c) {
+      const uint64_t a = q0 + ((i * kQChunks + c) * kSlotBytes >> 4);
+      const uint64_t b = r_k + (((slot + c) & 7u) * kSlotBytes >> 4);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        umma_f16_ss(tmem + i * 128, a + (kk * 32 >> 4), b + (kk * 32 >> 4), kIdQK, (c | kk) != 0 ? 1u : 0u);
+    }
+    umma_commit(&ctl.s_full[i]);
+  };
+  auto pv = [&](int i, uint32_t e, bool first) {
+    const uint32_t slot = entry_slot(e);
+#pragma unroll
+    for (int h = 0; h < kVSlots; ++h) {
+      const uint64_t b = r_v + (((slot + h) & 7u) * kSlotBytes >> 4);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        umma_f16_ts(tmem + kColO + i * 128, tmem + i * 128 + (h * 4 + kk) * 8, b + (kk * 2048 >> 4), kIdPV,
+                    first && (h | kk) == 0 ? 0u : 1u);
+    }
+  };
+  auto full = [&](uint32_t e) { return wait1(&ctl.full[e & 3u], e >> 2, ctl, kSiteMma, p.dev_err); };
+  Walk walk;
+  walk.init(p);
+  Item it;
+  int head;
+  while (ok && walk.next(p, it, head)) {
+    const int n[2] = {it.n0, it.n1}, nmax = max(it.n0, it.n1);
+    if (nmax == 0) continue;
+    for (int j = -1; ok && j < nmax; ++j) {
+      // step j: PV of keys j and QK of keys j + 1, tile by tile
+      const uint32_t ek = e0 + 2 * (j + 1), ev = e0 + 2 * j + 1;
+      bool k_here = false, v_here = false;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (j >= 0 && j < n[i]) {
+          if (!v_here && !(ok = full(ev))) break;
+          v_here = true;
+          if (!(ok = wait1(&ctl.p_full[i], np[i], ctl, kSiteMma, p.dev_err))) break;
+          ++np[i];
+          tc_fence_after();
+          pv(i, ev, j == 0);
+          if (j + 1 == n[i]) umma_commit(&ctl.o_full[i]);
+        }
+        if (i == 1 && v_here) umma_commit(&ctl.freed[ev & 3u]);
+        if (j + 1 < n[i]) {
+          if (j < 0) {
+            if (!(ok = wait1(&ctl.q_full[i], nq[i], ctl, kSiteMma, p.dev_err))) break;
+            ++nq[i];
+          }
+          if (!k_here && !(ok = full(ek))) break;
+          k_here = true;
+          tc_fence_after();
+          qk(i, ek);
+          if (j + 2 == n[i]) umma_commit(&ctl.q_free[i]);
+        }
+        if (i == 1 && k_here) umma_commit(&ctl.freed[ek & 3u]);
+      }
+    }
+    e0 += 2 * nmax;
+  }
+  // Every MMA must have landed before TMEM and shared memory are released.
+  umma_commit(&ctl.fin);
+  if (mbar_wait(&ctl.fin, 0, kLimitNs, nullptr) != 1) give_up(ctl, p.dev_err, kSiteEnd);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Softmax and epilogue of tile i, a query row per thread.
+__device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int i, int warp, int lane) {
+  const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+  const uint32_t t_s = tmem + lanes + i * 128, t_o = tmem + lanes + kColO + i * 128;
+  const int row = i * kTile + (warp & 3) * 32 + lane;  // of the item
+  uint32_t ns = 0, no = 0;
+  Walk walk;
+  walk.init(p);
+  Item it;
+  int head;
+  while (walk.next(p, it, head)) {
+    const int n = i == 0 ? it.n0 : it.n1;
+    float m = -INFINITY, l = 0.0f;  // m in units of log2
+    const int vis = min(it.kv_len, it.vis0 + it.step * row);
+    const int vis_warp = min(it.kv_len, it.vis0 + it.step * (row - lane));  // of the warp's first row
+    for (int j = 0; j < n; ++j) {
+      if (!wait_warp(&ctl.s_full[i], ns, ctl, kSiteSoftmax, p.dev_err)) return;
+      ++ns;
+      tc_fence_after();
+      float s[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32 * c, reinterpret_cast<uint32_t*>(s + 32 * c));
+      tmem_ld_wait();
+      if (vis_warp < (j + 1) * kTile) {
+        const int lim = vis - j * kTile;
+#pragma unroll
+        for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : -INFINITY;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 128; ++c) top = fmaxf(top, s[c]);
+      top *= p.scale_log2;
+      const bool raise = top > m + kRaise;  // (m = -inf: the first visible key)
+      float factor = 1.0f;
+      if (raise) {
+        factor = ex2(m - top);  // 0 where nothing has been seen yet
+        m = top;
+        l *= factor;
+      }
+      if (j > 0 && __any_sync(0xffffffffu, raise)) {
+        // (the scores' arrival says that PV of the keys before has completed too)
+#pragma unroll 1
+        for (int c = 0; c < 8; ++c) {
+          uint32_t o[16];
+          tmem_ld(t_o + 16 * c, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * factor);
+          tmem_st(t_o + 16 * c, o);
+        }
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+      const uint64_t sl = f32x2(p.scale_log2, p.scale_log2), mm = f32x2(-ref, -ref);
+      uint64_t sum = f32x2(0.0f, 0.0f);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          const uint64_t x = fma2(f32x2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), sl, mm);
+          const float a = ex2(lo2(x)), b = ex2(hi2(x));
+          sum = add2(sum, f32x2(a, b));
+          w[c] = pack_bf16(a, b);
+        }
+        tmem_st32(t_s + 32 * h, w);
+      }
+      l += lo2(sum) + hi2(sum);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.p_full[i]);
+    }
+    if (n > 0) {
+      if (!wait_warp(&ctl.o_full[i], no, ctl, kSiteSoftmax, p.dev_err)) return;
+      ++no;
+      tc_fence_after();
+    }
+    const bool mine = row < it.rows;
+    const bool none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
+    const float inv = 1.0f / l;
+    const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + head;
+    if (mine && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
+    uint4* dst = reinterpret_cast<uint4*>(p.out + at * kDv);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint32_t o[32];
+      if (n > 0) {
+        tmem_ld32(t_o + 32 * c, o);
+        tmem_ld_wait();
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        uint32_t w[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          w[y] = none ? 0u
+                      : pack_bf16(__uint_as_float(o[8 * x + 2 * y]) * inv, __uint_as_float(o[8 * x + 2 * y + 1]) * inv);
+        if (mine) dst[4 * c + x] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    tc_fence_before();
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+    prefill_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
+                   const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap tpe,
+                   const PrefillParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Ctl& ctl = *reinterpret_cast<Ctl*>(sm + kCtlOff);
+  const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl.q_full[i], 1);
+      mbar_init(&ctl.q_free[i], 1);
+      mbar_init(&ctl.s_full[i], 1);
+      mbar_init(&ctl.p_full[i], 4);
+      mbar_init(&ctl.o_full[i], 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&ctl.full[i], 1);
+      mbar_init(&ctl.freed[i], 1);
+    }
+    mbar_init(&ctl.tail, 1);
+    mbar_init(&ctl.fin, 1);
+    ctl.abort = 0u;
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(&ctl.tmem_base, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, ctl.tmem_base, 0);
+  griddep_wait();  // the plan, and with it everything before it in the stream
+  if (warp < kSoftWarps) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    softmax_role(p, ctl, tmem, warp >> 2, warp, lane);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kLoadWarp) {
+      load_role(p, tq, tk, tv, tpe, sm, ctl, lane);
+    } else if (warp != kMmaWarp) {
+      asm volatile("exit;");
+    } else if (elect_one()) {
+      mma_role(p, smem_u32(sm), ctl, tmem);
+    } else {
+      asm volatile("exit;");
+    }
+  }
+  tc_fence_before();
+  __syncthreads();  // (exited lanes do not take part)
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ------------------------------------------------------------------------ host
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+cudaError_t encode_fn(EncodeFn& fn) {
+  static EncodeFn found = nullptr;
+  if (found == nullptr) {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r);
+    if (e != cudaSuccess) return e;
+    if (r != cudaDriverEntryPointSuccess || f == nullptr) return cudaErrorNotSupported;
+    found = reinterpret_cast<EncodeFn>(f);
+  }
+  fn = found;
+  return cudaSuccess;
+}
+
+// Boxes of 64 channels x `rows` tokens of one head, 128-byte swizzled. heads = 0: a
+// tensor without a head axis.
+cudaError_t make_map(CUtensorMap& m, const void* base, int channels, int heads, int tokens, long long token_stride,
+                     long long head_stride, int rows) {
+  EncodeFn fn;
+  const cudaError_t e = encode_fn(fn);
+  if (e != cudaSuccess) return e;
+  const cuuint32_t rank = heads > 0 ? 3 : 2;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(channels), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(head_stride) * 2, static_cast<cuuint64_t>(token_stride) * 2};
+  cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(rows)}, steps[3] = {1, 1, 1};
+  if (rank == 2) {
+    dims[1] = dims[2];
+    strides[0] = strides[1];
+    box[1] = box[2];
+  }
+  const CUresult r = fn(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, steps,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t prefill_workspace_bytes(int batch, int n_q) { return workspace_layout(batch, n_q).total; }
+
+cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t stream) {
+  const Workspace w = workspace_layout(d.batch, d.n_q);
+  uint8_t* ws = static_cast<uint8_t*>(d.workspace);
+  PrefillParams p;
+  p.count = reinterpret_cast<const int*>(ws);
+  p.items = reinterpret_cast<const Item*>(ws + w.items_off);
+  p.heads = d.heads;
+  // Keys and values of a group of heads: at most 48 MB, so that the items that run
+  // at the same time find them in the 126 MB L2.
+  p.group = static_cast<int>(
+      std::min<long long>(d.heads, std::max<long long>(1, (48ll << 20) / (std::max(d.n_kv, 1) * 512ll))));
+  p.scale = d.softmax_scale;
+  p.scale_log2 = d.softmax_scale * 1.4426950408889634f;
+  p.out = d.out;
+  p.lse = d.lse;
+  p.dev_err = d.dev_err;
+  CUtensorMap tq, tk, tv, tpe;
+  // A stride of an axis of one element is never used; a valid one stands in its place.
+  // Without keys no copy of one is issued.
+  const bool keys = d.n_kv > 0;
+  auto stride = [](int n, long long s, long long least) { return n > 1 ? s : least; };
+  cudaError_t e = make_map(tq, d.q, kDn + kDr, d.heads, d.n_q, stride(d.n_q, d.q_token_stride, kDn + kDr),
+                           stride(d.heads, d.q_head_stride, kDn + kDr), kTile);
+  const void* any = d.q;
+  if (e == cudaSuccess)
+    e = make_map(tk, keys ? d.k : any, kDn, d.heads, std::max(d.n_kv, 1), stride(d.n_kv, d.k_token_stride, kDn),
+                 stride(d.heads, d.k_head_stride, kDn), kTile);
+  if (e == cudaSuccess)
+    e = make_map(tv, keys ? d.v : any, kDv, d.heads, std::max(d.n_kv, 1), stride(d.n_kv, d.v_token_stride, kDv),
+                 stride(d.heads, d.v_head_stride, kDv), 64);
+  if (e == cudaSuccess)
+    e = make_map(tpe, keys ? d.k_pe : any, kDr, 0, std::max(d.n_kv, 1), stride(d.n_kv, d.k_pe_stride, kDr), 0, kTile);
+  if (e != cudaSuccess) return e;
+  static int configured_device = -1;
+  int dev = 0;
+  if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+  if (configured_device != dev) {
+    if ((e = cudaFuncSetAttribute(prefill_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem)) != cudaSuccess)
+      return e;
+    configured_device = dev;
+  }
+  int shift = 0;
+  while (((d.n_kv / kTile + 1) >> shift) >= kPlanThreads) ++shift;
+  plan_kernel<<<1, kPlanThreads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.causal != 0, shift, w.max_items,
+                                              reinterpret_cast<int*>(ws), reinterpret_cast<int*>(ws + w.prefix_off),
+                                              reinterpret_cast<Item*>(ws + w.items_off), d.dev_err);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, static_cast<long long>(w.max_items) * d.heads)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, prefill_kernel, tq, tk, tv, tpe, p);
+}
+
+}  // namespace qmla

@@ -1,0 +1,122 @@
+// Position rotation and latent normalisation of bf16 rows, as the fused cache
+// writer and the query rotation apply them.
+//
+// Both results are RN_bf16(RN_f32(exact)): the arithmetic carries the rounding
+// errors of its fp32 operations along (error-free transformations: T. J. Dekker,
+// Numer. Math. 18, 1971; D. E. Knuth, TAOCP 2, 4.2.2), which leaves about 2^-46
+// relative. A plain fp32 evaluation is off by up to some 2^-22, which moves one
+// bf16 value in about 2^13 and with it, now and then, the 2- or 4-bit code or the
+// scale of a whole group; this way the cache holds the same bytes whatever order
+// the sums are taken in.
+#pragma once
+#include <cstdint>
+
+#include "ptx.cuh"
+
+namespace qmla {
+
+// A value hi + lo with hi = RN_f32(value).
+struct F2 {
+  float hi, lo;
+};
+__device__ __forceinline__ F2 two_sum(float a, float b) {
+  const float s = __fadd_rn(a, b);
+  const float t = __fsub_rn(s, a);
+  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ F2 two_prod(float a, float b) {
+  const float p = __fmul_rn(a, b);
+  return {p, __fmaf_rn(a, b, -p)};
+}
+__device__ __forceinline__ F2 add_f2(F2 a, F2 b) {
+  const F2 s = two_sum(a.hi, b.hi);
+  const float lo = __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo));
+  const float hi = __fadd_rn(s.hi, lo);
+  return {hi, __fsub_rn(lo, __fsub_rn(hi, s.hi))};
+}
+
+// RN_f32(a c + b s).
+__device__ __forceinline__ float rotate1(float a, float c, float b, float s) {
+  const F2 p = two_prod(a, c), q = two_prod(b, s);
+  const F2 d = two_sum(p.hi, q.hi);
+  return __fadd_rn(d.hi, __fadd_rn(d.lo, __fadd_rn(p.lo, q.lo)));
+}
+
+__device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Eight lanes hold one row of 64 channels, lane `piece` the channels 8 piece ..
+// 8 piece + 7 in w. t is the row's entry of the angle table (cos[32] | sin[32]).
+// All 32 lanes of the warp take part (t may be null in lanes without a row).
+//   half-split (interleaved = false): channel i < 32 turns with channel i + 32,
+//     which is four lanes away: x c - x' s below, x c + x' s above;
+//   interleaved: channels 2 i and 2 i + 1 turn together.
+struct Angles {
+  float c[8], s[8];  // half-split: eight of each; interleaved: the first four
+};
+__device__ __forceinline__ void load_angles(Angles& a, const float* t, int piece, bool interleaved) {
+  const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const float4* q = reinterpret_cast<const float4*>(t) + (interleaved ? piece : 2 * (piece & 3));
+  const bool on = t != nullptr;
+  const float4 c0 = on ? q[0] : z, s0 = on ? q[8] : z;
+  const float4 c1 = on && !interleaved ? q[1] : z, s1 = on && !interleaved ? q[9] : z;
+  a.c[0] = c0.x, a.c[1] = c0.y, a.c[2] = c0.z, a.c[3] = c0.w, a.c[4] = c1.x, a.c[5] = c1.y, a.c[6] = c1.z, a.c[7] = c1.w;
+  a.s[0] = s0.x, a.s[1] = s0.y, a.s[2] = s0.z, a.s[3] = s0.w, a.s[4] = s1.x, a.s[5] = s1.y, a.s[6] = s1.z, a.s[7] = s1.w;
+}
+__device__ __forceinline__ void rotate_row(uint32_t (&w)[4], const Angles& a, int piece, bool interleaved) {
+  if (interleaved) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = bf16_low(w[e]), y = bf16_high(w[e]);
+      w[e] = pack_bf16(rotate1(x, a.c[e], y, -a.s[e]), rotate1(x, a.s[e], y, a.c[e]));
+    }
+  } else {
+    const float sign = piece < 4 ? -1.0f : 1.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t o = __shfl_xor_sync(0xffffffffu, w[e], 4);
+      w[e] = pack_bf16(rotate1(bf16_low(w[e]), a.c[2 * e], bf16_low(o), sign * a.s[2 * e]),
+                       rotate1(bf16_high(w[e]), a.c[2 * e + 1], bf16_high(o), sign * a.s[2 * e + 1]));
+    }
+  }
+}
+
+// Sum of the squares of eight bf16 values (each exact in fp32), even and odd
+// channels side by side.
+__device__ __forceinline__ F2 square_sum8(const uint32_t (&w)[4]) {
+  F2 even = {0.0f, 0.0f}, odd = {0.0f, 0.0f};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = bf16_low(w[e]), y = bf16_high(w[e]);
+    const F2 a = two_sum(even.hi, __fmul_rn(x, x)), b = two_sum(odd.hi, __fmul_rn(y, y));
+    even = {a.hi, __fadd_rn(even.lo, a.lo)};
+    odd = {b.hi, __fadd_rn(odd.lo, b.lo)};
+  }
+  return add_f2(even, odd);
+}
+
+// 1 / sqrt(sum / 512 + eps), by one Newton step from an fp32 estimate whose
+// residual 1 - m y^2 is taken exactly.
+__device__ __forceinline__ F2 row_rstd(F2 sum, float eps) {
+  const F2 m = add_f2({__fmul_rn(sum.hi, 1.0f / 512.0f), __fmul_rn(sum.lo, 1.0f / 512.0f)}, {eps, 0.0f});
+  const float y = __frsqrt_rn(m.hi);
+  const F2 t = two_prod(y, y);
+  const F2 p = two_prod(m.hi, t.hi);
+  const float low = __fmaf_rn(m.lo, t.hi, __fmaf_rn(m.hi, t.lo, p.lo));
+  const float r = __fsub_rn(__fsub_rn(1.0f, p.hi), low);
+  return {y, __fmul_rn(0.5f, __fmul_rn(y, r))};
+}
+
+// RN_bf16(RN_f32(x w rstd)) of eight values in place (x w is exact in fp32).
+__device__ __forceinline__ float scale1(float v, F2 rstd) {
+  const F2 p = two_prod(v, rstd.hi);
+  return __fadd_rn(p.hi, __fmaf_rn(v, rstd.lo, p.lo));
+}
+__device__ __forceinline__ void scale_row(uint32_t (&w)[4], const uint32_t (&g)[4], F2 rstd) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    w[e] = pack_bf16(scale1(__fmul_rn(bf16_low(w[e]), bf16_low(g[e])), rstd),
+                     scale1(__fmul_rn(bf16_high(w[e]), bf16_high(g[e])), rstd));
+}
+
+}  // namespace qmla

@@ -389,46 +389,59 @@ def read_dev_err(dev_err: torch.Tensor, stream=None) -> int:
     return int(out.value)
 
 
-# The calls below take strided rows, so they look at shapes, types and devices too: a
-# tensor of another shape than the call's would be read out of range.
-def _want(name: str, t: torch.Tensor, dtype: torch.dtype, *shape) -> int:
-    """Address of a CUDA tensor of this type and shape (None: any size)."""
+# The calls below take strided rows, so they look at types, shapes and devices too: a
+# tensor of another shape than the call's would be read out of range. One comparison
+# per tensor on the way, the words only when it fails: small steps are bound by this.
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+_BLOCK_BYTES = {4: 20736, 2: 12544, "c4r4": 20480, "bf16": 73728}
+_device = torch._C._cuda_getDevice
+
+
+def _refuse(name: str, t, dtype: torch.dtype, shape: tuple, dev: int, rows: bool = False):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor, not {type(t).__name__}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() != len(shape) or any(w is not None and w != s for w, s in zip(shape, t.shape)):
+    if tuple(t.shape) != shape:
         raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current CUDA device, not on {t.device}")
+    if not (t.stride(-1) == 1 if rows else t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous" + " in its last axis" * rows)
+    raise ValueError(f"{name} must be on the current CUDA device, not on {t.device}")
+
+
+def _flat(name: str, t: torch.Tensor, dtype: torch.dtype, shape: tuple, dev: int) -> int:
+    """Address of a contiguous tensor of this type and shape on device dev."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(name, t, dtype, shape, dev)
     return t.data_ptr()
 
 
-def _flat(name: str, t: torch.Tensor | None, dtype: torch.dtype, *shape):
-    if t is None:
-        return None
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return _want(name, t, dtype, *shape)
+def _rows(name: str, t: torch.Tensor, shape: tuple, dev: int) -> int:
+    """The same for bf16 rows with strides of their own, contiguous in their last axis."""
+    if t.dtype is not _BF16 or t.shape != shape or t.get_device() != dev or t.stride(-1) != 1:
+        _refuse(name, t, _BF16, shape, dev, rows=True)
+    return t.data_ptr()
 
 
-def _strided(name: str, t: torch.Tensor, *shape) -> int:
-    """The same for bf16 rows whose last axis lies side by side."""
-    if t.size(-1) != 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name} must be contiguous in its last axis")
-    return _want(name, t, torch.bfloat16, *shape)
+def _current_device() -> int:
+    return _device() if torch.cuda.is_initialized() else -2  # (without one every tensor is refused)
 
 
-def _cache_fields(d, pool, cache_kind, seq_ids, positions, n, block_table, seq_lens, prot, dev_err) -> None:
-    if cache_kind not in CACHE_KINDS:
+def _raw_stream(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev: int):
+    """(pool, kind, blocks, table, sequences, blocks per sequence, lengths, protection rows, error word)."""
+    width = _BLOCK_BYTES.get(cache_kind)
+    if width is None:
         raise ValueError(f"unknown cache kind {cache_kind!r}")
-    width = {4: 20736, 2: 12544, "c4r4": 20480, "bf16": 73728}[cache_kind]
-    i32, seqs = torch.int32, block_table.size(0)
-    d.pool, d.cache_kind, d.num_blocks = _flat("pool", pool, torch.uint8, None, width), CACHE_KINDS[cache_kind], pool.size(0)
-    d.seq_ids, d.positions = _flat("seq_ids", seq_ids, i32, n), _flat("positions", positions, i32, n)
-    d.n, d.num_seqs = n, seqs
-    d.block_table, d.max_blocks = _flat("block_table", block_table, i32, None, None), block_table.size(1)
-    d.seq_lens = _flat("seq_lens", seq_lens, i32, seqs)
-    d.prot = _flat("prot", prot, torch.bfloat16, seqs, 132, 576)
-    d.dev_err = _flat("dev_err", dev_err, i32, None)
+    blocks, (seqs, per) = pool.size(0), block_table.shape
+    return (_flat("pool", pool, _U8, (blocks, width), dev), CACHE_KINDS[cache_kind], blocks,
+            _flat("block_table", block_table, _I32, (seqs, per), dev), seqs, per,
+            None if seq_lens is None else _flat("seq_lens", seq_lens, _I32, (seqs,), dev),
+            None if prot is None else _flat("prot", prot, _BF16, (seqs, 132, 576), dev),
+            _flat("dev_err", dev_err, _I32, (1,), dev))
 
 
 def rope_append(pool: torch.Tensor, cache_kind, latent: torch.Tensor, k_pe: torch.Tensor,
@@ -440,39 +453,51 @@ def rope_append(pool: torch.Tensor, cache_kind, latent: torch.Tensor, k_pe: torc
     [n,64] with any row stride (columns of one projection output); cos_sin f32
     [rope_len,64]; norm_weight bf16 [512] (norm=True without it: weights of one);
     with prot (and seq_lens = lengths after this call) also the sink/recent rows."""
-    n = latent.size(0)
-    d = AppendDesc()
-    d.latent, d.latent_stride = _strided("latent", latent, n, 512), latent.stride(0)
-    d.k_pe, d.k_pe_stride = _strided("k_pe", k_pe, n, 64), k_pe.stride(0)
-    d.norm, d.norm_eps = int(norm_weight is not None if norm is None else norm), eps
-    d.norm_weight = _flat("norm_weight", norm_weight, torch.bfloat16, 512)
-    d.cos_sin, d.rope_len = _flat("cos_sin", cos_sin, torch.float32, None, 64), cos_sin.size(0)
-    d.interleaved = int(interleaved)
-    _cache_fields(d, pool, cache_kind, seq_ids, positions, n, block_table, seq_lens, prot, dev_err)
-    _check("qmla_rope_append", lib().qmla_rope_append(ctypes.byref(d), _stream(stream)))
+    dev = _current_device()
+    n, rope_len = latent.size(0), cos_sin.size(0)
+    lat, kpe = _rows("latent", latent, (n, 512), dev), _rows("k_pe", k_pe, (n, 64), dev)
+    at, kind, blocks, table, seqs, per, lens, rows, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)
+    if norm is None:
+        norm = norm_weight is not None
+    d = AppendDesc(at, kind, blocks, lat, latent.stride(0), kpe, k_pe.stride(0), 1 if norm else 0, eps,
+                   None if norm_weight is None else _flat("norm_weight", norm_weight, _BF16, (512,), dev),
+                   _flat("cos_sin", cos_sin, _F32, (rope_len, 64), dev), rope_len, 1 if interleaved else 0,
+                   None if seq_ids is None else _flat("seq_ids", seq_ids, _I32, (n,), dev),
+                   _flat("positions", positions, _I32, (n,), dev), n, seqs, table, per, lens, rows, err)
+    st = lib().qmla_rope_append(d, _raw_stream(stream, dev))
+    if st:
+        raise QmlaError("qmla_rope_append", st)
 
 
 def cache_read(pool: torch.Tensor, cache_kind, seq_ids: torch.Tensor | None, positions: torch.Tensor,
                block_table: torch.Tensor, rows: torch.Tensor, dev_err: torch.Tensor,
                seq_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None, stream=None) -> None:
     """qmla_cache_read: the values of cached tokens into rows bf16 [n,576] (any row stride)."""
+    dev = _current_device()
     n = positions.size(0)
-    d = ReadDesc()
-    d.rows, d.row_stride = _strided("rows", rows, n, 576), rows.stride(0)
-    _cache_fields(d, pool, cache_kind, seq_ids, positions, n, block_table, seq_lens, prot, dev_err)
-    _check("qmla_cache_read", lib().qmla_cache_read(ctypes.byref(d), _stream(stream)))
+    at, kind, blocks, table, seqs, per, lens, kept, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)
+    d = ReadDesc(at, kind, blocks, None if seq_ids is None else _flat("seq_ids", seq_ids, _I32, (n,), dev),
+                 _flat("positions", positions, _I32, (n,), dev), n, seqs, table, per, lens, kept,
+                 _rows("rows", rows, (n, 576), dev), rows.stride(0), err)
+    st = lib().qmla_cache_read(d, _raw_stream(stream, dev))
+    if st:
+        raise QmlaError("qmla_cache_read", st)
 
 
 def rope_query(q_pe: torch.Tensor, positions: torch.Tensor, cos_sin: torch.Tensor, out: torch.Tensor,
                dev_err: torch.Tensor, interleaved: bool = False, stream=None) -> None:
     """qmla_rope_query: q_pe and out bf16 [n,heads,64] with any strides; out may be q_pe (in place)."""
-    n, heads = q_pe.size(0), q_pe.size(1)
-    st = lib().qmla_rope_query(_strided("q_pe", q_pe, n, heads, 64), q_pe.stride(0), q_pe.stride(1),
-                               _flat("positions", positions, torch.int32, n), n, heads,
-                               _flat("cos_sin", cos_sin, torch.float32, None, 64), cos_sin.size(0), int(interleaved),
-                               _strided("out", out, n, heads, 64), out.stride(0), out.stride(1),
-                               _flat("dev_err", dev_err, torch.int32, None), _stream(stream))
-    _check("qmla_rope_query", st)
+    dev = _current_device()
+    shape, rope_len = tuple(q_pe.shape), cos_sin.size(0)
+    n, heads = shape[:2]
+    shape = (n, heads, 64)
+    (qt, qh, _), (ot, oh, _) = q_pe.stride(), out.stride()
+    st = lib().qmla_rope_query(_rows("q_pe", q_pe, shape, dev), qt, qh, _flat("positions", positions, _I32, (n,), dev), n,
+                               heads, _flat("cos_sin", cos_sin, _F32, (rope_len, 64), dev), rope_len,
+                               1 if interleaved else 0, _rows("out", out, shape, dev), ot, oh,
+                               _flat("dev_err", dev_err, _I32, (1,), dev), _raw_stream(stream, dev))
+    if st:
+        raise QmlaError("qmla_rope_query", st)
 
 
 def prefill_workspace_bytes(batch: int, n_q: int) -> int:
@@ -484,19 +509,20 @@ def mla_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pe: torch.T
                 workspace: torch.Tensor, dev_err: torch.Tensor, causal: bool = True, stream=None) -> None:
     """qmla_mla_prefill: q bf16 [n_q,H,192], k and v bf16 [n_kv,H,128], k_pe bf16 [n_kv,64] with any
     strides; cu_q, cu_kv int32 [batch+1]; out bf16 [n_q,H,128], lse f32 [n_q,H]."""
-    nq, H, nkv = q.size(0), q.size(1), k.size(0)
-    d = PrefillDesc()
-    d.q, d.q_token_stride, d.q_head_stride = _strided("q", q, nq, H, 192), q.stride(0), q.stride(1)
-    d.k, d.k_token_stride, d.k_head_stride = _strided("k", k, nkv, H, 128), k.stride(0), k.stride(1)
-    d.v, d.v_token_stride, d.v_head_stride = _strided("v", v, nkv, H, 128), v.stride(0), v.stride(1)
-    d.k_pe, d.k_pe_stride = _strided("k_pe", k_pe, nkv, 64), k_pe.stride(0)
-    d.n_q, d.n_kv, d.heads, d.batch = nq, nkv, H, cu_q.size(0) - 1
-    d.cu_q, d.cu_kv = _flat("cu_q", cu_q, torch.int32, None), _flat("cu_kv", cu_kv, torch.int32, cu_q.size(0))
-    d.causal, d.softmax_scale = int(causal), float(softmax_scale)
-    d.out, d.lse = _flat("out", out, torch.bfloat16, nq, H, 128), _flat("lse", lse, torch.float32, nq, H)
-    d.workspace, d.workspace_bytes = _flat("workspace", workspace, torch.uint8, None), workspace.nbytes
-    d.dev_err = _flat("dev_err", dev_err, torch.int32, None)
-    _check("qmla_mla_prefill", lib().qmla_mla_prefill(ctypes.byref(d), _stream(stream)))
+    dev = _current_device()
+    nq, H, nkv, offsets = q.size(0), q.size(1), k.size(0), cu_q.size(0)
+    (qt, qh, _), (kt, kh, _), (vt, vh, _) = q.stride(), k.stride(), v.stride()
+    d = PrefillDesc(_rows("q", q, (nq, H, 192), dev), qt, qh, _rows("k", k, (nkv, H, 128), dev), kt, kh,
+                    _rows("v", v, (nkv, H, 128), dev), vt, vh, _rows("k_pe", k_pe, (nkv, 64), dev), k_pe.stride(0), nq,
+                    nkv, H, offsets - 1, _flat("cu_q", cu_q, _I32, (offsets,), dev),
+                    _flat("cu_kv", cu_kv, _I32, (offsets,), dev), 1 if causal else 0, softmax_scale,
+                    _flat("out", out, _BF16, (nq, H, 128), dev),
+                    None if lse is None else _flat("lse", lse, _F32, (nq, H), dev),
+                    _flat("workspace", workspace, _U8, (workspace.size(0),), dev), workspace.size(0),
+                    _flat("dev_err", dev_err, _I32, (1,), dev))
+    st = lib().qmla_mla_prefill(d, _raw_stream(stream, dev))
+    if st:
+        raise QmlaError("qmla_mla_prefill", st)
 
 
 def workspace_for(batch: int, heads: int, device="cuda") -> torch.Tensor:

@@ -405,6 +405,12 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
 // Softmax and epilogue of tile i, a query row per thread.
 __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int i, int warp, int lane) {
   const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -433,10 +439,16 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
 #pragma unroll
         for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : -INFINITY;
       }
-      float top = -INFINITY;
+      // (eight chains: a single one is 128 dependent steps)
+      float tops[8];
 #pragma unroll
-      for (int c = 0; c < 128; ++c) top = fmaxf(top, s[c]);
-      top *= p.scale_log2;
+      for (int c = 0; c < 8; ++c) tops[c] = fmaxf(s[c], s[c + 8]);
+#pragma unroll
+      for (int c = 16; c < 128; c += 16)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) tops[x] = max3(tops[x], s[c + x], s[c + 8 + x]);
+      const float top = p.scale_log2 * max3(max3(tops[0], tops[1], tops[2]), max3(tops[3], tops[4], tops[5]),
+                                            fmaxf(tops[6], tops[7]));
       const bool raise = top > m + kRaise;  // (m = -inf: the first visible key)
       float factor = 1.0f;
       if (raise) {
@@ -458,20 +470,21 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
       }
       const float ref = m == -INFINITY ? 0.0f : m;
       const uint64_t sl = f32x2(p.scale_log2, p.scale_log2), mm = f32x2(-ref, -ref);
-      uint64_t sum = f32x2(0.0f, 0.0f);
+      uint64_t sum[4] = {0, 0, 0, 0};  // (pairs of zeros)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t w[32];
+      for (int h = 0; h < 4; ++h) {
+        uint32_t w[16];
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          const uint64_t x = fma2(f32x2(s[64 * h + 2 * c], s[64 * h + 2 * c + 1]), sl, mm);
+        for (int c = 0; c < 16; ++c) {
+          const uint64_t x = fma2(f32x2(s[32 * h + 2 * c], s[32 * h + 2 * c + 1]), sl, mm);
           const float a = ex2(lo2(x)), b = ex2(hi2(x));
-          sum = add2(sum, f32x2(a, b));
+          sum[c & 3] = add2(sum[c & 3], f32x2(a, b));
           w[c] = pack_bf16(a, b);
         }
-        tmem_st32(t_s + 32 * h, w);
+        tmem_st(t_s + 16 * h, w);
       }
-      l += lo2(sum) + hi2(sum);
+      const uint64_t sums = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+      l += lo2(sums) + hi2(sums);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();

@@ -3,14 +3,16 @@
 // in PV.
 //
 // plan_kernel cuts every sequence into items of 256 query rows and orders them,
-// the longest first; prefill_kernel (persistent, one CTA per SM) works (item, head)
-// pairs off that list. In a CTA the two 128-row tiles of an item take turns on the
+// the longest first; prefill_kernel (persistent, one CTA per SM) draws (item, head)
+// pairs from that list. In a CTA the two 128-row tiles of an item take turns on the
 // tensor core: while one tile's scores are turned into weights, the other's MMAs
-// run (PV of the old keys, QK of the next).
+// run (PV of the old keys, QK of the next). An item of one tile (a short prompt, a
+// sequence's last rows) has its keys dealt to the two in turn instead: both hold
+// the same rows, every other key step each, and are merged at the end.
 //
 //   warps 0..3 / 4..7   softmax of tile 0 / 1, a query row per thread; epilogue
 //   warp 8              one thread that issues every MMA
-//   warp 9              TMA loads of queries, keys and values
+//   warp 9              draws the pairs; TMA loads of queries, keys and values
 //
 // Shared memory: the queries (2 x 3 chunks of 128 rows x 64 channels, 96 KB) and a
 // ring of eight 16 KB slots for keys (three slots per 128 tokens: two content
@@ -61,19 +63,28 @@ struct Ctl {
   uint64_t q_full[2], q_free[2];
   uint64_t full[4], freed[4];  // of entry e: [e & 3]
   uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t sched_full[2], sched_free[2];
+  uint64_t x_ready, x_done;  // tile 1's share of a one-tile item is there / has been read
   uint64_t tail, fin;
   uint32_t tmem_base, abort;
+  int4 work[2][3];
+  float2 share[kTile];  // (m, l) of tile 1's rows
 };
 constexpr int kSmem = kCtlOff + static_cast<int>(sizeof(Ctl)) + 1024;  // (the base is moved to a multiple of 1024)
 static_assert(kSmem <= 232448, "shared memory of a CTA");
 
 // Two tiles of one sequence: rows q_row .. of q, `rows` of them (at most 256); keys
 // kv_start .. + kv_len. Row r sees the first min(kv_len, vis0 + r * step) keys.
+// Items that lie side by side in a sequence form bundles: the list holds a bundle's
+// items for one head, then for the next, so that they meet the same keys in L2.
 struct Item {
   int q_row, rows, kv_start, kv_len;
-  int vis0, step, n0, n1;  // n0, n1: key steps of the tiles
+  int vis0, step, n0, n1;  // n0, n1: key steps of the tiles (dealt: of the one tile, 0)
+  int first, bundle;       // the bundle's first item and its length
+  int head;                // (of a pair; -1: no more)
+  int dealt;               // one tile, whose key steps the two tiles share out
 };
-static_assert(sizeof(Item) == 32, "two 16-byte loads");
+static_assert(sizeof(Item) == 48, "three 16-byte loads");
 
 struct Workspace {
   size_t prefix_off, items_off, total;
@@ -82,7 +93,7 @@ struct Workspace {
 Workspace workspace_layout(int batch, int n_q) {
   Workspace w;
   w.max_items = n_q / kItemRows + batch;  // disjoint sequences have no more
-  w.prefix_off = 256;                     // int: items written
+  w.prefix_off = 256;                     // int: items written; int: pairs drawn beyond one per CTA
   w.items_off = (w.prefix_off + 4 * (static_cast<size_t>(batch) + 1) + 255) / 256 * 256;
   w.total = w.items_off + sizeof(Item) * static_cast<size_t>(w.max_items);
   return w;
@@ -113,11 +124,12 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
   return (warp == 0 ? 0 : before) + x - v;  // exclusive
 }
 
-// One block. Items of a sequence: ceil(Lq / 256); a counting sort by their key steps
-// puts the longest first (the order among equals is free: items do not meet).
+// One block. A sequence has ceil(Lq / 256) items, in bundles of `bundle`; a counting
+// sort by key steps puts the longest bundles first (the order among equals is free:
+// items do not meet).
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ cu_q,
                                                             const int32_t* __restrict__ cu_kv, int batch, int n_q,
-                                                            int n_kv, int causal, int shift, int max_items,
+                                                            int n_kv, int causal, int bundle, int shift, int max_items,
                                                             int* __restrict__ count, int* __restrict__ prefix,
                                                             Item* __restrict__ items, uint32_t* dev_err) {
   __shared__ int warp_sums[32];
@@ -125,7 +137,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
   griddep_launch_dependents();  // prefill_kernel may start its set-up meanwhile
   const int tid = threadIdx.x;
   bucket[tid] = 0;
-  int base = 0;
+  int bundles = 0, total_items = 0;
   for (int b0 = 0; b0 < batch; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int tiles = 0;
@@ -137,19 +149,23 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         tiles = (q1 - q0 + kItemRows - 1) / kItemRows;
       }
     }
-    int total;
-    const int at = block_scan(tiles, warp_sums, total);
-    if (b < batch) prefix[b] = base + at;
-    base += total;
-    if (base > max_items) base = max_items + 1;  // (decreasing offsets can make sequences overlap)
+    int sum;
+    const int at = block_scan((tiles + bundle - 1) / bundle, warp_sums, sum);
+    if (b < batch) prefix[b] = bundles + at;
+    bundles += sum;
+    block_scan(tiles, warp_sums, sum);
+    total_items += sum;
+    // Decreasing offsets can make sequences overlap, which can be more than there is
+    // room for: then nothing is worked on.
+    if (total_items > max_items) break;
   }
-  if (base > max_items) {
+  if (total_items > max_items) {
     if (tid == 0) report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
-    base = max_items;
+    bundles = total_items = 0;
   }
   __syncthreads();
   for (int pass = 0; pass < 2; ++pass) {
-    for (int i = tid; i < base; i += kPlanThreads) {
+    for (int i = tid; i < bundles; i += kPlanThreads) {
       int lo = 0, hi = batch - 1;  // the last sequence with prefix <= i: it has items
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -160,69 +176,56 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         }
       }
       const int q0 = cu_q[lo], lq = cu_q[lo + 1] - q0, k0 = cu_kv[lo], lk = cu_kv[lo + 1] - k0;
-      const int r0 = (i - prefix[lo]) * kItemRows;
-      Item it;
-      it.q_row = q0 + r0;
-      it.rows = min(lq - r0, kItemRows);
-      it.kv_start = k0;
-      it.kv_len = lk;
-      it.vis0 = causal ? r0 + lk - lq + 1 : lk;
-      it.step = causal ? 1 : 0;
-      const int last0 = min(it.rows, kTile) - 1, last1 = it.rows - 1;
-      it.n0 = (max(min(lk, it.vis0 + it.step * last0), 0) + kTile - 1) / kTile;
-      it.n1 = it.rows > kTile ? (max(min(lk, it.vis0 + it.step * last1), 0) + kTile - 1) / kTile : 0;
-      const int key = kPlanThreads - 1 - min(max(it.n0, it.n1) >> shift, kPlanThreads - 1);
-      const int at = atomicAdd(&bucket[key], 1);
-      if (pass == 1 && at < max_items) items[at] = it;
+      const int tiles = (lq + kItemRows - 1) / kItemRows, t0 = (i - prefix[lo]) * bundle, k = min(bundle, tiles - t0);
+      // (the last item is the longest; it stands first)
+      int at = 0;
+      for (int x = 0; x < k; ++x) {
+        const int r0 = (t0 + k - 1 - x) * kItemRows;
+        Item it;
+        it.q_row = q0 + r0;
+        it.rows = min(lq - r0, kItemRows);
+        it.kv_start = k0;
+        it.kv_len = lk;
+        it.vis0 = causal ? r0 + lk - lq + 1 : lk;
+        it.step = causal ? 1 : 0;
+        const int last0 = min(it.rows, kTile) - 1, last1 = it.rows - 1;
+        it.n0 = (max(min(lk, it.vis0 + it.step * last0), 0) + kTile - 1) / kTile;
+        it.n1 = it.rows > kTile ? (max(min(lk, it.vis0 + it.step * last1), 0) + kTile - 1) / kTile : 0;
+        it.dealt = it.rows <= kTile && it.n0 > 1 ? 1 : 0;
+        it.head = 0;
+        if (x == 0) {
+          const int key = kPlanThreads - 1 - min(max(it.n0, it.n1) >> shift, kPlanThreads - 1);
+          at = atomicAdd(&bucket[key], k);
+          if (pass == 0) break;
+        }
+        it.first = at;
+        it.bundle = k;
+        items[at + x] = it;
+      }
     }
     __syncthreads();
     if (pass == 0) {
-      int total;
-      const int before = block_scan(bucket[tid], warp_sums, total);
+      int sum;
+      const int before = block_scan(bucket[tid], warp_sums, sum);
       bucket[tid] = before;
       __syncthreads();
     }
   }
-  if (tid == 0) *count = base;
+  if (tid == 0) {
+    count[0] = total_items;
+    count[1] = 0;
+  }
 }
 
 // ------------------------------------------------------------------------ main
 struct PrefillParams {
-  const int* count;
+  int* count;  // [0] items, [1] pairs drawn beyond one per CTA
   const Item* items;
-  int heads, group;  // group: heads that are worked on together (their keys fit into L2)
+  int heads;
   float scale, scale_log2;
   uint16_t* out;
   float* lse;
   uint32_t* dev_err;
-};
-
-// The (item, head) pairs of this CTA: the list goes by groups of heads, in a group
-// by item (longest first), then head; round k takes pair k * grid + cta, every other
-// round from the other end, which evens the sums out.
-struct Walk {
-  long long total;
-  int count, round;
-  __device__ __forceinline__ void init(const PrefillParams& p) {
-    count = *p.count;
-    total = static_cast<long long>(count) * p.heads;
-    round = 0;
-  }
-  __device__ __forceinline__ bool next(const PrefillParams& p, Item& it, int& head) {
-    const int g = static_cast<int>(gridDim.x), c = static_cast<int>(blockIdx.x);
-    const long long at = static_cast<long long>(round) * g + ((round & 1) ? g - 1 - c : c);
-    ++round;
-    if (at >= total) return false;
-    const long long per = static_cast<long long>(count) * p.group;
-    const int grp = static_cast<int>(at / per), rem = static_cast<int>(at - grp * per);
-    const int in = min(p.group, p.heads - grp * p.group);
-    const int i = rem / in;
-    head = grp * p.group + rem - i * in;
-    const int4* src = reinterpret_cast<const int4*>(p.items + i);
-    const int4 a = src[0], b = src[1];
-    it = Item{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    return true;
-  }
 };
 
 __device__ __forceinline__ void give_up(Ctl& c, uint32_t* dev_err, uint32_t site) {
@@ -240,76 +243,139 @@ __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl& c
   return __all_sync(0xffffffffu, wait1(bar, parity, c, site, dev_err));
 }
 
-// First slot of entry e: keys (even e) take three, values two.
-__device__ __forceinline__ uint32_t entry_slot(uint32_t e) { return 5u * (e >> 1) + 3u * (e & 1u); }
+// The pair at hand, k-th of this CTA: read from shared memory, where the load warp
+// leaves it. Called by whole warps (LANES) and by the MMA thread.
+template <bool LANES>
+__device__ __forceinline__ bool next_pair(Ctl& c, uint32_t k, Item& it, uint32_t site, uint32_t* dev_err) {
+  uint64_t* bar = &c.sched_full[k & 1u];
+  if (!(LANES ? wait_warp(bar, k >> 1, c, site, dev_err) : wait1(bar, k >> 1, c, site, dev_err))) return false;
+  const int4 x = c.work[k & 1u][0], y = c.work[k & 1u][1], z = c.work[k & 1u][2];
+  it = Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+  if (LANES) __syncwarp();
+  mbar_arrive_if(!LANES || (threadIdx.x & 31) == 0 ? 1u : 0u, &c.sched_free[k & 1u]);
+  return it.head >= 0;
+}
+
+// An entry of the ring: the keys (three slots) or the values (two) of a key step.
+// Three entries are on their way at once; no three in a row are all keys, so they
+// fit into the eight slots.
+struct Entry {
+  uint32_t e = 0, slot = 0;
+  __device__ __forceinline__ void next(uint32_t slots) {
+    ++e;
+    slot = (slot + slots) & 7u;
+  }
+};
 
 __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
                           const CUtensorMap& tpe, uint8_t* sm, Ctl& ctl, int lane) {
   uint8_t* ring = sm + kRingOff;
-  uint32_t e = 0, nq[2] = {0, 0}, tails = 0;
+  Entry en;
+  uint32_t nq[2] = {0, 0}, tails = 0;
   bool ok = true;
-  Walk walk;
-  walk.init(p);
   Item it;
-  int head;
   auto load_q = [&](int i) {
     if (nq[i] > 0 && !(ok = wait_warp(&ctl.q_free[i], nq[i] - 1, ctl, kSiteLoad, p.dev_err))) return;
     if (lane == 0) {
       mbar_arrive_expect_tx(&ctl.q_full[i], kQChunks * kSlotBytes);
       for (int c = 0; c < kQChunks; ++c)
-        tma_load_3d(sm + (i * kQChunks + c) * kSlotBytes, &tq, c * 64, head, it.q_row + i * kTile, &ctl.q_full[i]);
+        tma_load_3d(sm + (i * kQChunks + c) * kSlotBytes, &tq, c * 64, it.head, it.q_row + i * kTile, &ctl.q_full[i]);
     }
     ++nq[i];
   };
-  while (ok && walk.next(p, it, head)) {
+  auto room = [&]() {
+    if (en.e >= kInFlight)
+      ok = wait_warp(&ctl.freed[(en.e - kInFlight) & 3u], (en.e - kInFlight) >> 2, ctl, kSiteLoad, p.dev_err);
+    return ok;
+  };
+  auto load_k = [&](int j) {
+    if (!room()) return;
+    if (lane == 0) {
+      const int row = it.kv_start + j * kTile;
+      uint64_t* bar = &ctl.full[en.e & 3u];
+      mbar_arrive_expect_tx(bar, kKChunks * kSlotBytes);
+      for (int c = 0; c < 2; ++c)
+        tma_load_3d(ring + ((en.slot + c) & 7u) * kSlotBytes, &tk, c * 64, it.head, row, bar);
+      tma_load_2d(ring + ((en.slot + 2) & 7u) * kSlotBytes, &tpe, 0, row, bar);
+    }
+    en.next(kKChunks);
+  };
+  auto load_v = [&](int j) {
+    if (!room()) return;
+    const int row = it.kv_start + j * kTile;
+    uint64_t* bar = &ctl.full[en.e & 3u];
+    uint8_t* s0 = ring + en.slot * kSlotBytes;
+    uint8_t* s1 = ring + ((en.slot + 1) & 7u) * kSlotBytes;
+    // Rows behind the sequence's last token belong to others: their weights are 0,
+    // but 0 x inf is not, so they are cleared before the tensor core sees them.
+    const int left = it.kv_len - j * kTile;
+    uint64_t* on = left < kTile ? &ctl.tail : bar;
+    if (lane == 0) {
+      mbar_arrive_expect_tx(on, kVSlots * kSlotBytes);
+      for (int c = 0; c < 2; ++c) {
+        tma_load_3d(s0 + c * 8192, &tv, c * 64, it.head, row, on);
+        tma_load_3d(s1 + c * 8192, &tv, c * 64, it.head, row + 64, on);
+      }
+    }
+    if (left < kTile) {
+      if (!(ok = wait_warp(&ctl.tail, tails, ctl, kSiteLoad, p.dev_err))) {
+        if (lane == 0) mbar_wait(&ctl.tail, tails & 1u, kLimitNs, nullptr);  // (its copy may be on its way)
+        return;
+      }
+      ++tails;
+      for (int x = lane; x < (kTile - left) * 16; x += 32) {  // 16-byte pieces: 8 per row and half
+        const int t = left + (x >> 4), c = (x >> 3) & 1;
+        uint8_t* dst = (t < 64 ? s0 : s1) + c * 8192 + (t & 63) * 128 + (x & 7) * 16;
+        *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      mbar_arrive_if(lane == 0 ? 1u : 0u, bar);
+    }
+    en.next(kVSlots);
+  };
+  const int pairs = p.count[0] * p.heads;
+  for (uint32_t k = 0; ok; ++k) {
+    // Draw a pair: pair c for the CTA's first, then whichever is next.
+    int4 w[3];
+    if (k >= 2 && !(ok = wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err))) break;
+    int at = static_cast<int>(blockIdx.x);
+    if (k > 0) {
+      if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
+      at = __shfl_sync(0xffffffffu, at, 0);
+    }
+    w[0] = w[1] = make_int4(0, 0, 0, 0);
+    w[2] = make_int4(0, 0, -1, 0);
+    if (at < pairs) {
+      const int4* list = reinterpret_cast<const int4*>(p.items);
+      const int4 b = list[at / p.heads * 3 + 2];
+      const int rem = at - b.x * p.heads, head = rem / b.y;
+      const int i = b.x + rem - head * b.y;
+      w[0] = list[i * 3];
+      w[1] = list[i * 3 + 1];
+      w[2] = list[i * 3 + 2];
+      w[2].z = head;
+    }
+    it = Item{w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w, w[2].x, w[2].y, w[2].z, w[2].w};
+    if (lane == 0) {
+      for (int x = 0; x < 3; ++x) ctl.work[k & 1u][x] = w[x];
+    }
+    mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.sched_full[k & 1u]);
+    if (it.head < 0) break;
+    // In the order in which mma_role uses them up.
     const int n = max(it.n0, it.n1);
     if (it.n0 > 0) load_q(0);
-    for (int j = 0; ok && j < n; ++j) {
-      const int row = it.kv_start + j * kTile;
-      for (int v = 0; ok && v < 2; ++v, ++e) {
-        if (e >= kInFlight &&
-            !(ok = wait_warp(&ctl.freed[(e - kInFlight) & 3u], (e - kInFlight) >> 2, ctl, kSiteLoad, p.dev_err)))
-          break;
-        uint64_t* bar = &ctl.full[e & 3u];
-        const uint32_t slot = entry_slot(e);
-        uint8_t* s0 = ring + (slot & 7u) * kSlotBytes;
-        uint8_t* s1 = ring + ((slot + 1) & 7u) * kSlotBytes;
-        if (v == 0) {
-          if (lane == 0) {
-            mbar_arrive_expect_tx(bar, kKChunks * kSlotBytes);
-            tma_load_3d(s0, &tk, 0, head, row, bar);
-            tma_load_3d(s1, &tk, 64, head, row, bar);
-            tma_load_2d(ring + ((slot + 2) & 7u) * kSlotBytes, &tpe, 0, row, bar);
-          }
-          if (j == 0 && it.n1 > 0) load_q(1);
-          continue;
-        }
-        // Rows behind the sequence's last token belong to others: their weights are 0,
-        // but 0 x inf is not, so they are cleared before the tensor core sees them.
-        const int left = it.kv_len - j * kTile;
-        uint64_t* on = left < kTile ? &ctl.tail : bar;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(on, kVSlots * kSlotBytes);
-          for (int c = 0; c < 2; ++c) {
-            tma_load_3d(s0 + c * 8192, &tv, c * 64, head, row, on);
-            tma_load_3d(s1 + c * 8192, &tv, c * 64, head, row + 64, on);
-          }
-        }
-        if (left < kTile) {
-          if (!(ok = wait_warp(&ctl.tail, tails, ctl, kSiteLoad, p.dev_err))) {
-            if (lane == 0) mbar_wait(&ctl.tail, tails & 1u, kLimitNs, nullptr);  // (its copy may be on its way)
-            break;
-          }
-          ++tails;
-          for (int x = lane; x < (kTile - left) * 16; x += 32) {  // 16-byte pieces: 8 per row and half
-            const int t = left + (x >> 4), c = (x >> 3) & 1;
-            uint8_t* dst = (t < 64 ? s0 : s1) + c * 8192 + (t & 63) * 128 + (x & 7) * 16;
-            *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          mbar_arrive_if(lane == 0 ? 1u : 0u, bar);
-        }
+    if (it.dealt != 0) {
+      if (ok) load_k(0);
+      for (int j = 0; ok && j < n; ++j) {
+        if (j + 1 < n) load_k(j + 1);
+        if (ok) load_v(j);
+      }
+    } else {
+      for (int j = 0; ok && j < n; ++j) {
+        load_k(j);
+        if (ok && j == 0 && it.n1 > 0) load_q(1);
+        if (ok) load_v(j);
       }
     }
   }
@@ -318,8 +384,9 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
   // ignore the abort flag.
   for (int i = 0; i < 2; ++i)
     if (nq[i] > 0 && mbar_wait(&ctl.q_full[i], (nq[i] - 1) & 1u, kLimitNs, nullptr) != 1) give_up(ctl, p.dev_err, kSiteEnd);
-  for (uint32_t k = 1; k <= kInFlight && k <= e; ++k)
-    if (mbar_wait(&ctl.full[(e - k) & 3u], ((e - k) >> 2) & 1u, kLimitNs, nullptr) != 1) give_up(ctl, p.dev_err, kSiteEnd);
+  for (uint32_t k = 1; k <= kInFlight && k <= en.e; ++k)
+    if (mbar_wait(&ctl.full[(en.e - k) & 3u], ((en.e - k) >> 2) & 1u, kLimitNs, nullptr) != 1)
+      give_up(ctl, p.dev_err, kSiteEnd);
 }
 
 // One thread.
@@ -329,70 +396,96 @@ __device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32
   const uint64_t q0 = smem_desc(smem, 16, 1024, SWZ_128B);
   const uint64_t r_k = smem_desc(smem + kRingOff, 16, 1024, SWZ_128B);
   const uint64_t r_v = smem_desc(smem + kRingOff, 8192, 1024, SWZ_128B);
-  uint32_t e0 = 0, nq[2] = {0, 0}, np[2] = {0, 0};
+  Entry en;
+  uint32_t nq[2] = {0, 0}, np[2] = {0, 0};
   bool ok = true;
-  auto qk = [&](int i, uint32_t e) {
-    const uint32_t slot = entry_slot(e);
+  // S_i = Q (tile q of shared memory) K^T
+  auto qk = [&](int i, int q, const Entry& k) {
 #pragma unroll
     for (int c = 0; c < kKChunks; ++c) {
-      const uint64_t a = q0 + ((i * kQChunks + c) * kSlotBytes >> 4);
-      const uint64_t b = r_k + (((slot + c) & 7u) * kSlotBytes >> 4);
+      const uint64_t a = q0 + ((q * kQChunks + c) * kSlotBytes >> 4);
+      const uint64_t b = r_k + (((k.slot + c) & 7u) * kSlotBytes >> 4);
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
         umma_f16_ss(tmem + i * 128, a + (kk * 32 >> 4), b + (kk * 32 >> 4), kIdQK, (c | kk) != 0 ? 1u : 0u);
     }
     umma_commit(&ctl.s_full[i]);
   };
-  auto pv = [&](int i, uint32_t e, bool first) {
-    const uint32_t slot = entry_slot(e);
+  // O_i (+)= P_i V
+  auto pv = [&](int i, const Entry& v, bool first) {
 #pragma unroll
     for (int h = 0; h < kVSlots; ++h) {
-      const uint64_t b = r_v + (((slot + h) & 7u) * kSlotBytes >> 4);
+      const uint64_t b = r_v + (((v.slot + h) & 7u) * kSlotBytes >> 4);
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
         umma_f16_ts(tmem + kColO + i * 128, tmem + i * 128 + (h * 4 + kk) * 8, b + (kk * 2048 >> 4), kIdPV,
                     first && (h | kk) == 0 ? 0u : 1u);
     }
   };
-  auto full = [&](uint32_t e) { return wait1(&ctl.full[e & 3u], e >> 2, ctl, kSiteMma, p.dev_err); };
-  Walk walk;
-  walk.init(p);
+  auto full = [&](const Entry& x) { return ok = wait1(&ctl.full[x.e & 3u], x.e >> 2, ctl, kSiteMma, p.dev_err); };
+  auto query = [&](int q) { return ok = wait1(&ctl.q_full[q], nq[q]++, ctl, kSiteMma, p.dev_err); };
+  auto weights = [&](int i) { return ok = wait1(&ctl.p_full[i], np[i]++, ctl, kSiteMma, p.dev_err); };
   Item it;
-  int head;
-  while (ok && walk.next(p, it, head)) {
+  for (uint32_t pair = 0; ok && next_pair<false>(ctl, pair, it, kSiteMma, p.dev_err); ++pair) {
     const int n[2] = {it.n0, it.n1}, nmax = max(it.n0, it.n1);
     if (nmax == 0) continue;
+    if (it.dealt != 0) {
+      // Key steps u = 0, 2, .. are tile 0's, 1, 3, .. tile 1's. Entries: K0, K1, V0, K2, V1, ..
+      if (!query(0)) break;
+      Entry v = en;
+      for (int u = -2; ok && u < nmax; ++u) {
+        const int i = u & 1;
+        if (u >= 0) {
+          v = en;
+          if (!full(v) || !weights(i)) break;
+          tc_fence_after();
+          // (a step's values lie behind the next step's keys, but for the last)
+          pv(i, v, u < 2);
+          umma_commit(&ctl.freed[v.e & 3u]);
+          if (u + 2 >= nmax) umma_commit(&ctl.o_full[i]);
+          en.next(kVSlots);
+        }
+        if (u + 2 < nmax) {
+          if (!full(en)) break;
+          tc_fence_after();
+          qk(i, 0, en);
+          umma_commit(&ctl.freed[en.e & 3u]);
+          if (u + 3 == nmax) umma_commit(&ctl.q_free[0]);
+          en.next(kKChunks);
+        }
+      }
+      continue;
+    }
+    Entry k = en;  // keys of step j + 1
     for (int j = -1; ok && j < nmax; ++j) {
       // step j: PV of keys j and QK of keys j + 1, tile by tile
-      const uint32_t ek = e0 + 2 * (j + 1), ev = e0 + 2 * j + 1;
+      Entry v = k;  // values of step j, before those keys
+      if (j >= 0) k.next(kVSlots);
       bool k_here = false, v_here = false;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (j >= 0 && j < n[i]) {
-          if (!v_here && !(ok = full(ev))) break;
+          if (!v_here && !full(v)) break;
           v_here = true;
-          if (!(ok = wait1(&ctl.p_full[i], np[i], ctl, kSiteMma, p.dev_err))) break;
-          ++np[i];
+          if (!weights(i)) break;
           tc_fence_after();
-          pv(i, ev, j == 0);
+          pv(i, v, j == 0);
           if (j + 1 == n[i]) umma_commit(&ctl.o_full[i]);
         }
-        if (i == 1 && v_here) umma_commit(&ctl.freed[ev & 3u]);
+        if (i == 1 && v_here) umma_commit(&ctl.freed[v.e & 3u]);
         if (j + 1 < n[i]) {
-          if (j < 0) {
-            if (!(ok = wait1(&ctl.q_full[i], nq[i], ctl, kSiteMma, p.dev_err))) break;
-            ++nq[i];
-          }
-          if (!k_here && !(ok = full(ek))) break;
+          if (j < 0 && !query(i)) break;
+          if (!k_here && !full(k)) break;
           k_here = true;
           tc_fence_after();
-          qk(i, ek);
+          qk(i, i, k);
           if (j + 2 == n[i]) umma_commit(&ctl.q_free[i]);
         }
-        if (i == 1 && k_here) umma_commit(&ctl.freed[ek & 3u]);
+        if (i == 1 && k_here) umma_commit(&ctl.freed[k.e & 3u]);
       }
+      if (j + 1 < nmax) k.next(kKChunks);
     }
-    e0 += 2 * nmax;
+    en = k;
   }
   // Every MMA must have landed before TMEM and shared memory are released.
   umma_commit(&ctl.fin);
@@ -415,15 +508,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int i, int warp, int lane) {
   const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
   const uint32_t t_s = tmem + lanes + i * 128, t_o = tmem + lanes + kColO + i * 128;
-  const int row = i * kTile + (warp & 3) * 32 + lane;  // of the item
-  uint32_t ns = 0, no = 0;
-  Walk walk;
-  walk.init(p);
+  const int row_in = (warp & 3) * 32 + lane;  // of the tile
+  uint32_t ns = 0, no = 0, nx = 0;
   Item it;
-  int head;
-  while (walk.next(p, it, head)) {
-    const int n = i == 0 ? it.n0 : it.n1;
-    float m = -INFINITY, l = 0.0f;  // m in units of log2
+  for (uint32_t pair = 0; next_pair<true>(ctl, pair, it, kSiteSoftmax, p.dev_err); ++pair) {
+    const bool dealt = it.dealt != 0;
+    const int n = dealt ? (it.n0 + 1 - i) / 2 : (i == 0 ? it.n0 : it.n1);
+    const int row = dealt ? row_in : row_in + i * kTile;  // of the item
+    float m = -INFINITY, l = 0.0f;                        // m in units of log2
     const int vis = min(it.kv_len, it.vis0 + it.step * row);
     const int vis_warp = min(it.kv_len, it.vis0 + it.step * (row - lane));  // of the warp's first row
     for (int j = 0; j < n; ++j) {
@@ -434,8 +526,9 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
 #pragma unroll
       for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32 * c, reinterpret_cast<uint32_t*>(s + 32 * c));
       tmem_ld_wait();
-      if (vis_warp < (j + 1) * kTile) {
-        const int lim = vis - j * kTile;
+      const int key0 = (dealt ? 2 * j + i : j) * kTile;
+      if (vis_warp < key0 + kTile) {
+        const int lim = vis - key0;
 #pragma unroll
         for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : -INFINITY;
       }
@@ -495,30 +588,68 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
       ++no;
       tc_fence_after();
     }
-    const bool mine = row < it.rows;
+    float mine = 1.0f, theirs = 0.0f;  // weights of this tile's O and, dealt, of tile 1's
+    if (dealt) {
+      if (i == 1) {
+        // Leaves its sums and goes on once tile 0 has read them and O1.
+        ctl.share[row_in] = make_float2(m, l);
+        tc_fence_before();
+        __syncwarp();
+        mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.x_ready);
+        if (!wait_warp(&ctl.x_done, nx, ctl, kSiteSoftmax, p.dev_err)) return;
+        ++nx;
+        tc_fence_after();
+        continue;
+      }
+      if (!wait_warp(&ctl.x_ready, nx, ctl, kSiteSoftmax, p.dev_err)) return;
+      ++nx;
+      tc_fence_after();
+      const float2 other = ctl.share[row_in];
+      const float both = fmaxf(m, other.x);
+      const float ref = both == -INFINITY ? 0.0f : both;
+      mine = ex2(m - ref);
+      theirs = ex2(other.x - ref);
+      l = l * mine + other.y * theirs;
+      m = both;
+    }
+    const bool write = row < it.rows;
     const bool none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
     const float inv = 1.0f / l;
-    const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + head;
-    if (mine && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
+    const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + it.head;
+    if (write && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
     uint4* dst = reinterpret_cast<uint4*>(p.out + at * kDv);
+    mine *= inv;
+    theirs *= inv;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       uint32_t o[32];
       if (n > 0) {
         tmem_ld32(t_o + 32 * c, o);
         tmem_ld_wait();
+#pragma unroll
+        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * mine);
+      }
+      if (dealt) {
+        uint32_t o1[32];
+        tmem_ld32(t_o + 128 + 32 * c, o1);
+        tmem_ld_wait();
+#pragma unroll
+        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(fmaf(__uint_as_float(o1[x]), theirs, __uint_as_float(o[x])));
       }
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         uint32_t w[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          w[y] = none ? 0u
-                      : pack_bf16(__uint_as_float(o[8 * x + 2 * y]) * inv, __uint_as_float(o[8 * x + 2 * y + 1]) * inv);
-        if (mine) dst[4 * c + x] = make_uint4(w[0], w[1], w[2], w[3]);
+          w[y] = none ? 0u : pack_bf16(__uint_as_float(o[8 * x + 2 * y]), __uint_as_float(o[8 * x + 2 * y + 1]));
+        if (write) dst[4 * c + x] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
     tc_fence_before();
+    if (dealt) {
+      __syncwarp();
+      mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.x_done);
+    }
   }
 }
 
@@ -542,6 +673,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&ctl.full[i], 1);
       mbar_init(&ctl.freed[i], 1);
     }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl.sched_full[i], 1);
+      mbar_init(&ctl.sched_free[i], kSoftWarps + 1);
+    }
+    mbar_init(&ctl.x_ready, 4);
+    mbar_init(&ctl.x_done, 4);
     mbar_init(&ctl.tail, 1);
     mbar_init(&ctl.fin, 1);
     ctl.abort = 0u;
@@ -628,13 +765,9 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   const Workspace w = workspace_layout(d.batch, d.n_q);
   uint8_t* ws = static_cast<uint8_t*>(d.workspace);
   PrefillParams p;
-  p.count = reinterpret_cast<const int*>(ws);
+  p.count = reinterpret_cast<int*>(ws);
   p.items = reinterpret_cast<const Item*>(ws + w.items_off);
   p.heads = d.heads;
-  // Keys and values of a group of heads: at most 48 MB, so that the items that run
-  // at the same time find them in the 126 MB L2.
-  p.group = static_cast<int>(
-      std::min<long long>(d.heads, std::max<long long>(1, (48ll << 20) / (std::max(d.n_kv, 1) * 512ll))));
   p.scale = d.softmax_scale;
   p.scale_log2 = d.softmax_scale * 1.4426950408889634f;
   p.out = d.out;
@@ -665,14 +798,17 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
       return e;
     configured_device = dev;
   }
+  const long long pairs = static_cast<long long>(w.max_items) * d.heads;
+  // Items per bundle: with few pairs per SM single items even the load out better.
+  const int bundle = pairs >= 8ll * sms ? 4 : 1;
   int shift = 0;
   while (((d.n_kv / kTile + 1) >> shift) >= kPlanThreads) ++shift;
-  plan_kernel<<<1, kPlanThreads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.causal != 0, shift, w.max_items,
+  plan_kernel<<<1, kPlanThreads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.causal != 0, bundle, shift, w.max_items,
                                               reinterpret_cast<int*>(ws), reinterpret_cast<int*>(ws + w.prefix_off),
                                               reinterpret_cast<Item*>(ws + w.items_off), d.dev_err);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, static_cast<long long>(w.max_items) * d.heads)));
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, pairs)));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;

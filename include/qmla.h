@@ -506,7 +506,7 @@ int qmla_cache_read(const qmla_read_desc* desc, qmla_stream_t stream);
  *   cu_q, cu_kv     [batch + 1] int32 offsets, not decreasing. A sequence whose offsets
  *                   decrease, are negative or lie beyond n_q / n_kv is left out
  *                   (QMLA_DEVERR_BAD_OFFSETS)
- *   out             [n_q, heads, 128] bf16, contiguous, 16-byte aligned
+ *   out             [n_q, heads, 128] bf16, contiguous, 32-byte aligned
  *   lse             [n_q, heads] float32, contiguous, or NULL
  *                   Rows that belong to no sequence are left as they were
  *   workspace       >= qmla_prefill_workspace_bytes(batch, n_q) bytes, 256-byte aligned,

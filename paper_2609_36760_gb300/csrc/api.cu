@@ -450,7 +450,7 @@ int qmla_mla_prefill(const qmla_prefill_desc* d, qmla_stream_t stream) {
   if (d->q == nullptr || d->cu_q == nullptr || d->cu_kv == nullptr || d->out == nullptr || d->workspace == nullptr ||
       (d->n_kv > 0 && (d->k == nullptr || d->v == nullptr || d->k_pe == nullptr)))
     return QMLA_ERR_INVALID_ARG;
-  if (!aligned(d->q, 16) || !aligned(d->out, 16) || !aligned(d->cu_q, 4) || !aligned(d->cu_kv, 4) ||
+  if (!aligned(d->q, 16) || !aligned(d->out, 32) || !aligned(d->cu_q, 4) || !aligned(d->cu_kv, 4) ||
       !aligned(d->lse, 4) || !aligned(d->workspace, 256) ||
       (d->n_kv > 0 && (!aligned(d->k, 16) || !aligned(d->v, 16) || !aligned(d->k_pe, 16))))
     return QMLA_ERR_INVALID_ARG;

@@ -10,9 +10,14 @@
 // sequence's last rows) has its keys dealt to the two in turn instead: both hold
 // the same rows, every other key step each, and are merged at the end.
 //
-//   warps 0..3 / 4..7   softmax of tile 0 / 1, a query row per thread; epilogue
-//   warp 8              one thread that issues every MMA
-//   warp 9              draws the pairs; TMA loads of queries, keys and values
+//   warps 0..3 / 4..7   softmax of tile 0 / 1, a query row per thread
+//   warps 8..11         epilogue of both tiles
+//   warps 12, 14        one thread each, which issues tile 0's / tile 1's MMAs
+//   warp 13             draws the pairs; TMA loads of queries, keys and values
+//
+// The roles run through the pairs without a stop between them: a pair's first QK and
+// softmax run while the O of the one before is read out, and only its first PV waits
+// for that (o_free).
 //
 // Shared memory: the queries (2 x 3 chunks of 128 rows x 64 channels, 96 KB) and a
 // ring of eight 16 KB slots for keys (three slots per 128 tokens: two content
@@ -46,10 +51,10 @@ constexpr int kQChunks = 3, kKChunks = 3, kVSlots = 2;
 constexpr int kRing = 8;
 constexpr int kInFlight = 3;  // entries (a step's keys or values) that the ring holds at once
 constexpr int kSoftWarps = 8;
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
-constexpr int kThreads = 12 * 32;  // (two warps leave at once: registers are split by groups of four)
-// 168 registers a thread at launch: 2 x 208 + 88 = 3 x 168.
-constexpr int kSoftRegs = 208, kOtherRegs = 88;
+constexpr int kEpiWarp = 8, kMmaWarp = 12, kLoadWarp = 13;
+constexpr int kThreads = 16 * 32;  // (the last warp leaves at once: registers are split by groups of four)
+// 128 registers a thread at launch: 2 x 176 + 80 + 80 = 4 x 128.
+constexpr int kSoftRegs = 176, kEpiRegs = 80, kOtherRegs = 80;
 constexpr int kRingOff = 2 * kQChunks * kSlotBytes;
 constexpr int kCtlOff = kRingOff + kRing * kSlotBytes;
 constexpr uint32_t kColO = 256;  // O0; O1 128 columns on
@@ -57,20 +62,20 @@ constexpr uint64_t kLimitNs = 2000000000ull;  // of every wait
 constexpr float kRaise = 8.0f;                // log2 of the growth that raises a reference
 
 // Wait sites in the error word (bits 8 ..), after the decode's.
-enum : uint32_t { kSiteLoad = 10, kSiteMma, kSiteSoftmax, kSiteEnd };
+enum : uint32_t { kSiteLoad = 10, kSiteMma, kSiteSoftmax, kSiteEpilogue, kSiteEnd };
 
 struct Ctl {
   uint64_t q_full[2], q_free[2];
   uint64_t full[4], freed[4];  // of entry e: [e & 3]
   uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t l_full[2], o_free[2];  // a tile's (m, l) are in `sums`; they and O have been read
   uint64_t sched_full[2], sched_free[2];
-  uint64_t x_ready, x_done;  // tile 1's share of a one-tile item is there / has been read
   uint64_t tail, fin;
   uint32_t tmem_base, abort;
   int4 work[2][3];
-  float2 share[kTile];  // (m, l) of tile 1's rows
+  float2 sums[2][kTile];  // (m, l) of the tiles' rows
 };
-constexpr int kSmem = kCtlOff + static_cast<int>(sizeof(Ctl)) + 1024;  // (the base is moved to a multiple of 1024)
+constexpr int kSmem = kCtlOff + static_cast<int>(sizeof(Ctl));
 static_assert(kSmem <= 232448, "shared memory of a CTA");
 
 // Two tiles of one sequence: rows q_row .. of q, `rows` of them (at most 256); keys
@@ -232,8 +237,9 @@ __device__ __forceinline__ void give_up(Ctl& c, uint32_t* dev_err, uint32_t site
   report(dev_err, QMLA_DEVERR_TIMEOUT | (0x100u << site));
   *reinterpret_cast<volatile uint32_t*>(&c.abort) = 1u;
 }
-// One thread's bounded wait.
+// One thread's bounded wait. (The clock is read only after a first wait of up to 100 us.)
 __device__ __forceinline__ bool wait1(uint64_t* bar, uint32_t parity, Ctl& c, uint32_t site, uint32_t* dev_err) {
+  if (mbar_try_wait(bar, parity & 1u)) return true;
   const int r = mbar_wait(bar, parity & 1u, kLimitNs, &c.abort);
   if (r == 0) give_up(c, dev_err, site);
   return r == 1;
@@ -244,7 +250,7 @@ __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl& c
 }
 
 // The pair at hand, k-th of this CTA: read from shared memory, where the load warp
-// leaves it. Called by whole warps (LANES) and by the MMA thread.
+// leaves it. For whole warps (LANES) and single threads.
 template <bool LANES>
 __device__ __forceinline__ bool next_pair(Ctl& c, uint32_t k, Item& it, uint32_t site, uint32_t* dev_err) {
   uint64_t* bar = &c.sched_full[k & 1u];
@@ -334,28 +340,34 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
     }
     en.next(kVSlots);
   };
+  const int4* list = reinterpret_cast<const int4*>(p.items);
   const int pairs = p.count[0] * p.heads;
+  // The next pair: pair c for the CTA's first, then whichever is next. It is drawn a
+  // few loads before it is needed, in two steps, each a round trip to L2 (both at the
+  // end of a pair: 1.5 us in which nothing was loaded).
+  int at = static_cast<int>(blockIdx.x);
+  int4 place = make_int4(0, 1, 0, 0);  // the bundle of pair `at`: {first item, length, ...}
+  auto draw = [&]() {
+    if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
+  };
+  auto look_up = [&]() {
+    at = __shfl_sync(0xffffffffu, at, 0);
+    if (at < pairs) place = list[at / p.heads * 3 + 2];
+  };
+  look_up();
   for (uint32_t k = 0; ok; ++k) {
-    // Draw a pair: pair c for the CTA's first, then whichever is next.
     int4 w[3];
-    if (k >= 2 && !(ok = wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err))) break;
-    int at = static_cast<int>(blockIdx.x);
-    if (k > 0) {
-      if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
-      at = __shfl_sync(0xffffffffu, at, 0);
-    }
     w[0] = w[1] = make_int4(0, 0, 0, 0);
     w[2] = make_int4(0, 0, -1, 0);
     if (at < pairs) {
-      const int4* list = reinterpret_cast<const int4*>(p.items);
-      const int4 b = list[at / p.heads * 3 + 2];
-      const int rem = at - b.x * p.heads, head = rem / b.y;
-      const int i = b.x + rem - head * b.y;
+      const int rem = at - place.x * p.heads, head = rem / place.y;
+      const int i = place.x + rem - head * place.y;
       w[0] = list[i * 3];
       w[1] = list[i * 3 + 1];
       w[2] = list[i * 3 + 2];
       w[2].z = head;
     }
+    if (k >= 2 && !(ok = wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err))) break;
     it = Item{w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w, w[2].x, w[2].y, w[2].z, w[2].w};
     if (lane == 0) {
       for (int x = 0; x < 3; ++x) ctl.work[k & 1u][x] = w[x];
@@ -365,14 +377,21 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
     // In the order in which mma_role uses them up.
     const int n = max(it.n0, it.n1);
     if (it.n0 > 0) load_q(0);
+    if (n <= 2) draw();
+    if (n <= 1) look_up();
     if (it.dealt != 0) {
-      if (ok) load_k(0);
-      for (int j = 0; ok && j < n; ++j) {
-        if (j + 1 < n) load_k(j + 1);
-        if (ok) load_v(j);
+      for (int j = -2; ok && j < n; j += 2) {
+        if (n > 2 && (j == n - 4 || j == n - 3)) draw();
+        if (j == n - 2 || j == n - 1) look_up();
+        for (int i = 0; i < 2; ++i)
+          if (ok && j >= 0 && j + i < n) load_v(j + i);
+        for (int i = 2; i < 4; ++i)
+          if (ok && j + i < n) load_k(j + i);
       }
     } else {
       for (int j = 0; ok && j < n; ++j) {
+        if (n > 2 && j == n - 2) draw();
+        if (n > 1 && j == n - 1) look_up();
         load_k(j);
         if (ok && j == 0 && it.n1 > 0) load_q(1);
         if (ok) load_v(j);
@@ -389,103 +408,98 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
       give_up(ctl, p.dev_err, kSiteEnd);
 }
 
-// One thread.
-__device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32_t tmem) {
+// Tile i's MMAs, from one thread. What a thread does around them (waits, commits of 70
+// cycles, addresses: about 650 cycles per step) is more than the tensor core's queue
+// covers; with a thread for each tile it falls into the other's MMAs.
+__device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32_t tmem, int i) {
   constexpr uint32_t kIdQK = idesc_bf16_f32(kTile, kTile, false, false);
   constexpr uint32_t kIdPV = idesc_bf16_f32(kTile, kDv, false, true);
-  const uint64_t q0 = smem_desc(smem, 16, 1024, SWZ_128B);
-  const uint64_t r_k = smem_desc(smem + kRingOff, 16, 1024, SWZ_128B);
-  const uint64_t r_v = smem_desc(smem + kRingOff, 8192, 1024, SWZ_128B);
+  // Low words of the descriptors of the first chunks; a slot is 1,024 units on.
+  constexpr uint32_t kSlotUnits = kSlotBytes >> 4;
+  const uint32_t hi = static_cast<uint32_t>(smem_desc(0, 16, 1024, SWZ_128B) >> 32);
+  const uint32_t lo_q = static_cast<uint32_t>(smem_desc(smem, 16, 1024, SWZ_128B));
+  const uint32_t lo_k = static_cast<uint32_t>(smem_desc(smem + kRingOff, 16, 1024, SWZ_128B));
+  const uint32_t lo_v = static_cast<uint32_t>(smem_desc(smem + kRingOff, 8192, 1024, SWZ_128B));
+  const uint32_t t_s = tmem + i * 128, t_o = tmem + kColO + i * 128;
   Entry en;
-  uint32_t nq[2] = {0, 0}, np[2] = {0, 0};
+  uint32_t nq[2] = {0, 0}, np = 0, no = 0;
   bool ok = true;
-  // S_i = Q (tile q of shared memory) K^T
-  auto qk = [&](int i, int q, const Entry& k) {
+  auto wait = [&](uint64_t* bar, uint32_t phase) { return ok = wait1(bar, phase, ctl, kSiteMma, p.dev_err); };
+  // An entry of the other tile's: given back by this one as soon as it is there.
+  auto skip = [&](uint32_t slots) {
+    uint64_t* bar = &ctl.freed[en.e & 3u];
+    if (!wait(&ctl.full[en.e & 3u], en.e >> 2)) return;
+    mbar_arrive_if(1u, bar);
+    en.next(slots);
+  };
+  // S = Q (tile q of shared memory) K^T
+  auto qk = [&](int q, bool last) {
+    if (!wait(&ctl.full[en.e & 3u], en.e >> 2)) return;
 #pragma unroll
-    for (int c = 0; c < kKChunks; ++c) {
-      const uint64_t a = q0 + ((q * kQChunks + c) * kSlotBytes >> 4);
-      const uint64_t b = r_k + (((k.slot + c) & 7u) * kSlotBytes >> 4);
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-        umma_f16_ss(tmem + i * 128, a + (kk * 32 >> 4), b + (kk * 32 >> 4), kIdQK, (c | kk) != 0 ? 1u : 0u);
-    }
+    for (int c = 0; c < kKChunks; ++c)
+      umma_f16_ss_x4(t_s, lo_q + (q * kQChunks + c) * kSlotUnits, lo_k + ((en.slot + c) & 7u) * kSlotUnits, hi, kIdQK,
+                     c != 0 ? 1u : 0u);
     umma_commit(&ctl.s_full[i]);
+    umma_commit(&ctl.freed[en.e & 3u]);
+    if (last) umma_commit(&ctl.q_free[q]);
+    en.next(kKChunks);
   };
-  // O_i (+)= P_i V
-  auto pv = [&](int i, const Entry& v, bool first) {
+  // O (+)= P V
+  auto pv = [&](bool first, bool last) {
+    if (!wait(&ctl.full[en.e & 3u], en.e >> 2)) return;
+    if (first && no > 0 && !wait(&ctl.o_free[i], no - 1)) return;  // (the pair before's has been read)
+    if (!wait(&ctl.p_full[i], np)) return;
+    ++np;
+    tc_fence_after();
 #pragma unroll
-    for (int h = 0; h < kVSlots; ++h) {
-      const uint64_t b = r_v + (((v.slot + h) & 7u) * kSlotBytes >> 4);
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-        umma_f16_ts(tmem + kColO + i * 128, tmem + i * 128 + (h * 4 + kk) * 8, b + (kk * 2048 >> 4), kIdPV,
-                    first && (h | kk) == 0 ? 0u : 1u);
+    for (int h = 0; h < kVSlots; ++h)
+      umma_f16_ts_x4(t_o, t_s + h * 32, lo_v + ((en.slot + h) & 7u) * kSlotUnits, hi, kIdPV, first && h == 0 ? 0u : 1u);
+    if (last) {
+      umma_commit(&ctl.o_full[i]);
+      ++no;
     }
+    umma_commit(&ctl.freed[en.e & 3u]);
+    en.next(kVSlots);
   };
-  auto full = [&](const Entry& x) { return ok = wait1(&ctl.full[x.e & 3u], x.e >> 2, ctl, kSiteMma, p.dev_err); };
-  auto query = [&](int q) { return ok = wait1(&ctl.q_full[q], nq[q]++, ctl, kSiteMma, p.dev_err); };
-  auto weights = [&](int i) { return ok = wait1(&ctl.p_full[i], np[i]++, ctl, kSiteMma, p.dev_err); };
   Item it;
   for (uint32_t pair = 0; ok && next_pair<false>(ctl, pair, it, kSiteMma, p.dev_err); ++pair) {
-    const int n[2] = {it.n0, it.n1}, nmax = max(it.n0, it.n1);
-    if (nmax == 0) continue;
+    // Entries: K0, V0, K1, V1, .., all for both tiles; dealt: K0, K1, V0, V1, K2, K3, ..,
+    // the even ones tile 0's and the odd ones tile 1's. Query tile 0 is given back by
+    // both threads, by one that does not use it once an entry of the pair is there (so
+    // that the query before it has been given back).
     if (it.dealt != 0) {
-      // Key steps u = 0, 2, .. are tile 0's, 1, 3, .. tile 1's. Entries: K0, K1, V0, K2, V1, ..
-      if (!query(0)) break;
-      Entry v = en;
-      for (int u = -2; ok && u < nmax; ++u) {
-        const int i = u & 1;
-        if (u >= 0) {
-          v = en;
-          if (!full(v) || !weights(i)) break;
-          tc_fence_after();
-          // (a step's values lie behind the next step's keys, but for the last)
-          pv(i, v, u < 2);
-          umma_commit(&ctl.freed[v.e & 3u]);
-          if (u + 2 >= nmax) umma_commit(&ctl.o_full[i]);
-          en.next(kVSlots);
-        }
-        if (u + 2 < nmax) {
-          if (!full(en)) break;
-          tc_fence_after();
-          qk(i, 0, en);
-          umma_commit(&ctl.freed[en.e & 3u]);
-          if (u + 3 == nmax) umma_commit(&ctl.q_free[0]);
-          en.next(kKChunks);
+      // (both tiles work on the rows of query tile 0, which the last QK gives back)
+      if (it.n0 > 0 && !wait(&ctl.q_full[0], nq[0]++)) break;
+      for (int u = 0; ok && u < it.n0; u += 2) {
+        const bool two = u + 1 < it.n0;
+        if (i == 0) {
+          qk(0, u + 2 >= it.n0);
+          if (ok && two) skip(kKChunks);
+          if (ok) pv(u == 0, u + 2 >= it.n0);
+          if (ok && two) skip(kVSlots);
+        } else {
+          skip(kKChunks);
+          if (ok && two) qk(0, u + 3 >= it.n0);
+          if (ok) skip(kVSlots);
+          if (ok && two) pv(u == 0, u + 3 >= it.n0);
         }
       }
       continue;
     }
-    Entry k = en;  // keys of step j + 1
-    for (int j = -1; ok && j < nmax; ++j) {
-      // step j: PV of keys j and QK of keys j + 1, tile by tile
-      Entry v = k;  // values of step j, before those keys
-      if (j >= 0) k.next(kVSlots);
-      bool k_here = false, v_here = false;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (j >= 0 && j < n[i]) {
-          if (!v_here && !full(v)) break;
-          v_here = true;
-          if (!weights(i)) break;
-          tc_fence_after();
-          pv(i, v, j == 0);
-          if (j + 1 == n[i]) umma_commit(&ctl.o_full[i]);
-        }
-        if (i == 1 && v_here) umma_commit(&ctl.freed[v.e & 3u]);
-        if (j + 1 < n[i]) {
-          if (j < 0 && !query(i)) break;
-          if (!k_here && !full(k)) break;
-          k_here = true;
-          tc_fence_after();
-          qk(i, i, k);
-          if (j + 2 == n[i]) umma_commit(&ctl.q_free[i]);
-        }
-        if (i == 1 && k_here) umma_commit(&ctl.freed[k.e & 3u]);
-      }
-      if (j + 1 < nmax) k.next(kKChunks);
+    const int n = i == 0 ? it.n0 : it.n1, all = max(it.n0, it.n1);
+    if (n > 0 && !wait(&ctl.q_full[i], nq[i])) break;
+    nq[0] += it.n0 > 0 ? 1u : 0u;
+    nq[1] += it.n1 > 0 ? 1u : 0u;
+    for (int j = 0; ok && j < n; ++j) {
+      qk(i, j + 1 == n);
+      if (i == 1 && j == 0 && it.n0 > 0) mbar_arrive_if(1u, &ctl.q_free[0]);
+      if (ok) pv(j == 0, j + 1 == n);
     }
-    en = k;
+    for (int j = n; ok && j < all; ++j) {
+      skip(kKChunks);
+      if (i == 1 && j == 0 && it.n0 > 0) mbar_arrive_if(1u, &ctl.q_free[0]);
+      if (ok) skip(kVSlots);
+    }
   }
   // Every MMA must have landed before TMEM and shared memory are released.
   umma_commit(&ctl.fin);
@@ -504,12 +518,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return y;
 }
 
-// Softmax and epilogue of tile i, a query row per thread.
+// Softmax of tile i, a query row per thread.
 __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int i, int warp, int lane) {
   const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
   const uint32_t t_s = tmem + lanes + i * 128, t_o = tmem + lanes + kColO + i * 128;
   const int row_in = (warp & 3) * 32 + lane;  // of the tile
-  uint32_t ns = 0, no = 0, nx = 0;
+  uint32_t ns = 0, no = 0;
   Item it;
   for (uint32_t pair = 0; next_pair<true>(ctl, pair, it, kSiteSoftmax, p.dev_err); ++pair) {
     const bool dealt = it.dealt != 0;
@@ -584,71 +598,96 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
       mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.p_full[i]);
     }
     if (n > 0) {
-      if (!wait_warp(&ctl.o_full[i], no, ctl, kSiteSoftmax, p.dev_err)) return;
+      if (no > 0 && !wait_warp(&ctl.o_free[i], no - 1, ctl, kSiteSoftmax, p.dev_err)) return;
       ++no;
-      tc_fence_after();
-    }
-    float mine = 1.0f, theirs = 0.0f;  // weights of this tile's O and, dealt, of tile 1's
-    if (dealt) {
-      if (i == 1) {
-        // Leaves its sums and goes on once tile 0 has read them and O1.
-        ctl.share[row_in] = make_float2(m, l);
-        tc_fence_before();
-        __syncwarp();
-        mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.x_ready);
-        if (!wait_warp(&ctl.x_done, nx, ctl, kSiteSoftmax, p.dev_err)) return;
-        ++nx;
-        tc_fence_after();
-        continue;
-      }
-      if (!wait_warp(&ctl.x_ready, nx, ctl, kSiteSoftmax, p.dev_err)) return;
-      ++nx;
-      tc_fence_after();
-      const float2 other = ctl.share[row_in];
-      const float both = fmaxf(m, other.x);
-      const float ref = both == -INFINITY ? 0.0f : both;
-      mine = ex2(m - ref);
-      theirs = ex2(other.x - ref);
-      l = l * mine + other.y * theirs;
-      m = both;
-    }
-    const bool write = row < it.rows;
-    const bool none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
-    const float inv = 1.0f / l;
-    const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + it.head;
-    if (write && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
-    uint4* dst = reinterpret_cast<uint4*>(p.out + at * kDv);
-    mine *= inv;
-    theirs *= inv;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      uint32_t o[32];
-      if (n > 0) {
-        tmem_ld32(t_o + 32 * c, o);
-        tmem_ld_wait();
-#pragma unroll
-        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * mine);
-      }
-      if (dealt) {
-        uint32_t o1[32];
-        tmem_ld32(t_o + 128 + 32 * c, o1);
-        tmem_ld_wait();
-#pragma unroll
-        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(fmaf(__uint_as_float(o1[x]), theirs, __uint_as_float(o[x])));
-      }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        uint32_t w[4];
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          w[y] = none ? 0u : pack_bf16(__uint_as_float(o[8 * x + 2 * y]), __uint_as_float(o[8 * x + 2 * y + 1]));
-        if (write) dst[4 * c + x] = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-    tc_fence_before();
-    if (dealt) {
+      ctl.sums[i][row_in] = make_float2(m, l);
       __syncwarp();
-      mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.x_done);
+      mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.l_full[i]);
+    }
+  }
+}
+
+// 32 bytes of a row.
+__device__ __forceinline__ void st_v8(void* dst, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+// O / l and the log-sum-exp of both tiles, a query row per thread.
+__device__ void epilogue_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int warp, int lane) {
+  const uint32_t t_o = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kColO;
+  const int row_in = (warp & 3) * 32 + lane;
+  uint32_t no[2] = {0, 0};
+  Item it;
+  auto ready = [&](int i) {
+    if (!wait_warp(&ctl.l_full[i], no[i], ctl, kSiteEpilogue, p.dev_err)) return false;
+    if (!wait_warp(&ctl.o_full[i], no[i], ctl, kSiteEpilogue, p.dev_err)) return false;
+    ++no[i];
+    return true;
+  };
+  for (uint32_t pair = 0; next_pair<true>(ctl, pair, it, kSiteEpilogue, p.dev_err); ++pair) {
+    for (int i = 0; i < 2; ++i) {
+      const int row = i * kTile + row_in;
+      if (i * kTile >= it.rows) break;
+      const int n = i == 0 ? it.n0 : it.n1;
+      float m = -INFINITY, l = 0.0f, mine = 0.0f, theirs = 0.0f;
+      if (n > 0) {
+        if (!ready(i)) return;
+        if (it.dealt != 0 && !ready(1)) return;
+        tc_fence_after();
+        const float2 a = ctl.sums[i][row_in];
+        m = a.x, l = a.y, mine = 1.0f;
+        if (it.dealt != 0) {
+          const float2 c = ctl.sums[1][row_in];
+          m = fmaxf(a.x, c.x);
+          const float ref = m == -INFINITY ? 0.0f : m;
+          mine = ex2(a.x - ref);
+          theirs = ex2(c.x - ref);
+          l = a.y * mine + c.y * theirs;
+        }
+        const float inv = 1.0f / l;  // (l = 0, a row that sees no key: not used)
+        mine *= inv;
+        theirs *= inv;
+      }
+      const bool write = row < it.rows;
+      const bool none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
+      const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + it.head;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t o[32], w[16];
+        if (n > 0) {
+          tmem_ld32(t_o + i * 128 + 32 * c, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * mine);
+          if (it.dealt != 0) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              uint32_t e[8];
+              tmem_ld(t_o + 128 + 32 * c + 8 * y, e);
+              tmem_ld_wait();
+#pragma unroll
+              for (int x = 0; x < 8; ++x)
+                o[8 * y + x] = __float_as_uint(fmaf(__uint_as_float(e[x]), theirs, __uint_as_float(o[8 * y + x])));
+            }
+          }
+          if (c == 3) {
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[i]);
+            if (it.dealt != 0) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[1]);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          w[x] = none ? 0u : pack_bf16(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
+        if (write) {
+          st_v8(p.out + at * kDv + 32 * c, w);
+          st_v8(p.out + at * kDv + 32 * c + 16, w + 8);
+        }
+      }
+      if (write && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
     }
   }
 }
@@ -657,30 +696,29 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefill_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
                    const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap tpe,
                    const PrefillParams p) {
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  extern __shared__ __align__(1024) uint8_t sm[];
   Ctl& ctl = *reinterpret_cast<Ctl*>(sm + kCtlOff);
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&ctl.q_full[i], 1);
-      mbar_init(&ctl.q_free[i], 1);
+      mbar_init(&ctl.q_free[i], i == 0 ? 2 : 1);  // (query tile 0 can serve both tiles)
       mbar_init(&ctl.s_full[i], 1);
       mbar_init(&ctl.p_full[i], 4);
       mbar_init(&ctl.o_full[i], 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&ctl.full[i], 1);
-      mbar_init(&ctl.freed[i], 1);
+      mbar_init(&ctl.freed[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&ctl.sched_full[i], 1);
-      mbar_init(&ctl.sched_free[i], kSoftWarps + 1);
+      mbar_init(&ctl.sched_free[i], kSoftWarps + 4 + 2);
+      mbar_init(&ctl.l_full[i], 4);
+      mbar_init(&ctl.o_free[i], 4);
     }
-    mbar_init(&ctl.x_ready, 4);
-    mbar_init(&ctl.x_done, 4);
     mbar_init(&ctl.tail, 1);
-    mbar_init(&ctl.fin, 1);
+    mbar_init(&ctl.fin, 2);
     ctl.abort = 0u;
     fence_mbar_init();
   }
@@ -696,14 +734,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     softmax_role(p, ctl, tmem, warp >> 2, warp, lane);
+  } else if (warp < kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kEpiRegs));
+    epilogue_role(p, ctl, tmem, warp - kEpiWarp, lane);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kLoadWarp) {
       load_role(p, tq, tk, tv, tpe, sm, ctl, lane);
-    } else if (warp != kMmaWarp) {
+    } else if (warp == kLoadWarp + 2) {
       asm volatile("exit;");
     } else if (elect_one()) {
-      mma_role(p, smem_u32(sm), ctl, tmem);
+      mma_role(p, smem_u32(sm), ctl, tmem, warp == kMmaWarp ? 0 : 1);
     } else {
       asm volatile("exit;");
     }

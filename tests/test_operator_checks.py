@@ -88,7 +88,7 @@ def prefill_desc(**kw):
     {"v_head_stride": 129}, {"k_pe": None}, {"k_pe": FAKE + 8}, {"k_pe_stride": 0}, {"n_q": -1}, {"n_kv": -1},
     {"n_q": (1 << 28) + 1}, {"n_kv": (1 << 28) + 1}, {"heads": 0}, {"heads": 1025}, {"batch": 0}, {"batch": 65537},
     {"cu_q": None}, {"cu_kv": None}, {"cu_q": FAKE + 2}, {"causal": 2}, {"softmax_scale": 0.0},
-    {"softmax_scale": float("nan")}, {"softmax_scale": float("inf")}, {"out": None}, {"out": FAKE + 8},
+    {"softmax_scale": float("nan")}, {"softmax_scale": float("inf")}, {"out": None}, {"out": FAKE + 8}, {"out": FAKE + 16},
     {"lse": FAKE + 2}, {"workspace": None}, {"workspace": FAKE + 128},
 ])
 def test_mla_prefill_refuses(L, kw):

@@ -27,9 +27,11 @@
 //
 // Mathematics: online softmax. Row r keeps a reference m and the sum l of
 // 2^(s - m) over the keys seen; O accumulates P V with P = RN_bf16(2^(s - m)). m is
-// raised, and O and l rescaled, only when a score exceeds it by more than 2^8: the
-// weights then stay below 2^8, which fp32 sums and bf16 weights hold as well as
-// weights below one.
+// raised, and O and l rescaled, only when a score exceeds it by more than 2^16: the
+// weights then stay below 2^16, which fp32 sums and bf16 weights, being floating
+// point, hold as well as weights below one. So a step's weights are computed with the
+// reference as it is while its maximum is taken beside them, and again in the rare
+// case that it was too low.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -59,7 +61,7 @@ constexpr int kRingOff = 2 * kQChunks * kSlotBytes;
 constexpr int kCtlOff = kRingOff + kRing * kSlotBytes;
 constexpr uint32_t kColO = 256;  // O0; O1 128 columns on
 constexpr uint64_t kLimitNs = 2000000000ull;  // of every wait
-constexpr float kRaise = 8.0f;                // log2 of the growth that raises a reference
+constexpr float kRaise = 16.0f;               // log2 of the growth that raises a reference
 
 // Wait sites in the error word (bits 8 ..), after the decode's.
 enum : uint32_t { kSiteLoad = 10, kSiteMma, kSiteSoftmax, kSiteEpilogue, kSiteEnd };
@@ -67,11 +69,12 @@ enum : uint32_t { kSiteLoad = 10, kSiteMma, kSiteSoftmax, kSiteEpilogue, kSiteEn
 struct Ctl {
   uint64_t q_full[2], q_free[2];
   uint64_t full[4], freed[4];  // of entry e: [e & 3]
-  uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t s_full[2], p_full[2][2], o_full[2];  // p_full: of the halves, 64 keys each
   uint64_t l_full[2], o_free[2];  // a tile's (m, l) are in `sums`; they and O have been read
   uint64_t sched_full[2], sched_free[2];
   uint64_t tail, fin;
   uint32_t tmem_base, abort;
+  int turn;  // 1: a tile's MMAs are being issued
   int4 work[2][3];
   float2 sums[2][kTile];  // (m, l) of the tiles' rows
 };
@@ -425,21 +428,53 @@ __device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32
   uint32_t nq[2] = {0, 0}, np = 0, no = 0;
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t phase) { return ok = wait1(bar, phase, ctl, kSiteMma, p.dev_err); };
+  // One tile's PV and QK are issued without the other's in between: mixed, both tiles'
+  // scores would be ready at the same time, and the tensor core would idle through
+  // both softmaxes.
+  bool mine = false;
+  auto take = [&]() {
+    if (mine) return true;
+    uint64_t t0 = 0;
+    for (uint32_t k = 0; atomicCAS(&ctl.turn, 0, 1) != 0; ++k) {
+      if (*reinterpret_cast<volatile uint32_t*>(&ctl.abort) != 0u) return ok = false;
+      if ((k & 1023u) != 1023u) continue;
+      const uint64_t t = globaltimer_ns();
+      if (t0 == 0) t0 = t;
+      if (t - t0 > kLimitNs) {
+        give_up(ctl, p.dev_err, kSiteMma);
+        return ok = false;
+      }
+    }
+    return mine = true;
+  };
+  auto give = [&]() {
+    if (mine) atomicExch(&ctl.turn, 0);
+    mine = false;
+  };
   // An entry of the other tile's: given back by this one as soon as it is there.
   auto skip = [&](uint32_t slots) {
-    uint64_t* bar = &ctl.freed[en.e & 3u];
-    if (!wait(&ctl.full[en.e & 3u], en.e >> 2)) return;
-    mbar_arrive_if(1u, bar);
+    uint64_t* bar = &ctl.full[en.e & 3u];
+    if (!mbar_test(bar, (en.e >> 2) & 1u)) {
+      give();
+      if (!wait(bar, en.e >> 2)) return;
+    }
+    mbar_arrive_if(1u, &ctl.freed[en.e & 3u]);
     en.next(slots);
   };
   // S = Q (tile q of shared memory) K^T
   auto qk = [&](int q, bool last) {
-    if (!wait(&ctl.full[en.e & 3u], en.e >> 2)) return;
+    uint64_t* bar = &ctl.full[en.e & 3u];
+    if (!mbar_test(bar, (en.e >> 2) & 1u)) {
+      give();  // (the keys are late)
+      if (!wait(bar, en.e >> 2)) return;
+    }
+    if (!take()) return;
 #pragma unroll
     for (int c = 0; c < kKChunks; ++c)
       umma_f16_ss_x4(t_s, lo_q + (q * kQChunks + c) * kSlotUnits, lo_k + ((en.slot + c) & 7u) * kSlotUnits, hi, kIdQK,
                      c != 0 ? 1u : 0u);
     umma_commit(&ctl.s_full[i]);
+    give();
     umma_commit(&ctl.freed[en.e & 3u]);
     if (last) umma_commit(&ctl.q_free[q]);
     en.next(kKChunks);
@@ -448,17 +483,20 @@ __device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32
   auto pv = [&](bool first, bool last) {
     if (!wait(&ctl.full[en.e & 3u], en.e >> 2)) return;
     if (first && no > 0 && !wait(&ctl.o_free[i], no - 1)) return;  // (the pair before's has been read)
-    if (!wait(&ctl.p_full[i], np)) return;
-    ++np;
-    tc_fence_after();
 #pragma unroll
-    for (int h = 0; h < kVSlots; ++h)
+    for (int h = 0; h < kVSlots; ++h) {
+      if (!wait(&ctl.p_full[i][h], np)) return;
+      if (h == 0 && !take()) return;
+      tc_fence_after();
       umma_f16_ts_x4(t_o, t_s + h * 32, lo_v + ((en.slot + h) & 7u) * kSlotUnits, hi, kIdPV, first && h == 0 ? 0u : 1u);
+    }
+    ++np;
+    umma_commit(&ctl.freed[en.e & 3u]);
     if (last) {
       umma_commit(&ctl.o_full[i]);
       ++no;
+      give();
     }
-    umma_commit(&ctl.freed[en.e & 3u]);
     en.next(kVSlots);
   };
   Item it;
@@ -501,6 +539,7 @@ __device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32
       if (ok) skip(kVSlots);
     }
   }
+  give();
   // Every MMA must have landed before TMEM and shared memory are released.
   umma_commit(&ctl.fin);
   if (mbar_wait(&ctl.fin, 0, kLimitNs, nullptr) != 1) give_up(ctl, p.dev_err, kSiteEnd);
@@ -516,6 +555,44 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
+}
+
+// The largest of 64 scores, in four chains (a single one is 64 dependent steps).
+__device__ __forceinline__ float max64(const float (&s)[64]) {
+  float t[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) t[c] = fmaxf(s[c], s[c + 4]);
+#pragma unroll
+  for (int c = 8; c < 64; c += 8)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) t[x] = max3(t[x], s[c + x], s[c + 4 + x]);
+  return fmaxf(max3(t[0], t[1], t[2]), t[3]);
+}
+
+// 64 scores of this thread's row from tensor memory, those from key `lim` on hidden
+// (lim >= 64: none).
+__device__ __forceinline__ void load_scores64(float (&s)[64], uint32_t taddr) {
+  tmem_ld32(taddr, reinterpret_cast<uint32_t*>(s));
+  tmem_ld32(taddr + 32, reinterpret_cast<uint32_t*>(s + 32));
+}
+__device__ __forceinline__ void hide64(float (&s)[64], int lim) {
+#pragma unroll
+  for (int c = 0; c < 64; ++c) s[c] = c < lim ? s[c] : -INFINITY;
+}
+
+// 2^(s scale - ref) of 64 scores as pairs of bf16, and the sum (of the unrounded ones).
+__device__ __forceinline__ float weights64(const float (&s)[64], float scale, float ref, uint32_t (&w)[32]) {
+  const uint64_t sl = f32x2(scale, scale), mm = f32x2(-ref, -ref);
+  uint64_t sum[4] = {0, 0, 0, 0};  // (pairs of zeros)
+#pragma unroll
+  for (int c = 0; c < 32; ++c) {
+    const uint64_t x = fma2(f32x2(s[2 * c], s[2 * c + 1]), sl, mm);
+    const float a = ex2(lo2(x)), b = ex2(hi2(x));
+    sum[c & 3] = add2(sum[c & 3], f32x2(a, b));
+    w[c] = pack_bf16(a, b);
+  }
+  const uint64_t t = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+  return lo2(t) + hi2(t);
 }
 
 // Softmax of tile i, a query row per thread.
@@ -536,66 +613,54 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
       if (!wait_warp(&ctl.s_full[i], ns, ctl, kSiteSoftmax, p.dev_err)) return;
       ++ns;
       tc_fence_after();
-      float s[128];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(t_s + 32 * c, reinterpret_cast<uint32_t*>(s + 32 * c));
+      float s0[64], s1[64];
+      load_scores64(s0, t_s);
+      load_scores64(s1, t_s + 64);
       tmem_ld_wait();
       const int key0 = (dealt ? 2 * j + i : j) * kTile;
-      if (vis_warp < key0 + kTile) {
-        const int lim = vis - key0;
-#pragma unroll
-        for (int c = 0; c < 128; ++c) s[c] = c < lim ? s[c] : -INFINITY;
+      const bool hide = vis_warp < key0 + kTile;
+      if (hide) {
+        hide64(s0, vis - key0);
+        hide64(s1, vis - key0 - 64);
       }
-      // (eight chains: a single one is 128 dependent steps)
-      float tops[8];
-#pragma unroll
-      for (int c = 0; c < 8; ++c) tops[c] = fmaxf(s[c], s[c + 8]);
-#pragma unroll
-      for (int c = 16; c < 128; c += 16)
-#pragma unroll
-        for (int x = 0; x < 8; ++x) tops[x] = max3(tops[x], s[c + x], s[c + 8 + x]);
-      const float top = p.scale_log2 * max3(max3(tops[0], tops[1], tops[2]), max3(tops[3], tops[4], tops[5]),
-                                            fmaxf(tops[6], tops[7]));
-      const bool raise = top > m + kRaise;  // (m = -inf: the first visible key)
-      float factor = 1.0f;
-      if (raise) {
-        factor = ex2(m - top);  // 0 where nothing has been seen yet
-        m = top;
+      const float top1 = max64(s1);
+      if (j == 0) m = p.scale_log2 * fmaxf(max64(s0), top1);
+      float ref = m == -INFINITY ? 0.0f : m;
+      // The first half's weights with the reference as it is, and the row's maximum.
+      uint32_t w[32];
+      const float top = p.scale_log2 * fmaxf(max64(s0), top1);
+      float sum = weights64(s0, p.scale_log2, ref, w);
+      const bool raise = top > m + kRaise;
+      if (__any_sync(0xffffffffu, raise)) {
+        const float factor = raise ? ex2(m - top) : 1.0f;  // (0 where nothing has been seen yet)
+        if (raise) m = ref = top;
         l *= factor;
-      }
-      if (j > 0 && __any_sync(0xffffffffu, raise)) {
         // (the scores' arrival says that PV of the keys before has completed too)
 #pragma unroll 1
-        for (int c = 0; c < 8; ++c) {
-          uint32_t o[16];
-          tmem_ld(t_o + 16 * c, o);
+        for (int c = 0; c < 16; ++c) {
+          uint32_t o[8];
+          tmem_ld(t_o + 8 * c, o);
           tmem_ld_wait();
 #pragma unroll
-          for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * factor);
-          tmem_st(t_o + 16 * c, o);
+          for (int x = 0; x < 8; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * factor);
+          tmem_st(t_o + 8 * c, o);
         }
+        load_scores64(s0, t_s);
+        tmem_ld_wait();
+        if (hide) hide64(s0, vis - key0);
+        sum = weights64(s0, p.scale_log2, ref, w);
       }
-      const float ref = m == -INFINITY ? 0.0f : m;
-      const uint64_t sl = f32x2(p.scale_log2, p.scale_log2), mm = f32x2(-ref, -ref);
-      uint64_t sum[4] = {0, 0, 0, 0};  // (pairs of zeros)
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        uint32_t w[16];
-#pragma unroll
-        for (int c = 0; c < 16; ++c) {
-          const uint64_t x = fma2(f32x2(s[32 * h + 2 * c], s[32 * h + 2 * c + 1]), sl, mm);
-          const float a = ex2(lo2(x)), b = ex2(hi2(x));
-          sum[c & 3] = add2(sum[c & 3], f32x2(a, b));
-          w[c] = pack_bf16(a, b);
-        }
-        tmem_st(t_s + 16 * h, w);
-      }
-      const uint64_t sums = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-      l += lo2(sums) + hi2(sums);
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.p_full[i]);
+      l += sum;
+      auto hand_over = [&](int h) {
+        tmem_st32(t_s + 32 * h, w);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.p_full[i][h]);
+      };
+      hand_over(0);
+      l += weights64(s1, p.scale_log2, ref, w);
+      hand_over(1);
     }
     if (n > 0) {
       if (no > 0 && !wait_warp(&ctl.o_free[i], no - 1, ctl, kSiteSoftmax, p.dev_err)) return;
@@ -704,7 +769,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&ctl.q_full[i], 1);
       mbar_init(&ctl.q_free[i], i == 0 ? 2 : 1);  // (query tile 0 can serve both tiles)
       mbar_init(&ctl.s_full[i], 1);
-      mbar_init(&ctl.p_full[i], 4);
+      for (int h = 0; h < 2; ++h) mbar_init(&ctl.p_full[i][h], 4);
       mbar_init(&ctl.o_full[i], 1);
     }
     for (int i = 0; i < 4; ++i) {
@@ -720,6 +785,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&ctl.tail, 1);
     mbar_init(&ctl.fin, 2);
     ctl.abort = 0u;
+    ctl.turn = 0;
     fence_mbar_init();
   }
   if (warp == 0) {

@@ -435,7 +435,8 @@ int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream);
 
 /*
  * Turns the RoPE part of queries by the angles of their positions, with the
- * convention, table and rounding of qmla_rope_append:
+ * convention and table of qmla_rope_append, in fp32 (a product and an FMA), rounded to
+ * bf16:
  *   q_pe_dev        [n, heads, 64] bf16, rows q_token_stride and q_head_stride elements
  *                   apart (multiples of 8, not negative), 16-byte aligned. (So it may be
  *                   the last 64 columns of a [n, heads, 192] projection output.)

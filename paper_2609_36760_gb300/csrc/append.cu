@@ -133,36 +133,54 @@ __device__ __forceinline__ void transform_rows(uint4 (&raw)[NT], const RowTransf
       load_angles(a, pos >= 0 && pos < tr.rope_len ? tr.cos_sin + static_cast<size_t>(pos) * kDr : nullptr, piece,
                   tr.interleaved);
       uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-      rotate_row(w, a, piece, tr.interleaved);
+      rotate_row<true>(w, a, piece, tr.interleaved);
       raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
   if (!tr.norm) return;
+  // Lane i of four ends up with token i's sum (two halvings, then the other four
+  // lanes); with one token per lane all eight have it.
+  const int own = piece & (NT - 1);
   if (g < 8) {
+    F2 s[NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-      F2 s = square_sum8(w);
-#pragma unroll
-      for (int off = 1; off < 8; off <<= 1)
-        s = add_f2(s, {__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off)});
-      if (piece == 0) share[g][sub + 4 * i] = make_float2(s.hi, s.lo);
+      s[i] = square_sum8(w);
     }
+    auto with = [](F2 keep, F2 send, int off) {
+      return add_f2(keep, {__shfl_xor_sync(0xffffffffu, send.hi, off), __shfl_xor_sync(0xffffffffu, send.lo, off)});
+    };
+    if constexpr (NT == 4) {
+      const bool b0 = (piece & 1) != 0, b1 = (piece & 2) != 0;
+      const F2 x = with(b0 ? s[1] : s[0], b0 ? s[0] : s[1], 1);
+      const F2 y = with(b0 ? s[3] : s[2], b0 ? s[2] : s[3], 1);
+      s[0] = with(b1 ? y : x, b1 ? x : y, 2);
+    } else {
+      s[0] = with(s[0], s[0], 1);
+      s[0] = with(s[0], s[0], 2);
+    }
+    s[0] = with(s[0], s[0], 4);
+    if (piece < NT) share[g][sub + 4 * own] = make_float2(s[0].hi, s[0].lo);
   }
   __syncthreads();
   if (g == 8) return;
-  // this lane's share: token `own` of the lane's NT, handed round by shuffles
-  const int own = piece & (NT - 1);
+  // The row's sum: four shares here, the other four in the lane four away.
   F2 sum = {0.0f, 0.0f};
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float2 v = share[k][sub + 4 * own];
-    sum = add_f2(sum, {v.x, v.y});
+  for (int k = 0; k < 4; ++k) {
+    const float2 v = share[(piece & 4) + k][sub + 4 * own];
+    sum = k == 0 ? F2{v.x, v.y} : add_f2(sum, {v.x, v.y});
+  }
+  {
+    const F2 o = {__shfl_xor_sync(0xffffffffu, sum.hi, 4), __shfl_xor_sync(0xffffffffu, sum.lo, 4)};
+    sum = (piece & 4) == 0 ? add_f2(sum, o) : add_f2(o, sum);
   }
   const F2 rs = row_rstd(sum, tr.eps);
   const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
   const uint4 gv = tr.weight != nullptr ? tr.weight[g * 8 + piece] : ones;
-  const uint32_t gw[4] = {gv.x, gv.y, gv.z, gv.w};
+  const uint64_t gw[4] = {f32x2(bf16_low(gv.x), bf16_high(gv.x)), f32x2(bf16_low(gv.y), bf16_high(gv.y)),
+                          f32x2(bf16_low(gv.z), bf16_high(gv.z)), f32x2(bf16_low(gv.w), bf16_high(gv.w))};
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int from = (lane & 24) | i;

@@ -1,13 +1,13 @@
 // Position rotation and latent normalisation of bf16 rows, as the fused cache
 // writer and the query rotation apply them.
 //
-// Both results are RN_bf16(RN_f32(exact)): the arithmetic carries the rounding
+// The writer's results are RN_bf16(RN_f32(exact)): the arithmetic carries the rounding
 // errors of its fp32 operations along (error-free transformations: T. J. Dekker,
 // Numer. Math. 18, 1971; D. E. Knuth, TAOCP 2, 4.2.2), which leaves about 2^-46
 // relative. A plain fp32 evaluation is off by up to some 2^-22, which moves one
 // bf16 value in about 2^13 and with it, now and then, the 2- or 4-bit code or the
 // scale of a whole group; this way the cache holds the same bytes whatever order
-// the sums are taken in.
+// the sums are taken in. Queries, which nothing quantises, are rotated in plain fp32.
 #pragma once
 #include <cstdint>
 
@@ -33,6 +33,18 @@ __device__ __forceinline__ F2 add_f2(F2 a, F2 b) {
   const float lo = __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo));
   const float hi = __fadd_rn(s.hi, lo);
   return {hi, __fsub_rn(lo, __fsub_rn(hi, s.hi))};
+}
+
+// The same for two values at once (the packed operations round like the others).
+struct F2x2 {
+  uint64_t hi, lo;
+};
+__device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
+  return fma2(b, f32x2(-1.0f, -1.0f), a);
+}
+__device__ __forceinline__ F2x2 two_sum2(uint64_t a, uint64_t b) {
+  const uint64_t s = add2(a, b), t = sub2(s, a);
+  return {s, add2(sub2(a, sub2(s, t)), sub2(b, t))};
 }
 
 // RN_f32(a c + b s).
@@ -63,20 +75,27 @@ __device__ __forceinline__ void load_angles(Angles& a, const float* t, int piece
   a.c[0] = c0.x, a.c[1] = c0.y, a.c[2] = c0.z, a.c[3] = c0.w, a.c[4] = c1.x, a.c[5] = c1.y, a.c[6] = c1.z, a.c[7] = c1.w;
   a.s[0] = s0.x, a.s[1] = s0.y, a.s[2] = s0.z, a.s[3] = s0.w, a.s[4] = s1.x, a.s[5] = s1.y, a.s[6] = s1.z, a.s[7] = s1.w;
 }
+// EXACT: RN_bf16(RN_f32(exact)), else one fp32 product and one FMA.
+template <bool EXACT>
+__device__ __forceinline__ float rotate_value(float a, float c, float b, float s) {
+  if constexpr (EXACT) return rotate1(a, c, b, s);
+  return __fmaf_rn(a, c, __fmul_rn(b, s));
+}
+template <bool EXACT>
 __device__ __forceinline__ void rotate_row(uint32_t (&w)[4], const Angles& a, int piece, bool interleaved) {
   if (interleaved) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float x = bf16_low(w[e]), y = bf16_high(w[e]);
-      w[e] = pack_bf16(rotate1(x, a.c[e], y, -a.s[e]), rotate1(x, a.s[e], y, a.c[e]));
+      w[e] = pack_bf16(rotate_value<EXACT>(x, a.c[e], y, -a.s[e]), rotate_value<EXACT>(x, a.s[e], y, a.c[e]));
     }
   } else {
     const float sign = piece < 4 ? -1.0f : 1.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t o = __shfl_xor_sync(0xffffffffu, w[e], 4);
-      w[e] = pack_bf16(rotate1(bf16_low(w[e]), a.c[2 * e], bf16_low(o), sign * a.s[2 * e]),
-                       rotate1(bf16_high(w[e]), a.c[2 * e + 1], bf16_high(o), sign * a.s[2 * e + 1]));
+      w[e] = pack_bf16(rotate_value<EXACT>(bf16_low(w[e]), a.c[2 * e], bf16_low(o), sign * a.s[2 * e]),
+                       rotate_value<EXACT>(bf16_high(w[e]), a.c[2 * e + 1], bf16_high(o), sign * a.s[2 * e + 1]));
     }
   }
 }
@@ -84,15 +103,14 @@ __device__ __forceinline__ void rotate_row(uint32_t (&w)[4], const Angles& a, in
 // Sum of the squares of eight bf16 values (each exact in fp32), even and odd
 // channels side by side.
 __device__ __forceinline__ F2 square_sum8(const uint32_t (&w)[4]) {
-  F2 even = {0.0f, 0.0f}, odd = {0.0f, 0.0f};
+  F2x2 sum = {0, 0};  // (pairs of zeros)
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float x = bf16_low(w[e]), y = bf16_high(w[e]);
-    const F2 a = two_sum(even.hi, __fmul_rn(x, x)), b = two_sum(odd.hi, __fmul_rn(y, y));
-    even = {a.hi, __fadd_rn(even.lo, a.lo)};
-    odd = {b.hi, __fadd_rn(odd.lo, b.lo)};
+    const uint64_t x = f32x2(bf16_low(w[e]), bf16_high(w[e]));
+    const F2x2 t = two_sum2(sum.hi, mul2(x, x));
+    sum = {t.hi, add2(sum.lo, t.lo)};
   }
-  return add_f2(even, odd);
+  return add_f2({lo2(sum.hi), lo2(sum.lo)}, {hi2(sum.hi), hi2(sum.lo)});
 }
 
 // 1 / sqrt(sum / 512 + eps), by one Newton step from an fp32 estimate whose
@@ -107,16 +125,17 @@ __device__ __forceinline__ F2 row_rstd(F2 sum, float eps) {
   return {y, __fmul_rn(0.5f, __fmul_rn(y, r))};
 }
 
-// RN_bf16(RN_f32(x w rstd)) of eight values in place (x w is exact in fp32).
-__device__ __forceinline__ float scale1(float v, F2 rstd) {
-  const F2 p = two_prod(v, rstd.hi);
-  return __fadd_rn(p.hi, __fmaf_rn(v, rstd.lo, p.lo));
-}
-__device__ __forceinline__ void scale_row(uint32_t (&w)[4], const uint32_t (&g)[4], F2 rstd) {
+// RN_bf16(RN_f32(x g rstd)) of eight values in place (x g is exact in fp32).
+__device__ __forceinline__ void scale_row(uint32_t (&w)[4], const uint64_t (&g)[4], F2 rstd) {
+  const uint64_t hi = f32x2(rstd.hi, rstd.hi), lo = f32x2(rstd.lo, rstd.lo);
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    w[e] = pack_bf16(scale1(__fmul_rn(bf16_low(w[e]), bf16_low(g[e])), rstd),
-                     scale1(__fmul_rn(bf16_high(w[e]), bf16_high(g[e])), rstd));
+  for (int e = 0; e < 4; ++e) {
+    const uint64_t v = mul2(f32x2(bf16_low(w[e]), bf16_high(w[e])), g[e]);
+    const uint64_t p = mul2(v, hi);
+    const uint64_t low = fma2(v, lo, fma2(v, hi, p ^ 0x8000000080000000ull));  // (the product's rounding error)
+    const uint64_t y = add2(p, low);
+    w[e] = pack_bf16(lo2(y), hi2(y));
+  }
 }
 
 }  // namespace qmla

@@ -136,9 +136,16 @@ void launch_read_nt(const qmla_read_desc& d, cudaStream_t stream) {
       d.max_blocks, d.seq_lens, static_cast<const uint4*>(d.prot), d.rows, static_cast<size_t>(d.row_stride), d.dev_err);
 }
 
+// Tokens from which a lane takes four.
+constexpr int kFourPerLane = 4096;
+
 template <int CB>
 void launch_read(const qmla_read_desc& d, cudaStream_t stream) {
-  launch_read_nt<CB, 1>(d, stream);
+  if (d.n >= kFourPerLane) {
+    launch_read_nt<CB, 4>(d, stream);
+  } else {
+    launch_read_nt<CB, 1>(d, stream);
+  }
 }
 
 // Rotates rows of 64 channels, `heads` of them per token: eight lanes a row, each
@@ -182,7 +189,7 @@ __global__ void __launch_bounds__(kQueryThreads) rope_query_kernel(
     }
     if (tok[i] >= 0 && !good && piece == 0 && row == tok[i] * heads) report(dev_err, QMLA_DEVERR_BAD_POSITION);
     uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-    rotate_row(w, a, piece, interleaved);
+    rotate_row<false>(w, a, piece, interleaved);
     if (tok[i] >= 0 && good)
       *reinterpret_cast<uint4*>(out + tok[i] * out_token + (row - tok[i] * heads) * out_head + piece * 8) =
           make_uint4(w[0], w[1], w[2], w[3]);

@@ -27,11 +27,9 @@
 //
 // Mathematics: online softmax. Row r keeps a reference m and the sum l of
 // 2^(s - m) over the keys seen; O accumulates P V with P = RN_bf16(2^(s - m)). m is
-// raised, and O and l rescaled, only when a score exceeds it by more than 2^16: the
-// weights then stay below 2^16, which fp32 sums and bf16 weights, being floating
-// point, hold as well as weights below one. So a step's weights are computed with the
-// reference as it is while its maximum is taken beside them, and again in the rare
-// case that it was too low.
+// raised, and O and l rescaled, only when a score exceeds it by more than 2^8: the
+// weights then stay below 2^8, which fp32 sums and bf16 weights, being floating point,
+// hold as well as weights below one.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -61,7 +59,8 @@ constexpr int kRingOff = 2 * kQChunks * kSlotBytes;
 constexpr int kCtlOff = kRingOff + kRing * kSlotBytes;
 constexpr uint32_t kColO = 256;  // O0; O1 128 columns on
 constexpr uint64_t kLimitNs = 2000000000ull;  // of every wait
-constexpr float kRaise = 16.0f;               // log2 of the growth that raises a reference
+constexpr int kAhead = 4;  // steps before the end of a pair at which the next is drawn
+constexpr float kRaise = 8.0f;  // log2 of the growth that raises a reference
 
 // Wait sites in the error word (bits 8 ..), after the decode's.
 enum : uint32_t { kSiteLoad = 10, kSiteMma, kSiteSoftmax, kSiteEpilogue, kSiteEnd };
@@ -343,33 +342,41 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
     }
     en.next(kVSlots);
   };
+  // The next pair: pair c for the CTA's first, then whichever is next. It is drawn some
+  // steps before it is needed (three round trips to L2), and what its first steps read
+  // is asked into L2: its query tiles can only be loaded once this pair's last QKs are
+  // through, and nothing else covers the way from HBM then.
   const int4* list = reinterpret_cast<const int4*>(p.items);
   const int pairs = p.count[0] * p.heads;
-  // The next pair: pair c for the CTA's first, then whichever is next. It is drawn a
-  // few loads before it is needed, in two steps, each a round trip to L2 (both at the
-  // end of a pair: 1.5 us in which nothing was loaded).
-  int at = static_cast<int>(blockIdx.x);
-  int4 place = make_int4(0, 1, 0, 0);  // the bundle of pair `at`: {first item, length, ...}
-  auto draw = [&]() {
-    if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
-  };
-  auto look_up = [&]() {
-    at = __shfl_sync(0xffffffffu, at, 0);
-    if (at < pairs) place = list[at / p.heads * 3 + 2];
-  };
-  look_up();
-  for (uint32_t k = 0; ok; ++k) {
-    int4 w[3];
+  int4 w[3];
+  auto look_up = [&](int at) {
     w[0] = w[1] = make_int4(0, 0, 0, 0);
     w[2] = make_int4(0, 0, -1, 0);
-    if (at < pairs) {
-      const int rem = at - place.x * p.heads, head = rem / place.y;
-      const int i = place.x + rem - head * place.y;
-      w[0] = list[i * 3];
-      w[1] = list[i * 3 + 1];
-      w[2] = list[i * 3 + 2];
-      w[2].z = head;
+    if (at >= pairs) return;
+    const int4 place = list[at / p.heads * 3 + 2];  // {the bundle's first item, its length, ..}
+    const int rem = at - place.x * p.heads, head = rem / place.y;
+    const int i = place.x + rem - head * place.y;
+    w[0] = list[i * 3];
+    w[1] = list[i * 3 + 1];
+    w[2] = list[i * 3 + 2];
+    w[2].z = head;
+  };
+  auto draw = [&]() {
+    int at = 0;
+    if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
+    look_up(__shfl_sync(0xffffffffu, at, 0));
+    const int head = w[2].z, n0 = w[1].z, n1 = w[1].w;
+    if (head < 0) return;
+    if (lane < 6 && (lane < 3 ? n0 : n1) > 0)
+      tma_prefetch_3d(&tq, lane % 3 * 64, head, w[0].x + lane / 3 * kTile);
+    // (the first step's keys and values, of items that start together by one of them)
+    if (max(n0, n1) > 0) {
+      if (lane >= 8 && lane < 10) tma_prefetch_3d(&tk, (lane - 8) * 64, head, w[0].z);
+      if (lane >= 12 && lane < 16) tma_prefetch_3d(&tv, (lane & 1) * 64, head, w[0].z + (lane & 2) * 32);
     }
+  };
+  look_up(static_cast<int>(blockIdx.x));
+  for (uint32_t k = 0; ok; ++k) {
     if (k >= 2 && !(ok = wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err))) break;
     it = Item{w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w, w[2].x, w[2].y, w[2].z, w[2].w};
     if (lane == 0) {
@@ -377,28 +384,17 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
     }
     mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.sched_full[k & 1u]);
     if (it.head < 0) break;
-    // In the order in which mma_role uses them up.
-    const int n = max(it.n0, it.n1);
+    // In the order in which mma_role uses them up. (The next pair is drawn behind the
+    // loads of the step kAhead before the last.)
+    const int n = max(it.n0, it.n1), when = max(n - 1 - kAhead, 0);
+    const int per = it.dealt != 0 ? 2 : 1;  // key steps in a round
+    if (n == 0) draw();
     if (it.n0 > 0) load_q(0);
-    if (n <= 2) draw();
-    if (n <= 1) look_up();
-    if (it.dealt != 0) {
-      for (int j = -2; ok && j < n; j += 2) {
-        if (n > 2 && (j == n - 4 || j == n - 3)) draw();
-        if (j == n - 2 || j == n - 1) look_up();
-        for (int i = 0; i < 2; ++i)
-          if (ok && j >= 0 && j + i < n) load_v(j + i);
-        for (int i = 2; i < 4; ++i)
-          if (ok && j + i < n) load_k(j + i);
-      }
-    } else {
-      for (int j = 0; ok && j < n; ++j) {
-        if (n > 2 && j == n - 2) draw();
-        if (n > 1 && j == n - 1) look_up();
-        load_k(j);
-        if (ok && j == 0 && it.n1 > 0) load_q(1);
-        if (ok) load_v(j);
-      }
+    for (int j = 0; ok && j < n; j += per) {
+      for (int x = 0; ok && x < per && j + x < n; ++x) load_k(j + x);
+      if (ok && j == 0 && it.n1 > 0) load_q(1);
+      for (int x = 0; ok && x < per && j + x < n; ++x) load_v(j + x);
+      if (ok && when >= j && when < j + per) draw();
     }
   }
   if (lane != 0) return;
@@ -505,38 +501,29 @@ __device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32
     // the even ones tile 0's and the odd ones tile 1's. Query tile 0 is given back by
     // both threads, by one that does not use it once an entry of the pair is there (so
     // that the query before it has been given back).
-    if (it.dealt != 0) {
-      // (both tiles work on the rows of query tile 0, which the last QK gives back)
-      if (it.n0 > 0 && !wait(&ctl.q_full[0], nq[0]++)) break;
-      for (int u = 0; ok && u < it.n0; u += 2) {
-        const bool two = u + 1 < it.n0;
-        if (i == 0) {
-          qk(0, u + 2 >= it.n0);
-          if (ok && two) skip(kKChunks);
-          if (ok) pv(u == 0, u + 2 >= it.n0);
-          if (ok && two) skip(kVSlots);
+    // (One place for each kind of entry: the roles' code has to share the SM's instruction
+    // caches.)
+    const bool dealt = it.dealt != 0;
+    const int q = dealt ? 0 : i, all = max(it.n0, it.n1);
+    const int n = dealt ? (it.n0 + 1 - i) >> 1 : (i == 0 ? it.n0 : it.n1);  // of this tile
+    const int rounds = dealt ? (all + 1) >> 1 : all;
+    if (n > 0 && !wait(&ctl.q_full[q], nq[q])) break;
+    nq[0] += it.n0 > 0 ? 1u : 0u;
+    nq[1] += !dealt && it.n1 > 0 ? 1u : 0u;
+#pragma unroll 1
+    for (int x = 0; ok && x < 2 * rounds; ++x) {
+      const int j = x >> 1;
+      const uint32_t slots = (x & 1) == 0 ? kKChunks : kVSlots;
+      if (dealt ? i == 1 : j >= n) skip(slots);
+      if (ok && j < n) {
+        if ((x & 1) == 0) {
+          qk(q, j + 1 == n);
         } else {
-          skip(kKChunks);
-          if (ok && two) qk(0, u + 3 >= it.n0);
-          if (ok) skip(kVSlots);
-          if (ok && two) pv(u == 0, u + 3 >= it.n0);
+          pv(j == 0, j + 1 == n);
         }
       }
-      continue;
-    }
-    const int n = i == 0 ? it.n0 : it.n1, all = max(it.n0, it.n1);
-    if (n > 0 && !wait(&ctl.q_full[i], nq[i])) break;
-    nq[0] += it.n0 > 0 ? 1u : 0u;
-    nq[1] += it.n1 > 0 ? 1u : 0u;
-    for (int j = 0; ok && j < n; ++j) {
-      qk(i, j + 1 == n);
-      if (i == 1 && j == 0 && it.n0 > 0) mbar_arrive_if(1u, &ctl.q_free[0]);
-      if (ok) pv(j == 0, j + 1 == n);
-    }
-    for (int j = n; ok && j < all; ++j) {
-      skip(kKChunks);
-      if (i == 1 && j == 0 && it.n0 > 0) mbar_arrive_if(1u, &ctl.q_free[0]);
-      if (ok) skip(kVSlots);
+      if (ok && dealt && i == 0 && 2 * j + 1 < all) skip(slots);
+      if (x == 0 && i == 1 && !dealt && it.n0 > 0) mbar_arrive_if(1u, &ctl.q_free[0]);
     }
   }
   give();
@@ -569,12 +556,7 @@ __device__ __forceinline__ float max64(const float (&s)[64]) {
   return fmaxf(max3(t[0], t[1], t[2]), t[3]);
 }
 
-// 64 scores of this thread's row from tensor memory, those from key `lim` on hidden
-// (lim >= 64: none).
-__device__ __forceinline__ void load_scores64(float (&s)[64], uint32_t taddr) {
-  tmem_ld32(taddr, reinterpret_cast<uint32_t*>(s));
-  tmem_ld32(taddr + 32, reinterpret_cast<uint32_t*>(s + 32));
-}
+// Hides the scores from key `lim` on (lim >= 64: none).
 __device__ __forceinline__ void hide64(float (&s)[64], int lim) {
 #pragma unroll
   for (int c = 0; c < 64; ++c) s[c] = c < lim ? s[c] : -INFINITY;
@@ -613,31 +595,28 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
       if (!wait_warp(&ctl.s_full[i], ns, ctl, kSiteSoftmax, p.dev_err)) return;
       ++ns;
       tc_fence_after();
-      float s0[64], s1[64];
-      load_scores64(s0, t_s);
-      load_scores64(s1, t_s + 64);
+      float s0[64], s1[64], t[4];
+      tmem_ld32_max(t_s, s0, t[0]);
+      tmem_ld32_max(t_s + 32, s0 + 32, t[1]);
+      tmem_ld32_max(t_s + 64, s1, t[2]);
+      tmem_ld32_max(t_s + 96, s1 + 32, t[3]);
       tmem_ld_wait();
+      float top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
       const int key0 = (dealt ? 2 * j + i : j) * kTile;
-      const bool hide = vis_warp < key0 + kTile;
-      if (hide) {
+      if (vis_warp < key0 + kTile) {
         hide64(s0, vis - key0);
         hide64(s1, vis - key0 - 64);
+        top = fmaxf(max64(s0), max64(s1));
       }
-      const float top1 = max64(s1);
-      if (j == 0) m = p.scale_log2 * fmaxf(max64(s0), top1);
-      float ref = m == -INFINITY ? 0.0f : m;
-      // The first half's weights with the reference as it is, and the row's maximum.
-      uint32_t w[32];
-      const float top = p.scale_log2 * fmaxf(max64(s0), top1);
-      float sum = weights64(s0, p.scale_log2, ref, w);
-      const bool raise = top > m + kRaise;
+      top *= p.scale_log2;
+      const bool raise = top > m + kRaise;  // (m = -inf: the first visible key)
       if (__any_sync(0xffffffffu, raise)) {
-        const float factor = raise ? ex2(m - top) : 1.0f;  // (0 where nothing has been seen yet)
-        if (raise) m = ref = top;
+        const float factor = raise ? ex2(m - top) : 1.0f;  // 0 where nothing has been seen yet
+        if (raise) m = top;
         l *= factor;
         // (the scores' arrival says that PV of the keys before has completed too)
 #pragma unroll 1
-        for (int c = 0; c < 16; ++c) {
+        for (int c = j > 0 ? 0 : 16; c < 16; ++c) {
           uint32_t o[8];
           tmem_ld(t_o + 8 * c, o);
           tmem_ld_wait();
@@ -645,12 +624,9 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
           for (int x = 0; x < 8; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * factor);
           tmem_st(t_o + 8 * c, o);
         }
-        load_scores64(s0, t_s);
-        tmem_ld_wait();
-        if (hide) hide64(s0, vis - key0);
-        sum = weights64(s0, p.scale_log2, ref, w);
       }
-      l += sum;
+      const float ref = m == -INFINITY ? 0.0f : m;
+      uint32_t w[32];
       auto hand_over = [&](int h) {
         tmem_st32(t_s + 32 * h, w);
         tmem_st_wait();
@@ -658,6 +634,7 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
         __syncwarp();
         mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.p_full[i][h]);
       };
+      l += weights64(s0, p.scale_log2, ref, w);
       hand_over(0);
       l += weights64(s1, p.scale_log2, ref, w);
       hand_over(1);
@@ -672,17 +649,28 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
   }
 }
 
-// 32 bytes of a row.
-__device__ __forceinline__ void st_v8(void* dst, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
+// w[g] of lane q of a quad becomes w[q] of lane g: four lanes with two columns of
+// each of four groups end up with a group of eight each.
+__device__ __forceinline__ void transpose_quad(uint32_t (&w)[4], int lane) {
+  const bool odd = (lane & 1) != 0, high = (lane & 2) != 0;
+#pragma unroll
+  for (int x = 0; x < 4; x += 2) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? w[x] : w[x + 1], 1);
+    (odd ? w[x] : w[x + 1]) = got;
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, high ? w[x] : w[x + 2], 2);
+    (high ? w[x] : w[x + 2]) = got;
+  }
 }
 
-// O / l and the log-sum-exp of both tiles, a query row per thread.
+// O / l and the log-sum-exp of both tiles. O is read as matrix fragments and turned
+// round within quads, so that a store writes 64 bytes side by side of each of eight
+// rows: with a row per thread it touches 32 lines, and a pair of tiles took the one
+// load-store unit some 4,000 cycles.
 __device__ void epilogue_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int warp, int lane) {
   const uint32_t t_o = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kColO;
-  const int row_in = (warp & 3) * 32 + lane;
   uint32_t no[2] = {0, 0};
   Item it;
   auto ready = [&](int i) {
@@ -692,67 +680,86 @@ __device__ void epilogue_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, i
     return true;
   };
   for (uint32_t pair = 0; next_pair<true>(ctl, pair, it, kSiteEpilogue, p.dev_err); ++pair) {
+#pragma unroll 1
     for (int i = 0; i < 2; ++i) {
-      const int row = i * kTile + row_in;
       if (i * kTile >= it.rows) break;
       const int n = i == 0 ? it.n0 : it.n1;
-      float m = -INFINITY, l = 0.0f, mine = 0.0f, theirs = 0.0f;
+      const bool dealt = it.dealt != 0;
       if (n > 0) {
         if (!ready(i)) return;
-        if (it.dealt != 0 && !ready(1)) return;
+        if (dealt && !ready(1)) return;
         tc_fence_after();
-        const float2 a = ctl.sums[i][row_in];
-        m = a.x, l = a.y, mine = 1.0f;
-        if (it.dealt != 0) {
-          const float2 c = ctl.sums[1][row_in];
+      }
+      // Row `lane` of the warp: its weights of the tiles' O, and the log-sum-exp.
+      const int row0 = i * kTile + (warp & 3) * 32;
+      float mine = 0.0f, theirs = 0.0f, lse = -INFINITY;
+      bool none = true;
+      if (n > 0) {
+        const float2 a = ctl.sums[i][(warp & 3) * 32 + lane];
+        float m = a.x, l = a.y;
+        mine = 1.0f;
+        if (dealt) {
+          const float2 c = ctl.sums[1][(warp & 3) * 32 + lane];
           m = fmaxf(a.x, c.x);
           const float ref = m == -INFINITY ? 0.0f : m;
           mine = ex2(a.x - ref);
           theirs = ex2(c.x - ref);
           l = a.y * mine + c.y * theirs;
         }
-        const float inv = 1.0f / l;  // (l = 0, a row that sees no key: not used)
+        none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
+        const float inv = 1.0f / l;
         mine *= inv;
         theirs *= inv;
+        if (!none) lse = m * 0.6931471805599453f + logf(l);
       }
-      const bool write = row < it.rows;
-      const bool none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
-      const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + it.head;
+      const uint32_t nones = __ballot_sync(0xffffffffu, none);
+      if (row0 + lane < it.rows && p.lse != nullptr)
+        p.lse[static_cast<size_t>(it.q_row + row0 + lane) * p.heads + it.head] = lse;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {  // 16 rows: r and r + 8 of them in a lane
+        const int r = 16 * half + (lane >> 2);
+        const float mine0 = __shfl_sync(0xffffffffu, mine, r), mine1 = __shfl_sync(0xffffffffu, mine, r + 8);
+        const float theirs0 = __shfl_sync(0xffffffffu, theirs, r), theirs1 = __shfl_sync(0xffffffffu, theirs, r + 8);
+        uint16_t* dst = p.out + (static_cast<size_t>(it.q_row + row0 + r) * p.heads + it.head) * kDv + (lane & 3) * 8;
+        const size_t eight = static_cast<size_t>(p.heads) * (8 * kDv);
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          uint32_t o[16], w0[4], w1[4];
+          const uint32_t at = t_o + (static_cast<uint32_t>(16 * half) << 16) + 32 * c;
+          if (n > 0) {
+            tmem_ld_frag32(at + i * 128, o);
+            tmem_ld_wait();
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t o[32], w[16];
-        if (n > 0) {
-          tmem_ld32(t_o + i * 128 + 32 * c, o);
-          tmem_ld_wait();
-#pragma unroll
-          for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * mine);
-          if (it.dealt != 0) {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              uint32_t e[8];
-              tmem_ld(t_o + 128 + 32 * c + 8 * y, e);
+            for (int x = 0; x < 16; ++x)
+              o[x] = __float_as_uint(__uint_as_float(o[x]) * ((x & 2) == 0 ? mine0 : mine1));
+            if (dealt) {
+              uint32_t e[16];
+              tmem_ld_frag32(at + 128, e);
               tmem_ld_wait();
 #pragma unroll
-              for (int x = 0; x < 8; ++x)
-                o[8 * y + x] = __float_as_uint(fmaf(__uint_as_float(e[x]), theirs, __uint_as_float(o[8 * y + x])));
+              for (int x = 0; x < 16; ++x)
+                o[x] = __float_as_uint(fmaf(__uint_as_float(e[x]), (x & 2) == 0 ? theirs0 : theirs1, __uint_as_float(o[x])));
+            }
+            if (half == 1 && c == 3) {
+              tc_fence_before();
+              __syncwarp();
+              mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[i]);
+              if (dealt) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[1]);
             }
           }
-          if (c == 3) {
-            tc_fence_before();
-            __syncwarp();
-            mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[i]);
-            if (it.dealt != 0) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[1]);
-          }
-        }
+          const bool zero0 = (nones >> r & 1u) != 0, zero1 = (nones >> (r + 8) & 1u) != 0;
 #pragma unroll
-        for (int x = 0; x < 16; ++x)
-          w[x] = none ? 0u : pack_bf16(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
-        if (write) {
-          st_v8(p.out + at * kDv + 32 * c, w);
-          st_v8(p.out + at * kDv + 32 * c + 16, w + 8);
+          for (int k = 0; k < 4; ++k) {
+            w0[k] = zero0 ? 0u : pack_bf16(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]));
+            w1[k] = zero1 ? 0u : pack_bf16(__uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+          }
+          transpose_quad(w0, lane);
+          transpose_quad(w1, lane);
+          if (row0 + r < it.rows) *reinterpret_cast<uint4*>(dst + 32 * c) = make_uint4(w0[0], w0[1], w0[2], w0[3]);
+          if (row0 + r + 8 < it.rows)
+            *reinterpret_cast<uint4*>(dst + eight + 32 * c) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
         }
       }
-      if (write && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
     }
   }
 }

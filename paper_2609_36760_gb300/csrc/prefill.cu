@@ -544,16 +544,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return y;
 }
 
-// The largest of 64 scores, in four chains (a single one is 64 dependent steps).
-__device__ __forceinline__ float max64(const float (&s)[64]) {
-  float t[4];
+// Holds the registers of a TMEM load whose values are not used until here: the load
+// writes them some time before its wait.
+__device__ __forceinline__ void keep64(float (&s)[64]) {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) t[c] = fmaxf(s[c], s[c + 4]);
-#pragma unroll
-  for (int c = 8; c < 64; c += 8)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) t[x] = max3(t[x], s[c + x], s[c + 4 + x]);
-  return fmaxf(max3(t[0], t[1], t[2]), t[3]);
+  for (int c = 0; c < 64; c += 8)
+    asm volatile("" ::"f"(s[c]), "f"(s[c + 1]), "f"(s[c + 2]), "f"(s[c + 3]), "f"(s[c + 4]), "f"(s[c + 5]), "f"(s[c + 6]),
+                 "f"(s[c + 7]));
 }
 
 // Hides the scores from key `lim` on (lim >= 64: none).
@@ -595,18 +592,34 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
       if (!wait_warp(&ctl.s_full[i], ns, ctl, kSiteSoftmax, p.dev_err)) return;
       ++ns;
       tc_fence_after();
-      float s0[64], s1[64], t[4];
-      tmem_ld32_max(t_s, s0, t[0]);
-      tmem_ld32_max(t_s + 32, s0 + 32, t[1]);
-      tmem_ld32_max(t_s + 64, s1, t[2]);
-      tmem_ld32_max(t_s + 96, s1 + 32, t[3]);
-      tmem_ld_wait();
-      float top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
+      // The row's maximum comes with the load, but for rows that hide keys of this step.
+      // (Loops stay loops and the second half of the scores is read again: unrolled,
+      // with everything in registers, the code outgrows the instruction caches that the
+      // roles share, and every second issue slot waits for instructions.)
       const int key0 = (dealt ? 2 * j + i : j) * kTile;
-      if (vis_warp < key0 + kTile) {
-        hide64(s0, vis - key0);
-        hide64(s1, vis - key0 - 64);
-        top = fmaxf(max64(s0), max64(s1));
+      const bool masked = vis_warp < key0 + kTile;
+      float s[64], top;
+      {
+        float u[64], t[4];
+        tmem_ld32_max(t_s, s, t[0]);
+        tmem_ld32_max(t_s + 32, s + 32, t[1]);
+        tmem_ld32_max(t_s + 64, u, t[2]);
+        tmem_ld32_max(t_s + 96, u + 32, t[3]);
+        tmem_ld_wait();
+        keep64(u);
+        top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
+      }
+      if (masked) {
+        top = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          float u[32];
+          tmem_ld32(t_s + 32 * c, reinterpret_cast<uint32_t*>(u));
+          tmem_ld_wait();
+          const int lim = vis - key0 - 32 * c;
+#pragma unroll
+          for (int x = 0; x < 32; ++x) top = fmaxf(top, x < lim ? u[x] : -INFINITY);
+        }
       }
       top *= p.scale_log2;
       const bool raise = top > m + kRaise;  // (m = -inf: the first visible key)
@@ -626,18 +639,22 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
         }
       }
       const float ref = m == -INFINITY ? 0.0f : m;
-      uint32_t w[32];
-      auto hand_over = [&](int h) {
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        if (masked) hide64(s, vis - key0 - 64 * h);
+        uint32_t w[32];
+        l += weights64(s, p.scale_log2, ref, w);
         tmem_st32(t_s + 32 * h, w);
+        if (h == 0) {
+          tmem_ld32(t_s + 64, reinterpret_cast<uint32_t*>(s));
+          tmem_ld32(t_s + 96, reinterpret_cast<uint32_t*>(s + 32));
+        }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.p_full[i][h]);
-      };
-      l += weights64(s0, p.scale_log2, ref, w);
-      hand_over(0);
-      l += weights64(s1, p.scale_log2, ref, w);
-      hand_over(1);
+        tmem_ld_wait();
+      }
     }
     if (n > 0) {
       if (no > 0 && !wait_warp(&ctl.o_free[i], no - 1, ctl, kSiteSoftmax, p.dev_err)) return;

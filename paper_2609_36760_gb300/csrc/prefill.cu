@@ -666,117 +666,91 @@ __device__ void softmax_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, in
   }
 }
 
-// w[g] of lane q of a quad becomes w[q] of lane g: four lanes with two columns of
-// each of four groups end up with a group of eight each.
-__device__ __forceinline__ void transpose_quad(uint32_t (&w)[4], int lane) {
-  const bool odd = (lane & 1) != 0, high = (lane & 2) != 0;
-#pragma unroll
-  for (int x = 0; x < 4; x += 2) {
-    const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? w[x] : w[x + 1], 1);
-    (odd ? w[x] : w[x + 1]) = got;
-  }
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const uint32_t got = __shfl_xor_sync(0xffffffffu, high ? w[x] : w[x + 2], 2);
-    (high ? w[x] : w[x + 2]) = got;
-  }
+// 32 bytes of a row.
+__device__ __forceinline__ void st_v8(void* dst, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
 }
 
-// O / l and the log-sum-exp of both tiles. O is read as matrix fragments and turned
-// round within quads, so that a store writes 64 bytes side by side of each of eight
-// rows: with a row per thread it touches 32 lines, and a pair of tiles took the one
-// load-store unit some 4,000 cycles.
+// O / l and the log-sum-exp of both tiles, a query row per thread.
 __device__ void epilogue_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int warp, int lane) {
   const uint32_t t_o = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kColO;
+  const int row_in = (warp & 3) * 32 + lane;
   uint32_t no[2] = {0, 0};
   Item it;
-  auto ready = [&](int i) {
-    if (!wait_warp(&ctl.l_full[i], no[i], ctl, kSiteEpilogue, p.dev_err)) return false;
-    if (!wait_warp(&ctl.o_full[i], no[i], ctl, kSiteEpilogue, p.dev_err)) return false;
-    ++no[i];
-    return true;
-  };
   for (uint32_t pair = 0; next_pair<true>(ctl, pair, it, kSiteEpilogue, p.dev_err); ++pair) {
+    const bool dealt = it.dealt != 0;
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       if (i * kTile >= it.rows) break;
-      const int n = i == 0 ? it.n0 : it.n1;
-      const bool dealt = it.dealt != 0;
+      const int n = i == 0 ? it.n0 : it.n1, row = i * kTile + row_in;
+      float m = -INFINITY, l = 0.0f, mine = 0.0f, theirs = 0.0f;
       if (n > 0) {
-        if (!ready(i)) return;
-        if (dealt && !ready(1)) return;
+        // (dealt: tile 1's as well)
+#pragma unroll 1
+        for (int x = i; x <= (dealt ? 1 : i); ++x) {
+          if (!wait_warp(&ctl.l_full[x], no[x], ctl, kSiteEpilogue, p.dev_err)) return;
+          if (!wait_warp(&ctl.o_full[x], no[x], ctl, kSiteEpilogue, p.dev_err)) return;
+          ++no[x];
+        }
         tc_fence_after();
-      }
-      // Row `lane` of the warp: its weights of the tiles' O, and the log-sum-exp.
-      const int row0 = i * kTile + (warp & 3) * 32;
-      float mine = 0.0f, theirs = 0.0f, lse = -INFINITY;
-      bool none = true;
-      if (n > 0) {
-        const float2 a = ctl.sums[i][(warp & 3) * 32 + lane];
-        float m = a.x, l = a.y;
-        mine = 1.0f;
+        const float2 a = ctl.sums[i][row_in];
+        m = a.x, l = a.y, mine = 1.0f;
         if (dealt) {
-          const float2 c = ctl.sums[1][(warp & 3) * 32 + lane];
+          const float2 c = ctl.sums[1][row_in];
           m = fmaxf(a.x, c.x);
           const float ref = m == -INFINITY ? 0.0f : m;
           mine = ex2(a.x - ref);
           theirs = ex2(c.x - ref);
           l = a.y * mine + c.y * theirs;
         }
-        none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
-        const float inv = 1.0f / l;
+        const float inv = 1.0f / l;  // (l = 0, a row that sees no key: not used)
         mine *= inv;
         theirs *= inv;
-        if (!none) lse = m * 0.6931471805599453f + logf(l);
       }
-      const uint32_t nones = __ballot_sync(0xffffffffu, none);
-      if (row0 + lane < it.rows && p.lse != nullptr)
-        p.lse[static_cast<size_t>(it.q_row + row0 + lane) * p.heads + it.head] = lse;
+      const bool write = row < it.rows;
+      const bool none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
+      const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + it.head;
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {  // 16 rows: r and r + 8 of them in a lane
-        const int r = 16 * half + (lane >> 2);
-        const float mine0 = __shfl_sync(0xffffffffu, mine, r), mine1 = __shfl_sync(0xffffffffu, mine, r + 8);
-        const float theirs0 = __shfl_sync(0xffffffffu, theirs, r), theirs1 = __shfl_sync(0xffffffffu, theirs, r + 8);
-        uint16_t* dst = p.out + (static_cast<size_t>(it.q_row + row0 + r) * p.heads + it.head) * kDv + (lane & 3) * 8;
-        const size_t eight = static_cast<size_t>(p.heads) * (8 * kDv);
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          uint32_t o[16], w0[4], w1[4];
-          const uint32_t at = t_o + (static_cast<uint32_t>(16 * half) << 16) + 32 * c;
-          if (n > 0) {
-            tmem_ld_frag32(at + i * 128, o);
-            tmem_ld_wait();
+      for (int c = 0; c < 4; ++c) {
+        uint32_t o[32], w[16];
+        if (n > 0) {
+          tmem_ld32(t_o + i * 128 + 32 * c, o);
+          tmem_ld_wait();
 #pragma unroll
-            for (int x = 0; x < 16; ++x)
-              o[x] = __float_as_uint(__uint_as_float(o[x]) * ((x & 2) == 0 ? mine0 : mine1));
-            if (dealt) {
+          for (int x = 0; x < 16; ++x) {
+            const uint64_t v = mul2(f32x2(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1])), f32x2(mine, mine));
+            o[2 * x] = __float_as_uint(lo2(v));
+            o[2 * x + 1] = __float_as_uint(hi2(v));
+          }
+          if (dealt) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
               uint32_t e[16];
-              tmem_ld_frag32(at + 128, e);
+              tmem_ld(t_o + 128 + 32 * c + 16 * y, e);
               tmem_ld_wait();
 #pragma unroll
               for (int x = 0; x < 16; ++x)
-                o[x] = __float_as_uint(fmaf(__uint_as_float(e[x]), (x & 2) == 0 ? theirs0 : theirs1, __uint_as_float(o[x])));
-            }
-            if (half == 1 && c == 3) {
-              tc_fence_before();
-              __syncwarp();
-              mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[i]);
-              if (dealt) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[1]);
+                o[16 * y + x] = __float_as_uint(fmaf(__uint_as_float(e[x]), theirs, __uint_as_float(o[16 * y + x])));
             }
           }
-          const bool zero0 = (nones >> r & 1u) != 0, zero1 = (nones >> (r + 8) & 1u) != 0;
+          if (c == 3) {
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[i]);
+            if (dealt) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[1]);
+          }
+        }
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            w0[k] = zero0 ? 0u : pack_bf16(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]));
-            w1[k] = zero1 ? 0u : pack_bf16(__uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
-          }
-          transpose_quad(w0, lane);
-          transpose_quad(w1, lane);
-          if (row0 + r < it.rows) *reinterpret_cast<uint4*>(dst + 32 * c) = make_uint4(w0[0], w0[1], w0[2], w0[3]);
-          if (row0 + r + 8 < it.rows)
-            *reinterpret_cast<uint4*>(dst + eight + 32 * c) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+        for (int x = 0; x < 16; ++x)
+          w[x] = none ? 0u : pack_bf16(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
+        if (write) {
+          st_v8(p.out + at * kDv + 32 * c, w);
+          st_v8(p.out + at * kDv + 32 * c + 16, w + 8);
         }
       }
+      if (write && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
     }
   }
 }

@@ -239,12 +239,21 @@ __device__ __forceinline__ void give_up(Ctl& c, uint32_t* dev_err, uint32_t site
   report(dev_err, QMLA_DEVERR_TIMEOUT | (0x100u << site));
   *reinterpret_cast<volatile uint32_t*>(&c.abort) = 1u;
 }
-// One thread's bounded wait. (The clock is read only after a first wait of up to 100 us.)
+// One thread's bounded wait. (Each probe sleeps for up to 100 us; the clock is read
+// between them only.)
 __device__ __forceinline__ bool wait1(uint64_t* bar, uint32_t parity, Ctl& c, uint32_t site, uint32_t* dev_err) {
-  if (mbar_try_wait(bar, parity & 1u)) return true;
-  const int r = mbar_wait(bar, parity & 1u, kLimitNs, &c.abort);
-  if (r == 0) give_up(c, dev_err, site);
-  return r == 1;
+  uint64_t t0 = 0;
+#pragma unroll 1
+  while (!mbar_try_wait(bar, parity & 1u)) {
+    if (*reinterpret_cast<volatile uint32_t*>(&c.abort) != 0u) return false;
+    const uint64_t t = globaltimer_ns();
+    if (t0 == 0) t0 = t;
+    if (t - t0 > kLimitNs) {
+      give_up(c, dev_err, site);
+      return false;
+    }
+  }
+  return true;
 }
 // A whole warp's (every lane waits on the barrier itself).
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl& c, uint32_t site, uint32_t* dev_err) {

@@ -53,8 +53,8 @@ constexpr int kInFlight = 3;  // entries (a step's keys or values) that the ring
 constexpr int kSoftWarps = 8;
 constexpr int kEpiWarp = 8, kMmaWarp = 12, kLoadWarp = 13;
 constexpr int kThreads = 16 * 32;  // (the last warp leaves at once: registers are split by groups of four)
-// 128 registers a thread at launch: 2 x 176 + 80 + 80 = 4 x 128.
-constexpr int kSoftRegs = 176, kEpiRegs = 80, kOtherRegs = 80;
+// 128 registers a thread at launch: 2 x 160 + 96 + 96 = 4 x 128.
+constexpr int kSoftRegs = 160, kEpiRegs = 96, kOtherRegs = 96;
 constexpr int kRingOff = 2 * kQChunks * kSlotBytes;
 constexpr int kCtlOff = kRingOff + kRing * kSlotBytes;
 constexpr uint32_t kColO = 256;  // O0; O1 128 columns on
@@ -74,7 +74,7 @@ struct Ctl {
   uint64_t tail, fin;
   uint32_t tmem_base, abort;
   int turn;  // 1: a tile's MMAs are being issued
-  int4 work[2][3];
+  int4 work[2][4];
   float2 sums[2][kTile];  // (m, l) of the tiles' rows
 };
 constexpr int kSmem = kCtlOff + static_cast<int>(sizeof(Ctl));
@@ -90,62 +90,101 @@ struct Item {
   int first, bundle;       // the bundle's first item and its length
   int head;                // (of a pair; -1: no more)
   int dealt;               // one tile, whose key steps the two tiles share out
+  int part, parts;         // a long item's keys go in parts, each an item of its own
+  int slot;                // parts > 1: first of the heads x parts partial results
+  int unused;
 };
-static_assert(sizeof(Item) == 48, "three 16-byte loads");
+static_assert(sizeof(Item) == 64, "four 16-byte loads");
+
+// Keys are cut into parts where one pair would take half as long again as the SMs' fair
+// share of the whole call: parts of at most L = W / kShares rounds, W all the rounds, but
+// kLeastPart at least. An item of R > L rounds makes ceil(R / L) < 2 R / L parts, so there
+// are never more than 2 kShares partial results, nor more than kShares items cut up.
+constexpr int kShares = 160, kSlots = 2 * kShares, kLeastPart = 4;
+struct Join {  // an item cut up
+  int q_row, rows, slot, parts;
+};
+struct Partial {  // of a part and head: rows of the item
+  float o[kItemRows][kDv];   // unnormalised
+  float2 ml[kItemRows];      // reference (log2) and sum
+};
 
 struct Workspace {
-  size_t prefix_off, items_off, total;
-  int max_items;
+  size_t prefix_off, items_off, join_off, part_off, total;
+  int max_items, max_entries;
 };
 Workspace workspace_layout(int batch, int n_q) {
   Workspace w;
   w.max_items = n_q / kItemRows + batch;  // disjoint sequences have no more
-  w.prefix_off = 256;                     // int: items written; int: pairs drawn beyond one per CTA
+  w.prefix_off = 256;                     // ints: items written, pairs drawn beyond one per CTA, joins
   w.items_off = (w.prefix_off + 4 * (static_cast<size_t>(batch) + 1) + 255) / 256 * 256;
-  w.total = w.items_off + sizeof(Item) * static_cast<size_t>(w.max_items);
+  w.max_entries = w.max_items + kSlots;
+  w.join_off = w.items_off + sizeof(Item) * static_cast<size_t>(w.max_entries);
+  w.part_off = (w.join_off + sizeof(Join) * kShares + 255) / 256 * 256;
+  w.total = w.part_off + sizeof(Partial) * kSlots;
   return w;
 }
 
 // ------------------------------------------------------------------------- plan
-constexpr int kPlanThreads = 1024;
+// One block of kPlanThreads, or of kSmallPlan where that many sequences and items at
+// most can come up: a small call's time is the plan's chain of latencies.
+constexpr int kPlanThreads = 1024, kSmallPlan = 64;
+constexpr int kPlanOnChip = 2048;  // sequences whose prefix is kept in shared memory
 
-__device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int x = v;
+// Exclusive prefix of v (two counts in the halves) over the block, and the total.
+__device__ __forceinline__ long long block_scan(long long v, long long* warp_sums, long long& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  long long x = v;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, off);
+    const long long y = __shfl_up_sync(0xffffffffu, x, off);
     if (lane >= off) x += y;
   }
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  int s = warp_sums[lane];
+  long long s = lane < warps ? warp_sums[lane] : 0;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, s, off);
+    const long long y = __shfl_up_sync(0xffffffffu, s, off);
     if (lane >= off) s += y;
   }
   total = __shfl_sync(0xffffffffu, s, 31);
-  const int before = __shfl_sync(0xffffffffu, s, warp == 0 ? 0 : warp - 1);
+  const long long before = __shfl_sync(0xffffffffu, s, warp == 0 ? 0 : warp - 1);
   __syncthreads();
-  return (warp == 0 ? 0 : before) + x - v;  // exclusive
+  return (warp == 0 ? 0 : before) + x - v;
+}
+
+// Rounds of an item: key steps of its longer tile. Dealt, two of one tile's steps make a
+// round, but they load twice as many keys and take half as long again.
+__device__ __forceinline__ int rounds_of(const Item& it) {
+  return it.rows <= kTile ? (3 * it.n0 + 3) >> 2 : max(it.n0, it.n1);
 }
 
 // One block. A sequence has ceil(Lq / 256) items, in bundles of `bundle`; a counting
 // sort by key steps puts the longest bundles first (the order among equals is free:
-// items do not meet).
+// items do not meet). Passes: the rounds of all items, which say how long a part may
+// be; the sizes of the buckets; the list.
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ cu_q,
                                                             const int32_t* __restrict__ cu_kv, int batch, int n_q,
-                                                            int n_kv, int causal, int bundle, int shift, int max_items,
-                                                            int* __restrict__ count, int* __restrict__ prefix,
-                                                            Item* __restrict__ items, uint32_t* dev_err) {
-  __shared__ int warp_sums[32];
-  __shared__ int bucket[kPlanThreads];
+                                                            int n_kv, int heads, int causal, int bundle, int shift,
+                                                            int max_items, int* __restrict__ count,
+                                                            int* __restrict__ prefix_far, Item* __restrict__ items,
+                                                            Join* __restrict__ joins, uint32_t* dev_err) {
+  __shared__ long long warp_sums[32];
+  __shared__ int bucket[kPlanThreads];  // (as many as threads)
+  __shared__ int prefix_near[kPlanOnChip];
+  __shared__ unsigned long long rounds;
+  __shared__ int entries, slots, cut;
   griddep_launch_dependents();  // prefill_kernel may start its set-up meanwhile
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, threads = blockDim.x;
+  int* prefix = batch <= kPlanOnChip ? prefix_near : prefix_far;
   bucket[tid] = 0;
+  if (tid == 0) {
+    rounds = 0;
+    entries = slots = cut = 0;
+  }
   int bundles = 0, total_items = 0;
-  for (int b0 = 0; b0 < batch; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < batch; b0 += threads) {
     const int b = b0 + tid;
     int tiles = 0;
     if (b < batch) {
@@ -156,23 +195,26 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         tiles = (q1 - q0 + kItemRows - 1) / kItemRows;
       }
     }
-    int sum;
-    const int at = block_scan((tiles + bundle - 1) / bundle, warp_sums, sum);
-    if (b < batch) prefix[b] = bundles + at;
-    bundles += sum;
-    block_scan(tiles, warp_sums, sum);
-    total_items += sum;
+    long long sum;
+    const long long at =
+        block_scan((tiles + bundle - 1) / bundle | static_cast<long long>(tiles) << 32, warp_sums, sum);
+    if (b < batch) prefix[b] = bundles + static_cast<int>(at);
+    bundles += static_cast<int>(sum);
+    total_items += static_cast<int>(sum >> 32);
     // Decreasing offsets can make sequences overlap, which can be more than there is
     // room for: then nothing is worked on.
     if (total_items > max_items) break;
   }
   if (total_items > max_items) {
     if (tid == 0) report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
-    bundles = total_items = 0;
+    bundles = 0;
   }
   __syncthreads();
-  for (int pass = 0; pass < 2; ++pass) {
-    for (int i = tid; i < bundles; i += kPlanThreads) {
+  int longest = INT32_MAX;  // rounds of a part
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    unsigned long long mine = 0;
+    for (int i = tid; i < bundles; i += threads) {
       int lo = 0, hi = batch - 1;  // the last sequence with prefix <= i: it has items
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -185,8 +227,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
       const int q0 = cu_q[lo], lq = cu_q[lo + 1] - q0, k0 = cu_kv[lo], lk = cu_kv[lo + 1] - k0;
       const int tiles = (lq + kItemRows - 1) / kItemRows, t0 = (i - prefix[lo]) * bundle, k = min(bundle, tiles - t0);
       // (the last item is the longest; it stands first)
-      int at = 0;
-      for (int x = 0; x < k; ++x) {
+      auto item = [&](int x) {
         const int r0 = (t0 + k - 1 - x) * kItemRows;
         Item it;
         it.q_row = q0 + r0;
@@ -198,40 +239,93 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         const int last0 = min(it.rows, kTile) - 1, last1 = it.rows - 1;
         it.n0 = (max(min(lk, it.vis0 + it.step * last0), 0) + kTile - 1) / kTile;
         it.n1 = it.rows > kTile ? (max(min(lk, it.vis0 + it.step * last1), 0) + kTile - 1) / kTile : 0;
-        it.dealt = it.rows <= kTile && it.n0 > 1 ? 1 : 0;
-        it.head = 0;
-        if (x == 0) {
-          const int key = kPlanThreads - 1 - min(max(it.n0, it.n1) >> shift, kPlanThreads - 1);
-          at = atomicAdd(&bucket[key], k);
-          if (pass == 0) break;
+        return it;
+      };
+      auto parts_of = [&](const Item& it) {
+        const int r = rounds_of(it);
+        return r - longest > longest >> 1 ? (r + longest - 1) / longest : 1;
+      };
+      int all = 0;  // entries of the bundle
+      for (int x = 0; x < k; ++x) {
+        const Item it = item(x);
+        if (pass == 0) {
+          mine += static_cast<unsigned long long>(rounds_of(it)) * heads;
+        } else {
+          all += parts_of(it);
         }
-        it.first = at;
-        it.bundle = k;
-        items[at + x] = it;
       }
+      if (pass == 0) continue;
+      const int key = threads - 1 - min(min(rounds_of(item(0)), longest) >> shift, threads - 1);
+      int at = atomicAdd(&bucket[key], all);
+      if (pass == 1) {
+        atomicAdd(&entries, all);
+        continue;
+      }
+      const int first = at;
+      for (int x = 0; x < k; ++x) {
+        const Item whole = item(x);
+        // (dealt: an even number of steps, so that both tiles have as many)
+        const int parts = parts_of(whole), steps = max(whole.n0, whole.n1);
+        const int per = whole.rows <= kTile ? ((steps + 2 * parts - 1) / (2 * parts)) * 2 : (steps + parts - 1) / parts;
+        int slot = 0;
+        if (parts > 1) {
+          slot = atomicAdd(&slots, parts * heads);
+          joins[atomicAdd(&cut, 1)] = Join{whole.q_row, whole.rows, slot, parts};
+        }
+        for (int y = 0; y < parts; ++y, ++at) {
+          // A part is the item without the keys before it.
+          Item it = whole;
+          const int skip = parts > 1 ? y * per : 0;
+          it.kv_start += skip * kTile;
+          it.kv_len -= skip * kTile;
+          it.vis0 -= skip * kTile;
+          it.n0 = max(0, min(whole.n0 - skip, parts > 1 ? per : whole.n0));
+          it.n1 = max(0, min(whole.n1 - skip, parts > 1 ? per : whole.n1));
+          it.first = first;
+          it.bundle = all;
+          it.head = 0;
+          it.dealt = it.rows <= kTile && it.n0 > 1 ? 1 : 0;
+          it.part = y;
+          it.parts = parts;
+          it.slot = slot;
+          it.unused = 0;
+          items[at] = it;
+        }
+      }
+    }
+    if (pass == 0) {
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, off);
+      if ((tid & 31) == 0) atomicAdd(&rounds, mine);
     }
     __syncthreads();
     if (pass == 0) {
-      int sum;
-      const int before = block_scan(bucket[tid], warp_sums, sum);
-      bucket[tid] = before;
+      const unsigned long long share = (rounds + kShares - 1) / kShares;
+      longest = static_cast<int>(min(max(share, static_cast<unsigned long long>(kLeastPart)),
+                                     static_cast<unsigned long long>(INT32_MAX)));
+    } else if (pass == 1) {
+      long long sum;
+      const long long before = block_scan(bucket[tid], warp_sums, sum);
+      bucket[tid] = static_cast<int>(before);
       __syncthreads();
     }
   }
   if (tid == 0) {
-    count[0] = total_items;
+    count[0] = entries;
     count[1] = 0;
+    count[2] = cut;
   }
 }
 
 // ------------------------------------------------------------------------ main
 struct PrefillParams {
-  int* count;  // [0] items, [1] pairs drawn beyond one per CTA
+  int* count;  // [0] items, [1] pairs drawn beyond one per CTA, [2] joins
   const Item* items;
   int heads;
   float scale, scale_log2;
   uint16_t* out;
   float* lse;
+  Partial* partial;
   uint32_t* dev_err;
 };
 
@@ -266,8 +360,8 @@ template <bool LANES>
 __device__ __forceinline__ bool next_pair(Ctl& c, uint32_t k, Item& it, uint32_t site, uint32_t* dev_err) {
   uint64_t* bar = &c.sched_full[k & 1u];
   if (!(LANES ? wait_warp(bar, k >> 1, c, site, dev_err) : wait1(bar, k >> 1, c, site, dev_err))) return false;
-  const int4 x = c.work[k & 1u][0], y = c.work[k & 1u][1], z = c.work[k & 1u][2];
-  it = Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+  const int4 x = c.work[k & 1u][0], y = c.work[k & 1u][1], z = c.work[k & 1u][2], v = c.work[k & 1u][3];
+  it = Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w, v.x, v.y, v.z, v.w};
   if (LANES) __syncwarp();
   mbar_arrive_if(!LANES || (threadIdx.x & 31) == 0 ? 1u : 0u, &c.sched_free[k & 1u]);
   return it.head >= 0;
@@ -357,17 +451,16 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
   // through, and nothing else covers the way from HBM then.
   const int4* list = reinterpret_cast<const int4*>(p.items);
   const int pairs = p.count[0] * p.heads;
-  int4 w[3];
+  int4 w[4];
   auto look_up = [&](int at) {
-    w[0] = w[1] = make_int4(0, 0, 0, 0);
+    w[0] = w[1] = w[3] = make_int4(0, 0, 0, 0);
     w[2] = make_int4(0, 0, -1, 0);
     if (at >= pairs) return;
-    const int4 place = list[at / p.heads * 3 + 2];  // {the bundle's first item, its length, ..}
+    const int4 place = list[at / p.heads * 4 + 2];  // {the bundle's first item, its length, ..}
     const int rem = at - place.x * p.heads, head = rem / place.y;
     const int i = place.x + rem - head * place.y;
-    w[0] = list[i * 3];
-    w[1] = list[i * 3 + 1];
-    w[2] = list[i * 3 + 2];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) w[x] = list[i * 4 + x];
     w[2].z = head;
   };
   auto draw = [&]() {
@@ -387,9 +480,10 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
   look_up(static_cast<int>(blockIdx.x));
   for (uint32_t k = 0; ok; ++k) {
     if (k >= 2 && !(ok = wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err))) break;
-    it = Item{w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w, w[2].x, w[2].y, w[2].z, w[2].w};
+    it = Item{w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w,
+              w[2].x, w[2].y, w[2].z, w[2].w, w[3].x, w[3].y, w[3].z, w[3].w};
     if (lane == 0) {
-      for (int x = 0; x < 3; ++x) ctl.work[k & 1u][x] = w[x];
+      for (int x = 0; x < 4; ++x) ctl.work[k & 1u][x] = w[x];
     }
     mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.sched_full[k & 1u]);
     if (it.head < 0) break;
@@ -682,14 +776,16 @@ __device__ __forceinline__ void st_v8(void* dst, const uint32_t* w) {
                : "memory");
 }
 
-// O / l and the log-sum-exp of both tiles, a query row per thread.
+// O / l and the log-sum-exp of both tiles, a query row per thread. A part's O goes to
+// the workspace as it is, in fp32 with its (m, l), for join_kernel.
 __device__ void epilogue_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, int warp, int lane) {
   const uint32_t t_o = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kColO;
   const int row_in = (warp & 3) * 32 + lane;
   uint32_t no[2] = {0, 0};
   Item it;
   for (uint32_t pair = 0; next_pair<true>(ctl, pair, it, kSiteEpilogue, p.dev_err); ++pair) {
-    const bool dealt = it.dealt != 0;
+    const bool dealt = it.dealt != 0, whole = it.parts == 1;
+    Partial* part = whole ? nullptr : p.partial + it.slot + static_cast<size_t>(it.head) * it.parts + it.part;
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       if (i * kTile >= it.rows) break;
@@ -714,15 +810,17 @@ __device__ void epilogue_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, i
           theirs = ex2(c.x - ref);
           l = a.y * mine + c.y * theirs;
         }
-        const float inv = 1.0f / l;  // (l = 0, a row that sees no key: not used)
-        mine *= inv;
-        theirs *= inv;
+        if (whole) {
+          const float inv = 1.0f / l;  // (l = 0, a row that sees no key: not used)
+          mine *= inv;
+          theirs *= inv;
+        }
       }
       const bool write = row < it.rows;
       const bool none = l == 0.0f;  // the row sees no key (a visible one leaves l >= 1, or NaN)
       const size_t at = static_cast<size_t>(it.q_row + row) * p.heads + it.head;
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < (whole || n > 0 ? 4 : 0); ++c) {
         uint32_t o[32], w[16];
         if (n > 0) {
           tmem_ld32(t_o + i * 128 + 32 * c, o);
@@ -751,15 +849,24 @@ __device__ void epilogue_role(const PrefillParams& p, Ctl& ctl, uint32_t tmem, i
             if (dealt) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.o_free[1]);
           }
         }
+        if (!write) continue;
+        if (whole) {
 #pragma unroll
-        for (int x = 0; x < 16; ++x)
-          w[x] = none ? 0u : pack_bf16(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
-        if (write) {
+          for (int x = 0; x < 16; ++x)
+            w[x] = none ? 0u : pack_bf16(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
           st_v8(p.out + at * kDv + 32 * c, w);
           st_v8(p.out + at * kDv + 32 * c + 16, w + 8);
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) st_v8(part->o[row] + 32 * c + 8 * x, o + 8 * x);
         }
       }
-      if (write && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
+      if (!write) continue;
+      if (!whole) {
+        part->ml[row] = make_float2(m, l);
+      } else if (p.lse != nullptr) {
+        p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
+      }
     }
   }
 }
@@ -822,11 +929,67 @@ __global__ void __launch_bounds__(kThreads, 1)
       asm volatile("exit;");
     }
   }
+  griddep_launch_dependents();  // join_kernel may be scheduled as CTAs finish
   tc_fence_before();
   __syncthreads();  // (exited lanes do not take part)
   if (warp == 0) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
+  }
+}
+
+// The items that were cut up: a row of one head per warp and turn, a lane four
+// channels. A row's parts are added in their order; eight of them are on their way at
+// once, and the first eight while the maximum is found.
+constexpr int kJoinThreads = 256, kJoinRows = kJoinThreads / 32, kJoinAhead = 8;
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const PrefillParams p, const Join* __restrict__ joins) {
+  griddep_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int units = p.count[2] * p.heads * (kItemRows / kJoinRows);
+  for (int u = blockIdx.x; u < units; u += gridDim.x) {
+    const int pair = u / (kItemRows / kJoinRows), head = pair % p.heads;
+    const int row = u % (kItemRows / kJoinRows) * kJoinRows + warp;
+    const Join j = joins[pair / p.heads];
+    if (row >= j.rows) continue;
+    const Partial* part = p.partial + j.slot + static_cast<size_t>(head) * j.parts;
+    float4 v[kJoinAhead];
+    float2 x[kJoinAhead];
+    auto load = [&](int y0) {
+#pragma unroll
+      for (int k = 0; k < kJoinAhead; ++k) {
+        if (y0 + k < j.parts) {
+          x[k] = part[y0 + k].ml[row];
+          v[k] = *reinterpret_cast<const float4*>(part[y0 + k].o[row] + 4 * lane);
+        }
+      }
+    };
+    load(0);
+    float m = -INFINITY;
+    for (int y = lane; y < j.parts; y += 32) {
+      const float2 z = part[y].ml[row];
+      if (z.y != 0.0f) m = fmaxf(m, z.x);  // (a sum of 0: the row sees no key of this part)
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int y0 = 0; y0 < j.parts; y0 += kJoinAhead) {
+      if (y0 > 0) load(y0);
+#pragma unroll
+      for (int k = 0; k < kJoinAhead; ++k) {
+        if (y0 + k >= j.parts || x[k].y == 0.0f) continue;  // (then v was not written)
+        const float f = ex2(x[k].x - ref);
+        l = fmaf(x[k].y, f, l);
+        o = make_float4(fmaf(v[k].x, f, o.x), fmaf(v[k].y, f, o.y), fmaf(v[k].z, f, o.z), fmaf(v[k].w, f, o.w));
+      }
+    }
+    const bool none = l == 0.0f;
+    const float inv = 1.0f / l;
+    const size_t at = static_cast<size_t>(j.q_row + row) * p.heads + head;
+    *reinterpret_cast<uint2*>(p.out + at * kDv + 4 * lane) =
+        none ? make_uint2(0u, 0u) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    if (lane == 0 && p.lse != nullptr) p.lse[at] = none ? -INFINITY : m * 0.6931471805599453f + logf(l);
   }
 }
 
@@ -882,6 +1045,8 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   p.count = reinterpret_cast<int*>(ws);
   p.items = reinterpret_cast<const Item*>(ws + w.items_off);
   p.heads = d.heads;
+  Join* joins = reinterpret_cast<Join*>(ws + w.join_off);
+  p.partial = reinterpret_cast<Partial*>(ws + w.part_off);
   p.scale = d.softmax_scale;
   p.scale_log2 = d.softmax_scale * 1.4426950408889634f;
   p.out = d.out;
@@ -915,14 +1080,15 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   const long long pairs = static_cast<long long>(w.max_items) * d.heads;
   // Items per bundle: with few pairs per SM single items even the load out better.
   const int bundle = pairs >= 8ll * sms ? 4 : 1;
+  const int threads = w.max_items <= kSmallPlan && d.batch <= kSmallPlan ? kSmallPlan : kPlanThreads;
   int shift = 0;
-  while (((d.n_kv / kTile + 1) >> shift) >= kPlanThreads) ++shift;
-  plan_kernel<<<1, kPlanThreads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.causal != 0, bundle, shift, w.max_items,
-                                              reinterpret_cast<int*>(ws), reinterpret_cast<int*>(ws + w.prefix_off),
-                                              reinterpret_cast<Item*>(ws + w.items_off), d.dev_err);
+  while (((d.n_kv / kTile + 1) >> shift) >= threads) ++shift;
+  plan_kernel<<<1, threads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.heads, d.causal != 0, bundle,
+                                              shift, w.max_items, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
+                                              reinterpret_cast<Item*>(ws + w.items_off), joins, d.dev_err);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, pairs)));
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, pairs + kSlots)));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
@@ -931,7 +1097,13 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, prefill_kernel, tq, tk, tv, tpe, p);
+  if ((e = cudaLaunchKernelEx(&cfg, prefill_kernel, tq, tk, tv, tpe, p)) != cudaSuccess) return e;
+  // (no item has more than kLeastPart rounds, so none is cut up)
+  if (d.n_kv <= kLeastPart * kTile) return cudaSuccess;
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * sms));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, join_kernel, p, static_cast<const Join*>(joins));
 }
 
 }  // namespace qmla

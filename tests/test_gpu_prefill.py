@@ -115,6 +115,22 @@ def test_many_items_per_cta_and_head_groups():
     p.check()
 
 
+@pytest.mark.parametrize("n,m,heads", [(1, 40000, 1), (40, 5000, 1), (200, 20000, 1), (300, 9000, 3), (700, 3000, 2)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_rows_over_long_contexts(n, m, heads, causal):
+    """Keys in parts: up to 59 of them, of one and two tiles, joined from the workspace."""
+    p = Prompt([n], [m], heads, seed=n + m)
+    assert p.run(causal) == 0
+    p.check(causal)
+
+
+def test_one_long_sequence_among_short_ones():
+    """Only the long one's keys go in parts; rows without keys in some of them (causal)."""
+    p = Prompt([3, 600, 1, 0, 90], [3, 12000, 0, 7, 40], 4, seed=12)
+    assert p.run() == 0
+    p.check()
+
+
 def test_large_scores_raise_the_reference():
     """Scores whose maximum grows along the keys by far more than 2^8 a step: the running
     maximum is raised and the sums rescaled many times."""

@@ -72,6 +72,83 @@ __device__ __forceinline__ void codes8(const uint32_t (&w)[4], float s, float y,
   }
 }
 
+// Extrema of a group's 64 values, eight in each of eight lanes: (min, -max) as a bf16
+// pair, so that one packed minimum per shuffle serves both. bf16 minima are exact, and
+// NaNs lose against numbers as in fminf / fmaxf. All lanes of the warp take part.
+__device__ __forceinline__ uint32_t extrema64(const uint32_t (&w)[4]) {
+  __nv_bfloat162 lo = *reinterpret_cast<const __nv_bfloat162*>(&w[0]), hi = lo;
+#pragma unroll
+  for (int e = 1; e < 4; ++e) {
+    const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&w[e]);
+    lo = __hmin2(lo, v);
+    hi = __hmax2(hi, v);
+  }
+  lo = __hmin2(lo, __lowhigh2highlow(lo));
+  hi = __hmax2(hi, __lowhigh2highlow(hi));
+  uint32_t pk =
+      __byte_perm(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi) ^ 0x80008000u, 0x7610);
+#pragma unroll
+  for (int off = 1; off < 8; off <<= 1) {
+    const uint32_t o = __shfl_xor_sync(0xffffffffu, pk, off);
+    const __nv_bfloat162 r = __hmin2(*reinterpret_cast<const __nv_bfloat162*>(&pk),
+                                     *reinterpret_cast<const __nv_bfloat162*>(&o));
+    pk = *reinterpret_cast<const uint32_t*>(&r);
+  }
+  return pk;
+}
+
+// Scale, zero point and 1 / s of a group from its extrema; 1 / s is 0 for a group whose
+// values divide one by one (an infinite or NaN quotient among them; 1 / s is 0 when s is
+// infinite, and for the paper's fp32 RoPE scale).
+template <int CB>
+__device__ __forceinline__ void scale_of(uint32_t ext, bool content, int m, float& s, float& z, float& y) {
+  const float xmin = __uint_as_float(ext << 16), xmax = -__uint_as_float(ext & 0xFFFF0000u);
+  if constexpr (CB == kC4R4) {
+    paper_scale(xmin, xmax, content, s, z);
+  } else {
+    group_scale(xmin, xmax, m, s, z);
+  }
+  y = __frcp_rn(s);
+  if (!(fmaxf(fabsf(xmin), fabsf(xmax)) * y <= 16384.0f) || (CB == kC4R4 && !content)) y = 0.0f;
+}
+
+template <int CB>
+__device__ __forceinline__ void store_scale(uint8_t* blk, int g, int slot, float s, float z) {
+  using L = BlockLayout<CB>;
+  if constexpr (CB == kC4R4) {
+    if (g < 8) {
+      *reinterpret_cast<__nv_bfloat16*>(blk + L::c_scale_off(g, slot)) = __float2bfloat16_rn(s);  // exact
+    } else {
+      *reinterpret_cast<float*>(blk + L::pe_scale_off(slot)) = s;
+    }
+    blk[L::zero_off(g, slot)] = static_cast<uint8_t>(z);
+  } else {
+    *reinterpret_cast<__half2*>(blk + L::sz_off(g, slot)) =
+        __halves2half2(__float2half_rn(s), __float2half_rn(z));
+  }
+}
+
+// The codes of eight values, packed low bits first: INT4 byte j = code 2 j | code 2 j + 1
+// << 4 (four bytes), INT2 byte j = codes 4 j .. 4 j + 3 (two).
+__device__ __forceinline__ uint32_t pack_codes(const uint32_t (&w)[4], float s, float y, float z, int bits) {
+  const uint32_t m = (1u << bits) - 1u;
+  uint32_t c[4];  // codes 2 e and 2 e + 1 in the halves of c[e]
+  if (y > 0.0f) {
+    codes8(w, s, y, z, m, c);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      c[e] = quant_code(__uint_as_float(w[e] << 16), s, z, static_cast<float>(m)) |
+             quant_code(__uint_as_float(w[e] & 0xFFFF0000u), s, z, static_cast<float>(m)) << 16;
+  }
+  if (bits == 4) {
+    const uint32_t a = c[0] | c[1] << 8, b = c[2] | c[3] << 8;
+    return __byte_perm(a | a >> 12, b | b >> 12, 0x5410);
+  }
+  const uint32_t a = c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12;
+  return a | a >> 14;
+}
+
 // Looks up and validates the destination of token i: its block id, or -1 (after
 // recording the error) when the token cannot be written.
 __device__ __forceinline__ int token_block(int num_blocks, const int32_t* seq_ids, const int32_t* positions, int i,
@@ -283,59 +360,18 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
       return;
     }
   }
-  // Extrema of each token's 64 values: (min, -max) as a bf16 pair, so that one packed
-  // minimum per shuffle serves both. bf16 minima are exact, and NaNs lose against
-  // numbers as in fminf / fmaxf.
   uint32_t ext = 0;  // of token `own`
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-    __nv_bfloat162 lo = *reinterpret_cast<const __nv_bfloat162*>(&w[0]), hi = lo;
-#pragma unroll
-    for (int e = 1; e < 4; ++e) {
-      const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&w[e]);
-      lo = __hmin2(lo, v);
-      hi = __hmax2(hi, v);
-    }
-    lo = __hmin2(lo, __lowhigh2highlow(lo));
-    hi = __hmax2(hi, __lowhigh2highlow(hi));
-    uint32_t pk =
-        __byte_perm(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi) ^ 0x80008000u, 0x7610);
-#pragma unroll
-    for (int off = 1; off < 8; off <<= 1) {
-      const uint32_t o = __shfl_xor_sync(0xffffffffu, pk, off);
-      const __nv_bfloat162 r = __hmin2(*reinterpret_cast<const __nv_bfloat162*>(&pk),
-                                       *reinterpret_cast<const __nv_bfloat162*>(&o));
-      pk = *reinterpret_cast<const uint32_t*>(&r);
-    }
+    const uint32_t pk = extrema64(w);
     if (i == own) ext = pk;
   }
-  const float xmin = __uint_as_float(ext << 16), xmax = -__uint_as_float(ext & 0xFFFF0000u);
-  float s_own, z_own;
-  if constexpr (CB == kC4R4) {
-    paper_scale(xmin, xmax, g < 8, s_own, z_own);
-  } else {
-    group_scale(xmin, xmax, m, s_own, z_own);
-  }
-  // 1 / s, or 0 for a group whose values divide one by one (an infinite or NaN
-  // quotient among them; 1 / s is 0 when s is infinite)
-  float y_own = __frcp_rn(s_own);
-  if (!(fmaxf(fabsf(xmin), fabsf(xmax)) * y_own <= 16384.0f) || (CB == kC4R4 && g == 8)) y_own = 0.0f;
-  if (piece == own && dst >= 0) {
-    uint8_t* blk = pool + static_cast<size_t>(dst / kBlockTokens) * L::kBytes;
-    const int slot = dst % kBlockTokens;
-    if constexpr (CB == kC4R4) {
-      if (g < 8) {
-        *reinterpret_cast<__nv_bfloat16*>(blk + L::c_scale_off(g, slot)) = __float2bfloat16_rn(s_own);  // exact
-      } else {
-        *reinterpret_cast<float*>(blk + L::pe_scale_off(slot)) = s_own;
-      }
-      blk[L::zero_off(g, slot)] = static_cast<uint8_t>(z_own);
-    } else {
-      *reinterpret_cast<__half2*>(blk + L::sz_off(g, slot)) =
-          __halves2half2(__float2half_rn(s_own), __float2half_rn(z_own));
-    }
-  }
+  float s_own, z_own, y_own;
+  scale_of<CB>(ext, g < 8, m, s_own, z_own, y_own);
+  if (piece == own && dst >= 0)
+    store_scale<CB == kBf16Rows ? 4 : CB>(pool + static_cast<size_t>(dst / kBlockTokens) * L::kBytes, g,
+                                          dst % kBlockTokens, s_own, z_own);
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
@@ -345,24 +381,7 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     const float y = NT == 1 ? y_own : __shfl_sync(0xffffffffu, y_own, from);
     const float z = NT == 1 ? z_own : __shfl_sync(0xffffffffu, z_own, from);
     const int d = NT == 1 ? dst : __shfl_sync(0xffffffffu, dst, from);
-    uint32_t c[4];  // codes 2 e and 2 e + 1 in the halves of c[e]
-    if (y > 0.0f) {
-      codes8(w, s, y, z, m, c);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        c[e] = quant_code(__uint_as_float(w[e] << 16), s, z, static_cast<float>(m)) |
-               quant_code(__uint_as_float(w[e] & 0xFFFF0000u), s, z, static_cast<float>(m)) << 16;
-    }
-    // Packed low bits first: INT4 byte j = code 2 j | code 2 j + 1 << 4, INT2 byte j = codes 4 j .. 4 j + 3.
-    uint32_t word;
-    if (bits == 4) {
-      const uint32_t a = c[0] | c[1] << 8, b = c[2] | c[3] << 8;
-      word = __byte_perm(a | a >> 12, b | b >> 12, 0x5410);
-    } else {
-      const uint32_t a = c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12;
-      word = a | a >> 14;
-    }
+    const uint32_t word = pack_codes(w, s, y, z, bits);
     if (prot != nullptr) {
       const int rows[2] = {NT == 1 ? sink : __shfl_sync(0xffffffffu, sink, from),
                            NT == 1 ? ring : __shfl_sync(0xffffffffu, ring, from)};
@@ -376,6 +395,128 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
       reinterpret_cast<uint32_t*>(code)[piece] = word;
     } else {
       reinterpret_cast<uint16_t*>(code)[piece] = static_cast<uint16_t>(word);
+    }
+  }
+}
+
+// The fused writer for many tokens: eight lanes hold a whole token, lane l the eight
+// channels l of each of its nine groups, so that a warp writes four tokens without a
+// word to the others. The row's sum takes three shuffles instead of a way through shared
+// memory, and lane l works out the scale of group l, which shuffles hand round.
+//
+// What bounds it: the issue slots (about 350 warp instructions per token for INT4), then
+// the HBM traffic (1,152 bytes of the row and 256 of its angles read, 324 written). With
+// a warp per group, as for few tokens, it takes twice as many.
+constexpr int kWideThreads = 256;
+template <int CB>
+__global__ void __launch_bounds__(kWideThreads) wide_append_kernel(
+    uint8_t* __restrict__ pool, int num_blocks, const uint32_t* __restrict__ latent,
+    const uint32_t* __restrict__ k_pe, const int32_t* __restrict__ seq_ids,
+    const int32_t* __restrict__ positions, int n, const int32_t* __restrict__ table, int num_seqs,
+    int max_blocks, uint32_t* dev_err, uint4* __restrict__ prot, const int32_t* __restrict__ lens,
+    const RowTransform tr) {
+  using L = BlockLayout<CB == kBf16Rows ? 4 : CB>;
+  constexpr int kBits = CB == kC4R4 || CB == kBf16Rows ? 4 : CB;
+  griddep_launch_dependents();  // as in quant_append_kernel
+  const int lane = threadIdx.x & 31, piece = lane & 7;
+  const int tok = (blockIdx.x * (kWideThreads / 32) + (threadIdx.x >> 5)) * 4 + (lane >> 3);
+  uint32_t raw[kGroups][4];
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (tok < n) {
+      const size_t row = static_cast<size_t>(tok);
+      v = *reinterpret_cast<const uint4*>(g < 8 ? latent + row * tr.latent_words + g * 32 + piece * 4
+                                                : k_pe + row * tr.k_pe_words + piece * 4);
+    }
+    raw[g][0] = v.x, raw[g][1] = v.y, raw[g][2] = v.z, raw[g][3] = v.w;
+  }
+  int dst = -1, sink = -1, ring = -1;
+  const float* angles = nullptr;
+  if (tok < n) {
+    int seq = 0, pos = 0;
+    const int blk = token_block(num_blocks, seq_ids, positions, tok, table, num_seqs, max_blocks,
+                                piece == 0 ? dev_err : nullptr, seq, pos, tr.rope_len);
+    if (blk >= 0) {
+      dst = blk * kBlockTokens + pos % kBlockTokens;
+      if (prot != nullptr) {
+        if (pos < kSinkTokens) sink = seq * kProtRows + pos;
+        if (pos >= lens[seq] - kRecentTokens) ring = seq * kProtRows + kSinkTokens + pos % kRecentTokens;
+      }
+    }
+    if (pos >= 0 && pos < tr.rope_len) angles = tr.cos_sin + static_cast<size_t>(pos) * kDr;
+  }
+  {
+    Angles a;
+    load_angles(a, angles, piece, tr.interleaved);
+    rotate_row<true>(raw[8], a, piece, tr.interleaved);
+  }
+  if (tr.norm) {
+    F2x2 sum = {0, 0};
+#pragma unroll
+    for (int g = 0; g < 8; ++g) add_squares8(sum, raw[g]);
+    F2 s = add_f2({lo2(sum.hi), lo2(sum.lo)}, {hi2(sum.hi), hi2(sum.lo)});
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1)
+      s = add_f2(s, {__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off)});
+    const F2 rs = row_rstd(s, tr.eps);
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      const uint4 gv = tr.weight != nullptr ? __ldg(tr.weight + g * 8 + piece)
+                                            : make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+      const uint64_t gw[4] = {f32x2(bf16_low(gv.x), bf16_high(gv.x)), f32x2(bf16_low(gv.y), bf16_high(gv.y)),
+                              f32x2(bf16_low(gv.z), bf16_high(gv.z)), f32x2(bf16_low(gv.w), bf16_high(gv.w))};
+      scale_row(raw[g], gw, rs);
+    }
+  }
+  if (prot != nullptr) {
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const uint4 v = make_uint4(raw[g][0], raw[g][1], raw[g][2], raw[g][3]);
+      if (sink >= 0) prot[static_cast<size_t>(sink) * (kDqk * 2 / 16) + g * 8 + piece] = v;
+      if (ring >= 0) prot[static_cast<size_t>(ring) * (kDqk * 2 / 16) + g * 8 + piece] = v;
+    }
+  }
+  if constexpr (CB == kBf16Rows) {
+    if (dst < 0) return;
+    uint4* row = reinterpret_cast<uint4*>(pool + static_cast<size_t>(dst / kBlockTokens) * kBf16BlockBytes +
+                                          dst % kBlockTokens * (kDqk * 2)) + piece;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) row[g * 8] = make_uint4(raw[g][0], raw[g][1], raw[g][2], raw[g][3]);
+  } else {
+    uint8_t* blk = pool + static_cast<size_t>(max(dst, 0) / kBlockTokens) * L::kBytes;
+    const int slot = max(dst, 0) % kBlockTokens;
+    // Extrema; lane l keeps group l's (and every lane the RoPE key's).
+    uint32_t ext = 0, ext_pe = 0;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const uint32_t pk = extrema64(raw[g]);
+      if (g == piece) ext = pk;
+      if (g == 8) ext_pe = pk;
+    }
+    float s, z, y;
+    scale_of<CB>(ext, true, (1 << kBits) - 1, s, z, y);
+    float s_pe, z_pe, y_pe;
+    scale_of<CB>(ext_pe, false, 15, s_pe, z_pe, y_pe);
+    if (dst >= 0) {
+      store_scale<CB>(blk, piece, slot, s, z);
+      if (piece == 0) store_scale<CB>(blk, 8, slot, s_pe, z_pe);
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int from = (lane & 24) | g;
+      const float sg = g < 8 ? __shfl_sync(0xffffffffu, s, from) : s_pe;
+      const float yg = g < 8 ? __shfl_sync(0xffffffffu, y, from) : y_pe;
+      const float zg = g < 8 ? __shfl_sync(0xffffffffu, z, from) : z_pe;
+      const int bits = g < 8 ? kBits : kPeBits;
+      const uint32_t word = pack_codes(raw[g], sg, yg, zg, bits);
+      if (dst < 0) continue;
+      uint8_t* code = blk + L::code_off(g, slot);
+      if (bits == 4) {
+        reinterpret_cast<uint32_t*>(code)[piece] = word;
+      } else {
+        reinterpret_cast<uint16_t*>(code)[piece] = static_cast<uint16_t>(word);
+      }
     }
   }
 }
@@ -444,11 +585,27 @@ void launch_quant(const AppendArgs& a, const RowTransform& tr, cudaStream_t stre
 // 32,768 15.1 against 19.5 / 19.8 against 20.7.
 constexpr int kFourPerLane = 8192;
 
+// Tokens from which the fused writer gives a token to eight lanes.
+constexpr int kWide = 2048;
+
 template <int CB, bool FUSED>
 void launch_quant(const AppendArgs& a, const RowTransform& tr, bool vec, cudaStream_t stream) {
-  auto* f = !vec ? launch_quant<CB, 1, false, FUSED>
-                 : (a.n >= kFourPerLane ? launch_quant<CB, 4, true, FUSED> : launch_quant<CB, 1, true, FUSED>);
-  f(a, tr, stream);
+  if constexpr (FUSED) {
+    if (vec && a.n >= kWide) {
+      constexpr long long kPerBlock = kWideThreads / 8;
+      wide_append_kernel<CB><<<static_cast<unsigned>((a.n + kPerBlock - 1) / kPerBlock), kWideThreads, 0, stream>>>(
+          static_cast<uint8_t*>(a.pool), a.num_blocks, reinterpret_cast<const uint32_t*>(a.latent),
+          reinterpret_cast<const uint32_t*>(a.k_pe), a.seq_ids, a.positions, a.n, a.table, a.num_seqs, a.max_blocks,
+          a.dev_err, static_cast<uint4*>(a.prot), a.lens, tr);
+      return;
+    }
+    auto* f = vec ? launch_quant<CB, 1, true, true> : launch_quant<CB, 1, false, true>;
+    f(a, tr, stream);
+  } else {
+    auto* f = !vec ? launch_quant<CB, 1, false, false>
+                   : (a.n >= kFourPerLane ? launch_quant<CB, 4, true, false> : launch_quant<CB, 1, true, false>);
+    f(a, tr, stream);
+  }
 }
 
 }  // namespace

@@ -100,16 +100,19 @@ __device__ __forceinline__ void rotate_row(uint32_t (&w)[4], const Angles& a, in
   }
 }
 
-// Sum of the squares of eight bf16 values (each exact in fp32), even and odd
-// channels side by side.
-__device__ __forceinline__ F2 square_sum8(const uint32_t (&w)[4]) {
-  F2x2 sum = {0, 0};  // (pairs of zeros)
+// Adds the squares of eight bf16 values (each exact in fp32), even and odd channels
+// side by side.
+__device__ __forceinline__ void add_squares8(F2x2& sum, const uint32_t (&w)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint64_t x = f32x2(bf16_low(w[e]), bf16_high(w[e]));
     const F2x2 t = two_sum2(sum.hi, mul2(x, x));
     sum = {t.hi, add2(sum.lo, t.lo)};
   }
+}
+__device__ __forceinline__ F2 square_sum8(const uint32_t (&w)[4]) {
+  F2x2 sum = {0, 0};  // (pairs of zeros)
+  add_squares8(sum, w);
   return add_f2({lo2(sum.hi), lo2(sum.lo)}, {hi2(sum.hi), hi2(sum.lo)});
 }
 

@@ -11,7 +11,7 @@ namespace qmla {
 namespace {
 
 constexpr int kBf16Rows = 16;  // cache kind of the BF16 cache
-constexpr int kReadThreads = kGroups * 32;
+constexpr int kReadThreads = 128;
 
 __device__ __forceinline__ uint4 load16(const void* p) {
   uint4 r;
@@ -30,26 +30,28 @@ __device__ __forceinline__ uint32_t value2(uint32_t q0, uint32_t q1, uint64_t zz
   return pack_bf16(lo2(v), hi2(v));
 }
 
-// Reads n tokens: warp g of a block the 64 channels of group g of 4 NT tokens, eight
-// lanes a token with eight channels (a 16-byte store) each, as the writer has them.
-// Lane i of a token's NT looks the place of token i up; shuffles hand it round.
+// Reads n tokens: eight lanes a token, lane l the eight channels l of each of its nine
+// groups (4 or 2 bytes of codes, a 16-byte store), so that a token's place is looked up
+// once, all its loads are on their way together, and lane l fetches the scale of group l,
+// which a shuffle hands round.
 //
 // What bounds it: the HBM traffic, 1,152 bytes written and 196 to 1,152 read per
 // token, once enough tokens are in flight to cover the chain position -> block
 // table -> codes.
-template <int CB, int NT>
+template <int CB>
 __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(
     const uint8_t* __restrict__ pool, int num_blocks, const int32_t* __restrict__ seq_ids,
     const int32_t* __restrict__ positions, int n, const int32_t* __restrict__ table, int num_seqs, int max_blocks,
     const int32_t* __restrict__ lens, const uint4* __restrict__ prot, uint16_t* __restrict__ rows, size_t row_stride,
     uint32_t* dev_err) {
   using L = BlockLayout<CB == kBf16Rows ? 4 : CB>;
-  const int g = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane & 7;
-  const int tok0 = blockIdx.x * (4 * NT) + (lane >> 3);
-  const int own = piece & (NT - 1);
-  // >= 0: block id times 64 plus the slot; -1: nothing to read; -2 - r: protection row r
-  long long src = -1;
-  if (const int tok = tok0 + 4 * own; tok < n) {
+  const int lane = threadIdx.x & 31, piece = lane & 7;
+  const int tok = (blockIdx.x * (kReadThreads / 32) + (threadIdx.x >> 5)) * 4 + (lane >> 3);
+  // Where the token is: in the pool (blk), in the protection buffer (kept), or nowhere.
+  const uint8_t* blk = nullptr;
+  const uint4* kept = nullptr;
+  int slot = 0;
+  if (tok < n) {
     const int seq = seq_ids != nullptr ? seq_ids[tok] : tok;
     const int pos = positions[tok];
     uint32_t bad = 0;
@@ -59,93 +61,76 @@ __global__ void __launch_bounds__(kReadThreads) cache_read_kernel(
       bad = QMLA_DEVERR_BAD_POSITION;
     } else if (prot != nullptr && (pos < kSinkTokens || pos >= lens[seq] - kRecentTokens)) {
       const int row = pos < kSinkTokens ? pos : kSinkTokens + pos % kRecentTokens;
-      src = -2 - (static_cast<long long>(seq) * kProtRows + row);
+      kept = prot + (static_cast<size_t>(seq) * kProtRows + row) * (kDqk * 2 / 16) + piece;
     } else {
-      const int blk = table[static_cast<size_t>(seq) * max_blocks + pos / kBlockTokens];
-      if (blk < 0 || blk >= num_blocks) {
+      const int id = table[static_cast<size_t>(seq) * max_blocks + pos / kBlockTokens];
+      if (id < 0 || id >= num_blocks) {
         bad = QMLA_DEVERR_BAD_BLOCK;
       } else {
-        src = static_cast<long long>(blk) * kBlockTokens + pos % kBlockTokens;
+        blk = pool + static_cast<size_t>(id) * (CB == kBf16Rows ? kBf16BlockBytes : L::kBytes);
+        slot = pos % kBlockTokens;
       }
     }
-    if (bad != 0 && g == 0 && piece == own) report(dev_err, bad);
+    if (bad != 0 && piece == 0) report(dev_err, bad);
   }
-  const bool four = CB != 2 || g == 8;  // codes of four bits (uniform in the warp)
-  long long at[NT];
-  uint4 full[NT];  // a whole piece (bf16 rows, protection rows), or {codes, scale, zero, -}
+  uint4* out = reinterpret_cast<uint4*>(rows + static_cast<size_t>(max(tok < n ? tok : 0, 0)) * row_stride) + piece;
+  if (CB == kBf16Rows || kept != nullptr) {  // whole pieces
+    const uint4* src = kept;
+    if (CB == kBf16Rows && blk != nullptr) src = reinterpret_cast<const uint4*>(blk + slot * (kDqk * 2)) + piece;
+    if (src != nullptr) {
+      uint4 v[kGroups];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    at[i] = NT == 1 ? src : __shfl_sync(0xffffffffu, src, (lane & 24) | i);
-    full[i] = make_uint4(0, 0, 0, 0);
-    if (at[i] <= -2) {
-      full[i] = load16(prot + static_cast<size_t>(-2 - at[i]) * (kDqk * 2 / 16) + g * 8 + piece);
-    } else if (at[i] >= 0) {
-      const size_t blk = static_cast<size_t>(at[i]) / kBlockTokens;
-      const int slot = static_cast<int>(at[i] % kBlockTokens);
-      if constexpr (CB == kBf16Rows) {
-        full[i] = load16(pool + blk * kBf16BlockBytes + slot * (kDqk * 2) + (g * 8 + piece) * 16);
+      for (int g = 0; g < kGroups; ++g) v[g] = load16(src + g * 8);
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) out[g * 8] = v[g];
+    }
+  }
+  if constexpr (CB != kBf16Rows) {
+    // Codes, and the scales of group `piece` (own) and of the RoPE key (pe).
+    uint32_t c[kGroups];
+    float s_own = 0.0f, z_own = 0.0f, s_pe = 0.0f, z_pe = 0.0f;
+    if (blk != nullptr) {
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        const uint8_t* at = blk + L::code_off(g, slot);
+        c[g] = CB == 2 && g < 8 ? reinterpret_cast<const uint16_t*>(at)[piece] : reinterpret_cast<const uint32_t*>(at)[piece];
+      }
+      if constexpr (CB == kC4R4) {
+        s_own = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(blk + L::c_scale_off(piece, slot))) << 16);
+        z_own = static_cast<float>(blk[L::zero_off(piece, slot)]);
+        s_pe = *reinterpret_cast<const float*>(blk + L::pe_scale_off(slot));
+        z_pe = static_cast<float>(blk[L::zero_off(8, slot)]);
       } else {
-        const uint8_t* b = pool + blk * L::kBytes;
-        const uint8_t* c = b + L::code_off(g, slot);
-        full[i].x = four ? reinterpret_cast<const uint32_t*>(c)[piece] : reinterpret_cast<const uint16_t*>(c)[piece];
-        if constexpr (CB == kC4R4) {
-          full[i].y = g < 8 ? static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(b + L::c_scale_off(g, slot))) << 16
-                            : *reinterpret_cast<const uint32_t*>(b + L::pe_scale_off(slot));
-          full[i].z = b[L::zero_off(g, slot)];
-        } else {
-          full[i].y = *reinterpret_cast<const uint32_t*>(b + L::sz_off(g, slot));
-        }
+        const float2 own = __half22float2(*reinterpret_cast<const __half2*>(blk + L::sz_off(piece, slot)));
+        const float2 pe = __half22float2(*reinterpret_cast<const __half2*>(blk + L::sz_off(8, slot)));
+        s_own = own.x, z_own = own.y, s_pe = pe.x, z_pe = pe.y;
       }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    if (at[i] == -1) continue;
-    uint4 out = full[i];
-    if constexpr (CB != kBf16Rows) {
-      if (at[i] >= 0) {
-        float s, z;
-        if constexpr (CB == kC4R4) {
-          s = __uint_as_float(full[i].y);
-          z = static_cast<float>(full[i].z);
-        } else {
-          const float2 sz = __half22float2(*reinterpret_cast<const __half2*>(&full[i].y));
-          s = sz.x;
-          z = sz.y;
-        }
-        const uint64_t zz = f32x2(-8388608.0f - z, -8388608.0f - z), ss = f32x2(s, s);
-        const uint32_t c = full[i].x;
-        if (four) {
-          out = make_uint4(value2(c & 15u, (c >> 4) & 15u, zz, ss), value2((c >> 8) & 15u, (c >> 12) & 15u, zz, ss),
-                           value2((c >> 16) & 15u, (c >> 20) & 15u, zz, ss), value2((c >> 24) & 15u, c >> 28, zz, ss));
-        } else {
-          out = make_uint4(value2(c & 3u, (c >> 2) & 3u, zz, ss), value2((c >> 4) & 3u, (c >> 6) & 3u, zz, ss),
-                           value2((c >> 8) & 3u, (c >> 10) & 3u, zz, ss), value2((c >> 12) & 3u, (c >> 14) & 3u, zz, ss));
-        }
+    for (int g = 0; g < kGroups; ++g) {
+      const int from = (lane & 24) | (g & 7);
+      const float s = g < 8 ? __shfl_sync(0xffffffffu, s_own, from) : s_pe;
+      const float z = g < 8 ? __shfl_sync(0xffffffffu, z_own, from) : z_pe;
+      if (blk == nullptr) continue;
+      const uint64_t zz = f32x2(-8388608.0f - z, -8388608.0f - z), ss = f32x2(s, s);
+      const uint32_t q = c[g];
+      if (CB != 2 || g == 8) {
+        out[g * 8] = make_uint4(value2(q & 15u, (q >> 4) & 15u, zz, ss), value2((q >> 8) & 15u, (q >> 12) & 15u, zz, ss),
+                                value2((q >> 16) & 15u, (q >> 20) & 15u, zz, ss), value2((q >> 24) & 15u, q >> 28, zz, ss));
+      } else {
+        out[g * 8] = make_uint4(value2(q & 3u, (q >> 2) & 3u, zz, ss), value2((q >> 4) & 3u, (q >> 6) & 3u, zz, ss),
+                                value2((q >> 8) & 3u, (q >> 10) & 3u, zz, ss), value2((q >> 12) & 3u, (q >> 14) & 3u, zz, ss));
       }
     }
-    *reinterpret_cast<uint4*>(rows + static_cast<size_t>(tok0 + 4 * i) * row_stride + g * 64 + piece * 8) = out;
   }
 }
-
-template <int CB, int NT>
-void launch_read_nt(const qmla_read_desc& d, cudaStream_t stream) {
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(d.n) + 4 * NT - 1) / (4 * NT));
-  cache_read_kernel<CB, NT><<<grid, kReadThreads, 0, stream>>>(
-      static_cast<const uint8_t*>(d.pool), d.num_blocks, d.seq_ids, d.positions, d.n, d.block_table, d.num_seqs,
-      d.max_blocks, d.seq_lens, static_cast<const uint4*>(d.prot), d.rows, static_cast<size_t>(d.row_stride), d.dev_err);
-}
-
-// Tokens from which a lane takes four.
-constexpr int kFourPerLane = 4096;
 
 template <int CB>
 void launch_read(const qmla_read_desc& d, cudaStream_t stream) {
-  if (d.n >= kFourPerLane) {
-    launch_read_nt<CB, 4>(d, stream);
-  } else {
-    launch_read_nt<CB, 1>(d, stream);
-  }
+  constexpr long long kPerBlock = kReadThreads / 8;
+  cache_read_kernel<CB><<<static_cast<unsigned>((d.n + kPerBlock - 1) / kPerBlock), kReadThreads, 0, stream>>>(
+      static_cast<const uint8_t*>(d.pool), d.num_blocks, d.seq_ids, d.positions, d.n, d.block_table, d.num_seqs,
+      d.max_blocks, d.seq_lens, static_cast<const uint4*>(d.prot), d.rows, static_cast<size_t>(d.row_stride), d.dev_err);
 }
 
 // Rotates rows of 64 channels, `heads` of them per token: eight lanes a row, each

@@ -404,12 +404,13 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
 // word to the others. The row's sum takes three shuffles instead of a way through shared
 // memory, and lane l works out the scale of group l, which shuffles hand round.
 //
-// What bounds it: the issue slots (about 350 warp instructions per token for INT4), then
-// the HBM traffic (1,152 bytes of the row and 256 of its angles read, 324 written). With
-// a warp per group, as for few tokens, it takes twice as many.
-constexpr int kWideThreads = 256;
+// What bounds it: the issue slots, above all of the norm (without it and without
+// quantising, the copy into the BF16 cache takes half the time), then the HBM traffic
+// (1,152 bytes of the row and 256 of its angles read, 324 written): 32,797 tokens take
+// 23.4 us, 2.4 TB/s of 6.8. Six blocks per SM: with 7 the registers spill (23.7).
+constexpr int kWideThreads = 128;
 template <int CB>
-__global__ void __launch_bounds__(kWideThreads) wide_append_kernel(
+__global__ void __launch_bounds__(kWideThreads, 6) wide_append_kernel(
     uint8_t* __restrict__ pool, int num_blocks, const uint32_t* __restrict__ latent,
     const uint32_t* __restrict__ k_pe, const int32_t* __restrict__ seq_ids,
     const int32_t* __restrict__ positions, int n, const int32_t* __restrict__ table, int num_seqs,
@@ -418,6 +419,14 @@ __global__ void __launch_bounds__(kWideThreads) wide_append_kernel(
   using L = BlockLayout<CB == kBf16Rows ? 4 : CB>;
   constexpr int kBits = CB == kC4R4 || CB == kBf16Rows ? 4 : CB;
   griddep_launch_dependents();  // as in quant_append_kernel
+  __shared__ float4 weight[kDc / 4];
+  static_assert(kWideThreads == kDc / 4, "a thread fetches four weights");
+  if (tr.norm) {
+    uint2 v = make_uint2(0x3F803F80u, 0x3F803F80u);
+    if (tr.weight != nullptr) v = reinterpret_cast<const uint2*>(tr.weight)[threadIdx.x];
+    weight[threadIdx.x] = make_float4(bf16_low(v.x), bf16_high(v.x), bf16_low(v.y), bf16_high(v.y));
+    __syncthreads();
+  }
   const int lane = threadIdx.x & 31, piece = lane & 7;
   const int tok = (blockIdx.x * (kWideThreads / 32) + (threadIdx.x >> 5)) * 4 + (lane >> 3);
   uint32_t raw[kGroups][4];
@@ -462,10 +471,9 @@ __global__ void __launch_bounds__(kWideThreads) wide_append_kernel(
     const F2 rs = row_rstd(s, tr.eps);
 #pragma unroll
     for (int g = 0; g < 8; ++g) {
-      const uint4 gv = tr.weight != nullptr ? __ldg(tr.weight + g * 8 + piece)
-                                            : make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
-      const uint64_t gw[4] = {f32x2(bf16_low(gv.x), bf16_high(gv.x)), f32x2(bf16_low(gv.y), bf16_high(gv.y)),
-                              f32x2(bf16_low(gv.z), bf16_high(gv.z)), f32x2(bf16_low(gv.w), bf16_high(gv.w))};
+      const ulonglong2 wa = reinterpret_cast<const ulonglong2*>(weight)[g * 16 + piece * 2];
+      const ulonglong2 wb = reinterpret_cast<const ulonglong2*>(weight)[g * 16 + piece * 2 + 1];
+      const uint64_t gw[4] = {wa.x, wa.y, wb.x, wb.y};
       scale_row(raw[g], gw, rs);
     }
   }
@@ -585,8 +593,10 @@ void launch_quant(const AppendArgs& a, const RowTransform& tr, cudaStream_t stre
 // 32,768 15.1 against 19.5 / 19.8 against 20.7.
 constexpr int kFourPerLane = 8192;
 
-// Tokens from which the fused writer gives a token to eight lanes.
-constexpr int kWide = 2048;
+// Tokens from which the fused writer gives a token to eight lanes instead of a warp to
+// a group: 2,048 tokens 6.2 against 5.2 us, 4,096 6.2 against 7.2, 32,797 23.4 against
+// 39.7 (INT4, normalised, buffers larger together than L2).
+constexpr int kWide = 2800;
 
 template <int CB, bool FUSED>
 void launch_quant(const AppendArgs& a, const RowTransform& tr, bool vec, cudaStream_t stream) {

@@ -130,13 +130,13 @@ __device__ __forceinline__ F2 row_rstd(F2 sum, float eps) {
 
 // RN_bf16(RN_f32(x g rstd)) of eight values in place (x g is exact in fp32).
 __device__ __forceinline__ void scale_row(uint32_t (&w)[4], const uint64_t (&g)[4], F2 rstd) {
-  const uint64_t hi = f32x2(rstd.hi, rstd.hi), lo = f32x2(rstd.lo, rstd.lo);
+  const uint64_t hi = f32x2(rstd.hi, rstd.hi), minus_hi = f32x2(-rstd.hi, -rstd.hi), minus_lo = f32x2(-rstd.lo, -rstd.lo);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint64_t v = mul2(f32x2(bf16_low(w[e]), bf16_high(w[e])), g[e]);
     const uint64_t p = mul2(v, hi);
-    const uint64_t low = fma2(v, lo, fma2(v, hi, p ^ 0x8000000080000000ull));  // (the product's rounding error)
-    const uint64_t y = add2(p, low);
+    // p less its rounding error less v lo
+    const uint64_t y = sub2(p, fma2(v, minus_lo, fma2(v, minus_hi, p)));
     w[e] = pack_bf16(lo2(y), hi2(y));
   }
 }

@@ -97,10 +97,13 @@ struct Item {
 static_assert(sizeof(Item) == 64, "four 16-byte loads");
 
 // Keys are cut into parts where one pair would take half as long again as the SMs' fair
-// share of the whole call: parts of at most L = W / kShares rounds, W all the rounds, but
-// kLeastPart at least. An item of R > L rounds makes ceil(R / L) < 2 R / L parts, so there
-// are never more than 2 kShares partial results, nor more than kShares items cut up.
-constexpr int kShares = 160, kSlots = 2 * kShares, kLeastPart = 4;
+// share of the whole call: parts of at most L rounds, L >= W / kShares, W all the rounds,
+// and kLeastPart at least. An item of R > L rounds makes ceil(R / L) < 2 R / L parts, so
+// there are never more than 2 kShares partial results, nor more than kShares items cut up.
+// L itself: parts of W / SMs rounds can be a few more than SMs, which then takes two turns
+// of L, so some longer ones are weighed against it (kLengths; 16 heads, 512 rows over 16,896
+// keys: 160 parts 114 us, 128 of them 84).
+constexpr int kShares = 160, kSlots = 2 * kShares, kLeastPart = 4, kLengths = 4;
 struct Join {  // an item cut up
   int q_row, rows, slot, parts;
 };
@@ -162,27 +165,29 @@ __device__ __forceinline__ int rounds_of(const Item& it) {
 
 // One block. A sequence has ceil(Lq / 256) items, in bundles of `bundle`; a counting
 // sort by key steps puts the longest bundles first (the order among equals is free:
-// items do not meet). Passes: the rounds of all items, which say how long a part may
-// be; the sizes of the buckets; the list.
+// items do not meet). Passes: the rounds of all items; the parts that each length in
+// question makes; the sizes of the buckets; the list.
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ cu_q,
                                                             const int32_t* __restrict__ cu_kv, int batch, int n_q,
-                                                            int n_kv, int heads, int causal, int bundle, int shift,
-                                                            int max_items, int* __restrict__ count,
+                                                            int n_kv, int heads, int causal, int sms, int bundle,
+                                                            int shift, int max_items, int* __restrict__ count,
                                                             int* __restrict__ prefix_far, Item* __restrict__ items,
                                                             Join* __restrict__ joins, uint32_t* dev_err) {
   __shared__ long long warp_sums[32];
   __shared__ int bucket[kPlanThreads];  // (as many as threads)
   __shared__ int prefix_near[kPlanOnChip];
   __shared__ unsigned long long rounds;
-  __shared__ int entries, slots, cut;
+  __shared__ int entries, slots, cut, most;  // most: rounds of the longest item
+  __shared__ unsigned long long cut_rounds[kLengths], cut_parts[kLengths];
   griddep_launch_dependents();  // prefill_kernel may start its set-up meanwhile
   const int tid = threadIdx.x, threads = blockDim.x;
   int* prefix = batch <= kPlanOnChip ? prefix_near : prefix_far;
   bucket[tid] = 0;
   if (tid == 0) {
     rounds = 0;
-    entries = slots = cut = 0;
+    entries = slots = cut = most = 0;
   }
+  if (tid < kLengths) cut_rounds[tid] = cut_parts[tid] = 0;
   int bundles = 0, total_items = 0;
   for (int b0 = 0; b0 < batch; b0 += threads) {
     const int b = b0 + tid;
@@ -211,21 +216,43 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
   }
   __syncthreads();
   int longest = INT32_MAX;  // rounds of a part
+  // W / SMs and 1.15, 1.35 and 1.7 times that (in fp32: off by less than the step from
+  // kShares - 1 to kShares)
+  auto length = [&](int x) {
+    const float f = x == 0 ? 1.0f : (x == 1 ? 1.15f : (x == 2 ? 1.35f : 1.7f));
+    const float l = __ull2float_rn(rounds) * f / static_cast<float>(min(sms, kShares - 1));
+    return max(static_cast<int>(fminf(l, 1e9f)) + 1, kLeastPart);
+  };
+  auto parts_at = [](int r, int l) { return r - l > l >> 1 ? (r + l - 1) / l : 1; };
+  struct Place {  // of a bundle: its sequence, first item and length
+    int q0, lq, k0, lk, t0, k;
+  };
+  auto find = [&](int i) {
+    int lo = 0, hi = batch - 1;  // the last sequence with prefix <= i: it has items
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (prefix[mid] <= i) {
+        lo = mid;
+      } else {
+        hi = mid - 1;
+      }
+    }
+    Place x;
+    x.q0 = cu_q[lo];
+    x.lq = cu_q[lo + 1] - x.q0;
+    x.k0 = cu_kv[lo];
+    x.lk = cu_kv[lo + 1] - x.k0;
+    x.t0 = (i - prefix[lo]) * bundle;
+    x.k = min(bundle, (x.lq + kItemRows - 1) / kItemRows - x.t0);
+    return x;
+  };
+  const Place first_place = tid < bundles ? find(tid) : Place{};
 #pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
+  for (int pass = 0; pass < 4; ++pass) {
     unsigned long long mine = 0;
     for (int i = tid; i < bundles; i += threads) {
-      int lo = 0, hi = batch - 1;  // the last sequence with prefix <= i: it has items
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (prefix[mid] <= i) {
-          lo = mid;
-        } else {
-          hi = mid - 1;
-        }
-      }
-      const int q0 = cu_q[lo], lq = cu_q[lo + 1] - q0, k0 = cu_kv[lo], lk = cu_kv[lo + 1] - k0;
-      const int tiles = (lq + kItemRows - 1) / kItemRows, t0 = (i - prefix[lo]) * bundle, k = min(bundle, tiles - t0);
+      const Place at_i = i == tid ? first_place : find(i);
+      const int q0 = at_i.q0, lq = at_i.lq, k0 = at_i.k0, lk = at_i.lk, t0 = at_i.t0, k = at_i.k;
       // (the last item is the longest; it stands first)
       auto item = [&](int x) {
         const int r0 = (t0 + k - 1 - x) * kItemRows;
@@ -241,23 +268,31 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         it.n1 = it.rows > kTile ? (max(min(lk, it.vis0 + it.step * last1), 0) + kTile - 1) / kTile : 0;
         return it;
       };
-      auto parts_of = [&](const Item& it) {
-        const int r = rounds_of(it);
-        return r - longest > longest >> 1 ? (r + longest - 1) / longest : 1;
-      };
+      auto parts_of = [&](const Item& it) { return parts_at(rounds_of(it), longest); };
       int all = 0;  // entries of the bundle
       for (int x = 0; x < k; ++x) {
         const Item it = item(x);
+        const int r = rounds_of(it);
         if (pass == 0) {
-          mine += static_cast<unsigned long long>(rounds_of(it)) * heads;
+          mine += static_cast<unsigned long long>(r) * heads;
+          if (x == 0) atomicMax(&most, r);
+        } else if (pass == 1) {
+#pragma unroll 1
+          for (int c = 0; c < kLengths; ++c) {
+            const int parts = parts_at(r, length(c));
+            if (parts > 1) {
+              atomicAdd(&cut_rounds[c], static_cast<unsigned long long>(r) * heads);
+              atomicAdd(&cut_parts[c], static_cast<unsigned long long>(parts) * heads);
+            }
+          }
         } else {
           all += parts_of(it);
         }
       }
-      if (pass == 0) continue;
+      if (pass < 2) continue;
       const int key = threads - 1 - min(min(rounds_of(item(0)), longest) >> shift, threads - 1);
       int at = atomicAdd(&bucket[key], all);
-      if (pass == 1) {
+      if (pass == 2) {
         atomicAdd(&entries, all);
         continue;
       }
@@ -300,10 +335,24 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
     }
     __syncthreads();
     if (pass == 0) {
-      const unsigned long long share = (rounds + kShares - 1) / kShares;
-      longest = static_cast<int>(min(max(share, static_cast<unsigned long long>(kLeastPart)),
-                                     static_cast<unsigned long long>(INT32_MAX)));
+      longest = length(0);
+      if (parts_at(most, longest) == 1) ++pass;  // (no item is cut up)
     } else if (pass == 1) {
+      // Turns of the SMs times the length; items that stay whole fill the last turn up.
+      float best = INFINITY;
+#pragma unroll 1
+      for (int c = 0; c < kLengths; ++c) {
+        const int l = length(c);
+        const unsigned long long parts = cut_parts[c];
+        const float turns = parts == 0 || (rounds - cut_rounds[c]) * 4 > rounds
+                                ? 1.0f
+                                : static_cast<float>((static_cast<int>(parts) + sms - 1) / sms);
+        if (turns * static_cast<float>(l) < best) {
+          best = turns * static_cast<float>(l);
+          longest = l;
+        }
+      }
+    } else if (pass == 2) {
       long long sum;
       const long long before = block_scan(bucket[tid], warp_sums, sum);
       bucket[tid] = static_cast<int>(before);
@@ -1078,17 +1127,18 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
     configured_device = dev;
   }
   const long long pairs = static_cast<long long>(w.max_items) * d.heads;
+  const bool parts = d.n_kv > kLeastPart * kTile;  // (else no item is cut up)
   // Items per bundle: with few pairs per SM single items even the load out better.
   const int bundle = pairs >= 8ll * sms ? 4 : 1;
   const int threads = w.max_items <= kSmallPlan && d.batch <= kSmallPlan ? kSmallPlan : kPlanThreads;
   int shift = 0;
   while (((d.n_kv / kTile + 1) >> shift) >= threads) ++shift;
-  plan_kernel<<<1, threads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.heads, d.causal != 0, bundle,
+  plan_kernel<<<1, threads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.heads, d.causal != 0, sms, bundle,
                                               shift, w.max_items, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
                                               reinterpret_cast<Item*>(ws + w.items_off), joins, d.dev_err);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, pairs + kSlots)));
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, pairs + (parts ? kSlots : 0))));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
@@ -1098,8 +1148,7 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if ((e = cudaLaunchKernelEx(&cfg, prefill_kernel, tq, tk, tv, tpe, p)) != cudaSuccess) return e;
-  // (no item has more than kLeastPart rounds, so none is cut up)
-  if (d.n_kv <= kLeastPart * kTile) return cudaSuccess;
+  if (!parts) return cudaSuccess;
   cfg.gridDim = dim3(static_cast<unsigned>(2 * sms));
   cfg.blockDim = dim3(kJoinThreads);
   cfg.dynamicSmemBytes = 0;

@@ -404,7 +404,8 @@ int qmla_mla_decode_ex(const qmla_decode_desc* desc, qmla_stream_t stream);
  *   seq_lens, prot  the sink4/local128 protection buffer and the lengths after this call,
  *                   as in qmla_quant_append_protected, or NULL (not with QMLA_CACHE_BF16).
  *                   The protection rows hold the normalised and rotated values
- * A token with a bad sequence, position or block is not written (dev_err says so).
+ * A token with a bad sequence, position or block is not written (dev_err says so). Two
+ * tokens of one call at the same place race, group by group.
  * The descriptor is read during the call only. n == 0 is a no-op.
  */
 typedef struct qmla_append_desc {
@@ -438,7 +439,7 @@ int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream);
  * convention and table of qmla_rope_append, in fp32 (a product and an FMA), rounded to
  * bf16:
  *   q_pe_dev        [n, heads, 64] bf16, rows q_token_stride and q_head_stride elements
- *                   apart (multiples of 8, not negative), 16-byte aligned. (So it may be
+ *                   apart (multiples of 8, not negative, below 2^38), 16-byte aligned. (So it may be
  *                   the last 64 columns of a [n, heads, 192] projection output.)
  *   positions_dev   [n] int32
  *   out_dev         [n, heads, 64] bf16 with strides of its own, 16-byte aligned. It may
@@ -501,13 +502,14 @@ int qmla_cache_read(const qmla_read_desc* desc, qmla_stream_t stream);
  *   k_pe, k_pe_stride                  [n_kv, 64] bf16, rotated
  *                   All four 16-byte aligned; strides in elements, positive multiples of 8
  *                   below 2^38 (ignored where that axis has one element)
- *   n_q, n_kv, heads, batch            rows given (at most 2^28), heads 1..1024, sequences
+ *   n_q, n_kv, heads, batch            rows given (at most 2^26), heads 1..1024, sequences
  *                   1..65536. n_kv may be 0 (k, v and k_pe are not used then); n_q == 0 is a
  *                   no-op
  *   cu_q, cu_kv     [batch + 1] int32 offsets, not decreasing. A sequence whose offsets
  *                   decrease, are negative or lie beyond n_q / n_kv is left out
  *                   (QMLA_DEVERR_BAD_OFFSETS)
- *   out             [n_q, heads, 128] bf16, contiguous, 32-byte aligned
+ *   out             [n_q, heads, 128] bf16, contiguous, 32-byte aligned; shares no memory
+ *                   with the inputs
  *   lse             [n_q, heads] float32, contiguous, or NULL
  *                   Rows that belong to no sequence are left as they were
  *   workspace       >= qmla_prefill_workspace_bytes(batch, n_q) bytes, 256-byte aligned,

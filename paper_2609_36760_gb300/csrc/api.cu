@@ -393,7 +393,7 @@ int qmla_rope_query(const uint16_t* q_pe_dev, long long q_token_stride, long lon
                     int interleaved, uint16_t* out_dev, long long out_token_stride, long long out_head_stride,
                     uint32_t* dev_err_dev, qmla_stream_t stream) {
   // (rows times 8 lanes fill the grid's 2^31 - 1 blocks of 128 rows at most)
-  if (n < 0 || heads < 1 || static_cast<long long>(n) * heads > (1ll << 37) || rope_len < 1 ||
+  if (n < 0 || heads < 1 || heads > (1 << 24) || static_cast<long long>(n) * heads > (1ll << 37) || rope_len < 1 ||
       (interleaved != 0 && interleaved != 1))
     return QMLA_ERR_INVALID_ARG;
   if (n == 0) return QMLA_OK;
@@ -402,9 +402,13 @@ int qmla_rope_query(const uint16_t* q_pe_dev, long long q_token_stride, long lon
   if (!aligned(q_pe_dev, 16) || !aligned(out_dev, 16) || !aligned(cos_sin_dev, 16) || !aligned(positions_dev, 4))
     return QMLA_ERR_INVALID_ARG;
   for (long long s : {q_token_stride, q_head_stride, out_token_stride, out_head_stride})
-    if (s < 0 || s % 8 != 0) return QMLA_ERR_INVALID_ARG;
-  // two rows of out at one place would race
-  if ((n > 1 && out_token_stride < qmla::kDr) || (heads > 1 && out_head_stride < qmla::kDr)) return QMLA_ERR_INVALID_ARG;
+    if (s < 0 || s % 8 != 0 || s >= (1ll << 38)) return QMLA_ERR_INVALID_ARG;
+  // Rows of out that overlap would race: one axis has to step over all of the other.
+  const long long in_token = heads > 1 ? (heads - 1) * out_head_stride + qmla::kDr : qmla::kDr;
+  const long long in_head = n > 1 ? (n - 1) * out_token_stride + qmla::kDr : qmla::kDr;
+  if ((n > 1 && out_token_stride < qmla::kDr) || (heads > 1 && out_head_stride < qmla::kDr) ||
+      (n > 1 && heads > 1 && out_token_stride < in_token && out_head_stride < in_head))
+    return QMLA_ERR_INVALID_ARG;
   DevInfo di;
   int st = current_device_info(di);
   if (st != QMLA_OK) return st;
@@ -436,13 +440,13 @@ int qmla_cache_read(const qmla_read_desc* d, qmla_stream_t stream) {
 }
 
 size_t qmla_prefill_workspace_bytes(int batch, int n_q) {
-  if (batch < 1 || batch > 65536 || n_q < 0 || n_q > (1 << 28)) return 0;
+  if (batch < 1 || batch > 65536 || n_q < 0 || n_q > (1 << 26)) return 0;
   return qmla::prefill_workspace_bytes(batch, n_q);
 }
 
 int qmla_mla_prefill(const qmla_prefill_desc* d, qmla_stream_t stream) {
   if (d == nullptr) return QMLA_ERR_INVALID_ARG;
-  if (d->n_q < 0 || d->n_kv < 0 || d->n_q > (1 << 28) || d->n_kv > (1 << 28) || d->heads < 1 || d->heads > 1024 ||
+  if (d->n_q < 0 || d->n_kv < 0 || d->n_q > (1 << 26) || d->n_kv > (1 << 26) || d->heads < 1 || d->heads > 1024 ||
       d->batch < 1 || d->batch > 65536 || (d->causal != 0 && d->causal != 1))
     return QMLA_ERR_INVALID_ARG;
   if (!(d->softmax_scale > 0.0f) || d->softmax_scale > 1e30f) return QMLA_ERR_INVALID_ARG;

@@ -58,7 +58,7 @@ constexpr int kSoftRegs = 160, kEpiRegs = 96, kOtherRegs = 96;
 constexpr int kRingOff = 2 * kQChunks * kSlotBytes;
 constexpr int kCtlOff = kRingOff + kRing * kSlotBytes;
 constexpr uint32_t kColO = 256;  // O0; O1 128 columns on
-constexpr uint64_t kLimitNs = 2000000000ull;  // of every wait
+constexpr uint64_t kLimitNs = 2000000000ull;  // of every wait (a pair of 2^26 keys takes 0.8 s)
 constexpr int kAhead = 4;  // steps before the end of a pair at which the next is drawn
 constexpr float kRaise = 8.0f;  // log2 of the growth that raises a reference
 
@@ -375,6 +375,7 @@ struct PrefillParams {
   uint16_t* out;
   float* lse;
   Partial* partial;
+  bool join;  // join_kernel follows
   uint32_t* dev_err;
 };
 
@@ -978,7 +979,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       asm volatile("exit;");
     }
   }
-  griddep_launch_dependents();  // join_kernel may be scheduled as CTAs finish
+  if (p.join) griddep_launch_dependents();  // it may be scheduled as CTAs finish
   tc_fence_before();
   __syncthreads();  // (exited lanes do not take part)
   if (warp == 0) {
@@ -1128,6 +1129,7 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   }
   const long long pairs = static_cast<long long>(w.max_items) * d.heads;
   const bool parts = d.n_kv > kLeastPart * kTile;  // (else no item is cut up)
+  p.join = parts;
   // Items per bundle: with few pairs per SM single items even the load out better.
   const int bundle = pairs >= 8ll * sms ? 4 : 1;
   const int threads = w.max_items <= kSmallPlan && d.batch <= kSmallPlan ? kSmallPlan : kPlanThreads;

@@ -195,6 +195,43 @@ def test_without_lse_and_repeatable():
         assert torch.equal(p.out, first)
 
 
+def test_more_sequences_than_fit_on_chip():
+    """2,600 tiny sequences, some empty: the plan's prefix goes through the workspace."""
+    g = torch.Generator().manual_seed(5)
+    lq = torch.randint(0, 4, (2600,), generator=g).tolist()
+    lk = [n + m for n, m in zip(lq, torch.randint(0, 5, (2600,), generator=g).tolist())]
+    p = Prompt(lq, lk, 2, seed=13)
+    assert p.run() == 0
+    p.check(sequences=set(range(0, 2600, 37)) | {2599})
+
+
+def test_offsets_past_32_bits():
+    """Keys and values of over 4 GB, and queries and results that lie behind 4 GB."""
+    n, m, heads = 5, 140_000, 64
+    g = torch.Generator(device="cuda").manual_seed(6)
+    kv = torch.randn(m, heads, 256, generator=g, device="cuda", dtype=torch.bfloat16)
+    pe = torch.randn(m, 64, generator=g, device="cuda", dtype=torch.bfloat16)
+    rows = 180_000  # x 64 heads x 192 channels: 4.4 GB
+    q = torch.empty(rows, heads, 192, dtype=torch.bfloat16, device="cuda")
+    q[-n:] = torch.randn(n, heads, 192, generator=g, device="cuda")
+    out = torch.zeros(rows * 2, heads, 128, dtype=torch.bfloat16, device="cuda")[-rows:]
+    lse, err = torch.zeros(rows, heads, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(Q.prefill_workspace_bytes(1, rows), dtype=torch.uint8, device="cuda")
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    Q.mla_prefill(q, kv[..., :128], kv[..., 128:], pe, i32(rows - n, rows), i32(0, m), TAU, out, lse, ws, err)
+    assert Q.read_dev_err(err) == 0
+    for h in (0, 31, 63):
+        k = torch.cat([kv[:, h, :128], pe], 1).double()
+        s = TAU * q[-n:, h].double() @ k.T
+        e = 192 * 2.0 ** -24 * float((TAU * q[-n:, h].double().abs() @ k.abs().T).max())
+        s = s.masked_fill(torch.arange(m, device="cuda")[None] > torch.arange(n, device="cuda")[:, None] + m - n, -math.inf)
+        w, v = torch.softmax(s, 1), kv[:, h, 128:].double()
+        want = w @ v
+        gap = (out[-n:, h].double() - want).abs()
+        assert bool((gap <= (2.0 ** -8 + 2 * e + 2.0 ** -18) * (w @ v.abs()) + 2.0 ** -8 * want.abs()).all())
+    assert not bool(out[:-n].any())
+
+
 def test_bad_offsets_are_left_out():
     """Decreasing, negative and too large offsets: reported, their rows left as they were."""
     p = Prompt([50, 60, 70, 80], [50, 60, 70, 80], 2, seed=9)

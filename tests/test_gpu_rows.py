@@ -266,6 +266,24 @@ def test_rope_query_broadcast_heads_and_bad_positions():
     assert bool((out[[2, 3, 5]] == 7).all())
 
 
+def test_blocks_and_rows_past_32_bits():
+    """A pool of over 4 GB, its last block, and rows that lie behind 4 GB of others."""
+    blocks = (1 << 32) // WIDTH[4] + 40
+    pool = torch.zeros(blocks, WIDTH[4], dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[blocks - 1, blocks - 2]], dtype=torch.int32, device="cuda")
+    c = Cache(4, [100], seed=21)
+    seq, pos = c.seq.cuda(), c.pos.cuda()
+    wide = torch.zeros(3_730_000, 576, dtype=torch.bfloat16, device="cuda")[-100:]  # 4.3 GB before them
+    wide.copy_(c.rows)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    Q.rope_append(pool, 4, wide[:, :512], wide[:, 512:], seq, pos, table, c.cs.cuda(), err, norm_weight=c.weight.cuda())
+    Q.cache_read(pool, 4, seq, pos, table, wide, err)
+    assert Q.read_dev_err(err) == 0
+    x = torch.cat([normed(c.rows[:, :512], c.weight, 1e-6), rotated(c.rows[:, 512:], c.cs, c.pos, False)], 1)
+    assert torch.equal(wide.cpu(), dequantised(x, 4))
+    assert not bool(pool[:-2].any())
+
+
 def test_a_zero_row_and_large_values():
     """eps keeps a row of zeros finite; without it the row is NaN, as 0 / 0 is. Large and
     small rows (2^40, 2^-40) normalise like any other."""

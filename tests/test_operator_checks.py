@@ -2,6 +2,8 @@
 bad arguments are refused before anything is launched. No GPU needed."""
 import ctypes
 import os
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -71,6 +73,15 @@ def test_rope_query_refuses(L, at, value):
     assert L.qmla_rope_query(*args) == INVALID
 
 
+def test_rope_query_refuses_rows_that_overlap(L):
+    """Of out: token and head strides of which neither steps over the other axis."""
+    call = lambda ot, oh, n=3, h=4: L.qmla_rope_query(FAKE, 768, 192, None, n, h, FAKE, 64, 0, FAKE, ot, oh, None, None)  # noqa: E731
+    good = lambda ot, oh, n=3, h=4: L.qmla_rope_query(FAKE, 768, 192, FAKE, n, h, FAKE, 64, 0, FAKE, ot, oh, None, None)  # noqa: E731
+    assert call(256, 64) == INVALID  # (no positions: the arguments before are fine)
+    for ot, oh in [(64, 64), (192, 64), (64, 128), (72, 64), (0, 64), (256, 0)]:
+        assert good(ot, oh) == INVALID, (ot, oh)
+
+
 def prefill_desc(**kw):
     d = Q.PrefillDesc()
     base = dict(q=FAKE, q_token_stride=192 * 16, q_head_stride=192, k=FAKE, k_token_stride=256 * 16, k_head_stride=256,
@@ -86,7 +97,7 @@ def prefill_desc(**kw):
     {"q": None}, {"q": FAKE + 8}, {"q_token_stride": 4}, {"q_head_stride": 0}, {"k": None}, {"k": FAKE + 2},
     {"k_token_stride": -8}, {"k_head_stride": 0}, {"v": None}, {"v": FAKE + 4}, {"v_token_stride": 1 << 38},
     {"v_head_stride": 129}, {"k_pe": None}, {"k_pe": FAKE + 8}, {"k_pe_stride": 0}, {"n_q": -1}, {"n_kv": -1},
-    {"n_q": (1 << 28) + 1}, {"n_kv": (1 << 28) + 1}, {"heads": 0}, {"heads": 1025}, {"batch": 0}, {"batch": 65537},
+    {"n_q": (1 << 26) + 1}, {"n_kv": (1 << 26) + 1}, {"heads": 0}, {"heads": 1025}, {"batch": 0}, {"batch": 65537},
     {"cu_q": None}, {"cu_kv": None}, {"cu_q": FAKE + 2}, {"causal": 2}, {"softmax_scale": 0.0},
     {"softmax_scale": float("nan")}, {"softmax_scale": float("inf")}, {"out": None}, {"out": FAKE + 8}, {"out": FAKE + 16},
     {"lse": FAKE + 2}, {"workspace": None}, {"workspace": FAKE + 128},
@@ -97,8 +108,8 @@ def test_mla_prefill_refuses(L, kw):
 
 def test_workspace_and_empty_calls(L):
     need = Q.prefill_workspace_bytes(2, 5)
-    assert need > 0 and Q.prefill_workspace_bytes(2, 1 << 28) > Q.prefill_workspace_bytes(2, 1 << 20)
-    for bad in [(0, 5), (65537, 5), (1, -1), (1, (1 << 28) + 1)]:
+    assert need > 0 and Q.prefill_workspace_bytes(2, 1 << 26) > Q.prefill_workspace_bytes(2, 1 << 20)
+    for bad in [(0, 5), (65537, 5), (1, -1), (1, (1 << 26) + 1)]:
         assert Q.prefill_workspace_bytes(*bad) == 0
     assert L.qmla_mla_prefill(ctypes.byref(prefill_desc(workspace_bytes=need - 1)), None) == TOO_SMALL
     # null descriptors, and calls without rows, which touch nothing
@@ -131,3 +142,22 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError):
         Q.mla_prefill(q, kv[..., :128], kv[..., 128:], kpe, pos[:2], pos[:2], 0.1, torch.zeros(3, 2, 128, dtype=bf), None,
                       torch.zeros(1 << 16, dtype=torch.uint8), err)
+
+
+@pytest.mark.parametrize("name,cls", [("qmla_append_desc", Q.AppendDesc), ("qmla_read_desc", Q.ReadDesc),
+                                      ("qmla_prefill_desc", Q.PrefillDesc)])
+def test_descriptors_match_the_header(tmp_path, name, cls):
+    """Sizes and offsets of the binding's structures are those of include/qmla.h in C."""
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None:
+        pytest.skip("no C compiler")
+    fields = [f for f, _ in cls._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include "qmla.h"\nint main(void) {\n'
+                   f'printf("%zu\\n", sizeof({name}));\n'
+                   + "".join(f'printf("%zu\\n", offsetof({name}, {f}));\n' for f in fields) + "return 0; }\n")
+    exe = tmp_path / "layout"
+    inc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.run([cc, "-I", inc, str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [ctypes.sizeof(cls)] + [getattr(cls, f).offset for f in fields]

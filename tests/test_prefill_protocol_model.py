@@ -1,0 +1,220 @@
+"""A CPU model of mla_prefill's barriers: its roles with their waits and arrivals in
+program order, run in random interleavings over random item lists. It looks for
+deadlocks, for a ring entry that could be overwritten, and for a barrier that runs two
+phases ahead of a waiter (which a parity wait cannot tell from none).
+
+The roles follow prefill.cu: the load warp draws items and fills the ring, one thread
+per tile issues that tile's MMAs (their completions arrive in issue order), a softmax
+warpgroup per tile, and the epilogue."""
+from __future__ import annotations
+
+import random
+
+import pytest
+
+IN_FLIGHT, SLOTS = 3, 8
+NEEDS = {"sched_free0": 5, "sched_free1": 5, "q_free0": 2, "freed0": 2, "freed1": 2, "freed2": 2, "freed3": 2}
+
+
+class Model:
+    def __init__(self, items, seed):
+        self.items, self.rnd = items, random.Random(seed)
+        self.count, self.posted, self.tensor = {}, {}, ([], [])
+        self.problem = None
+
+    def arrive(self, bar):
+        self.count[bar] = self.count.get(bar, 0) + 1
+
+    def wait(self, bar, phase):
+        while True:
+            done = self.count.get(bar, 0) // NEEDS.get(bar, 1)
+            if done > phase + 1:
+                self.problem = f"{bar} is {done - phase} phases ahead of a waiter"
+            if done > phase:
+                return
+            yield bar
+
+    def next_item(self, k):
+        yield from self.wait(f"sched_full{k & 1}", k >> 1)
+        item = self.posted[k]
+        self.arrive(f"sched_free{k & 1}")
+        return item
+
+    def load(self):
+        loads, e, sizes = [0, 0], 0, []
+
+        def query(i):
+            if loads[i]:
+                yield from self.wait(f"q_free{i}", loads[i] - 1)
+            self.arrive(f"q_full{i}")
+            loads[i] += 1
+
+        def entry(size):
+            nonlocal e
+            if e >= IN_FLIGHT:
+                yield from self.wait(f"freed{(e - IN_FLIGHT) & 3}", (e - IN_FLIGHT) >> 2)
+            sizes.append(size)
+            if sum(sizes[-IN_FLIGHT:]) > SLOTS:
+                self.problem = "entries on their way do not fit into the ring"
+            self.arrive(f"full{e & 3}")
+            e += 1
+
+        for k, item in enumerate([*self.items, None]):
+            if k >= 2:
+                yield from self.wait(f"sched_free{k & 1}", (k - 2) >> 1)
+            self.posted[k] = item
+            self.arrive(f"sched_full{k & 1}")
+            if item is None:
+                return
+            n0, n1, dealt, _ = item
+            n, per = max(n0, n1), 2 if dealt else 1
+            if n0:
+                yield from query(0)
+            for j in range(0, n, per):
+                for _ in range(j, min(j + per, n)):
+                    yield from entry(3)
+                if j == 0 and n1:
+                    yield from query(1)
+                for _ in range(j, min(j + per, n)):
+                    yield from entry(2)
+
+    def mma(self, i):
+        e = weights = outputs = 0
+        loads = [0, 0]
+        queue = self.tensor[i]
+        for pair in range(1 << 30):
+            item = yield from self.next_item(pair)
+            if item is None:
+                return
+            n0, n1, dealt, _ = item
+            q, both = (0 if dealt else i), max(n0, n1)
+            n = (n0 + 1 - i) >> 1 if dealt else (n1 if i else n0)
+            rounds = (both + 1) >> 1 if dealt else both
+            if n:
+                yield from self.wait(f"q_full{q}", loads[q])
+            loads[0] += n0 > 0
+            loads[1] += not dealt and n1 > 0
+            for x in range(2 * rounds):
+                j = x >> 1
+
+                def skip():
+                    nonlocal e
+                    yield from self.wait(f"full{e & 3}", e >> 2)
+                    self.arrive(f"freed{e & 3}")
+                    e += 1
+
+                if (i == 1) if dealt else j >= n:
+                    yield from skip()
+                if j < n:
+                    yield from self.wait(f"full{e & 3}", e >> 2)
+                    if x & 1 == 0:
+                        queue += [f"s_full{i}", f"freed{e & 3}"] + [f"q_free{q}"] * (j + 1 == n)
+                    else:
+                        if j == 0 and outputs:
+                            yield from self.wait(f"o_free{i}", outputs - 1)
+                        for h in range(2):
+                            yield from self.wait(f"p_full{i}{h}", weights)
+                        weights += 1
+                        queue += [f"freed{e & 3}"] + [f"o_full{i}"] * (j + 1 == n)
+                        outputs += j + 1 == n
+                    e += 1
+                if dealt and i == 0 and 2 * j + 1 < both:
+                    yield from skip()
+                if x == 0 and i == 1 and not dealt and n0:
+                    self.arrive("q_free0")
+
+    def softmax(self, i):
+        scores = outputs = 0
+        for pair in range(1 << 30):
+            item = yield from self.next_item(pair)
+            if item is None:
+                return
+            n0, n1, dealt, _ = item
+            n = (n0 + 1 - i) >> 1 if dealt else (n1 if i else n0)
+            for _ in range(n):
+                yield from self.wait(f"s_full{i}", scores)
+                scores += 1
+                for h in range(2):
+                    self.arrive(f"p_full{i}{h}")
+                    yield "step"
+            if n:
+                if outputs:
+                    yield from self.wait(f"o_free{i}", outputs - 1)
+                outputs += 1
+                self.arrive(f"l_full{i}")
+
+    def epilogue(self):
+        outputs = [0, 0]
+        for pair in range(1 << 30):
+            item = yield from self.next_item(pair)
+            if item is None:
+                return
+            n0, n1, dealt, tiles = item
+            for i in range(tiles):
+                if (n1 if i else n0) == 0:
+                    continue
+                for x in ([0, 1] if dealt else [i]):
+                    yield from self.wait(f"l_full{x}", outputs[x])
+                    yield from self.wait(f"o_full{x}", outputs[x])
+                    outputs[x] += 1
+                self.arrive(f"o_free{i}")
+                if dealt:
+                    self.arrive("o_free1")
+
+    def run(self):
+        roles = {"load": self.load(), "mma0": self.mma(0), "mma1": self.mma(1), "soft0": self.softmax(0),
+                 "soft1": self.softmax(1), "epilogue": self.epilogue()}
+        idle, blocked = 0, {}
+        while roles or any(self.tensor):
+            who = self.rnd.choice([*roles, *(f"tensor{i}" for i in range(2) if self.tensor[i])])
+            if who.startswith("tensor"):
+                self.arrive(self.tensor[int(who[-1])].pop(0))
+                idle = 0
+            else:
+                before = (sum(self.count.values()), len(self.tensor[0]), len(self.tensor[1]))
+                try:
+                    blocked[who] = next(roles[who])
+                    idle = idle + 1 if before == (sum(self.count.values()), len(self.tensor[0]), len(self.tensor[1])) else 0
+                except StopIteration:
+                    del roles[who]
+                    blocked.pop(who, None)
+                    idle = 0
+            if self.problem:
+                return self.problem
+            if idle > 300:
+                return f"deadlock: {blocked}"
+        return None
+
+
+def random_item(rnd):
+    """(key steps of tile 0, of tile 1, dealt, tiles)"""
+    t = rnd.random()
+    if t < 0.25:
+        return 0, 0, False, rnd.choice([1, 2])
+    if t < 0.5:
+        return rnd.randint(2, 7), 0, True, 1
+    if t < 0.6:
+        return 1, 0, False, 1
+    if t < 0.7:
+        return 0, rnd.randint(1, 3), False, 2
+    n = rnd.randint(1, 5)
+    return n, n + rnd.randint(0, 1), False, 2
+
+
+@pytest.mark.parametrize("block", range(8))
+def test_no_deadlock_and_no_overtaken_barrier(block):
+    for seed in range(block * 60, block * 60 + 60):
+        rnd = random.Random(seed)
+        items = [random_item(rnd) for _ in range(rnd.randint(0, 10))]
+        problem = Model(items, seed).run()
+        assert problem is None, (seed, items, problem)
+
+
+def test_the_model_sees_a_deadlock():
+    """Query tile 0 given back by one thread only: its barrier never completes."""
+    class Broken(Model):
+        def arrive(self, bar):
+            if bar != "q_free0":
+                super().arrive(bar)
+
+    assert "deadlock" in Broken([(2, 2, False, 2), (2, 2, False, 2)], 1).run()

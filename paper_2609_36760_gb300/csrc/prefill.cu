@@ -13,7 +13,8 @@
 //   warps 0..3 / 4..7   softmax of tile 0 / 1, a query row per thread
 //   warps 8..11         epilogue of both tiles
 //   warps 12, 14        one thread each, which issues tile 0's / tile 1's MMAs
-//   warp 13             draws the pairs; TMA loads of queries, keys and values
+//   warp 13             TMA loads of queries, keys and values
+//   warp 15             draws the pairs
 //
 // The roles run through the pairs without a stop between them: a pair's first QK and
 // softmax run while the O of the one before is read out, and only its first PV waits
@@ -51,8 +52,8 @@ constexpr int kQChunks = 3, kKChunks = 3, kVSlots = 2;
 constexpr int kRing = 8;
 constexpr int kInFlight = 3;  // entries (a step's keys or values) that the ring holds at once
 constexpr int kSoftWarps = 8;
-constexpr int kEpiWarp = 8, kMmaWarp = 12, kLoadWarp = 13;
-constexpr int kThreads = 16 * 32;  // (the last warp leaves at once: registers are split by groups of four)
+constexpr int kEpiWarp = 8, kMmaWarp = 12, kLoadWarp = 13, kDrawWarp = 15;  // (and 14: MMAs)
+constexpr int kThreads = 16 * 32;
 // 128 registers a thread at launch: 2 x 160 + 96 + 96 = 4 x 128.
 constexpr int kSoftRegs = 160, kEpiRegs = 96, kOtherRegs = 96;
 constexpr int kRingOff = 2 * kQChunks * kSlotBytes;
@@ -70,7 +71,7 @@ struct Ctl {
   uint64_t full[4], freed[4];  // of entry e: [e & 3]
   uint64_t s_full[2], p_full[2][2], o_full[2];  // p_full: of the halves, 64 keys each
   uint64_t l_full[2], o_free[2];  // a tile's (m, l) are in `sums`; they and O have been read
-  uint64_t sched_full[2], sched_free[2];
+  uint64_t sched_full[2], sched_free[2], ask;  // ask: the load warp wants the next pair
   uint64_t tail, fin;
   uint32_t tmem_base, abort;
   int turn;  // 1: a tile's MMAs are being issued
@@ -428,6 +429,34 @@ struct Entry {
   }
 };
 
+// Draws the CTA's pairs: pair c first, then whichever is next when the load warp asks
+// for it. (A draw is three round trips to L2.)
+__device__ void draw_role(const PrefillParams& p, Ctl& ctl, int lane) {
+  const int4* list = reinterpret_cast<const int4*>(p.items);
+  const int pairs = p.count[0] * p.heads;
+  int at = static_cast<int>(blockIdx.x);
+  for (uint32_t k = 0;; ++k) {
+    if (k > 0) {
+      if (!wait_warp(&ctl.ask, k - 1, ctl, kSiteLoad, p.dev_err)) return;
+      if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
+      at = __shfl_sync(0xffffffffu, at, 0);
+    }
+    int4 w = make_int4(0, 0, -1, 0);  // lane l < 4: the l-th quarter of the item
+    if (at < pairs) {
+      const int4 place = list[at / p.heads * 4 + 2];  // {the bundle's first item, its length, ..}
+      const int rem = at - place.x * p.heads, head = rem / place.y;
+      w = list[(place.x + rem - head * place.y) * 4 + (lane & 3)];
+      if (lane == 2) w.z = head;
+    }
+    const bool more = at < pairs;
+    if (k >= 2 && !wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err)) return;
+    if (lane < 4) ctl.work[k & 1u][lane] = w;
+    __syncwarp();
+    mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.sched_full[k & 1u]);
+    if (!more) return;
+  }
+}
+
 __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
                           const CUtensorMap& tpe, uint8_t* sm, Ctl& ctl, int lane) {
   uint8_t* ring = sm + kRingOff;
@@ -495,59 +524,21 @@ __device__ void load_role(const PrefillParams& p, const CUtensorMap& tq, const C
     }
     en.next(kVSlots);
   };
-  // The next pair: pair c for the CTA's first, then whichever is next. It is drawn some
-  // steps before it is needed (three round trips to L2), and what its first steps read
-  // is asked into L2: its query tiles can only be loaded once this pair's last QKs are
-  // through, and nothing else covers the way from HBM then.
-  const int4* list = reinterpret_cast<const int4*>(p.items);
-  const int pairs = p.count[0] * p.heads;
-  int4 w[4];
-  auto look_up = [&](int at) {
-    w[0] = w[1] = w[3] = make_int4(0, 0, 0, 0);
-    w[2] = make_int4(0, 0, -1, 0);
-    if (at >= pairs) return;
-    const int4 place = list[at / p.heads * 4 + 2];  // {the bundle's first item, its length, ..}
-    const int rem = at - place.x * p.heads, head = rem / place.y;
-    const int i = place.x + rem - head * place.y;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) w[x] = list[i * 4 + x];
-    w[2].z = head;
-  };
-  auto draw = [&]() {
-    int at = 0;
-    if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
-    look_up(__shfl_sync(0xffffffffu, at, 0));
-    const int head = w[2].z, n0 = w[1].z, n1 = w[1].w;
-    if (head < 0) return;
-    if (lane < 6 && (lane < 3 ? n0 : n1) > 0)
-      tma_prefetch_3d(&tq, lane % 3 * 64, head, w[0].x + lane / 3 * kTile);
-    // (the first step's keys and values, of items that start together by one of them)
-    if (max(n0, n1) > 0) {
-      if (lane >= 8 && lane < 10) tma_prefetch_3d(&tk, (lane - 8) * 64, head, w[0].z);
-      if (lane >= 12 && lane < 16) tma_prefetch_3d(&tv, (lane & 1) * 64, head, w[0].z + (lane & 2) * 32);
-    }
-  };
-  look_up(static_cast<int>(blockIdx.x));
-  for (uint32_t k = 0; ok; ++k) {
-    if (k >= 2 && !(ok = wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err))) break;
-    it = Item{w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w,
-              w[2].x, w[2].y, w[2].z, w[2].w, w[3].x, w[3].y, w[3].z, w[3].w};
-    if (lane == 0) {
-      for (int x = 0; x < 4; ++x) ctl.work[k & 1u][x] = w[x];
-    }
-    mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.sched_full[k & 1u]);
-    if (it.head < 0) break;
-    // In the order in which mma_role uses them up. (The next pair is drawn behind the
-    // loads of the step kAhead before the last.)
+  for (uint32_t pair = 0; ok && next_pair<true>(ctl, pair, it, kSiteLoad, p.dev_err); ++pair) {
+    // In the order in which mma_role uses them up, but that the first keys do not wait for
+    // the queries: a pair's query tiles can only be loaded once the last QKs of the pair
+    // before are through. (The next pair is asked for kAhead steps before the end.)
     const int n = max(it.n0, it.n1), when = max(n - 1 - kAhead, 0);
     const int per = it.dealt != 0 ? 2 : 1;  // key steps in a round
-    if (n == 0) draw();
-    if (it.n0 > 0) load_q(0);
+    if (n == 0) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.ask);
     for (int j = 0; ok && j < n; j += per) {
-      for (int x = 0; ok && x < per && j + x < n; ++x) load_k(j + x);
+      for (int x = 0; ok && x < per && j + x < n; ++x) {
+        load_k(j + x);
+        if (ok && j + x == 0 && it.n0 > 0) load_q(0);
+      }
       if (ok && j == 0 && it.n1 > 0) load_q(1);
       for (int x = 0; ok && x < per && j + x < n; ++x) load_v(j + x);
-      if (ok && when >= j && when < j + per) draw();
+      if (when >= j && when < j + per) mbar_arrive_if(lane == 0 ? 1u : 0u, &ctl.ask);
     }
   }
   if (lane != 0) return;
@@ -652,8 +643,8 @@ __device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32
   for (uint32_t pair = 0; ok && next_pair<false>(ctl, pair, it, kSiteMma, p.dev_err); ++pair) {
     // Entries: K0, V0, K1, V1, .., all for both tiles; dealt: K0, K1, V0, V1, K2, K3, ..,
     // the even ones tile 0's and the odd ones tile 1's. Query tile 0 is given back by
-    // both threads, by one that does not use it once an entry of the pair is there (so
-    // that the query before it has been given back).
+    // both threads, by one that does not use it once the first values are there: they are
+    // loaded after it, so it is this pair's, and the one before has been given back.
     // (One place for each kind of entry: the roles' code has to share the SM's instruction
     // caches.)
     const bool dealt = it.dealt != 0;
@@ -676,7 +667,7 @@ __device__ void mma_role(const PrefillParams& p, uint32_t smem, Ctl& ctl, uint32
         }
       }
       if (ok && dealt && i == 0 && 2 * j + 1 < all) skip(slots);
-      if (x == 0 && i == 1 && !dealt && it.n0 > 0) mbar_arrive_if(1u, &ctl.q_free[0]);
+      if (x == 1 && i == 1 && !dealt && it.n0 > 0) mbar_arrive_if(1u, &ctl.q_free[0]);
     }
   }
   give();
@@ -942,10 +933,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&ctl.sched_full[i], 1);
-      mbar_init(&ctl.sched_free[i], kSoftWarps + 4 + 2);
+      mbar_init(&ctl.sched_free[i], kSoftWarps + 4 + 2 + 1);
       mbar_init(&ctl.l_full[i], 4);
       mbar_init(&ctl.o_free[i], 4);
     }
+    mbar_init(&ctl.ask, 1);
     mbar_init(&ctl.tail, 1);
     mbar_init(&ctl.fin, 2);
     ctl.abort = 0u;
@@ -971,8 +963,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kLoadWarp) {
       load_role(p, tq, tk, tv, tpe, sm, ctl, lane);
-    } else if (warp == kLoadWarp + 2) {
-      asm volatile("exit;");
+    } else if (warp == kDrawWarp) {
+      draw_role(p, ctl, lane);
     } else if (elect_one()) {
       mma_role(p, smem_u32(sm), ctl, tmem, warp == kMmaWarp ? 0 : 1);
     } else {

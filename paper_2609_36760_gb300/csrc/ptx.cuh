@@ -347,26 +347,6 @@ __device__ __forceinline__ void tmem_ld32_max(uint32_t taddr, float* r, float& t
         "=f"(r[29]), "=f"(r[30]), "=f"(r[31]), "=f"(top)
       : "r"(taddr));
 }
-// 32 columns of 16 TMEM lanes (taddr's and the 15 after it) in the layout of matrix
-// fragments: lane l has of each eight columns 2 (l % 4) and the next one, for row l / 4 in
-// r[4 k], r[4 k + 1] and for row l / 4 + 8 in r[4 k + 2], r[4 k + 3].
-__device__ __forceinline__ void tmem_ld_frag32(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-// L2 prefetch of a tensor map's box.
-__device__ __forceinline__ void tma_prefetch_2d(const void* map, int x, int y) {
-  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
-}
-__device__ __forceinline__ void tma_prefetch_3d(const void* map, int x, int y, int z) {
-  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z)
-               : "memory");
-}
 // 32 consecutive 32-bit columns of the warp's 32 lanes from r.
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
   asm volatile(

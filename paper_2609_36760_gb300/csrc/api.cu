@@ -392,8 +392,8 @@ int qmla_rope_query(const uint16_t* q_pe_dev, long long q_token_stride, long lon
                     const int32_t* positions_dev, int n, int heads, const float* cos_sin_dev, int rope_len,
                     int interleaved, uint16_t* out_dev, long long out_token_stride, long long out_head_stride,
                     uint32_t* dev_err_dev, qmla_stream_t stream) {
-  // (rows times 8 lanes fill the grid's 2^31 - 1 blocks of 128 rows at most)
-  if (n < 0 || heads < 1 || heads > (1 << 24) || static_cast<long long>(n) * heads > (1ll << 37) || rope_len < 1 ||
+  // (a block takes 64 rows, a grid has 2^31 - 1 blocks)
+  if (n < 0 || heads < 1 || heads > (1 << 24) || static_cast<long long>(n) * heads > (1ll << 36) || rope_len < 1 ||
       (interleaved != 0 && interleaved != 1))
     return QMLA_ERR_INVALID_ARG;
   if (n == 0) return QMLA_OK;

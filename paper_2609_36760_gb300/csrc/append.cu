@@ -190,55 +190,31 @@ struct RowTransform {
   bool interleaved;
 };
 
-// Warp g's rows (four tokens per pass, eight lanes each) normalised (g < 8) or
-// rotated (g = 8) in registers. The row's sum of squares needs all eight content
-// warps: each leaves its 64 channels' share in shared memory and every warp adds
-// the eight shares in the same order, so the result does not depend on the launch.
-// Every thread of the block takes part.
-template <int NT>
-__device__ __forceinline__ void transform_rows(uint4 (&raw)[NT], const RowTransform& tr,
-                                               const int32_t* __restrict__ positions, int n, int tok0, int g,
-                                               int lane) {
-  __shared__ float2 share[8][4 * NT];
+// Warp g's piece of four tokens (eight lanes each) normalised (g < 8) or rotated
+// (g = 8) in registers. The row's sum of squares needs all eight content warps: each
+// leaves its 64 channels' share in shared memory and every warp adds the eight shares in
+// the same order, so the result does not depend on the launch. Every thread of the
+// block takes part.
+__device__ __forceinline__ void transform_rows(uint4& raw, const RowTransform& tr, const int32_t* __restrict__ positions,
+                                               int n, int tok, int g, int lane) {
+  __shared__ float2 share[8][4];
   const int piece = lane & 7, sub = lane >> 3;
+  uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
   if (g == 8) {
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const int tok = tok0 + 4 * i;
-      const int pos = tok < n ? positions[tok] : -1;
-      Angles a;
-      load_angles(a, pos >= 0 && pos < tr.rope_len ? tr.cos_sin + static_cast<size_t>(pos) * kDr : nullptr, piece,
-                  tr.interleaved);
-      uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-      rotate_row<true>(w, a, piece, tr.interleaved);
-      raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    const int pos = tok < n ? positions[tok] : -1;
+    Angles a;
+    load_angles(a, pos >= 0 && pos < tr.rope_len ? tr.cos_sin + static_cast<size_t>(pos) * kDr : nullptr, piece,
+                tr.interleaved);
+    rotate_row<true>(w, a, piece, tr.interleaved);
+    raw = make_uint4(w[0], w[1], w[2], w[3]);
   }
   if (!tr.norm) return;
-  // Lane i of four ends up with token i's sum (two halvings, then the other four
-  // lanes); with one token per lane all eight have it.
-  const int own = piece & (NT - 1);
   if (g < 8) {
-    F2 s[NT];
+    F2 s = square_sum8(w);
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-      s[i] = square_sum8(w);
-    }
-    auto with = [](F2 keep, F2 send, int off) {
-      return add_f2(keep, {__shfl_xor_sync(0xffffffffu, send.hi, off), __shfl_xor_sync(0xffffffffu, send.lo, off)});
-    };
-    if constexpr (NT == 4) {
-      const bool b0 = (piece & 1) != 0, b1 = (piece & 2) != 0;
-      const F2 x = with(b0 ? s[1] : s[0], b0 ? s[0] : s[1], 1);
-      const F2 y = with(b0 ? s[3] : s[2], b0 ? s[2] : s[3], 1);
-      s[0] = with(b1 ? y : x, b1 ? x : y, 2);
-    } else {
-      s[0] = with(s[0], s[0], 1);
-      s[0] = with(s[0], s[0], 2);
-    }
-    s[0] = with(s[0], s[0], 4);
-    if (piece < NT) share[g][sub + 4 * own] = make_float2(s[0].hi, s[0].lo);
+    for (int off = 1; off < 8; off <<= 1)
+      s = add_f2(s, {__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off)});
+    if (piece == 0) share[g][sub] = make_float2(s.hi, s.lo);
   }
   __syncthreads();
   if (g == 8) return;
@@ -246,28 +222,19 @@ __device__ __forceinline__ void transform_rows(uint4 (&raw)[NT], const RowTransf
   F2 sum = {0.0f, 0.0f};
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const float2 v = share[(piece & 4) + k][sub + 4 * own];
+    const float2 v = share[(piece & 4) + k][sub];
     sum = k == 0 ? F2{v.x, v.y} : add_f2(sum, {v.x, v.y});
   }
-  {
-    const F2 o = {__shfl_xor_sync(0xffffffffu, sum.hi, 4), __shfl_xor_sync(0xffffffffu, sum.lo, 4)};
-    sum = (piece & 4) == 0 ? add_f2(sum, o) : add_f2(o, sum);
-  }
+  const F2 o = {__shfl_xor_sync(0xffffffffu, sum.hi, 4), __shfl_xor_sync(0xffffffffu, sum.lo, 4)};
+  sum = (piece & 4) == 0 ? add_f2(sum, o) : add_f2(o, sum);
   const F2 rs = row_rstd(sum, tr.eps);
   const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
   const uint4 gv = tr.weight != nullptr ? tr.weight[g * 8 + piece] : ones;
   const uint64_t gw[4] = {f32x2(bf16_low(gv.x), bf16_high(gv.x)), f32x2(bf16_low(gv.y), bf16_high(gv.y)),
                           f32x2(bf16_low(gv.z), bf16_high(gv.z)), f32x2(bf16_low(gv.w), bf16_high(gv.w))};
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int from = (lane & 24) | i;
-    const F2 r = NT == 1 ? rs : F2{__shfl_sync(0xffffffffu, rs.hi, from), __shfl_sync(0xffffffffu, rs.lo, from)};
-    uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-    scale_row(w, gw, r);
-    raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
+  scale_row(w, gw, rs);
+  raw = make_uint4(w[0], w[1], w[2], w[3]);
 }
-
 constexpr int kBf16Rows = 16;  // cache kind of the BF16 cache
 
 // Quantises and packs n tokens. CB: content bits (4, 2) or kC4R4 for the paper's
@@ -299,6 +266,7 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     const RowTransform tr) {
   static_assert(NT == 1 || NT == 4, "tokens per lane");
   static_assert(FUSED || CB != kBf16Rows, "bf16 rows have a writer of their own");
+  static_assert(!FUSED || NT == 1, "many tokens have a fused writer of their own");
   using L = BlockLayout<CB == kBf16Rows ? 4 : CB>;
   // The decode's prep kernel may start meanwhile: it does not read the cache, and it
   // neither writes anything nor ends before this kernel has ended. (A decode step with
@@ -348,15 +316,11 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     }
   }
   if constexpr (FUSED) {
-    transform_rows<NT>(raw, tr, positions, n, tok0, g, lane);
+    transform_rows(raw[0], tr, positions, n, tok0, g, lane);
     if constexpr (CB == kBf16Rows) {
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const int d = NT == 1 ? dst : __shfl_sync(0xffffffffu, dst, (lane & 24) | i);
-        if (d >= 0)
-          reinterpret_cast<uint4*>(pool + static_cast<size_t>(d / kBlockTokens) * kBf16BlockBytes +
-                                   d % kBlockTokens * (kDqk * 2))[g * 8 + piece] = raw[i];
-      }
+      if (dst >= 0)
+        reinterpret_cast<uint4*>(pool + static_cast<size_t>(dst / kBlockTokens) * kBf16BlockBytes +
+                                 dst % kBlockTokens * (kDqk * 2))[g * 8 + piece] = raw[0];
       return;
     }
   }

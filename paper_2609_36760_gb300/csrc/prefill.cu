@@ -133,6 +133,8 @@ Workspace workspace_layout(int batch, int n_q) {
 // One block of kPlanThreads, or of kSmallPlan where that many sequences and items at
 // most can come up: a small call's time is the plan's chain of latencies.
 constexpr int kPlanThreads = 1024, kSmallPlan = 64;
+// Sequences, rows and keys of a call without a plan, at most.
+constexpr int kUnplanned = 64, kUnplannedRows = 65536, kUnplannedKeys = 1024;
 constexpr int kPlanOnChip = 2048;  // sequences whose prefix is kept in shared memory
 
 // Exclusive prefix of v (two counts in the halves) over the block, and the total.
@@ -156,6 +158,27 @@ __device__ __forceinline__ long long block_scan(long long v, long long* warp_sum
   const long long before = __shfl_sync(0xffffffffu, s, warp == 0 ? 0 : warp - 1);
   __syncthreads();
   return (warp == 0 ? 0 : before) + x - v;
+}
+
+// The item of rows r0 .. of a sequence of lq queries and lk keys.
+__device__ __forceinline__ Item make_item(int q0, int lq, int k0, int lk, int r0, int causal) {
+  Item it = {};
+  it.q_row = q0 + r0;
+  it.rows = min(lq - r0, kItemRows);
+  it.kv_start = k0;
+  it.kv_len = lk;
+  it.vis0 = causal ? r0 + lk - lq + 1 : lk;
+  it.step = causal ? 1 : 0;
+  const int last0 = min(it.rows, kTile) - 1, last1 = it.rows - 1;
+  it.n0 = (max(min(lk, it.vis0 + it.step * last0), 0) + kTile - 1) / kTile;
+  it.n1 = it.rows > kTile ? (max(min(lk, it.vis0 + it.step * last1), 0) + kTile - 1) / kTile : 0;
+  it.dealt = it.rows <= kTile && it.n0 > 1 ? 1 : 0;
+  it.parts = 1;
+  return it;
+}
+// Whether a sequence's offsets are within the rows given.
+__device__ __forceinline__ bool good_offsets(int q0, int q1, int k0, int k1, int n_q, int n_kv) {
+  return q0 >= 0 && q1 >= q0 && q1 <= n_q && k0 >= 0 && k1 >= k0 && k1 <= n_kv;
 }
 
 // Rounds of an item: key steps of its longer tile. Dealt, two of one tile's steps make a
@@ -195,7 +218,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
     int tiles = 0;
     if (b < batch) {
       const int q0 = cu_q[b], q1 = cu_q[b + 1], k0 = cu_kv[b], k1 = cu_kv[b + 1];
-      if (q0 < 0 || q1 < q0 || q1 > n_q || k0 < 0 || k1 < k0 || k1 > n_kv) {
+      if (!good_offsets(q0, q1, k0, k1, n_q, n_kv)) {
         report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
       } else {
         tiles = (q1 - q0 + kItemRows - 1) / kItemRows;
@@ -255,20 +278,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
       const Place at_i = i == tid ? first_place : find(i);
       const int q0 = at_i.q0, lq = at_i.lq, k0 = at_i.k0, lk = at_i.lk, t0 = at_i.t0, k = at_i.k;
       // (the last item is the longest; it stands first)
-      auto item = [&](int x) {
-        const int r0 = (t0 + k - 1 - x) * kItemRows;
-        Item it;
-        it.q_row = q0 + r0;
-        it.rows = min(lq - r0, kItemRows);
-        it.kv_start = k0;
-        it.kv_len = lk;
-        it.vis0 = causal ? r0 + lk - lq + 1 : lk;
-        it.step = causal ? 1 : 0;
-        const int last0 = min(it.rows, kTile) - 1, last1 = it.rows - 1;
-        it.n0 = (max(min(lk, it.vis0 + it.step * last0), 0) + kTile - 1) / kTile;
-        it.n1 = it.rows > kTile ? (max(min(lk, it.vis0 + it.step * last1), 0) + kTile - 1) / kTile : 0;
-        return it;
-      };
+      auto item = [&](int x) { return make_item(q0, lq, k0, lk, (t0 + k - 1 - x) * kItemRows, causal); };
       auto parts_of = [&](const Item& it) { return parts_at(rounds_of(it), longest); };
       int all = 0;  // entries of the bundle
       for (int x = 0; x < k; ++x) {
@@ -377,6 +387,10 @@ struct PrefillParams {
   float* lse;
   Partial* partial;
   bool join;  // join_kernel follows
+  bool unplanned;  // no plan_kernel: the draw warps work the pairs out (at most kUnplanned sequences)
+  const int32_t* cu_q;
+  const int32_t* cu_kv;
+  int batch, n_q, n_kv, causal;
   uint32_t* dev_err;
 };
 
@@ -429,26 +443,86 @@ struct Entry {
   }
 };
 
+// The item that is the i-th of all (64 sequences at most, two to a lane: tiles and
+// prefix are their items and the prefix's end), or none.
+struct Few {
+  int q0[2], lq[2], k0[2], lk[2], tiles[2], end[2];
+  __device__ __forceinline__ int init(const PrefillParams& p, int lane) {
+    int total = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int b = 32 * h + lane;
+      q0[h] = lq[h] = k0[h] = lk[h] = tiles[h] = 0;
+      if (b < p.batch) {
+        const int q1 = p.cu_q[b + 1], k1 = p.cu_kv[b + 1];
+        q0[h] = p.cu_q[b];
+        k0[h] = p.cu_kv[b];
+        lq[h] = q1 - q0[h];
+        lk[h] = k1 - k0[h];
+        if (good_offsets(q0[h], q1, k0[h], k1, p.n_q, p.n_kv)) {
+          tiles[h] = (lq[h] + kItemRows - 1) / kItemRows;
+        } else if (blockIdx.x == 0) {
+          report(p.dev_err, QMLA_DEVERR_BAD_OFFSETS);
+        }
+      }
+      int x = tiles[h];
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+      }
+      end[h] = total + x;
+      total = __shfl_sync(0xffffffffu, end[h], 31);
+    }
+    return total;
+  }
+  __device__ __forceinline__ Item item(int i, int causal) const {
+    Item it = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t behind = __ballot_sync(0xffffffffu, end[h] > i);
+      if (behind == 0u || (h == 1 && it.parts != 0)) continue;
+      const int from = __ffs(behind) - 1;
+      auto of = [&](int v) { return __shfl_sync(0xffffffffu, v, from); };
+      // (a sequence's last item, the longest, first)
+      it = make_item(of(q0[h]), of(lq[h]), of(k0[h]), of(lk[h]), (of(end[h]) - 1 - i) * kItemRows, causal);
+    }
+    return it;
+  }
+};
+
 // Draws the CTA's pairs: pair c first, then whichever is next when the load warp asks
-// for it. (A draw is three round trips to L2.)
+// for it. (A draw is three round trips to L2.) Without a plan every SMs-th pair.
 __device__ void draw_role(const PrefillParams& p, Ctl& ctl, int lane) {
   const int4* list = reinterpret_cast<const int4*>(p.items);
-  const int pairs = p.count[0] * p.heads;
+  Few few;
+  const int pairs = (p.unplanned ? few.init(p, lane) : p.count[0]) * p.heads;
   int at = static_cast<int>(blockIdx.x);
   for (uint32_t k = 0;; ++k) {
     if (k > 0) {
       if (!wait_warp(&ctl.ask, k - 1, ctl, kSiteLoad, p.dev_err)) return;
-      if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
-      at = __shfl_sync(0xffffffffu, at, 0);
+      if (p.unplanned) {
+        at += static_cast<int>(gridDim.x);
+      } else {
+        if (lane == 0) at = static_cast<int>(gridDim.x) + atomicAdd(p.count + 1, 1);
+        at = __shfl_sync(0xffffffffu, at, 0);
+      }
     }
     int4 w = make_int4(0, 0, -1, 0);  // lane l < 4: the l-th quarter of the item
-    if (at < pairs) {
+    const bool more = at < pairs;
+    if (more && p.unplanned) {
+      Item it = few.item(at / p.heads, p.causal);
+      it.head = at % p.heads;
+      w = lane == 0   ? make_int4(it.q_row, it.rows, it.kv_start, it.kv_len)
+          : lane == 1 ? make_int4(it.vis0, it.step, it.n0, it.n1)
+          : lane == 2 ? make_int4(it.first, it.bundle, it.head, it.dealt)
+                      : make_int4(it.part, it.parts, it.slot, it.unused);
+    } else if (more) {
       const int4 place = list[at / p.heads * 4 + 2];  // {the bundle's first item, its length, ..}
       const int rem = at - place.x * p.heads, head = rem / place.y;
       w = list[(place.x + rem - head * place.y) * 4 + (lane & 3)];
       if (lane == 2) w.z = head;
     }
-    const bool more = at < pairs;
     if (k >= 2 && !wait_warp(&ctl.sched_free[k & 1u], (k - 2) >> 1, ctl, kSiteLoad, p.dev_err)) return;
     if (lane < 4) ctl.work[k & 1u][lane] = w;
     __syncwarp();
@@ -1120,17 +1194,29 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
     configured_device = dev;
   }
   const long long pairs = static_cast<long long>(w.max_items) * d.heads;
-  const bool parts = d.n_kv > kLeastPart * kTile;  // (else no item is cut up)
+  // A plan (and the join of what it cuts up) is worth its launches where items are long
+  // or many. With it and without: 16 heads x 37 rows 11.6 and 8.2 us, 128 x 500 28.7 and
+  // 25.2, 16 heads x 8 prompts of 20 to 180 rows 15.7 and SHORTS.
+  p.unplanned = d.n_kv <= kUnplannedKeys && d.batch <= kUnplanned && d.n_q <= kUnplannedRows;
+  const bool parts = !p.unplanned && d.n_kv > kLeastPart * kTile;  // (else no item is cut up)
   p.join = parts;
+  p.cu_q = d.cu_q;
+  p.cu_kv = d.cu_kv;
+  p.batch = d.batch;
+  p.n_q = d.n_q;
+  p.n_kv = d.n_kv;
+  p.causal = d.causal;
   // Items per bundle: with few pairs per SM single items even the load out better.
   const int bundle = pairs >= 8ll * sms ? 4 : 1;
-  const int threads = w.max_items <= kSmallPlan && d.batch <= kSmallPlan ? kSmallPlan : kPlanThreads;
-  int shift = 0;
-  while (((d.n_kv / kTile + 1) >> shift) >= threads) ++shift;
-  plan_kernel<<<1, threads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.heads, d.causal != 0, sms, bundle,
-                                              shift, w.max_items, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
-                                              reinterpret_cast<Item*>(ws + w.items_off), joins, d.dev_err);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  if (!p.unplanned) {
+    const int threads = w.max_items <= kSmallPlan && d.batch <= kSmallPlan ? kSmallPlan : kPlanThreads;
+    int shift = 0;
+    while (((d.n_kv / kTile + 1) >> shift) >= threads) ++shift;
+    plan_kernel<<<1, threads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.heads, d.causal != 0, sms, bundle,
+                                                shift, w.max_items, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
+                                                reinterpret_cast<Item*>(ws + w.items_off), joins, d.dev_err);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(sms, pairs + (parts ? kSlots : 0))));
   cfg.blockDim = dim3(kThreads);
@@ -1140,7 +1226,7 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.unplanned ? 0 : 1;  // (behind whatever the caller launched: in full)
   if ((e = cudaLaunchKernelEx(&cfg, prefill_kernel, tq, tk, tv, tpe, p)) != cudaSuccess) return e;
   if (!parts) return cudaSuccess;
   cfg.gridDim = dim3(static_cast<unsigned>(2 * sms));

@@ -388,9 +388,9 @@ int qmla_mla_decode_ex(const qmla_decode_desc* desc, qmla_stream_t stream);
  *                   as in qmla_quant_append; cache_kind 4, 2, QMLA_CACHE_C4R4 or
  *                   QMLA_CACHE_BF16
  *   latent, latent_stride
- *                   [n] rows of 512 bf16, latent_stride elements apart (even, >= 512 when n > 1)
+ *                   [n] rows of 512 bf16, latent_stride elements apart (even, >= 512; not used when n == 1)
  *   k_pe, k_pe_stride
- *                   [n] rows of 64 bf16, k_pe_stride elements apart (even, >= 64 when n > 1).
+ *                   [n] rows of 64 bf16, k_pe_stride elements apart (even, >= 64; not used when n == 1).
  *                   Both 4-byte aligned; 16-byte aligned rows are read in wider pieces.
  *                   (So the two may be the columns of one [n, 576] projection output.)
  *   norm, norm_weight, norm_eps
@@ -439,8 +439,9 @@ int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream);
  * convention and table of qmla_rope_append, in fp32 (a product and an FMA), rounded to
  * bf16:
  *   q_pe_dev        [n, heads, 64] bf16, rows q_token_stride and q_head_stride elements
- *                   apart (multiples of 8, not negative, below 2^38), 16-byte aligned. (So it may be
- *                   the last 64 columns of a [n, heads, 192] projection output.)
+ *                   apart (multiples of 8, not negative, below 2^38; not used where that axis
+ *                   has one element), 16-byte aligned. (So it may be the last 64 columns of a
+ *                   [n, heads, 192] projection output.)
  *   positions_dev   [n] int32
  *   out_dev         [n, heads, 64] bf16 with strides of its own, 16-byte aligned. It may
  *                   be q_pe_dev with the same strides (in place) or share no memory with it;
@@ -461,7 +462,7 @@ int qmla_rope_query(const uint16_t* q_pe_dev, long long q_token_stride, long lon
  *   seq_ids[i] (NULL: sequence i); the BF16 cache's rows and protected positions
  *   (prot non-NULL; P_L from seq_lens, as in qmla_mla_decode_protected) unchanged.
  *   rows, row_stride   [n] rows of 576 bf16, row_stride elements apart (a multiple of 8,
- *                   >= 576 when n > 1), 16-byte aligned
+ *                   >= 576; not used when n == 1), 16-byte aligned
  * Other fields as in qmla_append_desc. A token with a bad sequence, position (with prot
  * also one at or beyond its sequence's length) or block leaves its row unwritten
  * (dev_err says so). n == 0 is a no-op.

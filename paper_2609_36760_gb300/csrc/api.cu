@@ -367,8 +367,11 @@ int qmla_mla_decode_ex(const qmla_decode_desc* d, qmla_stream_t stream) {
                        d->ev_after_main, d->max_len);
 }
 
-int qmla_rope_append(const qmla_append_desc* d, qmla_stream_t stream) {
-  if (d == nullptr || !known_cache(d->cache_kind)) return QMLA_ERR_INVALID_ARG;
+int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream) {
+  if (desc == nullptr || !known_cache(desc->cache_kind)) return QMLA_ERR_INVALID_ARG;
+  qmla_append_desc own = *desc;  // (a single row's strides are not used)
+  if (own.n == 1) own.latent_stride = qmla::kDc, own.k_pe_stride = qmla::kDr;
+  const qmla_append_desc* d = &own;
   int st = append_common_checks(d->pool, d->num_blocks, d->latent, d->k_pe, d->positions, d->n, d->block_table,
                                 d->num_seqs, d->max_blocks);
   if (st != QMLA_OK) return st;
@@ -401,10 +404,13 @@ int qmla_rope_query(const uint16_t* q_pe_dev, long long q_token_stride, long lon
     return QMLA_ERR_INVALID_ARG;
   if (!aligned(q_pe_dev, 16) || !aligned(out_dev, 16) || !aligned(cos_sin_dev, 16) || !aligned(positions_dev, 4))
     return QMLA_ERR_INVALID_ARG;
+  if (n == 1) q_token_stride = out_token_stride = qmla::kDr;  // (not used)
+  if (heads == 1) q_head_stride = out_head_stride = qmla::kDr;
   for (long long s : {q_token_stride, q_head_stride, out_token_stride, out_head_stride})
     if (s < 0 || s % 8 != 0 || s >= (1ll << 38)) return QMLA_ERR_INVALID_ARG;
   // Rows of out that overlap would race: one axis has to step over all of the other.
   const long long in_token = heads > 1 ? (heads - 1) * out_head_stride + qmla::kDr : qmla::kDr;
+  if (out_token_stride > (1ll << 56) / n) return QMLA_ERR_INVALID_ARG;  // (more than there are addresses)
   const long long in_head = n > 1 ? (n - 1) * out_token_stride + qmla::kDr : qmla::kDr;
   if ((n > 1 && out_token_stride < qmla::kDr) || (heads > 1 && out_head_stride < qmla::kDr) ||
       (n > 1 && heads > 1 && out_token_stride < in_token && out_head_stride < in_head))
@@ -430,7 +436,7 @@ int qmla_cache_read(const qmla_read_desc* d, qmla_stream_t stream) {
   if (d->pool == nullptr || d->positions == nullptr || d->block_table == nullptr || d->rows == nullptr)
     return QMLA_ERR_INVALID_ARG;
   if (!aligned(d->pool, 32) || !aligned(d->rows, 16) || !aligned(d->seq_ids, 4) || !aligned(d->positions, 4) ||
-      !aligned(d->block_table, 4) || d->row_stride % 8 != 0 || (d->n > 1 && d->row_stride < qmla::kDqk))
+      !aligned(d->block_table, 4) || (d->n > 1 && (d->row_stride % 8 != 0 || d->row_stride < qmla::kDqk)))
     return QMLA_ERR_INVALID_ARG;
   DevInfo di;
   int st = current_device_info(di);

@@ -253,6 +253,32 @@ def test_rope_query(n, heads, interleaved):
     assert torch.equal(qd, torch.cat([q[..., :128].cuda(), out], -1)) and Q.read_dev_err(err) == 0
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_strides_of_a_single_row_are_not_used(kind):
+    """One token, one head: any stride may stand in the axes of one element."""
+    c = Cache(kind, [3])
+    one = lambda t, last: t.cuda().as_strided((1, last), (last + 1, 1))  # noqa: E731
+    lens_dev = torch.tensor([3], dtype=torch.int32, device="cuda")
+    at = torch.tensor([2])
+    x = torch.cat([normed(c.rows[at, :512], c.weight, 1e-6), rotated(c.rows[at, 512:], c.cs, c.pos[at], False)], 1)
+    want, want_prot = c.plain(x, lens_dev, at)
+    pool, prot, err = c.fresh()
+    seq, pos, table, cs = c.seq[at].cuda(), c.pos[at].cuda(), c.table.cuda(), c.cs.cuda()
+    Q.rope_append(pool, c.kind, one(c.rows[2, :512].contiguous(), 512), one(c.rows[2, 512:].contiguous(), 64), seq, pos, table,
+                  cs, err, norm_weight=c.weight.cuda(), seq_lens=lens_dev if c.protect else None, prot=prot)
+    assert torch.equal(pool, want) and (not c.protect or torch.equal(prot, want_prot))
+    keep = dict(seq_lens=lens_dev if c.protect else None, prot=prot)
+    rows = [torch.zeros(1, 576, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    Q.cache_read(pool, c.kind, seq, pos, table, rows[0], err, **keep)
+    Q.cache_read(pool, c.kind, seq, pos, table, rows[1].as_strided((1, 576), (577, 1)), err, **keep)
+    assert torch.equal(*rows) and bool(rows[0].any())
+    q = torch.randn(1, 1, 64).bfloat16().cuda()
+    out = [torch.zeros_like(q) for _ in range(2)]
+    Q.rope_query(q, pos, cs, out[0], err)
+    Q.rope_query(q.as_strided((1, 1, 64), (3, 5, 1)), pos, cs, out[1].as_strided((1, 1, 64), (65, 1, 1)), err)
+    assert torch.equal(*out) and bool(out[0].any()) and Q.read_dev_err(err) == 0
+
+
 def test_rope_query_broadcast_heads_and_bad_positions():
     g = torch.Generator().manual_seed(4)
     q = torch.randn(6, 1, 64, generator=g).bfloat16().cuda().expand(6, 5, 64)  # head stride 0: one row for all heads

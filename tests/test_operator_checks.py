@@ -82,6 +82,21 @@ def test_rope_query_refuses_rows_that_overlap(L):
         assert good(ot, oh) == INVALID, (ot, oh)
 
 
+def test_rope_query_refuses_strides_past_all_addresses(L):
+    """Token strides whose product with the tokens leaves 64 bits (and looks small there)."""
+    big = (1 << 38) - 8
+    assert L.qmla_rope_query(FAKE, 768, 192, FAKE, 1 << 30, 32, FAKE, 64, 0, FAKE, 1 << 37, big, None, None) == INVALID
+
+
+@pytest.mark.parametrize("fn,desc", [("qmla_rope_append", append_desc(n=1, latent_stride=3, k_pe_stride=-5)),
+                                     ("qmla_cache_read", read_desc(n=1, row_stride=-3))])
+def test_a_single_row_has_no_stride(L, fn, desc):
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not real")
+    assert getattr(L, fn)(ctypes.byref(desc), None) not in (0, INVALID)  # (no device: the checks before are through)
+    assert L.qmla_rope_query(FAKE, 3, -5, FAKE, 1, 1, FAKE, 64, 0, FAKE, 1, 7, None, None) not in (0, INVALID)
+
+
 def prefill_desc(**kw):
     d = Q.PrefillDesc()
     base = dict(q=FAKE, q_token_stride=192 * 16, q_head_stride=192, k=FAKE, k_token_stride=256 * 16, k_head_stride=256,

@@ -252,6 +252,54 @@ def test_bad_offsets_are_left_out():
     p.check()
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lq,lk", [([37], [37]), ([200, 1, 0, 129, 90], [200, 300, 40, 129, 0]), ([300, 256], [500, 256])])
+def test_calls_with_and_without_a_plan_agree(lq, lk, causal):
+    """The rows behind the last sequence make the second call a long one: the same items, from the plan's list."""
+    a, b = Prompt(lq, lk, 5, seed=12, pad_q=3), Prompt(lq, lk, 5, seed=12, pad_q=3, pad_kv=9000)
+    b.q.copy_(a.q), b.kv[:sum(lk)].copy_(a.kv), b.rows[:sum(lk)].copy_(a.rows)
+    b.kv[sum(lk):], b.rows[sum(lk):] = math.nan, math.inf
+    assert a.run(causal) == 0 and b.run(causal) == 0
+    a.check(causal)
+    assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+
+
+@pytest.mark.parametrize("pad_kv", [0, 9000])
+def test_the_sequences_beside_a_bad_one(pad_kv):
+    """A sequence whose offsets are bad is left out, in short calls and planned ones; the others are computed."""
+    dev = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    p = Prompt([50, 60, 70, 80], [50, 60, 70, 80], 2, seed=9, pad_kv=pad_kv)
+    for cq, ck, left in [(dev(0, 50, 110, 180, 261), cu(p.lk), {0, 1, 2}), (dev(-1, 50, 110, 180, 260), cu(p.lk), {1, 2, 3}),
+                         (cu(p.lq), dev(0, 50, 110, 180, 261 + pad_kv), {0, 1, 2}),
+                         (cu(p.lq), dev(0, 50, 110, -5, 0), {0, 1})]:
+        p.err.zero_()
+        p.out.fill_(7), p.lse.fill_(7)
+        assert p.run(cu_q=cq, cu_kv=ck) == Q.DEVERR_BAD_OFFSETS
+        p.check(sequences=left)
+        for b in {0, 1, 2, 3} - left:
+            assert bool((p.out[sum(p.lq[:b]):sum(p.lq[:b + 1])] == 7).all())
+
+
+def test_a_planned_call_in_a_graph_on_two_workspaces():
+    a, b = (Prompt([40, 200, 700], [9000, 200, 700], 8, seed=s) for s in (13, 14))
+    cq, ck = cu(a.lq), cu(a.lk)
+    graph, streams = torch.cuda.CUDAGraph(), [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        for s, p in zip(streams, (a, b)):
+            s.wait_stream(main)
+            Q.mla_prefill(p.q, p.kv[..., :128], p.kv[..., 128:], p.rows[:, 512:], cq, ck, TAU, p.out, p.lse, p.ws, p.err, stream=s)
+            main.wait_stream(s)
+    for _ in range(3):
+        a.out.fill_(7), b.out.fill_(7)
+        graph.replay()
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+    assert Q.read_dev_err(a.err) == 0 and Q.read_dev_err(b.err) == 0
+
+
 def test_two_streams_and_a_replayed_graph():
     a, b = Prompt([300], [300], 8, seed=10), Prompt([40, 200], [900, 200], 8, seed=11)
     sa, sb = torch.cuda.Stream(), torch.cuda.Stream()

@@ -4,11 +4,13 @@
 //
 // plan_kernel cuts every sequence into items of 256 query rows and orders them,
 // the longest first; prefill_kernel (persistent, one CTA per SM) draws (item, head)
-// pairs from that list. In a CTA the two 128-row tiles of an item take turns on the
-// tensor core: while one tile's scores are turned into weights, the other's MMAs
-// run (PV of the old keys, QK of the next). An item of one tile (a short prompt, a
-// sequence's last rows) has its keys dealt to the two in turn instead: both hold
-// the same rows, every other key step each, and are merged at the end.
+// pairs from that list. A short call (kUnplanned, kUnplannedRows, kUnplannedKeys) has
+// no plan: its CTAs work their items out of the offsets. In a CTA the two 128-row tiles
+// of an item take turns on the tensor core: while one tile's scores are turned into
+// weights, the other's MMAs run (PV of the old keys, QK of the next). An item of one
+// tile (a short prompt, a sequence's last rows) has its keys dealt to the two in turn
+// instead: both hold the same rows, every other key step each, and are merged at the
+// end.
 //
 //   warps 0..3 / 4..7   softmax of tile 0 / 1, a query row per thread
 //   warps 8..11         epilogue of both tiles
@@ -134,7 +136,7 @@ Workspace workspace_layout(int batch, int n_q) {
 // most can come up: a small call's time is the plan's chain of latencies.
 constexpr int kPlanThreads = 1024, kSmallPlan = 64;
 // Sequences, rows and keys of a call without a plan, at most.
-constexpr int kUnplanned = 64, kUnplannedRows = 65536, kUnplannedKeys = 1024;
+constexpr int kUnplanned = 64, kUnplannedRows = 65536, kUnplannedKeys = 2048;
 constexpr int kPlanOnChip = 2048;  // sequences whose prefix is kept in shared memory
 
 // Exclusive prefix of v (two counts in the halves) over the block, and the total.
@@ -382,7 +384,7 @@ struct PrefillParams {
   int* count;  // [0] items, [1] pairs drawn beyond one per CTA, [2] joins
   const Item* items;
   int heads;
-  float scale, scale_log2;
+  float scale_log2;
   uint16_t* out;
   float* lse;
   Partial* partial;
@@ -1163,7 +1165,6 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   p.heads = d.heads;
   Join* joins = reinterpret_cast<Join*>(ws + w.join_off);
   p.partial = reinterpret_cast<Partial*>(ws + w.part_off);
-  p.scale = d.softmax_scale;
   p.scale_log2 = d.softmax_scale * 1.4426950408889634f;
   p.out = d.out;
   p.lse = d.lse;
@@ -1195,8 +1196,10 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   }
   const long long pairs = static_cast<long long>(w.max_items) * d.heads;
   // A plan (and the join of what it cuts up) is worth its launches where items are long
-  // or many. With it and without: 16 heads x 37 rows 11.6 and 8.2 us, 128 x 500 28.7 and
-  // 25.7, 16 heads x 8 prompts of 20 to 180 rows 15.7 and 11.6.
+  // or many. With it and without, in us: 16 heads x 37 rows 11.6 and 8.2, over 1,037 keys
+  // 22.3 and 16.4, over 2,037 22.2 and 23.2, over 4,037 25.0 and 41.5; 128 heads x 500 rows
+  // 28.5 and 24.8, x 1,000 55.7 and 55.4, x 2,000 151 and 154; 16 heads x 2,000 rows 43.4
+  // and 36.9; 16 heads x 8 prompts of 20 to 110 rows 13.7 and 9.6.
   p.unplanned = d.n_kv <= kUnplannedKeys && d.batch <= kUnplanned && d.n_q <= kUnplannedRows;
   const bool parts = !p.unplanned && d.n_kv > kLeastPart * kTile;  // (else no item is cut up)
   p.join = parts;
@@ -1213,8 +1216,8 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
     int shift = 0;
     while (((d.n_kv / kTile + 1) >> shift) >= threads) ++shift;
     plan_kernel<<<1, threads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.heads, d.causal != 0, sms, bundle,
-                                                shift, w.max_items, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
-                                                reinterpret_cast<Item*>(ws + w.items_off), joins, d.dev_err);
+                                           shift, w.max_items, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
+                                           reinterpret_cast<Item*>(ws + w.items_off), joins, d.dev_err);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};

@@ -140,12 +140,14 @@ void launch_read(const qmla_read_desc& d, cudaStream_t stream) {
 // step_tokens and step_heads are what kQueryStep rows are in tokens and heads.
 //
 // What bounds it: the HBM traffic (256 bytes per row). 8,184 tokens x 128 heads, the RoPE
-// part of [n, heads, 192] queries, take 46.4 us, 5.8 TB/s of 6.8 (with a 64-bit division
-// per row 55; two rows per lane group 53, eight 61; blocks of 256 threads 47.8).
+// part of [n, heads, 192] queries, take 43.0 us, 6.3 TB/s of 6.8. Ten blocks per SM: with
+// the eight that the registers would leave 46.4 (a 64-bit division per row 55; two rows
+// per lane group 53, eight 61; blocks of 256 threads 47.8), with twelve 42.4, but 80
+// rows, which are all latency, 4.1 instead of 3.4.
 constexpr int kQueryThreads = 128;
 constexpr int kQueryRows = 4, kQueryStep = kQueryThreads / 8;
 
-__global__ void __launch_bounds__(kQueryThreads) rope_query_kernel(
+__global__ void __launch_bounds__(kQueryThreads, 10) rope_query_kernel(
     const uint16_t* q, size_t q_token, size_t q_head, const int32_t* __restrict__ positions, long long rows, int heads,
     int step_tokens, int step_heads, const float* __restrict__ cos_sin, int rope_len, bool interleaved, uint16_t* out,
     size_t out_token, size_t out_head, uint32_t* dev_err) {

@@ -1171,18 +1171,19 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
   p.dev_err = d.dev_err;
   CUtensorMap tq, tk, tv, tpe;
   // A stride of an axis of one element is never used; a valid one stands in its place.
-  // Without keys no copy of one is issued.
+  // Without keys no copy of one is issued, and none of their strides is looked at.
   const bool keys = d.n_kv > 0;
+  const int key_heads = keys ? d.heads : 1;
   auto stride = [](int n, long long s, long long least) { return n > 1 ? s : least; };
   cudaError_t e = make_map(tq, d.q, kDn + kDr, d.heads, d.n_q, stride(d.n_q, d.q_token_stride, kDn + kDr),
                            stride(d.heads, d.q_head_stride, kDn + kDr), kTile);
   const void* any = d.q;
   if (e == cudaSuccess)
     e = make_map(tk, keys ? d.k : any, kDn, d.heads, std::max(d.n_kv, 1), stride(d.n_kv, d.k_token_stride, kDn),
-                 stride(d.heads, d.k_head_stride, kDn), kTile);
+                 stride(key_heads, d.k_head_stride, kDn), kTile);
   if (e == cudaSuccess)
     e = make_map(tv, keys ? d.v : any, kDv, d.heads, std::max(d.n_kv, 1), stride(d.n_kv, d.v_token_stride, kDv),
-                 stride(d.heads, d.v_head_stride, kDv), 64);
+                 stride(key_heads, d.v_head_stride, kDv), 64);
   if (e == cudaSuccess)
     e = make_map(tpe, keys ? d.k_pe : any, kDr, 0, std::max(d.n_kv, 1), stride(d.n_kv, d.k_pe_stride, kDr), 0, kTile);
   if (e != cudaSuccess) return e;

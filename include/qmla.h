@@ -381,8 +381,11 @@ int qmla_mla_decode_ex(const qmla_decode_desc* desc, qmla_stream_t stream);
  *     k'   = RN_bf16(RN_f32(k turned by the angles of position p))
  * and (x', k') is then stored exactly as qmla_quant_append (_protected, _c4r4) or
  * qmla_bf16_append store a row. The sums and products carry their rounding errors
- * along, so that the stored bytes do not depend on the order of a sum. Squares are
- * taken in fp32: |x_c| below 2^60.
+ * along, so that the stored bytes do not depend on the order of a sum; that holds for every
+ * finite row, the smallest and the largest too, with |w_c| below 2^64 (results below 2^-80
+ * may be off by one step of bf16, or 2^-104). A NaN makes its row's latent NaN; in a row with
+ * an infinity the finite values become 0 and the infinite ones NaN; a row of zeros is NaN with
+ * eps = 0, as the formula has it.
  *
  *   pool, num_blocks, seq_ids, positions, n, block_table, num_seqs, max_blocks, dev_err
  *                   as in qmla_quant_append; cache_kind 4, 2, QMLA_CACHE_C4R4 or

@@ -193,11 +193,14 @@ struct RowTransform {
 // Warp g's piece of four tokens (eight lanes each) normalised (g < 8) or rotated
 // (g = 8) in registers. The row's sum of squares needs all eight content warps: each
 // leaves its 64 channels' share in shared memory and every warp adds the eight shares in
-// the same order, so the result does not depend on the launch. Every thread of the
-// block takes part.
+// the same order, so the result does not depend on the launch, and all eight come to the
+// same answer about far rows. Every thread of the block takes part; the eight content
+// warps meet at a barrier of their own.
+__device__ __forceinline__ void content_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 __device__ __forceinline__ void transform_rows(uint4& raw, const RowTransform& tr, const int32_t* __restrict__ positions,
                                                int n, int tok, int g, int lane) {
   __shared__ float2 share[8][4];
+  __shared__ uint32_t tops[8][4];
   const int piece = lane & 7, sub = lane >> 3;
   uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
   if (g == 8) {
@@ -207,27 +210,43 @@ __device__ __forceinline__ void transform_rows(uint4& raw, const RowTransform& t
                 tr.interleaved);
     rotate_row<true>(w, a, piece, tr.interleaved);
     raw = make_uint4(w[0], w[1], w[2], w[3]);
+    return;
   }
   if (!tr.norm) return;
-  if (g < 8) {
+  auto row_sum = [&]() {
     F2 s = square_sum8(w);
 #pragma unroll
     for (int off = 1; off < 8; off <<= 1)
       s = add_f2(s, {__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off)});
     if (piece == 0) share[g][sub] = make_float2(s.hi, s.lo);
-  }
-  __syncthreads();
-  if (g == 8) return;
-  // The row's sum: four shares here, the other four in the lane four away.
-  F2 sum = {0.0f, 0.0f};
+    content_barrier();
+    // The row's sum: four shares here, the other four in the lane four away.
+    F2 sum = {0.0f, 0.0f};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float2 v = share[(piece & 4) + k][sub];
-    sum = k == 0 ? F2{v.x, v.y} : add_f2(sum, {v.x, v.y});
+    for (int k = 0; k < 4; ++k) {
+      const float2 v = share[(piece & 4) + k][sub];
+      sum = k == 0 ? F2{v.x, v.y} : add_f2(sum, {v.x, v.y});
+    }
+    const F2 o = {__shfl_xor_sync(0xffffffffu, sum.hi, 4), __shfl_xor_sync(0xffffffffu, sum.lo, 4)};
+    return (piece & 4) == 0 ? add_f2(sum, o) : add_f2(o, sum);
+  };
+  F2 sum = row_sum(), rs;
+  const bool far = tok < n && far_row(sum, tr.eps);
+  if (!__any_sync(0xffffffffu, far)) {
+    rs = row_rstd(sum, tr.eps);
+  } else {
+    uint32_t top = largest8(w);
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+    if (piece == 0) tops[g][sub] = top;
+    content_barrier();  // (the shares have been read as well)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = max(top, tops[k][sub]);
+    const float f = far ? far_factor(top, tr.eps) : 1.0f;
+    scale_words(w, f);
+    sum = row_sum();
+    rs = far_rstd(sum, tr.eps, f, top);
   }
-  const F2 o = {__shfl_xor_sync(0xffffffffu, sum.hi, 4), __shfl_xor_sync(0xffffffffu, sum.lo, 4)};
-  sum = (piece & 4) == 0 ? add_f2(sum, o) : add_f2(o, sum);
-  const F2 rs = row_rstd(sum, tr.eps);
   const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
   const uint4 gv = tr.weight != nullptr ? tr.weight[g * 8 + piece] : ones;
   const uint64_t gw[4] = {f32x2(bf16_low(gv.x), bf16_high(gv.x)), f32x2(bf16_low(gv.y), bf16_high(gv.y)),
@@ -363,6 +382,81 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
   }
 }
 
+// A row's sum of squares from its eight lanes' pairs.
+__device__ __forceinline__ F2 wide_sum(F2x2 sum) {
+  F2 s = add_f2({lo2(sum.hi), lo2(sum.lo)}, {hi2(sum.hi), hi2(sum.lo)});
+#pragma unroll
+  for (int off = 1; off < 8; off <<= 1)
+    s = add_f2(s, {__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off)});
+  return s;
+}
+// Group g's eight values of a lane normalised; weight: the 512 in shared memory, fp32.
+__device__ __forceinline__ void scale_wide(uint32_t (&w)[4], const float4* weight, int g, int piece, F2 rs) {
+  const ulonglong2 wa = reinterpret_cast<const ulonglong2*>(weight)[g * 16 + piece * 2];
+  const ulonglong2 wb = reinterpret_cast<const ulonglong2*>(weight)[g * 16 + piece * 2 + 1];
+  const uint64_t gw[4] = {wa.x, wa.y, wb.x, wb.y};
+  scale_row(w, gw, rs);
+}
+// The four tokens of a warp of wide_append_kernel where a row is far: everything from the
+// norm on, from memory once more and a group at a time. (Led back into the kernel, scaled
+// rows cost all others 3%.)
+// row: the latent, or null; pe: the rotated RoPE key; dst, sink and ring as there.
+template <int CB>
+__device__ __noinline__ void far_tokens(const uint32_t* row, uint4 pe, const float4* weight, bool far, float eps, int piece,
+                                        uint8_t* pool, int dst, uint4* prot, int sink, int ring) {
+  using L = BlockLayout<CB == kBf16Rows ? 4 : CB>;
+  uint32_t w[4], top = 0;
+  auto load = [&](int g) {
+    const uint4 v = g == 8 ? pe : (row != nullptr ? *reinterpret_cast<const uint4*>(row + g * 32 + piece * 4) : make_uint4(0, 0, 0, 0));
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  };
+#pragma unroll 1
+  for (int g = 0; g < 8; ++g) {
+    load(g);
+    top = max(top, largest8(w));
+  }
+#pragma unroll
+  for (int off = 1; off < 8; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+  const float f = far ? far_factor(top, eps) : 1.0f;
+  F2x2 sum = {0, 0};
+#pragma unroll 1
+  for (int g = 0; g < 8; ++g) {
+    load(g);
+    scale_words(w, f);
+    add_squares8(sum, w);
+  }
+  const F2 rs = far_rstd(wide_sum(sum), eps, f, top);
+#pragma unroll 1
+  for (int g = 0; g < kGroups; ++g) {
+    load(g);
+    if (g < 8) {
+      scale_words(w, f);
+      scale_wide(w, weight, g, piece, rs);
+    }
+    const uint4 v = make_uint4(w[0], w[1], w[2], w[3]);
+    if (sink >= 0) prot[static_cast<size_t>(sink) * (kDqk * 2 / 16) + g * 8 + piece] = v;
+    if (ring >= 0) prot[static_cast<size_t>(ring) * (kDqk * 2 / 16) + g * 8 + piece] = v;
+    const int slot = max(dst, 0) % kBlockTokens;
+    const size_t id = static_cast<size_t>(max(dst, 0) / kBlockTokens);
+    if constexpr (CB == kBf16Rows) {
+      if (dst >= 0) reinterpret_cast<uint4*>(pool + id * kBf16BlockBytes + slot * (kDqk * 2))[g * 8 + piece] = v;
+    } else {
+      const int bits = g < 8 && CB != kC4R4 ? CB : kPeBits;
+      float s, z, y;
+      scale_of<CB>(extrema64(w), g < 8, (1 << bits) - 1, s, z, y);
+      const uint32_t word = pack_codes(w, s, y, z, bits);
+      if (dst < 0) continue;
+      uint8_t* blk = pool + id * L::kBytes;
+      if (piece == 0) store_scale<CB>(blk, g, slot, s, z);
+      if (bits == 4) {
+        reinterpret_cast<uint32_t*>(blk + L::code_off(g, slot))[piece] = word;
+      } else {
+        reinterpret_cast<uint16_t*>(blk + L::code_off(g, slot))[piece] = static_cast<uint16_t>(word);
+      }
+    }
+  }
+}
+
 // The fused writer for many tokens: eight lanes hold a whole token, lane l the eight
 // channels l of each of its nine groups, so that a warp writes four tokens without a
 // word to the others. The row's sum takes three shuffles instead of a way through shared
@@ -371,11 +465,11 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
 // What bounds it: the issue slots, above all of the norm (without it and without
 // quantising, the copy into the BF16 cache takes half the time), then the HBM traffic
 // (1,152 bytes of the row and 256 of its angles read, 324 written): 32,797 tokens take
-// 23.4 us, 2.4 TB/s of 6.8, of which about 4.5 are the launch and the first loads; 116,736
-// take 67, 3.0 TB/s. Six blocks per SM: with 7 the registers spill (23.7).
+// 22.7 us, 2.5 TB/s of 6.8, of which about 4.5 are the launch and the first loads; 116,736
+// take 67.6, 3.0 TB/s. Five blocks per SM: with six the registers spill (23.7 and 69.7).
 constexpr int kWideThreads = 128;
 template <int CB>
-__global__ void __launch_bounds__(kWideThreads, 6) wide_append_kernel(
+__global__ void __launch_bounds__(kWideThreads, 5) wide_append_kernel(
     uint8_t* __restrict__ pool, int num_blocks, const uint32_t* __restrict__ latent,
     const uint32_t* __restrict__ k_pe, const int32_t* __restrict__ seq_ids,
     const int32_t* __restrict__ positions, int n, const int32_t* __restrict__ table, int num_seqs,
@@ -429,18 +523,17 @@ __global__ void __launch_bounds__(kWideThreads, 6) wide_append_kernel(
     F2x2 sum = {0, 0};
 #pragma unroll
     for (int g = 0; g < 8; ++g) add_squares8(sum, raw[g]);
-    F2 s = add_f2({lo2(sum.hi), lo2(sum.lo)}, {hi2(sum.hi), hi2(sum.lo)});
-#pragma unroll
-    for (int off = 1; off < 8; off <<= 1)
-      s = add_f2(s, {__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off)});
+    const F2 s = wide_sum(sum);
+    const bool far = tok < n && far_row(s, tr.eps);
+    if (__any_sync(0xffffffffu, far)) {
+      far_tokens<CB>(tok < n ? latent + static_cast<size_t>(tok) * tr.latent_words : nullptr,
+                     make_uint4(raw[8][0], raw[8][1], raw[8][2], raw[8][3]), weight, far, tr.eps, piece, pool, dst, prot,
+                     sink, ring);
+      return;
+    }
     const F2 rs = row_rstd(s, tr.eps);
 #pragma unroll
-    for (int g = 0; g < 8; ++g) {
-      const ulonglong2 wa = reinterpret_cast<const ulonglong2*>(weight)[g * 16 + piece * 2];
-      const ulonglong2 wb = reinterpret_cast<const ulonglong2*>(weight)[g * 16 + piece * 2 + 1];
-      const uint64_t gw[4] = {wa.x, wa.y, wb.x, wb.y};
-      scale_row(raw[g], gw, rs);
-    }
+    for (int g = 0; g < 8; ++g) scale_wide(raw[g], weight, g, piece, rs);
   }
   if (prot != nullptr) {
 #pragma unroll

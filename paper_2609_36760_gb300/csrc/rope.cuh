@@ -4,7 +4,8 @@
 // The writer's results are RN_bf16(RN_f32(exact)): the arithmetic carries the rounding
 // errors of its fp32 operations along (error-free transformations: T. J. Dekker,
 // Numer. Math. 18, 1971; D. E. Knuth, TAOCP 2, 4.2.2), which leaves about 2^-46
-// relative. A plain fp32 evaluation is off by up to some 2^-22, which moves one
+// relative (of rows near the ends of fp32's range too, which far_row tells apart). A
+// plain fp32 evaluation is off by up to some 2^-22, which moves one
 // bf16 value in about 2^13 and with it, now and then, the 2- or 4-bit code or the
 // scale of a whole group; this way the cache holds the same bytes whatever order
 // the sums are taken in. Queries, which nothing quantises, are rotated in plain fp32.
@@ -126,6 +127,43 @@ __device__ __forceinline__ F2 row_rstd(F2 sum, float eps) {
   const float low = __fmaf_rn(m.lo, t.hi, __fmaf_rn(m.hi, t.lo, p.lo));
   const float r = __fsub_rn(__fsub_rn(1.0f, p.hi), low);
   return {y, __fmul_rn(0.5f, __fmul_rn(y, r))};
+}
+
+// Squares of fp32 leave its range long before the values do, and the errors that the sums
+// carry along leave it sooner still: that arithmetic holds where the mean square plus eps
+// lies within 2^-90 .. 2^90 (a square that underflows is then off by 2^-150, a residual
+// of y^2 lies above 2^-138). Any other row (`far`; a NaN or an infinite sum too) is first
+// multiplied by the power of two that brings the larger of its largest value and sqrt(eps)
+// to about 1: x / sqrt(mean + eps) is the same for (f x, f^2 eps).
+__device__ __forceinline__ bool far_row(F2 sum, float eps) {
+  const float m = __fmaf_rn(sum.hi, 1.0f / 512.0f, eps);
+  return !(m >= 0x1p-90f && m <= 0x1p90f);
+}
+// The largest of eight magnitudes, as the bits of a bf16 (above 0x7F80: a NaN).
+__device__ __forceinline__ uint32_t largest8(const uint32_t (&w)[4]) {
+  uint32_t v = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v = __vmaxu2(v, w[e] & 0x7FFF7FFFu);
+  return max(v & 0xFFFFu, v >> 16);
+}
+// f of a row whose largest magnitude is `top`. Its exponent stays within a float's normal
+// range; what then lies above 1 or below it does so by a factor of 2^7 at most.
+__device__ __forceinline__ float far_factor(uint32_t top, float eps) {
+  int k = static_cast<int>(top >> 7) - 127;
+  if (eps > 0.0f) k = max(k, (static_cast<int>(__float_as_uint(eps) >> 23) - 126) >> 1);
+  return __uint_as_float(static_cast<uint32_t>(127 - max(-126, min(126, k))) << 23);
+}
+// Eight values times f: exact in bf16, but for what falls below 2^-126 of a row scaled down.
+__device__ __forceinline__ void scale_words(uint32_t (&w)[4], float f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = pack_bf16(__fmul_rn(bf16_low(w[e]), f), __fmul_rn(bf16_high(w[e]), f));
+}
+// row_rstd of a row that has been scaled; with an infinite value 0 (x / inf), with a NaN NaN.
+__device__ __forceinline__ F2 far_rstd(F2 sum, float eps, float f, uint32_t top) {
+  const F2 r = row_rstd(sum, __fmul_rn(__fmul_rn(eps, f), f));
+  if (top < 0x7F80u) return r;
+  const float v = top == 0x7F80u ? 0.0f : __uint_as_float(0x7FC00000u);
+  return {v, v};
 }
 
 // RN_bf16(RN_f32(x g rstd)) of eight values in place (x g is exact in fp32).

@@ -48,11 +48,13 @@ __device__ __forceinline__ F2x2 two_sum2(uint64_t a, uint64_t b) {
   return {s, add2(sub2(a, sub2(s, t)), sub2(b, t))};
 }
 
-// RN_f32(a c + b s).
+// RN_f32(a c + b s). Of an infinity, and past the largest float, the errors are NaN; the
+// leading sum is then the result.
 __device__ __forceinline__ float rotate1(float a, float c, float b, float s) {
   const F2 p = two_prod(a, c), q = two_prod(b, s);
   const F2 d = two_sum(p.hi, q.hi);
-  return __fadd_rn(d.hi, __fadd_rn(d.lo, __fadd_rn(p.lo, q.lo)));
+  const float r = __fadd_rn(d.hi, __fadd_rn(d.lo, __fadd_rn(p.lo, q.lo)));
+  return fabsf(d.hi) <= 3.402823466e38f ? r : d.hi;
 }
 
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }

@@ -510,8 +510,9 @@ int qmla_cache_read(const qmla_read_desc* desc, qmla_stream_t stream);
  *                   1..65536. n_kv may be 0 (k, v and k_pe are not used then); n_q == 0 is a
  *                   no-op
  *   cu_q, cu_kv     [batch + 1] int32 offsets, not decreasing. A sequence whose offsets
- *                   decrease, are negative or lie beyond n_q / n_kv is left out
- *                   (QMLA_DEVERR_BAD_OFFSETS)
+ *                   decrease, are negative or lie beyond n_q / n_kv is left out, and so is
+ *                   one whose queries begin before the end of an earlier sequence that has
+ *                   none of these faults (QMLA_DEVERR_BAD_OFFSETS); the others are computed
  *   out             [n_q, heads, 128] bf16, contiguous, 32-byte aligned; shares no memory
  *                   with the inputs
  *   lse             [n_q, heads] float32, contiguous, or NULL

@@ -139,27 +139,35 @@ constexpr int kPlanThreads = 1024, kSmallPlan = 64;
 constexpr int kUnplanned = 64, kUnplannedRows = 65536, kUnplannedKeys = 2048;
 constexpr int kPlanOnChip = 2048;  // sequences whose prefix is kept in shared memory
 
-// Exclusive prefix of v (two counts in the halves) over the block, and the total.
-__device__ __forceinline__ long long block_scan(long long v, long long* warp_sums, long long& total) {
+struct Sum {
+  __device__ __forceinline__ int operator()(int a, int b) const { return a + b; }
+};
+struct Largest {
+  __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); }
+};
+// Exclusive prefix of v >= 0 over the block under op, and the total.
+template <class Op>
+__device__ __forceinline__ int block_scan(int v, int* warp_totals, int& total, Op op) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  long long x = v;
+  int x = v;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, off);
-    if (lane >= off) x += y;
+    const int y = __shfl_up_sync(0xffffffffu, x, off);
+    if (lane >= off) x = op(x, y);
   }
-  if (lane == 31) warp_sums[warp] = x;
+  if (lane == 31) warp_totals[warp] = x;
   __syncthreads();
-  long long s = lane < warps ? warp_sums[lane] : 0;
+  int s = lane < warps ? warp_totals[lane] : 0;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, s, off);
-    if (lane >= off) s += y;
+    const int y = __shfl_up_sync(0xffffffffu, s, off);
+    if (lane >= off) s = op(s, y);
   }
   total = __shfl_sync(0xffffffffu, s, 31);
-  const long long before = __shfl_sync(0xffffffffu, s, warp == 0 ? 0 : warp - 1);
+  const int before = __shfl_sync(0xffffffffu, s, warp == 0 ? 0 : warp - 1);
+  const int in_warp = __shfl_up_sync(0xffffffffu, x, 1);
   __syncthreads();
-  return (warp == 0 ? 0 : before) + x - v;
+  return op(warp == 0 ? 0 : before, lane == 0 ? 0 : in_warp);
 }
 
 // The item of rows r0 .. of a sequence of lq queries and lk keys.
@@ -178,7 +186,10 @@ __device__ __forceinline__ Item make_item(int q0, int lq, int k0, int lk, int r0
   it.parts = 1;
   return it;
 }
-// Whether a sequence's offsets are within the rows given.
+// Whether a sequence's offsets are within the rows given. Where a sequence's offsets
+// decrease, good ones can overlap: of those, what begins before an earlier one's end is left
+// out, so that the sequences worked on are disjoint, and have no more items than there is
+// room for.
 __device__ __forceinline__ bool good_offsets(int q0, int q1, int k0, int k1, int n_q, int n_kv) {
   return q0 >= 0 && q1 >= q0 && q1 <= n_q && k0 >= 0 && k1 >= k0 && k1 <= n_kv;
 }
@@ -196,10 +207,10 @@ __device__ __forceinline__ int rounds_of(const Item& it) {
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ cu_q,
                                                             const int32_t* __restrict__ cu_kv, int batch, int n_q,
                                                             int n_kv, int heads, int causal, int sms, int bundle,
-                                                            int shift, int max_items, int* __restrict__ count,
+                                                            int shift, int* __restrict__ count,
                                                             int* __restrict__ prefix_far, Item* __restrict__ items,
                                                             Join* __restrict__ joins, uint32_t* dev_err) {
-  __shared__ long long warp_sums[32];
+  __shared__ int warp_totals[32];
   __shared__ int bucket[kPlanThreads];  // (as many as threads)
   __shared__ int prefix_near[kPlanOnChip];
   __shared__ unsigned long long rounds;
@@ -214,31 +225,30 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
     entries = slots = cut = most = 0;
   }
   if (tid < kLengths) cut_rounds[tid] = cut_parts[tid] = 0;
-  int bundles = 0, total_items = 0;
+  int bundles = 0, reach = 0;  // reach: where the earlier sequences with good offsets end
+  bool any_bad = false;
   for (int b0 = 0; b0 < batch; b0 += threads) {
     const int b = b0 + tid;
-    int tiles = 0;
+    int q0 = 0, q1 = 0;
+    bool good = false;
     if (b < batch) {
-      const int q0 = cu_q[b], q1 = cu_q[b + 1], k0 = cu_kv[b], k1 = cu_kv[b + 1];
-      if (!good_offsets(q0, q1, k0, k1, n_q, n_kv)) {
-        report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
-      } else {
-        tiles = (q1 - q0 + kItemRows - 1) / kItemRows;
-      }
+      q0 = cu_q[b], q1 = cu_q[b + 1];
+      good = good_offsets(q0, q1, cu_kv[b], cu_kv[b + 1], n_q, n_kv);
     }
-    long long sum;
-    const long long at =
-        block_scan((tiles + bundle - 1) / bundle | static_cast<long long>(tiles) << 32, warp_sums, sum);
-    if (b < batch) prefix[b] = bundles + static_cast<int>(at);
-    bundles += static_cast<int>(sum);
-    total_items += static_cast<int>(sum >> 32);
-    // Decreasing offsets can make sequences overlap, which can be more than there is
-    // room for: then nothing is worked on.
-    if (total_items > max_items) break;
-  }
-  if (total_items > max_items) {
-    if (tid == 0) report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
-    bundles = 0;
+    if (__syncthreads_or(b < batch && !good) || any_bad) {
+      if (!any_bad && b0 > 0) reach = cu_q[b0];  // (none was bad: they do not decrease)
+      any_bad = true;
+      int end;
+      const int before = block_scan(good ? q1 : 0, warp_totals, end, Largest{});
+      good = good && q0 >= max(reach, before);
+      reach = max(reach, end);
+      if (b < batch && !good) report(dev_err, QMLA_DEVERR_BAD_OFFSETS);
+    }
+    const int tiles = good ? (q1 - q0 + kItemRows - 1) / kItemRows : 0;
+    int sum;
+    const int at = block_scan((tiles + bundle - 1) / bundle, warp_totals, sum, Sum{});
+    if (b < batch) prefix[b] = bundles + at;
+    bundles += sum;
   }
   __syncthreads();
   int longest = INT32_MAX;  // rounds of a part
@@ -366,9 +376,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         }
       }
     } else if (pass == 2) {
-      long long sum;
-      const long long before = block_scan(bucket[tid], warp_sums, sum);
-      bucket[tid] = static_cast<int>(before);
+      int sum;
+      const int before = block_scan(bucket[tid], warp_totals, sum, Sum{});
+      bucket[tid] = before;
       __syncthreads();
     }
   }
@@ -450,23 +460,38 @@ struct Entry {
 struct Few {
   int q0[2], lq[2], k0[2], lk[2], tiles[2], end[2];
   __device__ __forceinline__ int init(const PrefillParams& p, int lane) {
-    int total = 0;
+    int total = 0, reach = 0;  // reach: as in plan_kernel
+    bool any_bad = false;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int b = 32 * h + lane;
       q0[h] = lq[h] = k0[h] = lk[h] = tiles[h] = 0;
+      int q1 = 0;
+      bool good = false;
       if (b < p.batch) {
-        const int q1 = p.cu_q[b + 1], k1 = p.cu_kv[b + 1];
+        q1 = p.cu_q[b + 1];
+        const int k1 = p.cu_kv[b + 1];
         q0[h] = p.cu_q[b];
         k0[h] = p.cu_kv[b];
         lq[h] = q1 - q0[h];
         lk[h] = k1 - k0[h];
-        if (good_offsets(q0[h], q1, k0[h], k1, p.n_q, p.n_kv)) {
-          tiles[h] = (lq[h] + kItemRows - 1) / kItemRows;
-        } else if (blockIdx.x == 0) {
-          report(p.dev_err, QMLA_DEVERR_BAD_OFFSETS);
-        }
+        good = good_offsets(q0[h], q1, k0[h], k1, p.n_q, p.n_kv);
       }
+      if (__any_sync(0xffffffffu, b < p.batch && !good) || any_bad) {
+        if (!any_bad && h > 0) reach = __shfl_sync(0xffffffffu, q0[h], 0);
+        any_bad = true;
+        int x = good ? q1 : 0;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, off);
+          if (lane >= off) x = max(x, y);
+        }
+        const int before = __shfl_up_sync(0xffffffffu, x, 1);
+        good = good && q0[h] >= max(reach, lane == 0 ? 0 : before);
+        reach = max(reach, __shfl_sync(0xffffffffu, x, 31));
+        if (b < p.batch && !good && blockIdx.x == 0) report(p.dev_err, QMLA_DEVERR_BAD_OFFSETS);
+      }
+      if (good) tiles[h] = (lq[h] + kItemRows - 1) / kItemRows;
       int x = tiles[h];
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -1217,7 +1242,7 @@ cudaError_t launch_prefill(const qmla_prefill_desc& d, int sms, cudaStream_t str
     int shift = 0;
     while (((d.n_kv / kTile + 1) >> shift) >= threads) ++shift;
     plan_kernel<<<1, threads, 0, stream>>>(d.cu_q, d.cu_kv, d.batch, d.n_q, d.n_kv, d.heads, d.causal != 0, sms, bundle,
-                                           shift, w.max_items, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
+                                           shift, p.count, reinterpret_cast<int*>(ws + w.prefix_off),
                                            reinterpret_cast<Item*>(ws + w.items_off), joins, d.dev_err);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }

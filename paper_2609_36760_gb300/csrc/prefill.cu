@@ -289,7 +289,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
     for (int i = tid; i < bundles; i += threads) {
       const Place at_i = i == tid ? first_place : find(i);
       const int q0 = at_i.q0, lq = at_i.lq, k0 = at_i.k0, lk = at_i.lk, t0 = at_i.t0, k = at_i.k;
-      // (the last item is the longest; it stands first)
+      // (the last item stands first: it has the most keys. With one tile, whose rounds count
+      // 3/4, it can still be shorter than the one before it, which then is the longest.)
       auto item = [&](int x) { return make_item(q0, lq, k0, lk, (t0 + k - 1 - x) * kItemRows, causal); };
       auto parts_of = [&](const Item& it) { return parts_at(rounds_of(it), longest); };
       int all = 0;  // entries of the bundle
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         const int r = rounds_of(it);
         if (pass == 0) {
           mine += static_cast<unsigned long long>(r) * heads;
-          if (x == 0) atomicMax(&most, r);
+          if (x < 2) atomicMax(&most, r);
         } else if (pass == 1) {
 #pragma unroll 1
           for (int c = 0; c < kLengths; ++c) {
@@ -313,7 +314,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
         }
       }
       if (pass < 2) continue;
-      const int key = threads - 1 - min(min(rounds_of(item(0)), longest) >> shift, threads - 1);
+      const int top = k > 1 ? max(rounds_of(item(0)), rounds_of(item(1))) : rounds_of(item(0));
+      const int key = threads - 1 - min(min(top, longest) >> shift, threads - 1);
       int at = atomicAdd(&bucket[key], all);
       if (pass == 2) {
         atomicAdd(&entries, all);

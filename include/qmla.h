@@ -34,8 +34,8 @@
  *   argument launches nothing.
  * - Problems only visible on the device (a bad block id, a position beyond the
  *   block table, a pipeline wait that ran out) are OR-ed into the caller's
- *   32-bit error word `dev_err_dev` (QMLA_DEVERR_*). The offending access is
- *   skipped; no call traps or aborts. Read the word with qmla_read_dev_err.
+ *   32-bit error word `dev_err_dev` (QMLA_DEVERR_*), unless it is NULL. The offending
+ *   access is skipped; no call traps or aborts. Read the word with qmla_read_dev_err.
  * - bf16 / fp16 tensors are passed as uint16_t bit patterns.
  * - Plain launches on one stream keep stream order, whatever memory they share. Kernels
  *   that a caller launches with programmatic stream serialisation have to know two things.

@@ -392,6 +392,7 @@ def read_dev_err(dev_err: torch.Tensor, stream=None) -> int:
 # The calls below take strided rows, so they look at types, shapes and devices too: a
 # tensor of another shape than the call's would be read out of range. One comparison
 # per tensor on the way, the words only when it fails: small steps are bound by this.
+# dev_err may be None: nothing is reported then.
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 _BLOCK_BYTES = {4: 20736, 2: 12544, "c4r4": 20480, "bf16": 73728}
 _device = torch._C._cuda_getDevice
@@ -423,6 +424,10 @@ def _rows(name: str, t: torch.Tensor, shape: tuple, dev: int) -> int:
     return t.data_ptr()
 
 
+def _error_word(dev_err: torch.Tensor | None, dev: int):
+    return None if dev_err is None else _flat("dev_err", dev_err, _I32, (1,), dev)
+
+
 def _current_device() -> int:
     return _device() if torch.cuda.is_initialized() else -2  # (without one every tensor is refused)
 
@@ -441,12 +446,12 @@ def _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev: int):
             _flat("block_table", block_table, _I32, (seqs, per), dev), seqs, per,
             None if seq_lens is None else _flat("seq_lens", seq_lens, _I32, (seqs,), dev),
             None if prot is None else _flat("prot", prot, _BF16, (seqs, 132, 576), dev),
-            _flat("dev_err", dev_err, _I32, (1,), dev))
+            _error_word(dev_err, dev))
 
 
 def rope_append(pool: torch.Tensor, cache_kind, latent: torch.Tensor, k_pe: torch.Tensor,
                 seq_ids: torch.Tensor | None, positions: torch.Tensor, block_table: torch.Tensor,
-                cos_sin: torch.Tensor, dev_err: torch.Tensor, norm_weight: torch.Tensor | None = None,
+                cos_sin: torch.Tensor, dev_err: torch.Tensor | None, norm_weight: torch.Tensor | None = None,
                 eps: float = 1e-6, norm: bool | None = None, interleaved: bool = False,
                 seq_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None, stream=None) -> None:
     """qmla_rope_append: cache_kind 4, 2, "c4r4" or "bf16"; latent bf16 [n,512] and k_pe bf16
@@ -470,7 +475,7 @@ def rope_append(pool: torch.Tensor, cache_kind, latent: torch.Tensor, k_pe: torc
 
 
 def cache_read(pool: torch.Tensor, cache_kind, seq_ids: torch.Tensor | None, positions: torch.Tensor,
-               block_table: torch.Tensor, rows: torch.Tensor, dev_err: torch.Tensor,
+               block_table: torch.Tensor, rows: torch.Tensor, dev_err: torch.Tensor | None,
                seq_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None, stream=None) -> None:
     """qmla_cache_read: the values of cached tokens into rows bf16 [n,576] (any row stride)."""
     dev = _current_device()
@@ -485,7 +490,7 @@ def cache_read(pool: torch.Tensor, cache_kind, seq_ids: torch.Tensor | None, pos
 
 
 def rope_query(q_pe: torch.Tensor, positions: torch.Tensor, cos_sin: torch.Tensor, out: torch.Tensor,
-               dev_err: torch.Tensor, interleaved: bool = False, stream=None) -> None:
+               dev_err: torch.Tensor | None, interleaved: bool = False, stream=None) -> None:
     """qmla_rope_query: q_pe and out bf16 [n,heads,64] with any strides; out may be q_pe (in place)."""
     dev = _current_device()
     shape, rope_len = tuple(q_pe.shape), cos_sin.size(0)
@@ -495,7 +500,7 @@ def rope_query(q_pe: torch.Tensor, positions: torch.Tensor, cos_sin: torch.Tenso
     st = lib().qmla_rope_query(_rows("q_pe", q_pe, shape, dev), qt, qh, _flat("positions", positions, _I32, (n,), dev), n,
                                heads, _flat("cos_sin", cos_sin, _F32, (rope_len, 64), dev), rope_len,
                                1 if interleaved else 0, _rows("out", out, shape, dev), ot, oh,
-                               _flat("dev_err", dev_err, _I32, (1,), dev), _raw_stream(stream, dev))
+                               _error_word(dev_err, dev), _raw_stream(stream, dev))
     if st:
         raise QmlaError("qmla_rope_query", st)
 
@@ -506,9 +511,10 @@ def prefill_workspace_bytes(batch: int, n_q: int) -> int:
 
 def mla_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pe: torch.Tensor, cu_q: torch.Tensor,
                 cu_kv: torch.Tensor, softmax_scale: float, out: torch.Tensor, lse: torch.Tensor | None,
-                workspace: torch.Tensor, dev_err: torch.Tensor, causal: bool = True, stream=None) -> None:
+                workspace: torch.Tensor, dev_err: torch.Tensor | None, causal: bool = True, stream=None) -> None:
     """qmla_mla_prefill: q bf16 [n_q,H,192], k and v bf16 [n_kv,H,128], k_pe bf16 [n_kv,64] with any
-    strides; cu_q, cu_kv int32 [batch+1]; out bf16 [n_q,H,128], lse f32 [n_q,H]."""
+    strides; cu_q, cu_kv int32 [batch+1]; out bf16 [n_q,H,128], lse f32 [n_q,H]; workspace of
+    prefill_workspace_bytes(batch, n_q) bytes, any type and shape."""
     dev = _current_device()
     nq, H, nkv, offsets = q.size(0), q.size(1), k.size(0), cu_q.size(0)
     (qt, qh, _), (kt, kh, _), (vt, vh, _) = q.stride(), k.stride(), v.stride()
@@ -518,8 +524,8 @@ def mla_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pe: torch.T
                     _flat("cu_kv", cu_kv, _I32, (offsets,), dev), 1 if causal else 0, softmax_scale,
                     _flat("out", out, _BF16, (nq, H, 128), dev),
                     None if lse is None else _flat("lse", lse, _F32, (nq, H), dev),
-                    _flat("workspace", workspace, _U8, (workspace.size(0),), dev), workspace.size(0),
-                    _flat("dev_err", dev_err, _I32, (1,), dev))
+                    _flat("workspace", workspace, workspace.dtype, workspace.shape, dev), workspace.nbytes,
+                    _error_word(dev_err, dev))
     st = lib().qmla_mla_prefill(d, _raw_stream(stream, dev))
     if st:
         raise QmlaError("qmla_mla_prefill", st)

@@ -651,15 +651,24 @@ void launch_quant(const AppendArgs& a, const RowTransform& tr, cudaStream_t stre
 // 32,768 15.1 against 19.5 / 19.8 against 20.7.
 constexpr int kFourPerLane = 8192;
 
-// Tokens from which the fused writer gives a token to eight lanes instead of a warp to
-// a group: 2,048 tokens 6.2 against 5.2 us, 4,096 6.2 against 7.2, 32,797 23.4 against
-// 39.7 (INT4, normalised, buffers larger together than L2).
-constexpr int kWide = 2800;
+// Tokens up to which the fused writer gives a warp to a group; above, eight lanes to a
+// token. The border is one wave of the former: 152 SMs with five blocks of 288 threads (40
+// registers; seven where nothing is quantised, 32) of four tokens. A warp to a group / eight
+// lanes to a token, us, buffers larger together than L2:
+//                                  3,040          3,041          4,256          4,257
+//   INT4, normalised            5.64 / 6.25    6.42 / 6.28
+//   INT4, as it is              4.22 / 4.50    4.99 / 4.63
+//   INT4 / INT2, protected      5.9 / 6.5      6.7 / 6.5
+//   the paper's page            5.74 / 6.43    7.38 / 7.30
+//   BF16, normalised            4.84 / 5.37                   5.79 / 5.63    6.01 / 5.68
+//   BF16, as it is              3.51 / 3.76                   3.96 / 4.13    4.39 / 4.14
+template <int CB>
+constexpr int kOneWave = 152 * 4 * (CB == kBf16Rows ? 7 : 5);
 
 template <int CB, bool FUSED>
 void launch_quant(const AppendArgs& a, const RowTransform& tr, bool vec, cudaStream_t stream) {
   if constexpr (FUSED) {
-    if (vec && a.n >= kWide) {
+    if (vec && a.n > kOneWave<CB>) {
       constexpr long long kPerBlock = kWideThreads / 8;
       wide_append_kernel<CB><<<static_cast<unsigned>((a.n + kPerBlock - 1) / kPerBlock), kWideThreads, 0, stream>>>(
           static_cast<uint8_t*>(a.pool), a.num_blocks, reinterpret_cast<const uint32_t*>(a.latent),

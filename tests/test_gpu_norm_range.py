@@ -19,7 +19,7 @@ from test_gpu_rows import KINDS, Cache, rotated
 
 pytestmark = pytest.mark.gpu
 LARGEST = 3.3895313892515355e38  # of bf16
-FORMS = [7, 2900]  # tokens: a warp per group; a token in eight lanes
+FORMS = [7, 4300]  # tokens: a warp per group; a token in eight lanes
 
 
 def exact(x, w, eps):
@@ -116,14 +116,14 @@ def test_infinite_and_nan_rows(n):
 
 def test_far_rows_off_a_16_byte_boundary():
     """The form for rows in 4-byte pieces, over the wide form's border."""
-    c = Cache(4, [2900], seed=3)
+    c = Cache(4, [4300], seed=3)
     rows = c.rows.clone()
     rows[::5, :512] = (rows[::5, :512].double() * 2.0 ** 70).bfloat16()
     rows[2::5, :512] = (rows[2::5, :512].double() * 2.0 ** -70).bfloat16()
-    wide = torch.zeros(2900, 600, dtype=torch.bfloat16)
+    wide = torch.zeros(4300, 600, dtype=torch.bfloat16)
     wide[:, 2:578] = rows
     x = torch.cat([exact(rows[:, :512], c.weight, 0.0).float().bfloat16(), rotated(rows[:, 512:], c.cs, c.pos, False)], 1)
-    assert torch.equal(write(c, wide[:, 2:578], c.weight, 0.0, strided=True), c.plain(x, None, torch.arange(2900))[0])
+    assert torch.equal(write(c, wide[:, 2:578], c.weight, 0.0, strided=True), c.plain(x, None, torch.arange(4300))[0])
 
 
 @pytest.mark.parametrize("n", FORMS)

@@ -74,7 +74,7 @@ def test_bundles_give_what_single_items_give():
 
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("norm,weight", [(True, False), (False, False)])
-@pytest.mark.parametrize("n", [2799, 2800, 2801, 4099])
+@pytest.mark.parametrize("n", [3040, 3041, 4256, 4257, 4299])
 def test_the_writer_of_many_tokens_without_norm_or_weights(kind, norm, weight, n):
     c = Cache(kind, [n - 700, 700], protect=kind in (2, "c4r4"), seed=n)
     check_append(c, norm, weight, n % 2 == 0, torch.arange(n), strided=True)
@@ -84,5 +84,5 @@ def test_the_writer_of_many_tokens_without_norm_or_weights(kind, norm, weight, n
 @pytest.mark.parametrize("offset", [2, 8])
 def test_many_tokens_off_a_16_byte_boundary(kind, offset):
     """Rows in 4-byte pieces (2 elements off) take the form of few tokens at any length."""
-    c = Cache(kind, [2900], protect=kind == 4, seed=offset)
-    check_append(c, True, True, False, torch.arange(2900), strided=True, offset=offset)
+    c = Cache(kind, [4300], protect=kind == 4, seed=offset)
+    check_append(c, True, True, False, torch.arange(4300), strided=True, offset=offset)

@@ -12,8 +12,11 @@ namespace {
 
 thread_local int g_last_cuda_error = 0;
 
+// (The runtime keeps the error until it is read: the next launch that looks for one of its
+// own would report it again.)
 int cuda_fail(cudaError_t e) {
   g_last_cuda_error = static_cast<int>(e);
+  (void)cudaGetLastError();
   return QMLA_ERR_CUDA;
 }
 
@@ -135,7 +138,7 @@ int desc_checks(const qmla_decode_desc* d) {
 }  // namespace
 
 namespace qmla {
-void record_cuda_error(int err) { g_last_cuda_error = err; }
+void record_cuda_error(int err) { cuda_fail(static_cast<cudaError_t>(err)); }
 
 int check_decode_desc(const qmla_decode_desc* d, bool check_workspace) {
   int st = desc_checks(d);

@@ -7,7 +7,8 @@
 //
 // A block of nine warps writes a few tokens: warp g quantises group g (64
 // coordinates) of four or sixteen tokens, eight lanes per token with eight
-// coordinates (16 bytes) each. A warp then reads four whole 128-byte lines and,
+// coordinates (16 bytes) each. (The fused form for many tokens has another layout, a
+// whole token in eight lanes: wide_append_kernel.) A warp then reads four whole 128-byte lines and,
 // where the tokens take consecutive slots (a prefill), writes their code rows
 // and scales as contiguous runs; the bit width and the scale format are uniform
 // in a warp. See quant_append_kernel for what bounds it.
@@ -462,11 +463,13 @@ __device__ __noinline__ void far_tokens(const uint32_t* row, uint4 pe, const flo
 // word to the others. The row's sum takes three shuffles instead of a way through shared
 // memory, and lane l works out the scale of group l, which shuffles hand round.
 //
-// What bounds it: the issue slots, above all of the norm (without it and without
-// quantising, the copy into the BF16 cache takes half the time), then the HBM traffic
-// (1,152 bytes of the row and 256 of its angles read, 324 written): 32,797 tokens take
-// 22.7 us, 2.5 TB/s of 6.8, of which about 4.5 are the launch and the first loads; 116,736
-// take 67.6, 3.0 TB/s. Five blocks per SM: with six the registers spill (23.7 and 69.7).
+// What bounds it: neither the issue slots (57% busy) nor the HBM traffic (1,152 bytes of the
+// row and 256 of its angles read, 324 written) by itself. A warp loads its tokens, works and
+// stores, once; at 93 registers an SM has 20 warps, too few to cover each other's loads
+// (long scoreboard 1.8 and math pipe 1.1 of 7.8 cycles per instruction). Most of the work is
+// the norm: INT4 rows as they are take 16.7 us. 32,797 tokens take 22.7 us, 2.5 TB/s of 6.8,
+// of which about 4.5 are the launch and the first loads; 116,736 take 67.6, 3.0 TB/s. Five
+// blocks per SM: with six the registers spill (23.7 and 69.7).
 constexpr int kWideThreads = 128;
 template <int CB>
 __global__ void __launch_bounds__(kWideThreads, 5) wide_append_kernel(

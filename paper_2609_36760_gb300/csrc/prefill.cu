@@ -104,8 +104,11 @@ static_assert(sizeof(Item) == 64, "four 16-byte loads");
 // and kLeastPart at least. An item of R > L rounds makes ceil(R / L) < 2 R / L parts, so
 // there are never more than 2 kShares partial results, nor more than kShares items cut up.
 // L itself: parts of W / SMs rounds can be a few more than SMs, which then takes two turns
-// of L, so some longer ones are weighed against it (kLengths; 16 heads, 512 rows over 16,896
-// keys: 160 parts 114 us, 128 of them 84).
+// of L, so some longer ones are weighed against it (kLengths). What that does, us, with L alone
+// and weighed: 16 heads, 512 rows over 16,896 keys 114 / 84 (160 parts, then 128), 200 over
+// 20,200 80 / 61, 1 over 50,001 106 / 78, 50 over 9,050 29.2 / 31.2 (the weighing does not count
+// what a longer part costs where the parts are few rounds); 24 heads, 700 over 9,700 122 / 97;
+// 32 heads, two of 128 over 12,128 103 / 88; 8 heads, 300 over 30,300 68.1 / 68.6.
 constexpr int kShares = 160, kSlots = 2 * kShares, kLeastPart = 4, kLengths = 4;
 struct Join {  // an item cut up
   int q_row, rows, slot, parts;
@@ -433,7 +436,7 @@ __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl& c
   return __all_sync(0xffffffffu, wait1(bar, parity, c, site, dev_err));
 }
 
-// The pair at hand, k-th of this CTA: read from shared memory, where the load warp
+// The pair at hand, k-th of this CTA: read from shared memory, where the draw warp
 // leaves it. For whole warps (LANES) and single threads.
 template <bool LANES>
 __device__ __forceinline__ bool next_pair(Ctl& c, uint32_t k, Item& it, uint32_t site, uint32_t* dev_err) {
@@ -806,7 +809,11 @@ __device__ __forceinline__ void hide64(float (&s)[64], int lim) {
   for (int c = 0; c < 64; ++c) s[c] = c < lim ? s[c] : -INFINITY;
 }
 
-// 2^(s scale - ref) of 64 scores as pairs of bf16, and the sum (of the unrounded ones).
+// 2^(s scale - ref) of 64 scores as pairs of bf16, and the sum (of the unrounded ones). The
+// weights meet values in bf16 in one MMA, whose operands have to be of one type, and values in
+// fp16 would lose range; so each is off by up to 2^-8, as a value is. Their sum is taken
+// before that rounding: it is the exact one's to fp32, and the roundings of many weights,
+// which are as often up as down, do not enter the log-sum-exp.
 __device__ __forceinline__ float weights64(const float (&s)[64], float scale, float ref, uint32_t (&w)[32]) {
   const uint64_t sl = f32x2(scale, scale), mm = f32x2(-ref, -ref);
   uint64_t sum[4] = {0, 0, 0, 0};  // (pairs of zeros)

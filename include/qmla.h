@@ -395,7 +395,7 @@ int qmla_mla_decode_ex(const qmla_decode_desc* desc, qmla_stream_t stream);
  *   k_pe, k_pe_stride
  *                   [n] rows of 64 bf16, k_pe_stride elements apart (even, >= 64; not used when n == 1).
  *                   Both 4-byte aligned; 16-byte aligned rows (and strides that are multiples of
- *                   8) are read in wider pieces: 32,797 INT4 tokens 23 against 41 us
+ *                   8) are read in wider pieces: 32,797 INT4 tokens 23 against 39 us
  *                   (So the two may be the columns of one [n, 576] projection output.)
  *   norm, norm_weight, norm_eps
  *                   norm 0: the latent is stored as it is. Otherwise w is norm_weight

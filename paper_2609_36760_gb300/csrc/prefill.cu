@@ -467,25 +467,31 @@ struct Few {
   __device__ __forceinline__ int init(const PrefillParams& p, int lane) {
     int total = 0, reach = 0;  // reach: as in plan_kernel
     bool any_bad = false;
+    int q1[2];
+    bool in_range[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 2; ++h) {  // (all loads first)
       const int b = 32 * h + lane;
-      q0[h] = lq[h] = k0[h] = lk[h] = tiles[h] = 0;
-      int q1 = 0;
-      bool good = false;
+      q0[h] = lq[h] = k0[h] = lk[h] = tiles[h] = q1[h] = 0;
+      in_range[h] = false;
       if (b < p.batch) {
-        q1 = p.cu_q[b + 1];
+        q1[h] = p.cu_q[b + 1];
         const int k1 = p.cu_kv[b + 1];
         q0[h] = p.cu_q[b];
         k0[h] = p.cu_kv[b];
-        lq[h] = q1 - q0[h];
+        lq[h] = q1[h] - q0[h];
         lk[h] = k1 - k0[h];
-        good = good_offsets(q0[h], q1, k0[h], k1, p.n_q, p.n_kv);
+        in_range[h] = good_offsets(q0[h], q1[h], k0[h], k1, p.n_q, p.n_kv);
       }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int b = 32 * h + lane;
+      bool good = in_range[h];
       if (__any_sync(0xffffffffu, b < p.batch && !good) || any_bad) {
         if (!any_bad && h > 0) reach = __shfl_sync(0xffffffffu, q0[h], 0);
         any_bad = true;
-        int x = good ? q1 : 0;
+        int x = good ? q1[h] : 0;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
           const int y = __shfl_up_sync(0xffffffffu, x, off);

@@ -23,6 +23,9 @@
  *   qmla_rope_query     rotates the RoPE part of queries
  *   qmla_cache_read     cached tokens back as bf16 rows
  *   qmla_mla_prefill    attention of ragged prompts over expanded keys and values
+ *   qmla_mla_decode_tree  decode attention of a tree of drafted tokens
+ *   qmla_tree_verify    verification of such a tree against the target's probabilities
+ *   qmla_cache_keep     the accepted tokens' cache rows moved together, the new lengths
  *
  * Conventions for every call
  * --------------------------
@@ -98,7 +101,9 @@ enum qmla_device_error {
   QMLA_DEVERR_BAD_POSITION = 2u,  /* a position or sequence length < 0 or beyond max_blocks*64 */
   QMLA_DEVERR_BAD_SEQ = 4u,       /* an append sequence id outside [0, num_seqs) */
   QMLA_DEVERR_TIMEOUT = 8u,       /* an on-chip pipeline wait ran out; that kernel left early */
-  QMLA_DEVERR_BAD_OFFSETS = 16u   /* a prompt's offsets decrease or leave the rows given; it was left out */
+  QMLA_DEVERR_BAD_OFFSETS = 16u,  /* a prompt's offsets decrease or leave the rows given; it was left out */
+  QMLA_DEVERR_BAD_TREE = 32u,     /* a tree's node count, parent, token or path is not one (see the call) */
+  QMLA_DEVERR_BAD_PROBS = 64u     /* probabilities to draw a token from have no positive, finite sum */
 };
 
 /* Cache kinds besides the content bit widths 4 and 2: the paper's page, the BF16 cache. */
@@ -107,6 +112,13 @@ enum qmla_device_error {
 
 /* Most query tokens per sequence qmla_mla_decode_multi accepts. */
 #define QMLA_MAX_Q_TOKENS 8
+
+/* Most nodes of a tree of drafted tokens (qmla_mla_decode_tree and the calls beside it). */
+#define QMLA_MAX_TREE_NODES 64
+
+/* Types of probabilities (qmla_tree_verify). */
+#define QMLA_PROBS_F32 0
+#define QMLA_PROBS_BF16 1
 
 /* Bytes of one 64-token block for content bit width c_bits (4 -> 20736,
  * 2 -> 12544); 0 if c_bits is not supported. */
@@ -438,6 +450,12 @@ typedef struct qmla_append_desc {
 } qmla_append_desc;
 int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream);
 
+/* qmla_rope_append with the keys turned by the angles of rope_positions[i] ([n] int32)
+ * instead of those of the cache position positions[i]: the nodes of a tree of drafts lie side
+ * by side in the cache, but siblings have the same position in the text. A rope position
+ * below 0 or at or beyond rope_len is a bad position. NULL: as qmla_rope_append. */
+int qmla_rope_append_at(const qmla_append_desc* desc, const int32_t* rope_positions_dev, qmla_stream_t stream);
+
 /*
  * Turns the RoPE part of queries by the angles of their positions, with the
  * convention and table of qmla_rope_append, in fp32 (a product and an FMA), rounded to
@@ -550,6 +568,166 @@ int qmla_mla_prefill(const qmla_prefill_desc* desc, qmla_stream_t stream);
 /* Workspace bytes qmla_mla_prefill needs; 0 for bad arguments. Room for 320 partial results of
  * long contexts (42.6 MB) whatever the call, and 64 bytes per 256 rows and per sequence. */
 size_t qmla_prefill_workspace_bytes(int batch, int n_q);
+
+/*
+ * A step of speculative decoding with a tree of drafted tokens. Node 0 of a sequence's tree
+ * is its last committed token, the others are drafts; parents[b, t] is the node that node t
+ * continues: an earlier one, or -1. The nodes lie in the cache in their order, behind the
+ * context: with n nodes and L = seq_lens[b] tokens (the nodes included), node t is position
+ * ctx + t, ctx = L - n. (It is written there, and rotated by the angles of the position
+ * that it would have in the text, ctx + its depth.) A step is
+ *   qmla_rope_append_at    the nodes' rows into the cache
+ *   qmla_mla_decode_tree   their attention, in every layer
+ *   qmla_tree_verify       which of them the target accepts, and the token after them
+ *   qmla_cache_keep        their rows moved together behind the context, in every layer.
+ *
+ * qmla_mla_decode_tree: node t attends to the ctx positions of the context, to the nodes
+ * above it and to itself, A(t) = {t} U A(parents[t]):
+ *     S[b,t,h,p] = softmax_scale * (q_latent[b,t,h,:] . C_hat[b,p,:] + q_pe[b,t,h,:] . K_hat[b,p,:]),
+ *                  p < ctx or p - ctx in A(t)
+ *     out[b,t,h,:] = RN_bf16(sum_p softmax_p(S[b,t,h,:]) C_hat[b,p,:]);  lse[b,t,h] = log sum_p exp(S[b,t,h,p])
+ *   pool, cache_kind, num_blocks, block_table, max_blocks, max_len, softmax_scale, dev_err
+ *                   as in qmla_mla_decode_ex, any of the four cache kinds
+ *   q_latent, q_pe  [batch, nodes, heads, 512] and [batch, nodes, heads, 64] bf16, 16-byte aligned
+ *   nodes, heads    1 .. QMLA_MAX_TREE_NODES, 1 .. 128
+ *   parents         [batch, nodes] int32
+ *   seq_lens        [batch] int32, the nodes included
+ *   tree_lens       [batch] int32: nodes of each sequence (its first ones; 0: no tree), or
+ *                   NULL: all of them
+ *   prot, draft_rows  sink4/local128 protection, both or neither (not with QMLA_CACHE_BF16):
+ *                   the protection buffer holds the rows of the context, P_L for L = ctx, and
+ *                   draft_rows [batch][64][576] bf16, 16-byte aligned, the nodes' own rows
+ *                   (row t of sequence b: node t's latent, then its RoPE key), which are read
+ *                   in the place of their packed copies. (The drafts are not in the ring:
+ *                   they would take the places of context that is protected once they are
+ *                   refused. The layout is a BF16 cache's with one block a sequence, so that
+ *                   qmla_rope_append_at writes these rows too.)
+ *   out             [batch, nodes, heads, 512] bf16, 16-byte aligned
+ *   lse             [batch, nodes, heads] float32, or NULL
+ *   workspace       >= qmla_tree_workspace_bytes(batch, nodes, heads) bytes, 256-byte
+ *                   aligned, scratch as for qmla_mla_decode
+ * A node behind the last of its sequence gets out = 0 and lse = -inf. So do a node whose
+ * parent is not an earlier node or -1 and the nodes below it (QMLA_DEVERR_BAD_TREE), and
+ * every node of a sequence whose count is below 0, above `nodes` or above its length (the
+ * same) or whose length is bad (QMLA_DEVERR_BAD_POSITION). A value that is not finite in a
+ * node's cache row may reach nodes that do not see it (weight 0 x inf).
+ */
+typedef struct qmla_tree_desc {
+  const void* pool;
+  int cache_kind;
+  int num_blocks;
+  const uint16_t* q_latent;
+  const uint16_t* q_pe;
+  int batch, nodes, heads;
+  int max_len;
+  const int32_t* parents;
+  const int32_t* tree_lens;
+  const int32_t* block_table;
+  int max_blocks;
+  float softmax_scale;
+  const int32_t* seq_lens;
+  const void* prot;
+  const uint16_t* draft_rows;
+  uint16_t* out;
+  float* lse;
+  void* workspace;
+  size_t workspace_bytes;
+  uint32_t* dev_err;
+} qmla_tree_desc;
+int qmla_mla_decode_tree(const qmla_tree_desc* desc, qmla_stream_t stream);
+
+/* Workspace bytes qmla_mla_decode_tree needs on the current device; 0 for bad arguments. */
+size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads);
+
+/*
+ * Walks each tree from node 0 and keeps the drafts that the target accepts, so that the
+ * tokens kept and the one drawn after them are distributed as the target's own. At node c,
+ * with the target's probabilities p = target[b, c, :] of what follows it and the draft's
+ * q = draft[b, c, :], from which the tokens of c's children were drawn independently, the
+ * children x = tokens[b, t] are looked at in the order of their nodes:
+ *     r(v) = max(p(v) - a q(v), 0), R = 1 and a = 0 at first
+ *     the child is accepted if u_t q(x) R < r(x), u_t = uniforms[b, t]: the walk goes on at it;
+ *     if not, a grows by R and R becomes sum_v r(v) of the new a.
+ * (r / R is what is left of p after the refusals: max(r / R - q, 0) is r's next value over R.)
+ * With draft NULL the children's tokens were chosen without randomness: the child is accepted
+ * if u_t R < p(x); if not, R loses p(x), and p(x) becomes 0. Where no child is accepted the
+ * walk ends, and the next token is the first v with
+ *     sum_{w <= v} r(w) > u_0 sum_w r(w)
+ * (r = p where nothing was refused), the last v with r(v) > 0 where rounding leaves none.
+ * Sums and terms carry their rounding errors along, so that no decision depends on an order.
+ *
+ *   target, target_seq_stride, target_row_stride
+ *                   [batch, nodes, vocab] probabilities of type probs (QMLA_PROBS_*), rows
+ *                   and sequences that many elements apart (not negative, below 2^40; not used
+ *                   where that axis has one element). Values are taken as they are given: p
+ *                   below 0 counts as 0, rows are not normalised
+ *   draft, ...      the same for the draft, or NULL. Rows of nodes without children are not read
+ *   batch, nodes, vocab   1 .. 65535, 1 .. QMLA_MAX_TREE_NODES, 1 .. 2^24
+ *   tokens, parents [batch, nodes] int32; tree_lens [batch] int32 or NULL, as above
+ *   uniforms        [batch, nodes] float32 in [0, 1) (others count as the nearest, NaN as 0).
+ *                   The number of node 0, which is not drawn, is the one for the next token
+ *   path            [batch, nodes] int32 out: the kept nodes, 0 first, then -1
+ *   kept            [batch] int32 out: how many they are
+ *   next_token      [batch] int32 out
+ * A sequence without a tree gets kept = 0, next_token = -1 and no path, and so does one whose
+ * count is bad (QMLA_DEVERR_BAD_TREE). A node is passed over whose token is not in the
+ * vocabulary or whose parent is not an earlier node or -1 (the same). Where the sum of r is
+ * not positive and finite, next_token is -1 (QMLA_DEVERR_BAD_PROBS). Outputs share no memory
+ * with the inputs or one another.
+ */
+typedef struct qmla_verify_desc {
+  const void* target;
+  long long target_seq_stride, target_row_stride;
+  const void* draft;
+  long long draft_seq_stride, draft_row_stride;
+  int probs;
+  int batch, nodes, vocab;
+  const int32_t* tokens;
+  const int32_t* parents;
+  const int32_t* tree_lens;
+  const float* uniforms;
+  int32_t* path;
+  int32_t* kept;
+  int32_t* next_token;
+  uint32_t* dev_err;
+} qmla_verify_desc;
+int qmla_tree_verify(const qmla_verify_desc* desc, qmla_stream_t stream);
+
+/*
+ * Keeps the nodes path[b, 0 .. kept[b] - 1] of each sequence's tree in its cache and drops
+ * the others: the row at position ctx + path[b, i] moves to ctx + i, in place and unchanged,
+ * and new_lens[b] = ctx + kept[b] (ctx = seq_lens[b] - n, n = tree_lens[b] or `nodes`). One
+ * call per layer's cache.
+ *   pool, cache_kind, num_blocks, block_table, max_blocks, dev_err   as in qmla_append_desc
+ *   batch, nodes    sequences, 1 .. QMLA_MAX_TREE_NODES
+ *   path, kept      as qmla_tree_verify leaves them; path increases
+ *   prot, draft_rows  as in qmla_mla_decode_tree, both or neither: the kept nodes' rows are
+ *                   also copied from draft_rows into the protection buffer, which then holds
+ *                   P_L for L = new_lens[b]
+ *   seq_lens, new_lens   [batch] int32; they may be the same array (not with a second call of
+ *                   the step to follow)
+ * A sequence whose count, kept or path is bad (kept > n, a path that does not increase or
+ * leaves 0 .. n - 1: QMLA_DEVERR_BAD_TREE; or a bad length: QMLA_DEVERR_BAD_POSITION) is left
+ * as it is, with new_lens[b] = seq_lens[b]. A row from or to a bad block is not moved.
+ * Sequences that share blocks must not share those of their nodes.
+ */
+typedef struct qmla_keep_desc {
+  void* pool;
+  int cache_kind;
+  int num_blocks;
+  int batch, nodes;
+  const int32_t* block_table;
+  int max_blocks;
+  const int32_t* seq_lens;
+  const int32_t* tree_lens;
+  const int32_t* path;
+  const int32_t* kept;
+  void* prot;
+  const uint16_t* draft_rows;
+  int32_t* new_lens;
+  uint32_t* dev_err;
+} qmla_keep_desc;
+int qmla_cache_keep(const qmla_keep_desc* desc, qmla_stream_t stream);
 
 /* Bytes of the fixed device scratch array qmla_mla_decode_static uses
  * (32 MiB). */

@@ -24,6 +24,9 @@ DEVERR_BAD_POSITION = 2
 DEVERR_BAD_SEQ = 4
 DEVERR_TIMEOUT = 8
 DEVERR_BAD_OFFSETS = 16
+DEVERR_BAD_TREE = 32
+DEVERR_BAD_PROBS = 64
+MAX_TREE_NODES = 64
 
 
 CACHE_KINDS = {4: 4, 2: 2, "c4r4": 5, "bf16": 16}  # qmla_decode_desc.cache_kind codes
@@ -71,6 +74,38 @@ class PrefillDesc(ctypes.Structure):
                 ("cu_kv", ctypes.c_void_p), ("causal", ctypes.c_int), ("softmax_scale", ctypes.c_float),
                 ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t), ("dev_err", ctypes.c_void_p)]
+
+
+class TreeDesc(ctypes.Structure):
+    """qmla_tree_desc (include/qmla.h), field for field."""
+    _fields_ = [("pool", ctypes.c_void_p), ("cache_kind", ctypes.c_int), ("num_blocks", ctypes.c_int),
+                ("q_latent", ctypes.c_void_p), ("q_pe", ctypes.c_void_p), ("batch", ctypes.c_int),
+                ("nodes", ctypes.c_int), ("heads", ctypes.c_int), ("max_len", ctypes.c_int),
+                ("parents", ctypes.c_void_p), ("tree_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("max_blocks", ctypes.c_int), ("softmax_scale", ctypes.c_float), ("seq_lens", ctypes.c_void_p),
+                ("prot", ctypes.c_void_p), ("draft_rows", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                ("dev_err", ctypes.c_void_p)]
+
+
+class VerifyDesc(ctypes.Structure):
+    """qmla_verify_desc (include/qmla.h), field for field."""
+    _fields_ = [("target", ctypes.c_void_p), ("target_seq_stride", ctypes.c_longlong),
+                ("target_row_stride", ctypes.c_longlong), ("draft", ctypes.c_void_p),
+                ("draft_seq_stride", ctypes.c_longlong), ("draft_row_stride", ctypes.c_longlong),
+                ("probs", ctypes.c_int), ("batch", ctypes.c_int), ("nodes", ctypes.c_int), ("vocab", ctypes.c_int),
+                ("tokens", ctypes.c_void_p), ("parents", ctypes.c_void_p), ("tree_lens", ctypes.c_void_p),
+                ("uniforms", ctypes.c_void_p), ("path", ctypes.c_void_p), ("kept", ctypes.c_void_p),
+                ("next_token", ctypes.c_void_p), ("dev_err", ctypes.c_void_p)]
+
+
+class KeepDesc(ctypes.Structure):
+    """qmla_keep_desc (include/qmla.h), field for field."""
+    _fields_ = [("pool", ctypes.c_void_p), ("cache_kind", ctypes.c_int), ("num_blocks", ctypes.c_int),
+                ("batch", ctypes.c_int), ("nodes", ctypes.c_int), ("block_table", ctypes.c_void_p),
+                ("max_blocks", ctypes.c_int), ("seq_lens", ctypes.c_void_p), ("tree_lens", ctypes.c_void_p),
+                ("path", ctypes.c_void_p), ("kept", ctypes.c_void_p), ("prot", ctypes.c_void_p),
+                ("draft_rows", ctypes.c_void_p), ("new_lens", ctypes.c_void_p), ("dev_err", ctypes.c_void_p)]
 
 
 class QmlaError(RuntimeError):
@@ -136,12 +171,17 @@ def lib():
     L.qmla_mla_decode_c4r4.argtypes = [vp, i32, vp, vp, i32, i32, vp, i32, vp, vp, f32, vp, vp, vp, sz, vp, vp]
     L.qmla_mla_decode_c4r4.restype = i32
     L.qmla_rope_append.argtypes, L.qmla_rope_append.restype = [ctypes.POINTER(AppendDesc), vp], i32
+    L.qmla_rope_append_at.argtypes, L.qmla_rope_append_at.restype = [ctypes.POINTER(AppendDesc), vp, vp], i32
     L.qmla_cache_read.argtypes, L.qmla_cache_read.restype = [ctypes.POINTER(ReadDesc), vp], i32
     i64 = ctypes.c_longlong
     L.qmla_rope_query.argtypes = [vp, i64, i64, vp, i32, i32, vp, i32, i32, vp, i64, i64, vp, vp]
     L.qmla_rope_query.restype = i32
     L.qmla_mla_prefill.argtypes, L.qmla_mla_prefill.restype = [ctypes.POINTER(PrefillDesc), vp], i32
     L.qmla_prefill_workspace_bytes.argtypes, L.qmla_prefill_workspace_bytes.restype = [i32, i32], sz
+    L.qmla_mla_decode_tree.argtypes, L.qmla_mla_decode_tree.restype = [ctypes.POINTER(TreeDesc), vp], i32
+    L.qmla_tree_workspace_bytes.argtypes, L.qmla_tree_workspace_bytes.restype = [i32, i32, i32], sz
+    L.qmla_tree_verify.argtypes, L.qmla_tree_verify.restype = [ctypes.POINTER(VerifyDesc), vp], i32
+    L.qmla_cache_keep.argtypes, L.qmla_cache_keep.restype = [ctypes.POINTER(KeepDesc), vp], i32
     _lib = L
     return L
 
@@ -453,8 +493,9 @@ def rope_append(pool: torch.Tensor, cache_kind, latent: torch.Tensor, k_pe: torc
                 seq_ids: torch.Tensor | None, positions: torch.Tensor, block_table: torch.Tensor,
                 cos_sin: torch.Tensor, dev_err: torch.Tensor | None, norm_weight: torch.Tensor | None = None,
                 eps: float = 1e-6, norm: bool | None = None, interleaved: bool = False,
-                seq_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None, stream=None) -> None:
-    """qmla_rope_append: cache_kind 4, 2, "c4r4" or "bf16"; latent bf16 [n,512] and k_pe bf16
+                seq_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None, stream=None,
+                rope_positions: torch.Tensor | None = None) -> None:
+    """qmla_rope_append (with rope_positions int32 [n]: qmla_rope_append_at): cache_kind 4, 2, "c4r4" or "bf16"; latent bf16 [n,512] and k_pe bf16
     [n,64] with any row stride (columns of one projection output); cos_sin f32
     [rope_len,64]; norm_weight bf16 [512] (norm=True without it: weights of one);
     with prot (and seq_lens = lengths after this call) also the sink/recent rows."""
@@ -469,7 +510,10 @@ def rope_append(pool: torch.Tensor, cache_kind, latent: torch.Tensor, k_pe: torc
                    _flat("cos_sin", cos_sin, _F32, (rope_len, 64), dev), rope_len, 1 if interleaved else 0,
                    None if seq_ids is None else _flat("seq_ids", seq_ids, _I32, (n,), dev),
                    _flat("positions", positions, _I32, (n,), dev), n, seqs, table, per, lens, rows, err)
-    st = lib().qmla_rope_append(d, _raw_stream(stream, dev))
+    if rope_positions is None:
+        st = lib().qmla_rope_append(d, _raw_stream(stream, dev))
+    else:
+        st = lib().qmla_rope_append_at(d, _flat("rope_positions", rope_positions, _I32, (n,), dev), _raw_stream(stream, dev))
     if st:
         raise QmlaError("qmla_rope_append", st)
 
@@ -529,6 +573,98 @@ def mla_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pe: torch.T
     st = lib().qmla_mla_prefill(d, _raw_stream(stream, dev))
     if st:
         raise QmlaError("qmla_mla_prefill", st)
+
+
+def tree_workspace_bytes(batch: int, nodes: int, heads: int) -> int:
+    return int(lib().qmla_tree_workspace_bytes(batch, nodes, heads))
+
+
+def _ints(name: str, t, shape: tuple, dev: int):
+    return None if t is None else _flat(name, t, _I32, shape, dev)
+
+
+def _node_rows(draft_rows, seqs: int, dev: int):
+    return None if draft_rows is None else _flat("draft_rows", draft_rows, _BF16, (seqs, MAX_TREE_NODES, 576), dev)
+
+
+def mla_decode_tree(pool: torch.Tensor, cache_kind, q_latent: torch.Tensor, q_pe: torch.Tensor,
+                    block_table: torch.Tensor, seq_lens: torch.Tensor, parents: torch.Tensor, softmax_scale: float,
+                    out: torch.Tensor, lse: torch.Tensor | None, workspace: torch.Tensor,
+                    dev_err: torch.Tensor | None, tree_lens: torch.Tensor | None = None,
+                    prot: torch.Tensor | None = None, draft_rows: torch.Tensor | None = None, stream=None,
+                    max_len: int = 0) -> None:
+    """qmla_mla_decode_tree: cache_kind 4, 2, "c4r4" or "bf16"; q_latent bf16 [B,T,H,512], q_pe bf16
+    [B,T,H,64], parents int32 [B,T], seq_lens (nodes included) and tree_lens int32 [B]; out bf16
+    [B,T,H,512], lse f32 [B,T,H]; prot [B,132,576] with draft_rows bf16 [B,64,576]; workspace of
+    tree_workspace_bytes(B, T, H) bytes, any type and shape."""
+    dev = _current_device()
+    B, T, H, _ = q_latent.shape
+    at, kind, blocks, table, seqs, per, lens, kept, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)
+    if seqs != B:
+        _refuse("block_table", block_table, _I32, (B, per), dev)
+    d = TreeDesc(at, kind, blocks, _flat("q_latent", q_latent, _BF16, (B, T, H, 512), dev),
+                 _flat("q_pe", q_pe, _BF16, (B, T, H, 64), dev), B, T, H, max_len,
+                 _flat("parents", parents, _I32, (B, T), dev), _ints("tree_lens", tree_lens, (B,), dev), table, per,
+                 softmax_scale, lens, kept, _node_rows(draft_rows, B, dev), _flat("out", out, _BF16, (B, T, H, 512), dev),
+                 None if lse is None else _flat("lse", lse, _F32, (B, T, H), dev),
+                 _flat("workspace", workspace, workspace.dtype, workspace.shape, dev), workspace.nbytes, err)
+    st = lib().qmla_mla_decode_tree(d, _raw_stream(stream, dev))
+    if st:
+        raise QmlaError("qmla_mla_decode_tree", st)
+
+
+_PROBS = {_F32: 0, _BF16: 1}
+
+
+def _probs(name: str, t: torch.Tensor, dtype: torch.dtype, shape: tuple, dev: int) -> int:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or t.stride(-1) != 1:
+        _refuse(name, t, dtype, shape, dev, rows=True)
+    return t.data_ptr()
+
+
+def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.Tensor, parents: torch.Tensor,
+                uniforms: torch.Tensor, path: torch.Tensor, kept: torch.Tensor, next_token: torch.Tensor,
+                dev_err: torch.Tensor | None, tree_lens: torch.Tensor | None = None, stream=None) -> None:
+    """qmla_tree_verify: target and draft (None: drafts chosen without randomness) probabilities f32 or
+    bf16 [B,T,V] with any sequence and row strides; tokens, parents int32 [B,T], uniforms f32 [B,T],
+    tree_lens int32 [B]; path int32 [B,T], kept and next_token int32 [B] are written."""
+    dev = _current_device()
+    B, T, V = shape = tuple(target.shape)
+    dtype = target.dtype
+    if dtype not in _PROBS:
+        raise ValueError(f"target must be float32 or bfloat16, not {dtype}")
+    at = _probs("target", target, dtype, shape, dev)
+    ts, tr, _ = target.stride()
+    if draft is None:
+        q, ds, dr = None, 0, 0
+    else:
+        q = _probs("draft", draft, dtype, shape, dev)
+        ds, dr, _ = draft.stride()
+    d = VerifyDesc(at, ts, tr, q, ds, dr, _PROBS[dtype], B, T, V, _flat("tokens", tokens, _I32, (B, T), dev),
+                   _flat("parents", parents, _I32, (B, T), dev), _ints("tree_lens", tree_lens, (B,), dev),
+                   _flat("uniforms", uniforms, _F32, (B, T), dev), _flat("path", path, _I32, (B, T), dev),
+                   _flat("kept", kept, _I32, (B,), dev), _flat("next_token", next_token, _I32, (B,), dev),
+                   _error_word(dev_err, dev))
+    st = lib().qmla_tree_verify(d, _raw_stream(stream, dev))
+    if st:
+        raise QmlaError("qmla_tree_verify", st)
+
+
+def cache_keep(pool: torch.Tensor, cache_kind, block_table: torch.Tensor, seq_lens: torch.Tensor, path: torch.Tensor,
+               kept: torch.Tensor, new_lens: torch.Tensor, dev_err: torch.Tensor | None,
+               tree_lens: torch.Tensor | None = None, prot: torch.Tensor | None = None,
+               draft_rows: torch.Tensor | None = None, stream=None) -> None:
+    """qmla_cache_keep: path int32 [B,T] and kept int32 [B] as tree_verify leaves them; seq_lens (nodes
+    included), tree_lens and new_lens int32 [B]; new_lens may be seq_lens."""
+    dev = _current_device()
+    at, kind, blocks, table, seqs, per, lens, rows, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)
+    T = path.size(1)
+    d = KeepDesc(at, kind, blocks, seqs, T, table, per, lens, _ints("tree_lens", tree_lens, (seqs,), dev),
+                 _flat("path", path, _I32, (seqs, T), dev), _flat("kept", kept, _I32, (seqs,), dev), rows,
+                 _node_rows(draft_rows, seqs, dev), _flat("new_lens", new_lens, _I32, (seqs,), dev), err)
+    st = lib().qmla_cache_keep(d, _raw_stream(stream, dev))
+    if st:
+        raise QmlaError("qmla_cache_keep", st)
 
 
 def workspace_for(batch: int, heads: int, device="cuda") -> torch.Tensor:

@@ -48,6 +48,12 @@ int current_device_info(DevInfo& out) {
 
 bool known_cache(int kind) { return kind == 4 || kind == 2 || kind == QMLA_CACHE_C4R4 || kind == QMLA_CACHE_BF16; }
 
+// The protection buffer and the rows of a tree's nodes come together.
+bool bad_node_rows(int kind, const void* prot, const void* draft_rows) {
+  return (prot == nullptr) != (draft_rows == nullptr) || !aligned(prot, 16) || !aligned(draft_rows, 16) ||
+         (prot != nullptr && kind == QMLA_CACHE_BF16);
+}
+
 int append_common_checks(const void* pool, int num_blocks, const uint16_t* latent, const uint16_t* k_pe,
                          const int32_t* positions, int n, const int32_t* table, int num_seqs,
                          int max_blocks) {
@@ -371,6 +377,10 @@ int qmla_mla_decode_ex(const qmla_decode_desc* d, qmla_stream_t stream) {
 }
 
 int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream) {
+  return qmla_rope_append_at(desc, nullptr, stream);
+}
+
+int qmla_rope_append_at(const qmla_append_desc* desc, const int32_t* rope_positions_dev, qmla_stream_t stream) {
   if (desc == nullptr || !known_cache(desc->cache_kind)) return QMLA_ERR_INVALID_ARG;
   qmla_append_desc own = *desc;  // (a single row's strides are not used)
   if (own.n == 1) own.latent_stride = qmla::kDc, own.k_pe_stride = qmla::kDr;
@@ -385,12 +395,13 @@ int qmla_rope_append(const qmla_append_desc* desc, qmla_stream_t stream) {
                              !aligned(d->seq_lens, 4)))
     return QMLA_ERR_INVALID_ARG;
   if (d->n == 0) return QMLA_OK;
-  if (d->cos_sin == nullptr || !aligned(d->cos_sin, 16) || !aligned(d->seq_ids, 4)) return QMLA_ERR_INVALID_ARG;
+  if (d->cos_sin == nullptr || !aligned(d->cos_sin, 16) || !aligned(d->seq_ids, 4) || !aligned(rope_positions_dev, 4))
+    return QMLA_ERR_INVALID_ARG;
   if (d->latent_stride % 2 != 0 || d->k_pe_stride % 2 != 0 || (d->n > 1 && (d->latent_stride < qmla::kDc || d->k_pe_stride < qmla::kDr)))
     return QMLA_ERR_INVALID_ARG;
   DevInfo di;
   if ((st = current_device_info(di)) != QMLA_OK) return st;
-  cudaError_t e = qmla::launch_rope_append(*d, reinterpret_cast<cudaStream_t>(stream));
+  cudaError_t e = qmla::launch_rope_append(*d, rope_positions_dev, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
 }
 
@@ -477,6 +488,85 @@ int qmla_mla_prefill(const qmla_prefill_desc* d, qmla_stream_t stream) {
   int st = current_device_info(di);
   if (st != QMLA_OK) return st;
   cudaError_t e = qmla::launch_prefill(*d, di.sms, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
+}
+
+size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads) {
+  if (batch <= 0 || nodes < 1 || nodes > QMLA_MAX_TREE_NODES || heads < 1 || heads > 128) return 0;
+  DevInfo di;
+  if (current_device_info(di) != QMLA_OK) return 0;
+  return qmla::tree_workspace_bytes(batch, nodes * heads, di.sms);
+}
+
+int qmla_mla_decode_tree(const qmla_tree_desc* d, qmla_stream_t stream) {
+  if (d == nullptr || !known_cache(d->cache_kind)) return QMLA_ERR_INVALID_ARG;
+  if (d->batch <= 0 || d->nodes < 1 || d->nodes > QMLA_MAX_TREE_NODES || d->heads < 1 || d->heads > 128 ||
+      d->num_blocks <= 0 || d->max_blocks <= 0 || d->max_len < 0 ||
+      static_cast<long long>(d->max_blocks) * qmla::kBlockTokens > INT32_MAX)
+    return QMLA_ERR_INVALID_ARG;
+  if (!(d->softmax_scale > 0.0f) || d->softmax_scale > 1e30f) return QMLA_ERR_INVALID_ARG;
+  if (d->pool == nullptr || d->q_latent == nullptr || d->q_pe == nullptr || d->parents == nullptr ||
+      d->block_table == nullptr || d->seq_lens == nullptr || d->out == nullptr || d->workspace == nullptr)
+    return QMLA_ERR_INVALID_ARG;
+  if (!aligned(d->pool, 32) || !aligned(d->q_latent, 16) || !aligned(d->q_pe, 16) || !aligned(d->parents, 4) ||
+      !aligned(d->tree_lens, 4) || !aligned(d->block_table, 4) || !aligned(d->seq_lens, 4) || !aligned(d->out, 16) ||
+      !aligned(d->lse, 4) || !aligned(d->workspace, 256))
+    return QMLA_ERR_INVALID_ARG;
+  if (bad_node_rows(d->cache_kind, d->prot, d->draft_rows)) return QMLA_ERR_INVALID_ARG;
+  // (the plan counts 128-token tiles of 64-row groups in 32 bits)
+  const int groups = (d->nodes * d->heads + qmla::head_group_size(d->nodes * d->heads) - 1) / qmla::head_group_size(d->nodes * d->heads);
+  if (static_cast<long long>(d->batch) * groups * ((d->max_blocks + 1ll) / 2) > INT32_MAX) return QMLA_ERR_INVALID_ARG;
+  DevInfo di;
+  int st = current_device_info(di);
+  if (st != QMLA_OK) return st;
+  if (d->workspace_bytes < qmla::tree_workspace_bytes(d->batch, d->nodes * d->heads, di.sms))
+    return QMLA_ERR_WORKSPACE_TOO_SMALL;
+  cudaError_t e = qmla::launch_decode_tree(*d, di.sms, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
+}
+
+int qmla_tree_verify(const qmla_verify_desc* desc, qmla_stream_t stream) {
+  if (desc == nullptr || (desc->probs != QMLA_PROBS_F32 && desc->probs != QMLA_PROBS_BF16)) return QMLA_ERR_INVALID_ARG;
+  if (desc->batch < 1 || desc->batch > 65535 || desc->nodes < 1 || desc->nodes > QMLA_MAX_TREE_NODES ||
+      desc->vocab < 1 || desc->vocab > (1 << 24))
+    return QMLA_ERR_INVALID_ARG;
+  if (desc->target == nullptr || desc->tokens == nullptr || desc->parents == nullptr || desc->uniforms == nullptr ||
+      desc->path == nullptr || desc->kept == nullptr || desc->next_token == nullptr)
+    return QMLA_ERR_INVALID_ARG;
+  const uintptr_t size = desc->probs == QMLA_PROBS_F32 ? 4 : 2;
+  if (!aligned(desc->target, size) || !aligned(desc->draft, size) || !aligned(desc->tokens, 4) ||
+      !aligned(desc->parents, 4) || !aligned(desc->tree_lens, 4) || !aligned(desc->uniforms, 4) ||
+      !aligned(desc->path, 4) || !aligned(desc->kept, 4) || !aligned(desc->next_token, 4))
+    return QMLA_ERR_INVALID_ARG;
+  qmla_verify_desc d = *desc;  // (a single row's strides are not used)
+  if (d.batch == 1) d.target_seq_stride = d.draft_seq_stride = 0;
+  if (d.nodes == 1) d.target_row_stride = d.draft_row_stride = 0;
+  if (d.draft == nullptr) d.draft_seq_stride = d.draft_row_stride = 0;
+  for (long long s : {d.target_seq_stride, d.target_row_stride, d.draft_seq_stride, d.draft_row_stride})
+    if (s < 0 || s >= (1ll << 40)) return QMLA_ERR_INVALID_ARG;
+  DevInfo di;
+  int st = current_device_info(di);
+  if (st != QMLA_OK) return st;
+  cudaError_t e = qmla::launch_tree_verify(d, di.sms, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
+}
+
+int qmla_cache_keep(const qmla_keep_desc* d, qmla_stream_t stream) {
+  if (d == nullptr || !known_cache(d->cache_kind)) return QMLA_ERR_INVALID_ARG;
+  if (d->batch <= 0 || d->nodes < 1 || d->nodes > QMLA_MAX_TREE_NODES || d->num_blocks <= 0 || d->max_blocks <= 0 ||
+      static_cast<long long>(d->max_blocks) * qmla::kBlockTokens > INT32_MAX)
+    return QMLA_ERR_INVALID_ARG;
+  if (d->pool == nullptr || d->block_table == nullptr || d->seq_lens == nullptr || d->path == nullptr ||
+      d->kept == nullptr || d->new_lens == nullptr)
+    return QMLA_ERR_INVALID_ARG;
+  if (!aligned(d->pool, 32) || !aligned(d->block_table, 4) || !aligned(d->seq_lens, 4) || !aligned(d->tree_lens, 4) ||
+      !aligned(d->path, 4) || !aligned(d->kept, 4) || !aligned(d->new_lens, 4))
+    return QMLA_ERR_INVALID_ARG;
+  if (bad_node_rows(d->cache_kind, d->prot, d->draft_rows)) return QMLA_ERR_INVALID_ARG;
+  DevInfo di;
+  int st = current_device_info(di);
+  if (st != QMLA_OK) return st;
+  cudaError_t e = qmla::launch_cache_keep(*d, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
 }
 

@@ -151,17 +151,19 @@ __device__ __forceinline__ uint32_t pack_codes(const uint32_t (&w)[4], float s, 
 }
 
 // Looks up and validates the destination of token i: its block id, or -1 (after
-// recording the error) when the token cannot be written.
+// recording the error) when the token cannot be written. turns: the positions that the
+// fused writer takes the angles of, all below rope_len.
 __device__ __forceinline__ int token_block(int num_blocks, const int32_t* seq_ids, const int32_t* positions, int i,
                                            const int32_t* table, int num_seqs, int max_blocks, uint32_t* dev_err,
-                                           int& seq, int& pos, int rope_len = INT32_MAX) {
+                                           int& seq, int& pos, const int32_t* turns = nullptr, int rope_len = 0) {
   seq = seq_ids != nullptr ? seq_ids[i] : i;
   pos = positions[i];
+  const bool turned = turns == nullptr || static_cast<unsigned>(turns[i]) < static_cast<unsigned>(rope_len);
   if (seq < 0 || seq >= num_seqs) {
     report(dev_err, QMLA_DEVERR_BAD_SEQ);
     return -1;
   }
-  if (pos < 0 || pos >= max_blocks * kBlockTokens || pos >= rope_len) {
+  if (pos < 0 || pos >= max_blocks * kBlockTokens || !turned) {
     report(dev_err, QMLA_DEVERR_BAD_POSITION);
     return -1;
   }
@@ -188,6 +190,7 @@ struct RowTransform {
   float eps;
   const float* cos_sin;  // [rope_len][64]: cos[32] | sin[32]
   int rope_len;
+  const int32_t* turns;  // [n] position of each token's angles
   bool interleaved;
 };
 
@@ -198,14 +201,13 @@ struct RowTransform {
 // same answer about far rows. Every thread of the block takes part; the eight content
 // warps meet at a barrier of their own.
 __device__ __forceinline__ void content_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-__device__ __forceinline__ void transform_rows(uint4& raw, const RowTransform& tr, const int32_t* __restrict__ positions,
-                                               int n, int tok, int g, int lane) {
+__device__ __forceinline__ void transform_rows(uint4& raw, const RowTransform& tr, int n, int tok, int g, int lane) {
   __shared__ float2 share[8][4];
   __shared__ uint32_t tops[8][4];
   const int piece = lane & 7, sub = lane >> 3;
   uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
   if (g == 8) {
-    const int pos = tok < n ? positions[tok] : -1;
+    const int pos = tok < n ? tr.turns[tok] : -1;
     Angles a;
     load_angles(a, pos >= 0 && pos < tr.rope_len ? tr.cos_sin + static_cast<size_t>(pos) * kDr : nullptr, piece,
                 tr.interleaved);
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     const int tok = tok0 + 4 * own;
     int seq = 0, pos = 0;
     const int blk = token_block(num_blocks, seq_ids, positions, tok, table, num_seqs, max_blocks,
-                                piece == own && g == 0 ? dev_err : nullptr, seq, pos, FUSED ? tr.rope_len : INT32_MAX);
+                                piece == own && g == 0 ? dev_err : nullptr, seq, pos, FUSED ? tr.turns : nullptr, tr.rope_len);
     if (blk >= 0) {
       dst = blk * kBlockTokens + pos % kBlockTokens;
       if (prot != nullptr) {
@@ -336,7 +338,7 @@ __global__ void __launch_bounds__(kAppendThreads) quant_append_kernel(
     }
   }
   if constexpr (FUSED) {
-    transform_rows(raw[0], tr, positions, n, tok0, g, lane);
+    transform_rows(raw[0], tr, n, tok0, g, lane);
     if constexpr (CB == kBf16Rows) {
       if (dst >= 0)
         reinterpret_cast<uint4*>(pool + static_cast<size_t>(dst / kBlockTokens) * kBf16BlockBytes +
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(kWideThreads, 5) wide_append_kernel(
   if (tok < n) {
     int seq = 0, pos = 0;
     const int blk = token_block(num_blocks, seq_ids, positions, tok, table, num_seqs, max_blocks,
-                                piece == 0 ? dev_err : nullptr, seq, pos, tr.rope_len);
+                                piece == 0 ? dev_err : nullptr, seq, pos, tr.turns, tr.rope_len);
     if (blk >= 0) {
       dst = blk * kBlockTokens + pos % kBlockTokens;
       if (prot != nullptr) {
@@ -515,7 +517,8 @@ __global__ void __launch_bounds__(kWideThreads, 5) wide_append_kernel(
         if (pos >= lens[seq] - kRecentTokens) ring = seq * kProtRows + kSinkTokens + pos % kRecentTokens;
       }
     }
-    if (pos >= 0 && pos < tr.rope_len) angles = tr.cos_sin + static_cast<size_t>(pos) * kDr;
+    const int turn = tr.turns[tok];
+    if (turn >= 0 && turn < tr.rope_len) angles = tr.cos_sin + static_cast<size_t>(turn) * kDr;
   }
   {
     Angles a;
@@ -703,7 +706,7 @@ cudaError_t launch_quant_append(void* pool, int c_bits, int num_blocks, const ui
   return cudaGetLastError();
 }
 
-cudaError_t launch_rope_append(const qmla_append_desc& d, cudaStream_t stream) {
+cudaError_t launch_rope_append(const qmla_append_desc& d, const int32_t* rope_positions, cudaStream_t stream) {
   const AppendArgs a = {d.pool,        d.num_blocks, d.latent,     d.k_pe,    d.seq_ids, d.positions, d.n,
                         d.block_table, d.num_seqs,   d.max_blocks, d.dev_err, d.prot,    d.prot != nullptr ? d.seq_lens : nullptr};
   RowTransform tr;
@@ -714,6 +717,7 @@ cudaError_t launch_rope_append(const qmla_append_desc& d, cudaStream_t stream) {
   tr.eps = d.norm_eps;
   tr.cos_sin = d.cos_sin;
   tr.rope_len = d.rope_len;
+  tr.turns = rope_positions != nullptr ? rope_positions : d.positions;
   tr.interleaved = d.interleaved != 0;
   const bool vec = aligned16(d.latent, d.k_pe) && d.latent_stride % 8 == 0 && d.k_pe_stride % 8 == 0;
   auto* f = d.cache_kind == kC4R4

@@ -41,8 +41,17 @@
 
 #include "decode_common.cuh"
 
+// decode_tree.cu compiles these kernels once more for query rows that are the nodes of a
+// tree: masks in place of the causal limit, the nodes' rows beside the protected ones,
+// results in bf16. The constant keeps the plain decode's code free of all that.
+#ifndef QMLA_DECODE_TREE
+#define QMLA_DECODE_TREE 0
+#endif
+
 namespace qmla {
 namespace {
+
+constexpr bool kTree = QMLA_DECODE_TREE != 0;
 
 constexpr int kChunkBytes = kTileTokens * 128;   // 128 tokens x 64 fp16 channels
 constexpr int kWorkers = 8;                      // warps 0..7: dequantise, softmax, epilogue
@@ -167,6 +176,9 @@ __device__ __forceinline__ RowRef row_ref(const Params& p, const Sched& s, int r
   r.entry = p.table[static_cast<size_t>(b) * p.max_blocks + lb];
   return r;
 }
+__device__ __forceinline__ const uint8_t* row_source(const Params& p, const RowRef& r, int row) {
+  return kTree ? prot_row_tree(p, r, row) : prot_row(p, r, row);
+}
 // Query image of one unit: HG heads x 576 channels in fp16 laid out exactly as
 // the K-major, 128-byte-swizzled shared-memory operand ([chunk][head][128 B]),
 // channels permuted within each 8-channel piece like the cache rows. Piece
@@ -223,6 +235,12 @@ struct Cols {
 // heads of earlier query tokens do not see the last positions: Eq. mla_compact's
 // causal mask, see row_limit).
 
+// Whether head column i of the warp is admitted by the row's limit (of a tree: its mask).
+__device__ __forceinline__ bool sees(int lim, int i) {
+  if constexpr (kTree) return (static_cast<uint32_t>(lim) >> i) & 1u;
+  return i >= lim;
+}
+
 // W columns of this thread's row of S^T starting at t_s: the sum of the
 // kQkParts partials (HG columns apart), added in a fixed order.
 template <int HG, int W>
@@ -255,7 +273,7 @@ __device__ __forceinline__ void warp_tile_max(uint32_t t_s, float sl2, int lim, 
     load_s<HG>(t_s + c * C::kW, r);
 #pragma unroll
     for (int jj = 0; jj < C::kW; ++jj) {
-      const float x = c * C::kW + jj >= lim ? __uint_as_float(r[jj]) * sl2 : -INFINITY;
+      const float x = sees(lim, c * C::kW + jj) ? __uint_as_float(r[jj]) * sl2 : -INFINITY;
       const float mx = warp_max_f32(x);
       if (lane == jj) red_q[c * C::kW + jj] = mx;
     }
@@ -287,7 +305,7 @@ __device__ __forceinline__ bool compute_p(uint32_t t_s, const float* mr, float s
     for (int jj = 0; jj < C::kW; jj += 2) {
       const float x0 = __uint_as_float(r[jj]) * sl2 - m[jj];
       const float x1 = __uint_as_float(r[jj + 1]) * sl2 - m[jj + 1];
-      const bool ok0 = c * C::kW + jj >= lim, ok1 = c * C::kW + jj + 1 >= lim;
+      const bool ok0 = sees(lim, c * C::kW + jj), ok1 = sees(lim, c * C::kW + jj + 1);
       over |= (ok0 && x0 > kRescaleLog2) || (ok1 && x1 > kRescaleLog2);
       pk[c * (C::kW / 2) + (jj >> 1)] = pack_h2(ok0 ? ex2_approx(x0) : 0.0f, ok1 ? ex2_approx(x1) : 0.0f);
     }
@@ -309,6 +327,23 @@ __device__ __forceinline__ bool compute_p(uint32_t t_s, const float* mr, float s
 template <int HG>
 __device__ __forceinline__ int row_limit(const Params& p, const TileInfo& ti, int row, int cb0) {
   constexpr int kPer = Cols<HG>::kPerWarp;
+  static_assert(kPer <= 32, "a tree's mask");
+  if constexpr (kTree) {
+    // The nodes that see this position, each a run of hpt head columns.
+    if (row >= ti.ntok) return 0;
+    const TreeSeq& tree = p.trees[ti.b];
+    const int d = kTileTokens * ti.j + row - tree.ctx;
+    const uint64_t nodes = d < 0 ? tree.alive : tree.seen_by[d];
+    const int v0 = ti.hg * HG + cb0;
+    int t = v0 / p.hpt, left = p.hpt - (v0 - t * p.hpt);
+    uint32_t mask = 0u;
+#pragma unroll 1
+    for (int i = 0; i < kPer && t < kMaxNodes; ++t, i += left, left = p.hpt) {
+      const uint32_t run = (left >= 32 ? ~0u : (1u << left) - 1u) << i;
+      if ((nodes >> t) & 1u) mask |= run;
+    }
+    return static_cast<int>(mask);
+  }
   if (row >= ti.ntok) return kPer;
   const int d = kTileTokens * ti.j + row - (ti.len - p.q_tokens);
   if (d <= 0) return 0;
@@ -360,6 +395,8 @@ __device__ bool epilogue(const Params& p, const SegEnd& e, Ctrl& ctl, uint32_t t
   const int hn = min(HG, p.heads - h0);
   float* const obase =
       e.whole ? p.out + (static_cast<size_t>(e.b) * p.heads + h0) * kDc : p.part_o + e.pidx * HG * kDc;
+  __nv_bfloat16* const tbase =  // (a tree's results are bf16)
+      reinterpret_cast<__nv_bfloat16*>(p.out) + (static_cast<size_t>(e.b) * p.heads + h0) * kDc;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int P = i * 128 + row;  // position in the reconstructed row
@@ -382,7 +419,12 @@ __device__ bool epilogue(const Params& p, const SegEnd& e, Ctrl& ctl, uint32_t t
 #pragma unroll
       for (int jj = 0; jj < C::kW; ++jj) {
         const int h = cb0 + c * C::kW + jj;
-        if (h < hn) orow[static_cast<size_t>(h) * kDc] = __uint_as_float(r[jj]) * f[jj];
+        const float o = __uint_as_float(r[jj]) * f[jj];
+        if (kTree && e.whole) {
+          if (h < hn) tbase[static_cast<size_t>(h) * kDc + (P & ~7) + Perm<CB>::at(P & 7)] = __float2bfloat16_rn(o);
+        } else if (h < hn) {
+          orow[static_cast<size_t>(h) * kDc] = o;
+        }
       }
     }
   }
@@ -469,7 +511,7 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
     ref0.b = sc.u / p.n_hg;
   }
   // A protected row reads its BF16 row instead of the packed cache.
-  const uint8_t* psrc_cur = PROT ? prot_row(p, ref0, row) : nullptr;
+  const uint8_t* psrc_cur = PROT ? row_source(p, ref0, row) : nullptr;
   if constexpr (PROT) {
     if (psrc_cur != nullptr) {
 #pragma unroll
@@ -504,7 +546,7 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
     // The next tile's block pointer (its table entry was loaded a tile ago)
     // and the table entry of the tile after it.
     bool valid_nx = false;
-    const uint8_t* psrc_nx = PROT ? prot_row(p, ref_nx, row) : nullptr;
+    const uint8_t* psrc_nx = PROT ? row_source(p, ref_nx, row) : nullptr;
     if constexpr (PROT) {
       // The next tile's protected rows into L2 now (no registers held): their
       // chunk loads come after each slot wait and would otherwise miss to DRAM.
@@ -912,6 +954,66 @@ __global__ void __launch_bounds__(kThreads, 1) decode_main(const Params p) {
 // ------------------------------------------------------------ prep / combine
 constexpr int kPrepThreads = 1024;
 
+// Sets of nodes of kTreesPerBlock sequences from b0 on, a thread per node: each finds the
+// nodes above its own by doubling (after step i it holds 2^i of them, and its 2^i-th
+// ancestor). kMaxNodes stands for "none above".
+constexpr int kTreesPerBlock = kPrepThreads / kMaxNodes;
+__device__ __forceinline__ void make_trees(const Params& p, int b0) {
+  __shared__ uint64_t line[kTreesPerBlock][kMaxNodes + 1];
+  __shared__ uint8_t up[kTreesPerBlock][kMaxNodes + 1], bad[kTreesPerBlock][kMaxNodes + 1];
+  const int i = threadIdx.x / kMaxNodes, t = threadIdx.x % kMaxNodes, b = b0 + i;
+  const bool any = b < p.batch;
+  int n = 0, parent = -1;
+  if (any) {
+    n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
+    if (n < 0 || n > p.q_tokens || n > p.seq_lens[b]) n = 0;  // (reported with the lengths)
+    if (t < n) parent = p.parents[static_cast<size_t>(b) * p.q_tokens + t];
+  }
+  const bool wrong = t < n && (parent < -1 || parent >= t);
+  if (wrong) report(p.dev_err, QMLA_DEVERR_BAD_TREE);
+  line[i][t] = t < n ? 1ull << t : 0ull;
+  up[i][t] = static_cast<uint8_t>(wrong || parent < 0 ? kMaxNodes : parent);
+  bad[i][t] = wrong ? 1 : 0;
+  if (t == 0) {
+    line[i][kMaxNodes] = 0ull;
+    up[i][kMaxNodes] = kMaxNodes;
+    bad[i][kMaxNodes] = 0;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int s = 1; s < kMaxNodes; s *= 2) {
+    const int a = up[i][t];
+    const uint64_t l = line[i][t] | line[i][a];
+    const uint8_t w = bad[i][t] | bad[i][a], a2 = up[i][a];
+    __syncthreads();
+    line[i][t] = l;
+    bad[i][t] = w;
+    up[i][t] = a2;
+    __syncthreads();
+  }
+  const bool ok = t < n && bad[i][t] == 0;
+  const uint64_t mine = ok ? line[i][t] : 0ull;
+  __syncthreads();
+  line[i][t] = mine;
+  __syncthreads();
+  uint64_t below = 0ull, alive = 0ull;
+#pragma unroll 4
+  for (int u = 0; u < kMaxNodes; ++u) {
+    const uint64_t l = line[i][u];
+    if ((l >> t) & 1ull) below |= 1ull << u;
+    if (l != 0ull) alive |= 1ull << u;
+  }
+  griddep_wait();  // (see prep_kernel)
+  if (!any) return;
+  TreeSeq& o = p.trees[b];
+  o.seen_by[t] = below;
+  o.line[t] = mine;
+  if (t == 0) {
+    o.alive = alive;
+    o.ctx = p.seq_lens[b] - n;
+  }
+}
+
 // Block 0: tile prefix over units (u = b * n_hg + hg), tiles = ceil(len / 128).
 // Blocks 1..: one query-image piece (16 bytes) per thread.
 // The cache writers let this kernel start beside them, so until it has waited for its
@@ -928,6 +1030,13 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
     const long long idx = static_cast<long long>(blockIdx.x - 1) * kPrepThreads + threadIdx.x;
     constexpr int kPieces = kNumChunks * HG * 8;
     const long long images = static_cast<long long>(p.batch) * p.n_img;
+    if constexpr (kTree) {
+      const int first = static_cast<int>((images * kPieces + kPrepThreads - 1) / kPrepThreads) + 1;
+      if (static_cast<int>(blockIdx.x) >= first) {
+        make_trees(p, (static_cast<int>(blockIdx.x) - first) * kTreesPerBlock);
+        return;
+      }
+    }
     if (idx >= images * kPieces) return;
     const int u = static_cast<int>(idx / kPieces);
     const int b = u / p.n_img;
@@ -953,6 +1062,13 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
       if (len < 0 || len > p.max_blocks * kBlockTokens) {
         report(p.dev_err, QMLA_DEVERR_BAD_POSITION);
         len = 0;
+      }
+      if constexpr (kTree) {
+        const int n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
+        if (n < 0 || n > p.q_tokens || n > len) {
+          report(p.dev_err, QMLA_DEVERR_BAD_TREE);
+          len = 0;
+        }
       }
       tiles = (len + kTileTokens - 1) / kTileTokens;
     }
@@ -1041,6 +1157,17 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
 // running form rescales by 2^(M_old - M_new) when M grows). One block per
 // (unit, 4 heads), a warp per head, 16 channels per thread; the loads of the
 // next partial do not depend on the previous one's arithmetic.
+// Four results in a row, element `at` of the output on.
+__device__ __forceinline__ void store_out(const Params& p, size_t at, float4 v) {
+  if constexpr (kTree) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+    reinterpret_cast<uint2*>(p.out)[at / 4] =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  } else {
+    reinterpret_cast<float4*>(p.out)[at / 4] = v;
+  }
+}
+
 template <int HG>
 __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
   griddep_wait();  // the partials of the main kernel
@@ -1052,10 +1179,10 @@ __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
   const int h0 = (u - b * p.n_hg) * HG;
   if (h >= HG || h0 + h >= p.heads) return;
   const int P0 = p.prefix[u], P1 = p.prefix[u + 1], T = p.prefix[units];
-  float4* out = reinterpret_cast<float4*>(p.out + (static_cast<size_t>(b) * p.heads + h0 + h) * kDc) + lane * 4;
+  const size_t out = (static_cast<size_t>(b) * p.heads + h0 + h) * kDc + lane * 16;
   if (P0 == P1) {
 #pragma unroll
-    for (int v = 0; v < 4; ++v) out[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int v = 0; v < 4; ++v) store_out(p, out + 4 * v, make_float4(0.f, 0.f, 0.f, 0.f));
     if (p.lse != nullptr && lane == 0) p.lse[static_cast<size_t>(b) * p.heads + h0 + h] = -INFINITY;
     return;
   }
@@ -1089,7 +1216,8 @@ __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) out[v] = make_float4(acc[v].x * inv, acc[v].y * inv, acc[v].z * inv, acc[v].w * inv);
+  for (int v = 0; v < 4; ++v)
+    store_out(p, out + 4 * v, make_float4(acc[v].x * inv, acc[v].y * inv, acc[v].z * inv, acc[v].w * inv));
   if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(b) * p.heads + h0 + h] = (M + log2f(l)) * kLn2;
 }
 
@@ -1117,9 +1245,9 @@ __global__ void __launch_bounds__(kWideThreads) combine_wide_kernel(const Params
   const int P0 = p.prefix[u], P1 = p.prefix[u + 1], T = p.prefix[units];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int v = tid & 127, grp = tid >> 7;
-  float4* out = reinterpret_cast<float4*>(p.out + (static_cast<size_t>(b) * p.heads + h0 + h) * kDc) + v;
+  const size_t out = (static_cast<size_t>(b) * p.heads + h0 + h) * kDc + v * 4;
   if (P0 == P1) {
-    if (grp == 0) *out = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (grp == 0) store_out(p, out, make_float4(0.f, 0.f, 0.f, 0.f));
     if (p.lse != nullptr && tid == 0) p.lse[static_cast<size_t>(b) * p.heads + h0 + h] = -INFINITY;
     return;
   }
@@ -1175,7 +1303,7 @@ __global__ void __launch_bounds__(kWideThreads) combine_wide_kernel(const Params
       acc.w += q.w;
     }
     const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-    *out = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    store_out(p, out, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
     if (tid == 0 && p.lse != nullptr)
       p.lse[static_cast<size_t>(b) * p.heads + h0 + h] = any ? (M + log2f(L)) * kLn2 : -INFINITY;
   }
@@ -1283,7 +1411,8 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
   const bool pdl = ev0 == nullptr && ev1 == nullptr;
   const long long units = static_cast<long long>(prm.batch) * prm.n_hg;
   const long long pieces = static_cast<long long>(prm.batch) * prm.n_img * kNumChunks * HG * 8;
-  const unsigned prep_blocks = static_cast<unsigned>(1 + (pieces + kPrepThreads - 1) / kPrepThreads);
+  const unsigned prep_blocks = static_cast<unsigned>(1 + (pieces + kPrepThreads - 1) / kPrepThreads +
+                                                     (kTree ? (prm.batch + kTreesPerBlock - 1) / kTreesPerBlock : 0));
   if ((e = launch_k(prep_kernel<CB, HG, PAIR>, dim3(prep_blocks), dim3(kPrepThreads), 0, stream, pdl, prm)) != cudaSuccess)
     return e;
   if (ev0 != nullptr && (e = cudaEventRecord(ev0, stream)) != cudaSuccess) return e;
@@ -1313,6 +1442,8 @@ cudaError_t launch_hg(int hg, bool pair, const Params& prm, cudaStream_t stream,
 }
 
 }  // namespace
+
+#if !QMLA_DECODE_TREE
 
 #ifdef QMLA_TRACE_BUILD
 unsigned long long* g_trace_buf = nullptr;  // set by set_trace_buffer
@@ -1455,5 +1586,7 @@ cudaError_t set_trace_buffer(void* buf) {
   return cudaSuccess;
 }
 #endif
+
+#endif  // !QMLA_DECODE_TREE
 
 }  // namespace qmla

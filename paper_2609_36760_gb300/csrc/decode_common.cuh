@@ -12,6 +12,9 @@
 
 namespace qmla {
 
+constexpr int kMaxNodes = 64;  // of a tree (QMLA_MAX_TREE_NODES)
+struct TreeSeq;
+
 struct Params {
   const uint8_t* pool;
   // sink4/local128 protection buffer [batch][132][576] bf16, or null (unprotected).
@@ -46,6 +49,21 @@ struct Params {
   int grid;  // ranges the tile list is cut into
   int sms;
   unsigned long long* trace;  // trace builds only: per-CTA event clocks, else null
+  // Decodes of a tree of nodes (decode_tree.cu) only; q_tokens then counts the nodes.
+  const int32_t* parents;     // [batch][q_tokens]
+  const int32_t* tree_lens;   // [batch] nodes of each sequence, or null: q_tokens each
+  const uint8_t* draft_rows;  // [batch][64][576] bf16 rows of the nodes (with prot), or null
+  TreeSeq* trees;             // [batch], written by the prep kernel
+};
+
+// One sequence's tree as the kernels use it. Nodes are bits; a node with a bad parent, or
+// below one, is in no set. seen_by[j]: the nodes that see node j (itself and those below).
+struct TreeSeq {
+  uint64_t seen_by[kMaxNodes];
+  uint64_t line[kMaxNodes];  // the node and those above it, or 0
+  uint64_t alive;            // the nodes, all of which see the context
+  int ctx;                   // cached tokens before the tree
+  int pad;
 };
 
 // Main kernel of the CTA-pair decode (decode_pair.cu) for a plan over 128-head
@@ -251,6 +269,24 @@ __device__ __forceinline__ const uint8_t* prot_row(const Params& p, const RowRef
   if (pos < kSinkTokens) {
     pr = pos;
   } else if (pos >= r.len - kRecentTokens) {
+    pr = kSinkTokens + pos % kRecentTokens;
+  } else {
+    return nullptr;
+  }
+  return p.prot + (static_cast<size_t>(r.b) * kProtRows + pr) * (kDqk * 2);
+}
+// The same for a decode of a tree: P_L of the context alone, whose ring the drafts have not
+// touched; a node's row comes from the caller's rows of the nodes.
+__device__ __forceinline__ const uint8_t* prot_row_tree(const Params& p, const RowRef& r, int row) {
+  if (p.prot == nullptr || !r.has) return nullptr;
+  const int pos = kTileTokens * r.j + row;
+  if (pos >= r.len) return nullptr;
+  const int ctx = p.trees[r.b].ctx;
+  int pr;
+  if (pos >= ctx) return p.draft_rows + (static_cast<size_t>(r.b) * kMaxNodes + pos - ctx) * (kDqk * 2);
+  if (pos < kSinkTokens) {
+    pr = pos;
+  } else if (pos >= ctx - kRecentTokens) {
     pr = kSinkTokens + pos % kRecentTokens;
   } else {
     return nullptr;

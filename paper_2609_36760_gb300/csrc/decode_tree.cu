@@ -1,0 +1,80 @@
+// Attention of a tree of drafted tokens over a paged cache: query row (t, h), node t and
+// head h, sees the context and the nodes on its path (Eq. mla_compact, with a mask of nodes
+// in the place of the causal one).
+//
+// The kernels are the decode's (decode.cu, compiled here for trees); prep also finds the
+// sets of nodes above and below each node.
+#define QMLA_DECODE_TREE 1
+#include "decode.cu"
+
+namespace qmla {
+namespace {
+
+struct TreeWorkspace {
+  DecodeWorkspace decode;
+  size_t trees_off, total;
+};
+TreeWorkspace tree_workspace_layout(int batch, int rows, int grid) {
+  TreeWorkspace w;
+  w.decode = decode_workspace_layout(batch, rows, grid);
+  w.trees_off = (w.decode.total + 255) & ~static_cast<size_t>(255);
+  w.total = w.trees_off + static_cast<size_t>(batch) * sizeof(TreeSeq);
+  return w;
+}
+
+template <int CB, bool PROT>
+cudaError_t launch_rows(int hg, const Params& prm, cudaStream_t stream) {
+  if (hg == 16) return launch_impl<CB, 16, PROT, false>(prm, stream, nullptr, nullptr);
+  if (hg == 32) return launch_impl<CB, 32, PROT, false>(prm, stream, nullptr, nullptr);
+  return launch_impl<CB, 64, PROT, false>(prm, stream, nullptr, nullptr);
+}
+
+}  // namespace
+
+size_t tree_workspace_bytes(int batch, int rows, int grid) { return tree_workspace_layout(batch, rows, grid).total; }
+
+cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t stream) {
+  const int rows = d.nodes * d.heads, hg = head_group_size(rows);
+  const TreeWorkspace w = tree_workspace_layout(d.batch, rows, grid);
+  uint8_t* ws = static_cast<uint8_t*>(d.workspace);
+  Params prm{};
+  prm.pool = static_cast<const uint8_t*>(d.pool);
+  prm.prot = static_cast<const uint8_t*>(d.prot);
+  prm.num_blocks = d.num_blocks;
+  prm.q_lat = reinterpret_cast<const __nv_bfloat16*>(d.q_latent);
+  prm.q_pe = reinterpret_cast<const __nv_bfloat16*>(d.q_pe);
+  prm.batch = d.batch;
+  prm.heads = rows;
+  prm.n_img = prm.n_hg = (rows + hg - 1) / hg;
+  prm.grid = prm.sms = grid;
+  prm.q_tokens = d.nodes;
+  prm.hpt = d.heads;
+  prm.table = d.block_table;
+  prm.max_blocks = d.max_blocks;
+  prm.seq_lens = d.seq_lens;
+  prm.scale_log2 = d.softmax_scale * 1.4426950408889634f;
+  prm.out = reinterpret_cast<float*>(d.out);  // (bf16)
+  prm.lse = d.lse;
+  prm.prefix = reinterpret_cast<const int32_t*>(ws + w.decode.prefix_off);
+  prm.prefix_w = reinterpret_cast<int32_t*>(ws + w.decode.prefix_off);
+  prm.cta_info = reinterpret_cast<int4*>(ws + w.decode.cta_off);
+  prm.cta_first = prm.cta_info + grid;
+  prm.cta_t0 = reinterpret_cast<int32_t*>(prm.cta_first + grid);
+  prm.part_o = reinterpret_cast<float*>(ws + w.decode.part_o_off);
+  prm.part_ml = reinterpret_cast<float*>(ws + w.decode.part_ml_off);
+  prm.qimg = ws + w.decode.qimg_off;
+  prm.dev_err = d.dev_err;
+  prm.parents = d.parents;
+  prm.tree_lens = d.tree_lens;
+  prm.draft_rows = reinterpret_cast<const uint8_t*>(d.draft_rows);
+  prm.trees = reinterpret_cast<TreeSeq*>(ws + w.trees_off);
+  const bool prot = prm.prot != nullptr;
+  switch (d.cache_kind) {
+    case 4: return prot ? launch_rows<4, true>(hg, prm, stream) : launch_rows<4, false>(hg, prm, stream);
+    case 2: return prot ? launch_rows<2, true>(hg, prm, stream) : launch_rows<2, false>(hg, prm, stream);
+    case kC4R4: return prot ? launch_rows<kC4R4, true>(hg, prm, stream) : launch_rows<kC4R4, false>(hg, prm, stream);
+    default: return launch_rows<16, false>(hg, prm, stream);
+  }
+}
+
+}  // namespace qmla

@@ -20,8 +20,9 @@ cudaError_t launch_bf16_append(void* pool, int num_blocks, const uint16_t* laten
                                const int32_t* positions, int n, const int32_t* table, int num_seqs,
                                int max_blocks, uint32_t* dev_err, cudaStream_t stream);
 
-// The fused writer (see qmla_rope_append; d.n > 0).
-cudaError_t launch_rope_append(const qmla_append_desc& d, cudaStream_t stream);
+// The fused writer (see qmla_rope_append; d.n > 0). rope_positions: null, or the positions
+// whose angles turn the keys.
+cudaError_t launch_rope_append(const qmla_append_desc& d, const int32_t* rope_positions, cudaStream_t stream);
 cudaError_t launch_cache_read(const qmla_read_desc& d, cudaStream_t stream);
 cudaError_t launch_rope_query(const uint16_t* q, long long q_token, long long q_head, const int32_t* positions, int n,
                               int heads, const float* cos_sin, int rope_len, bool interleaved, uint16_t* out,
@@ -61,6 +62,12 @@ struct DecodeArgs {
   cudaEvent_t ev_after_main = nullptr;
 };
 cudaError_t launch_decode(const DecodeArgs& a, cudaStream_t stream);
+// The decode of a tree of nodes (decode_tree.cu), d checked.
+size_t tree_workspace_bytes(int batch, int rows, int grid);
+cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t stream);
+// Verification of a tree of drafts, and its accepted rows (speculate.cu), d checked.
+cudaError_t launch_tree_verify(const qmla_verify_desc& d, int sms, cudaStream_t stream);
+cudaError_t launch_cache_keep(const qmla_keep_desc& d, cudaStream_t stream);
 // Whether this decode runs on CTA pairs (decode_pair.cu) or on decode_main.
 bool decode_on_pairs(const DecodeArgs& a);
 // Test hook: tile j of sequence b as the decode kernel builds it, [128][576] fp16.

@@ -1,0 +1,498 @@
+// Verification of a tree of drafted tokens (qmla_tree_verify) and what its result does to a
+// cache (qmla_cache_keep).
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace qmla {
+namespace {
+
+constexpr int kMaxNodes = QMLA_MAX_TREE_NODES;
+
+// ------------------------------------------------------------- error-free sums
+// hi + lo with |lo| at most half a unit of hi: about 48 bits. A draw from 10^5 tokens has that
+// many borders a sum may fall on the wrong side of, and a decision that depended on the order
+// of a sum would differ from run to run of another launch shape; with an error of 2^-48 that
+// is one draw in 10^9. (In double the additions alone would take 40 us for 64 x 131,072
+// tokens: the card adds 1.25 T doubles a second.)
+struct Pair {
+  float hi, lo;
+};
+__device__ __forceinline__ Pair two_sum(float a, float b) {
+  const float s = __fadd_rn(a, b), bb = __fadd_rn(s, -a);
+  return {s, __fadd_rn(__fadd_rn(a, -__fadd_rn(s, -bb)), __fadd_rn(b, -bb))};
+}
+__device__ __forceinline__ Pair normal(float s, float e) {  // |s| >= |e|
+  const float h = __fadd_rn(s, e);
+  return {h, __fadd_rn(e, -__fadd_rn(h, -s))};
+}
+__device__ __forceinline__ Pair add(Pair a, Pair b) {
+  Pair s = two_sum(a.hi, b.hi);
+  const Pair t = two_sum(a.lo, b.lo);
+  s = normal(s.hi, __fadd_rn(s.lo, t.hi));
+  return normal(s.hi, __fadd_rn(s.lo, t.lo));
+}
+__device__ __forceinline__ Pair times(Pair a, float u) {
+  const float h = __fmul_rn(a.hi, u);
+  return normal(h, __fmaf_rn(a.lo, u, __fmaf_rn(a.hi, u, -h)));
+}
+__device__ __forceinline__ bool above(Pair a, Pair b) { return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo); }
+__device__ __forceinline__ double value(Pair a) { return static_cast<double>(a.hi) + static_cast<double>(a.lo); }
+__device__ __forceinline__ Pair shfl_up(Pair a, int d) {
+  return {__shfl_up_sync(0xffffffffu, a.hi, d), __shfl_up_sync(0xffffffffu, a.lo, d)};
+}
+// Sum over the lanes up to this one.
+__device__ __forceinline__ Pair warp_scan(Pair x, int lane) {
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const Pair y = shfl_up(x, d);
+    if (lane >= d) x = add(y, x);
+  }
+  return x;
+}
+
+// --------------------------------------------------------------- verification
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// What is left of p after refusals that took a times q: max(p - a q, 0), exact to 2^-48
+// (a NaN stays one).
+__device__ __forceinline__ Pair left_over(float p, float q, Pair a) {
+  const float h = __fmul_rn(a.hi, q);
+  const Pair s = two_sum(p, -h);
+  const Pair r = normal(s.hi, __fadd_rn(s.lo, -__fmaf_rn(a.lo, q, __fmaf_rn(a.hi, q, -h))));
+  return r.hi <= 0.0f ? Pair{0.0f, 0.0f} : r;
+}
+
+constexpr int kVerifyThreads = 512, kVerifyWarps = kVerifyThreads / 32;
+constexpr int kMaxCluster = 8;
+
+struct VerifyShared {
+  int token[kMaxNodes], parent[kMaxNodes];
+  float u[kMaxNodes], p[kMaxNodes], q[kMaxNodes];  // a node's token in its parent's distributions
+  Pair part[2][kMaxCluster * kVerifyWarps];        // every warp's sum, of every CTA
+  Pair before[kMaxCluster * kVerifyWarps];         // sum of the warps before
+  Pair total;
+  Pair scan[kVerifyWarps];
+  // the walk's state, written by warp 0
+  int cur, last, refused_n;
+  Pair a;
+  int refused[kMaxNodes];
+  unsigned long long found;
+};
+
+// The terms of the sums of a node: p and q its rows, `a` as in qmla_tree_verify; refused:
+// tokens that are out (no draft probabilities).
+template <typename T>
+struct Terms {
+  const T* p;
+  const T* q;  // null where a = 0
+  Pair a;
+  const int* refused;
+  int n;
+  __device__ __forceinline__ Pair at(int v) const {
+    const float x = as_float(p[v]);
+    if (q != nullptr) return left_over(x, as_float(q[v]), a);
+    Pair r = {x <= 0.0f ? 0.0f : x, 0.0f};
+    for (int i = 0; i < n; ++i)
+      if (refused[i] == v) r.hi = 0.0f;
+    return r;
+  }
+};
+
+// One cluster a sequence. The walk itself is a warp's, done alike in every CTA; the sums over
+// the vocabulary are all warps', warp w of the cluster taking the w-th piece of the row.
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const qmla_verify_desc d, int ctas) {
+  __shared__ VerifyShared sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = static_cast<int>(cluster_ctarank()), b = blockIdx.y;
+  const size_t first = static_cast<size_t>(b) * d.nodes;
+  int n = d.tree_lens != nullptr ? d.tree_lens[b] : d.nodes;
+  if (n < 0 || n > d.nodes) {
+    if (tid == 0 && rank == 0) report(d.dev_err, QMLA_DEVERR_BAD_TREE);
+    n = 0;
+  }
+  if (n == 0) {  // (alike in all CTAs of the cluster)
+    if (rank == 0 && tid < d.nodes) d.path[first + tid] = -1;
+    if (rank == 0 && tid == 0) {
+      d.kept[b] = 0;
+      d.next_token[b] = -1;
+    }
+    return;
+  }
+  const T* const target = static_cast<const T*>(d.target) + static_cast<size_t>(b) * d.target_seq_stride;
+  const T* const draft =
+      d.draft == nullptr ? nullptr : static_cast<const T*>(d.draft) + static_cast<size_t>(b) * d.draft_seq_stride;
+  if (tid < kMaxNodes) {
+    int token = -1, parent = -1;
+    float u = 0.0f, p = 0.0f, q = 0.0f;
+    if (tid < n) {
+      token = d.tokens[first + tid];
+      parent = d.parents[first + tid];
+      u = fminf(fmaxf(d.uniforms[first + tid], 0.0f), 1.0f - 0x1p-24f);
+      if (tid > 0) {
+        if (parent < -1 || parent >= tid || token < 0 || token >= d.vocab) {
+          if (rank == 0) report(d.dev_err, QMLA_DEVERR_BAD_TREE);
+          parent = -1;
+        }
+        if (parent >= 0) {
+          p = as_float(target[static_cast<size_t>(parent) * d.target_row_stride + token]);
+          if (draft != nullptr) q = as_float(draft[static_cast<size_t>(parent) * d.draft_row_stride + token]);
+        }
+      } else {
+        parent = -1;
+      }
+    }
+    sh.token[tid] = token;
+    sh.parent[tid] = parent;
+    sh.u[tid] = u;
+    sh.p[tid] = p;
+    sh.q[tid] = q;
+  }
+  __syncthreads();
+
+  const int chunk = (d.vocab + ctas * kVerifyWarps - 1) / (ctas * kVerifyWarps);
+  // Warp 0's state: the node, its children not yet looked at, the refusals so far.
+  int cur = 0, kept = 1;
+  uint64_t children = 0ull;
+  double a = 0.0, mass = 1.0;
+  int my_path = lane == 0 ? 0 : -1, my_path2 = -1;  // entries lane and lane + 32
+  auto enter = [&](int node) {
+    cur = node;
+    a = 0.0;
+    mass = 1.0;
+    const uint32_t lo = __ballot_sync(0xffffffffu, sh.parent[lane] == node);
+    const uint32_t hi = __ballot_sync(0xffffffffu, sh.parent[lane + 32] == node);
+    children = static_cast<uint64_t>(hi) << 32 | lo;
+  };
+  if (warp == 0) {
+    enter(0);
+    if (lane == 0) sh.refused_n = 0;
+    __syncwarp();
+  }
+  cluster_sync_all();  // every CTA of the cluster runs before another writes into it
+  for (int pass = 0;; ++pass) {
+    if (warp == 0) {
+      // On to the next sum that is needed: after a refusal, or where the walk ends.
+      bool refusal = false;
+      while (children != 0ull && !refusal) {
+        const int t = __ffsll(static_cast<long long>(children)) - 1;
+        children &= children - 1;
+        const double u = sh.u[t], p = sh.p[t], q = sh.q[t];
+        if (draft != nullptr) {
+          const double r = fmax(p - a * q, 0.0);
+          if (u * q * mass < r) {
+            if (lane == (kept & 31)) (kept < 32 ? my_path : my_path2) = t;
+            ++kept;
+            enter(t);
+          } else {
+            a += mass;
+            refusal = true;
+          }
+        } else {
+          bool gone = false;
+          const int m = sh.refused_n;
+          for (int i = 0; i < m; ++i) gone |= sh.refused[i] == sh.token[t];
+          const double r = gone ? 0.0 : fmax(p, 0.0);
+          __syncwarp();
+          if (u * mass < r) {
+            if (lane == (kept & 31)) (kept < 32 ? my_path : my_path2) = t;
+            ++kept;
+            enter(t);
+            if (lane == 0) sh.refused_n = 0;
+          } else if (!gone) {
+            mass -= r;
+            if (lane == 0) {
+              sh.refused[m] = sh.token[t];
+              sh.refused_n = m + 1;
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (lane == 0) {
+        sh.cur = cur;
+        sh.last = children == 0ull;
+        sh.a.hi = static_cast<float>(a);
+        sh.a.lo = static_cast<float>(a - static_cast<double>(sh.a.hi));
+        sh.found = ~0ull;
+      }
+    }
+    __syncthreads();
+    Terms<T> terms;
+    terms.p = target + static_cast<size_t>(sh.cur) * d.target_row_stride;
+    terms.a = sh.a;
+    terms.q = sh.a.hi != 0.0f ? draft + static_cast<size_t>(sh.cur) * d.draft_row_stride : nullptr;
+    terms.refused = sh.refused;
+    terms.n = sh.refused_n;
+    const bool last = sh.last;
+    // ---- this warp's piece of the sum
+    const int w = rank * kVerifyWarps + warp;
+    const int v0 = min(w * chunk, d.vocab), v1 = min(v0 + chunk, d.vocab);
+    Pair sum = {0.0f, 0.0f};
+    for (int v = v0 + lane; v < v1; v += 32) sum = add(sum, terms.at(v));
+    sum = warp_scan(sum, lane);
+    Pair* const part = sh.part[pass & 1];
+    if (lane == 31) {
+      for (int r = 0; r < ctas; ++r) {
+        const uint32_t to = cluster_map(smem_u32(&part[w]), r);
+        st_cluster_u32(to, __float_as_uint(sum.hi));
+        st_cluster_u32(to + 4, __float_as_uint(sum.lo));
+      }
+    }
+    cluster_sync_all();
+    if (warp == 0) {
+      Pair carry = {0.0f, 0.0f};
+      for (int i = 0; i < ctas * kVerifyWarps; i += 32) {
+        const bool any = i + lane < ctas * kVerifyWarps;
+        Pair x = any ? part[i + lane] : Pair{0.0f, 0.0f};
+        const Pair incl = add(carry, warp_scan(x, lane));
+        Pair excl = shfl_up(incl, 1);
+        if (lane == 0) excl = carry;
+        if (any) sh.before[i + lane] = excl;
+        carry = {__shfl_sync(0xffffffffu, incl.hi, 31), __shfl_sync(0xffffffffu, incl.lo, 31)};
+      }
+      if (lane == 0) sh.total = carry;
+      mass = value(carry);
+    }
+    __syncthreads();
+    if (!last) continue;
+
+    // ---- the draw: the warp whose piece the threshold lies in, then its tokens
+    const Pair total = sh.total;
+    const Pair cut = times(total, sh.u[0]);
+    const bool fine = total.hi > 0.0f && total.hi < INFINITY;
+    const int warps = ctas * kVerifyWarps;
+    // (the last piece with anything in it, where rounding leaves no piece above the cut)
+    if (fine && tid < warps) {
+      const Pair end = add(sh.before[tid], part[tid]);
+      if (above(end, cut)) atomicMin(&sh.found, static_cast<unsigned long long>(tid));
+    }
+    __syncthreads();
+    int piece = static_cast<int>(sh.found);
+    if (fine && sh.found == ~0ull)
+      for (piece = warps - 1; piece > 0 && !(part[piece].hi > 0.0f); --piece) {}
+    __syncthreads();
+    if (fine && piece / kVerifyWarps == rank) {
+      if (tid == 0) sh.found = ~0ull;
+      const int each = (chunk + kVerifyThreads - 1) / kVerifyThreads;
+      const int p0 = min(piece * chunk, d.vocab), p1 = min(p0 + chunk, d.vocab);
+      const int t0 = min(p0 + tid * each, p1), t1 = min(t0 + each, p1);
+      Pair s = {0.0f, 0.0f};
+      for (int v = t0; v < t1; ++v) s = add(s, terms.at(v));
+      Pair incl = warp_scan(s, lane);
+      if (lane == 31) sh.scan[warp] = incl;
+      Pair excl = shfl_up(incl, 1);
+      if (lane == 0) excl = {0.0f, 0.0f};
+      __syncthreads();
+      Pair base = sh.before[piece];
+      for (int i = 0; i < warp; ++i) base = add(base, sh.scan[i]);
+      Pair run = add(base, excl);
+      // (ordered so that a token above the cut comes before the fallback, the last with weight)
+      unsigned long long mine = ~0ull;
+      for (int v = t0; v < t1; ++v) {
+        const Pair x = terms.at(v);
+        run = add(run, x);
+        if (x.hi > 0.0f) {
+          if (above(run, cut)) {
+            mine = v;
+            break;
+          }
+          mine = (1ull << 40) - v;
+        }
+      }
+      if (mine != ~0ull) atomicMin(&sh.found, mine);
+      __syncthreads();
+      if (tid == 0) {
+        const unsigned long long f = sh.found;
+        d.next_token[b] = static_cast<int>(f < (1ull << 32) ? f : (1ull << 40) - f);
+      }
+    }
+    if (rank == 0 && warp == 0) {
+      if (lane < d.nodes) d.path[first + lane] = my_path;
+      if (lane + 32 < d.nodes) d.path[first + lane + 32] = my_path2;
+      if (lane == 0) {
+        d.kept[b] = kept;
+        if (!fine) {
+          d.next_token[b] = -1;
+          report(d.dev_err, QMLA_DEVERR_BAD_PROBS);
+        }
+      }
+    }
+    break;
+  }
+}
+
+// ----------------------------------------------------------------- kept rows
+// The bytes of a slot: pieces of 16, 4, 2 and 1 bytes, and where each lies.
+template <int CB>
+struct Slot;
+template <>
+struct Slot<4> {
+  using L = BlockLayout<4>;
+  static constexpr int n16 = 18, n4 = 9, n2 = 0, n1 = 0, bytes = L::kBytes;
+  __device__ static int at16(int k, int slot) { return L::code_off(k >> 1, slot) + 16 * (k & 1); }
+  __device__ static int at4(int k, int slot) { return L::sz_off(k, slot); }
+  __device__ static int at2(int, int) { return 0; }
+  __device__ static int at1(int, int) { return 0; }
+};
+template <>
+struct Slot<2> {
+  using L = BlockLayout<2>;
+  static constexpr int n16 = 10, n4 = 9, n2 = 0, n1 = 0, bytes = L::kBytes;
+  __device__ static int at16(int k, int slot) {
+    return k < 8 ? L::code_off(k, slot) : L::code_off(8, slot) + 16 * (k - 8);
+  }
+  __device__ static int at4(int k, int slot) { return L::sz_off(k, slot); }
+  __device__ static int at2(int, int) { return 0; }
+  __device__ static int at1(int, int) { return 0; }
+};
+template <>
+struct Slot<kC4R4> {
+  using L = BlockLayout<kC4R4>;
+  static constexpr int n16 = 18, n4 = 1, n2 = 8, n1 = 9, bytes = L::kBytes;
+  __device__ static int at16(int k, int slot) { return L::code_off(k >> 1, slot) + 16 * (k & 1); }
+  __device__ static int at4(int, int slot) { return L::pe_scale_off(slot); }
+  __device__ static int at2(int k, int slot) { return L::c_scale_off(k, slot); }
+  __device__ static int at1(int k, int slot) { return L::zero_off(k, slot); }
+};
+template <>
+struct Slot<16> {
+  static constexpr int n16 = 72, n4 = 0, n2 = 0, n1 = 0, bytes = kBf16BlockBytes;
+  __device__ static int at16(int k, int slot) { return slot * (kDqk * 2) + 16 * k; }
+  __device__ static int at4(int, int) { return 0; }
+  __device__ static int at2(int, int) { return 0; }
+  __device__ static int at1(int, int) { return 0; }
+};
+
+constexpr int kKeepThreads = 256;
+
+// One block a sequence. All rows are in registers before any is written: a row may lie where
+// another goes to.
+template <int CB>
+__global__ void __launch_bounds__(kKeepThreads) keep_kernel(const qmla_keep_desc d) {
+  using S = Slot<CB>;
+  __shared__ uint8_t* from[kMaxNodes];  // block of the row to move, or null
+  __shared__ uint8_t* to[kMaxNodes];
+  __shared__ int from_slot[kMaxNodes], to_slot[kMaxNodes], node[kMaxNodes];
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const int len = d.seq_lens[b], n = d.tree_lens != nullptr ? d.tree_lens[b] : d.nodes, kept = d.kept[b];
+  const bool bad_len = len < 0 || len > d.max_blocks * kBlockTokens;
+  bool good = !bad_len && n >= 0 && n <= d.nodes && n <= len && kept >= 0 && kept <= n;
+  if (good && tid < kept) {
+    const int32_t* path = d.path + static_cast<size_t>(b) * d.nodes;
+    const int me = path[tid], before = tid > 0 ? path[tid - 1] : -1;
+    good = me > before && me < n;
+    node[tid] = me;
+  }
+  good = __syncthreads_and(good);
+  if (tid == 0) {
+    if (bad_len) report(d.dev_err, QMLA_DEVERR_BAD_POSITION);
+    else if (!good) report(d.dev_err, QMLA_DEVERR_BAD_TREE);
+    d.new_lens[b] = good ? len - n + kept : len;
+  }
+  if (!good) return;
+  const int ctx = len - n;
+  uint8_t* const pool = static_cast<uint8_t*>(d.pool);
+  if (tid < kept) {
+    const int32_t* row = d.block_table + static_cast<size_t>(b) * d.max_blocks;
+    const int src = ctx + node[tid], dst = ctx + tid;
+    uint8_t *f = nullptr, *t = nullptr;
+    if (src != dst) {
+      const int sb = row[src / kBlockTokens], db = row[dst / kBlockTokens];
+      if (sb < 0 || sb >= d.num_blocks || db < 0 || db >= d.num_blocks) {
+        report(d.dev_err, QMLA_DEVERR_BAD_BLOCK);
+      } else {
+        f = pool + static_cast<size_t>(sb) * S::bytes;
+        t = pool + static_cast<size_t>(db) * S::bytes;
+      }
+    }
+    from[tid] = f;
+    to[tid] = t;
+    from_slot[tid] = src % kBlockTokens;
+    to_slot[tid] = dst % kBlockTokens;
+  }
+  __syncthreads();
+  constexpr int r16 = (kMaxNodes * S::n16 + kKeepThreads - 1) / kKeepThreads;
+  constexpr int r4 = (kMaxNodes * S::n4 + kKeepThreads - 1) / kKeepThreads;
+  constexpr int r2 = (kMaxNodes * S::n2 + kKeepThreads - 1) / kKeepThreads;
+  constexpr int r1 = (kMaxNodes * S::n1 + kKeepThreads - 1) / kKeepThreads;
+  uint4 x16[r16 > 0 ? r16 : 1];
+  uint32_t x4[r4 > 0 ? r4 : 1];
+  uint16_t x2[r2 > 0 ? r2 : 1];
+  uint8_t x1[r1 > 0 ? r1 : 1];
+#define QMLA_EACH(R, N, AT, TYPE, X, BASE, SLOT, BODY)                          \
+  _Pragma("unroll") for (int e = 0; e < (R); ++e) {                             \
+    const int item = e * kKeepThreads + tid;                                    \
+    const int i = item / ((N) > 0 ? (N) : 1), k = item - i * (N);               \
+    if (i < kept && from[i] != nullptr) {                                       \
+      TYPE* const at = reinterpret_cast<TYPE*>(BASE[i] + S::AT(k, SLOT[i]));    \
+      BODY;                                                                     \
+    }                                                                           \
+  }
+  QMLA_EACH(r16, S::n16, at16, uint4, x16, from, from_slot, x16[e] = *at)
+  QMLA_EACH(r4, S::n4, at4, uint32_t, x4, from, from_slot, x4[e] = *at)
+  QMLA_EACH(r2, S::n2, at2, uint16_t, x2, from, from_slot, x2[e] = *at)
+  QMLA_EACH(r1, S::n1, at1, uint8_t, x1, from, from_slot, x1[e] = *at)
+  __syncthreads();
+  QMLA_EACH(r16, S::n16, at16, uint4, x16, to, to_slot, *at = x16[e])
+  QMLA_EACH(r4, S::n4, at4, uint32_t, x4, to, to_slot, *at = x4[e])
+  QMLA_EACH(r2, S::n2, at2, uint16_t, x2, to, to_slot, *at = x2[e])
+  QMLA_EACH(r1, S::n1, at1, uint8_t, x1, to, to_slot, *at = x1[e])
+#undef QMLA_EACH
+  if (CB != 16 && d.prot != nullptr) {
+    // (64 positions at most, so no two in a ring row)
+    constexpr int kPieces = kDqk * 2 / 16;
+    const uint4* rows = reinterpret_cast<const uint4*>(d.draft_rows) + static_cast<size_t>(b) * kMaxNodes * kPieces;
+    uint4* const keep = static_cast<uint4*>(d.prot) + static_cast<size_t>(b) * kProtRows * kPieces;
+    for (int item = tid; item < kept * kPieces; item += kKeepThreads) {
+      const int i = item / kPieces, k = item - i * kPieces, pos = ctx + i;
+      const uint4 x = rows[node[i] * kPieces + k];
+      keep[(kSinkTokens + pos % kRecentTokens) * kPieces + k] = x;
+      if (pos < kSinkTokens) keep[pos * kPieces + k] = x;
+    }
+  }
+}
+
+template <typename T>
+cudaError_t launch_verify(const qmla_verify_desc& d, int ctas, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas, d.batch);
+  cfg.blockDim = dim3(kVerifyThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {static_cast<unsigned>(ctas), 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, verify_kernel<T>, d, ctas);
+}
+
+}  // namespace
+
+cudaError_t launch_tree_verify(const qmla_verify_desc& d, int /*sms*/, cudaStream_t stream) {
+  int ctas = 1;
+  while (ctas < kMaxCluster && d.vocab > 4096 * ctas) ctas *= 2;
+  return d.probs == QMLA_PROBS_F32 ? launch_verify<float>(d, ctas, stream)
+                                   : launch_verify<__nv_bfloat16>(d, ctas, stream);
+}
+
+cudaError_t launch_cache_keep(const qmla_keep_desc& d, cudaStream_t stream) {
+  const dim3 grid(d.batch), block(kKeepThreads);
+  switch (d.cache_kind) {
+    case 4: keep_kernel<4><<<grid, block, 0, stream>>>(d); break;
+    case 2: keep_kernel<2><<<grid, block, 0, stream>>>(d); break;
+    case kC4R4: keep_kernel<kC4R4><<<grid, block, 0, stream>>>(d); break;
+    default: keep_kernel<16><<<grid, block, 0, stream>>>(d); break;
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace qmla

@@ -586,8 +586,9 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *     S[b,t,h,p] = softmax_scale * (q_latent[b,t,h,:] . C_hat[b,p,:] + q_pe[b,t,h,:] . K_hat[b,p,:]),
  *                  p < ctx or p - ctx in A(t)
  *     out[b,t,h,:] = RN_bf16(sum_p softmax_p(S[b,t,h,:]) C_hat[b,p,:]);  lse[b,t,h] = log sum_p exp(S[b,t,h,p])
- *   pool, cache_kind, num_blocks, block_table, max_blocks, max_len, softmax_scale, dev_err
+ *   pool, cache_kind, num_blocks, block_table, max_blocks, softmax_scale, dev_err
  *                   as in qmla_mla_decode_ex, any of the four cache kinds
+ *   max_len         a bound of seq_lens, or 0 (max_blocks x 64 then). Longer sequences are bad ones
  *   q_latent, q_pe  [batch, nodes, heads, 512] and [batch, nodes, heads, 64] bf16, 16-byte aligned
  *   nodes, heads    1 .. QMLA_MAX_TREE_NODES, 1 .. 128
  *   parents         [batch, nodes] int32
@@ -604,8 +605,10 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *                   qmla_rope_append_at writes these rows too.)
  *   out             [batch, nodes, heads, 512] bf16, 16-byte aligned
  *   lse             [batch, nodes, heads] float32, or NULL
- *   workspace       >= qmla_tree_workspace_bytes(batch, nodes, heads) bytes, 256-byte
- *                   aligned, scratch as for qmla_mla_decode
+ *   workspace       >= qmla_tree_workspace_bytes(batch, nodes, heads, 0) bytes, 256-byte
+ *                   aligned, scratch as for qmla_mla_decode. With the bytes for the call's
+ *                   max_len (or max_blocks x 64) tokens the context is dequantised once for all
+ *                   rows of a sequence, in the workspace
  * A node behind the last of its sequence gets out = 0 and lse = -inf. So do a node whose
  * parent is not an earlier node or -1 and the nodes below it (QMLA_DEVERR_BAD_TREE), and
  * every node of a sequence whose count is below 0, above `nodes` or above its length (the
@@ -636,8 +639,10 @@ typedef struct qmla_tree_desc {
 } qmla_tree_desc;
 int qmla_mla_decode_tree(const qmla_tree_desc* desc, qmla_stream_t stream);
 
-/* Workspace bytes qmla_mla_decode_tree needs on the current device; 0 for bad arguments. */
-size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads);
+/* Workspace bytes of qmla_mla_decode_tree on the current device for sequences up to max_tokens
+ * (1,152 bytes for each token of them, and as much again for the first 1,024), or, with
+ * max_tokens 0, the least that it needs; 0 for bad arguments. */
+size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens);
 
 /*
  * Walks each tree from node 0 and keeps the drafts that the target accepts, so that the

@@ -23,11 +23,12 @@ def line_of(parents, t: int) -> list[int] | None:
     return line
 
 
-def attend_tree(q_lat, q_pe, C, K, parents, n: int, tau: float):
+def attend_tree(q_lat, q_pe, C, K, parents, n: int, tau: float, values=None):
     """All T nodes' rows (q_lat [T, H, 512], q_pe [T, H, 64]) over a sequence whose rows C [L, 512]
     and K [L, 64] end with those of its n nodes: (out [T, H, 512], lse [T, H], the same with
-    |C| in C's place, for error bounds)."""
+    |C| in C's place, for error bounds). values: what is summed in C's place."""
     q_lat, q_pe, C, K = (np.asarray(x, np.float64) for x in (q_lat, q_pe, C, K))
+    V = C if values is None else np.asarray(values, np.float64)
     T, H = q_lat.shape[:2]
     out, mass, lse = np.zeros((T, H, C.shape[1])), np.zeros((T, H, C.shape[1])), np.full((T, H), -np.inf)
     ctx = C.shape[0] - n
@@ -40,7 +41,7 @@ def attend_tree(q_lat, q_pe, C, K, parents, n: int, tau: float):
         top = S.max(1, keepdims=True)
         e = np.exp(S - top)
         den = e.sum(1, keepdims=True)
-        out[t], mass[t] = (e / den) @ C[at], (e / den) @ np.abs(C[at])
+        out[t], mass[t] = (e / den) @ V[at], (e / den) @ np.abs(V[at])
         lse[t] = (top + np.log(den))[:, 0]
     return out, lse, mass
 

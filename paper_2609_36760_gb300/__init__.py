@@ -179,7 +179,7 @@ def lib():
     L.qmla_mla_prefill.argtypes, L.qmla_mla_prefill.restype = [ctypes.POINTER(PrefillDesc), vp], i32
     L.qmla_prefill_workspace_bytes.argtypes, L.qmla_prefill_workspace_bytes.restype = [i32, i32], sz
     L.qmla_mla_decode_tree.argtypes, L.qmla_mla_decode_tree.restype = [ctypes.POINTER(TreeDesc), vp], i32
-    L.qmla_tree_workspace_bytes.argtypes, L.qmla_tree_workspace_bytes.restype = [i32, i32, i32], sz
+    L.qmla_tree_workspace_bytes.argtypes, L.qmla_tree_workspace_bytes.restype = [i32] * 4, sz
     L.qmla_tree_verify.argtypes, L.qmla_tree_verify.restype = [ctypes.POINTER(VerifyDesc), vp], i32
     L.qmla_cache_keep.argtypes, L.qmla_cache_keep.restype = [ctypes.POINTER(KeepDesc), vp], i32
     _lib = L
@@ -575,8 +575,9 @@ def mla_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pe: torch.T
         raise QmlaError("qmla_mla_prefill", st)
 
 
-def tree_workspace_bytes(batch: int, nodes: int, heads: int) -> int:
-    return int(lib().qmla_tree_workspace_bytes(batch, nodes, heads))
+def tree_workspace_bytes(batch: int, nodes: int, heads: int, max_tokens: int = 0) -> int:
+    """Bytes that mla_decode_tree needs; with max_tokens those that it uses for sequences up to that length."""
+    return int(lib().qmla_tree_workspace_bytes(batch, nodes, heads, max_tokens))
 
 
 def _ints(name: str, t, shape: tuple, dev: int):
@@ -596,7 +597,7 @@ def mla_decode_tree(pool: torch.Tensor, cache_kind, q_latent: torch.Tensor, q_pe
     """qmla_mla_decode_tree: cache_kind 4, 2, "c4r4" or "bf16"; q_latent bf16 [B,T,H,512], q_pe bf16
     [B,T,H,64], parents int32 [B,T], seq_lens (nodes included) and tree_lens int32 [B]; out bf16
     [B,T,H,512], lse f32 [B,T,H]; prot [B,132,576] with draft_rows bf16 [B,64,576]; workspace of
-    tree_workspace_bytes(B, T, H) bytes, any type and shape."""
+    tree_workspace_bytes(B, T, H) bytes or more, any type and shape."""
     dev = _current_device()
     B, T, H, _ = q_latent.shape
     at, kind, blocks, table, seqs, per, lens, kept, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)

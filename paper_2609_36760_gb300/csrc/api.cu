@@ -491,11 +491,11 @@ int qmla_mla_prefill(const qmla_prefill_desc* d, qmla_stream_t stream) {
   return e == cudaSuccess ? QMLA_OK : cuda_fail(e);
 }
 
-size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads) {
-  if (batch <= 0 || nodes < 1 || nodes > QMLA_MAX_TREE_NODES || heads < 1 || heads > 128) return 0;
+size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens) {
+  if (batch <= 0 || max_tokens < 0 || nodes < 1 || nodes > QMLA_MAX_TREE_NODES || heads < 1 || heads > 128) return 0;
   DevInfo di;
   if (current_device_info(di) != QMLA_OK) return 0;
-  return qmla::tree_workspace_bytes(batch, nodes * heads, di.sms);
+  return qmla::tree_workspace_bytes(batch, nodes * heads, max_tokens, di.sms);
 }
 
 int qmla_mla_decode_tree(const qmla_tree_desc* d, qmla_stream_t stream) {
@@ -519,7 +519,7 @@ int qmla_mla_decode_tree(const qmla_tree_desc* d, qmla_stream_t stream) {
   DevInfo di;
   int st = current_device_info(di);
   if (st != QMLA_OK) return st;
-  if (d->workspace_bytes < qmla::tree_workspace_bytes(d->batch, d->nodes * d->heads, di.sms))
+  if (d->workspace_bytes < qmla::tree_workspace_bytes(d->batch, d->nodes * d->heads, 0, di.sms))
     return QMLA_ERR_WORKSPACE_TOO_SMALL;
   cudaError_t e = qmla::launch_decode_tree(*d, di.sms, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? QMLA_OK : cuda_fail(e);

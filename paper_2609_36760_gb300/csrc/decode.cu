@@ -177,7 +177,7 @@ __device__ __forceinline__ RowRef row_ref(const Params& p, const Sched& s, int r
   return r;
 }
 __device__ __forceinline__ const uint8_t* row_source(const Params& p, const RowRef& r, int row) {
-  return kTree ? prot_row_tree(p, r, row) : prot_row(p, r, row);
+  return kTree ? prot_row_tree(p, r, row, r.has ? p.trees[r.b].ctx : 0) : prot_row(p, r, row);
 }
 // Query image of one unit: HG heads x 576 channels in fp16 laid out exactly as
 // the K-major, 128-byte-swizzled shared-memory operand ([chunk][head][128 B]),
@@ -953,11 +953,11 @@ __global__ void __launch_bounds__(kThreads, 1) decode_main(const Params p) {
 
 // ------------------------------------------------------------ prep / combine
 constexpr int kPrepThreads = 1024;
+constexpr int kTreesPerBlock = kPrepThreads / kMaxNodes;
 
 // Sets of nodes of kTreesPerBlock sequences from b0 on, a thread per node: each finds the
 // nodes above its own by doubling (after step i it holds 2^i of them, and its 2^i-th
 // ancestor). kMaxNodes stands for "none above".
-constexpr int kTreesPerBlock = kPrepThreads / kMaxNodes;
 __device__ __forceinline__ void make_trees(const Params& p, int b0) {
   __shared__ uint64_t line[kTreesPerBlock][kMaxNodes + 1];
   __shared__ uint8_t up[kTreesPerBlock][kMaxNodes + 1], bad[kTreesPerBlock][kMaxNodes + 1];
@@ -1014,6 +1014,97 @@ __device__ __forceinline__ void make_trees(const Params& p, int b0) {
   }
 }
 
+// Eight values of one cache row, channels 8 i .. 8 i + 7 of chunk k, as the attention sees them:
+// the row's own bf16 values where src is set, else the packed row in `slot` of blk.
+template <int CB>
+__device__ __forceinline__ void row_values(const uint8_t* src, const uint8_t* blk, int slot, int k, int i, float (&f)[8]) {
+  if (CB == 16 || src != nullptr) {
+    const uint4 raw = ldg_nc_v4((src != nullptr ? src : blk + slot * (kDqk * 2)) + k * 128 + i * 16);
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f[2 * e] = bf16_lo(w[e]);
+      f[2 * e + 1] = bf16_hi(w[e]);
+    }
+    return;
+  }
+  if constexpr (CB != 16) {
+    using L = BlockLayout<CB>;
+    const uint8_t* codes = blk + L::code_off(k, slot);
+    float s, z;
+    if constexpr (CB == kC4R4) {
+      s = __uint_as_float(k < 8 ? ldg_nc_u16(blk + L::c_scale_off(k, slot)) << 16 : ldg_nc_u32(blk + L::pe_scale_off(slot)));
+      z = static_cast<float>(ldg_nc_u8(blk + L::zero_off(k, slot)));
+    } else {
+      const uint32_t sz = ldg_nc_u32(blk + L::sz_off(k, slot));
+      const __half2 h = *reinterpret_cast<const __half2*>(&sz);
+      s = __low2float(h);
+      z = __high2float(h);
+    }
+    if (CB == 2 && k < 8) {
+      const uint32_t w = ldg_nc_u16(codes + 2 * i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = s * (static_cast<float>((w >> (2 * e)) & 3u) - z);
+    } else {
+      const uint32_t w = ldg_nc_u32(codes + 4 * i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = s * (static_cast<float>((w >> (4 * e)) & 15u) - z);
+    }
+  }
+}
+
+// Block idx % img_width of sequence idx / img_width as an fp16 image (see Params::images), zero
+// behind the sequence's end, and for short sequences the image of C - RN_f16(C).
+template <int CB>
+__device__ void expand_block(const Params& p, int idx) {
+  griddep_wait();  // (the cache may still be written until here)
+  const int b = idx / p.img_width, j = idx - b * p.img_width;
+  const int len = p.seq_lens[b], n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
+  if (len > p.max_tokens || n < 0 || n > p.q_tokens || n > len || j * kBlockTokens >= len) return;
+  const int ctx = len - n;
+  constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
+  const int entry = p.table[static_cast<size_t>(b) * p.max_blocks + j];
+  const bool known = entry >= 0 && entry < p.num_blocks;
+  const uint8_t* const blk = p.pool + static_cast<size_t>(known ? entry : 0) * kBlk;
+  uint8_t* const img = p.images + static_cast<size_t>(idx) * kImage;
+  uint8_t* const rest = p.rest_images != nullptr && len <= kExactTokens
+                            ? p.rest_images + (static_cast<size_t>(b) * p.rest_width + j) * kImage
+                            : nullptr;
+  constexpr int kItems = kBlockTokens * kNumChunks * 8;
+#pragma unroll 1
+  for (int item = threadIdx.x; item < kItems; item += kPrepThreads) {
+    const int i = item & 7, slot = (item >> 3) & 63, k = item >> 9;
+    const int pos = j * kBlockTokens + slot;
+    float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (pos < len) {
+      const uint8_t* src = nullptr;
+      if (p.prot != nullptr) {
+        RowRef r;
+        r.has = true;
+        r.j = pos / kTileTokens;
+        r.len = len;
+        r.b = b;
+        src = prot_row_tree(p, r, pos % kTileTokens, ctx);
+      }
+      if (src != nullptr || known) {
+        row_values<CB>(src, blk, slot, k, i, f);
+      } else {
+        report(p.dev_err, QMLA_DEVERR_BAD_BLOCK);
+      }
+    }
+    uint32_t w[4], d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __half2 h = __floats2half2_rn(f[2 * e], f[2 * e + 1]);
+      w[e] = *reinterpret_cast<const uint32_t*>(&h);
+      d[e] = pack_h2(f[2 * e] - __low2float(h), f[2 * e + 1] - __high2float(h));
+    }
+    const size_t at = (slot >> 5) * kHalfImage + k * 4096 + swz_off(slot & 31, i, 128);
+    *reinterpret_cast<uint4*>(img + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (rest != nullptr) *reinterpret_cast<uint4*>(rest + at) = make_uint4(d[0], d[1], d[2], d[3]);
+  }
+}
+
 // Block 0: tile prefix over units (u = b * n_hg + hg), tiles = ceil(len / 128).
 // Blocks 1..: one query-image piece (16 bytes) per thread.
 // The cache writers let this kernel start beside them, so until it has waited for its
@@ -1032,15 +1123,21 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
     const long long images = static_cast<long long>(p.batch) * p.n_img;
     if constexpr (kTree) {
       const int first = static_cast<int>((images * kPieces + kPrepThreads - 1) / kPrepThreads) + 1;
-      if (static_cast<int>(blockIdx.x) >= first) {
-        make_trees(p, (static_cast<int>(blockIdx.x) - first) * kTreesPerBlock);
+      const int block = static_cast<int>(blockIdx.x) - first;
+      const int trees = (p.batch + kTreesPerBlock - 1) / kTreesPerBlock;
+      if (PAIR && block >= trees) {
+        expand_block<CB>(p, block - trees);
+        return;
+      }
+      if (block >= 0) {
+        make_trees(p, block * kTreesPerBlock);
         return;
       }
     }
     if (idx >= images * kPieces) return;
     const int u = static_cast<int>(idx / kPieces);
     const int b = u / p.n_img;
-    query_piece<CB, HG>(p, p.qimg + static_cast<size_t>(u) * Cfg<HG>::kQBytes, b, (u - b * p.n_img) * HG,
+    query_piece<kTree && PAIR ? 16 : CB, HG>(p, p.qimg + static_cast<size_t>(u) * Cfg<HG>::kQBytes, b, (u - b * p.n_img) * HG,
                         static_cast<int>(idx - static_cast<long long>(u) * kPieces));
     return;
   }
@@ -1059,11 +1156,10 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
     int tiles = 0;
     if (b < p.batch) {
       int len = p.seq_lens[b];
-      if (len < 0 || len > p.max_blocks * kBlockTokens) {
+      if (len < 0 || len > (kTree ? p.max_tokens : p.max_blocks * kBlockTokens)) {
         report(p.dev_err, QMLA_DEVERR_BAD_POSITION);
         len = 0;
-      }
-      if constexpr (kTree) {
+      } else if constexpr (kTree) {
         const int n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
         if (n < 0 || n > p.q_tokens || n > len) {
           report(p.dev_err, QMLA_DEVERR_BAD_TREE);
@@ -1412,12 +1508,13 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
   const long long units = static_cast<long long>(prm.batch) * prm.n_hg;
   const long long pieces = static_cast<long long>(prm.batch) * prm.n_img * kNumChunks * HG * 8;
   const unsigned prep_blocks = static_cast<unsigned>(1 + (pieces + kPrepThreads - 1) / kPrepThreads +
-                                                     (kTree ? (prm.batch + kTreesPerBlock - 1) / kTreesPerBlock : 0));
+                                                     (kTree ? (prm.batch + kTreesPerBlock - 1) / kTreesPerBlock : 0) +
+                                                     (kTree && PAIR ? prm.batch * prm.img_width : 0));
   if ((e = launch_k(prep_kernel<CB, HG, PAIR>, dim3(prep_blocks), dim3(kPrepThreads), 0, stream, pdl, prm)) != cudaSuccess)
     return e;
   if (ev0 != nullptr && (e = cudaEventRecord(ev0, stream)) != cudaSuccess) return e;
   if constexpr (PAIR) {
-    e = launch_decode_pair(prm, CB, pdl, stream);
+    e = kTree ? launch_tree_pair(prm, stream) : launch_decode_pair(prm, CB, pdl, stream);
   } else {
     e = launch_main<CB, HG, PROT>(prm, pdl, stream);
   }

@@ -54,6 +54,13 @@ struct Params {
   const int32_t* tree_lens;   // [batch] nodes of each sequence, or null: q_tokens each
   const uint8_t* draft_rows;  // [batch][64][576] bf16 rows of the nodes (with prot), or null
   TreeSeq* trees;             // [batch], written by the prep kernel
+  int max_tokens;             // longer sequences are bad
+  // Only where the context is laid out as fp16 tiles (tree_pair.cu): images [batch][img_width]
+  // of its 64-token blocks, and rest_images [batch][rest_width], of what their rounding left
+  // off, of sequences up to kExactTokens.
+  uint8_t* images;
+  uint8_t* rest_images;
+  int img_width, rest_width;
 };
 
 // One sequence's tree as the kernels use it. Nodes are bits; a node with a bad parent, or
@@ -65,6 +72,14 @@ struct TreeSeq {
   int ctx;                   // cached tokens before the tree
   int pad;
 };
+
+// A block as two halves of 32 tokens, each nine chunks of [32][128 bytes], swizzled as the
+// tensor core reads them.
+constexpr int kHalfImage = 9 * 32 * 128, kImage = 2 * kHalfImage;
+// Sequences up to this length get the more exact scores (see tree_pair.cu).
+constexpr int kExactTokens = 1024;
+// Main kernel over these images; prm's plan is over 128-row units.
+cudaError_t launch_tree_pair(const Params& prm, cudaStream_t stream);
 
 // Main kernel of the CTA-pair decode (decode_pair.cu) for a plan over 128-head
 // units; pdl: it may overlap its predecessor's end.
@@ -277,11 +292,10 @@ __device__ __forceinline__ const uint8_t* prot_row(const Params& p, const RowRef
 }
 // The same for a decode of a tree: P_L of the context alone, whose ring the drafts have not
 // touched; a node's row comes from the caller's rows of the nodes.
-__device__ __forceinline__ const uint8_t* prot_row_tree(const Params& p, const RowRef& r, int row) {
+__device__ __forceinline__ const uint8_t* prot_row_tree(const Params& p, const RowRef& r, int row, int ctx) {
   if (p.prot == nullptr || !r.has) return nullptr;
   const int pos = kTileTokens * r.j + row;
   if (pos >= r.len) return nullptr;
-  const int ctx = p.trees[r.b].ctx;
   int pr;
   if (pos >= ctx) return p.draft_rows + (static_cast<size_t>(r.b) * kMaxNodes + pos - ctx) * (kDqk * 2);
   if (pos < kSinkTokens) {

@@ -4,22 +4,31 @@
 //
 // The kernels are the decode's (decode.cu, compiled here for trees); prep also finds the
 // sets of nodes above and below each node.
+#include <algorithm>
+
 #define QMLA_DECODE_TREE 1
 #include "decode.cu"
 
 namespace qmla {
 namespace {
 
+constexpr size_t round_up(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
 struct TreeWorkspace {
   DecodeWorkspace decode;
-  size_t trees_off, total;
+  size_t trees_off, images_off;  // images: what is left
 };
 TreeWorkspace tree_workspace_layout(int batch, int rows, int grid) {
   TreeWorkspace w;
-  w.decode = decode_workspace_layout(batch, rows, grid);
-  w.trees_off = (w.decode.total + 255) & ~static_cast<size_t>(255);
-  w.total = w.trees_off + static_cast<size_t>(batch) * sizeof(TreeSeq);
+  // (units of 128 rows have images for an even number of 64-row groups)
+  w.decode = decode_workspace_layout(batch, rows <= 64 ? 128 : (rows + 127) / 128 * 128, grid);
+  w.trees_off = round_up(w.decode.total);
+  w.images_off = round_up(w.trees_off + static_cast<size_t>(batch) * sizeof(TreeSeq));
   return w;
+}
+int image_blocks(long long tokens) { return static_cast<int>((tokens + kBlockTokens - 1) / kBlockTokens); }
+size_t image_bytes(int batch, int blocks) {
+  return static_cast<size_t>(batch) * (blocks + std::min(blocks, kExactTokens / kBlockTokens)) * kImage;
 }
 
 template <int CB, bool PROT>
@@ -31,7 +40,9 @@ cudaError_t launch_rows(int hg, const Params& prm, cudaStream_t stream) {
 
 }  // namespace
 
-size_t tree_workspace_bytes(int batch, int rows, int grid) { return tree_workspace_layout(batch, rows, grid).total; }
+size_t tree_workspace_bytes(int batch, int rows, int max_tokens, int grid) {
+  return tree_workspace_layout(batch, rows, grid).images_off + image_bytes(batch, image_blocks(max_tokens));
+}
 
 cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t stream) {
   const int rows = d.nodes * d.heads, hg = head_group_size(rows);
@@ -68,6 +79,24 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
   prm.tree_lens = d.tree_lens;
   prm.draft_rows = reinterpret_cast<const uint8_t*>(d.draft_rows);
   prm.trees = reinterpret_cast<TreeSeq*>(ws + w.trees_off);
+  prm.max_tokens = d.max_blocks * kBlockTokens;
+  if (d.max_len > 0) prm.max_tokens = std::min(prm.max_tokens, d.max_len);
+  const int blocks = image_blocks(prm.max_tokens);
+  if (w.images_off + image_bytes(d.batch, blocks) <= d.workspace_bytes) {
+    prm.images = ws + w.images_off;
+    prm.img_width = blocks;
+    prm.rest_images = prm.images + static_cast<size_t>(d.batch) * blocks * kImage;
+    prm.rest_width = std::min(blocks, kExactTokens / kBlockTokens);
+    prm.n_hg = (rows + 127) / 128;
+    prm.n_img = 2 * prm.n_hg;
+    prm.grid = grid / 2;
+    switch (d.cache_kind) {
+      case 4: return launch_impl<4, 64, false, true>(prm, stream, nullptr, nullptr);
+      case 2: return launch_impl<2, 64, false, true>(prm, stream, nullptr, nullptr);
+      case kC4R4: return launch_impl<kC4R4, 64, false, true>(prm, stream, nullptr, nullptr);
+      default: return launch_impl<16, 64, false, true>(prm, stream, nullptr, nullptr);
+    }
+  }
   const bool prot = prm.prot != nullptr;
   switch (d.cache_kind) {
     case 4: return prot ? launch_rows<4, true>(hg, prm, stream) : launch_rows<4, false>(hg, prm, stream);

@@ -63,7 +63,7 @@ struct DecodeArgs {
 };
 cudaError_t launch_decode(const DecodeArgs& a, cudaStream_t stream);
 // The decode of a tree of nodes (decode_tree.cu), d checked.
-size_t tree_workspace_bytes(int batch, int rows, int grid);
+size_t tree_workspace_bytes(int batch, int rows, int max_tokens, int grid);
 cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t stream);
 // Verification of a tree of drafts, and its accepted rows (speculate.cu), d checked.
 cudaError_t launch_tree_verify(const qmla_verify_desc& d, int sms, cudaStream_t stream);

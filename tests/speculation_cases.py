@@ -28,10 +28,11 @@ def trees(shape: str, batch: int, nodes: int, seed: int = 0) -> torch.Tensor:
     return p.int().contiguous()
 
 
-def tile_values(x: torch.Tensor, kind) -> np.ndarray:
-    """What the attention's fp16 tiles hold of rows x [n, 576]: RN_f16(s (q - z)), or the bf16 values."""
+def tile_values(x: torch.Tensor, kind, exact: bool = False) -> np.ndarray:
+    """What the attention's fp16 tiles hold of rows x [n, 576]: RN_f16(s (q - z)), or the bf16 values;
+    exact: before that rounding."""
     if kind == "bf16":
-        return x.half().double().numpy()
+        return (x if exact else x.half()).double().numpy()
     out = []
     for a, b, content in ((0, 512, True), (512, 576, False)):
         g = x[:, a:b].float().reshape(x.size(0), (b - a) // 64, 64)
@@ -47,7 +48,8 @@ def tile_values(x: torch.Tensor, kind) -> np.ndarray:
             z = (-lo.double() / s.double()).round().clamp(0, m).float()
             q = (g.double() / s.double() + z).round().clamp(0, m).float()
         out.append((s * (q - z)).flatten(1))
-    return torch.cat(out, 1).half().double().numpy()
+    out = torch.cat(out, 1)
+    return (out if exact else out.half()).double().numpy()
 
 
 class Cache:
@@ -101,11 +103,11 @@ class Cache:
         else:
             Q.quant_append(self.pool, self.kind, lat, kpe, seq, pos, self.table_d, self.err)
 
-    def seen(self, b) -> np.ndarray:
-        """Rows of sequence b as attention sees them, in its tiles."""
-        x = tile_values(self.rows[b], self.kind)
+    def seen(self, b, exact=False) -> np.ndarray:
+        """Rows of sequence b as attention sees them, in its tiles or before their rounding."""
+        x = tile_values(self.rows[b], self.kind, exact)
         if self.protect:
-            c, own = self.ctx[b], self.rows[b].half().double().numpy()
+            c, own = self.ctx[b], (self.rows[b] if exact else self.rows[b].half()).double().numpy()
             for p in range(c):
                 if p < 4 or p >= c - 128:
                     x[p] = own[p]

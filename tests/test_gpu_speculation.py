@@ -56,7 +56,7 @@ def test_steps_leave_the_cache_of_the_accepted_tokens(kind, protect, heads):
         write(side, x, seq, pos, lens if protect else None)
     seq_lens, new_lens = i32(lens), i32([0] * B)
     path, kept, nxt = i32(np.zeros((B, T))), i32([0] * B), i32([0] * B)
-    ws = torch.empty(Q.tree_workspace_bytes(B, T, heads), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(Q.tree_workspace_bytes(B, T, heads, 64 * cols), dtype=torch.uint8, device="cuda")
     for step in range(steps):
         parents = trees("any", B, T, step)
         dep = depths(parents)

@@ -96,7 +96,7 @@ def test_rope_positions_off_their_boundary(L):
 
 
 def test_workspace_bytes_of_bad_arguments(L):
-    for args in ((0, 8, 16), (-1, 8, 16), (2, 0, 16), (2, 65, 16), (2, 8, 0), (2, 8, 129)):
+    for args in ((0, 8, 16, 0), (-1, 8, 16, 0), (2, 0, 16, 0), (2, 65, 16, 0), (2, 8, 0, 0), (2, 8, 129, 0), (2, 8, 16, -1)):
         assert L.qmla_tree_workspace_bytes(*args) == 0
 
 

@@ -603,7 +603,7 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *                   they would take the places of context that is protected once they are
  *                   refused. The layout is a BF16 cache's with one block a sequence, so that
  *                   qmla_rope_append_at writes these rows too.)
- *   out             [batch, nodes, heads, 512] bf16, 16-byte aligned
+ *   out             [batch, nodes, heads, 512] bf16, 32-byte aligned
  *   lse             [batch, nodes, heads] float32, or NULL
  *   workspace       >= qmla_tree_workspace_bytes(batch, nodes, heads, 0) bytes, 256-byte
  *                   aligned, scratch as for qmla_mla_decode. With the bytes for the call's

@@ -509,7 +509,7 @@ int qmla_mla_decode_tree(const qmla_tree_desc* d, qmla_stream_t stream) {
       d->block_table == nullptr || d->seq_lens == nullptr || d->out == nullptr || d->workspace == nullptr)
     return QMLA_ERR_INVALID_ARG;
   if (!aligned(d->pool, 32) || !aligned(d->q_latent, 16) || !aligned(d->q_pe, 16) || !aligned(d->parents, 4) ||
-      !aligned(d->tree_lens, 4) || !aligned(d->block_table, 4) || !aligned(d->seq_lens, 4) || !aligned(d->out, 16) ||
+      !aligned(d->tree_lens, 4) || !aligned(d->block_table, 4) || !aligned(d->seq_lens, 4) || !aligned(d->out, 32) ||
       !aligned(d->lse, 4) || !aligned(d->workspace, 256))
     return QMLA_ERR_INVALID_ARG;
   if (bad_node_rows(d->cache_kind, d->prot, d->draft_rows)) return QMLA_ERR_INVALID_ARG;

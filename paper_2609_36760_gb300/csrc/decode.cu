@@ -952,7 +952,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_main(const Params p) {
 }
 
 // ------------------------------------------------------------ prep / combine
-constexpr int kPrepThreads = 1024;
+constexpr int kPrepThreads = kTree ? 512 : 1024;
 constexpr int kTreesPerBlock = kPrepThreads / kMaxNodes;
 
 // Sets of nodes of kTreesPerBlock sequences from b0 on, a thread per node: each finds the
@@ -1014,94 +1014,151 @@ __device__ __forceinline__ void make_trees(const Params& p, int b0) {
   }
 }
 
-// Eight values of one cache row, channels 8 i .. 8 i + 7 of chunk k, as the attention sees them:
-// the row's own bf16 values where src is set, else the packed row in `slot` of blk.
+// One 16-byte piece of a cache row as it is loaded, and its eight values.
+struct RowPiece {
+  uint4 raw;    // bf16 values, or codes in x and scale and zero in y, z
+};
+// Piece i of chunk k of the packed row in `slot` of blk (the BF16 cache: of its values).
 template <int CB>
-__device__ __forceinline__ void row_values(const uint8_t* src, const uint8_t* blk, int slot, int k, int i, float (&f)[8]) {
-  if (CB == 16 || src != nullptr) {
-    const uint4 raw = ldg_nc_v4((src != nullptr ? src : blk + slot * (kDqk * 2)) + k * 128 + i * 16);
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      f[2 * e] = bf16_lo(w[e]);
-      f[2 * e + 1] = bf16_hi(w[e]);
-    }
-    return;
-  }
-  if constexpr (CB != 16) {
+__device__ __forceinline__ RowPiece load_piece(const uint8_t* blk, int slot, int k, int i) {
+  RowPiece r;
+  r.raw = make_uint4(0, 0, 0, 0);
+  if constexpr (CB == 16) {
+    r.raw = ldg_nc_v4(blk + slot * (kDqk * 2) + k * 128 + i * 16);
+  } else {
     using L = BlockLayout<CB>;
     const uint8_t* codes = blk + L::code_off(k, slot);
+    r.raw.x = CB == 2 && k < 8 ? ldg_nc_u16(codes + 2 * i) : ldg_nc_u32(codes + 4 * i);
+    if constexpr (CB == kC4R4) {
+      r.raw.y = k < 8 ? ldg_nc_u16(blk + L::c_scale_off(k, slot)) : ldg_nc_u32(blk + L::pe_scale_off(slot));
+      r.raw.z = ldg_nc_u8(blk + L::zero_off(k, slot));
+    } else {
+      r.raw.y = ldg_nc_u32(blk + L::sz_off(k, slot));
+    }
+  }
+  return r;
+}
+__device__ __forceinline__ void bf16_values(const uint4& raw, float (&f)[8]) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[2 * e] = bf16_lo(w[e]);
+    f[2 * e + 1] = bf16_hi(w[e]);
+  }
+}
+template <int CB>
+__device__ __forceinline__ void piece_values(const RowPiece& r, int k, float (&f)[8]) {
+  if constexpr (CB == 16) {
+    bf16_values(r.raw, f);
+  } else {
     float s, z;
     if constexpr (CB == kC4R4) {
-      s = __uint_as_float(k < 8 ? ldg_nc_u16(blk + L::c_scale_off(k, slot)) << 16 : ldg_nc_u32(blk + L::pe_scale_off(slot)));
-      z = static_cast<float>(ldg_nc_u8(blk + L::zero_off(k, slot)));
+      s = __uint_as_float(k < 8 ? r.raw.y << 16 : r.raw.y);
+      z = static_cast<float>(r.raw.z);
     } else {
-      const uint32_t sz = ldg_nc_u32(blk + L::sz_off(k, slot));
-      const __half2 h = *reinterpret_cast<const __half2*>(&sz);
+      const __half2 h = *reinterpret_cast<const __half2*>(&r.raw.y);
       s = __low2float(h);
       z = __high2float(h);
     }
-    if (CB == 2 && k < 8) {
-      const uint32_t w = ldg_nc_u16(codes + 2 * i);
+    constexpr uint32_t kNarrow = 2, kWide = 4;
+    const uint32_t bits = CB == 2 && k < 8 ? kNarrow : kWide;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = s * (static_cast<float>((w >> (2 * e)) & 3u) - z);
-    } else {
-      const uint32_t w = ldg_nc_u32(codes + 4 * i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = s * (static_cast<float>((w >> (4 * e)) & 15u) - z);
-    }
+    for (int e = 0; e < 8; ++e)
+      f[e] = s * (static_cast<float>((r.raw.x >> (bits * e)) & ((1u << bits) - 1u)) - z);
   }
+}
+__device__ __forceinline__ uint4 half_piece(const float (&f)[8]) {
+  return make_uint4(pack_h2(f[0], f[1]), pack_h2(f[2], f[3]), pack_h2(f[4], f[5]), pack_h2(f[6], f[7]));
+}
+// What rounding to fp16 leaves off.
+__device__ __forceinline__ uint4 rest_piece(const float (&f)[8]) {
+  float d[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) d[e] = f[e] - __half2float(__float2half_rn(f[e]));
+  return half_piece(d);
 }
 
 // Block idx % img_width of sequence idx / img_width as an fp16 image (see Params::images), zero
-// behind the sequence's end, and for short sequences the image of C - RN_f16(C).
+// behind the sequence's end, and for short sequences the image of C - RN_f16(C). A thread has
+// the same eight channels of one row's nine chunks, all loaded before any is stored.
 template <int CB>
 __device__ void expand_block(const Params& p, int idx) {
+  static_assert(!kTree || kPrepThreads == kBlockTokens * 8, "a thread per row and piece");
   griddep_wait();  // (the cache may still be written until here)
   const int b = idx / p.img_width, j = idx - b * p.img_width;
+  const int entry = p.table[static_cast<size_t>(b) * p.max_blocks + j];
   const int len = p.seq_lens[b], n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
   if (len > p.max_tokens || n < 0 || n > p.q_tokens || n > len || j * kBlockTokens >= len) return;
   const int ctx = len - n;
   constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
-  const int entry = p.table[static_cast<size_t>(b) * p.max_blocks + j];
   const bool known = entry >= 0 && entry < p.num_blocks;
   const uint8_t* const blk = p.pool + static_cast<size_t>(known ? entry : 0) * kBlk;
-  uint8_t* const img = p.images + static_cast<size_t>(idx) * kImage;
+  const int i = threadIdx.x & 7, slot = threadIdx.x >> 3, pos = j * kBlockTokens + slot;
+  const size_t at = (slot >> 5) * kHalfImage + swz_off(slot & 31, i, 128);
+  uint8_t* const img = p.images + static_cast<size_t>(idx) * kImage + at;
   uint8_t* const rest = p.rest_images != nullptr && len <= kExactTokens
-                            ? p.rest_images + (static_cast<size_t>(b) * p.rest_width + j) * kImage
+                            ? p.rest_images + (static_cast<size_t>(b) * p.rest_width + j) * kImage + at
                             : nullptr;
-  constexpr int kItems = kBlockTokens * kNumChunks * 8;
-#pragma unroll 1
-  for (int item = threadIdx.x; item < kItems; item += kPrepThreads) {
-    const int i = item & 7, slot = (item >> 3) & 63, k = item >> 9;
-    const int pos = j * kBlockTokens + slot;
-    float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (pos < len) {
-      const uint8_t* src = nullptr;
-      if (p.prot != nullptr) {
-        RowRef r;
-        r.has = true;
-        r.j = pos / kTileTokens;
-        r.len = len;
-        r.b = b;
-        src = prot_row_tree(p, r, pos % kTileTokens, ctx);
-      }
-      if (src != nullptr || known) {
-        row_values<CB>(src, blk, slot, k, i, f);
-      } else {
-        report(p.dev_err, QMLA_DEVERR_BAD_BLOCK);
-      }
-    }
-    uint32_t w[4], d[4];
+  const uint8_t* src = nullptr;
+  if (CB != 16 && p.prot != nullptr) {
+    RowRef r;
+    r.has = true;
+    r.j = pos / kTileTokens;
+    r.len = len;
+    r.b = b;
+    src = prot_row_tree(p, r, pos % kTileTokens, ctx);
+  }
+  float f[8];
+  if (CB != 16 && src != nullptr) {
+    uint4 raw[kNumChunks];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const __half2 h = __floats2half2_rn(f[2 * e], f[2 * e + 1]);
-      w[e] = *reinterpret_cast<const uint32_t*>(&h);
-      d[e] = pack_h2(f[2 * e] - __low2float(h), f[2 * e + 1] - __high2float(h));
+    for (int k = 0; k < kNumChunks; ++k) raw[k] = ldg_nc_v4(src + k * 128 + i * 16);
+#pragma unroll
+    for (int k = 0; k < kNumChunks; ++k) {
+      bf16_values(raw[k], f);
+      *reinterpret_cast<uint4*>(img + k * 4096) = half_piece(f);
+      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * 4096) = rest_piece(f);
     }
-    const size_t at = (slot >> 5) * kHalfImage + k * 4096 + swz_off(slot & 31, i, 128);
-    *reinterpret_cast<uint4*>(img + at) = make_uint4(w[0], w[1], w[2], w[3]);
-    if (rest != nullptr) *reinterpret_cast<uint4*>(rest + at) = make_uint4(d[0], d[1], d[2], d[3]);
+  } else if (known && pos < len) {
+    RowPiece r[kNumChunks];
+#pragma unroll
+    for (int k = 0; k < kNumChunks; ++k) r[k] = load_piece<CB>(blk, slot, k, i);
+#pragma unroll
+    for (int k = 0; k < kNumChunks; ++k) {
+      piece_values<CB>(r[k], k, f);
+      *reinterpret_cast<uint4*>(img + k * 4096) = half_piece(f);
+      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * 4096) = rest_piece(f);
+    }
+  } else {
+    if (pos < len) report(p.dev_err, QMLA_DEVERR_BAD_BLOCK);
+#pragma unroll 1
+    for (int k = 0; k < kNumChunks; ++k) {
+      *reinterpret_cast<uint4*>(img + k * 4096) = make_uint4(0, 0, 0, 0);
+      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * 4096) = make_uint4(0, 0, 0, 0);
+    }
+  }
+}
+
+// The image of 64 query rows (see query_piece), in channel order; a thread's work as above.
+__device__ __forceinline__ void query_image(const Params& p, int u) {
+  const int b = u / p.n_img, i = threadIdx.x & 7, h = threadIdx.x >> 3;
+  const int row = (u - b * p.n_img) * 64 + h;
+  uint4 raw[kNumChunks];
+#pragma unroll
+  for (int k = 0; k < kNumChunks; ++k) raw[k] = make_uint4(0, 0, 0, 0);
+  if (row < p.heads) {
+    const size_t r = static_cast<size_t>(b) * p.heads + row;
+#pragma unroll
+    for (int k = 0; k < kNumChunks; ++k)
+      raw[k] = ldg_nc_v4(k < 8 ? p.q_lat + r * kDc + k * 64 + i * 8 : p.q_pe + r * kDr + i * 8);
+  }
+  griddep_wait();  // (see prep_kernel)
+  uint8_t* const img = p.qimg + static_cast<size_t>(u) * (kNumChunks * 64 * 128) + swz_off(h, i, 128);
+  float f[8];
+#pragma unroll
+  for (int k = 0; k < kNumChunks; ++k) {
+    bf16_values(raw[k], f);
+    *reinterpret_cast<uint4*>(img + k * 64 * 128) = half_piece(f);
   }
 }
 
@@ -1122,7 +1179,8 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
     constexpr int kPieces = kNumChunks * HG * 8;
     const long long images = static_cast<long long>(p.batch) * p.n_img;
     if constexpr (kTree) {
-      const int first = static_cast<int>((images * kPieces + kPrepThreads - 1) / kPrepThreads) + 1;
+      const int first = PAIR ? static_cast<int>(images) + 1
+                             : static_cast<int>((images * kPieces + kPrepThreads - 1) / kPrepThreads) + 1;
       const int block = static_cast<int>(blockIdx.x) - first;
       const int trees = (p.batch + kTreesPerBlock - 1) / kTreesPerBlock;
       if (PAIR && block >= trees) {
@@ -1133,11 +1191,15 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
         make_trees(p, block * kTreesPerBlock);
         return;
       }
+      if constexpr (PAIR) {
+        query_image(p, static_cast<int>(blockIdx.x) - 1);
+        return;
+      }
     }
     if (idx >= images * kPieces) return;
     const int u = static_cast<int>(idx / kPieces);
     const int b = u / p.n_img;
-    query_piece<kTree && PAIR ? 16 : CB, HG>(p, p.qimg + static_cast<size_t>(u) * Cfg<HG>::kQBytes, b, (u - b * p.n_img) * HG,
+    query_piece<CB, HG>(p, p.qimg + static_cast<size_t>(u) * Cfg<HG>::kQBytes, b, (u - b * p.n_img) * HG,
                         static_cast<int>(idx - static_cast<long long>(u) * kPieces));
     return;
   }
@@ -1507,7 +1569,9 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
   const bool pdl = ev0 == nullptr && ev1 == nullptr;
   const long long units = static_cast<long long>(prm.batch) * prm.n_hg;
   const long long pieces = static_cast<long long>(prm.batch) * prm.n_img * kNumChunks * HG * 8;
-  const unsigned prep_blocks = static_cast<unsigned>(1 + (pieces + kPrepThreads - 1) / kPrepThreads +
+  const long long query_blocks = kTree && PAIR ? static_cast<long long>(prm.batch) * prm.n_img
+                                               : (pieces + kPrepThreads - 1) / kPrepThreads;
+  const unsigned prep_blocks = static_cast<unsigned>(1 + query_blocks +
                                                      (kTree ? (prm.batch + kTreesPerBlock - 1) / kTreesPerBlock : 0) +
                                                      (kTree && PAIR ? prm.batch * prm.img_width : 0));
   if ((e = launch_k(prep_kernel<CB, HG, PAIR>, dim3(prep_blocks), dim3(kPrepThreads), 0, stream, pdl, prm)) != cudaSuccess)

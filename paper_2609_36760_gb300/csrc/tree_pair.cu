@@ -35,6 +35,9 @@ constexpr uint32_t kRows = 64;                        // query rows per CTA
 constexpr uint32_t kQBytes = kNumChunks * kRows * 128;
 constexpr uint32_t kKBytes = kHalfImage;              // own 32 tokens, K-major B of QK
 constexpr uint32_t kKChunk = 32 * 128;
+// Each K stage is filled, used and freed in two parts of five and four chunks, each V stage in
+// two of 128 channels, so that a copy has most of two tiles' time to arrive.
+constexpr uint32_t kKSplit = 5;
 constexpr uint32_t kVChunk = kTok * 128, kVBytes = 4 * kVChunk;  // own channels, MN-major B of PV
 constexpr uint32_t kPTile = kRows * 128;              // P, K-major A of PV
 constexpr uint32_t kKOff = kQBytes, kVOff = kKOff + 2 * kKBytes, kPOff = kVOff + 2 * kVBytes;
@@ -42,15 +45,14 @@ constexpr uint32_t kCtrlOff = kPOff + 2 * kPTile;
 constexpr uint32_t kColS = 256, kTmemCols = 512;
 
 struct __align__(16) TreeCtrl {
-  // Completed by this CTA's own copies (transaction counts).
-  uint64_t k_bar[2], v_bar[2], q_bar;
-  // The leader's: the other CTA's copies have landed; P written, S read (4 warps per CTA), O read.
-  uint64_t k_peer[2], v_peer[2], q_peer;
-  uint64_t p_full[2], s_free[4], o_free;
-  // Arrived on by MMA commits, multicast to both CTAs: scores complete, K stage free, PV complete
-  // (V stage and P free), every QK of a segment done.
-  uint64_t s_full[4], k_free[2], pv_done[2], q_free;
-  uint64_t halves[2];  // the two warps that share rows, [warp & 1]
+  // Operands are there, [stage][part]: this CTA's own copies (transaction counts), in the leader
+  // also an arrival for the other CTA's.
+  uint64_t k_bar[2][2], v_bar[2][2], q_bar;
+  // The leader's: P written (4 warps per CTA), O read.
+  uint64_t p_full[2], o_free;
+  // Arrived on by MMA commits, multicast to both CTAs: scores complete, part of a K stage free,
+  // part of a V stage free (the second: PV complete, P free), every QK of a segment done.
+  uint64_t s_full[4], k_free[2][2], v_free[2][2], q_free;
   uint64_t fin;
   uint32_t tmem_base, abort;
   float xch[2][128];
@@ -108,7 +110,7 @@ struct TreeSched {
 // The order in which the issuer takes QK and PV, and the copies come: QK of a tile goes before PV
 // of the tile before it, unless it starts a segment, whose query waits for the last QK of the
 // segment before. (QK of tile i so goes after PV of tile i - 2: who has its scores knows that
-// its P tile is free.)
+// its P tile is free, and the scores of tile i - 4, whose place it takes, have been read.)
 struct TreeOrder {
   TreeSched k, v;  // at tiles nk and nv
   uint32_t nk = 0, nv = 0;
@@ -120,12 +122,22 @@ __device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, TreeCtrl& 
   return wait_ok(mbar_wait(bar, parity, kWaitNs, &c.abort), site, c, dev_err);
 }
 // The same for a barrier of the leader that the other CTA arrives on: acquired from the cluster.
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ bool pwait_cluster(uint64_t* bar, uint32_t parity, TreeCtrl& c, uint32_t site,
                                               uint32_t* dev_err) {
   if (mbar_test_cluster(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
-    if (mbar_test_cluster(bar, parity)) return true;
+    if (try_wait_cluster(bar, parity)) return true;
     if (*reinterpret_cast<volatile uint32_t*>(&c.abort) != 0u) return false;
     if (globaltimer_ns() - t0 > kWaitNs) return wait_ok(0, site, c, dev_err);
   }
@@ -135,7 +147,7 @@ __device__ __forceinline__ bool pwait_cluster(uint64_t* bar, uint32_t parity, Tr
 __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, TreeCtrl& ctl, int rank) {
   TreeOrder o;
   o.k = o.v = sc;
-  uint32_t kk = 0, seg = 0;
+  uint32_t kk = 0, seg = 0, copies = 0, values = 0;
   bool ok = true;
   while (ok && o.live()) {
     if (o.score_next()) {
@@ -143,11 +155,17 @@ __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, Tre
       const int parts = o.k.parts(p);
       for (int part = 0; ok && part < parts; ++part, ++kk) {
         const uint32_t st = kk & 1u;
-        if (kk >= 2 && !(ok = pwait(&ctl.k_free[st], ((kk >> 1) - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
-        mbar_arrive_expect_tx(&ctl.k_bar[st], kKBytes);
         const uint8_t* src = part == 0 ? p.images + img * kImage
                                        : p.rest_images + (static_cast<size_t>(o.k.b) * p.rest_width + o.k.q) * kImage;
-        bulk_g2s(sm + kKOff + st * kKBytes, src + rank * kHalfImage, kKBytes, &ctl.k_bar[st]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          constexpr uint32_t kBytes[2] = {kKSplit * kKChunk, kKBytes - kKSplit * kKChunk};
+          if (kk >= 2 && !(ok = pwait(&ctl.k_free[st][i], ((kk >> 1) - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
+          mbar_arrive_expect_tx(&ctl.k_bar[st][i], kBytes[i]);
+          bulk_g2s(sm + kKOff + st * kKBytes + i * kBytes[0], src + rank * kHalfImage + i * kBytes[0], kBytes[i],
+                   &ctl.k_bar[st][i]);
+          ++copies;
+        }
       }
       if (ok && o.k.first()) {
         if (seg > 0 && !(ok = pwait(&ctl.q_free, (seg - 1) & 1u, ctl, kSiteMmaQFull, p.dev_err))) break;
@@ -159,54 +177,64 @@ __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, Tre
       o.k.next(p);
     } else {
       const uint32_t st = o.nv & 1u;
-      if (o.nv >= 2 && !(ok = pwait(&ctl.pv_done[st], ((o.nv >> 1) - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
-      mbar_arrive_expect_tx(&ctl.v_bar[st], kVBytes);
       const uint8_t* src = p.images + (static_cast<size_t>(o.v.b) * p.img_width + o.v.q) * kImage + 4 * rank * kKChunk;
 #pragma unroll 1
-      for (int i = 0; i < 8; ++i)  // chunk i / 2, tokens 32 (i & 1) ..
-        bulk_g2s(sm + kVOff + st * kVBytes + (i >> 1) * kVChunk + (i & 1) * kKChunk,
-                 src + (i & 1) * kHalfImage + (i >> 1) * kKChunk, kKChunk, &ctl.v_bar[st]);
+      for (int blk = 0; ok && blk < 2; ++blk) {
+        if (o.nv >= 2 && !(ok = pwait(&ctl.v_free[st][blk], ((o.nv >> 1) - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
+        mbar_arrive_expect_tx(&ctl.v_bar[st][blk], kVBytes / 2);
+#pragma unroll 1
+        for (int i = 4 * blk; i < 4 * blk + 4; ++i)  // chunk i / 2, tokens 32 (i & 1) ..
+          bulk_g2s(sm + kVOff + st * kVBytes + (i >> 1) * kVChunk + (i & 1) * kKChunk,
+                   src + (i & 1) * kHalfImage + (i >> 1) * kKChunk, kKChunk, &ctl.v_bar[st][blk]);
+        ++values;
+      }
       ++o.nv;
       o.v.next(p);
     }
   }
   if (!ok) set_abort(ctl, p.dev_err);
   // No copy and no commit may reach this CTA once it has left; these waits ignore the abort flag.
-  for (uint32_t st = 0; st < 2; ++st) {
-    const uint32_t nk = (kk + 1 - st) >> 1, nv = (o.nv + 1 - st) >> 1;  // phases begun on stage st
-    if (nk > 0) mbar_wait(&ctl.k_bar[st], (nk - 1) & 1u, kWaitNs, nullptr);
-    if (nv > 0) mbar_wait(&ctl.v_bar[st], (nv - 1) & 1u, kWaitNs, nullptr);
-    if (ok && nk > 0) mbar_wait(&ctl.k_free[st], (nk - 1) & 1u, kWaitNs, nullptr);
+  for (uint32_t i = 0; i < 4; ++i) {
+    const uint32_t nk = (copies + 3 - i) >> 2, nv = (values + 3 - i) >> 2;  // phases begun of part i & 1 of stage i / 2
+    if (nk > 0) mbar_wait(&ctl.k_bar[i >> 1][i & 1], (nk - 1) & 1u, kWaitNs, nullptr);
+    if (nv > 0) mbar_wait(&ctl.v_bar[i >> 1][i & 1], (nv - 1) & 1u, kWaitNs, nullptr);
+    if (ok && nk > 0) mbar_wait(&ctl.k_free[i >> 1][i & 1], (nk - 1) & 1u, kWaitNs, nullptr);
+    if (ok && nv > 0) mbar_wait(&ctl.v_free[i >> 1][i & 1], (nv - 1) & 1u, kWaitNs, nullptr);
   }
   if (seg > 0) mbar_wait(&ctl.q_bar, (seg - 1) & 1u, kWaitNs, nullptr);
   if (ok && seg > 0) mbar_wait(&ctl.q_free, (seg - 1) & 1u, kWaitNs, nullptr);
 }
 
 // The other CTA: tells the leader of each of its copies, in the order in which the issuer asks.
+// (The tensor core of this SM reads what they brought, and this thread has written nothing, so
+// the arrivals release nothing to the cluster: with that release each took more than a
+// thousand cycles, and a tile 4,700 instead of 1,830.)
 __device__ void relay_role(const Params& p, const TreeSched& sc, TreeCtrl& ctl) {
   TreeOrder o;
   o.k = o.v = sc;
   uint32_t kk = 0, seg = 0;
   bool ok = true;
-  const uint32_t kpeer = cluster_map(smem_u32(&ctl.k_peer[0]), 0), vpeer = cluster_map(smem_u32(&ctl.v_peer[0]), 0);
-  const uint32_t qpeer = cluster_map(smem_u32(&ctl.q_peer), 0);
+  const uint32_t kbar = cluster_map(smem_u32(&ctl.k_bar[0][0]), 0), vbar = cluster_map(smem_u32(&ctl.v_bar[0][0]), 0);
+  const uint32_t qbar = cluster_map(smem_u32(&ctl.q_bar), 0);
   while (ok && o.live()) {
     if (o.score_next()) {
       if (o.k.first()) {
         if (!(ok = pwait(&ctl.q_bar, seg & 1u, ctl, kSiteMmaQFull, p.dev_err))) break;
-        mbar_arrive_cluster(qpeer, true);
+        mbar_arrive_remote(qbar, true);
         ++seg;
       }
       const int parts = o.k.parts(p);
-      for (int part = 0; part < parts; ++part, ++kk) {
-        if (!(ok = pwait(&ctl.k_bar[kk & 1u], (kk >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
-        mbar_arrive_cluster(kpeer + (kk & 1u) * 8, true);
+      for (int part = 0; ok && part < 2 * parts; ++part, ++kk) {
+        if (!(ok = pwait(&ctl.k_bar[(kk >> 1) & 1u][kk & 1u], (kk >> 2) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+        mbar_arrive_remote(kbar + (kk & 3u) * 8, true);
       }
       ++o.nk;
       o.k.next(p);
     } else {
-      if (!(ok = pwait(&ctl.v_bar[o.nv & 1u], (o.nv >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
-      mbar_arrive_cluster(vpeer + (o.nv & 1u) * 8, true);
+      for (int blk = 0; blk < 2; ++blk) {
+        if (!(ok = pwait(&ctl.v_bar[o.nv & 1u][blk], (o.nv >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+        mbar_arrive_remote(vbar + ((o.nv & 1u) * 2 + blk) * 8, true);
+      }
       ++o.nv;
       o.v.next(p);
     }
@@ -229,29 +257,27 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
     if (o.score_next()) {
       const uint32_t n = o.nk;
       if (o.k.first()) {
-        if (!(ok = pwait(&ctl.q_bar, qseg & 1u, ctl, kSiteMmaQFull, p.dev_err) &&
-                   pwait_cluster(&ctl.q_peer, qseg & 1u, ctl, kSiteMmaQFull, p.dev_err)))
-          break;
+        if (!(ok = pwait_cluster(&ctl.q_bar, qseg & 1u, ctl, kSiteMmaQFull, p.dev_err))) break;
         ++qseg;
       }
-      if (n >= 4 && !(ok = pwait_cluster(&ctl.s_free[n & 3u], ((n >> 2) - 1) & 1u, ctl, kSiteSmSFull, p.dev_err))) break;
       const uint32_t ts = tmem + kColS + (n & 3u) * 32;
       const int parts = o.k.parts(p);
-      for (int part = 0; part < parts; ++part, ++kk) {
+      for (int part = 0; ok && part < parts; ++part, ++kk) {
         const uint32_t st = kk & 1u;
-        if (!(ok = pwait(&ctl.k_bar[st], (kk >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err) &&
-                   pwait_cluster(&ctl.k_peer[st], (kk >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err)))
-          break;
-        tc_fence_after();
         const uint64_t b1 = kb + ((st * kKBytes) >> 4);
 #pragma unroll
-        for (int k = 0; k < kNumChunks; ++k) {
+        for (int i = 0; i < 2; ++i) {
+          if (!(ok = pwait_cluster(&ctl.k_bar[st][i], (kk >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+          tc_fence_after();
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
-            umma2_f16_ss(ts, qa + ((k * kRows * 128 + s * 32) >> 4), b1 + ((k * kKChunk + s * 32) >> 4), kIdQK,
-                         k == 0 && s == 0 && part == 0 ? 0u : 1u);
+          for (int k = i * kKSplit; k < (i == 0 ? static_cast<int>(kKSplit) : kNumChunks); ++k) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+              umma2_f16_ss(ts, qa + ((k * kRows * 128 + s * 32) >> 4), b1 + ((k * kKChunk + s * 32) >> 4), kIdQK,
+                           k == 0 && s == 0 && part == 0 ? 0u : 1u);
+          }
+          umma2_commit(&ctl.k_free[st][i]);
         }
-        umma2_commit(&ctl.k_free[st]);
       }
       if (!ok) break;
       umma2_commit(&ctl.s_full[n & 3u]);
@@ -261,21 +287,21 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
     } else {
       const uint32_t st = o.nv & 1u, ph = (o.nv >> 1) & 1u;
       const bool first = o.v.first();
-      if (!(ok = pwait(&ctl.v_bar[st], ph, ctl, kSiteMmaChunk, p.dev_err) &&
-                 pwait_cluster(&ctl.v_peer[st], ph, ctl, kSiteMmaChunk, p.dev_err) &&
-                 pwait_cluster(&ctl.p_full[st], ph, ctl, kSiteMmaPFull, p.dev_err) &&
+      if (!(ok = pwait_cluster(&ctl.p_full[st], ph, ctl, kSiteMmaPFull, p.dev_err) &&
                  (!first || pseg == 0 || pwait_cluster(&ctl.o_free, (pseg - 1) & 1u, ctl, kSiteMmaOFree, p.dev_err))))
         break;
-      tc_fence_after();
       const uint64_t a1 = pa + ((st * kPTile) >> 4), b1 = vb + ((st * kVBytes) >> 4);
 #pragma unroll
       for (int blk = 0; blk < 2; ++blk) {
+        if (!(ok = pwait_cluster(&ctl.v_bar[st][blk], ph, ctl, kSiteMmaChunk, p.dev_err))) break;
+        tc_fence_after();
 #pragma unroll
         for (int s = 0; s < 4; ++s)
           umma2_f16_ss(tmem + blk * 128, a1 + ((s * 32) >> 4), b1 + ((blk * 2 * kVChunk + s * 2048) >> 4), kIdPV,
                        first && s == 0 ? 0u : 1u);
+        umma2_commit(&ctl.v_free[st][blk]);
       }
-      umma2_commit(&ctl.pv_done[st]);
+      if (!ok) break;
       if (o.v.last()) ++pseg;
       ++o.nv;
       o.v.next(p);
@@ -289,6 +315,11 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
 }
 
 // ------------------------------------------------------------------- softmax
+__device__ __forceinline__ void stg_v8(void* ptr, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(ptr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
 __device__ __forceinline__ void arrive_leader(int lane, uint32_t bar_addr) { mbar_arrive_remote(bar_addr, lane == 0); }
 
 // Thread (row, half): query row `row` of the CTA and half the tokens of a tile; in O, half the
@@ -300,23 +331,22 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
   const uint32_t t_o = tmem + lanes;
   const float sl2 = p.scale_log2;
-  const uint32_t sfree = cluster_map(smem_u32(&ctl.s_free[0]), 0), pfull = cluster_map(smem_u32(&ctl.p_full[0]), 0);
+  const uint32_t pfull = cluster_map(smem_u32(&ctl.p_full[0]), 0);
   const uint32_t ofree = cluster_map(smem_u32(&ctl.o_free), 0);
-  uint64_t* const both = &ctl.halves[warp & 1];
   uint32_t n = 0, ex = 0;
-  bool ok = true, whole = false;
+  bool ok = true, whole = false, all_alive = false;
   float m = -INFINITY, l = 0.0f;
   int ctx = 0;            // positions before the tree that this row sees (all or none)
   uint64_t line = 0ull;   // nodes that it sees
 
-  // The other half's value of a per-row quantity.
-  auto exchange = [&](float mine, float& other) {
-    const uint32_t buf = ex & 1u;
-    ctl.xch[buf][half * 64 + row] = mine;
-    __syncwarp();
-    mbar_arrive_if(lane == 0 ? 1u : 0u, both);
-    ok = wwait(both, buf, ctl, kSiteGrp, p.dev_err);
-    other = ctl.xch[buf][(1 - half) * 64 + row];
+  // A per-row quantity for the thread of the other half, and that one's. (The two warps that
+  // share rows meet at a barrier of theirs; one that gives up arrives there too, after it has
+  // set the abort word, which is therefore read behind the barrier.)
+  auto give = [&](float mine) { ctl.xch[ex & 1u][half * 64 + row] = mine; };
+  auto take = [&](float& other) {
+    asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 1)) : "memory");
+    other = ctl.xch[ex & 1u][(1 - half) * 64 + row];
+    ok = *reinterpret_cast<volatile uint32_t*>(&ctl.abort) == 0u;
     ++ex;
     return ok;
   };
@@ -332,39 +362,63 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
       m = -INFINITY;
       l = 0.0f;
       whole = sc.q == 0;
+      all_alive = __all_sync(0xffffffffu, line != 0ull);
     }
-    // which of the 32 columns the row sees
-    const int pos = kTok * sc.q + 32 * half, d = pos - ctx;
-    uint32_t mask = 0u;
-    if (line != 0ull) {
-      mask = d <= -32 ? ~0u : (d < 0 ? (1u << -d) - 1u : 0u);
-      if (d >= 0 && d < 64) mask |= static_cast<uint32_t>(line >> d);
-      if (d < 0 && d > -32) mask |= static_cast<uint32_t>(line << -d);
-    }
-    const bool full = __all_sync(0xffffffffu, mask == ~0u);
+    const int d = kTok * sc.q + 32 * half - ctx;  // node in the first of the 32 columns
+    const bool full = all_alive && d <= -32;
     if (!(ok = wwait(&ctl.s_full[n & 3u], (n >> 2) & 1u, ctl, kSiteSmSFull, p.dev_err))) break;
     tc_fence_after();
     float x[32], top;
     tmem_ld32_max(tmem + kColS + (n & 3u) * 32 + lanes, x, top);
     tmem_ld_wait();
-    tc_fence_before();
-    __syncwarp();
-    arrive_leader(lane, sfree + (n & 3u) * 8);
-    if (!full) {
+    if (!full) {  // the columns that the row sees: the context's, and the nodes of its line
+      uint32_t mask = 0u;
+      if (line != 0ull) {
+        mask = d <= -32 ? ~0u : (d < 0 ? (1u << -d) - 1u : 0u);
+        if (d >= 0 && d < 64) mask |= static_cast<uint32_t>(line >> d);
+        if (d < 0 && d > -32) mask |= static_cast<uint32_t>(line << -d);
+      }
       top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) top = fmaxf(top, (mask >> i) & 1u ? x[i] : -INFINITY);
+      for (int i = 0; i < 32; ++i) {
+        x[i] = (mask >> i) & 1u ? x[i] : -INFINITY;
+        top = fmaxf(top, x[i]);
+      }
     }
+    const uint32_t st = n & 1u;
+    const uint32_t ptile = smem + kPOff + st * kPTile;
+    float sum = 0.0f;
+    // (a row that has seen no key has no reference: its columns are all masked)
+    auto weights = [&]() {
+      const float ref = m == -INFINITY ? 0.0f : m;
+      float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[e] = ex2_approx(__fmaf_rn(x[i + e], sl2, -ref));
+          s[e & 3] += w[e];
+        }
+        sts_v4(ptile + swz_off(row, half * 4 + i / 8, 128), pack_h2(w[0], w[1]), pack_h2(w[2], w[3]),
+               pack_h2(w[4], w[5]), pack_h2(w[6], w[7]));
+      }
+      sum = (s[0] + s[1]) + (s[2] + s[3]);
+    };
+    // The weights go by the reference as it is while the other half's largest score is on its
+    // way, and once more in the rare tile that raises it.
     float mine = top * sl2, other = 0.0f;
-    if (!exchange(mine, other)) break;
+    give(mine);
+    if (!first) weights();
+    if (!take(other)) break;
     mine = fmaxf(mine, other);
     const bool raise = first ? mine > m : mine > m + kRescaleLog2;
-    if (__any_sync(0xffffffffu, raise)) {
+    if (first || __any_sync(0xffffffffu, raise)) {
       const float a = raise && m != -INFINITY ? exp2f(m - mine) : 1.0f;
       if (raise) m = mine;
       l *= a;
       if (!first && __any_sync(0xffffffffu, a != 1.0f)) {
-        if (!(ok = wwait(&ctl.pv_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, ctl, kSitePvEpi, p.dev_err))) break;
+        if (!(ok = wwait(&ctl.v_free[(n - 1) & 1u][1], ((n - 1) >> 1) & 1u, ctl, kSitePvEpi, p.dev_err))) break;
         tc_fence_after();
 #pragma unroll 1
         for (int c = 0; c < 256; c += 32) {
@@ -377,108 +431,70 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
         }
         tmem_st_wait();
       }
-    }
-    // (a row that has seen no key has no reference: its columns are all masked)
-    const float ref = m == -INFINITY ? 0.0f : m;
-    const uint32_t st = n & 1u;
-    const uint32_t ptile = smem + kPOff + st * kPTile;
-    float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; i += 8) {
-      float w[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float y = __fmaf_rn(x[i + e], sl2, -ref);
-        w[e] = ex2_approx(full || ((mask >> (i + e)) & 1u) ? y : -INFINITY);
-      }
-      s0 += w[0] + w[4];
-      s1 += w[1] + w[5];
-      s2 += w[2] + w[6];
-      s3 += w[3] + w[7];
-      sts_v4(ptile + swz_off(row, half * 4 + i / 8, 128), pack_h2(w[0], w[1]), pack_h2(w[2], w[3]), pack_h2(w[4], w[5]),
-             pack_h2(w[6], w[7]));
+      weights();
     }
     fence_proxy_async_smem();
     tc_fence_before();
     __syncwarp();
     arrive_leader(lane, pfull + st * 8);
-    l += (s0 + s1) + (s2 + s3);
+    l += sum;
     ++n;
     if (!sc.last()) continue;
 
     // ---- segment end: out = O / l in bf16, or the partial (m, l, o)
     whole = whole && sc.t1 >= sc.pu1;
     float lo = 0.0f;
-    if (!exchange(l, lo)) break;
+    give(l);
+    if (!take(lo)) break;
     const float lt = half == 0 ? l + lo : lo + l;
     const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
-    if (!(ok = wwait(&ctl.pv_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, ctl, kSitePvEpi, p.dev_err))) break;
+    if (!(ok = wwait(&ctl.v_free[(n - 1) & 1u][1], ((n - 1) >> 1) & 1u, ctl, kSitePvEpi, p.dev_err))) break;
     tc_fence_after();
-    // Through the P tiles, 128 bytes of a row at a time, so that a warp stores whole lines. The
-    // two warps that share 32 rows of both tiles take one tile each; the weights of the next
-    // segment come after the exchange of its first tile, when both are through.
+    // (32 bytes at a time, a whole sector of the thread's own row)
     const int h0 = (sc.g * 2 + rank) * static_cast<int>(kRows) + (warp & 1) * 32;  // the warp's first row
-    const int rows = min(32, p.heads - h0);
-    const uint32_t buf = smem + kPOff + half * kPTile + (warp & 1) * 4096;
-    if (whole) {
-      __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(p.out) +
-                                 (static_cast<size_t>(sc.b) * p.heads + h0) * kDc + half * 256 + (lane & 7) * 8;
+    const bool mine_out = h0 + lane < p.heads;
+    const size_t out_row = static_cast<size_t>(sc.b) * p.heads + h0 + lane;
+    const size_t part_row = (static_cast<size_t>(pair) + sc.unit) * 128 + rank * kRows + (warp & 1) * 32 + lane;
+    __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(p.out) + out_row * kDc + half * 256;
+    float* const part = p.part_o + part_row * kDc + half * 256;
 #pragma unroll 1
-      for (int c = 0; c < 256; c += 64) {
+    for (int c = 0; c < 256; c += 32) {
+      uint32_t r[32];
+      tmem_ld32(t_o + c, r);
+      tmem_ld_wait();
+      if (!mine_out) continue;
+      if (whole) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          uint32_t r[32];
-          tmem_ld32(t_o + c + 32 * part, r);
-          tmem_ld_wait();
+        for (int q = 0; q < 2; ++q) {
+          uint32_t w[8];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[e] = pack_bf16(__uint_as_float(r[8 * q + 2 * e]) * inv, __uint_as_float(r[8 * q + 2 * e + 1]) * inv);
-            sts_v4(buf + swz_off(lane, 4 * part + q, 128), w[0], w[1], w[2], w[3]);
-          }
+          for (int e = 0; e < 8; ++e)
+            w[e] = pack_bf16(__uint_as_float(r[16 * q + 2 * e]) * inv, __uint_as_float(r[16 * q + 2 * e + 1]) * inv);
+          stg_v8(dst + c + 16 * q, w);
         }
-        __syncwarp();
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int rr = 4 * i + (lane >> 3);
-          const uint4 o = lds_v4(buf + swz_off(rr, lane & 7, 128));
-          if (rr < rows) *reinterpret_cast<uint4*>(dst + static_cast<size_t>(rr) * kDc + c) = o;
-        }
-        __syncwarp();
-      }
-      if (half == 0 && lane < rows && p.lse != nullptr)
-        p.lse[static_cast<size_t>(sc.b) * p.heads + h0 + lane] = (m + log2f(lt)) * kLn2;
-    } else {
-      const size_t row0 = (static_cast<size_t>(pair) + sc.unit) * 128 + rank * kRows + (warp & 1) * 32;
-      float* const dst = p.part_o + row0 * kDc + half * 256 + (lane & 7) * 4;
-#pragma unroll 1
-      for (int c = 0; c < 256; c += 32) {
-        uint32_t r[32];
-        tmem_ld32(t_o + c, r);
-        tmem_ld_wait();
-#pragma unroll
-        for (int q = 0; q < 8; ++q) sts_v4(buf + swz_off(lane, q, 128), r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int rr = 4 * i + (lane >> 3);
-          const uint4 o = lds_v4(buf + swz_off(rr, lane & 7, 128));
-          if (rr < rows) *reinterpret_cast<uint4*>(dst + static_cast<size_t>(rr) * kDc + c) = o;
-        }
-        __syncwarp();
-      }
-      if (half == 0 && lane < rows) {
-        p.part_ml[(row0 + lane) * 2] = m;
-        p.part_ml[(row0 + lane) * 2 + 1] = lt;
+        for (int q = 0; q < 4; ++q) stg_v8(part + c + 8 * q, r + 8 * q);
       }
     }
+    if (half == 0 && mine_out) {
+      if (!whole) {
+        p.part_ml[part_row * 2] = m;
+        p.part_ml[part_row * 2 + 1] = lt;
+      } else if (p.lse != nullptr) {
+        p.lse[out_row] = (m + log2f(lt)) * kLn2;
+      }
+    }
+    __syncwarp();
     tc_fence_before();
     __syncwarp();
     arrive_leader(lane, ofree);
   }
-  if (!ok && lane == 0) set_abort(ctl, p.dev_err);
+  if (!ok) {
+    if (lane == 0) set_abort(ctl, p.dev_err);
+    __syncwarp();
+    asm volatile("bar.arrive %0, 64;" ::"r"(1 + (warp & 1)) : "memory");
+  }
 }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tree_pair(const __grid_constant__ Params p) {
@@ -491,22 +507,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tree_pa
   const int rank = static_cast<int>(cluster_ctarank());
   const int pair = static_cast<int>(blockIdx.x >> 1);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&ctl.k_bar[i], 1);
-      mbar_init(&ctl.v_bar[i], 1);
-      mbar_init(&ctl.k_peer[i], 1);
-      mbar_init(&ctl.v_peer[i], 1);
-      mbar_init(&ctl.p_full[i], 2 * kSoftWarps);
-      mbar_init(&ctl.s_free[i], 2 * kSoftWarps);
-      mbar_init(&ctl.s_free[i + 2], 2 * kSoftWarps);
+    const uint32_t copies = rank == 0 ? 2 : 1;  // (own, and in the leader the other CTA's)
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&ctl.k_bar[i >> 1][i & 1], copies);
+      mbar_init(&ctl.v_bar[i >> 1][i & 1], copies);
+      mbar_init(&ctl.k_free[i >> 1][i & 1], 1);
+      mbar_init(&ctl.v_free[i >> 1][i & 1], 1);
       mbar_init(&ctl.s_full[i], 1);
-      mbar_init(&ctl.s_full[i + 2], 1);
-      mbar_init(&ctl.k_free[i], 1);
-      mbar_init(&ctl.pv_done[i], 1);
-      mbar_init(&ctl.halves[i], 2);
     }
-    mbar_init(&ctl.q_bar, 1);
-    mbar_init(&ctl.q_peer, 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&ctl.p_full[i], 2 * kSoftWarps);
+    mbar_init(&ctl.q_bar, copies);
     mbar_init(&ctl.q_free, 1);
     mbar_init(&ctl.o_free, 2 * kSoftWarps);
     mbar_init(&ctl.fin, 1);

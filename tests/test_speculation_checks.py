@@ -42,7 +42,7 @@ def tree_desc(**kw):
     {"max_blocks": 0}, {"max_blocks": 1 << 26}, {"num_blocks": 0}, {"softmax_scale": 0.0},
     {"softmax_scale": float("nan")}, {"softmax_scale": 2e30}, {"seq_lens": None}, {"seq_lens": FAKE + 3}, {"prot": FAKE},
     {"draft_rows": FAKE}, {"prot": FAKE + 8, "draft_rows": FAKE}, {"prot": FAKE, "draft_rows": FAKE + 8},
-    {"prot": FAKE, "draft_rows": FAKE, "cache_kind": 16}, {"out": None}, {"out": FAKE + 8}, {"lse": FAKE + 2},
+    {"prot": FAKE, "draft_rows": FAKE, "cache_kind": 16}, {"out": None}, {"out": FAKE + 16}, {"lse": FAKE + 2},
     {"workspace": None}, {"workspace": FAKE + 16}, {"batch": 1 << 30, "max_blocks": 1 << 20},
 ])
 def test_mla_decode_tree_refuses(L, kw):

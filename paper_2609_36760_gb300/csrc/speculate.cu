@@ -61,14 +61,48 @@ __device__ __forceinline__ Pair warp_scan(Pair x, int lane) {
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// What is left of p after refusals that took a times q: max(p - a q, 0), exact to 2^-48
-// (a NaN stays one).
-__device__ __forceinline__ Pair left_over(float p, float q, Pair a) {
-  const float h = __fmul_rn(a.hi, q);
-  const Pair s = two_sum(p, -h);
-  const Pair r = normal(s.hi, __fadd_rn(s.lo, -__fmaf_rn(a.lo, q, __fmaf_rn(a.hi, q, -h))));
-  return r.hi <= 0.0f ? Pair{0.0f, 0.0f} : r;
+__device__ __forceinline__ float max_nan(float a, float b) {  // (a NaN stays one)
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
+
+// What the terms of a sum are made of: p alone, p and q with a = 1 (after a first refusal),
+// p and q.
+enum Mode { kWhole, kOnce, kMore };
+
+// What is left of p after refusals that took a times q: max(p - a q, 0), exact to 2^-48, a NaN
+// in p a NaN. With h + lo = a q, h > p leaves nothing, h < p leaves (p - h) - lo, positive since
+// p - h is more than lo then, and h = p what lo leaves. p - min(p, h) is exact as a pair (the
+// larger of the two comes first).
+template <Mode M>
+__device__ __forceinline__ Pair left_over(float p, float q, Pair a) {
+  if constexpr (M == kWhole) return {max_nan(p, 0.0f), 0.0f};
+  const float h = M == kOnce ? q : __fmul_rn(a.hi, q);
+  const float m = fminf(p, h), s = __fadd_rn(p, -m);
+  float e = -__fadd_rn(m, __fadd_rn(s, -p));
+  if constexpr (M == kMore) {
+    const float lo = __fmaf_rn(a.lo, q, __fmaf_rn(a.hi, q, -h));
+    if (h <= p) e = __fadd_rn(e, -lo);
+    if (s == 0.0f) e = fmaxf(e, 0.0f);
+  }
+  return {s, e};
+}
+
+// Two running sums of pairs, of the even and the odd terms (as packed fp32).
+struct Sums {
+  uint64_t hi = 0, lo = 0;
+  __device__ __forceinline__ void add(Pair x, Pair y) {
+    const uint64_t minus = f32x2(-1.0f, -1.0f);
+    const uint64_t b = f32x2(x.hi, y.hi), s = add2(hi, b), bb = fma2(hi, minus, s);
+    const uint64_t e = add2(fma2(fma2(bb, minus, s), minus, hi), fma2(bb, minus, b));
+    hi = s;
+    lo = add2(lo, add2(e, f32x2(x.lo, y.lo)));
+  }
+  __device__ __forceinline__ Pair total() const {
+    return qmla::add(two_sum(lo2(hi), lo2(lo)), two_sum(hi2(hi), hi2(lo)));
+  }
+};
 
 constexpr int kVerifyThreads = 512, kVerifyWarps = kVerifyThreads / 32;
 constexpr int kMaxCluster = 8;
@@ -87,33 +121,58 @@ struct VerifyShared {
   unsigned long long found;
 };
 
-// The terms of the sums of a node: p and q its rows, `a` as in qmla_tree_verify; refused:
-// tokens that are out (no draft probabilities).
-template <typename T>
-struct Terms {
-  const T* p;
-  const T* q;  // null where a = 0
-  Pair a;
-  const int* refused;
-  int n;
-  __device__ __forceinline__ Pair at(int v) const {
-    const float x = as_float(p[v]);
-    if (q != nullptr) return left_over(x, as_float(q[v]), a);
-    Pair r = {x <= 0.0f ? 0.0f : x, 0.0f};
-    for (int i = 0; i < n; ++i)
-      if (refused[i] == v) r.hi = 0.0f;
-    return r;
+// Sum of the terms v0 .. v1 - 1 of a node (p and q its rows), a share of it in each lane. Eight
+// values of each row are on their way at a time: of 16 bytes where both rows lie on such
+// borders (VEC; v0 and v1 are multiples of their values then), else one by one.
+template <typename T, Mode M, bool VEC>
+__device__ __forceinline__ Pair row_sum(const T* p, const T* q, Pair a, int v0, int v1, int lane) {
+  constexpr int kWide = VEC ? 16 / static_cast<int>(sizeof(T)) : 1, kLoads = 8 / kWide;
+  Sums sums;
+  for (int v = v0 + lane * kWide; v < v1; v += 32 * 8) {
+    float x[8], y[8];
+    if constexpr (VEC) {
+      uint4 rx[kLoads], ry[kLoads];
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const bool in = v + i * 32 * kWide < v1;
+        rx[i] = in ? __ldg(reinterpret_cast<const uint4*>(p + v + i * 32 * kWide)) : make_uint4(0, 0, 0, 0);
+        if (M != kWhole) ry[i] = in ? __ldg(reinterpret_cast<const uint4*>(q + v + i * 32 * kWide)) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = as_float(reinterpret_cast<const T*>(&rx[e / kWide])[e % kWide]);
+        if (M != kWhole) y[e] = as_float(reinterpret_cast<const T*>(&ry[e / kWide])[e % kWide]);
+      }
+    } else {
+      T rx[8], ry[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool in = v + e * 32 < v1;
+        rx[e] = in ? p[v + e * 32] : T(0.0f);
+        if (M != kWhole) ry[e] = in ? q[v + e * 32] : T(0.0f);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = as_float(rx[e]);
+        if (M != kWhole) y[e] = as_float(ry[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+      sums.add(left_over<M>(x[e], M != kWhole ? y[e] : 0.0f, a), left_over<M>(x[e + 1], M != kWhole ? y[e + 1] : 0.0f, a));
   }
-};
+  return sums.total();
+}
 
 // One cluster a sequence. The walk itself is a warp's, done alike in every CTA; the sums over
 // the vocabulary are all warps', warp w of the cluster taking the w-th piece of the row.
 template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const qmla_verify_desc d, int ctas) {
+__global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_verify_desc d, int ctas) {
   __shared__ VerifyShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = static_cast<int>(cluster_ctarank()), b = blockIdx.y;
   const size_t first = static_cast<size_t>(b) * d.nodes;
+  griddep_wait();
   int n = d.tree_lens != nullptr ? d.tree_lens[b] : d.nodes;
   if (n < 0 || n > d.nodes) {
     if (tid == 0 && rank == 0) report(d.dev_err, QMLA_DEVERR_BAD_TREE);
@@ -158,7 +217,11 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const qmla_verif
   }
   __syncthreads();
 
-  const int chunk = (d.vocab + ctas * kVerifyWarps - 1) / (ctas * kVerifyWarps);
+  // (pieces of whole vectors for every lane)
+  const int chunk = ((d.vocab + ctas * kVerifyWarps - 1) / (ctas * kVerifyWarps) + 255) / 256 * 256;
+  const bool vec = d.vocab % (16 / sizeof(T)) == 0 && d.target_row_stride % (16 / sizeof(T)) == 0 &&
+                   d.draft_row_stride % (16 / sizeof(T)) == 0 && (reinterpret_cast<uintptr_t>(target) & 15) == 0 &&
+                   (reinterpret_cast<uintptr_t>(draft) & 15) == 0;
   // Warp 0's state: the node, its children not yet looked at, the refusals so far.
   int cur = 0, kept = 1;
   uint64_t children = 0ull;
@@ -226,19 +289,35 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const qmla_verif
       }
     }
     __syncthreads();
-    Terms<T> terms;
-    terms.p = target + static_cast<size_t>(sh.cur) * d.target_row_stride;
-    terms.a = sh.a;
-    terms.q = sh.a.hi != 0.0f ? draft + static_cast<size_t>(sh.cur) * d.draft_row_stride : nullptr;
-    terms.refused = sh.refused;
-    terms.n = sh.refused_n;
+    const T* const p = target + static_cast<size_t>(sh.cur) * d.target_row_stride;
+    const T* const q = draft == nullptr ? nullptr : draft + static_cast<size_t>(sh.cur) * d.draft_row_stride;
+    const Pair took = sh.a;
+    const Mode mode = took.hi == 0.0f ? kWhole : (took.hi == 1.0f && took.lo == 0.0f ? kOnce : kMore);
+    const int refusals = sh.refused_n;  // (of certain drafts)
     const bool last = sh.last;
+    auto term = [&](int v) {
+      const float x = as_float(p[v]);
+      if (mode != kWhole) return left_over<kMore>(x, as_float(q[v]), took);
+      Pair r = left_over<kWhole>(x, 0.0f, took);
+      for (int i = 0; i < refusals; ++i)
+        if (sh.refused[i] == v) r.hi = 0.0f;
+      return r;
+    };
     // ---- this warp's piece of the sum
     const int w = rank * kVerifyWarps + warp;
     const int v0 = min(w * chunk, d.vocab), v1 = min(v0 + chunk, d.vocab);
-    Pair sum = {0.0f, 0.0f};
-    for (int v = v0 + lane; v < v1; v += 32) sum = add(sum, terms.at(v));
+    Pair sum;
+    if (mode == kWhole) {
+      sum = vec ? row_sum<T, kWhole, true>(p, q, took, v0, v1, lane) : row_sum<T, kWhole, false>(p, q, took, v0, v1, lane);
+    } else if (mode == kOnce) {
+      sum = vec ? row_sum<T, kOnce, true>(p, q, took, v0, v1, lane) : row_sum<T, kOnce, false>(p, q, took, v0, v1, lane);
+    } else {
+      sum = vec ? row_sum<T, kMore, true>(p, q, took, v0, v1, lane) : row_sum<T, kMore, false>(p, q, took, v0, v1, lane);
+    }
     sum = warp_scan(sum, lane);
+    for (int i = 0; i < refusals; ++i)
+      if (sh.refused[i] >= v0 && sh.refused[i] < v1)
+        sum = add(sum, {-left_over<kWhole>(as_float(p[sh.refused[i]]), 0.0f, took).hi, 0.0f});
     Pair* const part = sh.part[pass & 1];
     if (lane == 31) {
       for (int r = 0; r < ctas; ++r) {
@@ -286,7 +365,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const qmla_verif
       const int p0 = min(piece * chunk, d.vocab), p1 = min(p0 + chunk, d.vocab);
       const int t0 = min(p0 + tid * each, p1), t1 = min(t0 + each, p1);
       Pair s = {0.0f, 0.0f};
-      for (int v = t0; v < t1; ++v) s = add(s, terms.at(v));
+      for (int v = t0; v < t1; ++v) s = add(s, term(v));
       Pair incl = warp_scan(s, lane);
       if (lane == 31) sh.scan[warp] = incl;
       Pair excl = shfl_up(incl, 1);
@@ -298,7 +377,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const qmla_verif
       // (ordered so that a token above the cut comes before the fallback, the last with weight)
       unsigned long long mine = ~0ull;
       for (int v = t0; v < t1; ++v) {
-        const Pair x = terms.at(v);
+        const Pair x = term(v);
         run = add(run, x);
         if (x.hi > 0.0f) {
           if (above(run, cut)) {
@@ -383,6 +462,7 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const qmla_keep_desc
   __shared__ uint8_t* to[kMaxNodes];
   __shared__ int from_slot[kMaxNodes], to_slot[kMaxNodes], node[kMaxNodes];
   const int tid = threadIdx.x, b = blockIdx.x;
+  griddep_wait();
   const int len = d.seq_lens[b], n = d.tree_lens != nullptr ? d.tree_lens[b] : d.nodes, kept = d.kept[b];
   const bool bad_len = len < 0 || len > d.max_blocks * kBlockTokens;
   bool good = !bad_len && n >= 0 && n <= d.nodes && n <= len && kept >= 0 && kept <= n;
@@ -461,38 +541,39 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const qmla_keep_desc
   }
 }
 
-template <typename T>
-cudaError_t launch_verify(const qmla_verify_desc& d, int ctas, cudaStream_t stream) {
+// (Programmatic launches: the kernels' own start overlaps the end of what is before them, which
+// they wait for at once.)
+template <typename... Args>
+cudaError_t launch(void (*kern)(Args...), dim3 grid, int threads, int cluster, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas, d.batch);
-  cfg.blockDim = dim3(kVerifyThreads);
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim = {static_cast<unsigned>(ctas), 1, 1};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {static_cast<unsigned>(cluster), 1, 1};
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, verify_kernel<T>, d, ctas);
+  cfg.numAttrs = cluster > 0 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
 }  // namespace
 
-cudaError_t launch_tree_verify(const qmla_verify_desc& d, int /*sms*/, cudaStream_t stream) {
+cudaError_t launch_tree_verify(const qmla_verify_desc& d, int sms, cudaStream_t stream) {
+  // More CTAs a row while each has 4,096 tokens and all of them run at once (two an SM).
   int ctas = 1;
-  while (ctas < kMaxCluster && d.vocab > 4096 * ctas) ctas *= 2;
-  return d.probs == QMLA_PROBS_F32 ? launch_verify<float>(d, ctas, stream)
-                                   : launch_verify<__nv_bfloat16>(d, ctas, stream);
+  while (ctas < kMaxCluster && d.vocab > 4096 * ctas && 2 * ctas * d.batch <= 2 * sms) ctas *= 2;
+  auto* const kern = d.probs == QMLA_PROBS_F32 ? verify_kernel<float> : verify_kernel<__nv_bfloat16>;
+  return launch(kern, dim3(ctas, d.batch), kVerifyThreads, ctas, stream, d, ctas);
 }
 
 cudaError_t launch_cache_keep(const qmla_keep_desc& d, cudaStream_t stream) {
-  const dim3 grid(d.batch), block(kKeepThreads);
-  switch (d.cache_kind) {
-    case 4: keep_kernel<4><<<grid, block, 0, stream>>>(d); break;
-    case 2: keep_kernel<2><<<grid, block, 0, stream>>>(d); break;
-    case kC4R4: keep_kernel<kC4R4><<<grid, block, 0, stream>>>(d); break;
-    default: keep_kernel<16><<<grid, block, 0, stream>>>(d); break;
-  }
-  return cudaGetLastError();
+  auto* const kern = d.cache_kind == 4 ? keep_kernel<4>
+                                       : (d.cache_kind == 2 ? keep_kernel<2>
+                                                            : (d.cache_kind == kC4R4 ? keep_kernel<kC4R4> : keep_kernel<16>));
+  return launch(kern, dim3(d.batch), kKeepThreads, 0, stream, d);
 }
 
 }  // namespace qmla

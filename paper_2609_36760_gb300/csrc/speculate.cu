@@ -5,6 +5,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -33,10 +34,8 @@ __device__ __forceinline__ Pair normal(float s, float e) {  // |s| >= |e|
   return {h, __fadd_rn(e, -__fadd_rn(h, -s))};
 }
 __device__ __forceinline__ Pair add(Pair a, Pair b) {
-  Pair s = two_sum(a.hi, b.hi);
-  const Pair t = two_sum(a.lo, b.lo);
-  s = normal(s.hi, __fadd_rn(s.lo, t.hi));
-  return normal(s.hi, __fadd_rn(s.lo, t.lo));
+  const Pair s = two_sum(a.hi, b.hi);
+  return normal(s.hi, __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo)));
 }
 __device__ __forceinline__ Pair times(Pair a, float u) {
   const float h = __fmul_rn(a.hi, u);
@@ -121,45 +120,33 @@ struct VerifyShared {
   unsigned long long found;
 };
 
-// Sum of the terms v0 .. v1 - 1 of a node (p and q its rows), a share of it in each lane. Eight
-// values of each row are on their way at a time: of 16 bytes where both rows lie on such
+// Sum of the terms v0 .. v1 - 1 of a node (p and q its rows), a share of it in each lane. kFlight
+// values of each row are on their way at a time: in 16 bytes where both rows lie on such
 // borders (VEC; v0 and v1 are multiples of their values then), else one by one.
+constexpr int kFlight = 16;
 template <typename T, Mode M, bool VEC>
 __device__ __forceinline__ Pair row_sum(const T* p, const T* q, Pair a, int v0, int v1, int lane) {
-  constexpr int kWide = VEC ? 16 / static_cast<int>(sizeof(T)) : 1, kLoads = 8 / kWide;
+  constexpr int kWide = VEC ? 16 / static_cast<int>(sizeof(T)) : 1, kLoads = kFlight / kWide;
+  using Load = typename std::conditional<VEC, uint4, T>::type;
   Sums sums;
-  for (int v = v0 + lane * kWide; v < v1; v += 32 * 8) {
-    float x[8], y[8];
-    if constexpr (VEC) {
-      uint4 rx[kLoads], ry[kLoads];
+#pragma unroll 1
+  for (int v = v0 + lane * kWide; v < v1; v += 32 * kFlight) {
+    Load x[kLoads], y[kLoads];
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const bool in = v + i * 32 * kWide < v1;
-        rx[i] = in ? __ldg(reinterpret_cast<const uint4*>(p + v + i * 32 * kWide)) : make_uint4(0, 0, 0, 0);
-        if (M != kWhole) ry[i] = in ? __ldg(reinterpret_cast<const uint4*>(q + v + i * 32 * kWide)) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = as_float(reinterpret_cast<const T*>(&rx[e / kWide])[e % kWide]);
-        if (M != kWhole) y[e] = as_float(reinterpret_cast<const T*>(&ry[e / kWide])[e % kWide]);
-      }
-    } else {
-      T rx[8], ry[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool in = v + e * 32 < v1;
-        rx[e] = in ? p[v + e * 32] : T(0.0f);
-        if (M != kWhole) ry[e] = in ? q[v + e * 32] : T(0.0f);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = as_float(rx[e]);
-        if (M != kWhole) y[e] = as_float(ry[e]);
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = v + i * 32 * kWide;
+      x[i] = y[i] = Load{};
+      if (at < v1) {
+        x[i] = __ldg(reinterpret_cast<const Load*>(p + at));
+        if (M != kWhole) y[i] = __ldg(reinterpret_cast<const Load*>(q + at));
       }
     }
+    auto term = [&](int e) {
+      return left_over<M>(as_float(reinterpret_cast<const T*>(&x[e / kWide])[e % kWide]),
+                          M == kWhole ? 0.0f : as_float(reinterpret_cast<const T*>(&y[e / kWide])[e % kWide]), a);
+    };
 #pragma unroll
-    for (int e = 0; e < 8; e += 2)
-      sums.add(left_over<M>(x[e], M != kWhole ? y[e] : 0.0f, a), left_over<M>(x[e + 1], M != kWhole ? y[e + 1] : 0.0f, a));
+    for (int e = 0; e < kFlight; e += 2) sums.add(term(e), term(e + 1));
   }
   return sums.total();
 }
@@ -217,8 +204,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
   }
   __syncthreads();
 
-  // (pieces of whole vectors for every lane)
-  const int chunk = ((d.vocab + ctas * kVerifyWarps - 1) / (ctas * kVerifyWarps) + 255) / 256 * 256;
+  // (pieces of whole vectors)
+  const int chunk = ((d.vocab + ctas * kVerifyWarps - 1) / (ctas * kVerifyWarps) + 63) / 64 * 64;
   const bool vec = d.vocab % (16 / sizeof(T)) == 0 && d.target_row_stride % (16 / sizeof(T)) == 0 &&
                    d.draft_row_stride % (16 / sizeof(T)) == 0 && (reinterpret_cast<uintptr_t>(target) & 15) == 0 &&
                    (reinterpret_cast<uintptr_t>(draft) & 15) == 0;
@@ -327,22 +314,29 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
       }
     }
     cluster_sync_all();
-    if (warp == 0) {
-      Pair carry = {0.0f, 0.0f};
-      for (int i = 0; i < ctas * kVerifyWarps; i += 32) {
-        const bool any = i + lane < ctas * kVerifyWarps;
-        Pair x = any ? part[i + lane] : Pair{0.0f, 0.0f};
-        const Pair incl = add(carry, warp_scan(x, lane));
-        Pair excl = shfl_up(incl, 1);
-        if (lane == 0) excl = carry;
-        if (any) sh.before[i + lane] = excl;
-        carry = {__shfl_sync(0xffffffffu, incl.hi, 31), __shfl_sync(0xffffffffu, incl.lo, 31)};
+    if (warp == 0) {  // every lane a few of the partial sums in a row
+      constexpr int kEach = kMaxCluster * kVerifyWarps / 32;
+      const int warps = ctas * kVerifyWarps;
+      Pair run = {0.0f, 0.0f}, upto[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        upto[i] = run;
+        if (lane * kEach + i < warps) run = add(run, part[lane * kEach + i]);
       }
-      if (lane == 0) sh.total = carry;
-      mass = value(carry);
+      const Pair incl = warp_scan(run, lane);
+      Pair excl = shfl_up(incl, 1);
+      if (lane == 0) excl = {0.0f, 0.0f};
+      const Pair total = {__shfl_sync(0xffffffffu, incl.hi, 31), __shfl_sync(0xffffffffu, incl.lo, 31)};
+      mass = value(total);
+      if (last) {
+        if (lane == 0) sh.total = total;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+          if (lane * kEach + i < warps) sh.before[lane * kEach + i] = add(excl, upto[i]);
+      }
     }
-    __syncthreads();
     if (!last) continue;
+    __syncthreads();
 
     // ---- the draw: the warp whose piece the threshold lies in, then its tokens
     const Pair total = sh.total;
@@ -361,32 +355,36 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
     __syncthreads();
     if (fine && piece / kVerifyWarps == rank) {
       if (tid == 0) sh.found = ~0ull;
+      // (a few tokens in a row for each thread, their terms at hand if they are eight at most)
       const int each = (chunk + kVerifyThreads - 1) / kVerifyThreads;
+      constexpr int kHeld = 8;
+      Pair held[kHeld];
       const int p0 = min(piece * chunk, d.vocab), p1 = min(p0 + chunk, d.vocab);
       const int t0 = min(p0 + tid * each, p1), t1 = min(t0 + each, p1);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) held[i] = t0 + i < t1 ? term(t0 + i) : Pair{0.0f, 0.0f};
       Pair s = {0.0f, 0.0f};
-      for (int v = t0; v < t1; ++v) s = add(s, term(v));
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) s = add(s, held[i]);
+#pragma unroll 4
+      for (int v = t0 + kHeld; v < t1; ++v) s = add(s, term(v));
       Pair incl = warp_scan(s, lane);
       if (lane == 31) sh.scan[warp] = incl;
       Pair excl = shfl_up(incl, 1);
       if (lane == 0) excl = {0.0f, 0.0f};
       __syncthreads();
-      Pair base = sh.before[piece];
-      for (int i = 0; i < warp; ++i) base = add(base, sh.scan[i]);
-      Pair run = add(base, excl);
+      const Pair ends = warp_scan(lane < kVerifyWarps ? sh.scan[lane] : Pair{0.0f, 0.0f}, lane);
+      const Pair below = {__shfl_sync(0xffffffffu, ends.hi, max(warp - 1, 0)), __shfl_sync(0xffffffffu, ends.lo, max(warp - 1, 0))};
+      Pair run = add(warp > 0 ? add(sh.before[piece], below) : sh.before[piece], excl);
       // (ordered so that a token above the cut comes before the fallback, the last with weight)
       unsigned long long mine = ~0ull;
-      for (int v = t0; v < t1; ++v) {
-        const Pair x = term(v);
+      auto look = [&](int v, Pair x) {
         run = add(run, x);
-        if (x.hi > 0.0f) {
-          if (above(run, cut)) {
-            mine = v;
-            break;
-          }
-          mine = (1ull << 40) - v;
-        }
-      }
+        if (x.hi > 0.0f && mine > (1ull << 32)) mine = above(run, cut) ? v : (1ull << 40) - v;
+      };
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) look(t0 + i, held[i]);
+      for (int v = t0 + kHeld; v < t1; ++v) look(v, term(v));
       if (mine != ~0ull) atomicMin(&sh.found, mine);
       __syncthreads();
       if (tid == 0) {

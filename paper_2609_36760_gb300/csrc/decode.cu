@@ -1079,22 +1079,23 @@ __device__ __forceinline__ uint4 rest_piece(const float (&f)[8]) {
 }
 
 // Block idx % img_width of sequence idx / img_width as an fp16 image (see Params::images), zero
-// behind the sequence's end, and for short sequences the image of C - RN_f16(C). A thread has
+// behind the sequence's end up to a whole tile, and for short sequences the image of C - RN_f16(C). A thread has
 // the same eight channels of one row's nine chunks, all loaded before any is stored.
 template <int CB>
 __device__ void expand_block(const Params& p, int idx) {
   static_assert(!kTree || kPrepThreads == kBlockTokens * 8, "a thread per row and piece");
   griddep_wait();  // (the cache may still be written until here)
   const int b = idx / p.img_width, j = idx - b * p.img_width;
-  const int entry = p.table[static_cast<size_t>(b) * p.max_blocks + j];
+  const int entry = j < p.max_blocks ? p.table[static_cast<size_t>(b) * p.max_blocks + j] : -1;
   const int len = p.seq_lens[b], n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
-  if (len > p.max_tokens || n < 0 || n > p.q_tokens || n > len || j * kBlockTokens >= len) return;
+  if (len > p.max_tokens || n < 0 || n > p.q_tokens || n > len) return;
+  if (j >= (len + kTileTokens - 1) / kTileTokens * (kTileTokens / kBlockTokens)) return;
   const int ctx = len - n;
   constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
   const bool known = entry >= 0 && entry < p.num_blocks;
   const uint8_t* const blk = p.pool + static_cast<size_t>(known ? entry : 0) * kBlk;
   const int i = threadIdx.x & 7, slot = threadIdx.x >> 3, pos = j * kBlockTokens + slot;
-  const size_t at = (slot >> 5) * kHalfImage + swz_off(slot & 31, i, 128);
+  const size_t at = swz_off(slot, i, 128);
   uint8_t* const img = p.images + static_cast<size_t>(idx) * kImage + at;
   uint8_t* const rest = p.rest_images != nullptr && len <= kExactTokens
                             ? p.rest_images + (static_cast<size_t>(b) * p.rest_width + j) * kImage + at
@@ -1116,8 +1117,8 @@ __device__ void expand_block(const Params& p, int idx) {
 #pragma unroll
     for (int k = 0; k < kNumChunks; ++k) {
       bf16_values(raw[k], f);
-      *reinterpret_cast<uint4*>(img + k * 4096) = half_piece(f);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * 4096) = rest_piece(f);
+      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = half_piece(f);
+      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = rest_piece(f);
     }
   } else if (known && pos < len) {
     RowPiece r[kNumChunks];
@@ -1126,15 +1127,15 @@ __device__ void expand_block(const Params& p, int idx) {
 #pragma unroll
     for (int k = 0; k < kNumChunks; ++k) {
       piece_values<CB>(r[k], k, f);
-      *reinterpret_cast<uint4*>(img + k * 4096) = half_piece(f);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * 4096) = rest_piece(f);
+      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = half_piece(f);
+      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = rest_piece(f);
     }
   } else {
     if (pos < len) report(p.dev_err, QMLA_DEVERR_BAD_BLOCK);
 #pragma unroll 1
     for (int k = 0; k < kNumChunks; ++k) {
-      *reinterpret_cast<uint4*>(img + k * 4096) = make_uint4(0, 0, 0, 0);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * 4096) = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
+      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
     }
   }
 }

@@ -56,7 +56,7 @@ struct Params {
   TreeSeq* trees;             // [batch], written by the prep kernel
   int max_tokens;             // longer sequences are bad
   // Only where the context is laid out as fp16 tiles (tree_pair.cu): images [batch][img_width]
-  // of its 64-token blocks, and rest_images [batch][rest_width], of what their rounding left
+  // of its 64-token blocks (an even number of them), and rest_images [batch][rest_width], of what their rounding left
   // off, of sequences up to kExactTokens.
   uint8_t* images;
   uint8_t* rest_images;
@@ -73,9 +73,8 @@ struct TreeSeq {
   int pad;
 };
 
-// A block as two halves of 32 tokens, each nine chunks of [32][128 bytes], swizzled as the
-// tensor core reads them.
-constexpr int kHalfImage = 9 * 32 * 128, kImage = 2 * kHalfImage;
+// A block as nine chunks of [64 tokens][128 bytes], swizzled as the tensor core reads them.
+constexpr int kImage = 9 * 64 * 128;
 // Sequences up to this length get the more exact scores (see tree_pair.cu).
 constexpr int kExactTokens = 1024;
 // Main kernel over these images; prm's plan is over 128-row units.

@@ -26,7 +26,9 @@ TreeWorkspace tree_workspace_layout(int batch, int rows, int grid) {
   w.images_off = round_up(w.trees_off + static_cast<size_t>(batch) * sizeof(TreeSeq));
   return w;
 }
-int image_blocks(long long tokens) { return static_cast<int>((tokens + kBlockTokens - 1) / kBlockTokens); }
+int image_blocks(long long tokens) {  // of whole tiles
+  return static_cast<int>((tokens + kTileTokens - 1) / kTileTokens * (kTileTokens / kBlockTokens));
+}
 size_t image_bytes(int batch, int blocks) {
   return static_cast<size_t>(batch) * (blocks + std::min(blocks, kExactTokens / kBlockTokens)) * kImage;
 }

@@ -2,22 +2,25 @@
 // per CTA, with tcgen05 cta_group::2, over the context as fp16 tiles that the prep kernel has
 // laid out in memory once for all rows (decode_tree.cu, expand_block).
 //
-// A tile is one 64-token block, as M = 128 MMAs over the pair:
-//   S[r, t] = q[r, :] . C[t, :]     A: each CTA's 64 rows of q, B: each CTA's 32 tokens (N = 64), K = 576
+// A tile is 128 tokens, two cache blocks, as M = 128 MMAs over the pair:
+//   S[r, t] = q[r, :] . C[t, :]     A: each CTA's 64 rows of q, B: each CTA's block (N = 128), K = 576
 //   O[r, c] += P[r, :] C[:, c]      A: each CTA's 64 rows of P, B: each CTA's 256 channels (2 x N = 256),
-//                                   K = 64 tokens
-// Its operands come by bulk copies of the swizzled images: 36 KB of a CTA's own tokens for the
-// scores, 32 KB of its own channels for the values, two stages of each. So a block is
-// dequantised once for all row groups of its sequence instead of once (and a half) for each, and
-// the SM's warps only do the softmax: decode_pair, which dequantises, spends 3.35k cycles a tile
-// of which the MMAs are 1.5k.
+//                                   K = 128 tokens
+// Its operands come by bulk copies of the swizzled images: 72 KB of a CTA's own block for the
+// scores, 64 KB of its own channels of both blocks for the values. So a block is dequantised
+// once for all row groups of its sequence instead of once (and a half) for each, and the SM's
+// warps only do the softmax (decode_pair, which dequantises, spends 6.7k cycles on 128 tokens).
+//
+// There is room for one tile of each operand. Its parts (three of the keys', four of the
+// values') are filled, used and freed one by one: the scores of a tile take half of the time
+// that its values leave them, so that a part's copy has most of a tile's time to arrive.
 //
 // Short sequences (at most kExactTokens) also have images of what rounding to fp16 left off their
 // rows (C - RN_f16(C)), and their scores are the sum of both products: with few keys the
 // roundings do not average out of lse (200 INT4 tokens: 2e-5 of it against 1e-7).
 //
 // TMEM (per CTA; lanes 0..63 hold the first half of N for rows 0..63, lanes 64..127 the second):
-// O 2 x 128 columns, S 4 buffers of 32.
+// O 2 x 128 columns, S 2 buffers of 64.
 #include <cuda_runtime.h>
 
 #include <cstddef>
@@ -27,32 +30,32 @@
 namespace qmla {
 namespace {
 
-constexpr int kTok = 64;        // tokens per tile: one cache block
 constexpr int kSoftWarps = 4;   // warps 0..3, one per TMEM lane quarter
 constexpr int kLoadWarp = 5;    // bulk copies; warp 4: MMAs (leader), or arrivals on the leader for the copies
 constexpr int kThreads = 6 * 32;
 constexpr uint32_t kRows = 64;                        // query rows per CTA
-constexpr uint32_t kQBytes = kNumChunks * kRows * 128;
-constexpr uint32_t kKBytes = kHalfImage;              // own 32 tokens, K-major B of QK
-constexpr uint32_t kKChunk = 32 * 128;
-// Each K stage is filled, used and freed in two parts of five and four chunks, each V stage in
-// two of 128 channels, so that a copy has most of two tiles' time to arrive.
-constexpr uint32_t kKSplit = 5;
-constexpr uint32_t kVChunk = kTok * 128, kVBytes = 4 * kVChunk;  // own channels, MN-major B of PV
-constexpr uint32_t kPTile = kRows * 128;              // P, K-major A of PV
-constexpr uint32_t kKOff = kQBytes, kVOff = kKOff + 2 * kKBytes, kPOff = kVOff + 2 * kVBytes;
-constexpr uint32_t kCtrlOff = kPOff + 2 * kPTile;
+constexpr uint32_t kChunk = 64 * 128;                 // 64 rows or tokens x 64 channels
+constexpr uint32_t kQBytes = kNumChunks * kChunk;
+constexpr uint32_t kKBytes = kImage;                  // own block, K-major B of QK
+constexpr uint32_t kVChunk = 2 * kChunk, kVBytes = 4 * kVChunk;  // own channels, MN-major B of PV
+constexpr uint32_t kPBytes = 2 * kRows * 128;         // P, K-major A of PV: 64 tokens, then the others
+constexpr uint32_t kKOff = kQBytes, kVOff = kKOff + kKBytes, kPOff = kVOff + kVBytes;
+constexpr uint32_t kCtrlOff = kPOff + kPBytes;
 constexpr uint32_t kColS = 256, kTmemCols = 512;
+// Parts of the operands: three chunks of the keys (and of the query, where a segment starts);
+// 128 channels of 64 tokens of the values.
+constexpr int kKeyParts = 3, kValueParts = 4;
+constexpr uint32_t kKeyPart = 3 * kChunk, kValuePart = 2 * kChunk;
 
 struct __align__(16) TreeCtrl {
-  // Operands are there, [stage][part]: this CTA's own copies (transaction counts), in the leader
-  // also an arrival for the other CTA's.
-  uint64_t k_bar[2][2], v_bar[2][2], q_bar;
-  // The leader's: P written (4 warps per CTA), O read.
-  uint64_t p_full[2], o_free;
-  // Arrived on by MMA commits, multicast to both CTAs: scores complete, part of a K stage free,
-  // part of a V stage free (the second: PV complete, P free), every QK of a segment done.
-  uint64_t s_full[4], k_free[2][2], v_free[2][2], q_free;
+  // A part is there: this CTA's own copies (transaction counts), in the leader also an arrival
+  // for the other CTA's.
+  uint64_t k_bar[kKeyParts], v_bar[kValueParts];
+  // The leader's: P written (4 warps per CTA), and before it, where a segment starts, O read.
+  uint64_t p_full;
+  // Arrived on by MMA commits, multicast to both CTAs: scores complete, a part free (the last of
+  // the values': PV complete, P free).
+  uint64_t s_full[2], k_free[kKeyParts], v_free[kValueParts];
   uint64_t fin;
   uint32_t tmem_base, abort;
   float xch[2][128];
@@ -61,10 +64,10 @@ constexpr int kSmem = 1024 + kCtrlOff + static_cast<int>(sizeof(TreeCtrl));
 static_assert(kSmem <= 232448, "shared memory per CTA");
 
 // The tiles of one pair: its range of the plan's list of 128-token tiles, cut into segments at
-// unit ends. Tile q is 64-token block q of a sequence.
+// unit ends. Tile q is blocks 2 q and 2 q + 1 of a sequence.
 struct TreeSched {
   int q, qend, q0;    // current tile, end and first tile of the segment
-  int unit, pu0, pu1; // unit and its 128-token tiles in the plan's list
+  int unit, pu0, pu1; // unit and its tiles in the plan's list
   int b, g, len;
   int t0, t1;
   bool live;
@@ -72,8 +75,8 @@ struct TreeSched {
     b = unit / p.n_hg;
     g = unit - b * p.n_hg;
     len = p.seq_lens[b];
-    q = q0 = 2 * j;
-    qend = min(2 * (min(t1, pu1) - pu0), (len + kTok - 1) / kTok);
+    q = q0 = j;
+    qend = min(t1, pu1) - pu0;
   }
   __device__ void init(const Params& p, int pair) {
     const int4 info = p.cta_info[pair];
@@ -104,18 +107,17 @@ struct TreeSched {
     enter(p, 0);
   }
   // Products that make up the scores: of the images, and of what they leave off.
-  __device__ int parts(const Params& p) const { return p.rest_images != nullptr && len <= kExactTokens ? 2 : 1; }
+  __device__ int products(const Params& p) const { return p.rest_images != nullptr && len <= kExactTokens ? 2 : 1; }
 };
 
 // The order in which the issuer takes QK and PV, and the copies come: QK of a tile goes before PV
-// of the tile before it, unless it starts a segment, whose query waits for the last QK of the
-// segment before. (QK of tile i so goes after PV of tile i - 2: who has its scores knows that
-// its P tile is free, and the scores of tile i - 4, whose place it takes, have been read.)
+// of the tile before it. (So the softmax of a tile has the QK of the next one to work under, and
+// QK of tile i goes after PV of tile i - 2, whose P shows that its scores have been read.)
 struct TreeOrder {
   TreeSched k, v;  // at tiles nk and nv
   uint32_t nk = 0, nv = 0;
   __device__ bool live() const { return v.live; }
-  __device__ bool score_next() const { return k.live && nk < nv + 2 && !(k.first() && nk > nv); }
+  __device__ bool score_next() const { return k.live && nk < nv + 2; }
 };
 
 __device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, TreeCtrl& c, uint32_t site, uint32_t* dev_err) {
@@ -147,45 +149,38 @@ __device__ __forceinline__ bool pwait_cluster(uint64_t* bar, uint32_t parity, Tr
 __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, TreeCtrl& ctl, int rank) {
   TreeOrder o;
   o.k = o.v = sc;
-  uint32_t kk = 0, seg = 0, copies = 0, values = 0;
+  uint32_t pass = 0, copies = 0, values = 0;  // products begun; parts asked for
   bool ok = true;
   while (ok && o.live()) {
     if (o.score_next()) {
-      const size_t img = static_cast<size_t>(o.k.b) * p.img_width + o.k.q;
-      const int parts = o.k.parts(p);
-      for (int part = 0; ok && part < parts; ++part, ++kk) {
-        const uint32_t st = kk & 1u;
-        const uint8_t* src = part == 0 ? p.images + img * kImage
-                                       : p.rest_images + (static_cast<size_t>(o.k.b) * p.rest_width + o.k.q) * kImage;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          constexpr uint32_t kBytes[2] = {kKSplit * kKChunk, kKBytes - kKSplit * kKChunk};
-          if (kk >= 2 && !(ok = pwait(&ctl.k_free[st][i], ((kk >> 1) - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
-          mbar_arrive_expect_tx(&ctl.k_bar[st][i], kBytes[i]);
-          bulk_g2s(sm + kKOff + st * kKBytes + i * kBytes[0], src + rank * kHalfImage + i * kBytes[0], kBytes[i],
-                   &ctl.k_bar[st][i]);
+      const int products = o.k.products(p), block = 2 * o.k.q + rank;
+      const uint8_t* q = p.qimg + (static_cast<size_t>(o.k.b) * p.n_img + 2 * o.k.g + rank) * kQBytes;
+      for (int i = 0; ok && i < products; ++i, ++pass) {
+        const uint8_t* src = i == 0 ? p.images + (static_cast<size_t>(o.k.b) * p.img_width + block) * kImage
+                                    : p.rest_images + (static_cast<size_t>(o.k.b) * p.rest_width + block) * kImage;
+        const bool query = i == 0 && o.k.first();  // (its part's last reader was that of the keys')
+#pragma unroll 1
+        for (int part = 0; part < kKeyParts; ++part) {
+          uint64_t* const bar = &ctl.k_bar[part];
+          if (pass > 0 && !(ok = pwait(&ctl.k_free[part], (pass - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
+          mbar_arrive_expect_tx(bar, query ? 2 * kKeyPart : kKeyPart);
+          if (query) bulk_g2s(sm + part * kKeyPart, q + part * kKeyPart, kKeyPart, bar);
+          bulk_g2s(sm + kKOff + part * kKeyPart, src + part * kKeyPart, kKeyPart, bar);
           ++copies;
         }
-      }
-      if (ok && o.k.first()) {
-        if (seg > 0 && !(ok = pwait(&ctl.q_free, (seg - 1) & 1u, ctl, kSiteMmaQFull, p.dev_err))) break;
-        mbar_arrive_expect_tx(&ctl.q_bar, kQBytes);
-        bulk_g2s(sm, p.qimg + (static_cast<size_t>(o.k.b) * p.n_img + 2 * o.k.g + rank) * kQBytes, kQBytes, &ctl.q_bar);
-        ++seg;
       }
       ++o.nk;
       o.k.next(p);
     } else {
-      const uint32_t st = o.nv & 1u;
-      const uint8_t* src = p.images + (static_cast<size_t>(o.v.b) * p.img_width + o.v.q) * kImage + 4 * rank * kKChunk;
+      const uint8_t* src = p.images + (static_cast<size_t>(o.v.b) * p.img_width + 2 * o.v.q) * kImage + 4 * rank * kChunk;
 #pragma unroll 1
-      for (int blk = 0; ok && blk < 2; ++blk) {
-        if (o.nv >= 2 && !(ok = pwait(&ctl.v_free[st][blk], ((o.nv >> 1) - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
-        mbar_arrive_expect_tx(&ctl.v_bar[st][blk], kVBytes / 2);
-#pragma unroll 1
-        for (int i = 4 * blk; i < 4 * blk + 4; ++i)  // chunk i / 2, tokens 32 (i & 1) ..
-          bulk_g2s(sm + kVOff + st * kVBytes + (i >> 1) * kVChunk + (i & 1) * kKChunk,
-                   src + (i & 1) * kHalfImage + (i >> 1) * kKChunk, kKChunk, &ctl.v_bar[st][blk]);
+      for (int part = 0; part < kValueParts; ++part) {  // channels 128 (part / 2) .., block part & 1
+        uint64_t* const bar = &ctl.v_bar[part];
+        if (o.nv > 0 && !(ok = pwait(&ctl.v_free[part], (o.nv - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
+        mbar_arrive_expect_tx(bar, kValuePart);
+#pragma unroll
+        for (int c = part & ~1; c < (part & ~1) + 2; ++c)
+          bulk_g2s(sm + kVOff + c * kVChunk + (part & 1) * kChunk, src + (part & 1) * kImage + c * kChunk, kChunk, bar);
         ++values;
       }
       ++o.nv;
@@ -194,46 +189,45 @@ __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, Tre
   }
   if (!ok) set_abort(ctl, p.dev_err);
   // No copy and no commit may reach this CTA once it has left; these waits ignore the abort flag.
-  for (uint32_t i = 0; i < 4; ++i) {
-    const uint32_t nk = (copies + 3 - i) >> 2, nv = (values + 3 - i) >> 2;  // phases begun of part i & 1 of stage i / 2
-    if (nk > 0) mbar_wait(&ctl.k_bar[i >> 1][i & 1], (nk - 1) & 1u, kWaitNs, nullptr);
-    if (nv > 0) mbar_wait(&ctl.v_bar[i >> 1][i & 1], (nv - 1) & 1u, kWaitNs, nullptr);
-    if (ok && nk > 0) mbar_wait(&ctl.k_free[i >> 1][i & 1], (nk - 1) & 1u, kWaitNs, nullptr);
-    if (ok && nv > 0) mbar_wait(&ctl.v_free[i >> 1][i & 1], (nv - 1) & 1u, kWaitNs, nullptr);
+  for (uint32_t i = 0; i < kKeyParts; ++i) {
+    const uint32_t n = (copies + kKeyParts - 1 - i) / kKeyParts;  // phases begun
+    if (n > 0) mbar_wait(&ctl.k_bar[i], (n - 1) & 1u, kWaitNs, nullptr);
+    if (ok && n > 0) mbar_wait(&ctl.k_free[i], (n - 1) & 1u, kWaitNs, nullptr);
   }
-  if (seg > 0) mbar_wait(&ctl.q_bar, (seg - 1) & 1u, kWaitNs, nullptr);
-  if (ok && seg > 0) mbar_wait(&ctl.q_free, (seg - 1) & 1u, kWaitNs, nullptr);
+  for (uint32_t i = 0; i < kValueParts; ++i) {
+    const uint32_t n = (values + kValueParts - 1 - i) / kValueParts;
+    if (n > 0) mbar_wait(&ctl.v_bar[i], (n - 1) & 1u, kWaitNs, nullptr);
+    if (ok && n > 0) mbar_wait(&ctl.v_free[i], (n - 1) & 1u, kWaitNs, nullptr);
+  }
 }
 
 // The other CTA: tells the leader of each of its copies, in the order in which the issuer asks.
 // (The tensor core of this SM reads what they brought, and this thread has written nothing, so
 // the arrivals release nothing to the cluster: with that release each took more than a
-// thousand cycles, and a tile 4,700 instead of 1,830.)
+// thousand cycles, 4,700 instead of 1,830 for 64 tokens.)
 __device__ void relay_role(const Params& p, const TreeSched& sc, TreeCtrl& ctl) {
   TreeOrder o;
   o.k = o.v = sc;
-  uint32_t kk = 0, seg = 0;
+  uint32_t pass = 0;
   bool ok = true;
-  const uint32_t kbar = cluster_map(smem_u32(&ctl.k_bar[0][0]), 0), vbar = cluster_map(smem_u32(&ctl.v_bar[0][0]), 0);
-  const uint32_t qbar = cluster_map(smem_u32(&ctl.q_bar), 0);
+  const uint32_t kbar = cluster_map(smem_u32(&ctl.k_bar[0]), 0), vbar = cluster_map(smem_u32(&ctl.v_bar[0]), 0);
   while (ok && o.live()) {
     if (o.score_next()) {
-      if (o.k.first()) {
-        if (!(ok = pwait(&ctl.q_bar, seg & 1u, ctl, kSiteMmaQFull, p.dev_err))) break;
-        mbar_arrive_remote(qbar, true);
-        ++seg;
-      }
-      const int parts = o.k.parts(p);
-      for (int part = 0; ok && part < 2 * parts; ++part, ++kk) {
-        if (!(ok = pwait(&ctl.k_bar[(kk >> 1) & 1u][kk & 1u], (kk >> 2) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
-        mbar_arrive_remote(kbar + (kk & 3u) * 8, true);
+      const int products = o.k.products(p);
+      for (int i = 0; ok && i < products; ++i, ++pass) {
+#pragma unroll 1
+        for (int part = 0; part < kKeyParts; ++part) {
+          if (!(ok = pwait(&ctl.k_bar[part], pass & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+          mbar_arrive_remote(kbar + part * 8, true);
+        }
       }
       ++o.nk;
       o.k.next(p);
     } else {
-      for (int blk = 0; blk < 2; ++blk) {
-        if (!(ok = pwait(&ctl.v_bar[o.nv & 1u][blk], (o.nv >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
-        mbar_arrive_remote(vbar + ((o.nv & 1u) * 2 + blk) * 8, true);
+#pragma unroll 1
+      for (int part = 0; part < kValueParts; ++part) {
+        if (!(ok = pwait(&ctl.v_bar[part], o.nv & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+        mbar_arrive_remote(vbar + part * 8, true);
       }
       ++o.nv;
       o.v.next(p);
@@ -244,65 +238,54 @@ __device__ void relay_role(const Params& p, const TreeSched& sc, TreeCtrl& ctl) 
 
 // --------------------------------------------------------------------- MMAs
 __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, TreeCtrl& ctl, uint32_t tmem) {
-  constexpr uint32_t kIdQK = idesc_f16_f32(128, kTok, false, false);
+  constexpr uint32_t kIdQK = idesc_f16_f32(128, 128, false, false);
   constexpr uint32_t kIdPV = idesc_f16_f32(128, 256, false, true);
   const uint64_t qa = smem_desc(smem, 16, 1024, SWZ_128B), kb = smem_desc(smem + kKOff, 16, 1024, SWZ_128B);
   const uint64_t pa = smem_desc(smem + kPOff, 16, 1024, SWZ_128B);
   const uint64_t vb = smem_desc(smem + kVOff, kVChunk, 1024, SWZ_128B);
   TreeOrder o;
   o.k = o.v = sc;
-  uint32_t kk = 0, qseg = 0, pseg = 0;
+  uint32_t pass = 0;
   bool ok = true;
   while (ok && o.live()) {
     if (o.score_next()) {
-      const uint32_t n = o.nk;
-      if (o.k.first()) {
-        if (!(ok = pwait_cluster(&ctl.q_bar, qseg & 1u, ctl, kSiteMmaQFull, p.dev_err))) break;
-        ++qseg;
-      }
-      const uint32_t ts = tmem + kColS + (n & 3u) * 32;
-      const int parts = o.k.parts(p);
-      for (int part = 0; ok && part < parts; ++part, ++kk) {
-        const uint32_t st = kk & 1u;
-        const uint64_t b1 = kb + ((st * kKBytes) >> 4);
+      const uint32_t ts = tmem + kColS + (o.nk & 1u) * 64;
+      const int products = o.k.products(p);
+      for (int i = 0; ok && i < products; ++i, ++pass) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (!(ok = pwait_cluster(&ctl.k_bar[st][i], (kk >> 1) & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+        for (int part = 0; part < kKeyParts; ++part) {
+          if (!(ok = pwait_cluster(&ctl.k_bar[part], pass & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
           tc_fence_after();
 #pragma unroll
-          for (int k = i * kKSplit; k < (i == 0 ? static_cast<int>(kKSplit) : kNumChunks); ++k) {
+          for (int k = 3 * part; k < 3 * part + 3; ++k) {
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-              umma2_f16_ss(ts, qa + ((k * kRows * 128 + s * 32) >> 4), b1 + ((k * kKChunk + s * 32) >> 4), kIdQK,
-                           k == 0 && s == 0 && part == 0 ? 0u : 1u);
+              umma2_f16_ss(ts, qa + ((k * kChunk + s * 32) >> 4), kb + ((k * kChunk + s * 32) >> 4), kIdQK,
+                           k == 0 && s == 0 && i == 0 ? 0u : 1u);
           }
-          umma2_commit(&ctl.k_free[st][i]);
+          umma2_commit(&ctl.k_free[part]);
         }
       }
       if (!ok) break;
-      umma2_commit(&ctl.s_full[n & 3u]);
-      if (o.k.last()) umma2_commit(&ctl.q_free);
+      umma2_commit(&ctl.s_full[o.nk & 1u]);
       ++o.nk;
       o.k.next(p);
     } else {
-      const uint32_t st = o.nv & 1u, ph = (o.nv >> 1) & 1u;
+      const uint32_t ph = o.nv & 1u;
       const bool first = o.v.first();
-      if (!(ok = pwait_cluster(&ctl.p_full[st], ph, ctl, kSiteMmaPFull, p.dev_err) &&
-                 (!first || pseg == 0 || pwait_cluster(&ctl.o_free, (pseg - 1) & 1u, ctl, kSiteMmaOFree, p.dev_err))))
-        break;
-      const uint64_t a1 = pa + ((st * kPTile) >> 4), b1 = vb + ((st * kVBytes) >> 4);
+      if (!(ok = pwait_cluster(&ctl.p_full, ph, ctl, kSiteMmaPFull, p.dev_err))) break;
 #pragma unroll
-      for (int blk = 0; blk < 2; ++blk) {
-        if (!(ok = pwait_cluster(&ctl.v_bar[st][blk], ph, ctl, kSiteMmaChunk, p.dev_err))) break;
+      for (int part = 0; part < kValueParts; ++part) {
+        if (!(ok = pwait_cluster(&ctl.v_bar[part], ph, ctl, kSiteMmaChunk, p.dev_err))) break;
         tc_fence_after();
 #pragma unroll
         for (int s = 0; s < 4; ++s)
-          umma2_f16_ss(tmem + blk * 128, a1 + ((s * 32) >> 4), b1 + ((blk * 2 * kVChunk + s * 2048) >> 4), kIdPV,
-                       first && s == 0 ? 0u : 1u);
-        umma2_commit(&ctl.v_free[st][blk]);
+          umma2_f16_ss(tmem + (part >> 1) * 128, pa + (((part & 1) * kRows * 128 + s * 32) >> 4),
+                       vb + (((part >> 1) * 2 * kVChunk + (part & 1) * kChunk + s * 2048) >> 4), kIdPV,
+                       first && (part & 1) == 0 && s == 0 ? 0u : 1u);
+        umma2_commit(&ctl.v_free[part]);
       }
       if (!ok) break;
-      if (o.v.last()) ++pseg;
       ++o.nv;
       o.v.next(p);
     }
@@ -331,8 +314,7 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
   const uint32_t t_o = tmem + lanes;
   const float sl2 = p.scale_log2;
-  const uint32_t pfull = cluster_map(smem_u32(&ctl.p_full[0]), 0);
-  const uint32_t ofree = cluster_map(smem_u32(&ctl.o_free), 0);
+  const uint32_t pfull = cluster_map(smem_u32(&ctl.p_full), 0);
   uint32_t n = 0, ex = 0;
   bool ok = true, whole = false, all_alive = false;
   float m = -INFINITY, l = 0.0f;
@@ -350,6 +332,12 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
     ++ex;
     return ok;
   };
+  // PV of tile i has completed: its P may be overwritten, O moved or read.
+  auto wait_pv = [&](uint32_t i) {
+    ok = wwait(&ctl.v_free[kValueParts - 1], i & 1u, ctl, kSitePvEpi, p.dev_err);
+    tc_fence_after();
+    return ok;
+  };
 
   for (; ok && sc.live; sc.next(p)) {
     const bool first = sc.first();
@@ -364,44 +352,42 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
       whole = sc.q == 0;
       all_alive = __all_sync(0xffffffffu, line != 0ull);
     }
-    const int d = kTok * sc.q + 32 * half - ctx;  // node in the first of the 32 columns
-    const bool full = all_alive && d <= -32;
-    if (!(ok = wwait(&ctl.s_full[n & 3u], (n >> 2) & 1u, ctl, kSiteSmSFull, p.dev_err))) break;
+    const int d = kTileTokens * sc.q + 64 * half - ctx;  // node in the first of the 64 columns
+    const bool full = all_alive && d <= -64;
+    if (!(ok = wwait(&ctl.s_full[n & 1u], (n >> 1) & 1u, ctl, kSiteSmSFull, p.dev_err))) break;
     tc_fence_after();
-    float x[32], top;
-    tmem_ld32_max(tmem + kColS + (n & 3u) * 32 + lanes, x, top);
+    float x[64], top, top2;
+    tmem_ld32_max(tmem + kColS + (n & 1u) * 64 + lanes, x, top);
+    tmem_ld32_max(tmem + kColS + (n & 1u) * 64 + 32 + lanes, x + 32, top2);
     tmem_ld_wait();
+    top = fmaxf(top, top2);
     if (!full) {  // the columns that the row sees: the context's, and the nodes of its line
-      uint32_t mask = 0u;
+      uint64_t mask = 0ull;
       if (line != 0ull) {
-        mask = d <= -32 ? ~0u : (d < 0 ? (1u << -d) - 1u : 0u);
-        if (d >= 0 && d < 64) mask |= static_cast<uint32_t>(line >> d);
-        if (d < 0 && d > -32) mask |= static_cast<uint32_t>(line << -d);
+        if (d <= -64) mask = ~0ull;
+        else if (d < 0) mask = ((1ull << -d) - 1ull) | (line << -d);
+        else if (d < 64) mask = line >> d;
       }
+      const uint32_t lo = static_cast<uint32_t>(mask), hi = static_cast<uint32_t>(mask >> 32);
       top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        x[i] = (mask >> i) & 1u ? x[i] : -INFINITY;
+      for (int i = 0; i < 64; ++i) {
+        x[i] = ((i < 32 ? lo : hi) >> (i & 31)) & 1u ? x[i] : -INFINITY;
         top = fmaxf(top, x[i]);
       }
     }
-    const uint32_t st = n & 1u;
-    const uint32_t ptile = smem + kPOff + st * kPTile;
+    uint32_t pk[32];
     float sum = 0.0f;
     // (a row that has seen no key has no reference: its columns are all masked)
     auto weights = [&]() {
       const float ref = m == -INFINITY ? 0.0f : m;
       float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < 32; i += 8) {
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] = ex2_approx(__fmaf_rn(x[i + e], sl2, -ref));
-          s[e & 3] += w[e];
-        }
-        sts_v4(ptile + swz_off(row, half * 4 + i / 8, 128), pack_h2(w[0], w[1]), pack_h2(w[2], w[3]),
-               pack_h2(w[4], w[5]), pack_h2(w[6], w[7]));
+      for (int i = 0; i < 64; i += 2) {
+        const float w0 = ex2_approx(__fmaf_rn(x[i], sl2, -ref)), w1 = ex2_approx(__fmaf_rn(x[i + 1], sl2, -ref));
+        s[i & 3] += w0;
+        s[(i & 3) + 1] += w1;
+        pk[i / 2] = pack_h2(w0, w1);
       }
       sum = (s[0] + s[1]) + (s[2] + s[3]);
     };
@@ -413,13 +399,12 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
     if (!take(other)) break;
     mine = fmaxf(mine, other);
     const bool raise = first ? mine > m : mine > m + kRescaleLog2;
+    if (n > 0 && !wait_pv(n - 1)) break;
     if (first || __any_sync(0xffffffffu, raise)) {
       const float a = raise && m != -INFINITY ? exp2f(m - mine) : 1.0f;
       if (raise) m = mine;
       l *= a;
       if (!first && __any_sync(0xffffffffu, a != 1.0f)) {
-        if (!(ok = wwait(&ctl.v_free[(n - 1) & 1u][1], ((n - 1) >> 1) & 1u, ctl, kSitePvEpi, p.dev_err))) break;
-        tc_fence_after();
 #pragma unroll 1
         for (int c = 0; c < 256; c += 32) {
           uint32_t r[32];
@@ -433,10 +418,14 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
       }
       weights();
     }
+    const uint32_t ptile = smem + kPOff + half * (kRows * 128);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      sts_v4(ptile + swz_off(row, i, 128), pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
     fence_proxy_async_smem();
     tc_fence_before();
     __syncwarp();
-    arrive_leader(lane, pfull + st * 8);
+    arrive_leader(lane, pfull);
     l += sum;
     ++n;
     if (!sc.last()) continue;
@@ -448,8 +437,6 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
     if (!take(lo)) break;
     const float lt = half == 0 ? l + lo : lo + l;
     const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
-    if (!(ok = wwait(&ctl.v_free[(n - 1) & 1u][1], ((n - 1) >> 1) & 1u, ctl, kSitePvEpi, p.dev_err))) break;
-    tc_fence_after();
     // (32 bytes at a time, a whole sector of the thread's own row)
     const int h0 = (sc.g * 2 + rank) * static_cast<int>(kRows) + (warp & 1) * 32;  // the warp's first row
     const bool mine_out = h0 + lane < p.heads;
@@ -457,6 +444,7 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
     const size_t part_row = (static_cast<size_t>(pair) + sc.unit) * 128 + rank * kRows + (warp & 1) * 32 + lane;
     __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(p.out) + out_row * kDc + half * 256;
     float* const part = p.part_o + part_row * kDc + half * 256;
+    if (!wait_pv(n - 1)) break;
 #pragma unroll 1
     for (int c = 0; c < 256; c += 32) {
       uint32_t r[32];
@@ -486,9 +474,6 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
       }
     }
     __syncwarp();
-    tc_fence_before();
-    __syncwarp();
-    arrive_leader(lane, ofree);
   }
   if (!ok) {
     if (lane == 0) set_abort(ctl, p.dev_err);
@@ -508,17 +493,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tree_pa
   const int pair = static_cast<int>(blockIdx.x >> 1);
   if (threadIdx.x == 0) {
     const uint32_t copies = rank == 0 ? 2 : 1;  // (own, and in the leader the other CTA's)
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(&ctl.k_bar[i >> 1][i & 1], copies);
-      mbar_init(&ctl.v_bar[i >> 1][i & 1], copies);
-      mbar_init(&ctl.k_free[i >> 1][i & 1], 1);
-      mbar_init(&ctl.v_free[i >> 1][i & 1], 1);
-      mbar_init(&ctl.s_full[i], 1);
+    for (int i = 0; i < kKeyParts; ++i) {
+      mbar_init(&ctl.k_bar[i], copies);
+      mbar_init(&ctl.k_free[i], 1);
     }
-    for (int i = 0; i < 2; ++i) mbar_init(&ctl.p_full[i], 2 * kSoftWarps);
-    mbar_init(&ctl.q_bar, copies);
-    mbar_init(&ctl.q_free, 1);
-    mbar_init(&ctl.o_free, 2 * kSoftWarps);
+    for (int i = 0; i < kValueParts; ++i) {
+      mbar_init(&ctl.v_bar[i], copies);
+      mbar_init(&ctl.v_free[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) mbar_init(&ctl.s_full[i], 1);
+    mbar_init(&ctl.p_full, 2 * kSoftWarps);
     mbar_init(&ctl.fin, 1);
     ctl.abort = 0u;
     fence_mbar_init();

@@ -37,6 +37,7 @@
 //                  (combine_wide_kernel for a few long units).
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstddef>
 
 #include "decode_common.cuh"
@@ -1087,10 +1088,9 @@ __device__ void expand_block(const Params& p, int idx) {
   griddep_wait();  // (the cache may still be written until here)
   const int b = idx / p.img_width, j = idx - b * p.img_width;
   const int entry = j < p.max_blocks ? p.table[static_cast<size_t>(b) * p.max_blocks + j] : -1;
-  const int len = p.seq_lens[b], n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
-  if (len > p.max_tokens || n < 0 || n > p.q_tokens || n > len) return;
-  if (j >= (len + kTileTokens - 1) / kTileTokens * (kTileTokens / kBlockTokens)) return;
-  const int ctx = len - n;
+  int groups;
+  if (j >= tree_tiles(p, b, 1, groups, nullptr) * (kTileTokens / kBlockTokens) || groups == 0) return;
+  const int len = p.seq_lens[b], ctx = len - (p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens);
   constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
   const bool known = entry >= 0 && entry < p.num_blocks;
   const uint8_t* const blk = p.pool + static_cast<size_t>(known ? entry : 0) * kBlk;
@@ -1140,10 +1140,24 @@ __device__ void expand_block(const Params& p, int idx) {
   }
 }
 
-// The image of 64 query rows (see query_piece), in channel order; a thread's work as above.
+// The image of 64 query rows (see query_piece), in channel order; a thread's work as above. Rows
+// of a group without a node get their results.
 __device__ __forceinline__ void query_image(const Params& p, int u) {
   const int b = u / p.n_img, i = threadIdx.x & 7, h = threadIdx.x >> 3;
   const int row = (u - b * p.n_img) * 64 + h;
+  int groups;
+  const int tiles = tree_tiles(p, b, 128, groups, nullptr);
+  if (tiles == 0 || (u - b * p.n_img) / 2 >= groups) {
+    // No node has a row here: nothing runs for them but this.
+    if (row >= p.heads) return;
+    griddep_wait();
+    uint4* const out = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) +
+                                                (static_cast<size_t>(b) * p.heads + row) * kDc) + i * (kDc / 64);
+#pragma unroll
+    for (int e = 0; e < kDc / 64; ++e) out[e] = make_uint4(0, 0, 0, 0);
+    if (i == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(b) * p.heads + row] = -INFINITY;
+    return;
+  }
   uint4 raw[kNumChunks];
 #pragma unroll
   for (int k = 0; k < kNumChunks; ++k) raw[k] = make_uint4(0, 0, 0, 0);
@@ -1214,24 +1228,27 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
   if (!pf_on_chip) griddep_wait();  // (the prefix goes straight to the workspace)
   if (threadIdx.x == 0) carry = 0;
   __syncthreads();
-  for (int base = 0; base < p.batch; base += blockDim.x) {
+  // (of a tree, over units: groups without a node have no tiles)
+  const int entries = kTree ? p.batch * p.n_hg : p.batch;
+  for (int base = 0; base < entries; base += blockDim.x) {
     const int b = base + threadIdx.x;
     int tiles = 0;
-    if (b < p.batch) {
+    if constexpr (kTree) {
+      if (b < entries) {
+        int seq, g, groups;
+        tree_unit(p, b, seq, g);
+        tiles = tree_tiles(p, seq, PAIR ? 2 * HG : HG, groups, g == 0 ? p.dev_err : nullptr);
+        if (g >= groups) tiles = 0;
+      }
+    } else if (b < p.batch) {
       int len = p.seq_lens[b];
-      if (len < 0 || len > (kTree ? p.max_tokens : p.max_blocks * kBlockTokens)) {
+      if (len < 0 || len > p.max_blocks * kBlockTokens) {
         report(p.dev_err, QMLA_DEVERR_BAD_POSITION);
         len = 0;
-      } else if constexpr (kTree) {
-        const int n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
-        if (n < 0 || n > p.q_tokens || n > len) {
-          report(p.dev_err, QMLA_DEVERR_BAD_TREE);
-          len = 0;
-        }
       }
       tiles = (len + kTileTokens - 1) / kTileTokens;
     }
-    const int v = tiles * p.n_hg;
+    const int v = kTree ? tiles : tiles * p.n_hg;
     int x = v;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -1251,10 +1268,10 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
     }
     __syncthreads();
     const int excl = carry + (warp > 0 ? warp_sums[warp - 1] : 0) + x - v;
-    if (b < p.batch) {
-      for (int hg = 0; hg < p.n_hg; ++hg) {
+    if (b < entries) {
+      for (int hg = 0; hg < (kTree ? 1 : p.n_hg); ++hg) {
         int32_t* const pf = pf_on_chip ? pf_s : p.prefix_w;
-        pf[b * p.n_hg + hg] = excl + hg * tiles;
+        pf[kTree ? b : b * p.n_hg + hg] = excl + hg * tiles;
       }
     }
     __syncthreads();
@@ -1288,7 +1305,7 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
     }
     const int pu0 = pf[lo], pu1 = pf[lo + 1];
     // The first tile's block-table entries (clamped column, like row_ref) and length.
-    const int b = lo / p.n_hg;
+    const int b = kTree && p.by_group ? lo % p.batch : lo / p.n_hg;
     const int j = t0 - pu0;
     const bool any = t0 < static_cast<int>(static_cast<long long>(c + 1) * T / p.grid);
     int4 first = make_int4(-1, -1, 0, 0);
@@ -1330,14 +1347,37 @@ __device__ __forceinline__ void store_out(const Params& p, size_t at, float4 v) 
 template <int HG>
 __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
   griddep_wait();  // the partials of the main kernel
-  const int u = blockIdx.x;
   const int h = blockIdx.y * 4 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   const int units = p.batch * p.n_hg;
-  const int b = u / p.n_hg;
-  const int h0 = (u - b * p.n_hg) * HG;
+  int u, b, h0, P0, P1, T;
+  if constexpr (kTree && HG == 128) {
+    // A block per range: the unit that lies over its end and begins in it. (Whole units wrote
+    // their results, and prep those of units without tiles.)
+    const int c = blockIdx.x;
+    const int4 next = p.cta_info[c + 1];
+    const int end = p.cta_t0[c + 1];
+    u = next.x;
+    P0 = next.y;
+    P1 = next.z;
+    T = next.w;
+    if (P0 >= end || end >= P1 || cta_of(P0, T, p.grid) != c) return;
+    tree_unit(p, u, b, h0);
+    h0 *= HG;
+  } else {
+    u = blockIdx.x;
+    if constexpr (kTree) {
+      tree_unit(p, u, b, h0);
+    } else {
+      b = u / p.n_hg;
+      h0 = u - b * p.n_hg;
+    }
+    h0 *= HG;
+    P0 = p.prefix[u];
+    P1 = p.prefix[u + 1];
+    T = p.prefix[units];
+  }
   if (h >= HG || h0 + h >= p.heads) return;
-  const int P0 = p.prefix[u], P1 = p.prefix[u + 1], T = p.prefix[units];
   const size_t out = (static_cast<size_t>(b) * p.heads + h0 + h) * kDc + lane * 16;
   if (P0 == P1) {
 #pragma unroll
@@ -1398,8 +1438,9 @@ __global__ void __launch_bounds__(kWideThreads) combine_wide_kernel(const Params
   const int u = blockIdx.x;
   const int h = blockIdx.y;
   const int units = p.batch * p.n_hg;
-  const int b = u / p.n_hg;
-  const int h0 = (u - b * p.n_hg) * HG;
+  int b = u / p.n_hg, g = u - b * p.n_hg;
+  if constexpr (kTree) tree_unit(p, u, b, g);
+  const int h0 = g * HG;
   if (h0 + h >= p.heads) return;
   const int P0 = p.prefix[u], P1 = p.prefix[u + 1], T = p.prefix[units];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -1587,12 +1628,13 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
   if (ev1 != nullptr && (e = cudaEventRecord(ev1, stream)) != cudaSuccess) return e;
   // Few units split over many CTAs each (long contexts): spread each unit's
   // pieces over more threads; otherwise one warp per head.
-  if (units * 4 < prm.grid && prm.grid <= kWideThreads) {
+  const bool wide = !(kTree && PAIR) || prm.img_width > 16;  // (of a tree's unit: more than eight tiles)
+  if (wide && units * 4 < prm.grid && prm.grid <= kWideThreads) {
     return launch_k(combine_wide_kernel<kUnitHeads>, dim3(static_cast<unsigned>(units), kUnitHeads),
                     dim3(kWideThreads), 0, stream, pdl, prm);
   }
-  return launch_k(combine_kernel<kUnitHeads>, dim3(static_cast<unsigned>(units), (kUnitHeads + 3) / 4), dim3(128), 0,
-                  stream, pdl, prm);
+  const unsigned blocks = kTree && PAIR ? static_cast<unsigned>(std::max(prm.grid - 1, 1)) : static_cast<unsigned>(units);
+  return launch_k(combine_kernel<kUnitHeads>, dim3(blocks, (kUnitHeads + 3) / 4), dim3(128), 0, stream, pdl, prm);
 }
 
 template <int CB, bool PROT>

@@ -61,6 +61,8 @@ struct Params {
   uint8_t* images;
   uint8_t* rest_images;
   int img_width, rest_width;
+  // Order of the plan's units (sequence b, row group g): b * n_hg + g, or g * batch + b.
+  bool by_group;
 };
 
 // One sequence's tree as the kernels use it. Nodes are bits; a node with a bad parent, or
@@ -120,6 +122,29 @@ constexpr int kTraceCtas = 8, kTraceEvents = 128, kTraceTiles = 32;
   do {                              \
   } while (0)
 #endif
+
+// Sequence and row group of unit u of a tree's plan.
+__device__ __forceinline__ void tree_unit(const Params& p, int u, int& b, int& g) {
+  const int inner = p.by_group ? p.batch : p.n_hg;
+  const int i = u / inner, j = u - i * inner;
+  b = p.by_group ? j : i;
+  g = p.by_group ? i : j;
+}
+// Tiles of each row group of sequence b, and how many of the groups have a node's rows
+// (rows: query rows of a group). A sequence whose length or count is bad has none.
+__device__ __forceinline__ int tree_tiles(const Params& p, int b, int rows, int& groups, uint32_t* dev_err) {
+  const int len = p.seq_lens[b], n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
+  groups = 0;
+  if (len < 0 || len > p.max_tokens) {
+    report(dev_err, QMLA_DEVERR_BAD_POSITION);
+  } else if (n < 0 || n > p.q_tokens || n > len) {
+    report(dev_err, QMLA_DEVERR_BAD_TREE);
+  } else {
+    groups = (n * p.hpt + rows - 1) / rows;
+    return (len + 127) / 128;
+  }
+  return 0;
+}
 
 // Channel order inside each 8-channel (16-byte) piece of a reconstructed row:
 // the unpacking below yields nibble/crumb pairs in this order, and the query

@@ -4,8 +4,6 @@
 //
 // The kernels are the decode's (decode.cu, compiled here for trees); prep also finds the
 // sets of nodes above and below each node.
-#include <algorithm>
-
 #define QMLA_DECODE_TREE 1
 #include "decode.cu"
 
@@ -87,11 +85,20 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
   if (w.images_off + image_bytes(d.batch, blocks) <= d.workspace_bytes) {
     prm.images = ws + w.images_off;
     prm.img_width = blocks;
-    prm.rest_images = prm.images + static_cast<size_t>(d.batch) * blocks * kImage;
+    if (d.cache_kind != QMLA_CACHE_BF16)  // (whose values are fp16 ones, but the very small)
+      prm.rest_images = prm.images + static_cast<size_t>(d.batch) * blocks * kImage;
     prm.rest_width = std::min(blocks, kExactTokens / kBlockTokens);
     prm.n_hg = (rows + 127) / 128;
     prm.n_img = 2 * prm.n_hg;
     prm.grid = grid / 2;
+    // Images that L2 does not hold are read by all row groups of a sequence at once: the plan
+    // goes group by group, with as many ranges to each, which then keep step.
+    const int teams = prm.grid / prm.n_hg;
+    if (static_cast<size_t>(d.batch) * blocks * kImage > (96u << 20) && teams > 0 &&
+        (prm.grid - teams * prm.n_hg) * 12 <= prm.grid) {
+      prm.by_group = true;
+      prm.grid = teams * prm.n_hg;
+    }
     switch (d.cache_kind) {
       case 4: return launch_impl<4, 64, false, true>(prm, stream, nullptr, nullptr);
       case 2: return launch_impl<2, 64, false, true>(prm, stream, nullptr, nullptr);

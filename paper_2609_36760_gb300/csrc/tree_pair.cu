@@ -72,8 +72,7 @@ struct TreeSched {
   int t0, t1;
   bool live;
   __device__ void enter(const Params& p, int j) {
-    b = unit / p.n_hg;
-    g = unit - b * p.n_hg;
+    tree_unit(p, unit, b, g);
     len = p.seq_lens[b];
     q = q0 = j;
     qend = min(t1, pu1) - pu0;

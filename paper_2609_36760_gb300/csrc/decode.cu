@@ -1399,7 +1399,11 @@ __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
     const float4* o = reinterpret_cast<const float4*>(p.part_o + pi * kDc) + lane * 4;
     float4 ov[4];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) ov[v] = o[v];
+    for (int v = 0; v < 4; ++v) {
+      if constexpr (kTree && HG == 128)
+        o = reinterpret_cast<const float4*>(p.part_o + tree_part_at(static_cast<size_t>(c) + u, h, lane * 16 + 4 * v)) - v;
+      ov[v] = o[v];
+    }
     const float Mn = fmaxf(M, ml.x);
     // A partial that saw no key for this head has m = -inf and l = o = 0.
     const float a = M == Mn ? 1.0f : exp2f(M - Mn), w = ml.x == Mn ? 1.0f : exp2f(ml.x - Mn);
@@ -1483,7 +1487,9 @@ __global__ void __launch_bounds__(kWideThreads) combine_wide_kernel(const Params
 #pragma unroll 4
   for (int cc = c0 + grp; cc <= c1; cc += kWideGroups) {
     const float wc = wts[cc - c0];
-    const float4 o = __ldcg(ob + ((static_cast<size_t>(cc) + u) * HG + h) * (kDc / 4));
+    const float4 o = __ldcg(kTree && HG == 128
+                                ? reinterpret_cast<const float4*>(p.part_o + tree_part_at(static_cast<size_t>(cc) + u, h, v * 4))
+                                : ob + ((static_cast<size_t>(cc) + u) * HG + h) * (kDc / 4));
     if (wc != 0.0f) {  // a piece that wrote nothing is never multiplied in
       acc.x += wc * o.x;
       acc.y += wc * o.y;

@@ -123,6 +123,10 @@ constexpr int kTraceCtas = 8, kTraceEvents = 128, kTraceTiles = 32;
   } while (0)
 #endif
 
+// A partial result of a tree's 128-row unit in part_o: [64 pieces of 8 channels][128 rows][8].
+__device__ __forceinline__ size_t tree_part_at(size_t piece, int row, int channel) {
+  return piece * (128 * kDc) + static_cast<size_t>(channel / 8) * (128 * 8) + row * 8 + channel % 8;
+}
 // Sequence and row group of unit u of a tree's plan.
 __device__ __forceinline__ void tree_unit(const Params& p, int u, int& b, int& g) {
   const int inner = p.by_group ? p.batch : p.n_hg;

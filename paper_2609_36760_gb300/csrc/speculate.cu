@@ -42,7 +42,10 @@ __device__ __forceinline__ Pair times(Pair a, float u) {
   return normal(h, __fmaf_rn(a.lo, u, __fmaf_rn(a.hi, u, -h)));
 }
 __device__ __forceinline__ bool above(Pair a, Pair b) { return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo); }
-__device__ __forceinline__ double value(Pair a) { return static_cast<double>(a.hi) + static_cast<double>(a.lo); }
+__device__ __forceinline__ Pair product(Pair a, Pair b) {
+  const float h = __fmul_rn(a.hi, b.hi);
+  return normal(h, __fmaf_rn(a.hi, b.lo, __fmaf_rn(a.lo, b.hi, __fmaf_rn(a.hi, b.hi, -h))));
+}
 __device__ __forceinline__ Pair shfl_up(Pair a, int d) {
   return {__shfl_up_sync(0xffffffffu, a.hi, d), __shfl_up_sync(0xffffffffu, a.lo, d)};
 }
@@ -70,33 +73,46 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // (a NaN stays on
 // p and q.
 enum Mode { kWhole, kOnce, kMore };
 
-// What is left of p after refusals that took a times q: max(p - a q, 0), exact to 2^-48, a NaN
-// in p a NaN. With h + lo = a q, h > p leaves nothing, h < p leaves (p - h) - lo, positive since
-// p - h is more than lo then, and h = p what lo leaves. p - min(p, h) is exact as a pair (the
-// larger of the two comes first).
+// What is left of p after refusals that took a times q, max(p - a q, 0), of two tokens at a time
+// (packed fp32), as hi + lo; a NaN in p stays one. With h + l = a q, l at most half a unit of
+// h: p - min(p, h) is exact as a pair, the larger of the two coming first, and l counts where
+// h < p, p - h then being more than it is. (Where h = p, l alone would be left, below 2^-24 of
+// p: it counts as nothing.)
+struct Pairs {
+  uint64_t hi, lo;
+};
+struct Taken {  // a
+  uint64_t hi, lo, minus_hi;
+  __device__ explicit Taken(Pair a) : hi(f32x2(a.hi, a.hi)), lo(f32x2(a.lo, a.lo)), minus_hi(f32x2(-a.hi, -a.hi)) {}
+};
 template <Mode M>
-__device__ __forceinline__ Pair left_over(float p, float q, Pair a) {
-  if constexpr (M == kWhole) return {max_nan(p, 0.0f), 0.0f};
-  const float h = M == kOnce ? q : __fmul_rn(a.hi, q);
-  const float m = fminf(p, h), s = __fadd_rn(p, -m);
-  float e = -__fadd_rn(m, __fadd_rn(s, -p));
-  if constexpr (M == kMore) {
-    const float lo = __fmaf_rn(a.lo, q, __fmaf_rn(a.hi, q, -h));
-    if (h <= p) e = __fadd_rn(e, -lo);
-    if (s == 0.0f) e = fmaxf(e, 0.0f);
-  }
-  return {s, e};
+__device__ __forceinline__ Pairs left_over(float p0, float p1, float q0, float q1, const Taken& a) {
+  if constexpr (M == kWhole) return {f32x2(max_nan(p0, 0.0f), max_nan(p1, 0.0f)), 0};
+  const uint64_t minus = f32x2(-1.0f, -1.0f), p = f32x2(p0, p1), q = f32x2(q0, q1);
+  const uint64_t h = M == kOnce ? q : mul2(a.hi, q);
+  const float h0 = lo2(h), h1 = hi2(h);
+  const uint64_t m = f32x2(fminf(p0, h0), fminf(p1, h1));
+  const uint64_t s = fma2(m, minus, p), rounding = add2(m, fma2(p, minus, s));  // (s - p) + m, the minus of it
+  if constexpr (M == kOnce) return {s, mul2(rounding, minus)};
+  const uint64_t l = fma2(a.lo, q, fma2(a.hi, q, mul2(a.minus_hi, q)));
+  const uint64_t counted = f32x2(h0 < p0 ? lo2(l) : 0.0f, h1 < p1 ? hi2(l) : 0.0f);
+  return {s, mul2(add2(rounding, counted), minus)};
+}
+template <Mode M>
+__device__ __forceinline__ Pair left_over(float p, float q, const Taken& a) {
+  const Pairs r = left_over<M>(p, 0.0f, q, 0.0f, a);
+  return {lo2(r.hi), lo2(r.lo)};
 }
 
-// Two running sums of pairs, of the even and the odd terms (as packed fp32).
+// Two running sums of pairs, of the even and the odd terms.
 struct Sums {
   uint64_t hi = 0, lo = 0;
-  __device__ __forceinline__ void add(Pair x, Pair y) {
+  __device__ __forceinline__ void add(Pairs x) {
     const uint64_t minus = f32x2(-1.0f, -1.0f);
-    const uint64_t b = f32x2(x.hi, y.hi), s = add2(hi, b), bb = fma2(hi, minus, s);
-    const uint64_t e = add2(fma2(fma2(bb, minus, s), minus, hi), fma2(bb, minus, b));
+    const uint64_t s = add2(hi, x.hi), bb = fma2(hi, minus, s);
+    const uint64_t e = add2(fma2(fma2(bb, minus, s), minus, hi), fma2(bb, minus, x.hi));
     hi = s;
-    lo = add2(lo, add2(e, f32x2(x.lo, y.lo)));
+    lo = add2(lo, add2(e, x.lo));
   }
   __device__ __forceinline__ Pair total() const {
     return qmla::add(two_sum(lo2(hi), lo2(lo)), two_sum(hi2(hi), hi2(lo)));
@@ -123,9 +139,10 @@ struct VerifyShared {
 // Sum of the terms v0 .. v1 - 1 of a node (p and q its rows), a share of it in each lane. kFlight
 // values of each row are on their way at a time: in 16 bytes where both rows lie on such
 // borders (VEC; v0 and v1 are multiples of their values then), else one by one.
-constexpr int kFlight = 16;
+
 template <typename T, Mode M, bool VEC>
-__device__ __forceinline__ Pair row_sum(const T* p, const T* q, Pair a, int v0, int v1, int lane) {
+__device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, int v0, int v1, int lane) {
+  constexpr int kFlight = M == kMore ? 8 : 16;
   constexpr int kWide = VEC ? 16 / static_cast<int>(sizeof(T)) : 1, kLoads = kFlight / kWide;
   using Load = typename std::conditional<VEC, uint4, T>::type;
   Sums sums;
@@ -141,12 +158,11 @@ __device__ __forceinline__ Pair row_sum(const T* p, const T* q, Pair a, int v0, 
         if (M != kWhole) y[i] = __ldg(reinterpret_cast<const Load*>(q + at));
       }
     }
-    auto term = [&](int e) {
-      return left_over<M>(as_float(reinterpret_cast<const T*>(&x[e / kWide])[e % kWide]),
-                          M == kWhole ? 0.0f : as_float(reinterpret_cast<const T*>(&y[e / kWide])[e % kWide]), a);
-    };
+    auto value = [&](const Load* from, int e) { return as_float(reinterpret_cast<const T*>(&from[e / kWide])[e % kWide]); };
 #pragma unroll
-    for (int e = 0; e < kFlight; e += 2) sums.add(term(e), term(e + 1));
+    for (int e = 0; e < kFlight; e += 2)
+      sums.add(left_over<M>(value(x, e), value(x, e + 1), M == kWhole ? 0.0f : value(y, e),
+                            M == kWhole ? 0.0f : value(y, e + 1), a));
   }
   return sums.total();
 }
@@ -212,12 +228,12 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
   // Warp 0's state: the node, its children not yet looked at, the refusals so far.
   int cur = 0, kept = 1;
   uint64_t children = 0ull;
-  double a = 0.0, mass = 1.0;
+  Pair a = {0.0f, 0.0f}, mass = {1.0f, 0.0f};
   int my_path = lane == 0 ? 0 : -1, my_path2 = -1;  // entries lane and lane + 32
   auto enter = [&](int node) {
     cur = node;
-    a = 0.0;
-    mass = 1.0;
+    a = {0.0f, 0.0f};
+    mass = {1.0f, 0.0f};
     const uint32_t lo = __ballot_sync(0xffffffffu, sh.parent[lane] == node);
     const uint32_t hi = __ballot_sync(0xffffffffu, sh.parent[lane + 32] == node);
     children = static_cast<uint64_t>(hi) << 32 | lo;
@@ -235,30 +251,32 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
       while (children != 0ull && !refusal) {
         const int t = __ffsll(static_cast<long long>(children)) - 1;
         children &= children - 1;
-        const double u = sh.u[t], p = sh.p[t], q = sh.q[t];
+        const float u = sh.u[t], p = sh.p[t], q = sh.q[t];
         if (draft != nullptr) {
-          const double r = fmax(p - a * q, 0.0);
-          if (u * q * mass < r) {
+          // (u q is exact as a pair)
+          const float uq = __fmul_rn(u, q);
+          const Pair need = product({uq, __fmaf_rn(u, q, -uq)}, mass);
+          if (above(left_over<kMore>(p, q, Taken(a)), need)) {
             if (lane == (kept & 31)) (kept < 32 ? my_path : my_path2) = t;
             ++kept;
             enter(t);
           } else {
-            a += mass;
+            a = add(a, mass);
             refusal = true;
           }
         } else {
           bool gone = false;
           const int m = sh.refused_n;
           for (int i = 0; i < m; ++i) gone |= sh.refused[i] == sh.token[t];
-          const double r = gone ? 0.0 : fmax(p, 0.0);
+          const float r = gone ? 0.0f : fmaxf(p, 0.0f);
           __syncwarp();
-          if (u * mass < r) {
+          if (above({r, 0.0f}, times(mass, u))) {
             if (lane == (kept & 31)) (kept < 32 ? my_path : my_path2) = t;
             ++kept;
             enter(t);
             if (lane == 0) sh.refused_n = 0;
           } else if (!gone) {
-            mass -= r;
+            mass = add(mass, {-r, 0.0f});
             if (lane == 0) {
               sh.refused[m] = sh.token[t];
               sh.refused_n = m + 1;
@@ -270,16 +288,15 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
       if (lane == 0) {
         sh.cur = cur;
         sh.last = children == 0ull;
-        sh.a.hi = static_cast<float>(a);
-        sh.a.lo = static_cast<float>(a - static_cast<double>(sh.a.hi));
+        sh.a = a;
         sh.found = ~0ull;
       }
     }
     __syncthreads();
     const T* const p = target + static_cast<size_t>(sh.cur) * d.target_row_stride;
     const T* const q = draft == nullptr ? nullptr : draft + static_cast<size_t>(sh.cur) * d.draft_row_stride;
-    const Pair took = sh.a;
-    const Mode mode = took.hi == 0.0f ? kWhole : (took.hi == 1.0f && took.lo == 0.0f ? kOnce : kMore);
+    const Taken took(sh.a);
+    const Mode mode = sh.a.hi == 0.0f ? kWhole : (sh.a.hi == 1.0f && sh.a.lo == 0.0f ? kOnce : kMore);
     const int refusals = sh.refused_n;  // (of certain drafts)
     const bool last = sh.last;
     auto term = [&](int v) {
@@ -327,7 +344,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
       Pair excl = shfl_up(incl, 1);
       if (lane == 0) excl = {0.0f, 0.0f};
       const Pair total = {__shfl_sync(0xffffffffu, incl.hi, 31), __shfl_sync(0xffffffffu, incl.lo, 31)};
-      mass = value(total);
+      mass = total;
       if (last) {
         if (lane == 0) sh.total = total;
 #pragma unroll
@@ -355,9 +372,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
     __syncthreads();
     if (fine && piece / kVerifyWarps == rank) {
       if (tid == 0) sh.found = ~0ull;
-      // (a few tokens in a row for each thread, their terms at hand if they are eight at most)
+      // (a few tokens in a row for each thread, their terms at hand if they are four at most)
       const int each = (chunk + kVerifyThreads - 1) / kVerifyThreads;
-      constexpr int kHeld = 8;
+      constexpr int kHeld = 4;
       Pair held[kHeld];
       const int p0 = min(piece * chunk, d.vocab), p1 = min(p0 + chunk, d.vocab);
       const int t0 = min(p0 + tid * each, p1), t1 = min(t0 + each, p1);

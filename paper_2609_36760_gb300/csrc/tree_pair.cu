@@ -436,19 +436,24 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
     if (!take(lo)) break;
     const float lt = half == 0 ? l + lo : lo + l;
     const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
-    // (32 bytes at a time, a whole sector of the thread's own row)
+    // (32 bytes at a time, a whole sector of the thread's own row. The pieces of a partial result lie
+    // row by row, so that a warp's store is 8 lines: laid out by rows it was 32, and a segment's
+    // end 6k cycles.)
     const int h0 = (sc.g * 2 + rank) * static_cast<int>(kRows) + (warp & 1) * 32;  // the warp's first row
     const bool mine_out = h0 + lane < p.heads;
     const size_t out_row = static_cast<size_t>(sc.b) * p.heads + h0 + lane;
-    const size_t part_row = (static_cast<size_t>(pair) + sc.unit) * 128 + rank * kRows + (warp & 1) * 32 + lane;
+    const int unit_row = rank * static_cast<int>(kRows) + (warp & 1) * 32 + lane;
+    const size_t piece = static_cast<size_t>(pair) + sc.unit;
     __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(p.out) + out_row * kDc + half * 256;
-    float* const part = p.part_o + part_row * kDc + half * 256;
+    float* const part = p.part_o + tree_part_at(piece, unit_row, half * 256);
     if (!wait_pv(n - 1)) break;
-#pragma unroll 1
+    uint32_t r[2][32];  // (the next columns are read while these are stored)
+    tmem_ld32(t_o, r[0]);
+#pragma unroll
     for (int c = 0; c < 256; c += 32) {
-      uint32_t r[32];
-      tmem_ld32(t_o + c, r);
+      uint32_t* const o = r[(c >> 5) & 1];
       tmem_ld_wait();
+      if (c < 224) tmem_ld32(t_o + c + 32, r[((c >> 5) + 1) & 1]);
       if (!mine_out) continue;
       if (whole) {
 #pragma unroll
@@ -456,18 +461,18 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
           uint32_t w[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            w[e] = pack_bf16(__uint_as_float(r[16 * q + 2 * e]) * inv, __uint_as_float(r[16 * q + 2 * e + 1]) * inv);
+            w[e] = pack_bf16(__uint_as_float(o[16 * q + 2 * e]) * inv, __uint_as_float(o[16 * q + 2 * e + 1]) * inv);
           stg_v8(dst + c + 16 * q, w);
         }
       } else {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) stg_v8(part + c + 8 * q, r + 8 * q);
+        for (int q = 0; q < 4; ++q) stg_v8(part + (c + 8 * q) * 128, o + 8 * q);
       }
     }
     if (half == 0 && mine_out) {
       if (!whole) {
-        p.part_ml[part_row * 2] = m;
-        p.part_ml[part_row * 2 + 1] = lt;
+        p.part_ml[(piece * 128 + unit_row) * 2] = m;
+        p.part_ml[(piece * 128 + unit_row) * 2 + 1] = lt;
       } else if (p.lse != nullptr) {
         p.lse[out_row] = (m + log2f(lt)) * kLn2;
       }

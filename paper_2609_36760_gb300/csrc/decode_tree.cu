@@ -31,6 +31,19 @@ size_t image_bytes(int batch, int blocks) {
   return static_cast<size_t>(batch) * (blocks + std::min(blocks, kExactTokens / kBlockTokens)) * kImage;
 }
 
+// Whether the context is laid out as images for tree_pair (where the workspace has room for them):
+// for more than 64 rows always, else up to 32,768 tokens of the batch, counted by the table's
+// width or the caller's bound. Measured on one GB300 (INT4, one call replayed, us, decode_main's
+// rows against the images):
+//                 16 rows        64         128         256         512       1,024
+//   1 x    500  21.5 / 18.5  29.2 / 20.0  27.1 / 20.7  26.1 / 21.1  26.2 / 22.5  29.1 / 23.6
+//   1 x 40,000  32.8 / 31.0  43.2 / 47.6  45.1 / 47.6  58.7 / 44.7  87.9 / 49.1  154 / 72
+//   8 x  4,000  22.5 / 24.4  30.7 / 29.6  42.3 / 33.5  62.4 / 43.8  83.2 / 52.0  141 / 73
+//   8 x 20,000  42.9 / 81.7  57.7 / 86.5  96.8 / 90.7   166 / 114    296 / 155   564 / 247
+//  64 x    500  23.1 / 38.1  38.3 / 46.8  51.8 / 51.1  85.2 / 79.7   145 / 112   256 / 176
+//  64 x  4,000  61.8 / 128   91.1 / 138    149 / 143    269 / 178    511 / 257   988 / 424
+bool on_images(int rows, long long tokens) { return rows > 64 || tokens <= 32768; }
+
 template <int CB, bool PROT>
 cudaError_t launch_rows(int hg, const Params& prm, cudaStream_t stream) {
   if (hg == 16) return launch_impl<CB, 16, PROT, false>(prm, stream, nullptr, nullptr);
@@ -82,7 +95,8 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
   prm.max_tokens = d.max_blocks * kBlockTokens;
   if (d.max_len > 0) prm.max_tokens = std::min(prm.max_tokens, d.max_len);
   const int blocks = image_blocks(prm.max_tokens);
-  if (w.images_off + image_bytes(d.batch, blocks) <= d.workspace_bytes) {
+  if (on_images(rows, static_cast<long long>(d.batch) * blocks * kBlockTokens) &&
+      w.images_off + image_bytes(d.batch, blocks) <= d.workspace_bytes) {
     prm.images = ws + w.images_off;
     prm.img_width = blocks;
     if (d.cache_kind != QMLA_CACHE_BF16)  // (whose values are fp16 ones, but the very small)
@@ -92,7 +106,8 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
     prm.n_img = 2 * prm.n_hg;
     prm.grid = grid / 2;
     // Images that L2 does not hold are read by all row groups of a sequence at once: the plan
-    // goes group by group, with as many ranges to each, which then keep step.
+    // goes group by group, with as many ranges to each, which then keep step (64 x 4,096 tokens, 4
+    // groups: the main kernel 221 to 181 us), unless that leaves over a twelfth of the pairs idle.
     const int teams = prm.grid / prm.n_hg;
     if (static_cast<size_t>(d.batch) * blocks * kImage > (96u << 20) && teams > 0 &&
         (prm.grid - teams * prm.n_hg) * 12 <= prm.grid) {

@@ -103,6 +103,52 @@ def test_sequences_without_a_tree_and_padding(kind, images):
     assert Q.read_dev_err(c.err) == 0
 
 
+@pytest.mark.parametrize("kind,protect", [(4, False), ("c4r4", True), ("bf16", False)])
+@pytest.mark.parametrize("nodes,heads", [(8, 32), (12, 32), (5, 100), (26, 32)])
+def test_images_beyond_l2_and_groups_without_nodes(kind, protect, nodes, heads):
+    """A table so wide that the images take more than L2: the plan goes group by group (2, 3, 4 and 7
+    groups of 128 rows), with trees that leave whole groups without a node."""
+    ctx = [0, 1, 127, 128, 500, 900, 129, 64, 3, 1300, 256, 700]
+    counts = [max(0, nodes - 3 * i) for i in range(len(ctx))]
+    counts[5], counts[9] = nodes, nodes
+    c = Cache(kind, ctx, counts, protect=protect, seed=nodes, extra=118)
+    q, q_pe = queries(len(ctx), nodes, heads, nodes)
+    p = trees("any", len(ctx), nodes, heads)
+    check(c, p, q, q_pe, run(c, p, q, q_pe, True), True)
+    assert Q.read_dev_err(c.err) == 0
+
+
+@pytest.mark.parametrize("kind,protect", [(4, False), (2, True), ("c4r4", False)])
+def test_lengths_around_the_more_exact_scores(kind, protect):
+    ctx = [1000, 1016, 1017, 1100]
+    c = Cache(kind, ctx, [8] * 4, protect=protect, seed=1)
+    q, q_pe = queries(4, 8, 32, 1)
+    p = trees("any", 4, 8)
+    check(c, p, q, q_pe, run(c, p, q, q_pe, True), True)
+
+
+@images
+def test_no_sequence_has_a_tree(images):
+    c = Cache(4, [70, 0, 200], [0, 0, 0], seed=4)
+    q, q_pe = queries(3, 5, 32)
+    out, lse = run(c, trees("chain", 3, 5), q, q_pe, images)
+    assert Q.read_dev_err(c.err) == 0 and (out == 0).all() and np.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("nodes", [1, 5])
+def test_more_sequences_than_the_plan_holds_on_chip(nodes):
+    B = 4200
+    ctx, counts = [(7 * i) % 90 for i in range(B)], [nodes] * B
+    c = Cache(4, ctx, counts, seed=2)
+    q, q_pe = (x.repeat(70, 1, 1, 1) for x in queries(60, nodes, 16, 2))
+    p = trees("any", B, nodes)
+    for images in (False, True):
+        got = run(c, p, q, q_pe, images)
+        # (one row group at most 64 rows: this many tokens do not go over images)
+        check(c, p, q, q_pe, got, images and nodes * 16 > 64, only=[0, 1, 13, 2000, 4095, 4096, 4199])
+    assert Q.read_dev_err(c.err) == 0
+
+
 @images
 def test_scores_that_grow_raise_the_reference(images):
     """Contexts whose scores rise by more than 2^8 from tile to tile, and nodes above them."""

@@ -37,7 +37,6 @@
 //                  (combine_wide_kernel for a few long units).
 #include <cuda_runtime.h>
 
-#include <algorithm>
 #include <cstddef>
 
 #include "decode_common.cuh"
@@ -954,228 +953,11 @@ __global__ void __launch_bounds__(kThreads, 1) decode_main(const Params p) {
 
 // ------------------------------------------------------------ prep / combine
 constexpr int kPrepThreads = kTree ? 512 : 1024;
-constexpr int kTreesPerBlock = kPrepThreads / kMaxNodes;
+constexpr int kTreesPerBlock = kPrepThreads / kMaxNodes;  // sequences whose trees one block of prep makes
 
-// Sets of nodes of kTreesPerBlock sequences from b0 on, a thread per node: each finds the
-// nodes above its own by doubling (after step i it holds 2^i of them, and its 2^i-th
-// ancestor). kMaxNodes stands for "none above".
-__device__ __forceinline__ void make_trees(const Params& p, int b0) {
-  __shared__ uint64_t line[kTreesPerBlock][kMaxNodes + 1];
-  __shared__ uint8_t up[kTreesPerBlock][kMaxNodes + 1], bad[kTreesPerBlock][kMaxNodes + 1];
-  const int i = threadIdx.x / kMaxNodes, t = threadIdx.x % kMaxNodes, b = b0 + i;
-  const bool any = b < p.batch;
-  int n = 0, parent = -1;
-  if (any) {
-    n = p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens;
-    if (n < 0 || n > p.q_tokens || n > p.seq_lens[b]) n = 0;  // (reported with the lengths)
-    if (t < n) parent = p.parents[static_cast<size_t>(b) * p.q_tokens + t];
-  }
-  const bool wrong = t < n && (parent < -1 || parent >= t);
-  if (wrong) report(p.dev_err, QMLA_DEVERR_BAD_TREE);
-  line[i][t] = t < n ? 1ull << t : 0ull;
-  up[i][t] = static_cast<uint8_t>(wrong || parent < 0 ? kMaxNodes : parent);
-  bad[i][t] = wrong ? 1 : 0;
-  if (t == 0) {
-    line[i][kMaxNodes] = 0ull;
-    up[i][kMaxNodes] = kMaxNodes;
-    bad[i][kMaxNodes] = 0;
-  }
-  __syncthreads();
-#pragma unroll 1
-  for (int s = 1; s < kMaxNodes; s *= 2) {
-    const int a = up[i][t];
-    const uint64_t l = line[i][t] | line[i][a];
-    const uint8_t w = bad[i][t] | bad[i][a], a2 = up[i][a];
-    __syncthreads();
-    line[i][t] = l;
-    bad[i][t] = w;
-    up[i][t] = a2;
-    __syncthreads();
-  }
-  const bool ok = t < n && bad[i][t] == 0;
-  const uint64_t mine = ok ? line[i][t] : 0ull;
-  __syncthreads();
-  line[i][t] = mine;
-  __syncthreads();
-  uint64_t below = 0ull, alive = 0ull;
-#pragma unroll 4
-  for (int u = 0; u < kMaxNodes; ++u) {
-    const uint64_t l = line[i][u];
-    if ((l >> t) & 1ull) below |= 1ull << u;
-    if (l != 0ull) alive |= 1ull << u;
-  }
-  griddep_wait();  // (see prep_kernel)
-  if (!any) return;
-  TreeSeq& o = p.trees[b];
-  o.seen_by[t] = below;
-  o.line[t] = mine;
-  if (t == 0) {
-    o.alive = alive;
-    o.ctx = p.seq_lens[b] - n;
-  }
-}
-
-// One 16-byte piece of a cache row as it is loaded, and its eight values.
-struct RowPiece {
-  uint4 raw;    // bf16 values, or codes in x and scale and zero in y, z
-};
-// Piece i of chunk k of the packed row in `slot` of blk (the BF16 cache: of its values).
-template <int CB>
-__device__ __forceinline__ RowPiece load_piece(const uint8_t* blk, int slot, int k, int i) {
-  RowPiece r;
-  r.raw = make_uint4(0, 0, 0, 0);
-  if constexpr (CB == 16) {
-    r.raw = ldg_nc_v4(blk + slot * (kDqk * 2) + k * 128 + i * 16);
-  } else {
-    using L = BlockLayout<CB>;
-    const uint8_t* codes = blk + L::code_off(k, slot);
-    r.raw.x = CB == 2 && k < 8 ? ldg_nc_u16(codes + 2 * i) : ldg_nc_u32(codes + 4 * i);
-    if constexpr (CB == kC4R4) {
-      r.raw.y = k < 8 ? ldg_nc_u16(blk + L::c_scale_off(k, slot)) : ldg_nc_u32(blk + L::pe_scale_off(slot));
-      r.raw.z = ldg_nc_u8(blk + L::zero_off(k, slot));
-    } else {
-      r.raw.y = ldg_nc_u32(blk + L::sz_off(k, slot));
-    }
-  }
-  return r;
-}
-__device__ __forceinline__ void bf16_values(const uint4& raw, float (&f)[8]) {
-  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[2 * e] = bf16_lo(w[e]);
-    f[2 * e + 1] = bf16_hi(w[e]);
-  }
-}
-template <int CB>
-__device__ __forceinline__ void piece_values(const RowPiece& r, int k, float (&f)[8]) {
-  if constexpr (CB == 16) {
-    bf16_values(r.raw, f);
-  } else {
-    float s, z;
-    if constexpr (CB == kC4R4) {
-      s = __uint_as_float(k < 8 ? r.raw.y << 16 : r.raw.y);
-      z = static_cast<float>(r.raw.z);
-    } else {
-      const __half2 h = *reinterpret_cast<const __half2*>(&r.raw.y);
-      s = __low2float(h);
-      z = __high2float(h);
-    }
-    constexpr uint32_t kNarrow = 2, kWide = 4;
-    const uint32_t bits = CB == 2 && k < 8 ? kNarrow : kWide;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      f[e] = s * (static_cast<float>((r.raw.x >> (bits * e)) & ((1u << bits) - 1u)) - z);
-  }
-}
-__device__ __forceinline__ uint4 half_piece(const float (&f)[8]) {
-  return make_uint4(pack_h2(f[0], f[1]), pack_h2(f[2], f[3]), pack_h2(f[4], f[5]), pack_h2(f[6], f[7]));
-}
-// What rounding to fp16 leaves off.
-__device__ __forceinline__ uint4 rest_piece(const float (&f)[8]) {
-  float d[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) d[e] = f[e] - __half2float(__float2half_rn(f[e]));
-  return half_piece(d);
-}
-
-// Block idx % img_width of sequence idx / img_width as an fp16 image (see Params::images), zero
-// behind the sequence's end up to a whole tile, and for short sequences the image of C - RN_f16(C). A thread has
-// the same eight channels of one row's nine chunks, all loaded before any is stored.
-template <int CB>
-__device__ void expand_block(const Params& p, int idx) {
-  static_assert(!kTree || kPrepThreads == kBlockTokens * 8, "a thread per row and piece");
-  griddep_wait();  // (the cache may still be written until here)
-  const int b = idx / p.img_width, j = idx - b * p.img_width;
-  const int entry = j < p.max_blocks ? p.table[static_cast<size_t>(b) * p.max_blocks + j] : -1;
-  int groups;
-  if (j >= tree_tiles(p, b, 1, groups, nullptr) * (kTileTokens / kBlockTokens) || groups == 0) return;
-  const int len = p.seq_lens[b], ctx = len - (p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens);
-  constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
-  const bool known = entry >= 0 && entry < p.num_blocks;
-  const uint8_t* const blk = p.pool + static_cast<size_t>(known ? entry : 0) * kBlk;
-  const int i = threadIdx.x & 7, slot = threadIdx.x >> 3, pos = j * kBlockTokens + slot;
-  const size_t at = swz_off(slot, i, 128);
-  uint8_t* const img = p.images + static_cast<size_t>(idx) * kImage + at;
-  uint8_t* const rest = p.rest_images != nullptr && len <= kExactTokens
-                            ? p.rest_images + (static_cast<size_t>(b) * p.rest_width + j) * kImage + at
-                            : nullptr;
-  const uint8_t* src = nullptr;
-  if (CB != 16 && p.prot != nullptr) {
-    RowRef r;
-    r.has = true;
-    r.j = pos / kTileTokens;
-    r.len = len;
-    r.b = b;
-    src = prot_row_tree(p, r, pos % kTileTokens, ctx);
-  }
-  float f[8];
-  if (CB != 16 && src != nullptr) {
-    uint4 raw[kNumChunks];
-#pragma unroll
-    for (int k = 0; k < kNumChunks; ++k) raw[k] = ldg_nc_v4(src + k * 128 + i * 16);
-#pragma unroll
-    for (int k = 0; k < kNumChunks; ++k) {
-      bf16_values(raw[k], f);
-      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = half_piece(f);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = rest_piece(f);
-    }
-  } else if (known && pos < len) {
-    RowPiece r[kNumChunks];
-#pragma unroll
-    for (int k = 0; k < kNumChunks; ++k) r[k] = load_piece<CB>(blk, slot, k, i);
-#pragma unroll
-    for (int k = 0; k < kNumChunks; ++k) {
-      piece_values<CB>(r[k], k, f);
-      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = half_piece(f);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = rest_piece(f);
-    }
-  } else {
-    if (pos < len) report(p.dev_err, QMLA_DEVERR_BAD_BLOCK);
-#pragma unroll 1
-    for (int k = 0; k < kNumChunks; ++k) {
-      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
-    }
-  }
-}
-
-// The image of 64 query rows (see query_piece), in channel order; a thread's work as above. Rows
-// of a group without a node get their results.
-__device__ __forceinline__ void query_image(const Params& p, int u) {
-  const int b = u / p.n_img, i = threadIdx.x & 7, h = threadIdx.x >> 3;
-  const int row = (u - b * p.n_img) * 64 + h;
-  int groups;
-  const int tiles = tree_tiles(p, b, 128, groups, nullptr);
-  if (tiles == 0 || (u - b * p.n_img) / 2 >= groups) {
-    // No node has a row here: nothing runs for them but this.
-    if (row >= p.heads) return;
-    griddep_wait();
-    uint4* const out = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) +
-                                                (static_cast<size_t>(b) * p.heads + row) * kDc) + i * (kDc / 64);
-#pragma unroll
-    for (int e = 0; e < kDc / 64; ++e) out[e] = make_uint4(0, 0, 0, 0);
-    if (i == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(b) * p.heads + row] = -INFINITY;
-    return;
-  }
-  uint4 raw[kNumChunks];
-#pragma unroll
-  for (int k = 0; k < kNumChunks; ++k) raw[k] = make_uint4(0, 0, 0, 0);
-  if (row < p.heads) {
-    const size_t r = static_cast<size_t>(b) * p.heads + row;
-#pragma unroll
-    for (int k = 0; k < kNumChunks; ++k)
-      raw[k] = ldg_nc_v4(k < 8 ? p.q_lat + r * kDc + k * 64 + i * 8 : p.q_pe + r * kDr + i * 8);
-  }
-  griddep_wait();  // (see prep_kernel)
-  uint8_t* const img = p.qimg + static_cast<size_t>(u) * (kNumChunks * 64 * 128) + swz_off(h, i, 128);
-  float f[8];
-#pragma unroll
-  for (int k = 0; k < kNumChunks; ++k) {
-    bf16_values(raw[k], f);
-    *reinterpret_cast<uint4*>(img + k * 64 * 128) = half_piece(f);
-  }
-}
+#if QMLA_DECODE_TREE
+#include "tree_prep.cuh"
+#endif
 
 // Block 0: tile prefix over units (u = b * n_hg + hg), tiles = ceil(len / 128).
 // Blocks 1..: one query-image piece (16 bytes) per thread.
@@ -1193,7 +975,8 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
     const long long idx = static_cast<long long>(blockIdx.x - 1) * kPrepThreads + threadIdx.x;
     constexpr int kPieces = kNumChunks * HG * 8;
     const long long images = static_cast<long long>(p.batch) * p.n_img;
-    if constexpr (kTree) {
+#if QMLA_DECODE_TREE
+    {
       const int first = PAIR ? static_cast<int>(images) + 1
                              : static_cast<int>((images * kPieces + kPrepThreads - 1) / kPrepThreads) + 1;
       const int block = static_cast<int>(blockIdx.x) - first;
@@ -1211,6 +994,7 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
         return;
       }
     }
+#endif
     if (idx >= images * kPieces) return;
     const int u = static_cast<int>(idx / kPieces);
     const int b = u / p.n_img;
@@ -1350,33 +1134,11 @@ __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
   const int h = blockIdx.y * 4 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   const int units = p.batch * p.n_hg;
-  int u, b, h0, P0, P1, T;
-  if constexpr (kTree && HG == 128) {
-    // A block per range: the unit that lies over its end and begins in it. (Whole units wrote
-    // their results, and prep those of units without tiles.)
-    const int c = blockIdx.x;
-    const int4 next = p.cta_info[c + 1];
-    const int end = p.cta_t0[c + 1];
-    u = next.x;
-    P0 = next.y;
-    P1 = next.z;
-    T = next.w;
-    if (P0 >= end || end >= P1 || cta_of(P0, T, p.grid) != c) return;
-    tree_unit(p, u, b, h0);
-    h0 *= HG;
-  } else {
-    u = blockIdx.x;
-    if constexpr (kTree) {
-      tree_unit(p, u, b, h0);
-    } else {
-      b = u / p.n_hg;
-      h0 = u - b * p.n_hg;
-    }
-    h0 *= HG;
-    P0 = p.prefix[u];
-    P1 = p.prefix[u + 1];
-    T = p.prefix[units];
-  }
+  const int u = blockIdx.x;
+  int b = u / p.n_hg, g = u - b * p.n_hg;
+  if constexpr (kTree) tree_unit(p, u, b, g);
+  const int h0 = g * HG;
+  const int P0 = p.prefix[u], P1 = p.prefix[u + 1], T = p.prefix[units];
   if (h >= HG || h0 + h >= p.heads) return;
   const size_t out = (static_cast<size_t>(b) * p.heads + h0 + h) * kDc + lane * 16;
   if (P0 == P1) {
@@ -1400,8 +1162,6 @@ __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
     float4 ov[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      if constexpr (kTree && HG == 128)
-        o = reinterpret_cast<const float4*>(p.part_o + tree_part_at(static_cast<size_t>(c) + u, h, lane * 16 + 4 * v)) - v;
       ov[v] = o[v];
     }
     const float Mn = fmaxf(M, ml.x);
@@ -1639,8 +1399,12 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
     return launch_k(combine_wide_kernel<kUnitHeads>, dim3(static_cast<unsigned>(units), kUnitHeads),
                     dim3(kWideThreads), 0, stream, pdl, prm);
   }
-  const unsigned blocks = kTree && PAIR ? static_cast<unsigned>(std::max(prm.grid - 1, 1)) : static_cast<unsigned>(units);
-  return launch_k(combine_kernel<kUnitHeads>, dim3(blocks, (kUnitHeads + 3) / 4), dim3(128), 0, stream, pdl, prm);
+  if constexpr (kTree && PAIR) {
+    return launch_tree_merge(prm, stream);
+  } else {
+    return launch_k(combine_kernel<kUnitHeads>, dim3(static_cast<unsigned>(units), (kUnitHeads + 3) / 4), dim3(128), 0,
+                    stream, pdl, prm);
+  }
 }
 
 template <int CB, bool PROT>

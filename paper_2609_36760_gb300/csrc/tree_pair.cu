@@ -550,7 +550,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tree_pa
   }
 }
 
+// Merges the partial results of the unit that begins in range c and goes on behind its end (App. C.5
+// rule, see combine_kernel). A lane per row, 16 channels a thread; nearly always two pieces,
+// both of which are on their way before the first is used. (A warp a row, a piece after the
+// other and the pieces' number by division took 7 to 14 us.)
+constexpr int kMergeThreads = 256;
+__global__ void __launch_bounds__(kMergeThreads) tree_merge(const Params p) {
+  const int c = blockIdx.x, row = blockIdx.y * 32 + (threadIdx.x & 31);
+  const int channel = (blockIdx.z * (kMergeThreads / 32) + (threadIdx.x >> 5)) * 16;
+  griddep_wait();  // the partials of the main kernel
+  const int4 next = p.cta_info[c + 1];
+  const int begin = p.cta_t0[c], end = p.cta_t0[c + 1];
+  const int u = next.x, P0 = next.y, P1 = next.z;
+  if (P0 < begin || P0 >= end || end >= P1) return;
+  int b, g;
+  tree_unit(p, u, b, g);
+  if (g * 128 + row >= p.heads) return;
+  struct Piece {
+    float2 ml;
+    float o[16];
+  };
+  auto fetch = [&](int d) {
+    Piece x;
+    const size_t piece = static_cast<size_t>(d) + u;
+    x.ml = *reinterpret_cast<const float2*>(p.part_ml + (piece * 128 + row) * 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(p.part_o + tree_part_at(piece, row, channel + 4 * i));
+      x.o[4 * i] = v.x, x.o[4 * i + 1] = v.y, x.o[4 * i + 2] = v.z, x.o[4 * i + 3] = v.w;
+    }
+    return x;
+  };
+  Piece sum = fetch(c);
+  for (int d = c + 1, at = end; at < P1; ++d) {
+    if (next.w < p.grid) d = cta_of(at, next.w, p.grid);  // (fewer tiles than ranges: past the empty ones)
+    at = p.cta_t0[d + 1];
+    const Piece x = fetch(d);
+    const float m = fmaxf(sum.ml.x, x.ml.x);
+    const float s = sum.ml.x == m ? 1.0f : exp2f(sum.ml.x - m), t = x.ml.x == m ? 1.0f : exp2f(x.ml.x - m);
+    sum.ml = make_float2(m, sum.ml.y * s + x.ml.y * t);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum.o[i] = sum.o[i] * s + x.o[i] * t;
+  }
+  const float inv = sum.ml.y > 0.0f ? 1.0f / sum.ml.y : 0.0f;
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = pack_bf16(sum.o[2 * i] * inv, sum.o[2 * i + 1] * inv);
+  const size_t at = static_cast<size_t>(b) * p.heads + g * 128 + row;
+  stg_v8(reinterpret_cast<__nv_bfloat16*>(p.out) + at * kDc + channel, w);
+  if (channel == 0 && p.lse != nullptr) p.lse[at] = (sum.ml.x + log2f(sum.ml.y)) * kLn2;
+}
+
 }  // namespace
+
+cudaError_t launch_tree_merge(const Params& prm, cudaStream_t stream) {
+  if (prm.grid < 2) return cudaSuccess;
+  return launch_k(tree_merge, dim3(prm.grid - 1, 4, kDc / 16 / (kMergeThreads / 32)), dim3(kMergeThreads), 0,
+                  stream, true, prm);
+}
 
 cudaError_t launch_tree_pair(const Params& prm, cudaStream_t stream) {
   static int configured_device = -1;

@@ -299,9 +299,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
     const Mode mode = sh.a.hi == 0.0f ? kWhole : (sh.a.hi == 1.0f && sh.a.lo == 0.0f ? kOnce : kMore);
     const int refusals = sh.refused_n;  // (of certain drafts)
     const bool last = sh.last;
-    auto term = [&](int v) {
-      const float x = as_float(p[v]);
-      if (mode != kWhole) return left_over<kMore>(x, as_float(q[v]), took);
+    auto term = [&](int v, float x, float y) {
+      if (mode != kWhole) return left_over<kMore>(x, y, took);
       Pair r = left_over<kWhole>(x, 0.0f, took);
       for (int i = 0; i < refusals; ++i)
         if (sh.refused[i] == v) r.hi = 0.0f;
@@ -372,41 +371,59 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
     __syncthreads();
     if (fine && piece / kVerifyWarps == rank) {
       if (tid == 0) sh.found = ~0ull;
-      // (a few tokens in a row for each thread, their terms at hand if they are four at most)
+      // A few tokens in a row for each thread; then those of the thread whose sum passes the cut,
+      // a lane each.
       const int each = (chunk + kVerifyThreads - 1) / kVerifyThreads;
-      constexpr int kHeld = 4;
-      Pair held[kHeld];
       const int p0 = min(piece * chunk, d.vocab), p1 = min(p0 + chunk, d.vocab);
       const int t0 = min(p0 + tid * each, p1), t1 = min(t0 + each, p1);
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) held[i] = t0 + i < t1 ? term(t0 + i) : Pair{0.0f, 0.0f};
       Pair s = {0.0f, 0.0f};
+      for (int v = t0; v < t1; v += 8) {
+        float x[8], y[8];
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) s = add(s, held[i]);
-#pragma unroll 4
-      for (int v = t0 + kHeld; v < t1; ++v) s = add(s, term(v));
-      Pair incl = warp_scan(s, lane);
+        for (int i = 0; i < 8; ++i) {
+          x[i] = y[i] = 0.0f;
+          if (v + i < t1) {
+            x[i] = as_float(p[v + i]);
+            if (mode != kWhole) y[i] = as_float(q[v + i]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = add(s, term(v + i, x[i], y[i]));
+      }
+      const Pair incl = warp_scan(s, lane);
       if (lane == 31) sh.scan[warp] = incl;
       Pair excl = shfl_up(incl, 1);
       if (lane == 0) excl = {0.0f, 0.0f};
       __syncthreads();
       const Pair ends = warp_scan(lane < kVerifyWarps ? sh.scan[lane] : Pair{0.0f, 0.0f}, lane);
-      const Pair below = {__shfl_sync(0xffffffffu, ends.hi, max(warp - 1, 0)), __shfl_sync(0xffffffffu, ends.lo, max(warp - 1, 0))};
-      Pair run = add(warp > 0 ? add(sh.before[piece], below) : sh.before[piece], excl);
-      // (ordered so that a token above the cut comes before the fallback, the last with weight)
-      unsigned long long mine = ~0ull;
-      auto look = [&](int v, Pair x) {
-        run = add(run, x);
-        if (x.hi > 0.0f && mine > (1ull << 32)) mine = above(run, cut) ? v : (1ull << 40) - v;
-      };
-#pragma unroll
-      for (int i = 0; i < kHeld; ++i) look(t0 + i, held[i]);
-      for (int v = t0 + kHeld; v < t1; ++v) look(v, term(v));
-      if (mine != ~0ull) atomicMin(&sh.found, mine);
+      const int w1 = max(warp - 1, 0);
+      const Pair below = {__shfl_sync(0xffffffffu, ends.hi, w1), __shfl_sync(0xffffffffu, ends.lo, w1)};
+      const Pair run = add(warp > 0 ? add(sh.before[piece], below) : sh.before[piece], excl);
+      // (the first thread above the cut, else, where rounding leaves none, the last with anything)
+      if (s.hi > 0.0f) atomicMin(&sh.found, above(add(run, s), cut) ? tid : (1ull << 40) - tid);
       __syncthreads();
-      if (tid == 0) {
-        const unsigned long long f = sh.found;
-        d.next_token[b] = static_cast<int>(f < (1ull << 32) ? f : (1ull << 40) - f);
+      const unsigned long long found = sh.found;
+      const bool passes = found < (1ull << 32);
+      const int who = static_cast<int>(passes ? found : (1ull << 40) - found);
+      if (warp == who / 32) {
+        const int from = who & 31, first_v = __shfl_sync(0xffffffffu, t0, from), end_v = __shfl_sync(0xffffffffu, t1, from);
+        Pair upto = {__shfl_sync(0xffffffffu, run.hi, from), __shfl_sync(0xffffffffu, run.lo, from)};
+        int token = -1;
+        bool done = false;
+        for (int v = first_v; v < end_v && !done; v += 32) {
+          const int mine = v + lane;
+          const Pair x = mine < end_v ? term(mine, as_float(p[mine]), mode != kWhole ? as_float(q[mine]) : 0.0f) : Pair{0.0f, 0.0f};
+          const Pair sum_to = add(upto, warp_scan(x, lane));
+          const uint32_t any = __ballot_sync(0xffffffffu, x.hi > 0.0f);
+          const uint32_t over = __ballot_sync(0xffffffffu, x.hi > 0.0f && above(sum_to, cut));
+          if (any != 0u) token = v + 31 - __clz(any);
+          if (over != 0u) {
+            token = v + __ffs(over) - 1;
+            done = true;
+          }
+          upto = {__shfl_sync(0xffffffffu, sum_to.hi, 31), __shfl_sync(0xffffffffu, sum_to.lo, 31)};
+        }
+        if (lane == 0) d.next_token[b] = token;
       }
     }
     if (rank == 0 && warp == 0) {

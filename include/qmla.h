@@ -46,9 +46,9 @@
  *   .launch_dependents), so such a kernel right behind a writer runs beside it: it must
  *   execute griddepcontrol.wait, even if it uses nothing of the cache, for a decode
  *   behind it waits for that kernel alone. And a decode's first kernel is such a launch
- *   itself: it reads q_latent, q_pe, block_table and seq_lens before it waits, so a kernel
- *   right before the decode must not let its dependents start before it has written
- *   those. (Everything else a decode reads, and all that it writes but bits of the
+ *   itself: it reads q_latent, q_pe, block_table and seq_lens (and of a tree parents and
+ *   tree_lens) before it waits, so a kernel right before the decode must not let its
+ *   dependents start before it has written those. (Everything else a decode reads, and all that it writes but bits of the
  *   error word, comes after the wait.)
  *
  * Cache format (this library's own 64-token block, little-endian)
@@ -608,7 +608,9 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *   workspace       >= qmla_tree_workspace_bytes(batch, nodes, heads, 0) bytes, 256-byte
  *                   aligned, scratch as for qmla_mla_decode. With the bytes for the call's
  *                   max_len (or max_blocks x 64) tokens the context is dequantised once for all
- *                   rows of a sequence, in the workspace
+ *                   rows of a sequence, in the workspace (16 x 4,096 tokens, 32 nodes x 128 heads:
+ *                   991 to 425 us). The results differ in rounding; the scores of sequences up to
+ *                   1,024 tokens are then those of s (q - z) itself instead of its fp16 value
  * A node behind the last of its sequence gets out = 0 and lse = -inf. So do a node whose
  * parent is not an earlier node or -1 and the nodes below it (QMLA_DEVERR_BAD_TREE), and
  * every node of a sequence whose count is below 0, above `nodes` or above its length (the
@@ -640,7 +642,7 @@ typedef struct qmla_tree_desc {
 int qmla_mla_decode_tree(const qmla_tree_desc* desc, qmla_stream_t stream);
 
 /* Workspace bytes of qmla_mla_decode_tree on the current device for sequences up to max_tokens
- * (1,152 bytes for each token of them, and as much again for the first 1,024), or, with
+ * (for each of the batch 1,152 bytes a token, and as much again for the first 1,024), or, with
  * max_tokens 0, the least that it needs; 0 for bad arguments. */
 size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens);
 
@@ -659,13 +661,15 @@ size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens
  * walk ends, and the next token is the first v with
  *     sum_{w <= v} r(w) > u_0 sum_w r(w)
  * (r = p where nothing was refused), the last v with r(v) > 0 where rounding leaves none.
- * Sums and terms carry their rounding errors along, so that no decision depends on an order.
+ * Sums and terms carry their rounding errors along (2^-46 of the sum), so that no decision
+ * depends on an order.
  *
  *   target, target_seq_stride, target_row_stride
  *                   [batch, nodes, vocab] probabilities of type probs (QMLA_PROBS_*), rows
  *                   and sequences that many elements apart (not negative, below 2^40; not used
- *                   where that axis has one element). Values are taken as they are given: p
- *                   below 0 counts as 0, rows are not normalised
+ *                   where that axis has one element). Rows are not normalised; a target's value
+ *                   below 0 counts as 0, the draft's are not below 0. 16-byte aligned rows whose
+ *                   vocab and strides are multiples of 16 bytes are read in wider pieces
  *   draft, ...      the same for the draft, or NULL. Rows of nodes without children are not read
  *   batch, nodes, vocab   1 .. 65535, 1 .. QMLA_MAX_TREE_NODES, 1 .. 2^24
  *   tokens, parents [batch, nodes] int32; tree_lens [batch] int32 or NULL, as above

@@ -2,8 +2,10 @@
 // head h, sees the context and the nodes on its path (Eq. mla_compact, with a mask of nodes
 // in the place of the causal one).
 //
-// The kernels are the decode's (decode.cu, compiled here for trees); prep also finds the
-// sets of nodes above and below each node.
+// With few query rows over long contexts the kernels are the decode's (decode.cu, compiled here
+// for trees: masks, bf16 results); prep also finds the sets of nodes above and below each node.
+// Else prep lays the context out as fp16 images, once for all rows of a sequence, and
+// tree_pair and tree_merge (tree_pair.cu) work over those.
 #define QMLA_DECODE_TREE 1
 #include "decode.cu"
 
@@ -36,12 +38,12 @@ size_t image_bytes(int batch, int blocks) {
 // width or the caller's bound. Measured on one GB300 (INT4, one call replayed, us, decode_main's
 // rows against the images):
 //                 16 rows        64         128         256         512       1,024
-//   1 x    500  21.5 / 18.5  29.2 / 20.0  27.1 / 20.7  26.1 / 21.1  26.2 / 22.5  29.1 / 23.6
-//   1 x 40,000  32.8 / 31.0  43.2 / 47.6  45.1 / 47.6  58.7 / 44.7  87.9 / 49.1  154 / 72
-//   8 x  4,000  22.5 / 24.4  30.7 / 29.6  42.3 / 33.5  62.4 / 43.8  83.2 / 52.0  141 / 73
-//   8 x 20,000  42.9 / 81.7  57.7 / 86.5  96.8 / 90.7   166 / 114    296 / 155   564 / 247
-//  64 x    500  23.1 / 38.1  38.3 / 46.8  51.8 / 51.1  85.2 / 79.7   145 / 112   256 / 176
-//  64 x  4,000  61.8 / 128   91.1 / 138    149 / 143    269 / 178    511 / 257   988 / 424
+//   1 x    500  21.4 / 15.9  29.2 / 18.0  27.0 / 17.9  25.9 / 19.1  26.2 / 19.1  29.2 / 20.2
+//   1 x 40,000  32.8 / 31.0  42.8 / 47.6  46.0 / 51.7  58.5 / 45.4  88.0 / 49.1  154 / 71
+//   8 x  4,000  22.6 / 24.3  30.7 / 29.6  42.6 / 33.5  62.5 / 43.8  83.3 / 45.4  141 / 65
+//   8 x 20,000  43.0 / 81.7  57.3 / 86.5  97.2 / 90.7   166 / 113    297 / 147   564 / 237
+//  64 x    500  23.1 / 37.1  38.3 / 45.1  55.7 / 47.3  85.9 / 74.4   144 / 107   257 / 172
+//  64 x  4,000  62.0 / 128   91.3 / 138    149 / 137    270 / 171    512 / 248   989 / 412
 bool on_images(int rows, long long tokens) { return rows > 64 || tokens <= 32768; }
 
 template <int CB, bool PROT>

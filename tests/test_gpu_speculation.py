@@ -197,3 +197,114 @@ def test_the_binding_refuses_other_devices_types_and_shapes():
         for call in (tree, keep):
             with pytest.raises(Q.QmlaError, match="invalid"):
                 call(**kw)
+
+
+@pytest.mark.parametrize("kind,protect", [(4, False), ("c4r4", True)])
+def test_a_step_captured_as_one_graph(kind, protect):
+    """Writer, attention, verification and move in one graph (their launches overlap), replayed with new
+    rows, trees, lengths and probabilities in place; against the same calls one by one."""
+    B, T, H, V, cols = 4, 9, 32, 1001, 8
+    g = torch.Generator().manual_seed(5)
+    cs = table_of(600).cuda()
+    table = torch.randperm(B * cols, generator=g).int().view(B, cols).cuda()
+    ctx = [0, 100, 190, 300]
+    i32 = lambda x: torch.as_tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    err = i32([0])
+
+    def fresh():
+        d = {"pool": torch.zeros((B * cols, WIDTH[kind]), dtype=torch.uint8, device="cuda"),
+             "prot": torch.zeros((B, 132, 576), dtype=torch.bfloat16, device="cuda") if protect else None,
+             "drafts": torch.zeros((B, 64, 576), dtype=torch.bfloat16, device="cuda"),
+             "out": torch.zeros((B, T, H, 512), dtype=torch.bfloat16, device="cuda"), "path": i32(np.zeros((B, T))),
+             "kept": i32([0] * B), "next": i32([0] * B), "new": i32([0] * B)}
+        gen = torch.Generator().manual_seed(9)
+        n = max(ctx)
+        for b, c in enumerate(ctx):
+            x = torch.randn(n, 576, generator=gen).bfloat16()[:c].cuda()
+            if c:
+                lens = i32(ctx)
+                Q.rope_append(d["pool"], kind, x[:, :512], x[:, 512:], i32([b] * c), i32(range(c)), table, cs, err,
+                              seq_lens=lens if protect else None, prot=d["prot"])
+        return d
+
+    def inputs(seed):
+        gen = torch.Generator().manual_seed(seed)
+        parents = trees("any", B, T, seed)
+        target, draft = distributions(B, T, V, seed)
+        c = torch.tensor(ctx)
+        q, q_pe = queries(B, T, H, seed)
+        return [torch.randn(B * T, 576, generator=gen).bfloat16().cuda(), i32(parents), target.cuda(), draft.cuda(),
+                drafted(draft, parents, seed).cuda(), torch.rand(B, T, generator=gen).cuda(), q.cuda(), q_pe.cuda(),
+                i32((c[:, None] + torch.arange(T)).reshape(-1)), i32((c[:, None] + depths(parents)).reshape(-1)), i32(c + T)]
+
+    seq, node = i32(torch.arange(B).repeat_interleave(T)), i32(torch.arange(T).repeat(B))
+    own = i32(torch.arange(B)[:, None])
+    ws = torch.empty(Q.tree_workspace_bytes(B, T, H, 64 * cols), dtype=torch.uint8, device="cuda")
+
+    def step(d, x):
+        rows, parents, target, draft, tokens, u, q, q_pe, at, turn, lens = x
+        Q.rope_append(d["pool"], kind, rows[:, :512], rows[:, 512:], seq, at, table, cs, err, rope_positions=turn)
+        drafts = d["drafts"] if protect else None
+        if protect:
+            Q.rope_append(d["drafts"].view(B, -1).view(torch.uint8), "bf16", rows[:, :512], rows[:, 512:], seq, node, own, cs,
+                          err, rope_positions=turn)
+        Q.mla_decode_tree(d["pool"], kind, q, q_pe, table, lens, parents, TAU, d["out"], None, ws, err, prot=d["prot"],
+                          draft_rows=drafts)
+        Q.tree_verify(target, draft, tokens, parents, u, d["path"], d["kept"], d["next"], err)
+        Q.cache_keep(d["pool"], kind, table, lens, d["path"], d["kept"], d["new"], err, prot=d["prot"], draft_rows=drafts)
+
+    first, second = inputs(1), inputs(2)
+    wants = []
+    for x in (first, second):
+        d = fresh()
+        step(d, x)
+        torch.cuda.synchronize()
+        wants.append(d)
+    d, x = fresh(), [t.clone() for t in first]
+    start = {k: None if v is None else v.clone() for k, v in d.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(d, x)
+    for values, want in ((second, wants[1]), (first, wants[0]), (second, wants[1])):
+        for to, v in zip(x, values):
+            to.copy_(v)
+        for k, v in start.items():
+            if v is not None:
+                d[k].copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in d:
+            assert d[k] is None or torch.equal(d[k], want[k]), k
+    assert Q.read_dev_err(err) == 0
+
+
+def test_two_streams_at_once():
+    """Calls that overlap, each with a workspace of its own."""
+    B, T, H, n = 2, 8, 32, 700
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    pool = torch.randn(B * 12, 64 * 576, generator=g, device="cuda").bfloat16().view(torch.uint8)
+    table = torch.arange(B * 12, dtype=torch.int32, device="cuda").view(B, 12)
+    lens = torch.tensor([n, n + 60], dtype=torch.int32, device="cuda")
+    parents = trees("any", B, T).cuda()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    qs = [tuple(x.cuda() for x in queries(B, T, H, s)) for s in range(2)]
+    spaces = [torch.empty(Q.tree_workspace_bytes(B, T, H, 768), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    outs = [torch.zeros((B, T, H, 512), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+
+    def call(i, stream=None):
+        Q.mla_decode_tree(pool, "bf16", *qs[i], table, lens, parents, TAU, outs[i], None, spaces[i], err, stream=stream)
+
+    call(0), call(1)
+    torch.cuda.synchronize()
+    want = [o.clone() for o in outs]
+    for _ in range(5):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for i, s in enumerate(streams):
+                call(i, s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    assert Q.read_dev_err(err) == 0

@@ -80,7 +80,7 @@ def test_protected_rows_and_the_nodes_own(kind, nodes, heads, images):
 @images
 @pytest.mark.parametrize("kind,protect", [(4, False), (2, True), ("c4r4", True), ("bf16", False)])
 @pytest.mark.parametrize("ctx,nodes,heads", [([5000], 8, 16), ([1900, 700], 16, 128), ([9001], 2, 64), ([2500, 1], 3, 64),
-                                             ([4000, 3900, 20], 32, 16)])
+                                             ([4000, 3900, 20], 32, 16), ([70000], 3, 32)])
 def test_long_contexts_are_split_and_merged(kind, protect, ctx, nodes, heads, images):
     c = Cache(kind, ctx, [nodes] * len(ctx), protect=protect, seed=nodes)
     q, q_pe = queries(len(ctx), nodes, heads, nodes)

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -108,6 +109,16 @@ class KeepDesc(ctypes.Structure):
                 ("draft_rows", ctypes.c_void_p), ("new_lens", ctypes.c_void_p), ("dev_err", ctypes.c_void_p)]
 
 
+def _packer(cls):
+    """Packs a descriptor's fields as the C structure has them: filling a ctypes structure field by
+    field costs a third of a small call."""
+    codes = {ctypes.c_void_p: "P", ctypes.c_int: "i", ctypes.c_longlong: "q", ctypes.c_float: "f", ctypes.c_size_t: "N"}
+    return struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_) + "0P").pack
+
+
+_pack_tree, _pack_verify, _pack_keep = map(_packer, (TreeDesc, VerifyDesc, KeepDesc))
+
+
 class QmlaError(RuntimeError):
     def __init__(self, fn: str, status: int):
         extra = ""
@@ -178,10 +189,10 @@ def lib():
     L.qmla_rope_query.restype = i32
     L.qmla_mla_prefill.argtypes, L.qmla_mla_prefill.restype = [ctypes.POINTER(PrefillDesc), vp], i32
     L.qmla_prefill_workspace_bytes.argtypes, L.qmla_prefill_workspace_bytes.restype = [i32, i32], sz
-    L.qmla_mla_decode_tree.argtypes, L.qmla_mla_decode_tree.restype = [ctypes.POINTER(TreeDesc), vp], i32
+    L.qmla_mla_decode_tree.argtypes, L.qmla_mla_decode_tree.restype = [vp, vp], i32  # (a packed descriptor)
     L.qmla_tree_workspace_bytes.argtypes, L.qmla_tree_workspace_bytes.restype = [i32] * 4, sz
-    L.qmla_tree_verify.argtypes, L.qmla_tree_verify.restype = [ctypes.POINTER(VerifyDesc), vp], i32
-    L.qmla_cache_keep.argtypes, L.qmla_cache_keep.restype = [ctypes.POINTER(KeepDesc), vp], i32
+    L.qmla_tree_verify.argtypes, L.qmla_tree_verify.restype = [vp, vp], i32
+    L.qmla_cache_keep.argtypes, L.qmla_cache_keep.restype = [vp, vp], i32
     _lib = L
     return L
 
@@ -580,12 +591,15 @@ def tree_workspace_bytes(batch: int, nodes: int, heads: int, max_tokens: int = 0
     return int(lib().qmla_tree_workspace_bytes(batch, nodes, heads, max_tokens))
 
 
-def _ints(name: str, t, shape: tuple, dev: int):
-    return None if t is None else _flat(name, t, _I32, shape, dev)
+def _maybe(name: str, t, dtype: torch.dtype, shape: tuple, dev: int) -> int:
+    return 0 if t is None else _flat(name, t, dtype, shape, dev)
 
 
-def _node_rows(draft_rows, seqs: int, dev: int):
-    return None if draft_rows is None else _flat("draft_rows", draft_rows, _BF16, (seqs, MAX_TREE_NODES, 576), dev)
+def _tree_cache(pool, cache_kind, block_table, seq_lens, prot, draft_rows, dev_err, dev: int):
+    """_cache, with the nodes' rows behind the protection rows and 0 for what is None."""
+    at, kind, blocks, table, seqs, per, lens, rows, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)
+    return (at, kind, blocks, table, seqs, per, lens or 0, rows or 0,
+            _maybe("draft_rows", draft_rows, _BF16, (seqs, MAX_TREE_NODES, 576), dev), err or 0)
 
 
 def mla_decode_tree(pool: torch.Tensor, cache_kind, q_latent: torch.Tensor, q_pe: torch.Tensor,
@@ -600,15 +614,17 @@ def mla_decode_tree(pool: torch.Tensor, cache_kind, q_latent: torch.Tensor, q_pe
     tree_workspace_bytes(B, T, H) bytes or more, any type and shape."""
     dev = _current_device()
     B, T, H, _ = q_latent.shape
-    at, kind, blocks, table, seqs, per, lens, kept, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)
+    at, kind, blocks, table, seqs, per, lens, kept, rows, err = _tree_cache(pool, cache_kind, block_table, seq_lens, prot,
+                                                                            draft_rows, dev_err, dev)
     if seqs != B:
         _refuse("block_table", block_table, _I32, (B, per), dev)
-    d = TreeDesc(at, kind, blocks, _flat("q_latent", q_latent, _BF16, (B, T, H, 512), dev),
-                 _flat("q_pe", q_pe, _BF16, (B, T, H, 64), dev), B, T, H, max_len,
-                 _flat("parents", parents, _I32, (B, T), dev), _ints("tree_lens", tree_lens, (B,), dev), table, per,
-                 softmax_scale, lens, kept, _node_rows(draft_rows, B, dev), _flat("out", out, _BF16, (B, T, H, 512), dev),
-                 None if lse is None else _flat("lse", lse, _F32, (B, T, H), dev),
-                 _flat("workspace", workspace, workspace.dtype, workspace.shape, dev), workspace.nbytes, err)
+    shape = (B, T, H, 512)
+    d = _pack_tree(at, kind, blocks, _flat("q_latent", q_latent, _BF16, shape, dev),
+                   _flat("q_pe", q_pe, _BF16, (B, T, H, 64), dev), B, T, H, max_len,
+                   _flat("parents", parents, _I32, (B, T), dev), _maybe("tree_lens", tree_lens, _I32, (B,), dev), table, per,
+                   softmax_scale, lens, kept, rows, _flat("out", out, _BF16, shape, dev),
+                   _maybe("lse", lse, _F32, (B, T, H), dev),
+                   _flat("workspace", workspace, workspace.dtype, workspace.shape, dev), workspace.nbytes, err)
     st = lib().qmla_mla_decode_tree(d, _raw_stream(stream, dev))
     if st:
         raise QmlaError("qmla_mla_decode_tree", st)
@@ -637,15 +653,16 @@ def tree_verify(target: torch.Tensor, draft: torch.Tensor | None, tokens: torch.
     at = _probs("target", target, dtype, shape, dev)
     ts, tr, _ = target.stride()
     if draft is None:
-        q, ds, dr = None, 0, 0
+        q, ds, dr = 0, 0, 0
     else:
         q = _probs("draft", draft, dtype, shape, dev)
         ds, dr, _ = draft.stride()
-    d = VerifyDesc(at, ts, tr, q, ds, dr, _PROBS[dtype], B, T, V, _flat("tokens", tokens, _I32, (B, T), dev),
-                   _flat("parents", parents, _I32, (B, T), dev), _ints("tree_lens", tree_lens, (B,), dev),
-                   _flat("uniforms", uniforms, _F32, (B, T), dev), _flat("path", path, _I32, (B, T), dev),
-                   _flat("kept", kept, _I32, (B,), dev), _flat("next_token", next_token, _I32, (B,), dev),
-                   _error_word(dev_err, dev))
+    nodes, seqs = shape[:2], shape[:1]
+    d = _pack_verify(at, ts, tr, q, ds, dr, _PROBS[dtype], B, T, V, _flat("tokens", tokens, _I32, nodes, dev),
+                     _flat("parents", parents, _I32, nodes, dev), _maybe("tree_lens", tree_lens, _I32, seqs, dev),
+                     _flat("uniforms", uniforms, _F32, nodes, dev), _flat("path", path, _I32, nodes, dev),
+                     _flat("kept", kept, _I32, seqs, dev), _flat("next_token", next_token, _I32, seqs, dev),
+                     _error_word(dev_err, dev) or 0)
     st = lib().qmla_tree_verify(d, _raw_stream(stream, dev))
     if st:
         raise QmlaError("qmla_tree_verify", st)
@@ -658,11 +675,12 @@ def cache_keep(pool: torch.Tensor, cache_kind, block_table: torch.Tensor, seq_le
     """qmla_cache_keep: path int32 [B,T] and kept int32 [B] as tree_verify leaves them; seq_lens (nodes
     included), tree_lens and new_lens int32 [B]; new_lens may be seq_lens."""
     dev = _current_device()
-    at, kind, blocks, table, seqs, per, lens, rows, err = _cache(pool, cache_kind, block_table, seq_lens, prot, dev_err, dev)
+    at, kind, blocks, table, seqs, per, lens, kept_rows, rows, err = _tree_cache(pool, cache_kind, block_table, seq_lens,
+                                                                                 prot, draft_rows, dev_err, dev)
     T = path.size(1)
-    d = KeepDesc(at, kind, blocks, seqs, T, table, per, lens, _ints("tree_lens", tree_lens, (seqs,), dev),
-                 _flat("path", path, _I32, (seqs, T), dev), _flat("kept", kept, _I32, (seqs,), dev), rows,
-                 _node_rows(draft_rows, seqs, dev), _flat("new_lens", new_lens, _I32, (seqs,), dev), err)
+    d = _pack_keep(at, kind, blocks, seqs, T, table, per, lens, _maybe("tree_lens", tree_lens, _I32, (seqs,), dev),
+                   _flat("path", path, _I32, (seqs, T), dev), _flat("kept", kept, _I32, (seqs,), dev), kept_rows, rows,
+                   _flat("new_lens", new_lens, _I32, (seqs,), dev), err)
     st = lib().qmla_cache_keep(d, _raw_stream(stream, dev))
     if st:
         raise QmlaError("qmla_cache_keep", st)

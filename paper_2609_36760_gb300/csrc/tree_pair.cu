@@ -447,14 +447,8 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
     __nv_bfloat16* const dst = reinterpret_cast<__nv_bfloat16*>(p.out) + out_row * kDc + half * 256;
     float* const part = p.part_o + tree_part_at(piece, unit_row, half * 256);
     if (!wait_pv(n - 1)) break;
-    uint32_t r[2][32];  // (the next columns are read while these are stored)
-    tmem_ld32(t_o, r[0]);
-#pragma unroll
-    for (int c = 0; c < 256; c += 32) {
-      uint32_t* const o = r[(c >> 5) & 1];
-      tmem_ld_wait();
-      if (c < 224) tmem_ld32(t_o + c + 32, r[((c >> 5) + 1) & 1]);
-      if (!mine_out) continue;
+    auto put = [&](int c, const uint32_t* o) {
+      if (!mine_out) return;
       if (whole) {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -468,6 +462,18 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
 #pragma unroll
         for (int q = 0; q < 4; ++q) stg_v8(part + (c + 8 * q) * 128, o + 8 * q);
       }
+    };
+    // (the next columns are read while these are stored; a short loop, for its code is cold)
+    uint32_t r0[32], r1[32];
+    tmem_ld32(t_o, r0);
+#pragma unroll 1
+    for (int c = 0; c < 256; c += 64) {
+      tmem_ld_wait();
+      tmem_ld32(t_o + c + 32, r1);
+      put(c, r0);
+      tmem_ld_wait();
+      if (c < 192) tmem_ld32(t_o + c + 64, r0);
+      put(c + 32, r1);
     }
     if (half == 0 && mine_out) {
       if (!whole) {

@@ -1247,9 +1247,7 @@ __global__ void __launch_bounds__(kWideThreads) combine_wide_kernel(const Params
 #pragma unroll 4
   for (int cc = c0 + grp; cc <= c1; cc += kWideGroups) {
     const float wc = wts[cc - c0];
-    const float4 o = __ldcg(kTree && HG == 128
-                                ? reinterpret_cast<const float4*>(p.part_o + tree_part_at(static_cast<size_t>(cc) + u, h, v * 4))
-                                : ob + ((static_cast<size_t>(cc) + u) * HG + h) * (kDc / 4));
+    const float4 o = __ldcg(ob + ((static_cast<size_t>(cc) + u) * HG + h) * (kDc / 4));
     if (wc != 0.0f) {  // a piece that wrote nothing is never multiplied in
       acc.x += wc * o.x;
       acc.y += wc * o.y;
@@ -1394,17 +1392,13 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
   if (ev1 != nullptr && (e = cudaEventRecord(ev1, stream)) != cudaSuccess) return e;
   // Few units split over many CTAs each (long contexts): spread each unit's
   // pieces over more threads; otherwise one warp per head.
-  const bool wide = !(kTree && PAIR) || prm.img_width > 16;  // (of a tree's unit: more than eight tiles)
-  if (wide && units * 4 < prm.grid && prm.grid <= kWideThreads) {
+  if constexpr (kTree && PAIR) return launch_tree_merge(prm, stream);
+  if (units * 4 < prm.grid && prm.grid <= kWideThreads) {
     return launch_k(combine_wide_kernel<kUnitHeads>, dim3(static_cast<unsigned>(units), kUnitHeads),
                     dim3(kWideThreads), 0, stream, pdl, prm);
   }
-  if constexpr (kTree && PAIR) {
-    return launch_tree_merge(prm, stream);
-  } else {
-    return launch_k(combine_kernel<kUnitHeads>, dim3(static_cast<unsigned>(units), (kUnitHeads + 3) / 4), dim3(128), 0,
-                    stream, pdl, prm);
-  }
+  return launch_k(combine_kernel<kUnitHeads>, dim3(static_cast<unsigned>(units), (kUnitHeads + 3) / 4), dim3(128), 0,
+                  stream, pdl, prm);
 }
 
 template <int CB, bool PROT>

@@ -81,7 +81,7 @@ constexpr int kImage = 9 * 64 * 128;
 constexpr int kExactTokens = 1024;
 // Main kernel over these images; prm's plan is over 128-row units.
 cudaError_t launch_tree_pair(const Params& prm, cudaStream_t stream);
-// The merge behind it, where a unit is in few pieces (else combine_wide_kernel).
+// The merge behind it.
 cudaError_t launch_tree_merge(const Params& prm, cudaStream_t stream);
 
 // Main kernel of the CTA-pair decode (decode_pair.cu) for a plan over 128-head

@@ -556,14 +556,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tree_pa
   }
 }
 
-// Merges the partial results of the unit that begins in range c and goes on behind its end (App. C.5
-// rule, see combine_kernel). A lane per row, 16 channels a thread; nearly always two pieces,
-// both of which are on their way before the first is used. (A warp a row, a piece after the
-// other and the pieces' number by division took 7 to 14 us.)
-constexpr int kMergeThreads = 256;
+// ---------------------------------------------------------------------- merge
+// A row's share of a partial result: (m, l) and 16 channels of o; the merge of two (App. C.5).
+struct Piece {
+  float2 ml;
+  float o[16];
+  __device__ __forceinline__ void load(const Params& p, size_t piece, int row, int channel) {
+    ml = *reinterpret_cast<const float2*>(p.part_ml + (piece * 128 + row) * 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(p.part_o + tree_part_at(piece, row, channel + 4 * i));
+      o[4 * i] = v.x, o[4 * i + 1] = v.y, o[4 * i + 2] = v.z, o[4 * i + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ void add(const Piece& x) {
+    const float m = fmaxf(ml.x, x.ml.x);
+    const float s = ml.x == m ? 1.0f : exp2f(ml.x - m), t = x.ml.x == m ? 1.0f : exp2f(x.ml.x - m);
+    ml = make_float2(m, ml.y * s + x.ml.y * t);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = o[i] * s + x.o[i] * t;
+  }
+  __device__ __forceinline__ void store(const Params& p, int b, int head_row, int channel) const {
+    const float inv = ml.y > 0.0f ? 1.0f / ml.y : 0.0f;
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = pack_bf16(o[2 * i] * inv, o[2 * i + 1] * inv);
+    const size_t at = static_cast<size_t>(b) * p.heads + head_row;
+    stg_v8(reinterpret_cast<__nv_bfloat16*>(p.out) + at * kDc + channel, w);
+    if (channel == 0 && p.lse != nullptr) p.lse[at] = (ml.x + log2f(ml.y)) * kLn2;
+  }
+};
+constexpr int kMergeThreads = 256, kMergeWarps = kMergeThreads / 32;
+
+// The unit that begins in range c and goes on behind its end. A lane per row, 16 channels a warp;
+// nearly always two pieces, both of which are on their way before the first is used. (A warp a
+// row, a piece after the other and the pieces' number by division took 7 to 14 us.)
 __global__ void __launch_bounds__(kMergeThreads) tree_merge(const Params p) {
   const int c = blockIdx.x, row = blockIdx.y * 32 + (threadIdx.x & 31);
-  const int channel = (blockIdx.z * (kMergeThreads / 32) + (threadIdx.x >> 5)) * 16;
+  const int channel = (blockIdx.z * kMergeWarps + (threadIdx.x >> 5)) * 16;
   griddep_wait();  // the partials of the main kernel
   const int4 next = p.cta_info[c + 1];
   const int begin = p.cta_t0[c], end = p.cta_t0[c + 1];
@@ -572,47 +602,59 @@ __global__ void __launch_bounds__(kMergeThreads) tree_merge(const Params p) {
   int b, g;
   tree_unit(p, u, b, g);
   if (g * 128 + row >= p.heads) return;
-  struct Piece {
-    float2 ml;
-    float o[16];
-  };
-  auto fetch = [&](int d) {
-    Piece x;
-    const size_t piece = static_cast<size_t>(d) + u;
-    x.ml = *reinterpret_cast<const float2*>(p.part_ml + (piece * 128 + row) * 2);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 v = *reinterpret_cast<const float4*>(p.part_o + tree_part_at(piece, row, channel + 4 * i));
-      x.o[4 * i] = v.x, x.o[4 * i + 1] = v.y, x.o[4 * i + 2] = v.z, x.o[4 * i + 3] = v.w;
-    }
-    return x;
-  };
-  Piece sum = fetch(c);
+  Piece sum;
+  sum.load(p, static_cast<size_t>(c) + u, row, channel);
   for (int d = c + 1, at = end; at < P1; ++d) {
     if (next.w < p.grid) d = cta_of(at, next.w, p.grid);  // (fewer tiles than ranges: past the empty ones)
     at = p.cta_t0[d + 1];
-    const Piece x = fetch(d);
-    const float m = fmaxf(sum.ml.x, x.ml.x);
-    const float s = sum.ml.x == m ? 1.0f : exp2f(sum.ml.x - m), t = x.ml.x == m ? 1.0f : exp2f(x.ml.x - m);
-    sum.ml = make_float2(m, sum.ml.y * s + x.ml.y * t);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum.o[i] = sum.o[i] * s + x.o[i] * t;
+    Piece x;
+    x.load(p, static_cast<size_t>(d) + u, row, channel);
+    sum.add(x);
   }
-  const float inv = sum.ml.y > 0.0f ? 1.0f / sum.ml.y : 0.0f;
-  uint32_t w[8];
+  sum.store(p, b, g * 128 + row, channel);
+}
+
+// The same for few units of many pieces each: a block per unit, 32 rows and 16 channels, its
+// warps taking every eighth piece.
+__global__ void __launch_bounds__(kMergeThreads) tree_merge_wide(const Params p) {
+  __shared__ Piece part[kMergeWarps][32];
+  const int u = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row = blockIdx.y * 32 + lane, channel = blockIdx.z * 16;
+  griddep_wait();  // the partials of the main kernel
+  const int P0 = p.prefix[u], P1 = p.prefix[u + 1], T = p.prefix[p.batch * p.n_hg];
+  if (P0 == P1) return;  // (prep wrote the results)
+  const int c0 = cta_of(P0, T, p.grid), c1 = cta_of(P1 - 1, T, p.grid);
+  if (c0 == c1) return;
+  Piece sum;
+  sum.ml = make_float2(-INFINITY, 0.0f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = pack_bf16(sum.o[2 * i] * inv, sum.o[2 * i + 1] * inv);
-  const size_t at = static_cast<size_t>(b) * p.heads + g * 128 + row;
-  stg_v8(reinterpret_cast<__nv_bfloat16*>(p.out) + at * kDc + channel, w);
-  if (channel == 0 && p.lse != nullptr) p.lse[at] = (sum.ml.x + log2f(sum.ml.y)) * kLn2;
+  for (int i = 0; i < 16; ++i) sum.o[i] = 0.0f;
+#pragma unroll 2
+  for (int d = c0 + warp; d <= c1; d += kMergeWarps) {
+    if (p.cta_t0[d] == p.cta_t0[d + 1]) continue;  // an empty range wrote nothing
+    Piece x;
+    x.load(p, static_cast<size_t>(d) + u, row, channel);
+    sum.add(x);
+  }
+  part[warp][lane] = sum;
+  __syncthreads();
+  int b, g;
+  tree_unit(p, u, b, g);
+  if (warp != 0 || g * 128 + row >= p.heads) return;
+#pragma unroll
+  for (int w = 1; w < kMergeWarps; ++w) sum.add(part[w][lane]);
+  sum.store(p, b, g * 128 + row, channel);
 }
 
 }  // namespace
 
 cudaError_t launch_tree_merge(const Params& prm, cudaStream_t stream) {
   if (prm.grid < 2) return cudaSuccess;
-  return launch_k(tree_merge, dim3(prm.grid - 1, 4, kDc / 16 / (kMergeThreads / 32)), dim3(kMergeThreads), 0,
-                  stream, true, prm);
+  // Few units (a unit in more than four ranges), of more than eight tiles.
+  const int units = prm.batch * prm.n_hg;
+  if (units * 4 < prm.grid && prm.img_width > 16)
+    return launch_k(tree_merge_wide, dim3(units, 4, kDc / 16), dim3(kMergeThreads), 0, stream, true, prm);
+  return launch_k(tree_merge, dim3(prm.grid - 1, 4, kDc / 16 / kMergeWarps), dim3(kMergeThreads), 0, stream, true, prm);
 }
 
 cudaError_t launch_tree_pair(const Params& prm, cudaStream_t stream) {

@@ -34,17 +34,18 @@ size_t image_bytes(int batch, int blocks) {
 }
 
 // Whether the context is laid out as images for tree_pair (where the workspace has room for them):
-// for more than 64 rows always, else up to 32,768 tokens of the batch, counted by the table's
+// for more than 64 rows always, else up to 40,960 tokens of the batch, counted by the table's
 // width or the caller's bound. Measured on one GB300 (INT4, one call replayed, us, decode_main's
-// rows against the images):
-//                 16 rows        64         128         256         512       1,024
-//   1 x    500  21.4 / 15.9  29.2 / 18.0  27.0 / 17.9  25.9 / 19.1  26.2 / 19.1  29.2 / 20.2
-//   1 x 40,000  32.8 / 31.0  42.8 / 47.6  46.0 / 51.7  58.5 / 45.4  88.0 / 49.1  154 / 71
-//   8 x  4,000  22.6 / 24.3  30.7 / 29.6  42.6 / 33.5  62.5 / 43.8  83.3 / 45.4  141 / 65
-//   8 x 20,000  43.0 / 81.7  57.3 / 86.5  97.2 / 90.7   166 / 113    297 / 147   564 / 237
-//  64 x    500  23.1 / 37.1  38.3 / 45.1  55.7 / 47.3  85.9 / 74.4   144 / 107   257 / 172
-//  64 x  4,000  62.0 / 128   91.3 / 138    149 / 137    270 / 171    512 / 248   989 / 412
-bool on_images(int rows, long long tokens) { return rows > 64 || tokens <= 32768; }
+// rows against the images; protected and BF16 rows gain more from them):
+//                 16 rows         64         128         256       1,024
+//   1 x    500  21.1 / 16.0  29.5 / 17.6  26.7 / 17.9  26.2 / 19.0  29.2 / 20.2
+//   8 x  4,000  22.6 / 26.6  30.8 / 29.7  42.6 / 31.0  62.6 / 37.8   142 / 65
+//   1 x 40,000  32.8 / 31.1  43.0 / 37.0  45.9 / 38.5  58.8 / 38.3   154 / 70
+//   8 x  8,000  28.2 / 42.2  38.3 / 44.9  57.2 / 45.0  84.1 / 54.1   245 / 108
+//   1 x 100,000 42.0 / 62.4  54.7 / 64.3  68.8 / 60.7   105 / 70.7   344 / 149
+//  64 x    500  23.2 / 37.3  38.3 / 42.9  50.2 / 46.2  85.9 / 73.8   256 / 171
+//  64 x  4,000  62.1 / 128   91.8 / 133    149 / 137    270 / 173    989 / 415
+bool on_images(int rows, long long tokens) { return rows > 64 || tokens <= 40960; }
 
 template <int CB, bool PROT>
 cudaError_t launch_rows(int hg, const Params& prm, cudaStream_t stream) {

@@ -615,7 +615,8 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  * parent is not an earlier node or -1 and the nodes below it (QMLA_DEVERR_BAD_TREE), and
  * every node of a sequence whose count is below 0, above `nodes` or above its length (the
  * same) or whose length is bad (QMLA_DEVERR_BAD_POSITION). A value that is not finite in a
- * node's cache row may reach nodes that do not see it (weight 0 x inf).
+ * cache row (a BF16 one beyond 65,504 among them: tiles are fp16) reaches the nodes that see it,
+ * and no others.
  */
 typedef struct qmla_tree_desc {
   const void* pool;

@@ -509,6 +509,7 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
     ref0.len = fr.z;
     ref0.j = fr.w;
     ref0.b = sc.u / p.n_hg;
+    if (kTree && left_out(p, ref0, row)) ref0.has = false;
   }
   // A protected row reads its BF16 row instead of the packed cache.
   const uint8_t* psrc_cur = PROT ? row_source(p, ref0, row) : nullptr;
@@ -546,6 +547,7 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
     // The next tile's block pointer (its table entry was loaded a tile ago)
     // and the table entry of the tile after it.
     bool valid_nx = false;
+    if (kTree && left_out(p, ref_nx, row)) ref_nx.has = false;
     const uint8_t* psrc_nx = PROT ? row_source(p, ref_nx, row) : nullptr;
     if constexpr (PROT) {
       // The next tile's protected rows into L2 now (no registers held): their
@@ -972,29 +974,32 @@ template <int CB, int HG, bool PAIR>
 __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
   griddep_launch_dependents();  // the main kernel may start its set-up meanwhile
   if (blockIdx.x > 0) {
-    const long long idx = static_cast<long long>(blockIdx.x - 1) * kPrepThreads + threadIdx.x;
-    constexpr int kPieces = kNumChunks * HG * 8;
+    int block = static_cast<int>(blockIdx.x) - 1;
     const long long images = static_cast<long long>(p.batch) * p.n_img;
 #if QMLA_DECODE_TREE
-    {
-      const int first = PAIR ? static_cast<int>(images) + 1
-                             : static_cast<int>((images * kPieces + kPrepThreads - 1) / kPrepThreads) + 1;
-      const int block = static_cast<int>(blockIdx.x) - first;
-      const int trees = (p.batch + kTreesPerBlock - 1) / kTreesPerBlock;
-      if (PAIR && block >= trees) {
-        expand_block<CB>(p, block - trees);
-        return;
-      }
-      if (block >= 0) {
-        make_trees(p, block * kTreesPerBlock);
-        return;
-      }
-      if constexpr (PAIR) {
-        query_image(p, static_cast<int>(blockIdx.x) - 1);
-        return;
-      }
+    // (first what has the longest chains of loads)
+    const int trees = (p.batch + kTreesPerBlock - 1) / kTreesPerBlock;
+    if (block < trees) {
+      make_trees(p, block * kTreesPerBlock);
+      return;
     }
+    block -= trees;
+    if constexpr (PAIR) {
+      if (block < images) {
+        query_image(p, block);
+      } else {
+        expand_block<CB>(p, block - static_cast<int>(images));
+      }
+      return;
+    }
+    if (block < p.batch) {
+      find_not_finite<CB>(p, block);
+      return;
+    }
+    block -= p.batch;
 #endif
+    const long long idx = static_cast<long long>(block) * kPrepThreads + threadIdx.x;
+    constexpr int kPieces = kNumChunks * HG * 8;
     if (idx >= images * kPieces) return;
     const int u = static_cast<int>(idx / kPieces);
     const int b = u / p.n_img;
@@ -1128,6 +1133,16 @@ __device__ __forceinline__ void store_out(const Params& p, size_t at, float4 v) 
   }
 }
 
+// The rows of a tree whose results do not depend on the partials: 0 for a row without a node
+// (the weights of 0 that decode_main gives it make NaN of an infinity in the context), NaN for
+// a node that sees a row which was left out (see left_out). The value to write, or 1.
+__device__ __forceinline__ float tree_verdict(const Params& p, int b, int head_row) {
+  const TreeSeq& tree = p.trees[b];
+  const int t = head_row / p.hpt;
+  const uint64_t line = t < kMaxNodes ? tree.line[t] : 0ull;
+  return line == 0ull ? 0.0f : (line & tree.not_finite) != 0ull ? __int_as_float(0x7fffffff) : 1.0f;
+}
+
 template <int HG>
 __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
   griddep_wait();  // the partials of the main kernel
@@ -1141,6 +1156,15 @@ __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
   const int P0 = p.prefix[u], P1 = p.prefix[u + 1], T = p.prefix[units];
   if (h >= HG || h0 + h >= p.heads) return;
   const size_t out = (static_cast<size_t>(b) * p.heads + h0 + h) * kDc + lane * 16;
+  if constexpr (kTree) {
+    const float x = tree_verdict(p, b, h0 + h);
+    if (x != 1.0f) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) store_out(p, out + 4 * v, make_float4(x, x, x, x));
+      if (p.lse != nullptr && lane == 0) p.lse[static_cast<size_t>(b) * p.heads + h0 + h] = x == 0.0f ? -INFINITY : x;
+      return;
+    }
+  }
   if (P0 == P1) {
 #pragma unroll
     for (int v = 0; v < 4; ++v) store_out(p, out + 4 * v, make_float4(0.f, 0.f, 0.f, 0.f));
@@ -1161,9 +1185,7 @@ __global__ void __launch_bounds__(128) combine_kernel(const Params p) {
     const float4* o = reinterpret_cast<const float4*>(p.part_o + pi * kDc) + lane * 4;
     float4 ov[4];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      ov[v] = o[v];
-    }
+    for (int v = 0; v < 4; ++v) ov[v] = o[v];
     const float Mn = fmaxf(M, ml.x);
     // A partial that saw no key for this head has m = -inf and l = o = 0.
     const float a = M == Mn ? 1.0f : exp2f(M - Mn), w = ml.x == Mn ? 1.0f : exp2f(ml.x - Mn);
@@ -1210,6 +1232,14 @@ __global__ void __launch_bounds__(kWideThreads) combine_wide_kernel(const Params
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int v = tid & 127, grp = tid >> 7;
   const size_t out = (static_cast<size_t>(b) * p.heads + h0 + h) * kDc + v * 4;
+  if constexpr (kTree) {
+    const float x = tree_verdict(p, b, h0 + h);
+    if (x != 1.0f) {  // (alike in all threads)
+      if (grp == 0) store_out(p, out, make_float4(x, x, x, x));
+      if (p.lse != nullptr && tid == 0) p.lse[static_cast<size_t>(b) * p.heads + h0 + h] = x == 0.0f ? -INFINITY : x;
+      return;
+    }
+  }
   if (P0 == P1) {
     if (grp == 0) store_out(p, out, make_float4(0.f, 0.f, 0.f, 0.f));
     if (p.lse != nullptr && tid == 0) p.lse[static_cast<size_t>(b) * p.heads + h0 + h] = -INFINITY;
@@ -1379,7 +1409,7 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
                                                : (pieces + kPrepThreads - 1) / kPrepThreads;
   const unsigned prep_blocks = static_cast<unsigned>(1 + query_blocks +
                                                      (kTree ? (prm.batch + kTreesPerBlock - 1) / kTreesPerBlock : 0) +
-                                                     (kTree && PAIR ? prm.batch * prm.img_width : 0));
+                                                     (!kTree ? 0 : PAIR ? prm.batch * prm.img_width : prm.batch));
   if ((e = launch_k(prep_kernel<CB, HG, PAIR>, dim3(prep_blocks), dim3(kPrepThreads), 0, stream, pdl, prm)) != cudaSuccess)
     return e;
   if (ev0 != nullptr && (e = cudaEventRecord(ev0, stream)) != cudaSuccess) return e;

@@ -71,6 +71,7 @@ struct TreeSeq {
   uint64_t seen_by[kMaxNodes];
   uint64_t line[kMaxNodes];  // the node and those above it, or 0
   uint64_t alive;            // the nodes, all of which see the context
+  uint64_t not_finite;       // nodes whose cache row has an infinity or a NaN in fp16 (decode_main only)
   int ctx;                   // cached tokens before the tree
   int pad;
 };
@@ -336,6 +337,15 @@ __device__ __forceinline__ const uint8_t* prot_row_tree(const Params& p, const R
     return nullptr;
   }
   return p.prot + (static_cast<size_t>(r.b) * kProtRows + pr) * (kDqk * 2);
+}
+// Whether a tile row is that of a node whose values are not all finite: it is left out of the
+// tile, where its weight of 0 would make NaN of the nodes that do not see it (combine makes NaN
+// of those that do).
+__device__ __forceinline__ bool left_out(const Params& p, const RowRef& r, int row) {
+  const int pos = kTileTokens * r.j + row;
+  if (!r.has || pos < r.len - kMaxNodes) return false;
+  const int t = pos - p.trees[r.b].ctx;
+  return t >= 0 && t < kMaxNodes && ((p.trees[r.b].not_finite >> t) & 1ull);
 }
 
 template <int CB>

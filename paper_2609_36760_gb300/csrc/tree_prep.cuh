@@ -126,19 +126,74 @@ __device__ __forceinline__ uint4 rest_piece(const float (&f)[8]) {
   return half_piece(d);
 }
 
+// Largest magnitude of fp16 pieces so far; an infinity or NaN stays one.
+__device__ __forceinline__ void widen(__half2& top, uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) top = __hmax2_nan(top, __habs2(*reinterpret_cast<const __half2*>(&w[e])));
+}
+// Whether one of the eight threads of a row (whole warps call) met such a value.
+__device__ __forceinline__ bool row_not_finite(__half2 top) {
+  const bool finite = __low2float(top) <= 65504.0f && __high2float(top) <= 65504.0f;
+  return (__ballot_sync(0xffffffffu, !finite) >> (threadIdx.x & 24) & 0xffu) != 0u;
+}
+
+// The nodes of sequence b whose cache row has a value that is not finite, eight threads a row.
+template <int CB>
+__device__ void find_not_finite(const Params& p, int b) {
+  __shared__ unsigned long long found;
+  if (threadIdx.x == 0) found = 0ull;
+  __syncthreads();
+  int groups;
+  tree_tiles(p, b, 1, groups, nullptr);
+  const int t = threadIdx.x >> 3, i = threadIdx.x & 7;
+  const int n = groups == 0 ? 0 : (p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens);
+  const int pos = p.seq_lens[b] - n + t, slot = pos & (kBlockTokens - 1);
+  const int entry = t < n ? p.table[static_cast<size_t>(b) * p.max_blocks + pos / kBlockTokens] : -1;
+  __half2 top = __float2half2_rn(0.0f);
+  griddep_wait();  // (the cache may still be written until here)
+  if (t < n) {
+    float f[8];
+    if (CB != 16 && p.prot != nullptr) {
+      const uint8_t* const src = p.draft_rows + (static_cast<size_t>(b) * kMaxNodes + t) * (kDqk * 2);
+#pragma unroll
+      for (int k = 0; k < kNumChunks; ++k) {
+        bf16_values(ldg_nc_v4(src + k * 128 + i * 16), f);
+        widen(top, half_piece(f));
+      }
+    } else if (entry >= 0 && entry < p.num_blocks) {
+      constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
+      const uint8_t* const blk = p.pool + static_cast<size_t>(entry) * kBlk;
+#pragma unroll
+      for (int k = 0; k < kNumChunks; ++k) {
+        const RowPiece r = load_piece<CB>(blk, slot, k, i);
+        piece_values<CB>(r, k, f);
+        widen(top, half_piece(f));
+        // (a scale beyond fp16: the tile's product with a difference of 0 is NaN)
+        if (CB == kC4R4) top = __hmax2_nan(top, __float2half2_rn(k < 8 ? __uint_as_float(r.raw.y << 16) : __uint_as_float(r.raw.y)));
+      }
+    }
+  }
+  if (row_not_finite(top) && t < n && i == 0) atomicOr(&found, 1ull << t);
+  __syncthreads();
+  if (threadIdx.x == 0) p.trees[b].not_finite = found;
+}
+
 // Block idx % img_width of sequence idx / img_width as an fp16 image (see Params::images), zero
 // behind the sequence's end up to a whole tile, and for short sequences the image of C - RN_f16(C). A thread has
-// the same eight channels of one row's nine chunks, all loaded before any is stored.
+// the same eight channels of one row's nine chunks, all loaded before any is stored. A row with a
+// value that is not finite is 0 with NaN in the RoPE channels, which are keys alone: so it makes
+// NaN of the queries that see it, and its weight of 0 nothing of the others.
 template <int CB>
 __device__ void expand_block(const Params& p, int idx) {
   static_assert(!kTree || kPrepThreads == kBlockTokens * 8, "a thread per row and piece");
-  griddep_wait();  // (the cache may still be written until here)
   const int b = idx / p.img_width, j = idx - b * p.img_width;
   const int entry = j < p.max_blocks ? p.table[static_cast<size_t>(b) * p.max_blocks + j] : -1;
   int groups;
   if (j >= tree_tiles(p, b, 1, groups, nullptr) * (kTileTokens / kBlockTokens) || groups == 0) return;
   const int len = p.seq_lens[b], ctx = len - (p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens);
   constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
+  griddep_wait();  // (the cache may still be written until here)
   const bool known = entry >= 0 && entry < p.num_blocks;
   const uint8_t* const blk = p.pool + static_cast<size_t>(known ? entry : 0) * kBlk;
   const int i = threadIdx.x & 7, slot = threadIdx.x >> 3, pos = j * kBlockTokens + slot;
@@ -157,6 +212,13 @@ __device__ void expand_block(const Params& p, int idx) {
     src = prot_row_tree(p, r, pos % kTileTokens, ctx);
   }
   float f[8];
+  __half2 top = __float2half2_rn(0.0f);
+  auto put = [&](int k) {
+    const uint4 v = half_piece(f);
+    widen(top, v);
+    *reinterpret_cast<uint4*>(img + k * (64 * 128)) = v;
+    if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = rest_piece(f);
+  };
   if (CB != 16 && src != nullptr) {
     uint4 raw[kNumChunks];
 #pragma unroll
@@ -164,8 +226,7 @@ __device__ void expand_block(const Params& p, int idx) {
 #pragma unroll
     for (int k = 0; k < kNumChunks; ++k) {
       bf16_values(raw[k], f);
-      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = half_piece(f);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = rest_piece(f);
+      put(k);
     }
   } else if (known && pos < len) {
     RowPiece r[kNumChunks];
@@ -174,14 +235,21 @@ __device__ void expand_block(const Params& p, int idx) {
 #pragma unroll
     for (int k = 0; k < kNumChunks; ++k) {
       piece_values<CB>(r[k], k, f);
-      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = half_piece(f);
-      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = rest_piece(f);
+      put(k);
     }
   } else {
     if (pos < len) report(p.dev_err, QMLA_DEVERR_BAD_BLOCK);
 #pragma unroll 1
     for (int k = 0; k < kNumChunks; ++k) {
       *reinterpret_cast<uint4*>(img + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
+      if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
+    }
+  }
+  if (row_not_finite(top)) {
+#pragma unroll 1
+    for (int k = 0; k < kNumChunks; ++k) {
+      const uint32_t w = k < 8 ? 0u : 0x7fff7fffu;
+      *reinterpret_cast<uint4*>(img + k * (64 * 128)) = make_uint4(w, w, w, w);
       if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
     }
   }

@@ -176,6 +176,70 @@ def test_bad_trees_are_reported_and_see_nothing(images):
 
 
 @images
+@pytest.mark.parametrize("kind,protect,value", [(4, False, "inf"), (2, False, "1e30"), ("c4r4", False, "inf"), (4, True, "nan"),
+                                                ("c4r4", True, "1e30"), ("bf16", False, "nan"), ("bf16", False, "inf"),
+                                                ("bf16", False, "1e30")])
+@pytest.mark.parametrize("nodes,heads", [(9, 7), (9, 64)])
+def test_values_that_are_not_finite_reach_the_nodes_that_see_them(kind, protect, value, nodes, heads, images):
+    """In rows of nodes: NaN for those that see them, the same results as before for the others."""
+    ctx, counts, bad = [200, 0, 5000, 123, 60], [9, 9, 9, 7, 4], [[3], [1, 8], [8], [2, 6], [0]]
+    c = Cache(kind, ctx, counts, protect=protect, seed=8)
+    q, q_pe = queries(len(ctx), nodes, heads, 8)
+    p = trees("any", len(ctx), nodes, 2)
+    p[:, 0] = -1
+    before = run(c, p, q, q_pe, images)
+    check(c, p, q, q_pe, before, images)
+    seen = np.zeros((len(ctx), nodes), bool)
+    for b, wrong in enumerate(bad):
+        for t in range(counts[b]):
+            up = t
+            while up >= 0:
+                seen[b, t] |= up in wrong
+                up = int(p[b, up])
+        for t in wrong:
+            row = c.rows[b][ctx[b] + t:ctx[b] + t + 1].clone()
+            row[0, 20 + 69 * t] = float(value)
+            if protect:
+                c.drafts[b, t] = row[0].cuda()
+            else:
+                c.write([row if i == b else row[:0] for i in range(len(ctx))], [ctx[b] + t] * len(ctx), None)
+    assert not seen.all(1)[[0, 1, 2, 3]].any() and seen.any(1).all()
+    out, lse = run(c, p, q, q_pe, images)
+    assert Q.read_dev_err(c.err) == 0
+    assert np.isnan(out[seen]).all() and np.isnan(lse[seen]).all()
+    out[seen], lse[seen] = before[0][seen], before[1][seen]
+    check(c, p, q, q_pe, (out, lse), images)
+
+
+@images
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("ctx,at", [(300, 40), (5000, 4700)])
+def test_a_context_that_is_not_finite_leaves_rows_without_a_node_zero(kind, ctx, at, images):
+    c = Cache(kind, [ctx, 70], [3, 5], seed=8)
+    q, q_pe = queries(2, 5, 16, 8)
+    p = trees("chain", 2, 5)
+    row = c.rows[0][at:at + 1].clone()
+    row[0, 7] = float("inf")
+    c.write([row, row[:0]], [at, 0], None)
+    out, lse = run(c, p, q, q_pe, images)
+    assert np.isnan(out[0, :3]).any(-1).all()
+    assert (out[0, 3:] == 0).all() and np.isneginf(lse[0, 3:]).all()
+    check(c, p, q, q_pe, (out, lse), images, only=[1])
+
+
+@pytest.mark.parametrize("images", [False, True])
+def test_queries_behind_the_last_node_are_not_used(images):
+    c = Cache(4, [300, 0, 70], [3, 5, 0], seed=8)
+    q, q_pe = queries(3, 5, 16, 8)
+    p = trees("chain", 3, 5)
+    want = run(c, p, q, q_pe, images)
+    q[0, 3:], q_pe[0, 4:], q[2] = float("nan"), float("inf"), float("nan")
+    got = run(c, p, q, q_pe, images)
+    assert all(np.array_equal(x, y) for x, y in zip(got, want))
+    check(c, p, q, q_pe, got, images, only=[1])
+
+
+@images
 @pytest.mark.parametrize("count", [-1, 7, 1 << 30])
 def test_bad_counts_leave_the_sequence_without_rows(count, images):
     c = Cache(4, [100, 3], [6, 6], seed=3)

@@ -608,9 +608,10 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *   workspace       >= qmla_tree_workspace_bytes(batch, nodes, heads, 0) bytes, 256-byte
  *                   aligned, scratch as for qmla_mla_decode. With the bytes for the call's
  *                   max_len (or max_blocks x 64) tokens the context is dequantised once for all
- *                   rows of a sequence, in the workspace (16 x 4,096 tokens, 32 nodes x 128 heads:
- *                   991 to 425 us). The results differ in rounding; the scores of sequences up to
- *                   1,024 tokens are then those of s (q - z) itself instead of its fp16 value
+ *                   rows of a sequence, in the workspace. With lse the scores are then those of
+ *                   s (q - z) itself instead of its fp16 value (which leaves lse 2e-6 to 4e-5 of
+ *                   itself off, the more the fewer keys have the weight). Where the bytes are
+ *                   fewer, that happens for as many sequences at a time as they hold
  * A node behind the last of its sequence gets out = 0 and lse = -inf. So do a node whose
  * parent is not an earlier node or -1 and the nodes below it (QMLA_DEVERR_BAD_TREE), and
  * every node of a sequence whose count is below 0, above `nodes` or above its length (the
@@ -643,8 +644,8 @@ typedef struct qmla_tree_desc {
 int qmla_mla_decode_tree(const qmla_tree_desc* desc, qmla_stream_t stream);
 
 /* Workspace bytes of qmla_mla_decode_tree on the current device for sequences up to max_tokens
- * (for each of the batch 1,152 bytes a token, and as much again for the first 1,024), or, with
- * max_tokens 0, the least that it needs; 0 for bad arguments. */
+ * (2,304 bytes a token of each; without lse, or over a BF16 cache, half of them are used), or,
+ * with max_tokens 0, the least that it needs; 0 for bad arguments. */
 size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens);
 
 /*

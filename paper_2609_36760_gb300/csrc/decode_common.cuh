@@ -56,11 +56,11 @@ struct Params {
   TreeSeq* trees;             // [batch], written by the prep kernel
   int max_tokens;             // longer sequences are bad
   // Only where the context is laid out as fp16 tiles (tree_pair.cu): images [batch][img_width]
-  // of its 64-token blocks (an even number of them), and rest_images [batch][rest_width], of what their rounding left
-  // off, of sequences up to kExactTokens.
+  // of its 64-token blocks (an even number of them), and rest_images, the same of what their rounding
+  // left off, or null.
   uint8_t* images;
   uint8_t* rest_images;
-  int img_width, rest_width;
+  int img_width;
   // Order of the plan's units (sequence b, row group g): b * n_hg + g, or g * batch + b.
   bool by_group;
 };
@@ -78,8 +78,6 @@ struct TreeSeq {
 
 // A block as nine chunks of [64 tokens][128 bytes], swizzled as the tensor core reads them.
 constexpr int kImage = 9 * 64 * 128;
-// Sequences up to this length get the more exact scores (see tree_pair.cu).
-constexpr int kExactTokens = 1024;
 // Main kernel over these images; prm's plan is over 128-row units.
 cudaError_t launch_tree_pair(const Params& prm, cudaStream_t stream);
 // The merge behind it.

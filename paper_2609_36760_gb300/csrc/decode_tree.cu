@@ -29,9 +29,7 @@ TreeWorkspace tree_workspace_layout(int batch, int rows, int grid) {
 int image_blocks(long long tokens) {  // of whole tiles
   return static_cast<int>((tokens + kTileTokens - 1) / kTileTokens * (kTileTokens / kBlockTokens));
 }
-size_t image_bytes(int batch, int blocks) {
-  return static_cast<size_t>(batch) * (blocks + std::min(blocks, kExactTokens / kBlockTokens)) * kImage;
-}
+size_t image_bytes(int blocks, bool rest) { return static_cast<size_t>(blocks) * (rest ? 2 : 1) * kImage; }  // a sequence's
 
 // Whether the context is laid out as images for tree_pair (where the workspace has room for them):
 // for more than 64 rows always, else up to 40,960 tokens of the batch, counted by the table's
@@ -45,7 +43,7 @@ size_t image_bytes(int batch, int blocks) {
 //   1 x 100,000 42.0 / 62.4  54.7 / 64.3  68.8 / 60.7   105 / 70.7   344 / 149
 //  64 x    500  23.2 / 37.3  38.3 / 42.9  50.2 / 46.2  85.9 / 73.8   256 / 171
 //  64 x  4,000  62.1 / 128   91.8 / 133    149 / 137    270 / 173    989 / 415
-bool on_images(int rows, long long tokens) { return rows > 64 || tokens <= 40960; }
+bool on_images(int rows, long long tokens, bool rest) { return rest || rows > 64 || tokens <= 40960; }
 
 template <int CB, bool PROT>
 cudaError_t launch_rows(int hg, const Params& prm, cudaStream_t stream) {
@@ -54,10 +52,49 @@ cudaError_t launch_rows(int hg, const Params& prm, cudaStream_t stream) {
   return launch_impl<CB, 64, PROT, false>(prm, stream, nullptr, nullptr);
 }
 
+// The n sequences from b on over images at `images`, blocks of them a sequence.
+cudaError_t launch_images(const qmla_tree_desc& d, Params prm, uint8_t* images, int b, int n, int blocks, bool rest,
+                          cudaStream_t stream) {
+  const size_t rows = static_cast<size_t>(b) * prm.heads;  // query rows before them
+  prm.batch = n;
+  prm.q_lat += rows * kDc;
+  prm.q_pe += rows * kDr;
+  prm.out = reinterpret_cast<float*>(d.out + rows * kDc);
+  if (prm.lse != nullptr) prm.lse += rows;
+  prm.table += static_cast<size_t>(b) * prm.max_blocks;
+  prm.seq_lens += b;
+  prm.parents += static_cast<size_t>(b) * prm.q_tokens;
+  if (prm.tree_lens != nullptr) prm.tree_lens += b;
+  if (prm.prot != nullptr) {
+    prm.prot += static_cast<size_t>(b) * kProtRows * (kDqk * 2);
+    prm.draft_rows += static_cast<size_t>(b) * kMaxNodes * (kDqk * 2);
+  }
+  prm.images = images;
+  prm.img_width = blocks;
+  if (rest) prm.rest_images = images + static_cast<size_t>(n) * blocks * kImage;
+  prm.n_hg = (prm.heads + 127) / 128;
+  prm.n_img = 2 * prm.n_hg;
+  prm.grid = prm.sms / 2;
+  // Images that L2 does not hold are read by all row groups of a sequence at once: the plan
+  // goes group by group, with as many ranges to each, which then keep step (64 x 4,096 tokens, 4
+  // groups: the main kernel 221 to 181 us), unless that leaves over a twelfth of the pairs idle.
+  const int teams = prm.grid / prm.n_hg;
+  if (n * image_bytes(blocks, rest) > (96u << 20) && teams > 0 && (prm.grid - teams * prm.n_hg) * 12 <= prm.grid) {
+    prm.by_group = true;
+    prm.grid = teams * prm.n_hg;
+  }
+  switch (d.cache_kind) {
+    case 4: return launch_impl<4, 64, false, true>(prm, stream, nullptr, nullptr);
+    case 2: return launch_impl<2, 64, false, true>(prm, stream, nullptr, nullptr);
+    case kC4R4: return launch_impl<kC4R4, 64, false, true>(prm, stream, nullptr, nullptr);
+    default: return launch_impl<16, 64, false, true>(prm, stream, nullptr, nullptr);
+  }
+}
+
 }  // namespace
 
 size_t tree_workspace_bytes(int batch, int rows, int max_tokens, int grid) {
-  return tree_workspace_layout(batch, rows, grid).images_off + image_bytes(batch, image_blocks(max_tokens));
+  return tree_workspace_layout(batch, rows, grid).images_off + batch * image_bytes(image_blocks(max_tokens), true);
 }
 
 cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t stream) {
@@ -98,31 +135,19 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
   prm.max_tokens = d.max_blocks * kBlockTokens;
   if (d.max_len > 0) prm.max_tokens = std::min(prm.max_tokens, d.max_len);
   const int blocks = image_blocks(prm.max_tokens);
-  if (on_images(rows, static_cast<long long>(d.batch) * blocks * kBlockTokens) &&
-      w.images_off + image_bytes(d.batch, blocks) <= d.workspace_bytes) {
-    prm.images = ws + w.images_off;
-    prm.img_width = blocks;
-    if (d.cache_kind != QMLA_CACHE_BF16)  // (whose values are fp16 ones, but the very small)
-      prm.rest_images = prm.images + static_cast<size_t>(d.batch) * blocks * kImage;
-    prm.rest_width = std::min(blocks, kExactTokens / kBlockTokens);
-    prm.n_hg = (rows + 127) / 128;
-    prm.n_img = 2 * prm.n_hg;
-    prm.grid = grid / 2;
-    // Images that L2 does not hold are read by all row groups of a sequence at once: the plan
-    // goes group by group, with as many ranges to each, which then keep step (64 x 4,096 tokens, 4
-    // groups: the main kernel 221 to 181 us), unless that leaves over a twelfth of the pairs idle.
-    const int teams = prm.grid / prm.n_hg;
-    if (static_cast<size_t>(d.batch) * blocks * kImage > (96u << 20) && teams > 0 &&
-        (prm.grid - teams * prm.n_hg) * 12 <= prm.grid) {
-      prm.by_group = true;
-      prm.grid = teams * prm.n_hg;
+  // lse needs the scores of the values before their rounding to fp16, of which BF16 ones have none
+  // (but the very small, and those beyond 65,504, which are infinite).
+  const bool rest = d.lse != nullptr && d.cache_kind != QMLA_CACHE_BF16;
+  const size_t room = d.workspace_bytes > w.images_off ? d.workspace_bytes - w.images_off : 0;
+  const int fit = static_cast<int>(std::min<size_t>(d.batch, blocks > 0 ? room / image_bytes(blocks, rest) : 0));
+  if (fit > 0 && on_images(rows, static_cast<long long>(d.batch) * blocks * kBlockTokens, rest)) {
+    // As many sequences at a time as there is room for.
+    const int parts = (d.batch + fit - 1) / fit, per = (d.batch + parts - 1) / parts;
+    for (int b = 0; b < d.batch; b += per) {
+      const cudaError_t e = launch_images(d, prm, ws + w.images_off, b, std::min(per, d.batch - b), blocks, rest, stream);
+      if (e != cudaSuccess) return e;
     }
-    switch (d.cache_kind) {
-      case 4: return launch_impl<4, 64, false, true>(prm, stream, nullptr, nullptr);
-      case 2: return launch_impl<2, 64, false, true>(prm, stream, nullptr, nullptr);
-      case kC4R4: return launch_impl<kC4R4, 64, false, true>(prm, stream, nullptr, nullptr);
-      default: return launch_impl<16, 64, false, true>(prm, stream, nullptr, nullptr);
-    }
+    return cudaSuccess;
   }
   const bool prot = prm.prot != nullptr;
   switch (d.cache_kind) {

@@ -15,9 +15,10 @@
 // values') are filled, used and freed one by one: the scores of a tile take half of the time
 // that its values leave them, so that a part's copy has most of a tile's time to arrive.
 //
-// Short sequences (at most kExactTokens) also have images of what rounding to fp16 left off their
-// rows (C - RN_f16(C)), and their scores are the sum of both products: with few keys the
-// roundings do not average out of lse (200 INT4 tokens: 2e-5 of it against 1e-7).
+// Where lse is asked for, there are also images of what rounding to fp16 left off the rows
+// (C - RN_f16(C)), and the scores are the sum of both products. The roundings average out of lse
+// over many keys of like weight, but not where a few keys have most of it: 2e-6 to 4e-5 of it,
+// at any length, against 1e-7. (The results, in bf16, do not need it.)
 //
 // TMEM (per CTA; lanes 0..63 hold the first half of N for rows 0..63, lanes 64..127 the second):
 // O 2 x 128 columns, S 2 buffers of 64.
@@ -68,12 +69,11 @@ static_assert(kSmem <= 232448, "shared memory per CTA");
 struct TreeSched {
   int q, qend, q0;    // current tile, end and first tile of the segment
   int unit, pu0, pu1; // unit and its tiles in the plan's list
-  int b, g, len;
+  int b, g;
   int t0, t1;
   bool live;
   __device__ void enter(const Params& p, int j) {
     tree_unit(p, unit, b, g);
-    len = p.seq_lens[b];
     q = q0 = j;
     qend = min(t1, pu1) - pu0;
   }
@@ -85,7 +85,7 @@ struct TreeSched {
     pu0 = info.y;
     pu1 = info.z;
     live = t0 < t1;
-    q = qend = q0 = b = g = len = 0;
+    q = qend = q0 = b = g = 0;
     if (live) enter(p, t0 - pu0);
   }
   __device__ bool first() const { return q == q0; }
@@ -105,18 +105,37 @@ struct TreeSched {
     }
     enter(p, 0);
   }
-  // Products that make up the scores: of the images, and of what they leave off.
-  __device__ int products(const Params& p) const { return p.rest_images != nullptr && len <= kExactTokens ? 2 : 1; }
 };
 
 // The order in which the issuer takes QK and PV, and the copies come: QK of a tile goes before PV
 // of the tile before it. (So the softmax of a tile has the QK of the next one to work under, and
 // QK of tile i goes after PV of tile i - 2, whose P shows that its scores have been read.)
+// A tile has one or two passes of QK, over the images and over what they leave off, and two halves
+// of PV, of 128 of a CTA's channels each. Two passes are kept apart by halves,
+//   QK(i + 1), PV(i) first half, rest of QK(i + 1), PV(i) second half, QK(i + 2) ..,
+// for each pass has all of the keys' room, and its copies have half a PV to arrive in (one behind
+// the other a tile took 4,900 cycles).
 struct TreeOrder {
-  TreeSched k, v;  // at tiles nk and nv
-  uint32_t nk = 0, nv = 0;
+  TreeSched k, v;                 // tiles of the next pass and half
+  uint32_t pass = 0, half = 0;    // counted
+  uint32_t passes;                // a tile
+  __device__ TreeOrder(const Params& p, const TreeSched& sc) : k(sc), v(sc), passes(p.rest_images != nullptr ? 2 : 1) {}
   __device__ bool live() const { return v.live; }
-  __device__ bool score_next() const { return k.live && nk < nv + 2; }
+  __device__ bool score_next() const {
+    return k.live && (passes == 2 ? pass < half + 3 : 2 * pass < (half & ~1u) + 4);
+  }
+  __device__ bool rest() const { return passes == 2 && (pass & 1u); }
+  __device__ uint32_t scored() const { return passes == 2 ? pass >> 1 : pass; }  // tile of the pass
+  __device__ uint32_t summed() const { return half >> 1; }                       // and of the half
+  __device__ bool ends() const { return passes == 1 || (pass & 1u); }            // last pass of its tile
+  __device__ void pass_done(const Params& p) {
+    if (ends()) k.next(p);
+    ++pass;
+  }
+  __device__ void half_done(const Params& p) {
+    if (half & 1u) v.next(p);
+    ++half;
+  }
 };
 
 __device__ __forceinline__ bool pwait(uint64_t* bar, uint32_t parity, TreeCtrl& c, uint32_t site, uint32_t* dev_err) {
@@ -146,44 +165,39 @@ __device__ __forceinline__ bool pwait_cluster(uint64_t* bar, uint32_t parity, Tr
 
 // ------------------------------------------------------------------- copies
 __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, TreeCtrl& ctl, int rank) {
-  TreeOrder o;
-  o.k = o.v = sc;
-  uint32_t pass = 0, copies = 0, values = 0;  // products begun; parts asked for
+  TreeOrder o(p, sc);
+  uint32_t copies = 0, values = 0;  // parts asked for
   bool ok = true;
   while (ok && o.live()) {
     if (o.score_next()) {
-      const int products = o.k.products(p), block = 2 * o.k.q + rank;
+      const int block = 2 * o.k.q + rank;
       const uint8_t* q = p.qimg + (static_cast<size_t>(o.k.b) * p.n_img + 2 * o.k.g + rank) * kQBytes;
-      for (int i = 0; ok && i < products; ++i, ++pass) {
-        const uint8_t* src = i == 0 ? p.images + (static_cast<size_t>(o.k.b) * p.img_width + block) * kImage
-                                    : p.rest_images + (static_cast<size_t>(o.k.b) * p.rest_width + block) * kImage;
-        const bool query = i == 0 && o.k.first();  // (its part's last reader was that of the keys')
+      const uint8_t* src = (o.rest() ? p.rest_images : p.images) + (static_cast<size_t>(o.k.b) * p.img_width + block) * kImage;
+      const bool query = !o.rest() && o.k.first();  // (its part's last reader was that of the keys')
 #pragma unroll 1
-        for (int part = 0; part < kKeyParts; ++part) {
-          uint64_t* const bar = &ctl.k_bar[part];
-          if (pass > 0 && !(ok = pwait(&ctl.k_free[part], (pass - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
-          mbar_arrive_expect_tx(bar, query ? 2 * kKeyPart : kKeyPart);
-          if (query) bulk_g2s(sm + part * kKeyPart, q + part * kKeyPart, kKeyPart, bar);
-          bulk_g2s(sm + kKOff + part * kKeyPart, src + part * kKeyPart, kKeyPart, bar);
-          ++copies;
-        }
+      for (int part = 0; part < kKeyParts; ++part) {
+        uint64_t* const bar = &ctl.k_bar[part];
+        if (o.pass > 0 && !(ok = pwait(&ctl.k_free[part], (o.pass - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
+        mbar_arrive_expect_tx(bar, query ? 2 * kKeyPart : kKeyPart);
+        if (query) bulk_g2s(sm + part * kKeyPart, q + part * kKeyPart, kKeyPart, bar);
+        bulk_g2s(sm + kKOff + part * kKeyPart, src + part * kKeyPart, kKeyPart, bar);
+        ++copies;
       }
-      ++o.nk;
-      o.k.next(p);
+      o.pass_done(p);
     } else {
       const uint8_t* src = p.images + (static_cast<size_t>(o.v.b) * p.img_width + 2 * o.v.q) * kImage + 4 * rank * kChunk;
 #pragma unroll 1
-      for (int part = 0; part < kValueParts; ++part) {  // channels 128 (part / 2) .., block part & 1
+      for (int i = 0; i < 2; ++i) {  // channels 128 (part / 2) .., block part & 1
+        const int part = 2 * (o.half & 1u) + i;
         uint64_t* const bar = &ctl.v_bar[part];
-        if (o.nv > 0 && !(ok = pwait(&ctl.v_free[part], (o.nv - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
+        if (o.half > 1 && !(ok = pwait(&ctl.v_free[part], (o.summed() - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
         mbar_arrive_expect_tx(bar, kValuePart);
 #pragma unroll
         for (int c = part & ~1; c < (part & ~1) + 2; ++c)
           bulk_g2s(sm + kVOff + c * kVChunk + (part & 1) * kChunk, src + (part & 1) * kImage + c * kChunk, kChunk, bar);
         ++values;
       }
-      ++o.nv;
-      o.v.next(p);
+      o.half_done(p);
     }
   }
   if (!ok) set_abort(ctl, p.dev_err);
@@ -205,31 +219,25 @@ __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, Tre
 // the arrivals release nothing to the cluster: with that release each took more than a
 // thousand cycles, 4,700 instead of 1,830 for 64 tokens.)
 __device__ void relay_role(const Params& p, const TreeSched& sc, TreeCtrl& ctl) {
-  TreeOrder o;
-  o.k = o.v = sc;
-  uint32_t pass = 0;
+  TreeOrder o(p, sc);
   bool ok = true;
   const uint32_t kbar = cluster_map(smem_u32(&ctl.k_bar[0]), 0), vbar = cluster_map(smem_u32(&ctl.v_bar[0]), 0);
   while (ok && o.live()) {
     if (o.score_next()) {
-      const int products = o.k.products(p);
-      for (int i = 0; ok && i < products; ++i, ++pass) {
 #pragma unroll 1
-        for (int part = 0; part < kKeyParts; ++part) {
-          if (!(ok = pwait(&ctl.k_bar[part], pass & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
-          mbar_arrive_remote(kbar + part * 8, true);
-        }
+      for (int part = 0; part < kKeyParts; ++part) {
+        if (!(ok = pwait(&ctl.k_bar[part], o.pass & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+        mbar_arrive_remote(kbar + part * 8, true);
       }
-      ++o.nk;
-      o.k.next(p);
+      o.pass_done(p);
     } else {
 #pragma unroll 1
-      for (int part = 0; part < kValueParts; ++part) {
-        if (!(ok = pwait(&ctl.v_bar[part], o.nv & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+      for (int i = 0; i < 2; ++i) {
+        const int part = 2 * (o.half & 1u) + i;
+        if (!(ok = pwait(&ctl.v_bar[part], o.summed() & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
         mbar_arrive_remote(vbar + part * 8, true);
       }
-      ++o.nv;
-      o.v.next(p);
+      o.half_done(p);
     }
   }
   if (!ok) set_abort(ctl, p.dev_err);
@@ -242,39 +250,35 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
   const uint64_t qa = smem_desc(smem, 16, 1024, SWZ_128B), kb = smem_desc(smem + kKOff, 16, 1024, SWZ_128B);
   const uint64_t pa = smem_desc(smem + kPOff, 16, 1024, SWZ_128B);
   const uint64_t vb = smem_desc(smem + kVOff, kVChunk, 1024, SWZ_128B);
-  TreeOrder o;
-  o.k = o.v = sc;
-  uint32_t pass = 0;
+  TreeOrder o(p, sc);
   bool ok = true;
   while (ok && o.live()) {
     if (o.score_next()) {
-      const uint32_t ts = tmem + kColS + (o.nk & 1u) * 64;
-      const int products = o.k.products(p);
-      for (int i = 0; ok && i < products; ++i, ++pass) {
+      const uint32_t s_at = o.scored() & 1u, ts = tmem + kColS + s_at * 64;
+      const bool adds = o.rest();
 #pragma unroll
-        for (int part = 0; part < kKeyParts; ++part) {
-          if (!(ok = pwait_cluster(&ctl.k_bar[part], pass & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
-          tc_fence_after();
+      for (int part = 0; part < kKeyParts; ++part) {
+        if (!(ok = pwait_cluster(&ctl.k_bar[part], o.pass & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
+        tc_fence_after();
 #pragma unroll
-          for (int k = 3 * part; k < 3 * part + 3; ++k) {
+        for (int k = 3 * part; k < 3 * part + 3; ++k) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-              umma2_f16_ss(ts, qa + ((k * kChunk + s * 32) >> 4), kb + ((k * kChunk + s * 32) >> 4), kIdQK,
-                           k == 0 && s == 0 && i == 0 ? 0u : 1u);
-          }
-          umma2_commit(&ctl.k_free[part]);
+          for (int s = 0; s < 4; ++s)
+            umma2_f16_ss(ts, qa + ((k * kChunk + s * 32) >> 4), kb + ((k * kChunk + s * 32) >> 4), kIdQK,
+                         k == 0 && s == 0 && !adds ? 0u : 1u);
         }
+        umma2_commit(&ctl.k_free[part]);
       }
       if (!ok) break;
-      umma2_commit(&ctl.s_full[o.nk & 1u]);
-      ++o.nk;
-      o.k.next(p);
+      if (o.ends()) umma2_commit(&ctl.s_full[s_at]);
+      o.pass_done(p);
     } else {
-      const uint32_t ph = o.nv & 1u;
+      const uint32_t ph = o.summed() & 1u;
       const bool first = o.v.first();
-      if (!(ok = pwait_cluster(&ctl.p_full, ph, ctl, kSiteMmaPFull, p.dev_err))) break;
-#pragma unroll
-      for (int part = 0; part < kValueParts; ++part) {
+      if ((o.half & 1u) == 0 && !(ok = pwait_cluster(&ctl.p_full, ph, ctl, kSiteMmaPFull, p.dev_err))) break;
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        const int part = 2 * (o.half & 1u) + i;
         if (!(ok = pwait_cluster(&ctl.v_bar[part], ph, ctl, kSiteMmaChunk, p.dev_err))) break;
         tc_fence_after();
 #pragma unroll
@@ -285,8 +289,7 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
         umma2_commit(&ctl.v_free[part]);
       }
       if (!ok) break;
-      ++o.nv;
-      o.v.next(p);
+      o.half_done(p);
     }
   }
   if (!ok) set_abort(ctl, p.dev_err);

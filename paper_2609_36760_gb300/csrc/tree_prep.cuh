@@ -180,7 +180,7 @@ __device__ void find_not_finite(const Params& p, int b) {
 }
 
 // Block idx % img_width of sequence idx / img_width as an fp16 image (see Params::images), zero
-// behind the sequence's end up to a whole tile, and for short sequences the image of C - RN_f16(C). A thread has
+// behind the sequence's end up to a whole tile, and perhaps the image of C - RN_f16(C). A thread has
 // the same eight channels of one row's nine chunks, all loaded before any is stored. A row with a
 // value that is not finite is 0 with NaN in the RoPE channels, which are keys alone: so it makes
 // NaN of the queries that see it, and its weight of 0 nothing of the others.
@@ -199,9 +199,7 @@ __device__ void expand_block(const Params& p, int idx) {
   const int i = threadIdx.x & 7, slot = threadIdx.x >> 3, pos = j * kBlockTokens + slot;
   const size_t at = swz_off(slot, i, 128);
   uint8_t* const img = p.images + static_cast<size_t>(idx) * kImage + at;
-  uint8_t* const rest = p.rest_images != nullptr && len <= kExactTokens
-                            ? p.rest_images + (static_cast<size_t>(b) * p.rest_width + j) * kImage + at
-                            : nullptr;
+  uint8_t* const rest = p.rest_images != nullptr ? p.rest_images + static_cast<size_t>(idx) * kImage + at : nullptr;
   const uint8_t* src = nullptr;
   if (CB != 16 && p.prot != nullptr) {
     RowRef r;

@@ -18,9 +18,10 @@ class Hazard(Exception):
 
 
 class Model:
-    def __init__(self, segments, seed, without=""):
-        """segments: (tiles, products a tile) of each; without: a wait to leave out."""
-        self.tiles = [(s, products, i == 0, i == n - 1) for s, (n, products) in enumerate(segments) for i in range(n)]
+    def __init__(self, segments, passes, seed, without=""):
+        """segments: tiles of each; passes: of QK, a tile; without: a wait to leave out."""
+        self.tiles = [(s, i == 0, i == n - 1) for s, n in enumerate(segments) for i in range(n)]
+        self.passes = passes
         self.rnd, self.without = random.Random(seed), without
         self.count, self.needs = {}, {"p_full": 8}
         for part in range(KEYS):
@@ -69,75 +70,74 @@ class Model:
 
     # ---- roles
     def order(self):
-        """(score?, tile) in the order of the copies and the issuer."""
-        nk = nv = 0
-        while nv < len(self.tiles):
-            if nk < len(self.tiles) and nk < nv + 2:
-                yield True, nk
-                nk += 1
+        """(score?, pass or half of PV) in the order of the copies and the issuer."""
+        np = nh = 0
+        while nh < 2 * len(self.tiles):
+            more = np < nh + 3 if self.passes == 2 else 2 * np < nh // 2 * 2 + 4
+            if np < self.passes * len(self.tiles) and more:
+                yield True, np
+                np += 1
             else:
-                yield False, nv
-                nv += 1
+                yield False, nh
+                nh += 1
 
     def load(self, c):
-        run = 0
-        for score, n in self.order():
-            seg, products, first, _ = self.tiles[n]
+        for score, at in self.order():
             if score:
-                for i in range(products):
-                    for part in range(KEYS):
-                        if run:
-                            yield from self.wait(("k_free", c, part), run - 1, "k_free")
-                        writes = [(("K", c, part), (n, i))]
-                        if i == 0 and first:
-                            writes.append((("Q", c, part), seg))
-                        self.copy(("k_bar", c, part), writes)
-                        yield "step"
-                    run += 1
+                n, i = divmod(at, self.passes)
+                seg, first, _ = self.tiles[n]
+                for part in range(KEYS):
+                    if at:
+                        yield from self.wait(("k_free", c, part), at - 1, "k_free")
+                    writes = [(("K", c, part), (n, i))]
+                    if i == 0 and first:
+                        writes.append((("Q", c, part), seg))
+                    self.copy(("k_bar", c, part), writes)
+                    yield "step"
             else:
-                for part in range(VALUES):
+                n, half = divmod(at, 2)
+                for part in (2 * half, 2 * half + 1):
                     if n:
                         yield from self.wait(("v_free", c, part), n - 1, "v_free")
                     self.copy(("v_bar", c, part), [(("V", c, part), n)])
                     yield "step"
 
     def relay(self):
-        run = 0
-        for score, n in self.order():
+        for score, at in self.order():
             if score:
-                for _ in range(self.tiles[n][1]):
-                    for part in range(KEYS):
-                        yield from self.wait(("k_bar", 1, part), run, "relay")
-                        self.arrive(("k_bar", 0, part))
-                        yield "step"
-                    run += 1
+                for part in range(KEYS):
+                    yield from self.wait(("k_bar", 1, part), at, "relay")
+                    self.arrive(("k_bar", 0, part))
+                    yield "step"
             else:
-                for part in range(VALUES):
+                n, half = divmod(at, 2)
+                for part in (2 * half, 2 * half + 1):
                     yield from self.wait(("v_bar", 1, part), n)
                     self.arrive(("v_bar", 0, part))
                     yield "step"
 
     def issue(self):
-        run = 0
-        for score, n in self.order():
-            seg, products, first, last = self.tiles[n]
+        for score, at in self.order():
             if score:
+                n, i = divmod(at, self.passes)
+                seg = self.tiles[n][0]
                 if n >= 2 and self.scores_read.get(n - 2, 0) != 8:
                     raise Hazard("scores overwritten before every warp has read them")
-                for i in range(products):
-                    for part in range(KEYS):
-                        yield from self.wait(("k_bar", 0, part), run)
-                        self.mma([(("K", c, part), (n, i)) for c in (0, 1)] + [(("Q", c, part), seg) for c in (0, 1)],
-                                 ("S", n & 1, n))
-                        for c in (0, 1):
-                            self.commit(("k_free", c, part))
-                        yield "step"
-                    run += 1
-                for c in (0, 1):
-                    self.commit(("s_full", c, n & 1))
+                for part in range(KEYS):
+                    yield from self.wait(("k_bar", 0, part), at)
+                    self.mma([(("K", c, part), (n, i)) for c in (0, 1)] + [(("Q", c, part), seg) for c in (0, 1)],
+                             ("S", n & 1, n))
+                    for c in (0, 1):
+                        self.commit(("k_free", c, part))
+                    yield "step"
+                if i == self.passes - 1:
+                    for c in (0, 1):
+                        self.commit(("s_full", c, n & 1))
             else:
-                yield from self.wait("p_full", n, "p_full")
-                for part in range(VALUES):
+                n, half = divmod(at, 2)
+                if half == 0:
+                    yield from self.wait("p_full", n, "p_full")
+                for part in (2 * half, 2 * half + 1):
                     yield from self.wait(("v_bar", 0, part), n)
                     self.mma([(("V", c, part), n) for c in (0, 1)] + [(("P", c, w), n) for c in (0, 1) for w in range(4)],
                              ("O", None, n))
@@ -153,7 +153,7 @@ class Model:
 
     def softmax(self, c, w):
         met = 0
-        for n, (seg, products, first, last) in enumerate(self.tiles):
+        for n, (_, first, last) in enumerate(self.tiles):
             yield from self.wait(("s_full", c, n & 1), n >> 1)
             if self.holds.get(("S", n & 1)) != n:
                 raise Hazard(f"scores of tile {n} are not there")
@@ -228,13 +228,13 @@ class Model:
 
 
 def segments(rnd):
-    return [(rnd.choice([1, 1, 2, 3, 5]), rnd.choice([1, 1, 1, 2])) for _ in range(rnd.randint(1, 4))]
+    return [rnd.choice([1, 1, 2, 3, 5]) for _ in range(rnd.randint(1, 4))]
 
 
 @pytest.mark.parametrize("block", range(8))
 def test_no_hazard_and_no_deadlock(block):
     for seed in range(block * 40, block * 40 + 40):
-        Model(segments(random.Random(seed)), seed).run()
+        Model(segments(random.Random(seed)), 1 + seed % 2, seed).run()
 
 
 @pytest.mark.parametrize("without", ["k_free", "v_free", "relay", "p_full", "wait_pv", "end_pv"])
@@ -242,7 +242,7 @@ def test_a_wait_taken_out_is_seen(without):
     seen = 0
     for seed in range(60):
         try:
-            Model(segments(random.Random(seed)) + [(3, 1)], seed, without).run()
+            Model(segments(random.Random(seed)) + [3], 1 + seed % 2, seed, without).run()
         except Hazard:
             seen += 1
     assert seen > 20, seen

@@ -52,6 +52,14 @@ cudaError_t launch_rows(int hg, const Params& prm, cudaStream_t stream) {
   return launch_impl<CB, 64, PROT, false>(prm, stream, nullptr, nullptr);
 }
 
+// Images that L2 does not hold are read by all row groups of a sequence at once: the plan
+// goes group by group, with as many ranges to each, which then keep step (64 x 4,096 tokens, 4
+// groups: the main kernel 221 to 181 us), unless that leaves over a twelfth of the pairs idle.
+bool keep_step(int pairs, int groups) {
+  const int teams = pairs / groups;
+  return teams > 0 && (pairs - teams * groups) * 12 <= pairs;
+}
+
 // The n sequences from b on over images at `images`, blocks of them a sequence.
 cudaError_t launch_images(const qmla_tree_desc& d, Params prm, uint8_t* images, int b, int n, int blocks, bool rest,
                           cudaStream_t stream) {
@@ -75,13 +83,9 @@ cudaError_t launch_images(const qmla_tree_desc& d, Params prm, uint8_t* images, 
   prm.n_hg = (prm.heads + 127) / 128;
   prm.n_img = 2 * prm.n_hg;
   prm.grid = prm.sms / 2;
-  // Images that L2 does not hold are read by all row groups of a sequence at once: the plan
-  // goes group by group, with as many ranges to each, which then keep step (64 x 4,096 tokens, 4
-  // groups: the main kernel 221 to 181 us), unless that leaves over a twelfth of the pairs idle.
-  const int teams = prm.grid / prm.n_hg;
-  if (n * image_bytes(blocks, rest) > (96u << 20) && teams > 0 && (prm.grid - teams * prm.n_hg) * 12 <= prm.grid) {
+  if (n * image_bytes(blocks, rest) > (96u << 20) && keep_step(prm.grid, prm.n_hg)) {
     prm.by_group = true;
-    prm.grid = teams * prm.n_hg;
+    prm.grid = prm.grid / prm.n_hg * prm.n_hg;
   }
   switch (d.cache_kind) {
     case 4: return launch_impl<4, 64, false, true>(prm, stream, nullptr, nullptr);
@@ -139,9 +143,14 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
   // (but the very small, and those beyond 65,504, which are infinite).
   const bool rest = d.lse != nullptr && d.cache_kind != QMLA_CACHE_BF16;
   const size_t room = d.workspace_bytes > w.images_off ? d.workspace_bytes - w.images_off : 0;
-  const int fit = static_cast<int>(std::min<size_t>(d.batch, blocks > 0 ? room / image_bytes(blocks, rest) : 0));
+  int fit = static_cast<int>(std::min<size_t>(d.batch, blocks > 0 ? room / image_bytes(blocks, rest) : 0));
   if (fit > 0 && on_images(rows, static_cast<long long>(d.batch) * blocks * kBlockTokens, rest)) {
-    // As many sequences at a time as there is room for.
+    // As many sequences at a time as there is room for; and as L2 holds, where many row groups that
+    // do not keep step read their images (16 x 4,096 tokens, 32 groups, both passes: 714 us at once, 630
+    // by 80 MB, 598 by 60, 588 by 40; 2 x 30,000 435 and 398; 57 MB by 40 instead of at once 100 and 116).
+    const int groups = (rows + 127) / 128;
+    if (groups >= 8 && !keep_step(grid / 2, groups) && d.batch * image_bytes(blocks, rest) > (112u << 20))
+      fit = std::min(fit, std::max(1, static_cast<int>((56u << 20) / image_bytes(blocks, rest))));
     const int parts = (d.batch + fit - 1) / fit, per = (d.batch + parts - 1) / parts;
     for (int b = 0; b < d.batch; b += per) {
       const cudaError_t e = launch_images(d, prm, ws + w.images_off, b, std::min(per, d.batch - b), blocks, rest, stream);

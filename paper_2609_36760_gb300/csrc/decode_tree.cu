@@ -32,17 +32,20 @@ int image_blocks(long long tokens) {  // of whole tiles
 size_t image_bytes(int blocks, bool rest) { return static_cast<size_t>(blocks) * (rest ? 2 : 1) * kImage; }  // a sequence's
 
 // Whether the context is laid out as images for tree_pair (where the workspace has room for them):
-// for more than 64 rows always, else up to 40,960 tokens of the batch, counted by the table's
-// width or the caller's bound. Measured on one GB300 (INT4, one call replayed, us, decode_main's
-// rows against the images; protected and BF16 rows gain more from them):
+// where lse is asked for of a quantised cache, for its precision (with the second pass for it 8 x
+// 8,000 tokens and 16 rows take 69 us, 64 x 4,000 217); else for more than 64 rows, and up to
+// 40,960 tokens of the batch, counted by the table's width or the caller's bound. Measured on one GB300
+// (INT4 without lse, one call replayed, us, decode_main's rows against the images; protected and BF16
+// rows gain more from them):
 //                 16 rows         64         128         256       1,024
-//   1 x    500  21.1 / 16.0  29.5 / 17.6  26.7 / 17.9  26.2 / 19.0  29.2 / 20.2
-//   8 x  4,000  22.6 / 26.6  30.8 / 29.7  42.6 / 31.0  62.6 / 37.8   142 / 65
-//   1 x 40,000  32.8 / 31.1  43.0 / 37.0  45.9 / 38.5  58.8 / 38.3   154 / 70
-//   8 x  8,000  28.2 / 42.2  38.3 / 44.9  57.2 / 45.0  84.1 / 54.1   245 / 108
-//   1 x 100,000 42.0 / 62.4  54.7 / 64.3  68.8 / 60.7   105 / 70.7   344 / 149
-//  64 x    500  23.2 / 37.3  38.3 / 42.9  50.2 / 46.2  85.9 / 73.8   256 / 171
-//  64 x  4,000  62.1 / 128   91.8 / 133    149 / 137    270 / 173    989 / 415
+//   1 x    500  21.6 / 15.4  30.2 / 16.9  27.3 / 17.2  26.6 / 18.5  30.3 / 19.6
+//   8 x    500  17.9 / 16.3  26.8 / 18.1  29.7 / 19.0  36.9 / 22.4  55.9 / 31.3
+//   8 x  4,000  22.7 / 27.1  31.7 / 30.2  43.9 / 31.2  64.7 / 38.4   145 / 66
+//  64 x    500  23.8 / 27.2  38.7 / 32.1  54.0 / 35.5  85.8 / 51.3   261 / 120
+//   1 x 40,000  33.3 / 31.6  43.5 / 37.4  46.8 / 38.8  60.0 / 38.9   158 / 70
+//   8 x  8,000  28.5 / 42.6  39.4 / 45.2  59.0 / 45.3  87.2 / 54.7   250 / 109
+//   1 x 100,000 42.5 / 63.7  55.9 / 64.8  70.9 / 61.3   109 / 73     354 / 150
+//  64 x  4,000  61.9 / 130   95.5 / 135    152 / 139    273 / 176  1,004 / 420
 bool on_images(int rows, long long tokens, bool rest) { return rest || rows > 64 || tokens <= 40960; }
 
 template <int CB, bool PROT>

@@ -113,28 +113,29 @@ struct TreeSched {
 // A tile has one or two passes of QK, over the images and over what they leave off, and two halves
 // of PV, of 128 of a CTA's channels each. Two passes are kept apart by halves,
 //   QK(i + 1), PV(i) first half, rest of QK(i + 1), PV(i) second half, QK(i + 2) ..,
-// for each pass has all of the keys' room, and its copies have half a PV to arrive in (one behind
-// the other a tile took 4,900 cycles).
+// for each pass has all of the keys' room, and its copies have half a PV to arrive in (2 x 30,000
+// tokens, 64 nodes x 64 heads: 442 to 434 us).
+// (One pass and whole PVs are a kernel of their own: the counting of halves cost it 3%.)
+template <int PASSES>
 struct TreeOrder {
-  TreeSched k, v;                 // tiles of the next pass and half
-  uint32_t pass = 0, half = 0;    // counted
-  uint32_t passes;                // a tile
-  __device__ TreeOrder(const Params& p, const TreeSched& sc) : k(sc), v(sc), passes(p.rest_images != nullptr ? 2 : 1) {}
+  static constexpr int kParts = kValueParts / PASSES;  // of the values, in a step of PV
+  TreeSched k, v;                                      // tiles of the next pass and step of PV
+  uint32_t pass = 0, step = 0;                         // counted
+  __device__ explicit TreeOrder(const TreeSched& sc) : k(sc), v(sc) {}
   __device__ bool live() const { return v.live; }
-  __device__ bool score_next() const {
-    return k.live && (passes == 2 ? pass < half + 3 : 2 * pass < (half & ~1u) + 4);
-  }
-  __device__ bool rest() const { return passes == 2 && (pass & 1u); }
-  __device__ uint32_t scored() const { return passes == 2 ? pass >> 1 : pass; }  // tile of the pass
-  __device__ uint32_t summed() const { return half >> 1; }                       // and of the half
-  __device__ bool ends() const { return passes == 1 || (pass & 1u); }            // last pass of its tile
+  __device__ bool score_next() const { return k.live && pass < step + 1 + PASSES; }
+  __device__ bool rest() const { return PASSES == 2 && (pass & 1u); }
+  __device__ bool ends() const { return PASSES == 1 || (pass & 1u); }  // last pass of its tile
+  __device__ uint32_t scored() const { return pass / PASSES; }         // tile of the pass
+  __device__ uint32_t summed() const { return step / PASSES; }         // and of the step
+  __device__ int half() const { return PASSES == 1 ? 0 : step & 1u; }
   __device__ void pass_done(const Params& p) {
     if (ends()) k.next(p);
     ++pass;
   }
-  __device__ void half_done(const Params& p) {
-    if (half & 1u) v.next(p);
-    ++half;
+  __device__ void step_done(const Params& p) {
+    if (PASSES == 1 || (step & 1u)) v.next(p);
+    ++step;
   }
 };
 
@@ -164,8 +165,9 @@ __device__ __forceinline__ bool pwait_cluster(uint64_t* bar, uint32_t parity, Tr
 }
 
 // ------------------------------------------------------------------- copies
+template <int PASSES>
 __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, TreeCtrl& ctl, int rank) {
-  TreeOrder o(p, sc);
+  TreeOrder<PASSES> o(sc);
   uint32_t copies = 0, values = 0;  // parts asked for
   bool ok = true;
   while (ok && o.live()) {
@@ -187,17 +189,17 @@ __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, Tre
     } else {
       const uint8_t* src = p.images + (static_cast<size_t>(o.v.b) * p.img_width + 2 * o.v.q) * kImage + 4 * rank * kChunk;
 #pragma unroll 1
-      for (int i = 0; i < 2; ++i) {  // channels 128 (part / 2) .., block part & 1
-        const int part = 2 * (o.half & 1u) + i;
+      for (int i = 0; i < o.kParts; ++i) {  // channels 128 (part / 2) .., block part & 1
+        const int part = o.kParts * o.half() + i;
         uint64_t* const bar = &ctl.v_bar[part];
-        if (o.half > 1 && !(ok = pwait(&ctl.v_free[part], (o.summed() - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
+        if (o.summed() > 0 && !(ok = pwait(&ctl.v_free[part], (o.summed() - 1) & 1u, ctl, kSiteDqSlot, p.dev_err))) break;
         mbar_arrive_expect_tx(bar, kValuePart);
 #pragma unroll
         for (int c = part & ~1; c < (part & ~1) + 2; ++c)
           bulk_g2s(sm + kVOff + c * kVChunk + (part & 1) * kChunk, src + (part & 1) * kImage + c * kChunk, kChunk, bar);
         ++values;
       }
-      o.half_done(p);
+      o.step_done(p);
     }
   }
   if (!ok) set_abort(ctl, p.dev_err);
@@ -218,8 +220,9 @@ __device__ void load_role(const Params& p, const TreeSched& sc, uint8_t* sm, Tre
 // (The tensor core of this SM reads what they brought, and this thread has written nothing, so
 // the arrivals release nothing to the cluster: with that release each took more than a
 // thousand cycles, 4,700 instead of 1,830 for 64 tokens.)
+template <int PASSES>
 __device__ void relay_role(const Params& p, const TreeSched& sc, TreeCtrl& ctl) {
-  TreeOrder o(p, sc);
+  TreeOrder<PASSES> o(sc);
   bool ok = true;
   const uint32_t kbar = cluster_map(smem_u32(&ctl.k_bar[0]), 0), vbar = cluster_map(smem_u32(&ctl.v_bar[0]), 0);
   while (ok && o.live()) {
@@ -232,25 +235,26 @@ __device__ void relay_role(const Params& p, const TreeSched& sc, TreeCtrl& ctl) 
       o.pass_done(p);
     } else {
 #pragma unroll 1
-      for (int i = 0; i < 2; ++i) {
-        const int part = 2 * (o.half & 1u) + i;
+      for (int i = 0; i < o.kParts; ++i) {
+        const int part = o.kParts * o.half() + i;
         if (!(ok = pwait(&ctl.v_bar[part], o.summed() & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
         mbar_arrive_remote(vbar + part * 8, true);
       }
-      o.half_done(p);
+      o.step_done(p);
     }
   }
   if (!ok) set_abort(ctl, p.dev_err);
 }
 
 // --------------------------------------------------------------------- MMAs
+template <int PASSES>
 __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, TreeCtrl& ctl, uint32_t tmem) {
   constexpr uint32_t kIdQK = idesc_f16_f32(128, 128, false, false);
   constexpr uint32_t kIdPV = idesc_f16_f32(128, 256, false, true);
   const uint64_t qa = smem_desc(smem, 16, 1024, SWZ_128B), kb = smem_desc(smem + kKOff, 16, 1024, SWZ_128B);
   const uint64_t pa = smem_desc(smem + kPOff, 16, 1024, SWZ_128B);
   const uint64_t vb = smem_desc(smem + kVOff, kVChunk, 1024, SWZ_128B);
-  TreeOrder o(p, sc);
+  TreeOrder<PASSES> o(sc);
   bool ok = true;
   while (ok && o.live()) {
     if (o.score_next()) {
@@ -275,10 +279,10 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
     } else {
       const uint32_t ph = o.summed() & 1u;
       const bool first = o.v.first();
-      if ((o.half & 1u) == 0 && !(ok = pwait_cluster(&ctl.p_full, ph, ctl, kSiteMmaPFull, p.dev_err))) break;
-#pragma unroll 1
-      for (int i = 0; i < 2; ++i) {
-        const int part = 2 * (o.half & 1u) + i;
+      if (o.half() == 0 && !(ok = pwait_cluster(&ctl.p_full, ph, ctl, kSiteMmaPFull, p.dev_err))) break;
+#pragma unroll
+      for (int part = 0; part < kValueParts; ++part) {
+        if (part / o.kParts != o.half()) continue;
         if (!(ok = pwait_cluster(&ctl.v_bar[part], ph, ctl, kSiteMmaChunk, p.dev_err))) break;
         tc_fence_after();
 #pragma unroll
@@ -289,7 +293,7 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
         umma2_commit(&ctl.v_free[part]);
       }
       if (!ok) break;
-      o.half_done(p);
+      o.step_done(p);
     }
   }
   if (!ok) set_abort(ctl, p.dev_err);
@@ -495,6 +499,7 @@ __device__ void softmax_role(const Params& p, TreeSched sc, uint32_t smem, TreeC
   }
 }
 
+template <int PASSES>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tree_pair(const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -539,11 +544,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) tree_pa
     TreeSched sc;
     sc.init(p, pair);
     if (warp == kLoadWarp) {
-      load_role(p, sc, sm, ctl, rank);
+      load_role<PASSES>(p, sc, sm, ctl, rank);
     } else if (rank == 0) {
-      issue_role(p, sc, smem, ctl, tmem);
+      issue_role<PASSES>(p, sc, smem, ctl, tmem);
     } else {
-      relay_role(p, sc, ctl);
+      relay_role<PASSES>(p, sc, ctl);
     }
   } else {
     asm volatile("exit;");
@@ -666,11 +671,13 @@ cudaError_t launch_tree_pair(const Params& prm, cudaStream_t stream) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (configured_device != dev) {
-    e = cudaFuncSetAttribute(tree_pair, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (e != cudaSuccess) return e;
+    for (auto* kern : {tree_pair<1>, tree_pair<2>}) {
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+      if (e != cudaSuccess) return e;
+    }
     configured_device = dev;
   }
-  return launch_k(tree_pair, dim3(2 * prm.grid), dim3(kThreads), kSmem, stream, true, prm);
+  return launch_k(prm.rest_images != nullptr ? tree_pair<2> : tree_pair<1>, dim3(2 * prm.grid), dim3(kThreads), kSmem, stream, true, prm);
 }
 
 }  // namespace qmla

@@ -73,7 +73,7 @@ class Model:
         """(score?, pass or half of PV) in the order of the copies and the issuer."""
         np = nh = 0
         while nh < 2 * len(self.tiles):
-            more = np < nh + 3 if self.passes == 2 else 2 * np < nh // 2 * 2 + 4
+            more = np < nh + 3 if self.passes == 2 else np < nh // 2 + 2 and nh % 2 == 0
             if np < self.passes * len(self.tiles) and more:
                 yield True, np
                 np += 1

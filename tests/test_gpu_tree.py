@@ -104,10 +104,10 @@ def test_sequences_without_a_tree_and_padding(kind, images):
 
 
 @pytest.mark.parametrize("kind,protect", [(4, False), ("c4r4", True), ("bf16", False)])
-@pytest.mark.parametrize("nodes,heads", [(8, 32), (12, 32), (5, 100), (26, 32)])
+@pytest.mark.parametrize("nodes,heads", [(8, 32), (12, 32), (5, 100), (26, 32), (26, 64)])
 def test_images_beyond_l2_and_groups_without_nodes(kind, protect, nodes, heads):
     """A table so wide that the images take more than L2: the plan goes group by group (2, 3, 4 and 7
-    groups of 128 rows), with trees that leave whole groups without a node."""
+    groups of 128 rows), or some sequences at a time (13), with trees that leave whole groups without a node."""
     ctx = [0, 1, 127, 128, 500, 900, 129, 64, 3, 1300, 256, 700]
     counts = [max(0, nodes - 3 * i) for i in range(len(ctx))]
     counts[5], counts[9] = nodes, nodes

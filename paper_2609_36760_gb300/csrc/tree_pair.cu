@@ -260,7 +260,7 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
     if (o.score_next()) {
       const uint32_t s_at = o.scored() & 1u, ts = tmem + kColS + s_at * 64;
       const bool adds = o.rest();
-#pragma unroll
+#pragma unroll(PASSES == 1 ? kKeyParts : 1)
       for (int part = 0; part < kKeyParts; ++part) {
         if (!(ok = pwait_cluster(&ctl.k_bar[part], o.pass & 1u, ctl, kSiteMmaChunk, p.dev_err))) break;
         tc_fence_after();
@@ -280,9 +280,9 @@ __device__ void issue_role(const Params& p, const TreeSched& sc, uint32_t smem, 
       const uint32_t ph = o.summed() & 1u;
       const bool first = o.v.first();
       if (o.half() == 0 && !(ok = pwait_cluster(&ctl.p_full, ph, ctl, kSiteMmaPFull, p.dev_err))) break;
-#pragma unroll
-      for (int part = 0; part < kValueParts; ++part) {
-        if (part / o.kParts != o.half()) continue;
+#pragma unroll(PASSES == 1 ? kValueParts : 1)
+      for (int i = 0; i < o.kParts; ++i) {
+        const int part = o.kParts * o.half() + i;
         if (!(ok = pwait_cluster(&ctl.v_bar[part], ph, ctl, kSiteMmaChunk, p.dev_err))) break;
         tc_fence_after();
 #pragma unroll

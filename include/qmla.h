@@ -588,7 +588,8 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *     out[b,t,h,:] = RN_bf16(sum_p softmax_p(S[b,t,h,:]) C_hat[b,p,:]);  lse[b,t,h] = log sum_p exp(S[b,t,h,p])
  *   pool, cache_kind, num_blocks, block_table, max_blocks, softmax_scale, dev_err
  *                   as in qmla_mla_decode_ex, any of the four cache kinds
- *   max_len         a bound of seq_lens, or 0 (max_blocks x 64 then). Longer sequences are bad ones
+ *   max_len         a bound of seq_lens, or 0 (max_blocks x 64 then). Longer sequences are bad ones.
+ *                   (The launches and the room for images go by it: a near bound is faster)
  *   q_latent, q_pe  [batch, nodes, heads, 512] and [batch, nodes, heads, 64] bf16, 16-byte aligned
  *   nodes, heads    1 .. QMLA_MAX_TREE_NODES, 1 .. 128
  *   parents         [batch, nodes] int32

@@ -955,6 +955,13 @@ __global__ void __launch_bounds__(kThreads, 1) decode_main(const Params p) {
 
 // ------------------------------------------------------------ prep / combine
 constexpr int kPrepThreads = kTree ? 512 : 1024;
+// Blocks of prep for the images of a sequence's cache blocks; each goes on until it is behind the
+// sequence's end. (A wide table has many that no sequence reaches: 32,768 blocks of their own took 60 us
+// to find nothing.)
+__host__ __device__ __forceinline__ int expand_blocks(const Params& p) {
+  const int most = 4864 / p.batch;
+  return most < 1 ? 1 : (most < p.img_width ? most : p.img_width);
+}
 constexpr int kTreesPerBlock = kPrepThreads / kMaxNodes;  // sequences whose trees one block of prep makes
 
 #if QMLA_DECODE_TREE
@@ -988,7 +995,8 @@ __global__ void __launch_bounds__(kPrepThreads) prep_kernel(const Params p) {
       if (block < images) {
         query_image(p, block);
       } else {
-        expand_block<CB>(p, block - static_cast<int>(images));
+        const int per = expand_blocks(p), i = block - static_cast<int>(images), b = i / per;
+        for (int j = i - b * per; j < p.img_width && expand_block<CB>(p, b, j); j += per) {}
       }
       return;
     }
@@ -1409,7 +1417,7 @@ cudaError_t launch_impl(const Params& prm, cudaStream_t stream, cudaEvent_t ev0,
                                                : (pieces + kPrepThreads - 1) / kPrepThreads;
   const unsigned prep_blocks = static_cast<unsigned>(1 + query_blocks +
                                                      (kTree ? (prm.batch + kTreesPerBlock - 1) / kTreesPerBlock : 0) +
-                                                     (!kTree ? 0 : PAIR ? prm.batch * prm.img_width : prm.batch));
+                                                     (!kTree ? 0 : PAIR ? prm.batch * expand_blocks(prm) : prm.batch));
   if ((e = launch_k(prep_kernel<CB, HG, PAIR>, dim3(prep_blocks), dim3(kPrepThreads), 0, stream, pdl, prm)) != cudaSuccess)
     return e;
   if (ev0 != nullptr && (e = cudaEventRecord(ev0, stream)) != cudaSuccess) return e;

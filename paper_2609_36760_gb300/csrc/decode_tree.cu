@@ -151,9 +151,10 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
     // As many sequences at a time as there is room for; and as L2 holds, where many row groups that
     // do not keep step read their images (16 x 4,096 tokens, 32 groups, both passes: 714 us at once, 630
     // by 80 MB, 598 by 60, 588 by 40; 2 x 30,000 435 and 398; 57 MB by 40 instead of at once 100 and 116).
+    // Not over six launches for that: the lengths may be far below their bound.
     const int groups = (rows + 127) / 128;
     if (groups >= 8 && !keep_step(grid / 2, groups) && d.batch * image_bytes(blocks, rest) > (112u << 20))
-      fit = std::min(fit, std::max(1, static_cast<int>((56u << 20) / image_bytes(blocks, rest))));
+      fit = std::min(fit, std::max((d.batch + 5) / 6, static_cast<int>((56u << 20) / image_bytes(blocks, rest))));
     const int parts = (d.batch + fit - 1) / fit, per = (d.batch + parts - 1) / parts;
     for (int b = 0; b < d.batch; b += per) {
       const cudaError_t e = launch_images(d, prm, ws + w.images_off, b, std::min(per, d.batch - b), blocks, rest, stream);

@@ -179,18 +179,19 @@ __device__ void find_not_finite(const Params& p, int b) {
   if (threadIdx.x == 0) p.trees[b].not_finite = found;
 }
 
-// Block idx % img_width of sequence idx / img_width as an fp16 image (see Params::images), zero
+// Block j of sequence b as an fp16 image (see Params::images), zero
 // behind the sequence's end up to a whole tile, and perhaps the image of C - RN_f16(C). A thread has
 // the same eight channels of one row's nine chunks, all loaded before any is stored. A row with a
 // value that is not finite is 0 with NaN in the RoPE channels, which are keys alone: so it makes
-// NaN of the queries that see it, and its weight of 0 nothing of the others.
+// NaN of the queries that see it, and its weight of 0 nothing of the others. False: behind the
+// sequence's end.
 template <int CB>
-__device__ void expand_block(const Params& p, int idx) {
+__device__ bool expand_block(const Params& p, int b, int j) {
   static_assert(!kTree || kPrepThreads == kBlockTokens * 8, "a thread per row and piece");
-  const int b = idx / p.img_width, j = idx - b * p.img_width;
+  const size_t idx = static_cast<size_t>(b) * p.img_width + j;
   const int entry = j < p.max_blocks ? p.table[static_cast<size_t>(b) * p.max_blocks + j] : -1;
   int groups;
-  if (j >= tree_tiles(p, b, 1, groups, nullptr) * (kTileTokens / kBlockTokens) || groups == 0) return;
+  if (j >= tree_tiles(p, b, 1, groups, nullptr) * (kTileTokens / kBlockTokens) || groups == 0) return false;
   const int len = p.seq_lens[b], ctx = len - (p.tree_lens != nullptr ? p.tree_lens[b] : p.q_tokens);
   constexpr size_t kBlk = CB == 16 ? static_cast<size_t>(kBf16BlockBytes) : BlockLayout<CB == 16 ? 4 : CB>::kBytes;
   griddep_wait();  // (the cache may still be written until here)
@@ -198,8 +199,8 @@ __device__ void expand_block(const Params& p, int idx) {
   const uint8_t* const blk = p.pool + static_cast<size_t>(known ? entry : 0) * kBlk;
   const int i = threadIdx.x & 7, slot = threadIdx.x >> 3, pos = j * kBlockTokens + slot;
   const size_t at = swz_off(slot, i, 128);
-  uint8_t* const img = p.images + static_cast<size_t>(idx) * kImage + at;
-  uint8_t* const rest = p.rest_images != nullptr ? p.rest_images + static_cast<size_t>(idx) * kImage + at : nullptr;
+  uint8_t* const img = p.images + idx * kImage + at;
+  uint8_t* const rest = p.rest_images != nullptr ? p.rest_images + idx * kImage + at : nullptr;
   const uint8_t* src = nullptr;
   if (CB != 16 && p.prot != nullptr) {
     RowRef r;
@@ -251,6 +252,7 @@ __device__ void expand_block(const Params& p, int idx) {
       if (rest != nullptr) *reinterpret_cast<uint4*>(rest + k * (64 * 128)) = make_uint4(0, 0, 0, 0);
     }
   }
+  return true;
 }
 
 // The image of 64 query rows (see query_piece), in channel order; a thread's work as above. Rows

@@ -509,7 +509,6 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
     ref0.len = fr.z;
     ref0.j = fr.w;
     ref0.b = sc.u / p.n_hg;
-    if (kTree && left_out(p, ref0, row)) ref0.has = false;
   }
   // A protected row reads its BF16 row instead of the packed cache.
   const uint8_t* psrc_cur = PROT ? row_source(p, ref0, row) : nullptr;
@@ -520,6 +519,11 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
     }
   }
   const uint8_t* blk_cur = psrc_cur != nullptr ? nullptr : resolve_row<CB>(p, ref0, row, valid_cur);
+  // (A row that is left out keeps its block: that of lane 0 serves a warp's BF16 rows.)
+  if (kTree && left_out(p, ref0, row)) {
+    valid_cur = false;
+    psrc_cur = nullptr;
+  }
   if constexpr (kEarly) {
 #pragma unroll
     for (int kc = 0; kc < 4; ++kc) f[kc] = fetch_chunk<CB>(blk_cur, valid_cur, 2 * kc + par, slot);
@@ -531,7 +535,7 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
       if (k < kNumChunks) f[kc] = fetch_chunk<CB>(blk_cur, valid_cur, k, slot);
     }
   } else {
-    // (the warp's 32 rows share a block: lane 0's row is valid whenever any is)
+    // (the warp's 32 rows share a block: lane 0 has its address whenever a row is valid)
     const uint8_t* wblk = reinterpret_cast<const uint8_t*>(
         __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(blk_cur), 0));
     bf16_load_t(cur, wblk, __ballot_sync(0xffffffffu, valid_cur), slot & ~31, par, lane);
@@ -547,7 +551,6 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
     // The next tile's block pointer (its table entry was loaded a tile ago)
     // and the table entry of the tile after it.
     bool valid_nx = false;
-    if (kTree && left_out(p, ref_nx, row)) ref_nx.has = false;
     const uint8_t* psrc_nx = PROT ? row_source(p, ref_nx, row) : nullptr;
     if constexpr (PROT) {
       // The next tile's protected rows into L2 now (no registers held): their
@@ -558,6 +561,10 @@ __device__ void worker_role(const Params& p, Sched sc, uint32_t chunks, Ctrl& ct
       }
     }
     const uint8_t* blk_nx = psrc_nx != nullptr ? nullptr : resolve_row<CB>(p, ref_nx, row, valid_nx);
+    if (kTree && left_out(p, ref_nx, row)) {
+      valid_nx = false;
+      psrc_nx = nullptr;
+    }
     if constexpr (CB != 16) {
       // The next tile's two packed blocks into L2 by the bulk-copy engine (one
       // request each, from the threads of rows 0 and 64), so that the register

@@ -138,10 +138,12 @@ struct VerifyShared {
 
 // Sum of the terms v0 .. v1 - 1 of a node (p and q its rows), a share of it in each lane. kFlight
 // values of each row are on their way at a time: in 16 bytes where both rows lie on such
-// borders (VEC; v0 and v1 are multiples of their values then), else one by one.
-
-template <typename T, Mode M, bool VEC>
-__device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, int v0, int v1, int lane) {
+// borders (VEC; v0 and v1 are multiples of their values then), else one by one. SOME: the n tokens
+// `gone` count as 0. (Taken off the sum afterwards they leave its rounding behind, from which a
+// token of probability 0 would be drawn where nothing else is left.)
+template <typename T, Mode M, bool VEC, bool SOME = false>
+__device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, int v0, int v1, int lane,
+                                        const int* gone = nullptr, int n = 0) {
   constexpr int kFlight = M == kMore ? 8 : 16;
   constexpr int kWide = VEC ? 16 / static_cast<int>(sizeof(T)) : 1, kLoads = kFlight / kWide;
   using Load = typename std::conditional<VEC, uint4, T>::type;
@@ -158,6 +160,18 @@ __device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, 
         if (M != kWhole) y[i] = __ldg(reinterpret_cast<const Load*>(q + at));
       }
     }
+    if constexpr (SOME) {
+      uint32_t zero = 0u;  // of this lane's values, in the order in which they are added
+      for (int i = 0; i < n; ++i) {
+        const uint32_t d = static_cast<uint32_t>(gone[i] - (v - lane * kWide));
+        if (d < 32 * kFlight && d / kWide % 32 == static_cast<uint32_t>(lane)) zero |= 1u << (d / (32 * kWide) * kWide + d % kWide);
+      }
+      if (zero != 0u) {
+#pragma unroll
+        for (int e = 0; e < kFlight; ++e)
+          if ((zero >> e) & 1u) reinterpret_cast<T*>(&x[e / kWide])[e % kWide] = T(0.0f);
+      }
+    }
     auto value = [&](const Load* from, int e) { return as_float(reinterpret_cast<const T*>(&from[e / kWide])[e % kWide]); };
 #pragma unroll
     for (int e = 0; e < kFlight; e += 2)
@@ -165,6 +179,13 @@ __device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, 
                             M == kWhole ? 0.0f : value(y, e + 1), a));
   }
   return sums.total();
+}
+
+// A piece of a row that refused certain drafts lie in. (A call of its own: in line, its registers cost every
+// pass; 16 x 50,001 tokens, none refused: 34.3 us instead of 32.5.)
+template <typename T, bool VEC>
+__device__ __noinline__ Pair row_sum_without(const T* p, int v0, int v1, int lane, const int* gone, int n) {
+  return row_sum<T, kWhole, VEC, true>(p, nullptr, Taken({0.0f, 0.0f}), v0, v1, lane, gone, n);
 }
 
 // One cluster a sequence. The walk itself is a warp's, done alike in every CTA; the sums over
@@ -311,16 +332,19 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
     const int v0 = min(w * chunk, d.vocab), v1 = min(v0 + chunk, d.vocab);
     Pair sum;
     if (mode == kWhole) {
-      sum = vec ? row_sum<T, kWhole, true>(p, q, took, v0, v1, lane) : row_sum<T, kWhole, false>(p, q, took, v0, v1, lane);
+      auto mine = [&](int i) { return i < refusals && sh.refused[i] >= v0 && sh.refused[i] < v1; };
+      if (__any_sync(0xffffffffu, mine(lane) || mine(lane + 32))) {
+        sum = vec ? row_sum_without<T, true>(p, v0, v1, lane, sh.refused, refusals)
+                  : row_sum_without<T, false>(p, v0, v1, lane, sh.refused, refusals);
+      } else {
+        sum = vec ? row_sum<T, kWhole, true>(p, q, took, v0, v1, lane) : row_sum<T, kWhole, false>(p, q, took, v0, v1, lane);
+      }
     } else if (mode == kOnce) {
       sum = vec ? row_sum<T, kOnce, true>(p, q, took, v0, v1, lane) : row_sum<T, kOnce, false>(p, q, took, v0, v1, lane);
     } else {
       sum = vec ? row_sum<T, kMore, true>(p, q, took, v0, v1, lane) : row_sum<T, kMore, false>(p, q, took, v0, v1, lane);
     }
     sum = warp_scan(sum, lane);
-    for (int i = 0; i < refusals; ++i)
-      if (sh.refused[i] >= v0 && sh.refused[i] < v1)
-        sum = add(sum, {-left_over<kWhole>(as_float(p[sh.refused[i]]), 0.0f, took).hi, 0.0f});
     Pair* const part = sh.part[pass & 1];
     if (lane == 31) {
       for (int r = 0; r < ctas; ++r) {
@@ -359,8 +383,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
     const Pair cut = times(total, sh.u[0]);
     const bool fine = total.hi > 0.0f && total.hi < INFINITY;
     const int warps = ctas * kVerifyWarps;
-    // (the last piece with anything in it, where rounding leaves no piece above the cut)
-    if (fine && tid < warps) {
+    // (One with anything in it, for the sums up to a piece and up to the one before it are rounded apart;
+    // the last such where rounding leaves no piece above the cut.)
+    if (fine && tid < warps && part[tid].hi > 0.0f) {
       const Pair end = add(sh.before[tid], part[tid]);
       if (above(end, cut)) atomicMin(&sh.found, static_cast<unsigned long long>(tid));
     }

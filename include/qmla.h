@@ -664,8 +664,9 @@ size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens
  * walk ends, and the next token is the first v with
  *     sum_{w <= v} r(w) > u_0 sum_w r(w)
  * (r = p where nothing was refused), the last v with r(v) > 0 where rounding leaves none.
- * Sums and terms carry their rounding errors along (2^-46 of the sum), so that no decision
- * depends on an order.
+ * Sums and terms carry their rounding errors along: about 2^-46 of a sum is left, whatever
+ * the vocabulary. Only a decision whose two sides are that near each other depends on the order
+ * of a sum, which goes by vocab, batch and the rows' alignment; one call repeats itself exactly.
  *
  *   target, target_seq_stride, target_row_stride
  *                   [batch, nodes, vocab] probabilities of type probs (QMLA_PROBS_*), rows

@@ -19,9 +19,9 @@ constexpr int kMaxNodes = QMLA_MAX_TREE_NODES;
 // ------------------------------------------------------------- error-free sums
 // hi + lo with |lo| at most half a unit of hi: about 48 bits. A draw from 10^5 tokens has that
 // many borders a sum may fall on the wrong side of, and a decision that depended on the order
-// of a sum would differ from run to run of another launch shape; with an error of 2^-48 that
-// is one draw in 10^9. (In double the additions alone would take 40 us for 64 x 131,072
-// tokens: the card adds 1.25 T doubles a second.)
+// of a sum would differ from run to run of another launch shape; with an error of 2^-46 (an emulation of
+// rows' sums: 2^-45 at most, for up to 2^22 tokens a warp) that is one draw in 5 10^8. (In double the
+// additions alone would take 40 us for 64 x 131,072 tokens: the card adds 1.25 T doubles a second.)
 struct Pair {
   float hi, lo;
 };
@@ -114,6 +114,13 @@ struct Sums {
     hi = s;
     lo = add2(lo, add2(e, x.lo));
   }
+  // lo back below half a unit of hi: left to grow, it takes errors in with every term (2^-41 of a sum after
+  // 16,384 of them; kept small 2^-46).
+  __device__ __forceinline__ void renormalise() {
+    const uint64_t minus = f32x2(-1.0f, -1.0f), s = add2(hi, lo);
+    lo = fma2(fma2(hi, minus, s), minus, lo);
+    hi = s;
+  }
   __device__ __forceinline__ Pair total() const {
     return qmla::add(two_sum(lo2(hi), lo2(lo)), two_sum(hi2(hi), hi2(lo)));
   }
@@ -177,6 +184,7 @@ __device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, 
     for (int e = 0; e < kFlight; e += 2)
       sums.add(left_over<M>(value(x, e), value(x, e + 1), M == kWhole ? 0.0f : value(y, e),
                             M == kWhole ? 0.0f : value(y, e + 1), a));
+    sums.renormalise();
   }
   return sums.total();
 }

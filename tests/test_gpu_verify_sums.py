@@ -1,4 +1,6 @@
-"""tree_verify's sums where their rounding shows: nothing or next to nothing left of a row."""
+"""tree_verify's sums where their rounding shows: nothing left of a row, next to nothing left, and
+a row of millions of tokens whose draw lies next to a border."""
+import numpy as np
 import pytest
 import torch
 
@@ -49,3 +51,44 @@ def test_the_token_that_is_left_is_drawn_however_small(vocab, drafts, dtype):
     got = run(target, None, tokens, parents, u)
     assert got[3] == 0 and (got[1] == 1).all() and got[2].tolist() == left
     check(target, None, tokens, parents, u, got)
+
+
+def exact_sum(x):
+    """Sum of float32 values in units of 2^-149."""
+    mantissa, exponent = np.frexp(x.astype(np.float64))
+    whole = (mantissa * (1 << 24)).astype(np.int64)
+    return sum(int(whole[exponent == e].sum()) << int(e - 24 + 149) for e in np.unique(exponent[x > 0]))
+
+
+def parts(whole):
+    """The same as float32 values that add up to it."""
+    out = []
+    while whole:
+        low = max(whole.bit_length() - 24, 0)
+        top = whole >> low
+        out.append(np.float32(np.ldexp(float(top), low - 149)))
+        whole -= top << low
+    return out
+
+
+@pytest.mark.parametrize("batch", [1, 320])
+def test_a_border_in_a_row_of_millions(batch):
+    """The number 0.5 on a row of two equal halves and a token between them of 2^-42 of a half: that token
+    is drawn if the sums before it and in all are within 2^-43 of a half. The first half is
+    millions of tokens, the other a few, so that errors of the sums do not cancel. (An emulation of a lane's sums
+    in fp32 pairs is 2^-46 off for 2^20 tokens a warp, which is one CTA a row, if the pairs are kept
+    normal, and 2^-41 if they are not.)"""
+    vocab = 1 << 24
+    first = vocab - 1000
+    z = np.exp(2.5 * np.random.default_rng(7).standard_normal(first))
+    t = np.zeros(vocab, np.float32)
+    t[:first] = z / (2 * z.sum())
+    half = exact_sum(t[:first])
+    t[first] = np.float32(2.0 ** -42 * np.ldexp(float(half), -149))
+    rest = parts(half)
+    t[first + 500:first + 500 + len(rest)] = rest
+    assert exact_sum(t[first + 1:]) == half
+    shared = torch.from_numpy(t).cuda().view(1, 1, vocab).expand(batch, 1, vocab)
+    none = torch.full((batch, 1), -1, dtype=torch.int32)
+    got = run(shared, None, torch.zeros_like(none), none, torch.full((batch, 1), 0.5))
+    assert got[3] == 0 and got[2].tolist() == [first] * batch

@@ -684,9 +684,10 @@ size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens
  *   next_token      [batch] int32 out
  * A sequence without a tree gets kept = 0, next_token = -1 and no path, and so does one whose
  * count is bad (QMLA_DEVERR_BAD_TREE). A node is passed over whose token is not in the
- * vocabulary or whose parent is not an earlier node or -1 (the same). Where the sum of r is
- * not positive and finite, next_token is -1 (QMLA_DEVERR_BAD_PROBS). Outputs share no memory
- * with the inputs or one another.
+ * vocabulary or whose parent is not an earlier node or -1 (the same); but node 0 is kept
+ * whatever they are, and a parent of it other than -1 reported. Where the sum of r is not positive
+ * and finite, next_token is -1 (QMLA_DEVERR_BAD_PROBS). Outputs share no memory with the inputs
+ * or one another.
  */
 typedef struct qmla_verify_desc {
   const void* target;

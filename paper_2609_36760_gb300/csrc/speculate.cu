@@ -238,6 +238,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
           if (draft != nullptr) q = as_float(draft[static_cast<size_t>(parent) * d.draft_row_stride + token]);
         }
       } else {
+        if (parent != -1 && rank == 0) report(d.dev_err, QMLA_DEVERR_BAD_TREE);
         parent = -1;
       }
     }

@@ -589,7 +589,8 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *   pool, cache_kind, num_blocks, block_table, max_blocks, softmax_scale, dev_err
  *                   as in qmla_mla_decode_ex, any of the four cache kinds
  *   max_len         a bound of seq_lens, or 0 (max_blocks x 64 then). Longer sequences are bad ones.
- *                   (The launches and the room for images go by it: a near bound is faster)
+ *                   (The launches and each sequence's room in the workspace go by it: pass one with
+ *                   a table wider than its sequences)
  *   q_latent, q_pe  [batch, nodes, heads, 512] and [batch, nodes, heads, 64] bf16, 16-byte aligned
  *   nodes, heads    1 .. QMLA_MAX_TREE_NODES, 1 .. 128
  *   parents         [batch, nodes] int32
@@ -609,16 +610,20 @@ size_t qmla_prefill_workspace_bytes(int batch, int n_q);
  *   workspace       >= qmla_tree_workspace_bytes(batch, nodes, heads, 0) bytes, 256-byte
  *                   aligned, scratch as for qmla_mla_decode. With the bytes for the call's
  *                   max_len (or max_blocks x 64) tokens the context is dequantised once for all
- *                   rows of a sequence, in the workspace. With lse the scores are then those of
- *                   s (q - z) itself instead of its fp16 value (which leaves lse 2e-6 to 4e-5 of
- *                   itself off, the more the fewer keys have the weight). Where the bytes are
- *                   fewer, that happens for as many sequences at a time as they hold
+ *                   rows of a sequence, in the workspace; where they are fewer, for as many
+ *                   sequences at a time as they hold, in as many launches one after the other.
+ *                   (Not with up to 64 rows, nodes x heads, over more than 40,960 tokens, batch x
+ *                   bound, unless lse of a quantised cache is asked for.) lse is then of the scores
+ *                   of s (q - z) itself instead of its fp16 value (which leaves lse 2e-6 to 4e-5 of
+ *                   itself off, the more the fewer keys have the weight) and sums the weights before
+ *                   their rounding to fp16 (which leaves 4e-6)
  * A node behind the last of its sequence gets out = 0 and lse = -inf. So do a node whose
  * parent is not an earlier node or -1 and the nodes below it (QMLA_DEVERR_BAD_TREE), and
  * every node of a sequence whose count is below 0, above `nodes` or above its length (the
- * same) or whose length is bad (QMLA_DEVERR_BAD_POSITION). A value that is not finite in a
- * cache row (a BF16 one beyond 65,504 among them: tiles are fp16) reaches the nodes that see it,
- * and no others.
+ * same) or whose length is bad (QMLA_DEVERR_BAD_POSITION). Queries, cached values and weights are
+ * fp16 in the tensor core: BF16 values below 2^-14 lose bits, those beyond 65,504 are infinite. A
+ * value that is not finite in a cache row reaches the nodes that see it, and no others; one in a query
+ * leaves that row, and no other, without a result of meaning.
  */
 typedef struct qmla_tree_desc {
   const void* pool;

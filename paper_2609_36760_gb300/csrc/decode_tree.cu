@@ -150,7 +150,8 @@ cudaError_t launch_decode_tree(const qmla_tree_desc& d, int grid, cudaStream_t s
   if (fit > 0 && on_images(rows, static_cast<long long>(d.batch) * blocks * kBlockTokens, rest)) {
     // As many sequences at a time as there is room for; and as L2 holds, where many row groups that
     // do not keep step read their images (16 x 4,096 tokens, 32 groups, both passes: 714 us at once, 630
-    // by 80 MB, 598 by 60, 588 by 40; 2 x 30,000 435 and 398; 57 MB by 40 instead of at once 100 and 116).
+    // by 80 MB, 598 by 60, 588 by 40; 2 x 30,000 435 and 398; 57 MB by 40 instead of at once 100 and 116;
+    // between 57 and 151 MB nothing was measured).
     // Not over six launches for that: the lengths may be far below their bound.
     const int groups = (rows + 127) / 128;
     if (groups >= 8 && !keep_step(grid / 2, groups) && d.batch * image_bytes(blocks, rest) > (112u << 20))

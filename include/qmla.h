@@ -677,8 +677,9 @@ size_t qmla_tree_workspace_bytes(int batch, int nodes, int heads, int max_tokens
  *                   [batch, nodes, vocab] probabilities of type probs (QMLA_PROBS_*), rows
  *                   and sequences that many elements apart (not negative, below 2^40; not used
  *                   where that axis has one element). Rows are not normalised; a target's value
- *                   below 0 counts as 0, the draft's are not below 0. 16-byte aligned rows whose
- *                   vocab and strides are multiples of 16 bytes are read in wider pieces
+ *                   below 0 counts as 0; the draft's are not below 0, and one that is not finite
+ *                   leaves nothing of its token after a refusal. 16-byte aligned rows whose vocab
+ *                   and strides are multiples of 16 bytes are read in wider pieces
  *   draft, ...      the same for the draft, or NULL. Rows of nodes without children are not read
  *   batch, nodes, vocab   1 .. 65535, 1 .. QMLA_MAX_TREE_NODES, 1 .. 2^24
  *   tokens, parents [batch, nodes] int32; tree_lens [batch] int32 or NULL, as above

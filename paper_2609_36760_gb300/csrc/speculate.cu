@@ -69,39 +69,42 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // (a NaN stays on
   return r;
 }
 
-// What the terms of a sum are made of: p alone, p and q with a = 1 (after a first refusal),
-// p and q.
+// What the terms of a sum are made of: p alone, p and q after a first refusal, p and q after more.
 enum Mode { kWhole, kOnce, kMore };
 
-// What is left of p after refusals that took a times q, max(p - a q, 0), of two tokens at a time
-// (packed fp32), as hi + lo; a NaN in p stays one. With h + l = a q, l at most half a unit of
-// h: p - min(p, h) is exact as a pair, the larger of the two coming first, and l counts where
-// h < p, p - h then being more than it is. (Where h = p, l alone would be left, below 2^-24 of
-// p: it counts as nothing.)
+// What is left of p after refusals, max(p - a q, 0), of two tokens at a time (packed fp32), as
+// hi + lo. The first refusal takes q itself (R is 1 until then), and p - q is exact as a pair,
+// the larger coming first. The later ones take b q of that, b = a - 1. So where a draft is nearly the
+// target, and what is left are units of p's last place, they are known to 2^-46 of themselves.
+// (From p - a q, with a q to 2^-48 of it, draws went wrong there, and what was left came out below 0.
+// That took 53 us for 64 x 131,072 tokens and walks of up to six passes, this 60.) A NaN in p stays
+// one where p is alone and after one refusal, and so in b.
 struct Pairs {
   uint64_t hi, lo;
 };
-struct Taken {  // a
+struct Taken {  // b
   uint64_t hi, lo, minus_hi;
-  __device__ explicit Taken(Pair a) : hi(f32x2(a.hi, a.hi)), lo(f32x2(a.lo, a.lo)), minus_hi(f32x2(-a.hi, -a.hi)) {}
+  __device__ explicit Taken(Pair b) : hi(f32x2(b.hi, b.hi)), lo(f32x2(b.lo, b.lo)), minus_hi(f32x2(-b.hi, -b.hi)) {}
 };
 template <Mode M>
-__device__ __forceinline__ Pairs left_over(float p0, float p1, float q0, float q1, const Taken& a) {
+__device__ __forceinline__ Pairs left_over(float p0, float p1, float q0, float q1, const Taken& b) {
   if constexpr (M == kWhole) return {f32x2(max_nan(p0, 0.0f), max_nan(p1, 0.0f)), 0};
   const uint64_t minus = f32x2(-1.0f, -1.0f), p = f32x2(p0, p1), q = f32x2(q0, q1);
-  const uint64_t h = M == kOnce ? q : mul2(a.hi, q);
-  const float h0 = lo2(h), h1 = hi2(h);
-  const uint64_t m = f32x2(fminf(p0, h0), fminf(p1, h1));
+  const uint64_t m = M == kOnce ? f32x2(fminf(p0, q0), fminf(p1, q1)) : q;
   const uint64_t s = fma2(m, minus, p), rounding = add2(m, fma2(p, minus, s));  // (s - p) + m, the minus of it
   if constexpr (M == kOnce) return {s, mul2(rounding, minus)};
-  const uint64_t l = fma2(a.lo, q, fma2(a.hi, q, mul2(a.minus_hi, q)));
-  const uint64_t counted = f32x2(h0 < p0 ? lo2(l) : 0.0f, h1 < p1 ? hi2(l) : 0.0f);
-  return {s, mul2(add2(rounding, counted), minus)};
+  // (b q = l - h; t + e is s + h, or t is far below 0. The pair is not normal: lo may be more than t, and
+  // decides the sign then. Where q is more than p, or no number, hi is below 0 or a NaN.)
+  const uint64_t h = mul2(b.minus_hi, q), l = fma2(b.lo, q, fma2(b.hi, q, h));
+  const uint64_t t = add2(s, h), e = add2(fma2(t, minus, s), h);
+  const uint64_t lo = fma2(add2(rounding, l), minus, e), hi = add2(t, lo);
+  const bool some0 = lo2(hi) > 0.0f, some1 = hi2(hi) > 0.0f;
+  return {f32x2(some0 ? lo2(t) : 0.0f, some1 ? hi2(t) : 0.0f), f32x2(some0 ? lo2(lo) : 0.0f, some1 ? hi2(lo) : 0.0f)};
 }
-template <Mode M>
-__device__ __forceinline__ Pair left_over(float p, float q, const Taken& a) {
-  const Pairs r = left_over<M>(p, 0.0f, q, 0.0f, a);
-  return {lo2(r.hi), lo2(r.lo)};
+// Of one token, as a normal pair; q and b 0 where nothing was refused.
+__device__ __forceinline__ Pair left_over(float p, float q, const Taken& b) {
+  const Pairs r = left_over<kMore>(p, 0.0f, q, 0.0f, b);
+  return two_sum(lo2(r.hi), lo2(r.lo));
 }
 
 // Two running sums of pairs, of the even and the odd terms.
@@ -138,7 +141,8 @@ struct VerifyShared {
   Pair scan[kVerifyWarps];
   // the walk's state, written by warp 0
   int cur, last, refused_n;
-  Pair a;
+  bool taken;  // a is 1 + b, not 0
+  Pair b;
   int refused[kMaxNodes];
   unsigned long long found;
 };
@@ -149,7 +153,7 @@ struct VerifyShared {
 // `gone` count as 0. (Taken off the sum afterwards they leave its rounding behind, from which a
 // token of probability 0 would be drawn where nothing else is left.)
 template <typename T, Mode M, bool VEC, bool SOME = false>
-__device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, int v0, int v1, int lane,
+__device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& b, int v0, int v1, int lane,
                                         const int* gone = nullptr, int n = 0) {
   constexpr int kFlight = M == kMore ? 8 : 16;
   constexpr int kWide = VEC ? 16 / static_cast<int>(sizeof(T)) : 1, kLoads = kFlight / kWide;
@@ -183,7 +187,7 @@ __device__ __forceinline__ Pair row_sum(const T* p, const T* q, const Taken& a, 
 #pragma unroll
     for (int e = 0; e < kFlight; e += 2)
       sums.add(left_over<M>(value(x, e), value(x, e + 1), M == kWhole ? 0.0f : value(y, e),
-                            M == kWhole ? 0.0f : value(y, e + 1), a));
+                            M == kWhole ? 0.0f : value(y, e + 1), b));
     sums.renormalise();
   }
   return sums.total();
@@ -258,11 +262,13 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
   // Warp 0's state: the node, its children not yet looked at, the refusals so far.
   int cur = 0, kept = 1;
   uint64_t children = 0ull;
-  Pair a = {0.0f, 0.0f}, mass = {1.0f, 0.0f};
+  bool taken = false;
+  Pair more = {0.0f, 0.0f}, mass = {1.0f, 0.0f};  // a = 1 + more once taken, R
   int my_path = lane == 0 ? 0 : -1, my_path2 = -1;  // entries lane and lane + 32
   auto enter = [&](int node) {
     cur = node;
-    a = {0.0f, 0.0f};
+    taken = false;
+    more = {0.0f, 0.0f};
     mass = {1.0f, 0.0f};
     const uint32_t lo = __ballot_sync(0xffffffffu, sh.parent[lane] == node);
     const uint32_t hi = __ballot_sync(0xffffffffu, sh.parent[lane + 32] == node);
@@ -286,13 +292,13 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
           // (u q is exact as a pair)
           const float uq = __fmul_rn(u, q);
           const Pair need = product({uq, __fmaf_rn(u, q, -uq)}, mass);
-          if (above(left_over<kMore>(p, q, Taken(a)), need)) {
+          if (above(left_over(p, taken ? q : 0.0f, Taken(more)), need)) {
             if (lane == (kept & 31)) (kept < 32 ? my_path : my_path2) = t;
             ++kept;
             enter(t);
           } else {
-            a = add(a, mass);
-            refusal = true;
+            if (taken) more = add(more, mass);
+            taken = refusal = true;
           }
         } else {
           bool gone = false;
@@ -318,22 +324,21 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
       if (lane == 0) {
         sh.cur = cur;
         sh.last = children == 0ull;
-        sh.a = a;
+        sh.taken = taken;
+        sh.b = more;
         sh.found = ~0ull;
       }
     }
     __syncthreads();
     const T* const p = target + static_cast<size_t>(sh.cur) * d.target_row_stride;
     const T* const q = draft == nullptr ? nullptr : draft + static_cast<size_t>(sh.cur) * d.draft_row_stride;
-    const Taken took(sh.a);
-    const Mode mode = sh.a.hi == 0.0f ? kWhole : (sh.a.hi == 1.0f && sh.a.lo == 0.0f ? kOnce : kMore);
+    const Taken took(sh.b);
+    const Mode mode = !sh.taken ? kWhole : (sh.b.hi == 0.0f ? kOnce : kMore);
     const int refusals = sh.refused_n;  // (of certain drafts)
     const bool last = sh.last;
-    auto term = [&](int v, float x, float y) {
-      if (mode != kWhole) return left_over<kMore>(x, y, took);
-      Pair r = left_over<kWhole>(x, 0.0f, took);
+    auto counted = [&](int v, Pair r) {  // what is left of token v
       for (int i = 0; i < refusals; ++i)
-        if (sh.refused[i] == v) r.hi = 0.0f;
+        if (sh.refused[i] == v) r = {0.0f, 0.0f};
       return r;
     };
     // ---- this warp's piece of the sum
@@ -422,7 +427,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = add(s, term(v + i, x[i], y[i]));
+        for (int i = 0; i < 8; i += 2) {
+          const Pairs r = left_over<kMore>(x[i], x[i + 1], y[i], y[i + 1], took);
+          s = add(s, counted(v + i, two_sum(lo2(r.hi), lo2(r.lo))));
+          s = add(s, counted(v + i + 1, two_sum(hi2(r.hi), hi2(r.lo))));
+        }
       }
       const Pair incl = warp_scan(s, lane);
       if (lane == 31) sh.scan[warp] = incl;
@@ -446,7 +455,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
         bool done = false;
         for (int v = first_v; v < end_v && !done; v += 32) {
           const int mine = v + lane;
-          const Pair x = mine < end_v ? term(mine, as_float(p[mine]), mode != kWhole ? as_float(q[mine]) : 0.0f) : Pair{0.0f, 0.0f};
+          Pair x = {0.0f, 0.0f};
+          if (mine < end_v)
+            x = counted(mine, left_over(as_float(p[mine]), mode != kWhole ? as_float(q[mine]) : 0.0f, took));
           const Pair sum_to = add(upto, warp_scan(x, lane));
           const uint32_t any = __ballot_sync(0xffffffffu, x.hi > 0.0f);
           const uint32_t over = __ballot_sync(0xffffffffu, x.hi > 0.0f && above(sum_to, cut));

@@ -292,7 +292,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) verify_kernel(const qmla_ve
           // (u q is exact as a pair)
           const float uq = __fmul_rn(u, q);
           const Pair need = product({uq, __fmaf_rn(u, q, -uq)}, mass);
-          if (above(left_over(p, taken ? q : 0.0f, Taken(more)), need)) {
+          const Pair r = taken ? left_over(p, q, Taken(more)) : Pair{fmaxf(p, 0.0f), 0.0f};
+          if (above(r, need)) {
             if (lane == (kept & 31)) (kept < 32 ? my_path : my_path2) = t;
             ++kept;
             enter(t);
